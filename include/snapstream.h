@@ -20,7 +20,11 @@
  * the normalisers of Eq. 4, and the compression that consumes them),
  * and snap_block_stats + snap_block_select + snap_decode_attn_blocks (a per-step block top-K
  * over the whole middle of the prompt instead of the one-time top-K, the variant the paper's
- * related-work section leaves to future work).
+ * related-work section leaves to future work),
+ * and, for the uncompressed cache a serving program keeps next to it: snap_rope (rotary positions
+ * of queries and keys), snap_paged_append + snap_paged_decode_attn (a cache in pages and the
+ * attention of one new token per sequence over it) and snap_paged_evict (cutting a paged cache
+ * back to l_sink + topk + l_recent rows by accumulated attention weight).
  *
  * Conventions
  *   - "dev" pointers are CUDA device pointers on the current device, "host" pointers are plain
@@ -85,6 +89,9 @@ typedef enum snap_status {
                                        -DSNAP_DEBUG_BOUNDS): a data-dependent index -- a selected
                                        position, a ring slot, an output rank, a band entry -- fell
                                        outside its array; the access was skipped */
+
+#define SNAP_DEV_BAD_PAGE 16u       /* paged cache: a page number outside [0, n_pages), or a row or a length past
+                                       the page table: those rows were skipped */
 
 /* One attention layer's shape and SnapStream hyper-parameters (appendix table
  * "SnapStream Hyperparameters": sink, top-K, recent, observation window, pooling kernel). */
@@ -391,6 +398,168 @@ int snap_decode_attn_blocks(const snap_config_t* cfg, const snap_layout_t* layou
                             const int32_t* valid_topk_dev, int32_t block_tokens, int32_t n_blocks,
                             const int32_t* block_idx_dev, const int32_t* n_selected_dev, void* out_dev,
                             void* workspace_dev, size_t workspace_bytes, uint32_t* status_dev, void* cuda_stream);
+
+/*
+ * Rotary positions (the encoding that Section 3.2 takes as applied before caching).
+ *
+ * Pair i of rot_dim / 2 turns by the angle position * f_i:
+ *     a' = m (a cos - b sin),   b' = m (b cos + a sin)
+ * with (a, b) the dims (rot_offset + i, rot_offset + rot_dim / 2 + i) of a head, or, interleaved,
+ * (rot_offset + 2 i, rot_offset + 2 i + 1); the head's other dims pass unchanged.  The frequencies
+ * f_i are radians per position in double precision, on the device; snap_rope_table fills a host
+ * array with them (any other frequencies can be passed as well):
+ *   PLAIN    f_i = base^(-2 i / rot_dim)
+ *   LINEAR   f_i / factor
+ *   LLAMA3   f_i / factor for wavelengths over original_len / low_freq, f_i for those under
+ *            original_len / high_freq, between them ((1 - s) / factor + s) f_i with
+ *            s = (original_len / wavelength - low_freq) / (high_freq - low_freq)
+ *   YARN     (1 - r) f_i + r f_i / factor, r = clamp((i - lo) / (hi - lo), 0, 1) with
+ *            lo = floor(c(beta_fast)), hi = ceil(c(beta_slow)), limited to [0, rot_dim - 1], and
+ *            c(n) = rot_dim ln(original_len / (2 pi n)) / (2 ln base)
+ * and m = magnitude, or, when that is 0, 1 (YARN: 0.1 ln(factor) + 1).
+ */
+#define SNAP_ROPE_PLAIN 0
+#define SNAP_ROPE_LINEAR 1
+#define SNAP_ROPE_LLAMA3 2
+#define SNAP_ROPE_YARN 3
+typedef struct snap_rope_config {
+  int32_t rot_dim;        /* dims of a head that are rotated: even, >= 2 */
+  int32_t rot_offset;     /* the first of them (latent layout: 512 of 576) */
+  int32_t interleaved;    /* 0: a pair is dims i and i + rot_dim / 2, 1: dims 2 i and 2 i + 1 */
+  int32_t scaling;        /* SNAP_ROPE_* */
+  double base, factor;    /* > 1; >= 1 (LINEAR, LLAMA3, YARN) */
+  double original_len;    /* LLAMA3, YARN: the context the model was trained on */
+  double low_freq, high_freq;    /* LLAMA3, 0 < low_freq < high_freq */
+  double beta_fast, beta_slow;   /* YARN, beta_fast > beta_slow > 0 */
+  double magnitude;       /* >= 0; 0: the scaling's own */
+} snap_rope_config_t;
+
+/* Host only: the rot_dim / 2 frequencies and the magnitude (either may be NULL). */
+int snap_rope_table(const snap_rope_config_t* rope, double* freqs_host, double* magnitude_host);
+
+/*
+ * Rotates the queries and / or keys of n_tokens tokens; token t is at positions_dev[t].
+ *   q_dev, q_out_dev  element (t, h, c) at [t * token_stride + h * head_stride + c], Hq heads; k_dev, k_out_dev
+ *             alike with Hkv heads.  q_dev and q_out_dev, or k_dev and k_out_dev, may both be NULL.
+ *             An output may be its own input (same pointer and strides); any other overlap is not allowed.
+ *             Strides in elements, multiples of 16 bytes, and no head of an output may overlap another.
+ *   freqs_dev [rot_dim / 2] double;  positions_dev [n_tokens] int32, any value
+ *   inverse   1: turns by minus the angle (magnitude as before): the transposed map, i.e. the
+ *             gradient with respect to the input, given the gradient of the output
+ * Angles and their reduction are in double precision, the rotation in single, one rounding at the
+ * end.  Only rot_dim, rot_offset, interleaved, scaling, factor and magnitude of rope are used.  No workspace.
+ */
+int snap_rope(const snap_config_t* cfg, const snap_rope_config_t* rope, const double* freqs_dev,
+              const int32_t* positions_dev, int32_t n_tokens,
+              const void* q_dev, int64_t q_token_stride, int64_t q_head_stride,
+              void* q_out_dev, int64_t q_out_token_stride, int64_t q_out_head_stride,
+              const void* k_dev, int64_t k_token_stride, int64_t k_head_stride,
+              void* k_out_dev, int64_t k_out_token_stride, int64_t k_out_head_stride,
+              int32_t inverse, void* cuda_stream);
+
+/*
+ * A cache in pages (the uncompressed cache that the paper's baseline decodes over).
+ *
+ * A page holds page_tokens rows of every KV head; row r of a sequence is row r mod page_tokens of
+ * its page number page_table[slot][r / page_tokens].  Element c of row o of KV head h of page p is
+ *     k_pages_dev[p * k_page_stride + h * k_head_stride + o * k_row_stride + c]
+ * (strides in elements, multiples of 16 bytes; both [page][head][row][dim] and [page][row][head][dim]
+ * are such layouts), V alike with d_v.
+ *   page_table_dev  [max_seqs][max_pages] int32; entries past a sequence's last row are not read
+ *   seq_len_dev     [max_seqs] int32: rows of each slot's sequence
+ *   weights         [max_seqs][Hkv][max_pages * page_tokens] float: accumulated attention weight of each row
+ * Rows need not be in position order: attention does not depend on it, and snap_paged_append takes
+ * positions apart from rows.  Sequences may share pages that are only read.
+ * The calls take heads up to 256 wide and no latent layout (SNAP_ERR_UNSUPPORTED otherwise); bf16 layers with
+ * d_qk = d_v of 64, 128 or 256 and pages of a multiple of 16 rows run on tensor cores.  All are safe to capture.
+ */
+typedef struct snap_paged {
+  int32_t page_tokens;    /* rows of a page, >= 1 */
+  int32_t n_pages;        /* pages of the pool */
+  int32_t max_pages;      /* entries of a page-table row; page_tokens * max_pages <= 2^30 */
+  int32_t reserved;       /* 0 */
+  int64_t k_page_stride, k_head_stride, k_row_stride;
+  int64_t v_page_stride, v_head_stride, v_row_stride;
+} snap_paged_t;
+
+/*
+ * Writes the K/V rows of n_tokens new tokens, rotating the keys (and queries) on the way when rope is given.
+ *   slot_ids_dev [n_tokens] int32: the slot of each token's sequence; -1 = padding, nothing of that token is
+ *             read or written
+ *   rows_dev  [n_tokens] int32: the row each token is written to; afterwards seq_len[slot] is at least row + 1.
+ *             No (slot, row) twice.  NULL: every token is its sequence's next one, row = seq_len[slot], and
+ *             seq_len[slot] grows by one; a slot that is listed a second time in the call is skipped
+ *             (SNAP_DEV_BAD_SLOT).
+ *   rope, freqs_dev, positions_dev: as in snap_rope; rope NULL = the keys are stored as given (the other
+ *             two are ignored); positions_dev NULL = the position is the row
+ *   k_dev, v_dev  (t, h, c) at [t * token_stride + h * head_stride + c]
+ *   k_out_dev NULL, or [n_tokens][Hkv][d_qk] dense: the keys as stored (what snap_prefill_attn reads); may be
+ *             k_dev when that is dense
+ *   q_dev, q_out_dev  NULL, or the queries and where they go rotated, q_out dense [n_tokens][Hq][d_qk]; may be
+ *             q_dev when that is dense
+ *   weights_dev  NULL, or the weights array: the entries of the rows written are set to 0
+ * A token whose row lies past the page table, or on a page number out of range, is skipped (SNAP_DEV_BAD_PAGE),
+ * its outputs too.  No workspace.
+ */
+int snap_paged_append(const snap_config_t* cfg, const snap_paged_t* paged,
+                      const int32_t* slot_ids_dev, const int32_t* rows_dev, int32_t n_tokens,
+                      const snap_rope_config_t* rope, const double* freqs_dev, const int32_t* positions_dev,
+                      const void* q_dev, int64_t q_token_stride, int64_t q_head_stride, void* q_out_dev,
+                      const void* k_dev, int64_t k_token_stride, int64_t k_head_stride, void* k_out_dev,
+                      const void* v_dev, int64_t v_token_stride, int64_t v_head_stride,
+                      void* k_pages_dev, void* v_pages_dev, const int32_t* page_table_dev,
+                      int32_t* seq_len_dev, float* weights_dev, uint32_t* status_dev, void* cuda_stream);
+
+/*
+ * Attention of one token per sequence over its pages: out[i][h] = softmax(scale * q[i][h] . K^T) V over rows
+ * [0, seq_len[slot_ids[i]]) of KV head h / (Hq/Hkv).  Nothing is appended.
+ *   q_dev [n_active][Hq][d_qk], out_dev [n_active][Hq][d_v], dense.  A sequence without rows, and a slot out of
+ *             range (SNAP_DEV_BAD_SLOT), get zeros; a slot id of -1 is padding: its out rows are zeros too.
+ *             Rows on a page number out of range are left out (SNAP_DEV_BAD_PAGE), as are rows past the page table.
+ *   seq_len_dev  need not be the cache's own lengths: with shorter ones the token sees the rows before them
+ *   weights_out_dev  NULL, or the weights array: for every row r the token attends,
+ *                 weights_out[slot][kvh][r] = weights_in[slot][kvh][r] + sum over the group's heads of its softmax weight
+ *             (weights_in_dev NULL = 0; it may be weights_out_dev).  Other entries are left alone.  The slots of
+ *             one call must then be distinct: of a slot that is listed again only the first entry's weights
+ *             count (SNAP_DEV_BAD_SLOT).
+ * The rows of all sequences are split evenly over the GPU whatever their lengths and joined in a fixed order:
+ * equal inputs give equal bits.
+ * Scratch: snap_paged_decode_workspace_bytes(cfg, paged, n_active, with_weights); calls that can overlap on the
+ * GPU need scratch of their own.
+ */
+int64_t snap_paged_decode_workspace_bytes(const snap_config_t* cfg, const snap_paged_t* paged, int32_t n_active,
+                                          int32_t with_weights);
+int snap_paged_decode_attn(const snap_config_t* cfg, const snap_paged_t* paged, const void* q_dev,
+                           const int32_t* slot_ids_dev, int32_t n_active,
+                           const void* k_pages_dev, const void* v_pages_dev, const int32_t* page_table_dev,
+                           const int32_t* seq_len_dev, const float* weights_in_dev, float* weights_out_dev,
+                           void* out_dev, void* workspace_dev, size_t workspace_bytes,
+                           uint32_t* status_dev, void* cuda_stream);
+
+/*
+ * Eviction by accumulated attention weight.  For each of n_seqs sequences the rows that stay are copied from
+ * slot src_slots[i] to slot dst_slots[i] (whose page-table row holds the caller's free pages), per KV head and
+ * in order: of len = seq_len[src] rows,
+ *     all of them                                                          when len <= Ls + K + Lr
+ *     [0, Ls), the K rows of [Ls, len - Lr) with the largest weights_in[src][kvh][row]
+ *     (ties to the lower row; NaN ranks lowest), [len - Lr, len)           otherwise
+ * with l_sink, topk and l_recent of cfg.  The source slot and its pages stay as they are; the caller then uses
+ * dst and frees src.
+ *   seq_len_dev   [max_seqs]; seq_len[dst] = min(len, Ls + K + Lr)
+ *   weights_out_dev  NULL, or the weights array the kept rows' weights go to at [dst] (weights_in_dev itself is fine)
+ *   kept_rows_dev NULL, or [n_seqs][Hkv][Ls + K + Lr] int32: the source rows kept, -1 after the last
+ * A slot out of range, or a dst that is a src of the call or an earlier entry's dst, skips that sequence
+ * (SNAP_DEV_BAD_SLOT; its kept_rows are -1).  A destination page may hold nothing that is in use, the source's rows
+ * included, and is listed once (not checked).  A source or destination page number out of range skips its rows
+ * (SNAP_DEV_BAD_PAGE).
+ * Scratch: snap_paged_evict_workspace_bytes(cfg, paged, n_seqs).
+ */
+int64_t snap_paged_evict_workspace_bytes(const snap_config_t* cfg, const snap_paged_t* paged, int32_t n_seqs);
+int snap_paged_evict(const snap_config_t* cfg, const snap_paged_t* paged, const int32_t* src_slots_dev,
+                     const int32_t* dst_slots_dev, int32_t n_seqs, void* k_pages_dev, void* v_pages_dev,
+                     const int32_t* page_table_dev, int32_t* seq_len_dev, const float* weights_in_dev,
+                     float* weights_out_dev, int32_t* kept_rows_dev, void* workspace_dev, size_t workspace_bytes,
+                     uint32_t* status_dev, void* cuda_stream);
 
 /*
  * Testing and tuning aids (the paper has no counterpart).  Each option is one non-negative

@@ -20,6 +20,8 @@ _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)),
 SNAP_F32, SNAP_BF16 = 0, 1
 SNAP_POOL_AVG, SNAP_POOL_MAX = 0, 1
 SNAP_DEV_BAD_SLOT, SNAP_DEV_WAIT_TIMEOUT, SNAP_DEV_BAND_OVERFLOW, SNAP_DEV_INDEX_CHECK = 1, 2, 4, 8
+SNAP_DEV_BAD_PAGE = 16
+SNAP_ROPE_PLAIN, SNAP_ROPE_LINEAR, SNAP_ROPE_LLAMA3, SNAP_ROPE_YARN = range(4)
 
 
 class SnapConfig(C.Structure):
@@ -33,6 +35,18 @@ class SnapLayout(C.Structure):
     _fields_ += [(n, C.c_int64) for n in ("k_row_bytes", "v_row_bytes", "k_head_stride_bytes",
                                           "v_head_stride_bytes", "k_seq_stride_bytes", "v_seq_stride_bytes",
                                           "k_cache_bytes", "v_cache_bytes")]
+
+
+class SnapRope(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("rot_dim", "rot_offset", "interleaved", "scaling")]
+    _fields_ += [(n, C.c_double) for n in ("base", "factor", "original_len", "low_freq", "high_freq", "beta_fast", "beta_slow",
+                                           "magnitude")]
+
+
+class SnapPaged(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("page_tokens", "n_pages", "max_pages", "reserved")]
+    _fields_ += [(n, C.c_int64) for n in ("k_page_stride", "k_head_stride", "k_row_stride", "v_page_stride", "v_head_stride",
+                                          "v_row_stride")]
 
 
 class SnapError(RuntimeError):
@@ -99,6 +113,22 @@ def lib() -> C.CDLL:
     L.snap_decode_blocks_workspace_bytes.argtypes = [pcfg, i32, i32, i32]
     L.snap_decode_attn_blocks.restype = C.c_int
     L.snap_decode_attn_blocks.argtypes = [pcfg, play, vp, vp, vp, vp, i32, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, sz, vp, vp]
+    prope, ppaged = C.POINTER(SnapRope), C.POINTER(SnapPaged)
+    L.snap_rope_table.restype = C.c_int
+    L.snap_rope_table.argtypes = [prope, C.POINTER(C.c_double), C.POINTER(C.c_double)]
+    L.snap_rope.restype = C.c_int
+    L.snap_rope.argtypes = [pcfg, prope, vp, vp, i32] + [vp, i64, i64] * 4 + [i32, vp]
+    L.snap_paged_append.restype = C.c_int
+    L.snap_paged_append.argtypes = [pcfg, ppaged, vp, vp, i32, prope, vp, vp, vp, i64, i64, vp, vp, i64, i64, vp, vp, i64, i64,
+                                    vp, vp, vp, vp, vp, vp, vp]
+    L.snap_paged_decode_workspace_bytes.restype = i64
+    L.snap_paged_decode_workspace_bytes.argtypes = [pcfg, ppaged, i32, i32]
+    L.snap_paged_decode_attn.restype = C.c_int
+    L.snap_paged_decode_attn.argtypes = [pcfg, ppaged, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp, vp]
+    L.snap_paged_evict_workspace_bytes.restype = i64
+    L.snap_paged_evict_workspace_bytes.argtypes = [pcfg, ppaged, i32]
+    L.snap_paged_evict.restype = C.c_int
+    L.snap_paged_evict.argtypes = [pcfg, ppaged, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp, vp]
     _lib = L
     return L
 
@@ -109,7 +139,8 @@ EXPORTS = ("snap_cache_layout", "snap_compress_workspace_bytes", "snap_decode_wo
            "snap_kernel_launch_count", "snap_prefill_attn", "snap_compress_with_row_stats", "snap_debug_set_option",
            "snap_block_stats_bytes", "snap_block_stats", "snap_block_select", "snap_block_select_workspace_bytes",
            "snap_decode_blocks_workspace_bytes",
-           "snap_decode_attn_blocks")
+           "snap_decode_attn_blocks", "snap_rope_table", "snap_rope", "snap_paged_append", "snap_paged_decode_workspace_bytes",
+           "snap_paged_decode_attn", "snap_paged_evict_workspace_bytes", "snap_paged_evict")
 
 # testing / tuning options of snap_debug_set_option
 (SNAP_OPT_SCORE_KERNEL, SNAP_OPT_DECODE_GQA_KERNEL, SNAP_OPT_DECODE_LATENT_KERNEL, SNAP_OPT_DECODE_NSPLIT,
@@ -353,3 +384,162 @@ def snap_decode_attn_blocks(cfg: SnapConfig, layout: SnapLayout, q, k_new, v_new
                                          int(n_active), _ptr(k_cache), _ptr(v_cache), _ptr(seq_len), _ptr(valid_topk),
                                          int(block_tokens), int(n_blocks), _ptr(block_idx), _ptr(n_selected), _ptr(out),
                                          _ptr(workspace), ws_bytes, _ptr(status), _stream(stream)), "snap_decode_attn_blocks")
+
+
+# --- rotary positions and the paged cache ---
+_DTYPES = {SNAP_F32: torch.float32, SNAP_BF16: torch.bfloat16}
+
+
+def _expect(where: str, *named) -> Optional[int]:
+    """The tensors of a call: (name, tensor or None, dtype, shape or None, dense).  They have to be what the library is
+    told they are, and on one device.  Returns that device."""
+    device = None
+    for name, t, dtype, shape, dense in named:
+        if t is None:
+            continue
+        if t.dtype != dtype:
+            raise ValueError(f"{where}: {name} is {t.dtype}, expected {dtype}")
+        if shape is not None and tuple(t.shape) != shape:
+            raise ValueError(f"{where}: {name} has shape {tuple(t.shape)}, expected {shape}")
+        if dense and not t.is_contiguous():
+            raise ValueError(f"{where}: {name} must be dense")
+        if not dense and t.dim() > 1 and t.shape[-1] > 1 and t.stride(-1) != 1:
+            raise ValueError(f"{where}: {name} needs a dense last dim")
+        at = t.get_device() if t.is_cuda else -1
+        if device is None:
+            device = at
+        elif at != device:
+            raise ValueError(f"{where}: {name} is on device {at}, not {device}")
+    if device is not None and device < 0:
+        raise ValueError(f"{where}: the tensors are not on a CUDA device")
+    return device
+
+
+def _current(where: str, device: Optional[int]) -> None:
+    if device is not None and device != torch.cuda.current_device():
+        raise ValueError(f"{where}: the tensors are on device {device}, the current device is {torch.cuda.current_device()}")
+
+
+def _strides(t: Optional[torch.Tensor]):
+    return (0, 0) if t is None else (t.stride(0), t.stride(1))
+
+
+def make_rope(*, rot_dim: int, rot_offset: int = 0, interleaved: bool = False, scaling="plain", base: float = 10000.0,
+              factor: float = 1.0, original_len: float = 0.0, low_freq: float = 1.0, high_freq: float = 4.0,
+              beta_fast: float = 32.0, beta_slow: float = 1.0, magnitude: float = 0.0) -> SnapRope:
+    if isinstance(scaling, str):
+        scaling = {"plain": SNAP_ROPE_PLAIN, "linear": SNAP_ROPE_LINEAR, "llama3": SNAP_ROPE_LLAMA3, "yarn": SNAP_ROPE_YARN}[scaling]
+    return SnapRope(int(rot_dim), int(rot_offset), int(bool(interleaved)), int(scaling), float(base), float(factor), float(original_len),
+                    float(low_freq), float(high_freq), float(beta_fast), float(beta_slow), float(magnitude))
+
+
+def snap_rope_table(rope: SnapRope):
+    """(frequencies [rot_dim / 2] float64 on the host, magnitude)."""
+    freqs, magnitude = (C.c_double * max(rope.rot_dim // 2, 1))(), C.c_double()
+    _check(lib().snap_rope_table(C.byref(rope), freqs, C.byref(magnitude)), "snap_rope_table")
+    return torch.tensor(list(freqs), dtype=torch.float64), magnitude.value
+
+
+def snap_rope(cfg: SnapConfig, rope: SnapRope, freqs, positions, q=None, k=None, q_out=None, k_out=None, inverse: bool = False,
+              stream=None) -> None:
+    """Rotate q [T, Hq, d] and / or k [T, Hkv, d] (any strides with a dense last dim) into q_out and k_out, which may be
+    the inputs themselves.  freqs: float64 [rot_dim / 2], positions: int32 [T], on the device.  inverse: by minus the
+    angle (the gradient's direction)."""
+    where, dt, n = "snap_rope", _DTYPES.get(cfg.dtype), positions.shape[0]
+    sq, sk = (n, cfg.n_q_heads, cfg.d_qk), (n, cfg.n_kv_heads, cfg.d_qk)
+    _current(where, _expect(where, ("freqs", freqs, torch.float64, (rope.rot_dim // 2,), True),
+                            ("positions", positions, torch.int32, (n,), True), ("q", q, dt, sq, False), ("k", k, dt, sk, False),
+                            ("q_out", q_out, dt, sq, False), ("k_out", k_out, dt, sk, False)))
+    _check(lib().snap_rope(C.byref(cfg), C.byref(rope), _ptr(freqs), _ptr(positions), n, _ptr(q), *_strides(q), _ptr(q_out),
+                           *_strides(q_out), _ptr(k), *_strides(k), _ptr(k_out), *_strides(k_out), int(bool(inverse)),
+                           _stream(stream)), where)
+
+
+def make_paged(k_pages, v_pages, page_table) -> SnapPaged:
+    """Describe a paged cache: k_pages [n_pages, Hkv, page_tokens, d_qk], v_pages [n_pages, Hkv, page_tokens, d_v] (any
+    strides with a dense last dim: pages stored rows first are passed as their transposed view), page_table
+    [max_seqs, max_pages]."""
+    if k_pages.dim() != 4 or v_pages.dim() != 4 or k_pages.shape[:3] != v_pages.shape[:3] or page_table.dim() != 2:
+        raise ValueError("make_paged: k_pages and v_pages are [pages, heads, rows, dim], page_table [seqs, pages]")
+    (kp, kh, kr, _), (vp, vh, vr, _) = k_pages.stride(), v_pages.stride()
+    return SnapPaged(k_pages.shape[2], k_pages.shape[0], page_table.shape[1], 0, kp, kh, kr, vp, vh, vr)
+
+
+def _expect_paged(where, cfg, paged, k_pages, v_pages, page_table, seq_len, workspace, status, more) -> None:
+    dt, head = _DTYPES.get(cfg.dtype), (paged.n_pages, cfg.n_kv_heads, paged.page_tokens)
+    weights = (cfg.max_seqs, cfg.n_kv_heads, paged.max_pages * paged.page_tokens)
+    named = [("k_pages", k_pages, dt, head + (cfg.d_qk,), False), ("v_pages", v_pages, dt, head + (cfg.d_v,), False),
+             ("page_table", page_table, torch.int32, (cfg.max_seqs, paged.max_pages), True),
+             ("seq_len", seq_len, torch.int32, (cfg.max_seqs,), True), ("status", status, torch.int32, None, True)]
+    if workspace is not None:
+        named.append(("workspace", workspace, workspace.dtype, None, True))
+    named += [(name, t, dtype, weights if shape == "weights" else shape, dense) for name, t, dtype, shape, dense in more]
+    _current(where, _expect(where, *named))
+    if (k_pages.stride()[:3] != (paged.k_page_stride, paged.k_head_stride, paged.k_row_stride) or
+            v_pages.stride()[:3] != (paged.v_page_stride, paged.v_head_stride, paged.v_row_stride)):
+        raise ValueError(f"{where}: the pages' strides are not those of the description")
+
+
+def snap_paged_append(cfg: SnapConfig, paged: SnapPaged, slot_ids_dev, rows_dev, k, v, k_pages, v_pages, page_table, seq_len,
+                      rope: Optional[SnapRope] = None, freqs=None, positions=None, q=None, q_out=None, k_out=None, weights=None,
+                      status=None, stream=None) -> None:
+    """Write the rows of k [T, Hkv, d_qk], v [T, Hkv, d_v] into the pages, rotated on the way when rope is given; rows_dev
+    None: each token is its sequence's next row.  q -> q_out and k_out: the rotated queries and keys, dense."""
+    where, dt, n = "snap_paged_append", _DTYPES.get(cfg.dtype), slot_ids_dev.shape[0]
+    sq, sk, sv = (n, cfg.n_q_heads, cfg.d_qk), (n, cfg.n_kv_heads, cfg.d_qk), (n, cfg.n_kv_heads, cfg.d_v)
+    _expect_paged(where, cfg, paged, k_pages, v_pages, page_table, seq_len, None, status, [
+        ("slot_ids", slot_ids_dev, torch.int32, (n,), True), ("rows", rows_dev, torch.int32, (n,), True),
+        ("freqs", freqs, torch.float64, None if rope is None else (rope.rot_dim // 2,), True),
+        ("positions", positions, torch.int32, (n,), True), ("q", q, dt, sq, False), ("q_out", q_out, dt, sq, True),
+        ("k", k, dt, sk, False), ("k_out", k_out, dt, sk, True), ("v", v, dt, sv, False),
+        ("weights", weights, torch.float32, "weights", True)])
+    _check(lib().snap_paged_append(C.byref(cfg), C.byref(paged), _ptr(slot_ids_dev), _ptr(rows_dev), n,
+                                   None if rope is None else C.byref(rope), _ptr(freqs), _ptr(positions), _ptr(q), *_strides(q),
+                                   _ptr(q_out), _ptr(k), *_strides(k), _ptr(k_out), _ptr(v), *_strides(v), _ptr(k_pages),
+                                   _ptr(v_pages), _ptr(page_table), _ptr(seq_len), _ptr(weights), _ptr(status), _stream(stream)),
+           where)
+
+
+def snap_paged_decode_workspace_bytes(cfg: SnapConfig, paged: SnapPaged, n_active: int, with_weights: bool = False) -> int:
+    n = lib().snap_paged_decode_workspace_bytes(C.byref(cfg), C.byref(paged), int(n_active), int(bool(with_weights)))
+    if n < 0:
+        raise SnapError(int(n), "snap_paged_decode_workspace_bytes")
+    return int(n)
+
+
+def snap_paged_decode_attn(cfg: SnapConfig, paged: SnapPaged, q, slot_ids_dev, n_active: int, k_pages, v_pages, page_table,
+                           seq_len, out, workspace, weights_in=None, weights_out=None, status=None, stream=None) -> None:
+    """Attention of one token per sequence, q [n, Hq, d_qk] -> out [n, Hq, d_v], over the rows in its pages; weights_out
+    [max_seqs, Hkv, max_pages * page_tokens] float32 receives weights_in (None = 0) plus the group's softmax weights."""
+    where, dt, n = "snap_paged_decode_attn", _DTYPES.get(cfg.dtype), int(n_active)
+    _expect_paged(where, cfg, paged, k_pages, v_pages, page_table, seq_len, workspace, status, [
+        ("q", q, dt, (n, cfg.n_q_heads, cfg.d_qk), True), ("out", out, dt, (n, cfg.n_q_heads, cfg.d_v), True),
+        ("slot_ids", slot_ids_dev, torch.int32, (n,), True), ("weights_in", weights_in, torch.float32, "weights", True),
+        ("weights_out", weights_out, torch.float32, "weights", True)])
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib().snap_paged_decode_attn(C.byref(cfg), C.byref(paged), _ptr(q), _ptr(slot_ids_dev), n, _ptr(k_pages), _ptr(v_pages),
+                                        _ptr(page_table), _ptr(seq_len), _ptr(weights_in), _ptr(weights_out), _ptr(out),
+                                        _ptr(workspace), ws_bytes, _ptr(status), _stream(stream)), where)
+
+
+def snap_paged_evict_workspace_bytes(cfg: SnapConfig, paged: SnapPaged, n_seqs: int) -> int:
+    n = lib().snap_paged_evict_workspace_bytes(C.byref(cfg), C.byref(paged), int(n_seqs))
+    if n < 0:
+        raise SnapError(int(n), "snap_paged_evict_workspace_bytes")
+    return int(n)
+
+
+def snap_paged_evict(cfg: SnapConfig, paged: SnapPaged, src_slots_dev, dst_slots_dev, n_seqs: int, k_pages, v_pages, page_table,
+                     seq_len, weights_in, weights_out, workspace, kept_rows=None, status=None, stream=None) -> None:
+    """Copy the rows that stay (sinks, the topk of the middle by weight, the recent ones) of each source slot to its
+    destination slot's pages; kept_rows [n, Hkv, l_sink + topk + l_recent] int32 receives their source rows."""
+    where, n = "snap_paged_evict", int(n_seqs)
+    keep = cfg.l_sink + cfg.topk + cfg.l_recent
+    _expect_paged(where, cfg, paged, k_pages, v_pages, page_table, seq_len, workspace, status, [
+        ("src_slots", src_slots_dev, torch.int32, (n,), True), ("dst_slots", dst_slots_dev, torch.int32, (n,), True),
+        ("weights_in", weights_in, torch.float32, "weights", True), ("weights_out", weights_out, torch.float32, "weights", True),
+        ("kept_rows", kept_rows, torch.int32, (n, cfg.n_kv_heads, keep), True)])
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib().snap_paged_evict(C.byref(cfg), C.byref(paged), _ptr(src_slots_dev), _ptr(dst_slots_dev), n, _ptr(k_pages),
+                                  _ptr(v_pages), _ptr(page_table), _ptr(seq_len), _ptr(weights_in), _ptr(weights_out),
+                                  _ptr(kept_rows), _ptr(workspace), ws_bytes, _ptr(status), _stream(stream)), where)

@@ -45,8 +45,6 @@ bool decode_use_gqa_mma(int dtype, const Shape& s) {
   return decode_gqa_mma_supported(dtype, s);
 }
 
-namespace {
-
 int sm_count() {
   static int cached[kMaxDevices] = {};
   int dev = 0, n = 0;
@@ -63,7 +61,7 @@ int sm_count() {
 
 int elt_bytes(int dtype) { return dtype == SNAP_F32 ? 4 : 2; }
 
-int validate(const snap_config_t* c) {
+int validate_config(const snap_config_t* c) {
   if (!c) return SNAP_ERR_NULL_POINTER;
   if (c->dtype != SNAP_F32 && c->dtype != SNAP_BF16) return SNAP_ERR_INVALID_ARG;
   if (c->n_q_heads < 1 || c->n_kv_heads < 1 || c->n_q_heads % c->n_kv_heads) return SNAP_ERR_INVALID_ARG;
@@ -90,12 +88,7 @@ Shape make_shape(const snap_config_t* c) {
   return s;
 }
 
-size_t align_up(size_t x, size_t a = 256) { return (x + a - 1) / a * a; }
-// Every device buffer must start on a 16-byte boundary (the kernels use 16-byte accesses and bulk copies); a
-// pointer that does not is refused here rather than left to fault on the device.  NULL passes: optional
-// arguments are checked for presence separately.
-template <typename... P>
-bool misaligned(const P*... p) { return (((reinterpret_cast<uintptr_t>(p) & 15u) != 0) || ...); }
+namespace {
 
 // Option SNAP_OPT_SCORE_KERNEL = 1 (mma.sync) or 2 (SIMT) forces a slower score kernel, 3 keeps the
 // tcgen05 kernels but without CTA pairs (testing aids); default: the best one.
@@ -243,7 +236,7 @@ int decode_step_with_scratch(const snap_config_t* cfg, const snap_layout_t* layo
                              int32_t n_active, void* k_cache_dev, void* v_cache_dev, int32_t* seq_len_dev,
                              const int32_t* valid_topk_dev, void* out_dev, float* scratch, size_t scratch_bytes,
                              size_t slack_bytes, int too_small, uint32_t* status_dev, void* cuda_stream) {
-  const int rc = validate(cfg);
+  const int rc = validate_config(cfg);
   if (rc != SNAP_OK) return rc;
   if (!layout) return SNAP_ERR_NULL_POINTER;
   if (n_active < 0) return SNAP_ERR_INVALID_ARG;
@@ -308,7 +301,7 @@ int snap_debug_set_option(int opt, int value) {
 
 int snap_cache_layout(const snap_config_t* cfg, snap_layout_t* out) {
   if (!cfg || !out) return SNAP_ERR_NULL_POINTER;
-  const int rc = validate(cfg);
+  const int rc = validate_config(cfg);
   if (rc != SNAP_OK) return rc;
   const int eb = elt_bytes(cfg->dtype);
   out->slots = cfg->l_sink + cfg->l_recent + cfg->topk;
@@ -328,7 +321,7 @@ int snap_cache_layout(const snap_config_t* cfg, snap_layout_t* out) {
 
 int64_t snap_compress_workspace_bytes(const snap_config_t* cfg, const int32_t* cu_seqlens_host,
                                       int32_t n_seq) {
-  int rc = validate(cfg);
+  int rc = validate_config(cfg);
   if (rc != SNAP_OK) return rc;
   rc = check_cu(cu_seqlens_host, n_seq);
   if (rc != SNAP_OK) return rc;
@@ -343,7 +336,7 @@ int64_t snap_compress_workspace_bytes(const snap_config_t* cfg, const int32_t* c
 }
 
 int64_t snap_decode_workspace_bytes(const snap_config_t* cfg, int32_t n_active) {
-  const int rc = validate(cfg);
+  const int rc = validate_config(cfg);
   if (rc != SNAP_OK) return rc;
   if (n_active < 0) return SNAP_ERR_INVALID_ARG;
   const Shape s = make_shape(cfg);
@@ -369,7 +362,7 @@ int snap_prefill_attn(const snap_config_t* cfg, const void* q_dev,
                       const void* v_dev, int64_t v_token_stride, int64_t v_head_stride,
                       const int32_t* cu_seqlens_host, int32_t n_seq, void* out_dev, float* row_mu_dev,
                       uint32_t* status_dev, void* cuda_stream) {
-  int rc = validate(cfg);
+  int rc = validate_config(cfg);
   if (rc != SNAP_OK) return rc;
   rc = check_cu(cu_seqlens_host, n_seq);
   if (rc != SNAP_OK) return rc;
@@ -412,7 +405,7 @@ int snap_compress_with_row_stats(const snap_config_t* cfg, const snap_layout_t* 
                                  void* k_cache_dev, void* v_cache_dev, int32_t* seq_len_dev,
                                  int32_t* valid_topk_dev, int32_t* topk_idx_dev, void* workspace_dev,
                                  size_t workspace_bytes, uint32_t* status_dev, void* cuda_stream) {
-  int rc = validate(cfg);
+  int rc = validate_config(cfg);
   if (rc != SNAP_OK) return rc;
   if (!layout || !slot_ids_host) return SNAP_ERR_NULL_POINTER;
   rc = check_cu(cu_seqlens_host, n_seq);
@@ -514,7 +507,7 @@ int snap_append_kv(const snap_config_t* cfg, const snap_layout_t* layout, const 
                    const void* v_new_dev, const int32_t* slot_ids_dev, int32_t n_active,
                    void* k_cache_dev, void* v_cache_dev, int32_t* seq_len_dev,
                    uint32_t* status_dev, void* cuda_stream) {
-  const int rc = validate(cfg);
+  const int rc = validate_config(cfg);
   if (rc != SNAP_OK) return rc;
   if (!layout) return SNAP_ERR_NULL_POINTER;
   if (n_active < 0) return SNAP_ERR_INVALID_ARG;
@@ -576,7 +569,7 @@ static StepStage step_stage(const snap_config_t* cfg, const Shape& s, int n_acti
 }
 
 int64_t snap_decode_multi_workspace_bytes(const snap_config_t* cfg, int32_t n_active, int32_t q_len) {
-  const int rc = validate(cfg);
+  const int rc = validate_config(cfg);
   if (rc != SNAP_OK) return rc;
   if (n_active < 0) return SNAP_ERR_INVALID_ARG;
   const Shape s = make_shape(cfg);
@@ -607,7 +600,7 @@ static Shape blocks_shape(Shape s, int block_tokens, int n_blocks) {
 }
 
 int64_t snap_block_stats_bytes(const snap_config_t* cfg, int32_t block_tokens) {
-  const int rc = validate(cfg);
+  const int rc = validate_config(cfg);
   if (rc != SNAP_OK) return rc;
   const Shape s = make_shape(cfg);
   const int bc = blocks_check(cfg, s, block_tokens);
@@ -618,7 +611,7 @@ int64_t snap_block_stats_bytes(const snap_config_t* cfg, int32_t block_tokens) {
 int snap_block_stats(const snap_config_t* cfg, const snap_layout_t* layout, const int32_t* slot_ids_dev, int32_t n_seqs,
                      const void* k_cache_dev, const int32_t* valid_topk_dev, int32_t block_tokens, void* stats_dev,
                      uint32_t* status_dev, void* cuda_stream) {
-  const int rc = validate(cfg);
+  const int rc = validate_config(cfg);
   if (rc != SNAP_OK) return rc;
   if (!layout) return SNAP_ERR_NULL_POINTER;
   if (n_seqs < 0) return SNAP_ERR_INVALID_ARG;
@@ -638,7 +631,7 @@ int snap_block_select(const snap_config_t* cfg, const snap_layout_t* layout, con
                       int32_t n_active, const void* stats_dev, const int32_t* valid_topk_dev, int32_t block_tokens,
                       int32_t n_blocks, int32_t* block_idx_dev, int32_t* n_selected_dev, void* workspace_dev,
                       size_t workspace_bytes, uint32_t* status_dev, void* cuda_stream) {
-  const int rc = validate(cfg);
+  const int rc = validate_config(cfg);
   if (rc != SNAP_OK) return rc;
   if (!layout) return SNAP_ERR_NULL_POINTER;
   if (n_active < 0 || n_blocks < 1) return SNAP_ERR_INVALID_ARG;
@@ -658,7 +651,7 @@ int snap_block_select(const snap_config_t* cfg, const snap_layout_t* layout, con
 }
 
 int64_t snap_block_select_workspace_bytes(const snap_config_t* cfg, int32_t n_active, int32_t block_tokens) {
-  const int rc = validate(cfg);
+  const int rc = validate_config(cfg);
   if (rc != SNAP_OK) return rc;
   if (n_active < 0) return SNAP_ERR_INVALID_ARG;
   const Shape s = make_shape(cfg);
@@ -668,7 +661,7 @@ int64_t snap_block_select_workspace_bytes(const snap_config_t* cfg, int32_t n_ac
 }
 
 int64_t snap_decode_blocks_workspace_bytes(const snap_config_t* cfg, int32_t n_active, int32_t block_tokens, int32_t n_blocks) {
-  const int rc = validate(cfg);
+  const int rc = validate_config(cfg);
   if (rc != SNAP_OK) return rc;
   if (n_active < 0 || n_blocks < 1) return SNAP_ERR_INVALID_ARG;
   const Shape s = make_shape(cfg);
@@ -683,7 +676,7 @@ int snap_decode_attn_blocks(const snap_config_t* cfg, const snap_layout_t* layou
                             void* v_cache_dev, int32_t* seq_len_dev, const int32_t* valid_topk_dev, int32_t block_tokens,
                             int32_t n_blocks, const int32_t* block_idx_dev, const int32_t* n_selected_dev, void* out_dev,
                             void* workspace_dev, size_t workspace_bytes, uint32_t* status_dev, void* cuda_stream) {
-  const int rc = validate(cfg);
+  const int rc = validate_config(cfg);
   if (rc != SNAP_OK) return rc;
   if (!layout) return SNAP_ERR_NULL_POINTER;
   if (n_active < 0 || n_blocks < 1) return SNAP_ERR_INVALID_ARG;
@@ -713,7 +706,7 @@ int snap_decode_attn_multi(const snap_config_t* cfg, const snap_layout_t* layout
                            int32_t n_active, int32_t q_len, void* k_cache_dev, void* v_cache_dev,
                            int32_t* seq_len_dev, const int32_t* valid_topk_dev, void* out_dev,
                            void* workspace_dev, size_t workspace_bytes, uint32_t* status_dev, void* cuda_stream) {
-  const int rc = validate(cfg);
+  const int rc = validate_config(cfg);
   if (rc != SNAP_OK) return rc;
   if (!layout) return SNAP_ERR_NULL_POINTER;
   if (n_active < 0) return SNAP_ERR_INVALID_ARG;

@@ -249,8 +249,6 @@ __global__ void __launch_bounds__(NT) append_kernel(const AppendArgs a) {
   if (threadIdx.x == 0) a.seq_len[slot] = t + 1;
 }
 
-inline int elt_bytes(int dtype) { return dtype == SNAP_F32 ? 4 : 2; }
-
 }  // namespace
 
 cudaError_t launch_gather(int dtype, const Shape& s, const SeqBatch& b, const KVSource& src,

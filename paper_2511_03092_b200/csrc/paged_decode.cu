@@ -1,0 +1,991 @@
+// Attention of one token per sequence over a cache in pages (snap_paged_decode_attn).
+//
+//     out[i][h] = sum_r p_r V_r / sum_r p_r,   p_r = exp(scale q.K_r - max),   r over the sequence's rows
+//
+// Every cache row is read once and serves the whole head group, so HBM bounds the call.  The rows of all
+// sequences are cut into tiles of 16; (sequence, KV head, head block) is a unit, and the tiles of all units in a
+// row form one line that is divided evenly between the CTAs: sequences of any lengths load the GPU evenly and the
+// host need not know the lengths.  A CTA walks over its stretch of the line, which holds whole units and at most
+// one cut one at either end.  A whole unit's output is written at once; a cut one leaves the sum, the maximum and
+// the unnormalised output of its piece, which the second launch joins in a fixed order (no atomics: equal inputs
+// give equal bits).
+//
+// Tensor-core kernel (bf16, heads of 64, 128 or 256, pages of a multiple of 16 rows): the group's heads are the N
+// side of mma.sync.m16n8k16, S^T = K tile . Q^T and O^T += V tile^T . P^T, so the cost of a row does not grow with
+// the group.  Each warp runs a pipeline of its own over tiles fetched by TMA (four-dimensional map: dim, row of a
+// page, KV head, page) with the 128-byte swizzle; the pipeline runs ahead over unit borders, and the page number
+// of the tile after next is fetched while a tile is computed.  The probabilities enter the second product as two bf16
+// numbers (p and what its rounding left), which keeps their rounding out of the result: 2^-17 instead of 2^-9.
+//
+// Portable kernel (fp32, other heads, pages of any size): a lane holds four dims of a row, a warp eight rows at a
+// time straight from global memory; the 8 x heads partial dot products are reduced by halving exchanges (after
+// which a lane owns one (row, head) pair: one shuffle per pair instead of five) and every lane does one
+// exponential.
+//
+// With weights, the split kernel also stores the logits, and CTAs of the second launch turn them into the group's
+// attention weight of each row once the unit's maximum and sum are known.
+#include <cuda.h>
+
+#include "mma_helpers.cuh"
+#include "snap_internal.cuh"
+#include "umma_helpers.cuh"
+
+namespace snap {
+namespace {
+
+using namespace mmasync;
+using umma::mbar_expect_tx;
+using umma::mbar_init;
+using umma::mbar_try_wait;
+using umma::smem_u32;
+
+constexpr int TR = 16;                          // rows of a tile
+constexpr int MAX_CTAS = 1024;
+constexpr unsigned kPagedWaitLimit = 1u << 22;
+
+struct PagedArgs {
+  const void* q; void* out;
+  const void* kp; const void* vp;
+  const int* slots; const int* seq_len;
+  int n, Hq, Hkv, g, gb, nhb, U, d_qk, d_v, max_seqs;    // U = Hkv * nhb units per sequence, gb heads each (the last block fewer)
+  float scale_log2;
+  PageMap map;
+  long long* prefix;                            // [n + 1] tiles of a unit before sequence i
+  float2* ml_unit;                              // [n * U][gb]: (max, sum), log2 domain, of units that one CTA did whole
+  float2* ml_part; float* o_part;               // [2 * CTAs][gb], [2 * CTAs][gb][d_v]: a CTA's first / last piece, if cut
+  float* scores;                                // NULL, or [n * U][cap][gb] logits in the log2 domain
+  const float* w_in; float* w_out;
+  uint32_t* status;
+  int ctas;
+};
+
+__device__ __forceinline__ int rows_of(const PagedArgs& a, int slot) {
+  if (slot < 0 || slot >= a.max_seqs) return 0;
+  return min(max(a.seq_len[slot], 0), a.map.cap);
+}
+__device__ __forceinline__ int tiles_of(int rows) { return (rows + TR - 1) / TR; }
+
+// CTAs that share W tiles (at least MIN_TILES each where there are that many CTAs), and who has tile t
+constexpr int MIN_TILES = 4;
+__device__ __forceinline__ int active_ctas(long long W, int ctas) {
+  const long long n = (W + MIN_TILES - 1) / MIN_TILES;
+  return n < ctas ? (int)n : ctas;
+}
+__device__ __forceinline__ long long first_tile(long long W, int active, int c) { return W * c / active; }
+__device__ __forceinline__ int owner_of(long long t, long long W, int active) { return (int)(((t + 1) * active - 1) / W); }
+
+// A place on the line of tiles.
+struct Place { int e, u, t, nt, slot, len; };   // sequence, unit, tile of the unit, tiles per unit, slot, rows
+__device__ __forceinline__ void load_entry(const PagedArgs& a, Place& p) {
+  if (p.e >= a.n) {                             // not reached unless another stream changes the lengths during the call
+    p.slot = -1; p.len = 0; p.nt = 1 << 30; p.e = a.n - 1;
+    return;
+  }
+  p.slot = a.slots[p.e];
+  p.len = rows_of(a, p.slot);
+  p.nt = tiles_of(p.len);
+}
+// `step` tiles on; the caller knows that the line reaches that far
+__device__ __forceinline__ void advance(const PagedArgs& a, Place& p, int step) {
+  p.t += step;
+  while (p.t >= p.nt) {
+    p.t -= p.nt;
+    if (++p.u == a.U) {
+      p.u = 0;
+      do { ++p.e; load_entry(a, p); } while (p.nt == 0);
+    }
+  }
+}
+
+// All threads of the CTA: the CTA's stretch [x0, x1) of the line and the place of x0.  Returns false (to all) when it
+// is empty.  CTA 0 also writes the prefix array and reports bad slots and lengths.
+template <int NT>
+__device__ bool locate(const PagedArgs& a, long long& x0, long long& x1, Place& p, long long* scan /* shared, NT / 32 + 2 */) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, c = blockIdx.x;
+  const int per = (a.n + NT - 1) / NT, e0 = min(tid * per, a.n), e1 = min(e0 + per, a.n);
+  long long mine = 0;
+  unsigned bad = 0;
+  for (int e = e0; e < e1; ++e) {
+    const int slot = a.slots[e];
+    mine += tiles_of(rows_of(a, slot));
+    if (slot < -1 || slot >= a.max_seqs) bad |= SNAP_DEV_BAD_SLOT;
+    else if (slot >= 0 && a.seq_len[slot] > a.map.cap) bad |= SNAP_DEV_BAD_PAGE;
+  }
+  long long incl = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) { const long long v = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += v; }
+  if (lane == 31) scan[warp] = incl;
+  __syncthreads();
+  long long before = incl - mine, total = 0;
+#pragma unroll
+  for (int w = 0; w < NT / 32; ++w) { const long long v = scan[w]; total += v; if (w < warp) before += v; }
+  if (c == 0) {
+    long long at = before;
+    for (int e = e0; e < e1; ++e) { a.prefix[e] = at; at += tiles_of(rows_of(a, a.slots[e])); }
+    if (tid == 0) a.prefix[a.n] = total;
+    if (bad && a.status) atomicOr(a.status, bad);
+  }
+  const long long W = total * a.U;
+  const int active = active_ctas(W, a.ctas);
+  if (c >= active) return false;
+  x0 = first_tile(W, active, c);
+  x1 = first_tile(W, active, c + 1);
+  __shared__ int s_e;
+  __shared__ long long s_before;
+  if (tid == 0) { s_e = 0; s_before = 0; }
+  __syncthreads();
+  if (x0 >= before * a.U && x0 < (before + mine) * a.U) {                 // exactly one thread
+    for (int e = e0; e < e1; ++e) {
+      const int nt = tiles_of(rows_of(a, a.slots[e]));
+      if (x0 < (before + nt) * a.U) { s_e = e; s_before = before; break; }
+      before += nt;
+    }
+  }
+  __syncthreads();
+  p.e = s_e;
+  load_entry(a, p);
+  p.nt = max(p.nt, 1);                                                   // (as in load_entry: stays in bounds whatever the lengths do)
+  const long long rel = x0 - s_before * a.U;
+  p.u = (int)min(rel / p.nt, (long long)a.U - 1);
+  p.t = (int)(rel - (long long)p.u * p.nt);
+  return true;
+}
+
+// The CTA's joined result of a segment, [cols][ld] in shared memory, leaves for the output (a whole unit) or the
+// scratch of pieces.  L, M: per column in shared memory.
+template <typename T, int NT>
+__device__ __forceinline__ void write_segment(const PagedArgs& a, const float* buf, int ld, const float* M, const float* L, int e, int u,
+                                              int nh, bool whole, int piece) {
+  const int tid = threadIdx.x, d4 = a.d_v / 4;
+  const int kvh = u / a.nhb, hb = u - kvh * a.nhb;
+  if (whole) {
+    T* out = static_cast<T*>(a.out) + ((long long)e * a.Hq + kvh * a.g + hb * a.gb) * a.d_v;
+    for (int x = tid; x < nh * d4; x += NT) {
+      const int h = x / d4, c = (x - h * d4) * 4;
+      const float4 o = *reinterpret_cast<const float4*>(buf + h * ld + c);
+      const float inv = L[h] > 0.f ? 1.f / L[h] : L[h];                    // no row: zero; NaN stays
+      alignas(16) T r[4] = {from_f32<T>(o.x * inv), from_f32<T>(o.y * inv), from_f32<T>(o.z * inv), from_f32<T>(o.w * inv)};
+      if (sizeof(T) == 4) *reinterpret_cast<uint4*>(out + h * a.d_v + c) = *reinterpret_cast<const uint4*>(r);
+      else *reinterpret_cast<uint2*>(out + h * a.d_v + c) = *reinterpret_cast<const uint2*>(r);
+    }
+    if (a.scores && tid < nh) a.ml_unit[((long long)e * a.U + u) * a.gb + tid] = make_float2(M[tid], L[tid]);
+  } else {
+    float* o = a.o_part + (long long)piece * a.gb * a.d_v;
+    for (int x = tid; x < nh * d4; x += NT) {
+      const int h = x / d4, c = (x - h * d4) * 4;
+      *reinterpret_cast<float4*>(o + h * a.d_v + c) = *reinterpret_cast<const float4*>(buf + h * ld + c);
+    }
+    if (tid < nh) a.ml_part[(long long)piece * a.gb + tid] = make_float2(M[tid], L[tid]);
+  }
+}
+
+__device__ __forceinline__ bool wait_bounded(uint32_t bar, unsigned parity) {
+  for (unsigned it = 0; it < kPagedWaitLimit; ++it)
+    if (mbar_try_wait(bar, parity)) return true;
+  return false;
+}
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, int c3, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+      ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar) : "memory");
+}
+// byte offset of row r, 16-byte chunk c (0..7) inside a 128-byte-swizzled slab
+__device__ __forceinline__ uint32_t swz(int r, int c) { return (uint32_t)(r * 128 + ((c ^ (r & 7)) << 4)); }
+
+// ---------------------------------------------------------------------------------------------------------------
+// tensor-core kernel
+// ---------------------------------------------------------------------------------------------------------------
+constexpr int SLAB_B = TR * 128;                 // one 64-dim slab of a tile
+
+template <int D, int NWARP, int NSTAGE, int NG> struct MmaShape {
+  static constexpr int NT = NWARP * 32, NSL = D / 64, KS = D / 16, NCOL = 8 * NG;
+  static constexpr int TENS_B = NSL * SLAB_B, STAGE_B = 2 * TENS_B;
+  static constexpr int LD = D + 4;               // column stride of the exchange buffers: fragments store without bank conflicts
+  static constexpr size_t stages_b = (size_t)NWARP * NSTAGE * STAGE_B;
+  static constexpr size_t bars_b = NWARP * NSTAGE * 8;
+  static constexpr size_t smem = 1024 + stages_b + bars_b + (size_t)(2 * NCOL * LD + 2 * NWARP * NCOL + 2 * NCOL) * sizeof(float);
+};
+
+template <int D, int NWARP, int NSTAGE, int NG, int CTAS>
+__global__ void __launch_bounds__(NWARP * 32, CTAS)
+paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v) {
+  using S = MmaShape<D, NWARP, NSTAGE, NG>;
+  constexpr int KS = S::KS, NCOL = S::NCOL, LD = S::LD;
+  extern __shared__ unsigned char smem_dyn[];
+  unsigned char* stages = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~uintptr_t(1023));
+  uint64_t* bars = reinterpret_cast<uint64_t*>(stages + S::stages_b);
+  float* buf = reinterpret_cast<float*>(bars + NWARP * NSTAGE);          // [2][NCOL][LD]
+  float* wm = buf + 2 * NCOL * LD;                                       // [NWARP][NCOL] maxima, then sums
+  float* wl = wm + NWARP * NCOL;
+  float* jm = wl + NWARP * NCOL;                                         // [NCOL] joined maxima, then sums
+  float* jl = jm + NCOL;
+  __shared__ long long scan[S::NT / 32 + 2];
+
+  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, gq = lane >> 2, tq = lane & 3;
+  unsigned char* wstages = stages + w * NSTAGE * S::STAGE_B;
+  const uint32_t stage0 = smem_u32(wstages), bar0 = smem_u32(bars + w * NSTAGE);
+  if (lane == 0) {
+    for (int s = 0; s < NSTAGE; ++s) mbar_init(bar0 + 8 * s, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncwarp();
+  pdl_wait();
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+  long long x0, x1;
+  Place at;
+  if (!locate<S::NT>(a, x0, x1, at, scan)) return;
+  const int total = (int)(x1 - x0);                                      // this CTA's tiles; warp w takes w, w + NWARP, ...
+  const int mine = total > w ? (total - w + NWARP - 1) / NWARP : 0;
+
+  // ---- the warp's producer: runs NSTAGE tiles ahead of the consumer, over unit borders ----
+  Place pr = at;
+  int pid = 0, n_issued = 0;
+  unsigned bad_stage = 0;                                                // bit s: the tile in stage s is on a bad page
+  const int tpp = a.map.page / TR;
+  const auto fetch_pid = [&]() { pid = pr.len > 0 ? a.map.table[(long long)pr.slot * a.map.max_pages + pr.t / tpp] : -1; };
+  const auto issue = [&]() {
+    const int s = n_issued % NSTAGE;
+    const bool bad = pid < 0 || pid >= a.map.n_pages;
+    bad_stage = bad ? bad_stage | (1u << s) : bad_stage & ~(1u << s);
+    if (lane == 0) {
+      const uint32_t dst = stage0 + s * S::STAGE_B, bar = bar0 + 8 * s;
+      const int row = (pr.t % tpp) * TR, kvh = pr.u / a.nhb, page = bad ? 0 : pid;
+      mbar_expect_tx(bar, (unsigned)S::STAGE_B);
+#pragma unroll
+      for (int h = 0; h < S::NSL; ++h) {
+        tma_load_4d(dst + h * SLAB_B, &tmap_k, 64 * h, row, kvh, page, bar);
+        tma_load_4d(dst + S::TENS_B + h * SLAB_B, &tmap_v, 64 * h, row, kvh, page, bar);
+      }
+      if (bad && a.status) atomicOr(a.status, SNAP_DEV_BAD_PAGE);
+    }
+    if (++n_issued < mine) { advance(a, pr, NWARP); fetch_pid(); }
+  };
+  if (mine > 0) {
+    if (w > 0) advance(a, pr, w);
+    fetch_pid();
+    for (int s = 0; s < NSTAGE && n_issued < mine; ++s) issue();
+  }
+
+  // ldmatrix lane roles: K (plain): row (lane & 7) + 8 * bit3, chunk + bit4; V (transposed): row (lane & 7) + 8 * bit4, chunk + bit3
+  const int k_row = (lane & 7) + ((lane >> 3) & 1) * 8, k_cadd = lane >> 4;
+  const int v_row = (lane & 7) + ((lane >> 4) & 1) * 8, v_cadd = (lane >> 3) & 1;
+
+  bool dead = false;                                                     // a bounded wait ran out: nothing more is read
+  int n = 0, seg0 = 0;                                                   // tiles done by this warp; the segment's first tile
+  const __nv_bfloat16* q_all = static_cast<const __nv_bfloat16*>(a.q);
+  while (seg0 < total) {
+    // ---- a segment: the CTA's tiles of one unit ----
+    const int seg1 = min(total, seg0 + at.nt - at.t);
+    const int kvh = at.u / a.nhb, hb = at.u - kvh * a.nhb, nh = min(a.gb, a.g - hb * a.gb);
+    const bool whole = at.t == 0 && seg1 - seg0 == at.nt;
+    uint32_t qb[NG][KS][2];                                              // B fragments of Q^T: column 8 gi + gq, dims 16 ks + 2 tq (+8)
+#pragma unroll
+    for (int gi = 0; gi < NG; ++gi) {
+      const int col = 8 * gi + gq;
+      const __nv_bfloat16* qp = q_all + ((long long)at.e * a.Hq + kvh * a.g + hb * a.gb + (col < nh ? col : 0)) * D + 2 * tq;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        qb[gi][ks][0] = col < nh ? *reinterpret_cast<const uint32_t*>(qp + 16 * ks) : 0u;
+        qb[gi][ks][1] = col < nh ? *reinterpret_cast<const uint32_t*>(qp + 16 * ks + 8) : 0u;
+      }
+    }
+    float oacc[NG][KS][4], m_ref[NG][2], l_part[NG][2];                  // O^T: dims 16 db + gq (+8), columns 8 gi + 2 tq (+1)
+#pragma unroll
+    for (int gi = 0; gi < NG; ++gi) {
+      m_ref[gi][0] = m_ref[gi][1] = -INFINITY;
+      l_part[gi][0] = l_part[gi][1] = 0.f;
+#pragma unroll
+      for (int db = 0; db < KS; ++db)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) oacc[gi][db][x] = 0.f;
+    }
+    float* srow = a.scores ? a.scores + ((long long)at.e * a.U + at.u) * a.map.cap * a.gb : nullptr;
+
+    for (; n < mine && w + n * NWARP < seg1 && !dead; ++n) {
+      const int s = n % NSTAGE;
+      const bool landed = wait_bounded(bar0 + 8 * s, (unsigned)(n / NSTAGE) & 1u);
+      if (__any_sync(0xffffffffu, !landed)) { dead = true; break; }
+      const int row0 = (at.t + (w + n * NWARP - seg0)) * TR;
+      const int nrows = (bad_stage >> s) & 1u ? 0 : min(at.len - row0, TR);
+      const uint32_t sK = stage0 + s * S::STAGE_B, sV = sK + S::TENS_B;
+      if (nrows < TR) {
+        // rows past the end may hold anything, and a zero probability does not silence a NaN in V: clear them
+        constexpr int CPR = D / 8;
+        for (int x = lane; x < (TR - nrows) * CPR; x += 32) {
+          const int r = nrows + x / CPR, c = x % CPR;
+          *reinterpret_cast<uint4*>(wstages + s * S::STAGE_B + S::TENS_B + (c >> 3) * SLAB_B + swz(r, c & 7)) = make_uint4(0, 0, 0, 0);
+        }
+        __syncwarp();
+      }
+      // ---- S^T = K tile . Q^T ----
+      float v[NG][4];
+#pragma unroll
+      for (int gi = 0; gi < NG; ++gi) v[gi][0] = v[gi][1] = v[gi][2] = v[gi][3] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        uint32_t af[4];
+        ldsm4(sK + (ks >> 2) * SLAB_B + swz(k_row, (ks & 3) * 2 + k_cadd), af);
+#pragma unroll
+        for (int gi = 0; gi < NG; ++gi) mma16816(v[gi], af, qb[gi][ks][0], qb[gi][ks][1]);
+      }
+      bool refresh = false;
+#pragma unroll
+      for (int gi = 0; gi < NG; ++gi) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) v[gi][x] = gq + (x >> 1) * 8 < nrows ? v[gi][x] * a.scale_log2 : -INFINITY;
+        refresh = refresh || fmaxf(v[gi][0], v[gi][2]) > m_ref[gi][0] + 8.f || fmaxf(v[gi][1], v[gi][3]) > m_ref[gi][1] + 8.f;
+      }
+      if (srow) {
+#pragma unroll
+        for (int gi = 0; gi < NG; ++gi) {
+          const int col = 8 * gi + 2 * tq;
+#pragma unroll
+          for (int r8 = 0; r8 < 2; ++r8) {
+            const int row = row0 + gq + 8 * r8;
+            if (row >= at.len) continue;                                 // (a bad page's rows are written: as -inf)
+            float* sp = srow + (long long)row * a.gb + col;
+            if (col < nh) sp[0] = v[gi][2 * r8];
+            if (col + 1 < nh) sp[1] = v[gi][2 * r8 + 1];
+          }
+        }
+      }
+      // The reference of the exponentials follows the maximum lazily: it moves (and the sums are rescaled) only when
+      // a logit lies 8 above it, i.e. before a probability passes 2^8.
+      if (__any_sync(0xffffffffu, refresh)) {
+#pragma unroll
+        for (int gi = 0; gi < NG; ++gi) {
+          float mx0 = fmaxf(v[gi][0], v[gi][2]), mx1 = fmaxf(v[gi][1], v[gi][3]);
+#pragma unroll
+          for (int o = 4; o <= 16; o <<= 1) {
+            mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, o));
+            mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, o));
+          }
+          const float n0 = fmaxf(m_ref[gi][0], mx0), n1 = fmaxf(m_ref[gi][1], mx1);
+          const float a0 = m_ref[gi][0] == -INFINITY ? 0.f : exp2f(m_ref[gi][0] - n0);
+          const float a1 = m_ref[gi][1] == -INFINITY ? 0.f : exp2f(m_ref[gi][1] - n1);
+          m_ref[gi][0] = n0; m_ref[gi][1] = n1;
+          l_part[gi][0] *= a0; l_part[gi][1] *= a1;
+#pragma unroll
+          for (int db = 0; db < KS; ++db) {
+            oacc[gi][db][0] *= a0; oacc[gi][db][1] *= a1; oacc[gi][db][2] *= a0; oacc[gi][db][3] *= a1;
+          }
+        }
+      }
+      uint32_t ph[NG][2], pl[NG][2];                                     // P^T as B operands: the rounded p and the rest
+#pragma unroll
+      for (int gi = 0; gi < NG; ++gi) {
+        const float r0 = m_ref[gi][0] == -INFINITY ? 0.f : m_ref[gi][0], r1 = m_ref[gi][1] == -INFINITY ? 0.f : m_ref[gi][1];
+#pragma unroll
+        for (int r8 = 0; r8 < 2; ++r8) {
+          const float p0 = fast_exp2(v[gi][2 * r8] - r0), p1 = fast_exp2(v[gi][2 * r8 + 1] - r1);
+          l_part[gi][0] += p0;
+          l_part[gi][1] += p1;
+          const uint32_t hi = pack_bf16(p0, p1);
+          const float h0 = __uint_as_float(hi << 16), h1 = __uint_as_float(hi & 0xffff0000u);
+          ph[gi][r8] = movmatrix_t(hi);
+          pl[gi][r8] = movmatrix_t(pack_bf16(p0 - h0, p1 - h1));
+        }
+      }
+      // ---- O^T += V tile^T . P^T ----
+#pragma unroll
+      for (int db = 0; db < KS; ++db) {
+        uint32_t af[4];
+        ldsm4t(sV + (db >> 2) * SLAB_B + swz(v_row, (db & 3) * 2 + v_cadd), af);
+#pragma unroll
+        for (int gi = 0; gi < NG; ++gi) {
+          mma16816(oacc[gi][db], af, ph[gi][0], ph[gi][1]);
+          mma16816(oacc[gi][db], af, pl[gi][0], pl[gi][1]);
+        }
+      }
+      __syncwarp();
+      if (n_issued < mine) {
+        // the stage was read, and possibly cleared, through the generic proxy; the copy that refills it is of the async proxy
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        issue();
+      }
+    }
+
+    // ---- join the warps: maxima first, then the outputs pairwise through two buffers ----
+#pragma unroll
+    for (int gi = 0; gi < NG; ++gi) {
+#pragma unroll
+      for (int o = 4; o <= 16; o <<= 1) {
+        l_part[gi][0] += __shfl_xor_sync(0xffffffffu, l_part[gi][0], o);
+        l_part[gi][1] += __shfl_xor_sync(0xffffffffu, l_part[gi][1], o);
+      }
+      if (gq == 0) {
+        const int c = w * NCOL + 8 * gi + 2 * tq;
+        wm[c] = m_ref[gi][0]; wm[c + 1] = m_ref[gi][1];
+        wl[c] = l_part[gi][0]; wl[c + 1] = l_part[gi][1];
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int gi = 0; gi < NG; ++gi) {
+      float f[2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        float M = -INFINITY;
+#pragma unroll
+        for (int ww = 0; ww < NWARP; ++ww) M = fmaxf(M, wm[ww * NCOL + 8 * gi + 2 * tq + x]);
+        f[x] = m_ref[gi][x] == -INFINITY ? 0.f : exp2f(m_ref[gi][x] - M);
+      }
+#pragma unroll
+      for (int db = 0; db < KS; ++db) {
+        oacc[gi][db][0] *= f[0]; oacc[gi][db][1] *= f[1]; oacc[gi][db][2] *= f[0]; oacc[gi][db][3] *= f[1];
+      }
+    }
+    if (tid < NCOL) {
+      float M = -INFINITY, L = 0.f;
+#pragma unroll
+      for (int ww = 0; ww < NWARP; ++ww) M = fmaxf(M, wm[ww * NCOL + tid]);
+#pragma unroll
+      for (int ww = 0; ww < NWARP; ++ww) {
+        const float mw = wm[ww * NCOL + tid];
+        L += mw == -INFINITY ? 0.f : wl[ww * NCOL + tid] * exp2f(mw - M);
+      }
+      jm[tid] = M; jl[tid] = L;
+    }
+    const auto exchange = [&](float* b, bool store) {
+#pragma unroll
+      for (int gi = 0; gi < NG; ++gi)
+#pragma unroll
+        for (int db = 0; db < KS; ++db)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            float* p = b + (8 * gi + 2 * tq + (x & 1)) * LD + 16 * db + gq + 8 * (x >> 1);
+            if (store) *p = oacc[gi][db][x];
+            else oacc[gi][db][x] += *p;
+          }
+    };
+    if (NWARP == 4) {
+      if (w >= 2) exchange(buf + (w - 2) * NCOL * LD, true);
+      __syncthreads();
+      if (w < 2) exchange(buf + w * NCOL * LD, false);
+    }
+    if (w == 1) exchange(buf + NCOL * LD, true);
+    __syncthreads();
+    if (w == 0) {
+      exchange(buf + NCOL * LD, false);
+      exchange(buf, true);
+    }
+    __syncthreads();
+    write_segment<__nv_bfloat16, S::NT>(a, buf, LD, jm, jl, at.e, at.u, nh, whole, 2 * blockIdx.x + (seg0 > 0));
+
+    if (seg1 < total) advance(a, at, seg1 - seg0);
+    seg0 = seg1;
+  }
+  if (dead) {
+    if (a.status) atomicOr(a.status, SNAP_DEV_WAIT_TIMEOUT);
+    for (int x = n; x < n_issued; ++x) (void)wait_bounded(bar0 + 8 * (x % NSTAGE), (unsigned)(x / NSTAGE) & 1u);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// portable kernel
+// ---------------------------------------------------------------------------------------------------------------
+template <typename T> struct Four;                // four consecutive elements as loaded
+template <> struct Four<float> {
+  float4 r;
+  __device__ __forceinline__ void load(const float* p) {
+    asm volatile("ld.global.L1::no_allocate.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(r.x), "=f"(r.y), "=f"(r.z), "=f"(r.w) : "l"(p));
+  }
+  __device__ __forceinline__ void zero() { r = make_float4(0.f, 0.f, 0.f, 0.f); }
+  __device__ __forceinline__ float4 f() const { return r; }
+};
+template <> struct Four<__nv_bfloat16> {
+  uint2 r;
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) {
+    asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(r.x), "=r"(r.y) : "l"(p));
+  }
+  __device__ __forceinline__ void zero() { r = make_uint2(0u, 0u); }
+  __device__ __forceinline__ float4 f() const {
+    return make_float4(__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xffff0000u), __uint_as_float(r.y << 16),
+                       __uint_as_float(r.y & 0xffff0000u));
+  }
+};
+
+constexpr int SNW = 4, SNT = SNW * 32;            // warps and threads of a CTA
+
+// NV: 128-dim chunks of a row, HB: heads of a unit (a power of two)
+template <typename T, int NV, int HB, int CTAS>
+__global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_constant__ PagedArgs a) {
+  constexpr int LD = 128 * NV + 4;
+  constexpr int NVAL = 8 * HB, VPL = NVAL > 32 ? NVAL / 32 : 1;          // (row, head) values of eight rows; per lane after the exchange
+  __shared__ __align__(16) float buf[2 * HB * LD];
+  __shared__ float wm[SNW * HB], wl[SNW * HB], jm[HB], jl[HB];
+  __shared__ long long scan[SNT / 32 + 2];
+  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+  pdl_wait();
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  long long x0, x1;
+  Place at;
+  if (!locate<SNT>(a, x0, x1, at, scan)) return;
+  const int total = (int)(x1 - x0), mine = total > w ? (total - w + SNW - 1) / SNW : 0;
+  // After the exchange lane l owns row l / 4 of the eight and head (or heads) head_of(l & 3, k).
+  const int my_head = HB >= 8 ? 2 * (lane & 3) : HB == 4 ? (lane & 3) : HB == 2 ? ((lane & 3) >> 1) : 0;
+  const T* kbase = static_cast<const T*>(a.kp);
+  const T* vbase = static_cast<const T*>(a.vp);
+
+  // rows of the warp's next tile, a lane each: page number and row of the page
+  Place pr = at;
+  int pid = -1, prow = 0, ahead = 0;
+  const auto fetch = [&]() {
+    const int row = pr.t * TR + (lane & 15);
+    pid = -1;
+    if (row < pr.len) {
+      const int pg = row / a.map.page;
+      prow = row - pg * a.map.page;
+      pid = a.map.table[(long long)pr.slot * a.map.max_pages + pg];
+      if (pid < 0 || pid >= a.map.n_pages) { pid = -1; if (a.status) atomicOr(a.status, SNAP_DEV_BAD_PAGE); }
+    }
+  };
+  if (mine > 0) {
+    if (w > 0) advance(a, pr, w);
+    fetch();
+  }
+  int n = 0, seg0 = 0;
+  while (seg0 < total) {
+    const int seg1 = min(total, seg0 + at.nt - at.t);
+    const int kvh = at.u / a.nhb, hb = at.u - kvh * a.nhb, nh = min(a.gb, a.g - hb * a.gb);
+    const bool whole = at.t == 0 && seg1 - seg0 == at.nt;
+    float q[HB][NV][4], o[HB][NV][4], m_ref[VPL], l_part[VPL];
+#pragma unroll
+    for (int h = 0; h < HB; ++h)
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const int d = 4 * lane + 128 * j;
+        Four<T> x;
+        x.zero();
+        if (h < nh && d < a.d_qk) x.load(static_cast<const T*>(a.q) + ((long long)at.e * a.Hq + kvh * a.g + hb * a.gb + h) * a.d_qk + d);
+        const float4 f = x.f();
+        q[h][j][0] = f.x; q[h][j][1] = f.y; q[h][j][2] = f.z; q[h][j][3] = f.w;
+        o[h][j][0] = o[h][j][1] = o[h][j][2] = o[h][j][3] = 0.f;
+      }
+#pragma unroll
+    for (int k = 0; k < VPL; ++k) { m_ref[k] = -INFINITY; l_part[k] = 0.f; }
+    float* srow = a.scores ? a.scores + ((long long)at.e * a.U + at.u) * a.map.cap * a.gb : nullptr;
+
+    for (; n < mine && w + n * SNW < seg1; ++n) {
+      const int row0 = (at.t + (w + n * SNW - seg0)) * TR;
+      const int tpid = pid, tprow = prow;
+      if (++ahead < mine) { advance(a, pr, SNW); fetch(); }
+#pragma unroll 1
+      for (int r0 = 0; r0 < TR; r0 += 8) {
+        if (row0 + r0 >= at.len) break;
+        Four<T> kx[8][NV], vx[8][NV];
+        unsigned okay = 0;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+          const int p = __shfl_sync(0xffffffffu, tpid, r0 + r), x = __shfl_sync(0xffffffffu, tprow, r0 + r);
+          const T* kr = kbase + p * a.map.kp + kvh * a.map.kh + x * a.map.kr + 4 * lane;
+          const T* vr = vbase + p * a.map.vp + kvh * a.map.vh + x * a.map.vr + 4 * lane;
+          okay |= p >= 0 ? 1u << r : 0u;
+#pragma unroll
+          for (int j = 0; j < NV; ++j) {
+            kx[r][j].zero();
+            vx[r][j].zero();
+            if (p >= 0 && 4 * lane + 128 * j < a.d_qk) kx[r][j].load(kr + 128 * j);
+            if (p >= 0 && 4 * lane + 128 * j < a.d_v) vx[r][j].load(vr + 128 * j);
+          }
+        }
+        float s[NVAL];
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+#pragma unroll
+          for (int h = 0; h < HB; ++h) {
+            float x = 0.f;
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+              const float4 f = kx[r][j].f();
+              x = fmaf(f.x, q[h][j][0], x); x = fmaf(f.y, q[h][j][1], x); x = fmaf(f.z, q[h][j][2], x); x = fmaf(f.w, q[h][j][3], x);
+            }
+            s[r * HB + h] = x;
+          }
+        // halving exchange: each step sums over one lane bit and leaves a lane half of the values
+        int left = NVAL;
+#pragma unroll
+        for (int b = 16; b > 0; b >>= 1) {
+          if (left > 1) {
+            left >>= 1;
+#pragma unroll
+            for (int x = 0; x < NVAL / 2; ++x)
+              if (x < left) {
+                const bool up = lane & b;
+                const float give = up ? s[x] : s[x + left], keep = up ? s[x + left] : s[x];
+                s[x] = keep + __shfl_xor_sync(0xffffffffu, give, b);
+              }
+          } else {
+            s[0] += __shfl_xor_sync(0xffffffffu, s[0], b);
+          }
+        }
+        const int row = row0 + r0 + (lane >> 2);
+        const bool ok = (okay >> (lane >> 2)) & 1u;
+        float v[VPL];
+        bool refresh = false;
+#pragma unroll
+        for (int k = 0; k < VPL; ++k) {
+          v[k] = ok ? s[k] * a.scale_log2 : -INFINITY;
+          refresh = refresh || v[k] > m_ref[k] + 8.f;
+        }
+        if (srow && row < at.len) {
+          // HB = 2 and 1: the pairs are held by two and four lanes, all writing the same value
+#pragma unroll
+          for (int k = 0; k < VPL; ++k)
+            if (my_head + k < nh) srow[(long long)row * a.gb + my_head + k] = v[k];
+        }
+        if (__any_sync(0xffffffffu, refresh)) {
+          float al[VPL];
+#pragma unroll
+          for (int k = 0; k < VPL; ++k) {
+            float mx = v[k];
+#pragma unroll
+            for (int b = 4; b <= 16; b <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, b));
+            const float nm = fmaxf(m_ref[k], mx);
+            al[k] = m_ref[k] == -INFINITY ? 0.f : exp2f(m_ref[k] - nm);
+            m_ref[k] = nm;
+            l_part[k] *= al[k];
+          }
+#pragma unroll
+          for (int h = 0; h < HB; ++h) {
+            const float f = __shfl_sync(0xffffffffu, al[HB >= 8 ? (h & 1) : 0], HB >= 8 ? h / 2 : HB == 4 ? h : HB == 2 ? 2 * h : 0);
+#pragma unroll
+            for (int j = 0; j < NV; ++j) { o[h][j][0] *= f; o[h][j][1] *= f; o[h][j][2] *= f; o[h][j][3] *= f; }
+          }
+        }
+        float p[VPL];
+#pragma unroll
+        for (int k = 0; k < VPL; ++k) {
+          p[k] = fast_exp2(v[k] - (m_ref[k] == -INFINITY ? 0.f : m_ref[k]));
+          l_part[k] += p[k];
+        }
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+          float4 f[NV];
+#pragma unroll
+          for (int j = 0; j < NV; ++j) f[j] = vx[r][j].f();
+#pragma unroll
+          for (int h = 0; h < HB; ++h) {
+            const float pr_ = __shfl_sync(0xffffffffu, p[HB >= 8 ? (h & 1) : 0], 4 * r + (HB >= 8 ? h / 2 : HB == 4 ? h : HB == 2 ? 2 * h : 0));
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+              o[h][j][0] = fmaf(pr_, f[j].x, o[h][j][0]); o[h][j][1] = fmaf(pr_, f[j].y, o[h][j][1]);
+              o[h][j][2] = fmaf(pr_, f[j].z, o[h][j][2]); o[h][j][3] = fmaf(pr_, f[j].w, o[h][j][3]);
+            }
+          }
+        }
+      }
+    }
+
+    // ---- join the warps ----
+#pragma unroll
+    for (int k = 0; k < VPL; ++k) {
+#pragma unroll
+      for (int b = 4; b <= 16; b <<= 1) l_part[k] += __shfl_xor_sync(0xffffffffu, l_part[k], b);
+      if (lane < 4) { wm[w * HB + my_head + k] = m_ref[k]; wl[w * HB + my_head + k] = l_part[k]; }   // (equal values where lanes share a head)
+    }
+    __syncthreads();
+#pragma unroll
+    for (int h = 0; h < HB; ++h) {
+      float M = -INFINITY;
+#pragma unroll
+      for (int ww = 0; ww < SNW; ++ww) M = fmaxf(M, wm[ww * HB + h]);
+      const float mw = wm[w * HB + h], f = mw == -INFINITY ? 0.f : exp2f(mw - M);
+#pragma unroll
+      for (int j = 0; j < NV; ++j) { o[h][j][0] *= f; o[h][j][1] *= f; o[h][j][2] *= f; o[h][j][3] *= f; }
+      if (tid == h) {
+        float L = 0.f;
+#pragma unroll
+        for (int ww = 0; ww < SNW; ++ww) {
+          const float mx = wm[ww * HB + h];
+          L += mx == -INFINITY ? 0.f : wl[ww * HB + h] * exp2f(mx - M);
+        }
+        jm[h] = M; jl[h] = L;
+      }
+    }
+    const auto exchange = [&](float* b, bool store) {
+#pragma unroll
+      for (int h = 0; h < HB; ++h)
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+          float4* x = reinterpret_cast<float4*>(b + h * LD + 128 * j + 4 * lane);
+          if (store) *x = make_float4(o[h][j][0], o[h][j][1], o[h][j][2], o[h][j][3]);
+          else { const float4 f = *x; o[h][j][0] += f.x; o[h][j][1] += f.y; o[h][j][2] += f.z; o[h][j][3] += f.w; }
+        }
+    };
+    if (w >= 2) exchange(buf + (w - 2) * HB * LD, true);
+    __syncthreads();
+    if (w < 2) exchange(buf + w * HB * LD, false);
+    if (w == 1) exchange(buf + HB * LD, true);
+    __syncthreads();
+    if (w == 0) { exchange(buf + HB * LD, false); exchange(buf, true); }
+    __syncthreads();
+    write_segment<T, SNT>(a, buf, LD, jm, jl, at.e, at.u, nh, whole, 2 * blockIdx.x + (seg0 > 0));
+    if (seg1 < total) advance(a, at, seg1 - seg0);
+    seg0 = seg1;
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// second launch: joins the pieces of cut units, zeroes the outputs of empty sequences, sums the weights
+// ---------------------------------------------------------------------------------------------------------------
+constexpr int JNT = 256, JROWS = 4 * JNT;         // rows of a weights CTA
+
+struct Pieces { int np, c0, first; };              // pieces of a unit: index first, then 2 (c0 + k); np <= 1: done whole
+__device__ __forceinline__ Pieces pieces_of(const PagedArgs& a, int e, int u, int nt) {
+  Pieces p;
+  const long long W = a.prefix[a.n] * a.U, t0 = a.prefix[e] * a.U + (long long)u * nt;
+  const int active = active_ctas(W, a.ctas);
+  p.c0 = owner_of(t0, W, active);
+  p.np = owner_of(t0 + nt - 1, W, active) - p.c0 + 1;
+  p.first = 2 * p.c0 + (first_tile(W, active, p.c0) != t0);
+  return p;
+}
+__device__ __forceinline__ int piece_at(const Pieces& p, int k) { return k == 0 ? p.first : 2 * (p.c0 + k); }
+
+template <typename T>
+__global__ void __launch_bounds__(JNT) paged_join_kernel(const __grid_constant__ PagedArgs a) {
+  __shared__ __align__(16) float acc_s[JNT / 32][256];
+  __shared__ float f_s[MAX_CTAS], red[JNT / 32];
+  __shared__ float mu_s[16];
+  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+  pdl_wait();
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int merges = a.n * a.Hq;
+  if ((int)blockIdx.x < merges) {
+    // ---- one query head's output ----
+    const int e = blockIdx.x / a.Hq, head = blockIdx.x - e * a.Hq;
+    const int kvh = head / a.g, x = head - kvh * a.g, hb = x / a.gb, col = x - hb * a.gb;
+    const int nt = (int)(a.prefix[e + 1] - a.prefix[e]);
+    T* out = static_cast<T*>(a.out) + (long long)blockIdx.x * a.d_v;
+    if (nt == 0) {
+      for (int c = tid; c < a.d_v; c += JNT) out[c] = from_f32<T>(0.f);
+      return;
+    }
+    const Pieces p = pieces_of(a, e, kvh * a.nhb + hb, nt);
+    if (p.np <= 1) return;
+    float m = -INFINITY;
+    for (int k = tid; k < p.np; k += JNT) m = fmaxf(m, a.ml_part[(long long)piece_at(p, k) * a.gb + col].x);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if (lane == 0) red[w] = m;
+    __syncthreads();
+    m = red[0];
+#pragma unroll
+    for (int k = 1; k < JNT / 32; ++k) m = fmaxf(m, red[k]);
+    float l = 0.f;
+    for (int k = tid; k < p.np; k += JNT) {
+      const float2 ml = a.ml_part[(long long)piece_at(p, k) * a.gb + col];
+      const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - m);
+      f_s[k] = f;
+      l += f == 0.f ? 0.f : ml.y * f;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+    __syncthreads();                                                     // red has been read
+    if (lane == 0) red[w] = l;
+    __syncthreads();
+    l = 0.f;
+#pragma unroll
+    for (int k = 0; k < JNT / 32; ++k) l += red[k];
+    // a warp per piece, a lane per four dims
+    float4 acc[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
+#pragma unroll 4
+    for (int k = w; k < p.np; k += JNT / 32) {
+      const float* o = a.o_part + ((long long)piece_at(p, k) * a.gb + col) * a.d_v;
+      const float f = f_s[k];
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        if (4 * lane + 128 * j < a.d_v) {
+          const float4 v = *reinterpret_cast<const float4*>(o + 4 * lane + 128 * j);
+          acc[j].x = fmaf(f, v.x, acc[j].x); acc[j].y = fmaf(f, v.y, acc[j].y);
+          acc[j].z = fmaf(f, v.z, acc[j].z); acc[j].w = fmaf(f, v.w, acc[j].w);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      if (4 * lane + 128 * j < a.d_v) *reinterpret_cast<float4*>(&acc_s[w][4 * lane + 128 * j]) = acc[j];
+    __syncthreads();
+    const float inv = l > 0.f ? 1.f / l : l;
+    for (int c = tid; c < a.d_v; c += JNT) {
+      float s = 0.f;
+#pragma unroll
+      for (int k = 0; k < JNT / 32; ++k) s += acc_s[k][c];
+      out[c] = from_f32<T>(s * inv);
+    }
+    return;
+  }
+  // ---- JROWS rows' weights of one (sequence, KV head) ----
+  const int chunks = (a.map.cap + JROWS - 1) / JROWS;
+  const int id = blockIdx.x - merges, chunk = id % chunks, kvh = (id / chunks) % a.Hkv, e = id / chunks / a.Hkv;
+  const int nt = (int)(a.prefix[e + 1] - a.prefix[e]);
+  if (chunk * JROWS >= nt * TR) return;
+  const int slot = a.slots[e];
+  int again = 0;                                                         // the slot was listed before: its first entry counts
+  for (int x = tid; x < e; x += JNT) again |= a.slots[x] == slot;
+  if (__syncthreads_or(again)) {
+    if (tid == 0 && a.status) atomicOr(a.status, SNAP_DEV_BAD_SLOT);
+    return;
+  }
+  const int len = rows_of(a, slot);
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int hb = 0; hb < a.nhb; ++hb) {
+    const int u = kvh * a.nhb + hb, nh = min(a.gb, a.g - hb * a.gb);
+    const Pieces p = pieces_of(a, e, u, nt);
+    __syncthreads();                                                     // mu_s of the block before has been read
+    for (int col = w; col < nh; col += JNT / 32) {
+      float m = -INFINITY, l = 0.f;
+      if (p.np <= 1) {
+        const float2 ml = a.ml_unit[((long long)e * a.U + u) * a.gb + col];
+        m = ml.x; l = ml.y;
+      } else {
+        for (int k = lane; k < p.np; k += 32) m = fmaxf(m, a.ml_part[(long long)piece_at(p, k) * a.gb + col].x);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        for (int k = lane; k < p.np; k += 32) {
+          const float2 ml = a.ml_part[(long long)piece_at(p, k) * a.gb + col];
+          l += ml.x == -INFINITY ? 0.f : ml.y * exp2f(ml.x - m);
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+      }
+      if (lane == 0) mu_s[col] = l == 0.f ? INFINITY : m + log2f(l);     // p = 2^(score - mu); no valid row: 0
+    }
+    __syncthreads();
+    const float* sc = a.scores + ((long long)e * a.U + u) * a.map.cap * a.gb;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int row = chunk * JROWS + j * JNT + tid;
+      if (row < len) {
+        const float* sr = sc + (long long)row * a.gb;
+        if (a.gb % 4 == 0) {
+          for (int c = 0; c < nh; c += 4) {
+            const float4 v = *reinterpret_cast<const float4*>(sr + c);
+            sum[j] += exp2f(v.x - mu_s[c]);
+            if (c + 1 < nh) sum[j] += exp2f(v.y - mu_s[c + 1]);
+            if (c + 2 < nh) sum[j] += exp2f(v.z - mu_s[c + 2]);
+            if (c + 3 < nh) sum[j] += exp2f(v.w - mu_s[c + 3]);
+          }
+        } else {
+          for (int c = 0; c < nh; ++c) sum[j] += exp2f(sr[c] - mu_s[c]);
+        }
+      }
+    }
+  }
+  const long long base = ((long long)slot * a.Hkv + kvh) * a.map.cap;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int row = chunk * JROWS + j * JNT + tid;
+    if (row < len) a.w_out[base + row] = (a.w_in ? a.w_in[base + row] : 0.f) + sum[j];
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------------------------------------------
+template <int D, int NWARP, int NSTAGE, int NG, int CTAS>
+cudaError_t launch_mma(const PagedArgs& a, const CUtensorMap& tk, const CUtensorMap& tv, cudaStream_t st) {
+  using S = MmaShape<D, NWARP, NSTAGE, NG>;
+  static SmemLimit limit = {};
+  if (cudaError_t e = ensure_dyn_smem(paged_mma_kernel<D, NWARP, NSTAGE, NG, CTAS>, S::smem, limit)) return e;
+  const cudaError_t e = launch_pdl(paged_mma_kernel<D, NWARP, NSTAGE, NG, CTAS>, dim3(a.ctas), dim3(S::NT), S::smem, st, a, tk, tv);
+  count_launch();
+  return e;
+}
+
+// CTAs per SM that the kernels are built for (launch bounds, and the shared memory of the tensor-core ones)
+constexpr int kMmaCtas = 3, kMmaCtasWide = 2;
+constexpr int simt_ctas(bool wide, int gb) { return wide ? 2 : gb <= 2 ? 4 : 3; }
+
+template <typename T, int NV>
+cudaError_t launch_simt(const PagedArgs& a, cudaStream_t st) {
+  constexpr bool W = NV > 1;
+  cudaError_t e;
+  if (a.gb <= 1) e = launch_pdl(paged_simt_kernel<T, NV, 1, simt_ctas(W, 1)>, dim3(a.ctas), dim3(SNT), 0, st, a);
+  else if (a.gb <= 2) e = launch_pdl(paged_simt_kernel<T, NV, 2, simt_ctas(W, 2)>, dim3(a.ctas), dim3(SNT), 0, st, a);
+  else if (W || a.gb <= 4) e = launch_pdl(paged_simt_kernel<T, NV, 4, simt_ctas(W, 4)>, dim3(a.ctas), dim3(SNT), 0, st, a);
+  else e = launch_pdl(paged_simt_kernel<T, 1, 8, simt_ctas(false, 8)>, dim3(a.ctas), dim3(SNT), 0, st, a);
+  count_launch();
+  return e;
+}
+
+bool mma_shape(int dtype, const Shape& s, const PageMap& m) {
+  return dtype == SNAP_BF16 && s.d_qk == s.d_v && (s.d_qk == 64 || s.d_qk == 128 || s.d_qk == 256) && m.page % TR == 0 &&
+         umma::encode_tiled_fn() != nullptr;
+}
+
+}  // namespace
+
+int paged_decode_plan(int dtype, const Shape& s, const PageMap& m, int n_active, bool weights, int sms, PagedDecodePlan* p) {
+  p->mma = mma_shape(dtype, s, m);
+  const bool wide = s.d_qk > 128 || s.d_v > 128;
+  const int most = p->mma ? 16 : wide ? 4 : 8;                          // heads of a unit
+  p->nhb = (s.g + most - 1) / most;
+  p->gb = (s.g + p->nhb - 1) / p->nhb;
+  const int per_sm = p->mma ? (p->gb > 8 ? kMmaCtasWide : kMmaCtas) : simt_ctas(wide, p->gb);
+  p->ctas = sms * per_sm < MAX_CTAS ? sms * per_sm : MAX_CTAS;
+  const long long units = (long long)n_active * s.Hkv * p->nhb;
+  const long long chunks = (m.cap + JROWS - 1) / JROWS;
+  // grid and index limits; a line of tiles and the scratch have to be countable
+  if (units > (1LL << 30) || (long long)n_active * s.Hq + (weights ? (long long)n_active * s.Hkv * chunks : 0) > 0x7fffffffLL ||
+      units * ((m.cap + TR - 1) / TR) > (1LL << 50) / MAX_CTAS)
+    return SNAP_ERR_UNSUPPORTED;
+  size_t off = 0;
+  p->prefix_off = off; off += align_up((size_t)(n_active + 1) * sizeof(long long));
+  p->ml_off = off;     off += align_up(((size_t)units + 2 * (size_t)p->ctas) * p->gb * sizeof(float2));
+  p->o_off = off;      off += align_up(2 * (size_t)p->ctas * p->gb * s.d_v * sizeof(float));
+  p->score_off = off;
+  if (weights) off += align_up((size_t)units * m.cap * p->gb * sizeof(float));
+  p->bytes = off;
+  return SNAP_OK;
+}
+
+cudaError_t launch_paged_decode(int dtype, const Shape& s, const PageMap& m, const PagedDecodePlan& p, const void* q,
+                                const int* slots, int n_active, const void* k_pages, const void* v_pages, const int* seq_len,
+                                const float* w_in, float* w_out, void* out, char* scratch, uint32_t* status, cudaStream_t st) {
+  PagedArgs a;
+  a.q = q; a.out = out; a.kp = k_pages; a.vp = v_pages; a.slots = slots; a.seq_len = seq_len;
+  a.n = n_active; a.Hq = s.Hq; a.Hkv = s.Hkv; a.g = s.g; a.gb = p.gb; a.nhb = p.nhb; a.U = s.Hkv * p.nhb;
+  a.d_qk = s.d_qk; a.d_v = s.d_v; a.max_seqs = s.max_seqs;
+  a.scale_log2 = s.scale * 1.4426950408889634f;
+  a.map = m;
+  a.prefix = reinterpret_cast<long long*>(scratch + p.prefix_off);
+  a.ml_unit = reinterpret_cast<float2*>(scratch + p.ml_off);
+  a.ml_part = a.ml_unit + (size_t)n_active * a.U * p.gb;
+  a.o_part = reinterpret_cast<float*>(scratch + p.o_off);
+  a.scores = w_out ? reinterpret_cast<float*>(scratch + p.score_off) : nullptr;
+  a.w_in = w_in; a.w_out = w_out; a.status = status; a.ctas = p.ctas;
+  cudaError_t e;
+  if (p.mma) {
+    const umma::EncodeTiledFn enc = umma::encode_tiled_fn();
+    CUtensorMap tk, tv;
+    const auto encode = [&](CUtensorMap* t, const void* base, long long ps, long long hs, long long rs) {
+      const cuuint64_t dims[4] = {(cuuint64_t)s.d_qk, (cuuint64_t)m.page, (cuuint64_t)s.Hkv, (cuuint64_t)m.n_pages};
+      // a stride that is never applied (one KV head, one page) may be anything: the map gets one that it takes
+      const cuuint64_t strides[3] = {(cuuint64_t)rs * 2, s.Hkv > 1 ? (cuuint64_t)hs * 2 : (cuuint64_t)s.d_qk * 2,
+                                     m.n_pages > 1 ? (cuuint64_t)ps * 2 : (cuuint64_t)s.d_qk * 2};
+      const cuuint32_t box[4] = {64, (cuuint32_t)TR, 1, 1}, estr[4] = {1, 1, 1, 1};
+      return enc(t, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                 CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    };
+    if (!encode(&tk, k_pages, m.kp, m.kh, m.kr) || !encode(&tv, v_pages, m.vp, m.vh, m.vr)) return cudaErrorInvalidValue;
+    const bool two = p.gb > 8;
+    if (s.d_qk == 128) e = two ? launch_mma<128, 4, 2, 2, kMmaCtasWide>(a, tk, tv, st) : launch_mma<128, 4, 2, 1, kMmaCtas>(a, tk, tv, st);
+    else if (s.d_qk == 64) e = two ? launch_mma<64, 4, 4, 2, kMmaCtasWide>(a, tk, tv, st) : launch_mma<64, 4, 4, 1, kMmaCtas>(a, tk, tv, st);
+    else e = two ? launch_mma<256, 2, 2, 2, kMmaCtasWide>(a, tk, tv, st) : launch_mma<256, 2, 2, 1, kMmaCtas>(a, tk, tv, st);
+  } else if (dtype == SNAP_F32) {
+    e = s.d_qk > 128 || s.d_v > 128 ? launch_simt<float, 2>(a, st) : launch_simt<float, 1>(a, st);
+  } else {
+    e = s.d_qk > 128 || s.d_v > 128 ? launch_simt<__nv_bfloat16, 2>(a, st) : launch_simt<__nv_bfloat16, 1>(a, st);
+  }
+  if (e != cudaSuccess) return e;
+  const int chunks = (m.cap + JROWS - 1) / JROWS;
+  const dim3 grid((unsigned)(n_active * s.Hq + (w_out ? n_active * s.Hkv * chunks : 0)));
+  e = dtype == SNAP_F32 ? launch_pdl(paged_join_kernel<float>, grid, dim3(JNT), 0, st, a)
+                        : launch_pdl(paged_join_kernel<__nv_bfloat16>, grid, dim3(JNT), 0, st, a);
+  count_launch();
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+}  // namespace snap

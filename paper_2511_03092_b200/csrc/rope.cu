@@ -1,0 +1,223 @@
+// Rotary positions of queries and keys, and the same pass with the keys and values going to the pages of a
+// paged cache (snap_rope, snap_paged_append).
+//
+// Pair i of a head turns by the angle position * f_i: (a, b) -> m (a cos - b sin, b cos + a sin).  The angle and
+// its reduction modulo 2 pi are in double precision (at position 10^6 a single-precision angle is off by up to
+// 0.03), the sine and cosine of the reduced angle in single with the reduction's rounding put back to first
+// order, the rotation in single, and the result is rounded once.
+//
+// A pass reads and writes every element once and computes next to nothing, so memory bounds it.  A thread keeps
+// the cosines and sines of its V pairs (two 16-byte vectors of a head) in registers and walks over the heads of
+// its token with the loads of several heads in flight; the angles of a token are computed once, by the whole
+// block, and handed over in shared memory.  Threads are laid out as [tokens][heads][items of a head]: consecutive
+// threads are on consecutive vectors, and few tokens spread over more threads per token.
+#include "snap_internal.cuh"
+
+namespace snap {
+namespace {
+
+constexpr int NT = 256;
+constexpr int BATCH = 4;           // heads whose loads a thread has in flight
+
+template <int BYTES> struct RawOf;
+template <> struct RawOf<16> { using type = uint4; };
+template <> struct RawOf<8> { using type = uint2; };
+template <> struct RawOf<4> { using type = unsigned; };
+template <> struct RawOf<2> { using type = unsigned short; };
+
+template <typename T, int V> union Vec {
+  typename RawOf<V * (int)sizeof(T)>::type raw;
+  T e[V];
+  __device__ Vec() {}
+};
+
+struct RopeLaunch { RopeArgs a; int nj, nc, X, Y, Z; };   // items and copied vectors of a head; thread layout
+
+// cos and sin of position * f
+__device__ __forceinline__ float2 cos_sin(int pos, double f) {
+  const double angle = (double)pos * f;
+  const double n = rint(angle * 0.15915494309189535);                    // 1 / (2 pi)
+  double r = fma(-n, 6.283185307179586, angle);                          // 2 pi in two parts
+  r = fma(-n, 2.4492935982947064e-16, r);
+  const float rh = (float)r, rl = (float)(r - (double)rh);
+  float s, c;
+  sincosf(rh, &s, &c);
+  return make_float2(fmaf(-rl, s, c), fmaf(rl, c, s));
+}
+
+template <typename T, int V>
+__global__ void __launch_bounds__(NT) rope_kernel(const __grid_constant__ RopeLaunch L) {
+  using VT = Vec<T, V>;
+  using Raw = decltype(VT::raw);
+  const RopeArgs& a = L.a;
+  extern __shared__ float2 table[];                                      // [Z][rot / 2]
+  __shared__ int dup[NT];
+  const int tid = threadIdx.x, x = tid % L.X, y = (tid / L.X) % L.Y, z = tid / (L.X * L.Y);
+  const int t = blockIdx.x * L.Z + z, half = a.rot / 2;
+  const bool mine = z < L.Z && t < a.n_tokens;                            // the block may have spare threads
+  const bool paged = a.k_pages != nullptr;
+  if (tid < L.Z) dup[tid] = 0;
+  pdl_wait();
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+  // ---- where the token goes ----
+  bool skip = !mine;
+  int slot = 0, row = 0, page = 0, off = 0;
+  unsigned bad = 0;
+  if (mine && paged) {
+    slot = a.slots[t];
+    if (slot < 0 || slot >= a.max_seqs) {
+      skip = true;
+      bad = slot == -1 ? 0u : SNAP_DEV_BAD_SLOT;
+    } else {
+      row = a.rows ? a.rows[t] : a.seq_len[slot];
+      if (row < 0 || row >= a.map.cap) { skip = true; bad = SNAP_DEV_BAD_PAGE; }
+      else {
+        off = row % a.map.page;
+        page = a.map.table[(long long)slot * a.map.max_pages + row / a.map.page];
+        if (page < 0 || page >= a.map.n_pages) { skip = true; bad = SNAP_DEV_BAD_PAGE; }
+      }
+    }
+  }
+  __syncthreads();                                                        // dup is zero
+  if (paged && !a.rows && !skip)                                          // listed earlier in this call?
+    for (int e = tid - z * L.X * L.Y; e < t; e += L.X * L.Y)
+      if (a.slots[e] == slot) dup[z] = 1;
+
+  // ---- the angles of the block's tokens ----
+  for (int e = tid; e < L.Z * half; e += NT) {
+    const int ez = e / half, et = blockIdx.x * L.Z + ez, i = e - ez * half;
+    if (et >= a.n_tokens) break;
+    int pos = 0;
+    if (a.positions) pos = a.positions[et];
+    else if (a.rows) pos = a.rows[et];
+    else { const int es = a.slots[et]; if (es >= 0 && es < a.max_seqs) pos = a.seq_len[es]; }
+    const float2 cs = cos_sin(pos, a.freqs[i]);
+    table[e] = make_float2(cs.x * a.magnitude, cs.y * (a.magnitude * a.sign));
+  }
+  __syncthreads();                                                        // everyone has read seq_len
+  if (mine && paged && dup[z] && !skip) { skip = true; bad = SNAP_DEV_BAD_SLOT; }
+  if (mine && paged && x == 0 && y == 0) {
+    if (bad && a.status) atomicOr(a.status, bad);
+    if (!skip) {
+      if (a.rows) atomicMax(&a.seq_len[slot], row + 1);
+      else a.seq_len[slot] = row + 1;                                     // this token alone has the slot
+    }
+  }
+  if (skip) return;
+
+  const T* q = static_cast<const T*>(a.q) + t * a.q_tok;
+  const T* k = static_cast<const T*>(a.k) + t * a.k_tok;
+  T* qo = static_cast<T*>(a.q_out) + t * a.qo_tok;
+  T* ko = a.k_out ? static_cast<T*>(a.k_out) + t * a.ko_tok : nullptr;
+  T* kp = paged ? static_cast<T*>(a.k_pages) + page * a.map.kp + off * a.map.kr : nullptr;
+  const int H = a.Hq + a.Hkv;
+  const auto source = [&](int h) { return h < a.Hq ? q + h * a.q_head : k + (h - a.Hq) * a.k_head; };
+  const auto put = [&](int h, int at, Raw v) {
+    if (h < a.Hq) *reinterpret_cast<Raw*>(qo + h * a.qo_head + at) = v;
+    else {
+      if (ko) *reinterpret_cast<Raw*>(ko + (h - a.Hq) * a.ko_head + at) = v;
+      if (kp) *reinterpret_cast<Raw*>(kp + (h - a.Hq) * a.map.kh + at) = v;
+    }
+  };
+
+  // ---- values: copied to the page (first: these loads wait for nothing) ----
+  if (paged) {
+    const T* v = static_cast<const T*>(a.v) + t * a.v_tok;
+    T* vp = static_cast<T*>(a.v_pages) + page * a.map.vp + off * a.map.vr;
+    for (int h = y; h < a.Hkv; h += L.Y)
+      for (int c = x; c < a.d_v / V; c += L.X)
+        *reinterpret_cast<Raw*>(vp + h * a.map.vh + c * V) = *reinterpret_cast<const Raw*>(v + h * a.v_head + c * V);
+    if (a.weights && x == 0)
+      for (int h = y; h < a.Hkv; h += L.Y) a.weights[((long long)slot * a.Hkv + h) * a.map.cap + row] = 0.f;
+  }
+
+  // ---- rotated dims ----
+  for (int j = x; j < L.nj; j += L.X) {
+    float2 cs[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) cs[i] = table[z * half + j * V + i];
+    const int at_a = a.offset + (a.interleaved ? 2 * j * V : j * V), at_b = a.interleaved ? at_a + V : at_a + half;
+    for (int h0 = y; h0 < H; h0 += BATCH * L.Y) {
+      VT va[BATCH], vb[BATCH];
+#pragma unroll
+      for (int u = 0; u < BATCH; ++u) {
+        const int h = h0 + u * L.Y;
+        if (h < H) {
+          const T* s = source(h);
+          va[u].raw = *reinterpret_cast<const Raw*>(s + at_a);
+          vb[u].raw = *reinterpret_cast<const Raw*>(s + at_b);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < BATCH; ++u) {
+        const int h = h0 + u * L.Y;
+        if (h < H) {
+          VT oa, ob;
+#pragma unroll
+          for (int i = 0; i < V; ++i) {
+            // interleaved: the item's 2 V elements are V neighbouring pairs, else pair i is (va[i], vb[i])
+            const float p = to_f32<T>(a.interleaved ? (2 * i < V ? va[u].e[(2 * i) % V] : vb[u].e[(2 * i) % V]) : va[u].e[i]);
+            const float r = to_f32<T>(a.interleaved ? (2 * i + 1 < V ? va[u].e[(2 * i + 1) % V] : vb[u].e[(2 * i + 1) % V]) : vb[u].e[i]);
+            const T c0 = from_f32<T>(fmaf(p, cs[i].x, -(r * cs[i].y))), c1 = from_f32<T>(fmaf(r, cs[i].x, p * cs[i].y));
+            if (a.interleaved) {
+              if (2 * i < V) oa.e[(2 * i) % V] = c0; else ob.e[(2 * i) % V] = c0;
+              if (2 * i + 1 < V) oa.e[(2 * i + 1) % V] = c1; else ob.e[(2 * i + 1) % V] = c1;
+            } else {
+              oa.e[i] = c0;
+              ob.e[i] = c1;
+            }
+          }
+          put(h, at_a, oa.raw);
+          put(h, at_b, ob.raw);
+        }
+      }
+    }
+  }
+  // ---- the head's other dims ----
+  for (int c = x; c < L.nc; c += L.X) {
+    const int at = c * V < a.offset ? c * V : c * V + a.rot;
+    for (int h = y; h < H; h += L.Y) put(h, at, *reinterpret_cast<const Raw*>(source(h) + at));
+  }
+}
+
+template <typename T, int V>
+cudaError_t launch_v(const RopeArgs& a, int sms, cudaStream_t st) {
+  RopeLaunch L;
+  L.a = a;
+  const bool in_place = !a.k_pages && (!a.q || a.q == a.q_out) && (!a.k || a.k == a.k_out);
+  L.nj = a.rot / 2 / V;
+  L.nc = in_place ? 0 : (a.d_qk - a.rot) / V;
+  const int items = L.nj > 0 ? L.nj : L.nc;
+  L.X = items < 64 ? items : 64;
+  const int H = a.Hq + a.Hkv, per = NT / L.X;                             // (token, head) pairs of a block
+  // Many tokens: a thread takes about BATCH heads of its token, so that the angles it reads are used that often;
+  // few: as many threads per token as there are heads.
+  int Y = (long long)a.n_tokens * H / per >= 4LL * sms ? (H + BATCH - 1) / BATCH : H;
+  L.Y = Y < per ? Y : per;
+  L.Z = per / L.Y;
+  if (L.Z > a.n_tokens) L.Z = a.n_tokens;
+  const size_t smem = (size_t)L.Z * (a.rot / 2) * sizeof(float2);        // at most 2048 pairs: X covers them or Z is small
+  const cudaError_t e = launch_pdl(rope_kernel<T, V>, dim3((a.n_tokens + L.Z - 1) / L.Z), dim3(NT), smem, st, L);
+  count_launch();
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+}  // namespace
+
+// V: the widest vector (16 bytes at most) that neither the rotated part's start nor its half cuts.
+cudaError_t launch_rope(int dtype, const RopeArgs& a, cudaStream_t st) {
+  const int sms = sm_count();
+  const int g = a.rot ? (a.offset | (a.rot / 2)) : 16;
+  if (dtype == SNAP_F32) {
+    if (g % 4 == 0) return launch_v<float, 4>(a, sms, st);
+    if (g % 2 == 0) return launch_v<float, 2>(a, sms, st);
+    return launch_v<float, 1>(a, sms, st);
+  }
+  if (g % 8 == 0) return launch_v<__nv_bfloat16, 8>(a, sms, st);
+  if (g % 4 == 0) return launch_v<__nv_bfloat16, 4>(a, sms, st);
+  if (g % 2 == 0) return launch_v<__nv_bfloat16, 2>(a, sms, st);
+  return launch_v<__nv_bfloat16, 1>(a, sms, st);
+}
+
+}  // namespace snap

@@ -81,6 +81,18 @@ inline void count_launch() { ++g_launches; }
 // Current value of a process-wide testing / tuning option (SNAP_OPT_* of snapstream.h).
 int option(int which);
 
+// Shared by the host entry points (api.cu): the device's SM count, element size, validation and shape of a config.
+int sm_count();
+int elt_bytes(int dtype);
+int validate_config(const snap_config_t* c);
+Shape make_shape(const snap_config_t* c);
+inline size_t align_up(size_t x, size_t a = 256) { return (x + a - 1) / a * a; }
+// Every device buffer must start on a 16-byte boundary (the kernels use 16-byte accesses and bulk copies); a
+// pointer that does not is refused here rather than left to fault on the device.  NULL passes: optional
+// arguments are checked for presence separately.
+template <typename... P>
+bool misaligned(const P*... p) { return (((reinterpret_cast<uintptr_t>(p) & 15u) != 0) || ...); }
+
 // Body of snap_decode_attn with the scratch passed as a plain pointer (api.cu).
 int decode_step_with_scratch(const snap_config_t* cfg, const snap_layout_t* layout, const void* q_dev,
                              const void* k_new_dev, const void* v_new_dev, const int32_t* slot_ids_dev,
@@ -226,6 +238,45 @@ size_t decode_mla_stream_partial_floats(const Shape& s, int n_active, int nsplit
 cudaError_t launch_decode_mla_stream(const Shape& s, const void* q, const void* k_new, const int* slot_ids,
                                      int n_active, void* k_cache, int* seq_len, const int* valid_topk, void* out,
                                      float* partials, int nsplit, uint32_t* status, cudaStream_t st, int q_len = 1, int u = 0);
+
+// --- rotary positions and the paged cache (rope.cu, paged_decode.cu, paged_evict.cu; entry points in api_paged.cu) ---
+struct PageMap {                    // where row r of a slot lives; strides in elements
+  int page, n_pages, max_pages, cap;    // rows of a page; pages of the pool; entries of a table row; page * max_pages
+  long long kp, kh, kr, vp, vh, vr;
+  const int* table;
+};
+// One rotation pass over the heads of n_tokens tokens: queries, keys and (append only) values.
+struct RopeArgs {
+  const void* q; const void* k; const void* v;
+  void* q_out; void* k_out;
+  long long q_tok, q_head, qo_tok, qo_head, k_tok, k_head, ko_tok, ko_head, v_tok, v_head;   // elements
+  const double* freqs; const int* positions;
+  int n_tokens, Hq, Hkv, d_qk, d_v;
+  int rot, offset, interleaved;     // rot = 0: no rotation
+  float magnitude, sign;            // sign: -1 for the inverse
+  // append: k_pages non-NULL
+  void* k_pages; void* v_pages;
+  const int* slots; const int* rows; int* seq_len; float* weights;
+  int max_seqs;
+  PageMap map;
+  uint32_t* status;
+};
+cudaError_t launch_rope(int dtype, const RopeArgs& a, cudaStream_t st);
+
+struct PagedDecodePlan {
+  bool mma;
+  int ctas, gb, nhb;                // CTAs of the split kernel; heads of a unit, units per KV head
+  size_t prefix_off, ml_off, o_off, score_off, bytes;
+};
+int paged_decode_plan(int dtype, const Shape& s, const PageMap& m, int n_active, bool weights, int sms, PagedDecodePlan* p);
+cudaError_t launch_paged_decode(int dtype, const Shape& s, const PageMap& m, const PagedDecodePlan& p, const void* q,
+                                const int* slots, int n_active, const void* k_pages, const void* v_pages, const int* seq_len,
+                                const float* w_in, float* w_out, void* out, char* scratch, uint32_t* status, cudaStream_t st);
+
+size_t paged_evict_scratch_bytes(const Shape& s, int n_seqs);
+cudaError_t launch_paged_evict(int dtype, const Shape& s, const PageMap& m, const int* src, const int* dst, int n_seqs,
+                               void* k_pages, void* v_pages, int* seq_len, const float* w_in, float* w_out, int* kept,
+                               char* scratch, uint32_t* status, cudaStream_t st);
 
 // Checked indexing for the debugging build (-DSNAP_DEBUG_BOUNDS): a data-dependent index that falls
 // outside [0, n) raises SNAP_DEV_INDEX_CHECK in the status word and the access is skipped -- nothing
