@@ -387,41 +387,54 @@ def snap_decode_attn_blocks(cfg: SnapConfig, layout: SnapLayout, q, k_new, v_new
 
 
 # --- rotary positions and the paged cache ---
+# These calls check their tensors here: the library sees addresses only.  A serving step makes them many times, so each
+# call tests its tensors with plain expressions and only a failed test goes through _refuse, which finds the words.
 _DTYPES = {SNAP_F32: torch.float32, SNAP_BF16: torch.bfloat16}
+_I32, _F32, _F64 = torch.int32, torch.float32, torch.float64
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _expect(where: str, *named) -> Optional[int]:
-    """The tensors of a call: (name, tensor or None, dtype, shape or None, dense).  They have to be what the library is
-    told they are, and on one device.  Returns that device."""
-    device = None
+def _dense(t, dtype, shape, device) -> bool:
+    return t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == device
+
+
+def _rows(t, dtype, shape, device) -> bool:
+    """Any strides, the last dim dense."""
+    return t.dtype is dtype and t.shape == shape and t.stride()[-1] == 1 and t.get_device() == device
+
+
+def _refuse(where: str, device: int, *named) -> None:
+    """Raise for the first of (name, tensor or None, dtype, shape or None, dense) that is not what the call is told it is."""
     for name, t, dtype, shape, dense in named:
         if t is None:
             continue
-        if t.dtype != dtype:
+        if dtype is not None and t.dtype != dtype:
             raise ValueError(f"{where}: {name} is {t.dtype}, expected {dtype}")
-        if shape is not None and tuple(t.shape) != shape:
-            raise ValueError(f"{where}: {name} has shape {tuple(t.shape)}, expected {shape}")
+        if shape is not None and tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{where}: {name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
         if dense and not t.is_contiguous():
             raise ValueError(f"{where}: {name} must be dense")
-        if not dense and t.dim() > 1 and t.shape[-1] > 1 and t.stride(-1) != 1:
+        if not dense and t.stride()[-1] != 1:
             raise ValueError(f"{where}: {name} needs a dense last dim")
-        at = t.get_device() if t.is_cuda else -1
-        if device is None:
-            device = at
-        elif at != device:
-            raise ValueError(f"{where}: {name} is on device {at}, not {device}")
-    if device is not None and device < 0:
+    for name, t, *_ in named:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"{where}: {name} is on device {t.get_device()}, not {device}")
+    raise ValueError(f"{where}: the pages' strides are not those of the description")
+
+
+def _launch_stream(where: str, device: int, stream) -> int:
+    """The stream's handle; the tensors' device has to be the current one (the library launches there)."""
+    if device < 0:
         raise ValueError(f"{where}: the tensors are not on a CUDA device")
-    return device
-
-
-def _current(where: str, device: Optional[int]) -> None:
-    if device is not None and device != torch.cuda.current_device():
+    if device != torch.cuda.current_device():
         raise ValueError(f"{where}: the tensors are on device {device}, the current device is {torch.cuda.current_device()}")
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(device)
+    return _stream(stream)
 
 
 def _strides(t: Optional[torch.Tensor]):
-    return (0, 0) if t is None else (t.stride(0), t.stride(1))
+    return (0, 0) if t is None else t.stride()[:2]
 
 
 def make_rope(*, rot_dim: int, rot_offset: int = 0, interleaved: bool = False, scaling="plain", base: float = 10000.0,
@@ -445,14 +458,16 @@ def snap_rope(cfg: SnapConfig, rope: SnapRope, freqs, positions, q=None, k=None,
     """Rotate q [T, Hq, d] and / or k [T, Hkv, d] (any strides with a dense last dim) into q_out and k_out, which may be
     the inputs themselves.  freqs: float64 [rot_dim / 2], positions: int32 [T], on the device.  inverse: by minus the
     angle (the gradient's direction)."""
-    where, dt, n = "snap_rope", _DTYPES.get(cfg.dtype), positions.shape[0]
-    sq, sk = (n, cfg.n_q_heads, cfg.d_qk), (n, cfg.n_kv_heads, cfg.d_qk)
-    _current(where, _expect(where, ("freqs", freqs, torch.float64, (rope.rot_dim // 2,), True),
-                            ("positions", positions, torch.int32, (n,), True), ("q", q, dt, sq, False), ("k", k, dt, sk, False),
-                            ("q_out", q_out, dt, sq, False), ("k_out", k_out, dt, sk, False)))
-    _check(lib().snap_rope(C.byref(cfg), C.byref(rope), _ptr(freqs), _ptr(positions), n, _ptr(q), *_strides(q), _ptr(q_out),
-                           *_strides(q_out), _ptr(k), *_strides(k), _ptr(k_out), *_strides(k_out), int(bool(inverse)),
-                           _stream(stream)), where)
+    where, dt, n, dev = "snap_rope", _DTYPES.get(cfg.dtype), positions.shape[0], positions.get_device()
+    sq, sk, sf = (n, cfg.n_q_heads, cfg.d_qk), (n, cfg.n_kv_heads, cfg.d_qk), (rope.rot_dim // 2,)
+    if not (_dense(freqs, _F64, sf, dev) and _dense(positions, _I32, (n,), dev) and
+            (q is None or _rows(q, dt, sq, dev)) and (q_out is None or _rows(q_out, dt, sq, dev)) and
+            (k is None or _rows(k, dt, sk, dev)) and (k_out is None or _rows(k_out, dt, sk, dev))):
+        _refuse(where, dev, ("freqs", freqs, _F64, sf, True), ("positions", positions, _I32, (n,), True), ("q", q, dt, sq, False),
+                ("k", k, dt, sk, False), ("q_out", q_out, dt, sq, False), ("k_out", k_out, dt, sk, False))
+    _check(lib().snap_rope(C.byref(cfg), C.byref(rope), freqs.data_ptr(), positions.data_ptr(), n, _ptr(q), *_strides(q), _ptr(q_out),
+                           *_strides(q_out), _ptr(k), *_strides(k), _ptr(k_out), *_strides(k_out), 1 if inverse else 0,
+                           _launch_stream(where, dev, stream)), where)
 
 
 def make_paged(k_pages, v_pages, page_table) -> SnapPaged:
@@ -465,19 +480,25 @@ def make_paged(k_pages, v_pages, page_table) -> SnapPaged:
     return SnapPaged(k_pages.shape[2], k_pages.shape[0], page_table.shape[1], 0, kp, kh, kr, vp, vh, vr)
 
 
-def _expect_paged(where, cfg, paged, k_pages, v_pages, page_table, seq_len, workspace, status, more) -> None:
-    dt, head = _DTYPES.get(cfg.dtype), (paged.n_pages, cfg.n_kv_heads, paged.page_tokens)
-    weights = (cfg.max_seqs, cfg.n_kv_heads, paged.max_pages * paged.page_tokens)
-    named = [("k_pages", k_pages, dt, head + (cfg.d_qk,), False), ("v_pages", v_pages, dt, head + (cfg.d_v,), False),
-             ("page_table", page_table, torch.int32, (cfg.max_seqs, paged.max_pages), True),
-             ("seq_len", seq_len, torch.int32, (cfg.max_seqs,), True), ("status", status, torch.int32, None, True)]
-    if workspace is not None:
-        named.append(("workspace", workspace, workspace.dtype, None, True))
-    named += [(name, t, dtype, weights if shape == "weights" else shape, dense) for name, t, dtype, shape, dense in more]
-    _current(where, _expect(where, *named))
-    if (k_pages.stride()[:3] != (paged.k_page_stride, paged.k_head_stride, paged.k_row_stride) or
-            v_pages.stride()[:3] != (paged.v_page_stride, paged.v_head_stride, paged.v_row_stride)):
-        raise ValueError(f"{where}: the pages' strides are not those of the description")
+def _paged_ok(cfg, paged, dt, dev, k_pages, v_pages, page_table, seq_len, status) -> bool:
+    pages, heads, rows = paged.n_pages, cfg.n_kv_heads, paged.page_tokens
+    return (k_pages.dtype is dt and v_pages.dtype is dt and k_pages.shape == (pages, heads, rows, cfg.d_qk) and
+            v_pages.shape == (pages, heads, rows, cfg.d_v) and v_pages.get_device() == dev and
+            k_pages.stride() == (paged.k_page_stride, paged.k_head_stride, paged.k_row_stride, 1) and
+            v_pages.stride() == (paged.v_page_stride, paged.v_head_stride, paged.v_row_stride, 1) and
+            _dense(page_table, _I32, (cfg.max_seqs, paged.max_pages), dev) and _dense(seq_len, _I32, (cfg.max_seqs,), dev) and
+            (status is None or _dense(status, _I32, status.shape, dev)))
+
+
+def _paged_named(cfg, paged, dt, k_pages, v_pages, page_table, seq_len, status):
+    head = (paged.n_pages, cfg.n_kv_heads, paged.page_tokens)
+    return (("k_pages", k_pages, dt, head + (cfg.d_qk,), False), ("v_pages", v_pages, dt, head + (cfg.d_v,), False),
+            ("page_table", page_table, _I32, (cfg.max_seqs, paged.max_pages), True), ("seq_len", seq_len, _I32, (cfg.max_seqs,), True),
+            ("status", status, _I32, None, True))
+
+
+def _weights_shape(cfg, paged):
+    return (cfg.max_seqs, cfg.n_kv_heads, paged.max_pages * paged.page_tokens)
 
 
 def snap_paged_append(cfg: SnapConfig, paged: SnapPaged, slot_ids_dev, rows_dev, k, v, k_pages, v_pages, page_table, seq_len,
@@ -485,19 +506,26 @@ def snap_paged_append(cfg: SnapConfig, paged: SnapPaged, slot_ids_dev, rows_dev,
                       status=None, stream=None) -> None:
     """Write the rows of k [T, Hkv, d_qk], v [T, Hkv, d_v] into the pages, rotated on the way when rope is given; rows_dev
     None: each token is its sequence's next row.  q -> q_out and k_out: the rotated queries and keys, dense."""
-    where, dt, n = "snap_paged_append", _DTYPES.get(cfg.dtype), slot_ids_dev.shape[0]
-    sq, sk, sv = (n, cfg.n_q_heads, cfg.d_qk), (n, cfg.n_kv_heads, cfg.d_qk), (n, cfg.n_kv_heads, cfg.d_v)
-    _expect_paged(where, cfg, paged, k_pages, v_pages, page_table, seq_len, None, status, [
-        ("slot_ids", slot_ids_dev, torch.int32, (n,), True), ("rows", rows_dev, torch.int32, (n,), True),
-        ("freqs", freqs, torch.float64, None if rope is None else (rope.rot_dim // 2,), True),
-        ("positions", positions, torch.int32, (n,), True), ("q", q, dt, sq, False), ("q_out", q_out, dt, sq, True),
-        ("k", k, dt, sk, False), ("k_out", k_out, dt, sk, True), ("v", v, dt, sv, False),
-        ("weights", weights, torch.float32, "weights", True)])
-    _check(lib().snap_paged_append(C.byref(cfg), C.byref(paged), _ptr(slot_ids_dev), _ptr(rows_dev), n,
+    where, dt, n, dev = "snap_paged_append", _DTYPES.get(cfg.dtype), slot_ids_dev.shape[0], k_pages.get_device()
+    hq, hkv, d, one = cfg.n_q_heads, cfg.n_kv_heads, cfg.d_qk, (n,)
+    sq, sk, sv = (n, hq, d), (n, hkv, d), (n, hkv, cfg.d_v)
+    sf = None if rope is None else (rope.rot_dim // 2,)
+    if not (_paged_ok(cfg, paged, dt, dev, k_pages, v_pages, page_table, seq_len, status) and _dense(slot_ids_dev, _I32, one, dev) and
+            _rows(k, dt, sk, dev) and _rows(v, dt, sv, dev) and (rows_dev is None or _dense(rows_dev, _I32, one, dev)) and
+            (rope is None or freqs is None or _dense(freqs, _F64, sf, dev)) and
+            (positions is None or _dense(positions, _I32, one, dev)) and (q is None or _rows(q, dt, sq, dev)) and
+            (q_out is None or _dense(q_out, dt, sq, dev)) and (k_out is None or _dense(k_out, dt, sk, dev)) and
+            (weights is None or _dense(weights, _F32, _weights_shape(cfg, paged), dev))):
+        _refuse(where, dev, ("slot_ids", slot_ids_dev, _I32, one, True), ("rows", rows_dev, _I32, one, True),
+                ("freqs", None if rope is None else freqs, _F64, sf, True), ("positions", positions, _I32, one, True),
+                ("q", q, dt, sq, False), ("q_out", q_out, dt, sq, True), ("k", k, dt, sk, False), ("k_out", k_out, dt, sk, True),
+                ("v", v, dt, sv, False), ("weights", weights, _F32, _weights_shape(cfg, paged), True),
+                *_paged_named(cfg, paged, dt, k_pages, v_pages, page_table, seq_len, status))
+    _check(lib().snap_paged_append(C.byref(cfg), C.byref(paged), slot_ids_dev.data_ptr(), _ptr(rows_dev), n,
                                    None if rope is None else C.byref(rope), _ptr(freqs), _ptr(positions), _ptr(q), *_strides(q),
-                                   _ptr(q_out), _ptr(k), *_strides(k), _ptr(k_out), _ptr(v), *_strides(v), _ptr(k_pages),
-                                   _ptr(v_pages), _ptr(page_table), _ptr(seq_len), _ptr(weights), _ptr(status), _stream(stream)),
-           where)
+                                   _ptr(q_out), k.data_ptr(), *k.stride()[:2], _ptr(k_out), v.data_ptr(), *v.stride()[:2],
+                                   k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), seq_len.data_ptr(), _ptr(weights),
+                                   _ptr(status), _launch_stream(where, dev, stream)), where)
 
 
 def snap_paged_decode_workspace_bytes(cfg: SnapConfig, paged: SnapPaged, n_active: int, with_weights: bool = False) -> int:
@@ -511,15 +539,21 @@ def snap_paged_decode_attn(cfg: SnapConfig, paged: SnapPaged, q, slot_ids_dev, n
                            seq_len, out, workspace, weights_in=None, weights_out=None, status=None, stream=None) -> None:
     """Attention of one token per sequence, q [n, Hq, d_qk] -> out [n, Hq, d_v], over the rows in its pages; weights_out
     [max_seqs, Hkv, max_pages * page_tokens] float32 receives weights_in (None = 0) plus the group's softmax weights."""
-    where, dt, n = "snap_paged_decode_attn", _DTYPES.get(cfg.dtype), int(n_active)
-    _expect_paged(where, cfg, paged, k_pages, v_pages, page_table, seq_len, workspace, status, [
-        ("q", q, dt, (n, cfg.n_q_heads, cfg.d_qk), True), ("out", out, dt, (n, cfg.n_q_heads, cfg.d_v), True),
-        ("slot_ids", slot_ids_dev, torch.int32, (n,), True), ("weights_in", weights_in, torch.float32, "weights", True),
-        ("weights_out", weights_out, torch.float32, "weights", True)])
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib().snap_paged_decode_attn(C.byref(cfg), C.byref(paged), _ptr(q), _ptr(slot_ids_dev), n, _ptr(k_pages), _ptr(v_pages),
-                                        _ptr(page_table), _ptr(seq_len), _ptr(weights_in), _ptr(weights_out), _ptr(out),
-                                        _ptr(workspace), ws_bytes, _ptr(status), _stream(stream)), where)
+    where, dt, n, dev = "snap_paged_decode_attn", _DTYPES.get(cfg.dtype), int(n_active), k_pages.get_device()
+    sq, so = (n, cfg.n_q_heads, cfg.d_qk), (n, cfg.n_q_heads, cfg.d_v)
+    if not (_paged_ok(cfg, paged, dt, dev, k_pages, v_pages, page_table, seq_len, status) and _dense(q, dt, sq, dev) and
+            _dense(out, dt, so, dev) and _dense(slot_ids_dev, _I32, (n,), dev) and
+            (weights_in is None or _dense(weights_in, _F32, _weights_shape(cfg, paged), dev)) and
+            (weights_out is None or _dense(weights_out, _F32, _weights_shape(cfg, paged), dev)) and
+            workspace.is_contiguous() and workspace.get_device() == dev):
+        _refuse(where, dev, ("q", q, dt, sq, True), ("out", out, dt, so, True), ("slot_ids", slot_ids_dev, _I32, (n,), True),
+                ("weights_in", weights_in, _F32, _weights_shape(cfg, paged), True),
+                ("weights_out", weights_out, _F32, _weights_shape(cfg, paged), True), ("workspace", workspace, None, None, True),
+                *_paged_named(cfg, paged, dt, k_pages, v_pages, page_table, seq_len, status))
+    _check(lib().snap_paged_decode_attn(C.byref(cfg), C.byref(paged), q.data_ptr(), slot_ids_dev.data_ptr(), n, k_pages.data_ptr(),
+                                        v_pages.data_ptr(), page_table.data_ptr(), seq_len.data_ptr(), _ptr(weights_in),
+                                        _ptr(weights_out), out.data_ptr(), workspace.data_ptr(), workspace.nbytes, _ptr(status),
+                                        _launch_stream(where, dev, stream)), where)
 
 
 def snap_paged_evict_workspace_bytes(cfg: SnapConfig, paged: SnapPaged, n_seqs: int) -> int:
@@ -533,13 +567,17 @@ def snap_paged_evict(cfg: SnapConfig, paged: SnapPaged, src_slots_dev, dst_slots
                      seq_len, weights_in, weights_out, workspace, kept_rows=None, status=None, stream=None) -> None:
     """Copy the rows that stay (sinks, the topk of the middle by weight, the recent ones) of each source slot to its
     destination slot's pages; kept_rows [n, Hkv, l_sink + topk + l_recent] int32 receives their source rows."""
-    where, n = "snap_paged_evict", int(n_seqs)
-    keep = cfg.l_sink + cfg.topk + cfg.l_recent
-    _expect_paged(where, cfg, paged, k_pages, v_pages, page_table, seq_len, workspace, status, [
-        ("src_slots", src_slots_dev, torch.int32, (n,), True), ("dst_slots", dst_slots_dev, torch.int32, (n,), True),
-        ("weights_in", weights_in, torch.float32, "weights", True), ("weights_out", weights_out, torch.float32, "weights", True),
-        ("kept_rows", kept_rows, torch.int32, (n, cfg.n_kv_heads, keep), True)])
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib().snap_paged_evict(C.byref(cfg), C.byref(paged), _ptr(src_slots_dev), _ptr(dst_slots_dev), n, _ptr(k_pages),
-                                  _ptr(v_pages), _ptr(page_table), _ptr(seq_len), _ptr(weights_in), _ptr(weights_out),
-                                  _ptr(kept_rows), _ptr(workspace), ws_bytes, _ptr(status), _stream(stream)), where)
+    where, dt, n, dev = "snap_paged_evict", _DTYPES.get(cfg.dtype), int(n_seqs), k_pages.get_device()
+    sk, sw = (n, cfg.n_kv_heads, cfg.l_sink + cfg.topk + cfg.l_recent), _weights_shape(cfg, paged)
+    if not (_paged_ok(cfg, paged, dt, dev, k_pages, v_pages, page_table, seq_len, status) and _dense(src_slots_dev, _I32, (n,), dev) and
+            _dense(dst_slots_dev, _I32, (n,), dev) and _dense(weights_in, _F32, sw, dev) and
+            (weights_out is None or _dense(weights_out, _F32, sw, dev)) and (kept_rows is None or _dense(kept_rows, _I32, sk, dev)) and
+            workspace.is_contiguous() and workspace.get_device() == dev):
+        _refuse(where, dev, ("src_slots", src_slots_dev, _I32, (n,), True), ("dst_slots", dst_slots_dev, _I32, (n,), True),
+                ("weights_in", weights_in, _F32, sw, True), ("weights_out", weights_out, _F32, sw, True),
+                ("kept_rows", kept_rows, _I32, sk, True), ("workspace", workspace, None, None, True),
+                *_paged_named(cfg, paged, dt, k_pages, v_pages, page_table, seq_len, status))
+    _check(lib().snap_paged_evict(C.byref(cfg), C.byref(paged), src_slots_dev.data_ptr(), dst_slots_dev.data_ptr(), n, k_pages.data_ptr(),
+                                  v_pages.data_ptr(), page_table.data_ptr(), seq_len.data_ptr(), weights_in.data_ptr(),
+                                  _ptr(weights_out), _ptr(kept_rows), workspace.data_ptr(), workspace.nbytes, _ptr(status),
+                                  _launch_stream(where, dev, stream)), where)

@@ -2,15 +2,16 @@
 // sinks, the topk rows of the middle with the largest weight and the last l_recent rows move, in order, to the
 // pages of another slot.
 //
-// Selection: a cluster of CTAs per (sequence, KV head), each with a slice of the middle's weights in shared
-// memory as order-preserving integers.  The topk-th largest is found by radix steps of 11 bits over the range
-// that the keys really span (weights of one layer lie within a few octaves, so the digits of the raw bit pattern
-// would fall into a handful of bins and the counting atomics would queue on them); each CTA counts its slice and
-// reads the others' counts through distributed shared memory.  Equal keys at the threshold go to the lower rows;
-// the chosen rows leave in ascending order by counting ranks per CTA, warp and lane (nothing depends on timing).
+// Selection: one CTA per (sequence, KV head), or a cluster of eight for very long middles, with its slice of the
+// middle's weights in shared memory as order-preserving integers.  The topk-th largest is found by radix steps of
+// 11 bits over the range that the keys really span (weights of one layer lie within a few octaves, so the digits
+// of the raw bit pattern would fall into a handful of bins and the counting atomics would queue on them); the CTAs
+// of a cluster read each other's counts through distributed shared memory.  Equal keys at the threshold go to the
+// lower rows; the chosen rows leave in ascending order by counting ranks per CTA, warp and lane (nothing depends on
+// timing).
 //
-// Copy: bound by HBM (each kept row read and written once).  A warp moves eight rows with all their loads in
-// flight; page numbers and source rows are looked up by one lane per row.
+// Copy: bound by HBM (each kept row read and written once).  A lane looks up one row's pages, then the warp moves
+// its rows with eight 16-byte loads per lane in flight.
 #include <cooperative_groups.h>
 
 #include "snap_internal.cuh"
@@ -20,7 +21,7 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int ENT = 512, NB = 2048, NB_BITS = 11;       // threads of a selection CTA, bins of a radix step
+constexpr int ENT = 1024, NB = 2048, NB_BITS = 11;      // threads of a selection CTA, bins of a radix step
 constexpr int MAX_KEYS = 45000;                          // keys of a slice that are kept in shared memory (180 KB)
 
 struct EvictArgs {
@@ -34,6 +35,7 @@ struct EvictArgs {
   int* kept;                           // NULL or [n][Hkv][Ls + K + Lr]
   char* kp; char* vp;
   int k_vecs, v_vecs, eb;              // 16-byte pieces of a row; bytes of an element
+  unsigned k_magic, v_magic;           // p / k_vecs = p * k_magic >> 20 for the pieces of a warp
   uint32_t* status;
   int keys_cap;                        // keys of a slice that fit the launch's shared memory (0: read from global every time)
 };
@@ -55,15 +57,19 @@ __device__ bool entry_ok(const EvictArgs& a, int i, int& src, int& dst) {
   return !__syncthreads_or(clash);
 }
 
+// CLUSTER: eight CTAs share a middle; otherwise one has it all and the cluster's barriers and reads fall away.
+template <bool CLUSTER>
 __global__ void __launch_bounds__(ENT) evict_select_kernel(const __grid_constant__ EvictArgs a) {
   extern __shared__ unsigned keys[];                     // [keys_cap]
   __shared__ __align__(16) int hist[2][NB];
-  __shared__ int warp_s[ENT / 32];
-  __shared__ unsigned s_lo, s_hi, s_red[2][ENT / 32];
+  __shared__ int warp_s[ENT / 32], warp_e[ENT / 32];
+  __shared__ unsigned s_red[2][ENT / 32], s_range[2];
   __shared__ int s_bin, s_above, s_in, s_cnt[2], s_len;
   cg::cluster_group cl = cg::this_cluster();
-  const int CL = (int)cl.num_blocks(), rank = (int)cl.block_rank();
+  const int CL = CLUSTER ? (int)cl.num_blocks() : 1, rank = CLUSTER ? (int)cl.block_rank() : 0;
+  const auto barrier = [&]() { if (CLUSTER) cl.sync(); else __syncthreads(); };
   const int kvh = blockIdx.y, i = blockIdx.z, tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+  for (int b = tid; b < 2 * NB; b += ENT) (&hist[0][0])[b] = 0;
   pdl_wait();
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   int src = 0, dst;
@@ -77,11 +83,11 @@ __global__ void __launch_bounds__(ENT) evict_select_kernel(const __grid_constant
       a.len[i] = s_len;
     }
   }
-  cl.sync();
-  const int len = *cl.map_shared_rank(&s_len, 0);
+  barrier();
+  const int len = CLUSTER ? *cl.map_shared_rank(&s_len, 0) : s_len;
   const int keep = a.Ls + a.K + a.Lr;
   if (len <= keep || a.K == 0) {                         // uniform over the cluster: nothing to select
-    cl.sync();                                           // (the length has been read everywhere)
+    if (CLUSTER) cl.sync();                              // (the length has been read everywhere)
     return;
   }
   const int m = len - a.Ls - a.Lr;                       // candidates: more than K
@@ -92,7 +98,7 @@ __global__ void __launch_bounds__(ENT) evict_select_kernel(const __grid_constant
 
   // ---- the range the keys span ----
   unsigned lo = 0xffffffffu, hi = 0u;
-#pragma unroll 4
+#pragma unroll 8
   for (int e = tid; e < mine; e += ENT) {
     const unsigned k = key_of(wt[e]);
     if (held) keys[e] = k;
@@ -102,20 +108,14 @@ __global__ void __launch_bounds__(ENT) evict_select_kernel(const __grid_constant
   lo = __reduce_min_sync(0xffffffffu, lo);
   hi = __reduce_max_sync(0xffffffffu, hi);
   if (lane == 0) { s_red[0][w] = lo; s_red[1][w] = hi; }
-  for (int b = tid; b < 2 * NB; b += ENT) (&hist[0][0])[b] = 0;
   __syncthreads();
-  if (w == 0) {
-    lo = lane < ENT / 32 ? s_red[0][lane] : 0xffffffffu;
-    hi = lane < ENT / 32 ? s_red[1][lane] : 0u;
-    lo = __reduce_min_sync(0xffffffffu, lo);
-    hi = __reduce_max_sync(0xffffffffu, hi);
-    if (lane == 0) { s_lo = lo; s_hi = hi; }
-  }
-  cl.sync();
-  lo = 0xffffffffu; hi = 0u;
-  for (int r = 0; r < CL; ++r) {
-    lo = min(lo, *cl.map_shared_rank(&s_lo, r));
-    hi = max(hi, *cl.map_shared_rank(&s_hi, r));
+  lo = __reduce_min_sync(0xffffffffu, s_red[0][lane]);   // 32 warps: every warp reduces them all
+  hi = __reduce_max_sync(0xffffffffu, s_red[1][lane]);
+  if (CLUSTER) {
+    if (tid == 0) { s_range[0] = lo; s_range[1] = hi; }
+    cl.sync();
+    lo = __reduce_min_sync(0xffffffffu, lane < CL ? cl.map_shared_rank(s_range, lane)[0] : 0xffffffffu);
+    hi = __reduce_max_sync(0xffffffffu, lane < CL ? cl.map_shared_rank(s_range, lane)[1] : 0u);
   }
 
   // ---- the K-th largest key: it lies in [base, base + 2^bits), `need` keys of that range are wanted ----
@@ -127,37 +127,41 @@ __global__ void __launch_bounds__(ENT) evict_select_kernel(const __grid_constant
     int* h = hist[step & 1];
     const int shift = max(bits - NB_BITS, 0);
     const unsigned span = bits == 32 ? 0xffffffffu : (1u << bits) - 1u;
+#pragma unroll 4
     for (int e = tid; e < mine; e += ENT) {
       const unsigned k = key(e);
       if (k >= base && k - base <= span) atomicAdd(&h[(k - base) >> shift], 1);
     }
-    cl.sync();                                           // every CTA's counts are there
-    // thread t has bins NB - 1 - 4 t and the three below: descending order over threads
+    barrier();                                           // every CTA's counts are there
+    // thread t has bins NB - 1 - 2 t and the one below: descending order over threads
     constexpr int BPT = NB / ENT;
-    int cnt[BPT], sum = 0;
+    static_assert(BPT == 2, "a thread reads its two bins as one int2");
+    int cnt[BPT] = {0, 0};
+    if (CLUSTER) {
 #pragma unroll
-    for (int b = 0; b < BPT; ++b) cnt[b] = 0;
-    for (int r = 0; r < CL; ++r) {
-      const int* hr = cl.map_shared_rank(h, r);
-      const int4 v = *reinterpret_cast<const int4*>(hr + NB - BPT * (tid + 1));
-      cnt[0] += v.w; cnt[1] += v.z; cnt[2] += v.y; cnt[3] += v.x;
+      for (int r = 0; r < 8; ++r)
+        if (r < CL) {
+          const int2 v = *reinterpret_cast<const int2*>(cl.map_shared_rank(h, r) + NB - BPT * (tid + 1));
+          cnt[0] += v.y; cnt[1] += v.x;
+        }
+    } else {
+      const int2 v = *reinterpret_cast<const int2*>(h + NB - BPT * (tid + 1));
+      cnt[0] = v.y; cnt[1] = v.x;
     }
-#pragma unroll
-    for (int b = 0; b < BPT; ++b) sum += cnt[b];
+    const int sum = cnt[0] + cnt[1];
     int incl = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) { const int x = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += x; }
     if (lane == 31) warp_s[w] = incl;
+    // the other buffer is free again: every CTA has read it before the barrier above
+    for (int b = tid; b < NB; b += ENT) hist[(step + 1) & 1][b] = 0;
     __syncthreads();
-    int above = incl - sum;
-    for (int x = 0; x < w; ++x) above += warp_s[x];
+    int above = incl - sum + __reduce_add_sync(0xffffffffu, lane < w ? warp_s[lane] : 0);
 #pragma unroll
     for (int b = 0; b < BPT; ++b) {
       if (above < need && above + cnt[b] >= need) { s_bin = NB - 1 - BPT * tid - b; s_above = above; s_in = cnt[b]; }   // one thread
       above += cnt[b];
     }
-    // the other buffer is free again: every CTA has read it before the barrier above
-    for (int b = tid; b < NB; b += ENT) hist[(step + 1) & 1][b] = 0;
     __syncthreads();
     base += (unsigned)s_bin << shift;
     need -= s_above;
@@ -170,6 +174,7 @@ __global__ void __launch_bounds__(ENT) evict_select_kernel(const __grid_constant
   // ---- emission in row order: counts per CTA, then per warp ----
   const int seg = ((mine + ENT / 32 - 1) / (ENT / 32) + 31) & ~31, e0 = min(w * seg, mine), e1 = min(e0 + seg, mine);
   int gt = 0, eq = 0;
+#pragma unroll 4
   for (int e = e0 + lane; e < e1; e += 32) {
     const unsigned k = key(e);
     const bool at = k >= base && k - base <= span;
@@ -179,15 +184,15 @@ __global__ void __launch_bounds__(ENT) evict_select_kernel(const __grid_constant
   gt = __reduce_add_sync(0xffffffffu, gt);
   eq = __reduce_add_sync(0xffffffffu, eq);
   __syncthreads();                                       // warp_s has been read
-  if (lane == 0) { warp_s[w] = gt; s_red[0][w] = (unsigned)eq; }
+  if (lane == 0) { warp_s[w] = gt; warp_e[w] = eq; }
   __syncthreads();
-  int gt_before = 0, eq_before = 0;
-  for (int x = 0; x < w; ++x) { gt_before += warp_s[x]; eq_before += (int)s_red[0][x]; }
-  if (tid == ENT - 1) { s_cnt[0] = gt_before + gt; s_cnt[1] = eq_before + eq; }
-  cl.sync();
-  for (int r = 0; r < rank; ++r) {
-    gt_before += *cl.map_shared_rank(&s_cnt[0], r);
-    eq_before += *cl.map_shared_rank(&s_cnt[1], r);
+  int gt_before = __reduce_add_sync(0xffffffffu, lane < w ? warp_s[lane] : 0);
+  int eq_before = __reduce_add_sync(0xffffffffu, lane < w ? warp_e[lane] : 0);
+  if (CLUSTER) {
+    if (tid == ENT - 1) { s_cnt[0] = gt_before + gt; s_cnt[1] = eq_before + eq; }
+    cl.sync();
+    gt_before += __reduce_add_sync(0xffffffffu, lane < rank ? cl.map_shared_rank(s_cnt, lane)[0] : 0);
+    eq_before += __reduce_add_sync(0xffffffffu, lane < rank ? cl.map_shared_rank(s_cnt, lane)[1] : 0);
   }
   int* out = a.idx + ((long long)i * a.Hkv + kvh) * a.K;
   const unsigned below = (1u << lane) - 1u;
@@ -201,23 +206,25 @@ __global__ void __launch_bounds__(ENT) evict_select_kernel(const __grid_constant
     gt_before += __popc(m_gt);
     eq_before += __popc(m_eq);
   }
-  cl.sync();                                             // no CTA leaves while another may read its counts
+  if (CLUSTER) cl.sync();                                // no CTA leaves while another may read its counts
 }
 
-constexpr int CNT = 256, CROWS = 8, CTA_ROWS = CNT / 32 * CROWS;      // rows of a warp, of a CTA
+constexpr int CNT = 256;                                 // threads of a copy CTA
 
-// grid (row groups, KV heads, sequences)
-__global__ void __launch_bounds__(CNT) evict_copy_kernel(const __grid_constant__ EvictArgs a) {
+// grid (row groups, KV heads, sequences); a warp moves CROWS rows.  SAME: keys and values are laid out alike, so that one
+// offset serves both.
+template <int CROWS, bool SAME>
+__global__ void __launch_bounds__(CNT, 4) evict_copy_kernel(const __grid_constant__ EvictArgs a) {
+  const int kvh = blockIdx.y, i = blockIdx.z, lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  const int keep = a.Ls + a.K + a.Lr, r0 = (blockIdx.x * (CNT / 32) + w) * CROWS;
   pdl_wait();
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const int kvh = blockIdx.y, i = blockIdx.z, lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  const int len = a.len[i], keep = a.Ls + a.K + a.Lr, rows = len < keep ? len : keep;
-  const int r0 = (blockIdx.x * (CNT / 32) + w) * CROWS;
   if (r0 >= keep) return;
+  const int len = a.len[i], rows = len < keep ? len : keep;
   const int src = len >= 0 ? a.src[i] : 0, dst = len >= 0 ? a.dst[i] : 0;
   if (len >= 0 && kvh == 0 && blockIdx.x == 0 && threadIdx.x == 0) a.seq_len[dst] = rows;
-  // lane l < CROWS: row r0 + l of the destination
-  long long ks = -1, vs = 0, kd = 0, vd = 0;             // byte offsets; ks < 0: nothing to copy
+  // lane l < CROWS: row r0 + l of the destination; byte offsets of its source and destination, ks < 0: nothing to copy
+  long long ks = -1, kd = 0, vs = 0, vd = 0;
   if (lane < CROWS) {
     const int r = r0 + lane;
     int from = -1;
@@ -237,8 +244,8 @@ __global__ void __launch_bounds__(CNT) evict_copy_kernel(const __grid_constant__
       } else {
         const int so = from - sp * a.map.page, dof = r - dp * a.map.page;
         ks = (s_page * a.map.kp + kvh * a.map.kh + so * a.map.kr) * a.eb;
-        vs = (s_page * a.map.vp + kvh * a.map.vh + so * a.map.vr) * a.eb;
         kd = (d_page * a.map.kp + kvh * a.map.kh + dof * a.map.kr) * a.eb;
+        vs = (s_page * a.map.vp + kvh * a.map.vh + so * a.map.vr) * a.eb;
         vd = (d_page * a.map.vp + kvh * a.map.vh + dof * a.map.vr) * a.eb;
         if (a.w_out) {
           const long long b = (long long)kvh * a.map.cap, per = (long long)a.Hkv * a.map.cap;
@@ -247,29 +254,41 @@ __global__ void __launch_bounds__(CNT) evict_copy_kernel(const __grid_constant__
       }
     }
   }
-  // rows of 16-byte pieces, key pieces then value pieces of a row; U pieces per lane in flight
-  constexpr int U = 8;
-  const int vecs = a.k_vecs + a.v_vecs, total = CROWS * vecs;
-  for (int b = 0; b < total; b += 32 * U) {
-    uint4 x[U];
-    char* to[U];
+  // the rows' 16-byte pieces, U per lane and tensor in flight
+  const auto move = [&](int vecs, unsigned magic, long long s_off, long long d_off, char* p0, char* p1) {
+    constexpr int U = 4;
+    for (int b = 0; b < CROWS * vecs; b += 32 * U) {
+      uint4 x[U], y[SAME ? U : 1];
+      long long to[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int p = b + 32 * u + lane, row = p / vecs, c = p - row * vecs;
-      const int from = row < CROWS ? row : 0;
-      const long long s_k = __shfl_sync(0xffffffffu, ks, from), s_v = __shfl_sync(0xffffffffu, vs, from);
-      const long long d_k = __shfl_sync(0xffffffffu, kd, from), d_v = __shfl_sync(0xffffffffu, vd, from);
-      to[u] = nullptr;
-      if (row < CROWS && s_k >= 0) {
-        const bool isk = c < a.k_vecs;
-        x[u] = *reinterpret_cast<const uint4*>(isk ? a.kp + s_k + 16 * c : a.vp + s_v + 16 * (c - a.k_vecs));
-        to[u] = isk ? a.kp + d_k + 16 * c : a.vp + d_v + 16 * (c - a.k_vecs);
+      for (int u = 0; u < U; ++u) {
+        const unsigned p = b + 32 * u + lane, row = p * magic >> 20, c = p - row * vecs;
+        const int from = row < CROWS ? (int)row : 0;
+        const long long s = __shfl_sync(0xffffffffu, s_off, from), d = __shfl_sync(0xffffffffu, d_off, from);
+        to[u] = row < CROWS && s >= 0 ? d + 16 * c : -1;
+        if (to[u] >= 0) {
+          x[u] = *reinterpret_cast<const uint4*>(p0 + s + 16 * c);
+          if (SAME) y[SAME ? u : 0] = *reinterpret_cast<const uint4*>(p1 + s + 16 * c);
+        }
       }
-    }
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (to[u]) *reinterpret_cast<uint4*>(to[u]) = x[u];
-  }
+      for (int u = 0; u < U; ++u)
+        if (to[u] >= 0) {
+          *reinterpret_cast<uint4*>(p0 + to[u]) = x[u];
+          if (SAME) *reinterpret_cast<uint4*>(p1 + to[u]) = y[SAME ? u : 0];
+        }
+    }
+  };
+  move(a.k_vecs, a.k_magic, ks, kd, a.kp, a.vp);
+  if (!SAME) move(a.v_vecs, a.v_magic, ks < 0 ? -1 : vs, vd, a.vp, nullptr);
+}
+
+template <int CROWS>
+cudaError_t launch_copy(const EvictArgs& a, int keep, bool same, cudaStream_t st) {
+  constexpr int per = CNT / 32 * CROWS;
+  const dim3 grid((keep + per - 1) / per, a.Hkv, a.n);
+  return same ? launch_pdl(evict_copy_kernel<CROWS, true>, grid, dim3(CNT), 0, st, a)
+              : launch_pdl(evict_copy_kernel<CROWS, false>, grid, dim3(CNT), 0, st, a);
 }
 
 }  // namespace
@@ -289,33 +308,43 @@ cudaError_t launch_paged_evict(int dtype, const Shape& s, const PageMap& m, cons
   a.kp = static_cast<char*>(k_pages); a.vp = static_cast<char*>(v_pages);
   a.eb = elt_bytes(dtype);
   a.k_vecs = s.d_qk * a.eb / 16; a.v_vecs = s.d_v * a.eb / 16;
-  // A short middle fits one CTA; longer ones are cut over eight.
+  a.k_magic = ((1u << 20) + a.k_vecs - 1) / a.k_vecs;       // exact below 2^20 / vecs: a warp has 32 rows of 64 pieces at most
+  a.v_magic = ((1u << 20) + a.v_vecs - 1) / a.v_vecs;
   const int most = m.cap - s.Ls - s.Lr;                    // candidates there can be
-  const int CL = most <= 4096 ? 1 : 8;
-  const int per = most > 0 ? (most + CL - 1) / CL : 0;
+  const bool cluster = most > MAX_KEYS;
+  const int CL = cluster ? 8 : 1, per = most > 0 ? (most + CL - 1) / CL : 0;
   a.keys_cap = per <= MAX_KEYS ? per : 0;
   const size_t smem = (size_t)a.keys_cap * sizeof(unsigned);
-  static SmemLimit limit = {};
-  cudaError_t e = ensure_dyn_smem(evict_select_kernel, smem < 1024 ? 1024 : smem, limit);
-  if (e != cudaSuccess) return e;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = (unsigned)CL;
-  attr[1].val.clusterDim.y = 1;
-  attr[1].val.clusterDim.z = 1;
-  cudaLaunchConfig_t lc = {};
-  lc.gridDim = dim3(CL, s.Hkv, n_seqs);
-  lc.blockDim = dim3(ENT);
-  lc.dynamicSmemBytes = smem;
-  lc.stream = st;
-  lc.attrs = attr;
-  lc.numAttrs = 2;
-  e = cudaLaunchKernelEx(&lc, evict_select_kernel, a);
+  cudaError_t e;
+  if (cluster) {
+    static SmemLimit limit = {};
+    if ((e = ensure_dyn_smem(evict_select_kernel<true>, smem < 1024 ? 1024 : smem, limit)) != cudaSuccess) return e;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)CL;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t lc = {};
+    lc.gridDim = dim3(CL, s.Hkv, n_seqs);
+    lc.blockDim = dim3(ENT);
+    lc.dynamicSmemBytes = smem;
+    lc.stream = st;
+    lc.attrs = attr;
+    lc.numAttrs = 2;
+    e = cudaLaunchKernelEx(&lc, evict_select_kernel<true>, a);
+  } else {
+    static SmemLimit limit = {};
+    if ((e = ensure_dyn_smem(evict_select_kernel<false>, smem < 1024 ? 1024 : smem, limit)) != cudaSuccess) return e;
+    e = launch_pdl(evict_select_kernel<false>, dim3(1, s.Hkv, n_seqs), dim3(ENT), smem, st, a);
+  }
   count_launch();
   if (e != cudaSuccess) return e;
-  e = launch_pdl(evict_copy_kernel, dim3((s.Sc + CTA_ROWS - 1) / CTA_ROWS, s.Hkv, n_seqs), dim3(CNT), 0, st, a);
+  const bool same = m.kp == m.vp && m.kh == m.vh && m.kr == m.vr && a.k_vecs == a.v_vecs;
+  // Many rows: 32 per warp, so that a warp's look-ups serve four batches of loads; few: 8, to have more warps.
+  const bool many = (long long)n_seqs * s.Hkv * s.Sc >= 2048LL * sm_count();
+  e = many ? launch_copy<32>(a, s.Sc, same, st) : launch_copy<8>(a, s.Sc, same, st);
   count_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
 }

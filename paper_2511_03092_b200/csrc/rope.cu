@@ -2,9 +2,9 @@
 // paged cache (snap_rope, snap_paged_append).
 //
 // Pair i of a head turns by the angle position * f_i: (a, b) -> m (a cos - b sin, b cos + a sin).  The angle and
-// its reduction modulo 2 pi are in double precision (at position 10^6 a single-precision angle is off by up to
-// 0.03), the sine and cosine of the reduced angle in single with the reduction's rounding put back to first
-// order, the rotation in single, and the result is rounded once.
+// its reduction to one turn are in double precision (at position 10^6 a single-precision angle is off by up to
+// 0.03), the sine and cosine of the reduced angle in single with its rounding to single put back to first order,
+// the rotation in single, and the result is rounded once.
 //
 // A pass reads and writes every element once and computes next to nothing, so memory bounds it.  A thread keeps
 // the cosines and sines of its V pairs (two 16-byte vectors of a head) in registers and walks over the heads of
@@ -17,7 +17,7 @@ namespace snap {
 namespace {
 
 constexpr int NT = 256;
-constexpr int BATCH = 4;           // heads whose loads a thread has in flight
+constexpr int BATCH = 2;           // heads whose loads a thread has in flight
 
 template <int BYTES> struct RawOf;
 template <> struct RawOf<16> { using type = uint4; };
@@ -33,20 +33,18 @@ template <typename T, int V> union Vec {
 
 struct RopeLaunch { RopeArgs a; int nj, nc, X, Y, Z; };   // items and copied vectors of a head; thread layout
 
-// cos and sin of position * f
+// cos and sin of position * f, the angle taken in half turns: its whole turns come off exactly
 __device__ __forceinline__ float2 cos_sin(int pos, double f) {
-  const double angle = (double)pos * f;
-  const double n = rint(angle * 0.15915494309189535);                    // 1 / (2 pi)
-  double r = fma(-n, 6.283185307179586, angle);                          // 2 pi in two parts
-  r = fma(-n, 2.4492935982947064e-16, r);
-  const float rh = (float)r, rl = (float)(r - (double)rh);
+  const double u = (double)pos * f * 0.3183098861837907;                 // 1 / pi
+  const double r = fma(-2.0, rint(0.5 * u), u);                          // [-1, 1]
+  const float rh = (float)r, rl = (float)(r - (double)rh) * 3.14159265f;
   float s, c;
-  sincosf(rh, &s, &c);
+  sincospif(rh, &s, &c);
   return make_float2(fmaf(-rl, s, c), fmaf(rl, c, s));
 }
 
-template <typename T, int V>
-__global__ void __launch_bounds__(NT) rope_kernel(const __grid_constant__ RopeLaunch L) {
+template <typename T, int V, bool INTER>
+__global__ void __launch_bounds__(NT, 4) rope_kernel(const __grid_constant__ RopeLaunch L) {
   using VT = Vec<T, V>;
   using Raw = decltype(VT::raw);
   const RopeArgs& a = L.a;
@@ -84,6 +82,27 @@ __global__ void __launch_bounds__(NT) rope_kernel(const __grid_constant__ RopeLa
     for (int e = tid - z * L.X * L.Y; e < t; e += L.X * L.Y)
       if (a.slots[e] == slot) dup[z] = 1;
 
+  const T* q = static_cast<const T*>(a.q) + t * a.q_tok;
+  const T* k = static_cast<const T*>(a.k) + t * a.k_tok;
+  const int H = a.Hq + a.Hkv;
+  const auto source = [&](int h) { return h < a.Hq ? q + h * a.q_head : k + (h - a.Hq) * a.k_head; };
+  // item j of a head: its two vectors
+  const auto first_of = [&](int j) { return a.offset + (INTER ? 2 * j * V : j * V); };
+  const int to_second = INTER ? V : half;
+  VT va[BATCH], vb[BATCH];
+  const auto load = [&](int j, int h0) {
+#pragma unroll
+    for (int u = 0; u < BATCH; ++u) {
+      const int h = h0 + u * L.Y;
+      if (h < H) {
+        const T* s = source(h) + first_of(j);
+        va[u].raw = *reinterpret_cast<const Raw*>(s);
+        vb[u].raw = *reinterpret_cast<const Raw*>(s + to_second);
+      }
+    }
+  };
+  if (mine && x < L.nj) load(x, y);                                       // on their way while the angles are computed
+
   // ---- the angles of the block's tokens ----
   for (int e = tid; e < L.Z * half; e += NT) {
     const int ez = e / half, et = blockIdx.x * L.Z + ez, i = e - ez * half;
@@ -106,13 +125,9 @@ __global__ void __launch_bounds__(NT) rope_kernel(const __grid_constant__ RopeLa
   }
   if (skip) return;
 
-  const T* q = static_cast<const T*>(a.q) + t * a.q_tok;
-  const T* k = static_cast<const T*>(a.k) + t * a.k_tok;
   T* qo = static_cast<T*>(a.q_out) + t * a.qo_tok;
   T* ko = a.k_out ? static_cast<T*>(a.k_out) + t * a.ko_tok : nullptr;
   T* kp = paged ? static_cast<T*>(a.k_pages) + page * a.map.kp + off * a.map.kr : nullptr;
-  const int H = a.Hq + a.Hkv;
-  const auto source = [&](int h) { return h < a.Hq ? q + h * a.q_head : k + (h - a.Hq) * a.k_head; };
   const auto put = [&](int h, int at, Raw v) {
     if (h < a.Hq) *reinterpret_cast<Raw*>(qo + h * a.qo_head + at) = v;
     else {
@@ -121,34 +136,14 @@ __global__ void __launch_bounds__(NT) rope_kernel(const __grid_constant__ RopeLa
     }
   };
 
-  // ---- values: copied to the page (first: these loads wait for nothing) ----
-  if (paged) {
-    const T* v = static_cast<const T*>(a.v) + t * a.v_tok;
-    T* vp = static_cast<T*>(a.v_pages) + page * a.map.vp + off * a.map.vr;
-    for (int h = y; h < a.Hkv; h += L.Y)
-      for (int c = x; c < a.d_v / V; c += L.X)
-        *reinterpret_cast<Raw*>(vp + h * a.map.vh + c * V) = *reinterpret_cast<const Raw*>(v + h * a.v_head + c * V);
-    if (a.weights && x == 0)
-      for (int h = y; h < a.Hkv; h += L.Y) a.weights[((long long)slot * a.Hkv + h) * a.map.cap + row] = 0.f;
-  }
-
   // ---- rotated dims ----
   for (int j = x; j < L.nj; j += L.X) {
     float2 cs[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) cs[i] = table[z * half + j * V + i];
-    const int at_a = a.offset + (a.interleaved ? 2 * j * V : j * V), at_b = a.interleaved ? at_a + V : at_a + half;
+    const int at_a = first_of(j), at_b = at_a + to_second;
     for (int h0 = y; h0 < H; h0 += BATCH * L.Y) {
-      VT va[BATCH], vb[BATCH];
-#pragma unroll
-      for (int u = 0; u < BATCH; ++u) {
-        const int h = h0 + u * L.Y;
-        if (h < H) {
-          const T* s = source(h);
-          va[u].raw = *reinterpret_cast<const Raw*>(s + at_a);
-          vb[u].raw = *reinterpret_cast<const Raw*>(s + at_b);
-        }
-      }
+      if (j != x || h0 != y) load(j, h0);
 #pragma unroll
       for (int u = 0; u < BATCH; ++u) {
         const int h = h0 + u * L.Y;
@@ -157,10 +152,10 @@ __global__ void __launch_bounds__(NT) rope_kernel(const __grid_constant__ RopeLa
 #pragma unroll
           for (int i = 0; i < V; ++i) {
             // interleaved: the item's 2 V elements are V neighbouring pairs, else pair i is (va[i], vb[i])
-            const float p = to_f32<T>(a.interleaved ? (2 * i < V ? va[u].e[(2 * i) % V] : vb[u].e[(2 * i) % V]) : va[u].e[i]);
-            const float r = to_f32<T>(a.interleaved ? (2 * i + 1 < V ? va[u].e[(2 * i + 1) % V] : vb[u].e[(2 * i + 1) % V]) : vb[u].e[i]);
+            const float p = to_f32<T>(INTER ? (2 * i < V ? va[u].e[(2 * i) % V] : vb[u].e[(2 * i) % V]) : va[u].e[i]);
+            const float r = to_f32<T>(INTER ? (2 * i + 1 < V ? va[u].e[(2 * i + 1) % V] : vb[u].e[(2 * i + 1) % V]) : vb[u].e[i]);
             const T c0 = from_f32<T>(fmaf(p, cs[i].x, -(r * cs[i].y))), c1 = from_f32<T>(fmaf(r, cs[i].x, p * cs[i].y));
-            if (a.interleaved) {
+            if (INTER) {
               if (2 * i < V) oa.e[(2 * i) % V] = c0; else ob.e[(2 * i) % V] = c0;
               if (2 * i + 1 < V) oa.e[(2 * i + 1) % V] = c1; else ob.e[(2 * i + 1) % V] = c1;
             } else {
@@ -179,6 +174,16 @@ __global__ void __launch_bounds__(NT) rope_kernel(const __grid_constant__ RopeLa
     const int at = c * V < a.offset ? c * V : c * V + a.rot;
     for (int h = y; h < H; h += L.Y) put(h, at, *reinterpret_cast<const Raw*>(source(h) + at));
   }
+  // ---- values: copied to the page ----
+  if (paged) {
+    const T* v = static_cast<const T*>(a.v) + t * a.v_tok;
+    T* vp = static_cast<T*>(a.v_pages) + page * a.map.vp + off * a.map.vr;
+    for (int h = y; h < a.Hkv; h += L.Y)
+      for (int c = x; c < a.d_v / V; c += L.X)
+        *reinterpret_cast<Raw*>(vp + h * a.map.vh + c * V) = *reinterpret_cast<const Raw*>(v + h * a.v_head + c * V);
+    if (a.weights && x == 0)
+      for (int h = y; h < a.Hkv; h += L.Y) a.weights[((long long)slot * a.Hkv + h) * a.map.cap + row] = 0.f;
+  }
 }
 
 template <typename T, int V>
@@ -191,14 +196,22 @@ cudaError_t launch_v(const RopeArgs& a, int sms, cudaStream_t st) {
   const int items = L.nj > 0 ? L.nj : L.nc;
   L.X = items < 64 ? items : 64;
   const int H = a.Hq + a.Hkv, per = NT / L.X;                             // (token, head) pairs of a block
-  // Many tokens: a thread takes about BATCH heads of its token, so that the angles it reads are used that often;
-  // few: as many threads per token as there are heads.
-  int Y = (long long)a.n_tokens * H / per >= 4LL * sms ? (H + BATCH - 1) / BATCH : H;
-  L.Y = Y < per ? Y : per;
+  // Few tokens: as many threads per token as there are heads.  Many: a thread takes four to eight heads of its token, so
+  // that the angles it reads are used that often, in the split that leaves the fewest threads without one.
+  L.Y = H < per ? H : per;
+  if ((long long)a.n_tokens * H / per >= 4LL * sms) {
+    int best = 0;
+    for (int its = 8; its >= 4; --its) {
+      const int Y = (H + its - 1) / its, used = Y <= per ? per / Y * H * 64 / its : 0;   // head slots that do work
+      if (used > best) { best = used; L.Y = Y; }
+    }
+  }
   L.Z = per / L.Y;
   if (L.Z > a.n_tokens) L.Z = a.n_tokens;
   const size_t smem = (size_t)L.Z * (a.rot / 2) * sizeof(float2);        // at most 2048 pairs: X covers them or Z is small
-  const cudaError_t e = launch_pdl(rope_kernel<T, V>, dim3((a.n_tokens + L.Z - 1) / L.Z), dim3(NT), smem, st, L);
+  const dim3 grid((a.n_tokens + L.Z - 1) / L.Z);
+  const cudaError_t e = a.interleaved ? launch_pdl(rope_kernel<T, V, true>, grid, dim3(NT), smem, st, L)
+                                      : launch_pdl(rope_kernel<T, V, false>, grid, dim3(NT), smem, st, L);
   count_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
 }
