@@ -2,13 +2,13 @@
 //
 //     out[i][h] = sum_r p_r V_r / sum_r p_r,   p_r = exp(scale q.K_r - max),   r over the sequence's rows
 //
-// Every cache row is read once and serves the whole head group, so HBM bounds the call.  The rows of all
-// sequences are cut into tiles of 16; (sequence, KV head, head block) is a unit, and the tiles of all units in a
-// row form one line that is divided evenly between the CTAs: sequences of any lengths load the GPU evenly and the
-// host need not know the lengths.  A CTA walks over its stretch of the line, which holds whole units and at most
-// one cut one at either end.  A whole unit's output is written at once; a cut one leaves the sum, the maximum and
-// the unnormalised output of its piece, which the second launch joins in a fixed order (no atomics: equal inputs
-// give equal bits).
+// Every cache row is read once and serves the whole head group, so HBM bounds the call.  (sequence, KV head, head
+// block) is a unit; its rows are cut into tiles.  The units in a row form one line, each as long as its tiles plus a
+// fixed share for what a unit costs however short it is (its queries, its joining), and the line is divided evenly
+// between the CTAs: sequences of any lengths load the GPU evenly and the host need not know the lengths.  A CTA walks over
+// its stretch, which holds whole units and at most one cut one at either end; units of a few tiles are never cut.  A whole
+// unit's output is written at once; a cut one leaves the sum, the maximum and the unnormalised output of its piece,
+// which the second launch joins in a fixed order (no atomics: equal inputs give equal bits).
 //
 // Tensor-core kernel (bf16, heads of 64, 128 or 256, pages of a multiple of 16 rows): the group's heads are the N
 // side of mma.sync.m16n8k16, S^T = K tile . Q^T and O^T += V tile^T . P^T, so the cost of a row does not grow with
@@ -17,10 +17,10 @@
 // of the tile after next is fetched while a tile is computed.  The probabilities enter the second product as two bf16
 // numbers (p and what its rounding left), which keeps their rounding out of the result: 2^-17 instead of 2^-9.
 //
-// Portable kernel (fp32, other heads, pages of any size): a lane holds four dims of a row, a warp eight rows at a
-// time straight from global memory; the 8 x heads partial dot products are reduced by halving exchanges (after
-// which a lane owns one (row, head) pair: one shuffle per pair instead of five) and every lane does one
-// exponential.
+// Portable kernel (fp32, other heads, pages of any size): the same pipelines per warp over tiles of eight rows, brought in
+// by bulk copies (one per row, or one for all where they lie together); a lane holds four dims of a row; the 8 x heads
+// partial dot products are reduced by halving exchanges (after which a lane owns one (row, head) pair: one shuffle per
+// pair instead of five) and every lane does one exponential.
 //
 // With weights, the split kernel also stores the logits, and CTAs of the second launch turn them into the group's
 // attention weight of each row once the unit's maximum and sum are known.
@@ -39,8 +39,10 @@ using umma::mbar_init;
 using umma::mbar_try_wait;
 using umma::smem_u32;
 
-constexpr int TR = 16;                          // rows of a tile
-constexpr int MAX_CTAS = 1024;
+constexpr int TR = 16, STR = 8;                 // rows of a tile: tensor-core kernel, portable kernel
+constexpr int UNIT_TILES = 4;                   // what a unit costs besides its tiles, in tiles; units of at most that many stay whole
+constexpr int MIN_TILES = 4;                    // a CTA gets at least that much beyond one unit's share
+constexpr int MAX_CTAS = 1024, MAX_HELD = 128;  // sequences whose slot and length a CTA keeps in shared memory
 constexpr unsigned kPagedWaitLimit = 1u << 22;
 
 struct PagedArgs {
@@ -50,66 +52,95 @@ struct PagedArgs {
   int n, Hq, Hkv, g, gb, nhb, U, d_qk, d_v, max_seqs;    // U = Hkv * nhb units per sequence, gb heads each (the last block fewer)
   float scale_log2;
   PageMap map;
-  long long* prefix;                            // [n + 1] tiles of a unit before sequence i
+  int tr;                                       // rows of a tile
+  long long* prefix;                            // [n + 1]: the line before sequence i, per unit of a sequence
   float2* ml_unit;                              // [n * U][gb]: (max, sum), log2 domain, of units that one CTA did whole
-  float2* ml_part; float* o_part;               // [2 * CTAs][gb], [2 * CTAs][gb][d_v]: a CTA's first / last piece, if cut
+  float2* ml_part; float* o_part;               // [2 * CTAs][gb], [2 * CTAs][gb][d_v]: pieces of cut units; CTA c's is 2 c, or
+                                                // 2 c + 1 when it holds the unit's first tile (it has one of either at most)
   float* scores;                                // NULL, or [n * U][cap][gb] logits in the log2 domain
   const float* w_in; float* w_out;
   uint32_t* status;
   int ctas;
+  int stages, joined;                           // portable kernel: stages of a warp; 1, 2: a tile's key, value rows lie together
 };
 
 __device__ __forceinline__ int rows_of(const PagedArgs& a, int slot) {
   if (slot < 0 || slot >= a.max_seqs) return 0;
   return min(max(a.seq_len[slot], 0), a.map.cap);
 }
-__device__ __forceinline__ int tiles_of(int rows) { return (rows + TR - 1) / TR; }
+__device__ __forceinline__ int tiles_of(const PagedArgs& a, int rows) { return (rows + a.tr - 1) / a.tr; }
+__device__ __forceinline__ int length_of(int nt) { return nt > 0 ? nt + UNIT_TILES : 0; }           // on the line
+// Where tile t of a unit begins on the line, counted from the unit: the first tile carries the unit's share, and all
+// tiles of a short unit begin (and so stay) with the first.
+__device__ __forceinline__ int begin_of(int t, int nt) { return t == 0 || nt <= UNIT_TILES ? 0 : UNIT_TILES + t; }
 
-// CTAs that share W tiles (at least MIN_TILES each where there are that many CTAs), and who has tile t
-constexpr int MIN_TILES = 4;
+// CTAs that share a line of length W, where CTA c's stretch begins, and whose stretch position x lies in.  (32-bit
+// arithmetic where it suffices: 64-bit divisions are long instruction sequences.)
 __device__ __forceinline__ int active_ctas(long long W, int ctas) {
-  const long long n = (W + MIN_TILES - 1) / MIN_TILES;
-  return n < ctas ? (int)n : ctas;
+  if (W >= (long long)ctas * (MIN_TILES + UNIT_TILES)) return ctas;
+  return W > 0 ? max((int)W / (MIN_TILES + UNIT_TILES), 1) : 0;
 }
-__device__ __forceinline__ long long first_tile(long long W, int active, int c) { return W * c / active; }
-__device__ __forceinline__ int owner_of(long long t, long long W, int active) { return (int)(((t + 1) * active - 1) / W); }
+__device__ __forceinline__ long long stretch_begin(long long W, int active, int c) {
+  return W < (1 << 21) ? (long long)((unsigned)W * (unsigned)c / (unsigned)active) : W * c / active;
+}
+__device__ __forceinline__ int owner_of(long long x, long long W, int active) {
+  return W < (1 << 21) ? (int)((((unsigned)x + 1) * (unsigned)active - 1) / (unsigned)W) : (int)(((x + 1) * active - 1) / W);
+}
 
-// A place on the line of tiles.
-struct Place { int e, u, t, nt, slot, len; };   // sequence, unit, tile of the unit, tiles per unit, slot, rows
-__device__ __forceinline__ void load_entry(const PagedArgs& a, Place& p) {
-  if (p.e >= a.n) {                             // not reached unless another stream changes the lengths during the call
-    p.slot = -1; p.len = 0; p.nt = 1 << 30; p.e = a.n - 1;
+// Slots and lengths of the call's sequences, in shared memory when they fit.
+struct Held { int2 e[MAX_HELD]; };
+// A place on the line.  pos: where its unit begins, from the CTA's first unit on.
+struct Place { int e, u, t, nt, slot, len, pos; };   // sequence, unit, tile of the unit, tiles per unit, slot, rows
+__device__ __forceinline__ void load_entry(const PagedArgs& a, const Held& held, Place& p) {
+  if (p.e >= a.n) {                             // the end of the line
+    p.slot = -1; p.len = 0; p.nt = 1 << 29; p.e = a.n;
     return;
   }
-  p.slot = a.slots[p.e];
-  p.len = rows_of(a, p.slot);
-  p.nt = tiles_of(p.len);
+  if (a.n <= MAX_HELD) { const int2 v = held.e[p.e]; p.slot = v.x; p.len = v.y; }
+  else { p.slot = a.slots[p.e]; p.len = rows_of(a, p.slot); }
+  p.nt = tiles_of(a, p.len);
 }
-// `step` tiles on; the caller knows that the line reaches that far
-__device__ __forceinline__ void advance(const PagedArgs& a, Place& p, int step) {
+__device__ __forceinline__ void next_unit(const PagedArgs& a, const Held& held, Place& p) {
+  p.pos += length_of(p.nt);
+  if (++p.u == a.U) {
+    p.u = 0;
+    do { ++p.e; load_entry(a, held, p); } while (p.nt == 0);
+  }
+}
+// `step` tiles on, or (false) past `end`, the end of the CTA's stretch
+__device__ __forceinline__ bool advance(const PagedArgs& a, const Held& held, Place& p, int step, int end) {
   p.t += step;
   while (p.t >= p.nt) {
     p.t -= p.nt;
-    if (++p.u == a.U) {
-      p.u = 0;
-      do { ++p.e; load_entry(a, p); } while (p.nt == 0);
-    }
+    next_unit(a, held, p);
+    if (p.e >= a.n || p.pos >= end) return false;
   }
+  return p.pos + begin_of(p.t, p.nt) < end;
 }
 
-// All threads of the CTA: the CTA's stretch [x0, x1) of the line and the place of x0.  Returns false (to all) when it
-// is empty.  CTA 0 also writes the prefix array and reports bad slots and lengths.
+// All threads of the CTA: the place of its first tile and the end of its stretch (both counted from that tile's unit).
+// Returns false (to all) when it has none.  CTA 0 also writes the prefix array and reports bad slots and lengths.
 template <int NT>
-__device__ bool locate(const PagedArgs& a, long long& x0, long long& x1, Place& p, long long* scan /* shared, NT / 32 + 2 */) {
+__device__ bool locate(const PagedArgs& a, Place& p, int& end, Held& held, long long* scan /* shared, NT / 32 */) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, c = blockIdx.x;
   const int per = (a.n + NT - 1) / NT, e0 = min(tid * per, a.n), e1 = min(e0 + per, a.n);
+  __shared__ int s_e;
+  __shared__ long long s_before;
+  if (tid == 0) { s_e = 0; s_before = 0; }
   long long mine = 0;
   unsigned bad = 0;
   for (int e = e0; e < e1; ++e) {
     const int slot = a.slots[e];
-    mine += tiles_of(rows_of(a, slot));
-    if (slot < -1 || slot >= a.max_seqs) bad |= SNAP_DEV_BAD_SLOT;
-    else if (slot >= 0 && a.seq_len[slot] > a.map.cap) bad |= SNAP_DEV_BAD_PAGE;
+    int len = 0;
+    if (slot >= 0 && slot < a.max_seqs) {
+      len = a.seq_len[slot];
+      if (len > a.map.cap) { bad |= SNAP_DEV_BAD_PAGE; len = a.map.cap; }
+      len = max(len, 0);
+    } else if (slot != -1) {
+      bad |= SNAP_DEV_BAD_SLOT;
+    }
+    if (a.n <= MAX_HELD) held.e[e] = make_int2(slot, len);
+    mine += length_of(tiles_of(a, len));
   }
   long long incl = mine;
 #pragma unroll
@@ -119,36 +150,50 @@ __device__ bool locate(const PagedArgs& a, long long& x0, long long& x1, Place& 
   long long before = incl - mine, total = 0;
 #pragma unroll
   for (int w = 0; w < NT / 32; ++w) { const long long v = scan[w]; total += v; if (w < warp) before += v; }
+  const auto entry_length = [&](int e) {
+    return length_of(tiles_of(a, a.n <= MAX_HELD ? held.e[e].y : rows_of(a, a.slots[e])));
+  };
   if (c == 0) {
     long long at = before;
-    for (int e = e0; e < e1; ++e) { a.prefix[e] = at; at += tiles_of(rows_of(a, a.slots[e])); }
+    for (int e = e0; e < e1; ++e) { a.prefix[e] = at; at += entry_length(e); }
     if (tid == 0) a.prefix[a.n] = total;
     if (bad && a.status) atomicOr(a.status, bad);
   }
   const long long W = total * a.U;
   const int active = active_ctas(W, a.ctas);
   if (c >= active) return false;
-  x0 = first_tile(W, active, c);
-  x1 = first_tile(W, active, c + 1);
-  __shared__ int s_e;
-  __shared__ long long s_before;
-  if (tid == 0) { s_e = 0; s_before = 0; }
-  __syncthreads();
+  const long long x0 = stretch_begin(W, active, c), x1 = stretch_begin(W, active, c + 1);
   if (x0 >= before * a.U && x0 < (before + mine) * a.U) {                 // exactly one thread
     for (int e = e0; e < e1; ++e) {
-      const int nt = tiles_of(rows_of(a, a.slots[e]));
-      if (x0 < (before + nt) * a.U) { s_e = e; s_before = before; break; }
-      before += nt;
+      const int len = entry_length(e);
+      if (x0 < (before + len) * a.U) { s_e = e; s_before = before; break; }
+      before += len;
     }
   }
   __syncthreads();
   p.e = s_e;
-  load_entry(a, p);
-  p.nt = max(p.nt, 1);                                                   // (as in load_entry: stays in bounds whatever the lengths do)
+  load_entry(a, held, p);
+  p.nt = max(p.nt, 1);                          // (only if another stream changes the lengths during the call: stay in bounds)
   const long long rel = x0 - s_before * a.U;
-  p.u = (int)min(rel / p.nt, (long long)a.U - 1);
-  p.t = (int)(rel - (long long)p.u * p.nt);
+  const int unit = length_of(p.nt);
+  p.u = (int)min(rel < (1LL << 31) ? (long long)((unsigned)rel / (unsigned)unit) : rel / unit, (long long)a.U - 1);
+  const int o = (int)(rel - (long long)p.u * unit);
+  // the first tile that begins at or after x0
+  p.t = o <= 0 ? 0 : p.nt <= UNIT_TILES ? p.nt : max(1, o - UNIT_TILES);
+  p.pos = 0;
+  end = (int)min(x1 - x0 + max(o, 0), (long long)(1 << 30));
+  if (p.t >= p.nt) {
+    p.t = 0;
+    next_unit(a, held, p);
+    end -= p.pos;
+    p.pos = 0;
+    if (p.e >= a.n || end <= 0) return false;
+  }
   return true;
+}
+// Tiles of the unit at p, from p.t on, that begin before the end of the stretch: the end of that range of tiles
+__device__ __forceinline__ int segment_end(const Place& p, int end) {
+  return p.nt <= UNIT_TILES ? p.nt : min(p.nt, max(end - p.pos - UNIT_TILES, 1));
 }
 
 // The CTA's joined result of a segment, [cols][ld] in shared memory, leaves for the output (a whole unit) or the
@@ -219,7 +264,8 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
   float* wl = wm + NWARP * NCOL;
   float* jm = wl + NWARP * NCOL;                                         // [NCOL] joined maxima, then sums
   float* jl = jm + NCOL;
-  __shared__ long long scan[S::NT / 32 + 2];
+  __shared__ long long scan[S::NT / 32];
+  __shared__ Held held;
 
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, gq = lane >> 2, tq = lane & 3;
   unsigned char* wstages = stages + w * NSTAGE * S::STAGE_B;
@@ -232,14 +278,14 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
   pdl_wait();
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-  long long x0, x1;
   Place at;
-  if (!locate<S::NT>(a, x0, x1, at, scan)) return;
-  const int total = (int)(x1 - x0);                                      // this CTA's tiles; warp w takes w, w + NWARP, ...
-  const int mine = total > w ? (total - w + NWARP - 1) / NWARP : 0;
+  int end;
+  if (!locate<S::NT>(a, at, end, held, scan)) return;
 
-  // ---- the warp's producer: runs NSTAGE tiles ahead of the consumer, over unit borders ----
+  // ---- the warp's producer: runs NSTAGE tiles ahead of the consumer, over unit borders; warp w takes the CTA's tiles
+  // w, w + NWARP, ... ----
   Place pr = at;
+  bool more = w == 0 || advance(a, held, pr, w, end);
   int pid = 0, n_issued = 0;
   unsigned bad_stage = 0;                                                // bit s: the tile in stage s is on a bad page
   const int tpp = a.map.page / TR;
@@ -259,26 +305,25 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
       }
       if (bad && a.status) atomicOr(a.status, SNAP_DEV_BAD_PAGE);
     }
-    if (++n_issued < mine) { advance(a, pr, NWARP); fetch_pid(); }
+    ++n_issued;
+    more = advance(a, held, pr, NWARP, end);
+    if (more) fetch_pid();
   };
-  if (mine > 0) {
-    if (w > 0) advance(a, pr, w);
-    fetch_pid();
-    for (int s = 0; s < NSTAGE && n_issued < mine; ++s) issue();
-  }
+  if (more) fetch_pid();
+  for (int s = 0; s < NSTAGE && more; ++s) issue();
 
   // ldmatrix lane roles: K (plain): row (lane & 7) + 8 * bit3, chunk + bit4; V (transposed): row (lane & 7) + 8 * bit4, chunk + bit3
   const int k_row = (lane & 7) + ((lane >> 3) & 1) * 8, k_cadd = lane >> 4;
   const int v_row = (lane & 7) + ((lane >> 4) & 1) * 8, v_cadd = (lane >> 3) & 1;
 
   bool dead = false;                                                     // a bounded wait ran out: nothing more is read
-  int n = 0, seg0 = 0;                                                   // tiles done by this warp; the segment's first tile
+  int n = 0, done = 0;                                                   // tiles done by this warp; by the CTA before this segment
   const __nv_bfloat16* q_all = static_cast<const __nv_bfloat16*>(a.q);
-  while (seg0 < total) {
-    // ---- a segment: the CTA's tiles of one unit ----
-    const int seg1 = min(total, seg0 + at.nt - at.t);
+  while (true) {
+    // ---- a segment: the CTA's tiles [at.t, tb) of one unit ----
+    const int tb = segment_end(at, end), cnt = tb - at.t;
     const int kvh = at.u / a.nhb, hb = at.u - kvh * a.nhb, nh = min(a.gb, a.g - hb * a.gb);
-    const bool whole = at.t == 0 && seg1 - seg0 == at.nt;
+    const bool whole = cnt == at.nt;
     uint32_t qb[NG][KS][2];                                              // B fragments of Q^T: column 8 gi + gq, dims 16 ks + 2 tq (+8)
 #pragma unroll
     for (int gi = 0; gi < NG; ++gi) {
@@ -302,11 +347,11 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
     }
     float* srow = a.scores ? a.scores + ((long long)at.e * a.U + at.u) * a.map.cap * a.gb : nullptr;
 
-    for (; n < mine && w + n * NWARP < seg1 && !dead; ++n) {
+    for (; w + n * NWARP < done + cnt && !dead; ++n) {
       const int s = n % NSTAGE;
       const bool landed = wait_bounded(bar0 + 8 * s, (unsigned)(n / NSTAGE) & 1u);
       if (__any_sync(0xffffffffu, !landed)) { dead = true; break; }
-      const int row0 = (at.t + (w + n * NWARP - seg0)) * TR;
+      const int row0 = (at.t + (w + n * NWARP - done)) * TR;
       const int nrows = (bad_stage >> s) & 1u ? 0 : min(at.len - row0, TR);
       const uint32_t sK = stage0 + s * S::STAGE_B, sV = sK + S::TENS_B;
       if (nrows < TR) {
@@ -399,7 +444,7 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
         }
       }
       __syncwarp();
-      if (n_issued < mine) {
+      if (more) {
         // the stage was read, and possibly cleared, through the generic proxy; the copy that refills it is of the async proxy
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         issue();
@@ -471,10 +516,13 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
       exchange(buf, true);
     }
     __syncthreads();
-    write_segment<__nv_bfloat16, S::NT>(a, buf, LD, jm, jl, at.e, at.u, nh, whole, 2 * blockIdx.x + (seg0 > 0));
+    write_segment<__nv_bfloat16, S::NT>(a, buf, LD, jm, jl, at.e, at.u, nh, whole, 2 * blockIdx.x + (at.t == 0));
 
-    if (seg1 < total) advance(a, at, seg1 - seg0);
-    seg0 = seg1;
+    if (tb < at.nt) break;
+    done += cnt;
+    at.t = 0;
+    next_unit(a, held, at);
+    if (at.e >= a.n || at.pos >= end) break;
   }
   if (dead) {
     if (a.status) atomicOr(a.status, SNAP_DEV_WAIT_TIMEOUT);
@@ -485,81 +533,106 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
 // ---------------------------------------------------------------------------------------------------------------
 // portable kernel
 // ---------------------------------------------------------------------------------------------------------------
-template <typename T> struct Four;                // four consecutive elements as loaded
-template <> struct Four<float> {
-  float4 r;
-  __device__ __forceinline__ void load(const float* p) {
-    asm volatile("ld.global.L1::no_allocate.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(r.x), "=f"(r.y), "=f"(r.z), "=f"(r.w) : "l"(p));
-  }
-  __device__ __forceinline__ void zero() { r = make_float4(0.f, 0.f, 0.f, 0.f); }
-  __device__ __forceinline__ float4 f() const { return r; }
-};
-template <> struct Four<__nv_bfloat16> {
-  uint2 r;
-  __device__ __forceinline__ void load(const __nv_bfloat16* p) {
-    asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(r.x), "=r"(r.y) : "l"(p));
-  }
-  __device__ __forceinline__ void zero() { r = make_uint2(0u, 0u); }
-  __device__ __forceinline__ float4 f() const {
-    return make_float4(__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xffff0000u), __uint_as_float(r.y << 16),
-                       __uint_as_float(r.y & 0xffff0000u));
-  }
-};
+template <typename T> __device__ __forceinline__ float4 four(const T* p);      // four consecutive elements
+template <> __device__ __forceinline__ float4 four<float>(const float* p) { return *reinterpret_cast<const float4*>(p); }
+template <> __device__ __forceinline__ float4 four<__nv_bfloat16>(const __nv_bfloat16* p) {
+  const uint2 r = *reinterpret_cast<const uint2*>(p);
+  return make_float4(__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xffff0000u), __uint_as_float(r.y << 16),
+                     __uint_as_float(r.y & 0xffff0000u));
+}
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, unsigned bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
 
 constexpr int SNW = 4, SNT = SNW * 32;            // warps and threads of a CTA
+constexpr int MAX_STAGES = 6;                     // of a warp
 
 // NV: 128-dim chunks of a row, HB: heads of a unit (a power of two)
 template <typename T, int NV, int HB, int CTAS>
 __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_constant__ PagedArgs a) {
   constexpr int LD = 128 * NV + 4;
-  constexpr int NVAL = 8 * HB, VPL = NVAL > 32 ? NVAL / 32 : 1;          // (row, head) values of eight rows; per lane after the exchange
+  constexpr int NVAL = 8 * HB, VPL = NVAL > 32 ? NVAL / 32 : 1;          // (row, head) values of a tile; per lane after the exchange
+  extern __shared__ __align__(128) unsigned char stages[];               // [SNW][a.stages][8 key rows | 8 value rows]
   __shared__ __align__(16) float buf[2 * HB * LD];
   __shared__ float wm[SNW * HB], wl[SNW * HB], jm[HB], jl[HB];
-  __shared__ long long scan[SNT / 32 + 2];
+  __shared__ uint64_t bars[SNW * MAX_STAGES];
+  __shared__ long long scan[SNT / 32];
+  __shared__ Held held;
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+  const unsigned krow_b = a.d_qk * sizeof(T), vrow_b = a.d_v * sizeof(T), stage_b = STR * (krow_b + vrow_b);
+  const unsigned char* wstages = stages + w * a.stages * stage_b;
+  const uint32_t stage0 = smem_u32(wstages), bar0 = smem_u32(bars + w * MAX_STAGES);
+  if (lane == 0) {
+    for (int s = 0; s < a.stages; ++s) mbar_init(bar0 + 8 * s, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncwarp();
   pdl_wait();
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  long long x0, x1;
   Place at;
-  if (!locate<SNT>(a, x0, x1, at, scan)) return;
-  const int total = (int)(x1 - x0), mine = total > w ? (total - w + SNW - 1) / SNW : 0;
-  // After the exchange lane l owns row l / 4 of the eight and head (or heads) head_of(l & 3, k).
+  int end;
+  if (!locate<SNT>(a, at, end, held, scan)) return;
+  // After the exchange lane l owns row l / 4 of the tile and head (or heads) my_head (+ 1).
   const int my_head = HB >= 8 ? 2 * (lane & 3) : HB == 4 ? (lane & 3) : HB == 2 ? ((lane & 3) >> 1) : 0;
-  const T* kbase = static_cast<const T*>(a.kp);
-  const T* vbase = static_cast<const T*>(a.vp);
 
-  // rows of the warp's next tile, a lane each: page number and row of the page
+  // ---- the warp's producer: lane r (< 8) looks up row r of the tile after the one being issued ----
   Place pr = at;
-  int pid = -1, prow = 0, ahead = 0;
+  bool more = w == 0 || advance(a, held, pr, w, end);
+  int pid = -1, prow = 0, s_in = 0, in_flight = 0;
+  unsigned long long okay_of = 0;                                        // 8 bits per stage: the rows that are there
   const auto fetch = [&]() {
-    const int row = pr.t * TR + (lane & 15);
+    const int row = pr.t * STR + (lane & 7);
     pid = -1;
     if (row < pr.len) {
       const int pg = row / a.map.page;
       prow = row - pg * a.map.page;
       pid = a.map.table[(long long)pr.slot * a.map.max_pages + pg];
-      if (pid < 0 || pid >= a.map.n_pages) { pid = -1; if (a.status) atomicOr(a.status, SNAP_DEV_BAD_PAGE); }
     }
   };
-  if (mine > 0) {
-    if (w > 0) advance(a, pr, w);
-    fetch();
-  }
-  int n = 0, seg0 = 0;
-  while (seg0 < total) {
-    const int seg1 = min(total, seg0 + at.nt - at.t);
+  const auto issue = [&]() {
+    if (pr.t * STR + (lane & 7) < pr.len && (pid < 0 || pid >= a.map.n_pages)) {
+      pid = -1;
+      if (lane < 8 && a.status) atomicOr(a.status, SNAP_DEV_BAD_PAGE);
+    }
+    const unsigned okay = __ballot_sync(0xffffffffu, pid >= 0) & 0xffu;
+    okay_of = (okay_of & ~(0xffull << (8 * s_in))) | ((unsigned long long)okay << (8 * s_in));
+    const uint32_t bar = bar0 + 8 * s_in, dst = stage0 + s_in * stage_b;
+    const int rows = __popc(okay), kvh = pr.u / a.nhb;
+    if (lane == 0) mbar_expect_tx(bar, rows * (krow_b + vrow_b));
+    __syncwarp();
+    if (pid >= 0) {
+      const T* ks = static_cast<const T*>(a.kp) + pid * a.map.kp + kvh * a.map.kh + prow * a.map.kr;
+      const T* vs = static_cast<const T*>(a.vp) + pid * a.map.vp + kvh * a.map.vh + prow * a.map.vr;
+      const uint32_t kd = dst + lane * krow_b, vd = dst + STR * krow_b + lane * vrow_b;
+      if (a.joined & 1) { if (lane == 0) bulk_load(kd, ks, rows * krow_b, bar); }
+      else if (lane < 8) bulk_load(kd, ks, krow_b, bar);
+      if (a.joined & 2) { if (lane == 0) bulk_load(vd, vs, rows * vrow_b, bar); }
+      else if (lane < 8) bulk_load(vd, vs, vrow_b, bar);
+    }
+    ++in_flight;
+    if (++s_in == a.stages) s_in = 0;
+    more = advance(a, held, pr, SNW, end);
+    if (more) fetch();
+  };
+  if (more) fetch();
+  for (int s = 0; s < a.stages && more; ++s) issue();
+
+  bool dead = false;                                                     // a bounded wait ran out: nothing more is read
+  int n = 0, done = 0, s_out = 0;
+  unsigned parity = 0;
+  while (true) {
+    const int tb = segment_end(at, end), cnt = tb - at.t;
     const int kvh = at.u / a.nhb, hb = at.u - kvh * a.nhb, nh = min(a.gb, a.g - hb * a.gb);
-    const bool whole = at.t == 0 && seg1 - seg0 == at.nt;
+    const bool whole = cnt == at.nt;
     float q[HB][NV][4], o[HB][NV][4], m_ref[VPL], l_part[VPL];
 #pragma unroll
     for (int h = 0; h < HB; ++h)
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
         const int d = 4 * lane + 128 * j;
-        Four<T> x;
-        x.zero();
-        if (h < nh && d < a.d_qk) x.load(static_cast<const T*>(a.q) + ((long long)at.e * a.Hq + kvh * a.g + hb * a.gb + h) * a.d_qk + d);
-        const float4 f = x.f();
+        float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (h < nh && d < a.d_qk) f = four<T>(static_cast<const T*>(a.q) + ((long long)at.e * a.Hq + kvh * a.g + hb * a.gb + h) * a.d_qk + d);
         q[h][j][0] = f.x; q[h][j][1] = f.y; q[h][j][2] = f.z; q[h][j][3] = f.w;
         o[h][j][0] = o[h][j][1] = o[h][j][2] = o[h][j][3] = 0.f;
       }
@@ -567,115 +640,109 @@ __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_cons
     for (int k = 0; k < VPL; ++k) { m_ref[k] = -INFINITY; l_part[k] = 0.f; }
     float* srow = a.scores ? a.scores + ((long long)at.e * a.U + at.u) * a.map.cap * a.gb : nullptr;
 
-    for (; n < mine && w + n * SNW < seg1; ++n) {
-      const int row0 = (at.t + (w + n * SNW - seg0)) * TR;
-      const int tpid = pid, tprow = prow;
-      if (++ahead < mine) { advance(a, pr, SNW); fetch(); }
-#pragma unroll 1
-      for (int r0 = 0; r0 < TR; r0 += 8) {
-        if (row0 + r0 >= at.len) break;
-        Four<T> kx[8][NV], vx[8][NV];
-        unsigned okay = 0;
+    for (; w + n * SNW < done + cnt && !dead; ++n) {
+      const bool landed = wait_bounded(bar0 + 8 * s_out, parity);
+      if (__any_sync(0xffffffffu, !landed)) { dead = true; break; }
+      --in_flight;
+      const int row0 = (at.t + (w + n * SNW - done)) * STR;
+      const unsigned okay = (unsigned)(okay_of >> (8 * s_out)) & 0xffu;
+      const T* kx = reinterpret_cast<const T*>(wstages + s_out * stage_b) + 4 * lane;
+      const T* vx = reinterpret_cast<const T*>(wstages + s_out * stage_b + STR * krow_b) + 4 * lane;
+      float s[NVAL];
 #pragma unroll
-        for (int r = 0; r < 8; ++r) {
-          const int p = __shfl_sync(0xffffffffu, tpid, r0 + r), x = __shfl_sync(0xffffffffu, tprow, r0 + r);
-          const T* kr = kbase + p * a.map.kp + kvh * a.map.kh + x * a.map.kr + 4 * lane;
-          const T* vr = vbase + p * a.map.vp + kvh * a.map.vh + x * a.map.vr + 4 * lane;
-          okay |= p >= 0 ? 1u << r : 0u;
+      for (int r = 0; r < 8; ++r) {
+        float4 f[NV];
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+          f[j] = 4 * lane + 128 * j < a.d_qk ? four<T>(kx + r * a.d_qk + 128 * j) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int h = 0; h < HB; ++h) {
+          float x = 0.f;
 #pragma unroll
           for (int j = 0; j < NV; ++j) {
-            kx[r][j].zero();
-            vx[r][j].zero();
-            if (p >= 0 && 4 * lane + 128 * j < a.d_qk) kx[r][j].load(kr + 128 * j);
-            if (p >= 0 && 4 * lane + 128 * j < a.d_v) vx[r][j].load(vr + 128 * j);
+            x = fmaf(f[j].x, q[h][j][0], x); x = fmaf(f[j].y, q[h][j][1], x);
+            x = fmaf(f[j].z, q[h][j][2], x); x = fmaf(f[j].w, q[h][j][3], x);
           }
+          s[r * HB + h] = x;
         }
-        float s[NVAL];
+      }
+      // halving exchange: each step sums over one lane bit and leaves a lane half of the values
+      int left = NVAL;
 #pragma unroll
-        for (int r = 0; r < 8; ++r)
+      for (int b = 16; b > 0; b >>= 1) {
+        if (left > 1) {
+          left >>= 1;
 #pragma unroll
-          for (int h = 0; h < HB; ++h) {
-            float x = 0.f;
-#pragma unroll
-            for (int j = 0; j < NV; ++j) {
-              const float4 f = kx[r][j].f();
-              x = fmaf(f.x, q[h][j][0], x); x = fmaf(f.y, q[h][j][1], x); x = fmaf(f.z, q[h][j][2], x); x = fmaf(f.w, q[h][j][3], x);
+          for (int x = 0; x < NVAL / 2; ++x)
+            if (x < left) {
+              const bool up = lane & b;
+              const float give = up ? s[x] : s[x + left], keep = up ? s[x + left] : s[x];
+              s[x] = keep + __shfl_xor_sync(0xffffffffu, give, b);
             }
-            s[r * HB + h] = x;
-          }
-        // halving exchange: each step sums over one lane bit and leaves a lane half of the values
-        int left = NVAL;
-#pragma unroll
-        for (int b = 16; b > 0; b >>= 1) {
-          if (left > 1) {
-            left >>= 1;
-#pragma unroll
-            for (int x = 0; x < NVAL / 2; ++x)
-              if (x < left) {
-                const bool up = lane & b;
-                const float give = up ? s[x] : s[x + left], keep = up ? s[x + left] : s[x];
-                s[x] = keep + __shfl_xor_sync(0xffffffffu, give, b);
-              }
-          } else {
-            s[0] += __shfl_xor_sync(0xffffffffu, s[0], b);
-          }
+        } else {
+          s[0] += __shfl_xor_sync(0xffffffffu, s[0], b);
         }
-        const int row = row0 + r0 + (lane >> 2);
-        const bool ok = (okay >> (lane >> 2)) & 1u;
-        float v[VPL];
-        bool refresh = false;
+      }
+      const int row = row0 + (lane >> 2);
+      const bool ok = (okay >> (lane >> 2)) & 1u;                        // rows that are not there hold anything
+      float v[VPL];
+      bool refresh = false;
+#pragma unroll
+      for (int k = 0; k < VPL; ++k) {
+        v[k] = ok ? s[k] * a.scale_log2 : -INFINITY;
+        refresh = refresh || v[k] > m_ref[k] + 8.f;
+      }
+      if (srow && row < at.len) {
+        // HB = 2 and 1: the pairs are held by two and four lanes, all writing the same value
+#pragma unroll
+        for (int k = 0; k < VPL; ++k)
+          if (my_head + k < nh) srow[(long long)row * a.gb + my_head + k] = v[k];
+      }
+      if (__any_sync(0xffffffffu, refresh)) {                            // the reference moves lazily, as in the kernel above
+        float al[VPL];
 #pragma unroll
         for (int k = 0; k < VPL; ++k) {
-          v[k] = ok ? s[k] * a.scale_log2 : -INFINITY;
-          refresh = refresh || v[k] > m_ref[k] + 8.f;
-        }
-        if (srow && row < at.len) {
-          // HB = 2 and 1: the pairs are held by two and four lanes, all writing the same value
+          float mx = v[k];
 #pragma unroll
-          for (int k = 0; k < VPL; ++k)
-            if (my_head + k < nh) srow[(long long)row * a.gb + my_head + k] = v[k];
-        }
-        if (__any_sync(0xffffffffu, refresh)) {
-          float al[VPL];
-#pragma unroll
-          for (int k = 0; k < VPL; ++k) {
-            float mx = v[k];
-#pragma unroll
-            for (int b = 4; b <= 16; b <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, b));
-            const float nm = fmaxf(m_ref[k], mx);
-            al[k] = m_ref[k] == -INFINITY ? 0.f : exp2f(m_ref[k] - nm);
-            m_ref[k] = nm;
-            l_part[k] *= al[k];
-          }
-#pragma unroll
-          for (int h = 0; h < HB; ++h) {
-            const float f = __shfl_sync(0xffffffffu, al[HB >= 8 ? (h & 1) : 0], HB >= 8 ? h / 2 : HB == 4 ? h : HB == 2 ? 2 * h : 0);
-#pragma unroll
-            for (int j = 0; j < NV; ++j) { o[h][j][0] *= f; o[h][j][1] *= f; o[h][j][2] *= f; o[h][j][3] *= f; }
-          }
-        }
-        float p[VPL];
-#pragma unroll
-        for (int k = 0; k < VPL; ++k) {
-          p[k] = fast_exp2(v[k] - (m_ref[k] == -INFINITY ? 0.f : m_ref[k]));
-          l_part[k] += p[k];
+          for (int b = 4; b <= 16; b <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, b));
+          const float nm = fmaxf(m_ref[k], mx);
+          al[k] = m_ref[k] == -INFINITY ? 0.f : exp2f(m_ref[k] - nm);
+          m_ref[k] = nm;
+          l_part[k] *= al[k];
         }
 #pragma unroll
-        for (int r = 0; r < 8; ++r) {
-          float4 f[NV];
+        for (int h = 0; h < HB; ++h) {
+          const float f = __shfl_sync(0xffffffffu, al[HB >= 8 ? (h & 1) : 0], HB >= 8 ? h / 2 : HB == 4 ? h : HB == 2 ? 2 * h : 0);
 #pragma unroll
-          for (int j = 0; j < NV; ++j) f[j] = vx[r][j].f();
+          for (int j = 0; j < NV; ++j) { o[h][j][0] *= f; o[h][j][1] *= f; o[h][j][2] *= f; o[h][j][3] *= f; }
+        }
+      }
+      float p[VPL];
 #pragma unroll
-          for (int h = 0; h < HB; ++h) {
-            const float pr_ = __shfl_sync(0xffffffffu, p[HB >= 8 ? (h & 1) : 0], 4 * r + (HB >= 8 ? h / 2 : HB == 4 ? h : HB == 2 ? 2 * h : 0));
+      for (int k = 0; k < VPL; ++k) {
+        p[k] = fast_exp2(v[k] - (m_ref[k] == -INFINITY ? 0.f : m_ref[k]));
+        l_part[k] += p[k];
+      }
 #pragma unroll
-            for (int j = 0; j < NV; ++j) {
-              o[h][j][0] = fmaf(pr_, f[j].x, o[h][j][0]); o[h][j][1] = fmaf(pr_, f[j].y, o[h][j][1]);
-              o[h][j][2] = fmaf(pr_, f[j].z, o[h][j][2]); o[h][j][3] = fmaf(pr_, f[j].w, o[h][j][3]);
-            }
+      for (int r = 0; r < 8; ++r) {
+        if (!((okay >> r) & 1u)) continue;                               // a zero probability does not silence a NaN
+        float4 f[NV];
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+          f[j] = 4 * lane + 128 * j < a.d_v ? four<T>(vx + r * a.d_v + 128 * j) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int h = 0; h < HB; ++h) {
+          const float x = __shfl_sync(0xffffffffu, p[HB >= 8 ? (h & 1) : 0], 4 * r + (HB >= 8 ? h / 2 : HB == 4 ? h : HB == 2 ? 2 * h : 0));
+#pragma unroll
+          for (int j = 0; j < NV; ++j) {
+            o[h][j][0] = fmaf(x, f[j].x, o[h][j][0]); o[h][j][1] = fmaf(x, f[j].y, o[h][j][1]);
+            o[h][j][2] = fmaf(x, f[j].z, o[h][j][2]); o[h][j][3] = fmaf(x, f[j].w, o[h][j][3]);
           }
         }
       }
+      if (++s_out == a.stages) { s_out = 0; parity ^= 1u; }
+      __syncwarp();                                                      // the stage has been read
+      if (more) issue();
     }
 
     // ---- join the warps ----
@@ -721,9 +788,19 @@ __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_cons
     __syncthreads();
     if (w == 0) { exchange(buf + HB * LD, false); exchange(buf, true); }
     __syncthreads();
-    write_segment<T, SNT>(a, buf, LD, jm, jl, at.e, at.u, nh, whole, 2 * blockIdx.x + (seg0 > 0));
-    if (seg1 < total) advance(a, at, seg1 - seg0);
-    seg0 = seg1;
+    write_segment<T, SNT>(a, buf, LD, jm, jl, at.e, at.u, nh, whole, 2 * blockIdx.x + (at.t == 0));
+    if (tb < at.nt) break;
+    done += cnt;
+    at.t = 0;
+    next_unit(a, held, at);
+    if (at.e >= a.n || at.pos >= end) break;
+  }
+  if (dead) {
+    if (a.status) atomicOr(a.status, SNAP_DEV_WAIT_TIMEOUT);
+    for (; in_flight > 0; --in_flight) {
+      (void)wait_bounded(bar0 + 8 * s_out, parity);
+      if (++s_out == a.stages) { s_out = 0; parity ^= 1u; }
+    }
   }
 }
 
@@ -732,17 +809,16 @@ __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_cons
 // ---------------------------------------------------------------------------------------------------------------
 constexpr int JNT = 256, JROWS = 4 * JNT;         // rows of a weights CTA
 
-struct Pieces { int np, c0, first; };              // pieces of a unit: index first, then 2 (c0 + k); np <= 1: done whole
-__device__ __forceinline__ Pieces pieces_of(const PagedArgs& a, int e, int u, int nt) {
+struct Pieces { int np, c0; };                     // pieces of a unit; np <= 1: done whole
+__device__ __forceinline__ Pieces pieces_of(const PagedArgs& a, int u, long long before, long long total, int nt) {
   Pieces p;
-  const long long W = a.prefix[a.n] * a.U, t0 = a.prefix[e] * a.U + (long long)u * nt;
+  const long long W = total * a.U, x = before * a.U + (long long)u * length_of(nt);
   const int active = active_ctas(W, a.ctas);
-  p.c0 = owner_of(t0, W, active);
-  p.np = owner_of(t0 + nt - 1, W, active) - p.c0 + 1;
-  p.first = 2 * p.c0 + (first_tile(W, active, p.c0) != t0);
+  p.c0 = owner_of(x, W, active);
+  p.np = owner_of(x + begin_of(nt - 1, nt), W, active) - p.c0 + 1;
   return p;
 }
-__device__ __forceinline__ int piece_at(const Pieces& p, int k) { return k == 0 ? p.first : 2 * (p.c0 + k); }
+__device__ __forceinline__ int piece_at(const Pieces& p, int k) { return 2 * (p.c0 + k) + (k == 0); }
 
 template <typename T>
 __global__ void __launch_bounds__(JNT) paged_join_kernel(const __grid_constant__ PagedArgs a) {
@@ -757,13 +833,14 @@ __global__ void __launch_bounds__(JNT) paged_join_kernel(const __grid_constant__
     // ---- one query head's output ----
     const int e = blockIdx.x / a.Hq, head = blockIdx.x - e * a.Hq;
     const int kvh = head / a.g, x = head - kvh * a.g, hb = x / a.gb, col = x - hb * a.gb;
-    const int nt = (int)(a.prefix[e + 1] - a.prefix[e]);
+    const long long before = a.prefix[e], line = a.prefix[a.n];
+    const int nt = max((int)(a.prefix[e + 1] - before) - UNIT_TILES, 0);
     T* out = static_cast<T*>(a.out) + (long long)blockIdx.x * a.d_v;
     if (nt == 0) {
       for (int c = tid; c < a.d_v; c += JNT) out[c] = from_f32<T>(0.f);
       return;
     }
-    const Pieces p = pieces_of(a, e, kvh * a.nhb + hb, nt);
+    const Pieces p = pieces_of(a, kvh * a.nhb + hb, before, line, nt);
     if (p.np <= 1) return;
     float m = -INFINITY;
     for (int k = tid; k < p.np; k += JNT) m = fmaxf(m, a.ml_part[(long long)piece_at(p, k) * a.gb + col].x);
@@ -819,8 +896,9 @@ __global__ void __launch_bounds__(JNT) paged_join_kernel(const __grid_constant__
   // ---- JROWS rows' weights of one (sequence, KV head) ----
   const int chunks = (a.map.cap + JROWS - 1) / JROWS;
   const int id = blockIdx.x - merges, chunk = id % chunks, kvh = (id / chunks) % a.Hkv, e = id / chunks / a.Hkv;
-  const int nt = (int)(a.prefix[e + 1] - a.prefix[e]);
-  if (chunk * JROWS >= nt * TR) return;
+  const long long before = a.prefix[e], line = a.prefix[a.n];
+  const int nt = max((int)(a.prefix[e + 1] - before) - UNIT_TILES, 0);
+  if (chunk * JROWS >= nt * a.tr) return;
   const int slot = a.slots[e];
   int again = 0;                                                         // the slot was listed before: its first entry counts
   for (int x = tid; x < e; x += JNT) again |= a.slots[x] == slot;
@@ -832,7 +910,7 @@ __global__ void __launch_bounds__(JNT) paged_join_kernel(const __grid_constant__
   float sum[4] = {0.f, 0.f, 0.f, 0.f};
   for (int hb = 0; hb < a.nhb; ++hb) {
     const int u = kvh * a.nhb + hb, nh = min(a.gb, a.g - hb * a.gb);
-    const Pieces p = pieces_of(a, e, u, nt);
+    const Pieces p = pieces_of(a, u, before, line, nt);
     __syncthreads();                                                     // mu_s of the block before has been read
     for (int col = w; col < nh; col += JNT / 32) {
       float m = -INFINITY, l = 0.f;
@@ -896,18 +974,29 @@ cudaError_t launch_mma(const PagedArgs& a, const CUtensorMap& tk, const CUtensor
 
 // CTAs per SM that the kernels are built for (launch bounds, and the shared memory of the tensor-core ones)
 constexpr int kMmaCtas = 3, kMmaCtasWide = 2;
-constexpr int simt_ctas(bool wide, int gb) { return wide ? 2 : gb <= 2 ? 4 : 3; }
+constexpr int simt_ctas(bool wide, int gb) { return wide ? 2 : gb <= 4 ? 3 : 2; }
+// Stages of a warp of the portable kernel: what the CTAs of an SM leave each other of its shared memory.
+int simt_stages(const Shape& s, int eb, int ctas) {
+  const int stage = STR * (s.d_qk + s.d_v) * eb, n = (210 * 1024 / ctas - 20 * 1024) / (SNW * stage);
+  return n < 2 ? 2 : n > MAX_STAGES ? MAX_STAGES : n;
+}
 
-template <typename T, int NV>
-cudaError_t launch_simt(const PagedArgs& a, cudaStream_t st) {
-  constexpr bool W = NV > 1;
-  cudaError_t e;
-  if (a.gb <= 1) e = launch_pdl(paged_simt_kernel<T, NV, 1, simt_ctas(W, 1)>, dim3(a.ctas), dim3(SNT), 0, st, a);
-  else if (a.gb <= 2) e = launch_pdl(paged_simt_kernel<T, NV, 2, simt_ctas(W, 2)>, dim3(a.ctas), dim3(SNT), 0, st, a);
-  else if (W || a.gb <= 4) e = launch_pdl(paged_simt_kernel<T, NV, 4, simt_ctas(W, 4)>, dim3(a.ctas), dim3(SNT), 0, st, a);
-  else e = launch_pdl(paged_simt_kernel<T, 1, 8, simt_ctas(false, 8)>, dim3(a.ctas), dim3(SNT), 0, st, a);
+template <typename T, int NV, int HB>
+cudaError_t launch_simt_hb(const PagedArgs& a, cudaStream_t st) {
+  constexpr int C = simt_ctas(NV > 1, HB);
+  static SmemLimit limit = {};
+  const size_t smem = (size_t)SNW * a.stages * STR * (a.d_qk + a.d_v) * sizeof(T);
+  if (cudaError_t e = ensure_dyn_smem(paged_simt_kernel<T, NV, HB, C>, smem, limit)) return e;
+  const cudaError_t e = launch_pdl(paged_simt_kernel<T, NV, HB, C>, dim3(a.ctas), dim3(SNT), smem, st, a);
   count_launch();
   return e;
+}
+template <typename T, int NV>
+cudaError_t launch_simt(const PagedArgs& a, cudaStream_t st) {
+  if (a.gb <= 1) return launch_simt_hb<T, NV, 1>(a, st);
+  if (a.gb <= 2) return launch_simt_hb<T, NV, 2>(a, st);
+  if (NV > 1 || a.gb <= 4) return launch_simt_hb<T, NV, 4>(a, st);
+  return launch_simt_hb<T, 1, 8>(a, st);
 }
 
 bool mma_shape(int dtype, const Shape& s, const PageMap& m) {
@@ -929,7 +1018,7 @@ int paged_decode_plan(int dtype, const Shape& s, const PageMap& m, int n_active,
   const long long chunks = (m.cap + JROWS - 1) / JROWS;
   // grid and index limits; a line of tiles and the scratch have to be countable
   if (units > (1LL << 30) || (long long)n_active * s.Hq + (weights ? (long long)n_active * s.Hkv * chunks : 0) > 0x7fffffffLL ||
-      units * ((m.cap + TR - 1) / TR) > (1LL << 50) / MAX_CTAS)
+      units * ((m.cap + STR - 1) / STR + UNIT_TILES) > (1LL << 37))
     return SNAP_ERR_UNSUPPORTED;
   size_t off = 0;
   p->prefix_off = off; off += align_up((size_t)(n_active + 1) * sizeof(long long));
@@ -956,6 +1045,10 @@ cudaError_t launch_paged_decode(int dtype, const Shape& s, const PageMap& m, con
   a.o_part = reinterpret_cast<float*>(scratch + p.o_off);
   a.scores = w_out ? reinterpret_cast<float*>(scratch + p.score_off) : nullptr;
   a.w_in = w_in; a.w_out = w_out; a.status = status; a.ctas = p.ctas;
+  a.tr = p.mma ? TR : STR;
+  const bool wide = s.d_qk > 128 || s.d_v > 128;
+  a.stages = simt_stages(s, elt_bytes(dtype), simt_ctas(wide, p.gb));
+  a.joined = m.page % STR ? 0 : (m.kr == s.d_qk ? 1 : 0) | (m.vr == s.d_v ? 2 : 0);
   cudaError_t e;
   if (p.mma) {
     const umma::EncodeTiledFn enc = umma::encode_tiled_fn();
@@ -975,9 +1068,9 @@ cudaError_t launch_paged_decode(int dtype, const Shape& s, const PageMap& m, con
     else if (s.d_qk == 64) e = two ? launch_mma<64, 4, 4, 2, kMmaCtasWide>(a, tk, tv, st) : launch_mma<64, 4, 4, 1, kMmaCtas>(a, tk, tv, st);
     else e = two ? launch_mma<256, 2, 2, 2, kMmaCtasWide>(a, tk, tv, st) : launch_mma<256, 2, 2, 1, kMmaCtas>(a, tk, tv, st);
   } else if (dtype == SNAP_F32) {
-    e = s.d_qk > 128 || s.d_v > 128 ? launch_simt<float, 2>(a, st) : launch_simt<float, 1>(a, st);
+    e = wide ? launch_simt<float, 2>(a, st) : launch_simt<float, 1>(a, st);
   } else {
-    e = s.d_qk > 128 || s.d_v > 128 ? launch_simt<__nv_bfloat16, 2>(a, st) : launch_simt<__nv_bfloat16, 1>(a, st);
+    e = wide ? launch_simt<__nv_bfloat16, 2>(a, st) : launch_simt<__nv_bfloat16, 1>(a, st);
   }
   if (e != cudaSuccess) return e;
   const int chunks = (m.cap + JROWS - 1) / JROWS;
