@@ -53,7 +53,7 @@ struct PagedArgs {
   float scale_log2;
   PageMap map;
   int tr;                                       // rows of a tile
-  long long* prefix;                            // [n + 1]: the line before sequence i, per unit of a sequence
+  int* prefix;                                  // [n + 1]: the line before sequence i, per unit of a sequence
   float2* ml_unit;                              // [n * U][gb]: (max, sum), log2 domain, of units that one CTA did whole
   float2* ml_part; float* o_part;               // [2 * CTAs][gb], [2 * CTAs][gb][d_v]: pieces of cut units; CTA c's is 2 c, or
                                                 // 2 c + 1 when it holds the unit's first tile (it has one of either at most)
@@ -68,7 +68,7 @@ __device__ __forceinline__ int rows_of(const PagedArgs& a, int slot) {
   if (slot < 0 || slot >= a.max_seqs) return 0;
   return min(max(a.seq_len[slot], 0), a.map.cap);
 }
-__device__ __forceinline__ int tiles_of(const PagedArgs& a, int rows) { return (rows + a.tr - 1) / a.tr; }
+template <int ROWS> __device__ __forceinline__ int tiles_of(int rows) { return (int)(((unsigned)rows + ROWS - 1) / ROWS); }
 __device__ __forceinline__ int length_of(int nt) { return nt > 0 ? nt + UNIT_TILES : 0; }           // on the line
 // Where tile t of a unit begins on the line, counted from the unit: the first tile carries the unit's share, and all
 // tiles of a short unit begin (and so stay) with the first.
@@ -91,90 +91,138 @@ __device__ __forceinline__ int owner_of(long long x, long long W, int active) {
 struct Held { int2 e[MAX_HELD]; };
 // A place on the line.  pos: where its unit begins, from the CTA's first unit on.
 struct Place { int e, u, t, nt, slot, len, pos; };   // sequence, unit, tile of the unit, tiles per unit, slot, rows
-__device__ __forceinline__ void load_entry(const PagedArgs& a, const Held& held, Place& p) {
+template <int ROWS> __device__ __forceinline__ void load_entry(const PagedArgs& a, const Held& held, Place& p) {
   if (p.e >= a.n) {                             // the end of the line
     p.slot = -1; p.len = 0; p.nt = 1 << 29; p.e = a.n;
     return;
   }
   if (a.n <= MAX_HELD) { const int2 v = held.e[p.e]; p.slot = v.x; p.len = v.y; }
   else { p.slot = a.slots[p.e]; p.len = rows_of(a, p.slot); }
-  p.nt = tiles_of(a, p.len);
+  p.nt = tiles_of<ROWS>(p.len);
 }
-__device__ __forceinline__ void next_unit(const PagedArgs& a, const Held& held, Place& p) {
+template <int ROWS> __device__ __forceinline__ void next_unit(const PagedArgs& a, const Held& held, Place& p) {
   p.pos += length_of(p.nt);
   if (++p.u == a.U) {
     p.u = 0;
-    do { ++p.e; load_entry(a, held, p); } while (p.nt == 0);
+    do { ++p.e; load_entry<ROWS>(a, held, p); } while (p.nt == 0);
   }
 }
 // `step` tiles on, or (false) past `end`, the end of the CTA's stretch
-__device__ __forceinline__ bool advance(const PagedArgs& a, const Held& held, Place& p, int step, int end) {
+template <int ROWS> __device__ __forceinline__ bool advance(const PagedArgs& a, const Held& held, Place& p, int step, int end) {
   p.t += step;
   while (p.t >= p.nt) {
     p.t -= p.nt;
-    next_unit(a, held, p);
+    next_unit<ROWS>(a, held, p);
     if (p.e >= a.n || p.pos >= end) return false;
   }
   return p.pos + begin_of(p.t, p.nt) < end;
 }
 
+__device__ __forceinline__ int warp_inclusive(int v, int lane) {
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) { const int x = __shfl_up_sync(0xffffffffu, v, o); if (lane >= o) v += x; }
+  return v;
+}
+// Slot and rows of sequence e; conditions to report
+__device__ __forceinline__ int2 read_entry(const PagedArgs& a, int e, unsigned& bad) {
+  const int slot = a.slots[e];
+  int len = 0;
+  if (slot >= 0 && slot < a.max_seqs) {
+    len = a.seq_len[slot];
+    if (len > a.map.cap) { bad |= SNAP_DEV_BAD_PAGE; len = a.map.cap; }
+    len = max(len, 0);
+  } else if (slot != -1) {
+    bad |= SNAP_DEV_BAD_SLOT;
+  }
+  return make_int2(slot, len);
+}
+
 // All threads of the CTA: the place of its first tile and the end of its stretch (both counted from that tile's unit).
 // Returns false (to all) when it has none.  CTA 0 also writes the prefix array and reports bad slots and lengths.
-template <int NT>
-__device__ bool locate(const PagedArgs& a, Place& p, int& end, Held& held, long long* scan /* shared, NT / 32 */) {
+// Up to MAX_HELD sequences every warp does all of it by itself (no barrier; the shared copies are written by all warps
+// alike), with more the CTA does it together.
+template <int ROWS, int NT>
+__device__ __forceinline__ bool locate(const PagedArgs& a, Place& p, int& end, Held& held, int* scan /* shared, NT / 32 + 2 */) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, c = blockIdx.x;
-  const int per = (a.n + NT - 1) / NT, e0 = min(tid * per, a.n), e1 = min(e0 + per, a.n);
-  __shared__ int s_e;
-  __shared__ long long s_before;
-  if (tid == 0) { s_e = 0; s_before = 0; }
-  long long mine = 0;
   unsigned bad = 0;
-  for (int e = e0; e < e1; ++e) {
-    const int slot = a.slots[e];
-    int len = 0;
-    if (slot >= 0 && slot < a.max_seqs) {
-      len = a.seq_len[slot];
-      if (len > a.map.cap) { bad |= SNAP_DEV_BAD_PAGE; len = a.map.cap; }
-      len = max(len, 0);
-    } else if (slot != -1) {
-      bad |= SNAP_DEV_BAD_SLOT;
-    }
-    if (a.n <= MAX_HELD) held.e[e] = make_int2(slot, len);
-    mine += length_of(tiles_of(a, len));
-  }
-  long long incl = mine;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) { const long long v = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += v; }
-  if (lane == 31) scan[warp] = incl;
-  __syncthreads();
-  long long before = incl - mine, total = 0;
-#pragma unroll
-  for (int w = 0; w < NT / 32; ++w) { const long long v = scan[w]; total += v; if (w < warp) before += v; }
-  const auto entry_length = [&](int e) {
-    return length_of(tiles_of(a, a.n <= MAX_HELD ? held.e[e].y : rows_of(a, a.slots[e])));
+  int total = 0, e_at = 0, before_at = 0;
+  long long W = 0, x0 = 0, x1 = 0;
+  int active = 0;
+  const auto stretch = [&]() {
+    W = (long long)total * a.U;
+    active = active_ctas(W, a.ctas);
+    if (c >= active) return false;
+    x0 = stretch_begin(W, active, c);
+    x1 = stretch_begin(W, active, c + 1);
+    return true;
   };
-  if (c == 0) {
-    long long at = before;
-    for (int e = e0; e < e1; ++e) { a.prefix[e] = at; at += entry_length(e); }
-    if (tid == 0) a.prefix[a.n] = total;
-    if (bad && a.status) atomicOr(a.status, bad);
-  }
-  const long long W = total * a.U;
-  const int active = active_ctas(W, a.ctas);
-  if (c >= active) return false;
-  const long long x0 = stretch_begin(W, active, c), x1 = stretch_begin(W, active, c + 1);
-  if (x0 >= before * a.U && x0 < (before + mine) * a.U) {                 // exactly one thread
+  if (a.n <= MAX_HELD) {
+    const int per = (a.n + 31) / 32, e0 = min(lane * per, a.n), e1 = min(e0 + per, a.n);   // a lane's sequences
+    int mine = 0;
+#pragma unroll 1
     for (int e = e0; e < e1; ++e) {
-      const int len = entry_length(e);
-      if (x0 < (before + len) * a.U) { s_e = e; s_before = before; break; }
-      before += len;
+      const int2 v = read_entry(a, e, bad);
+      held.e[e] = v;
+      mine += length_of(tiles_of<ROWS>(v.y));
     }
+    const int incl = warp_inclusive(mine, lane);
+    int before = incl - mine;
+    total = __shfl_sync(0xffffffffu, incl, 31);
+    if (c == 0 && warp == 0) {
+      int at = before;
+#pragma unroll 1
+      for (int e = e0; e < e1; ++e) { a.prefix[e] = at; at += length_of(tiles_of<ROWS>(held.e[e].y)); }
+      if (lane == 0) a.prefix[a.n] = total;
+      if (bad && a.status) atomicOr(a.status, bad);
+    }
+    __syncwarp();
+    if (!stretch()) return false;
+    int e = e0;
+    const bool here = x0 >= (long long)before * a.U && x0 < (long long)incl * a.U;       // one lane
+    if (here) {
+#pragma unroll 1
+      for (; e < e1 - 1; ++e) {
+        const int len = length_of(tiles_of<ROWS>(held.e[e].y));
+        if (x0 < (long long)(before + len) * a.U) break;
+        before += len;
+      }
+    }
+    const int from = max(__ffs(__ballot_sync(0xffffffffu, here)) - 1, 0);
+    e_at = __shfl_sync(0xffffffffu, e, from);
+    before_at = __shfl_sync(0xffffffffu, before, from);
+  } else {
+    const int per = (a.n + NT - 1) / NT, e0 = min(tid * per, a.n), e1 = min(e0 + per, a.n);
+    int mine = 0;
+    for (int e = e0; e < e1; ++e) mine += length_of(tiles_of<ROWS>(read_entry(a, e, bad).y));
+    const int incl = warp_inclusive(mine, lane);
+    if (lane == 31) scan[warp] = incl;
+    if (tid == 0) scan[NT / 32] = scan[NT / 32 + 1] = 0;
+    __syncthreads();
+    int before = incl - mine;
+#pragma unroll
+    for (int w = 0; w < NT / 32; ++w) { const int x = scan[w]; total += x; if (w < warp) before += x; }
+    if (c == 0) {
+      int at = before;
+      for (int e = e0; e < e1; ++e) { a.prefix[e] = at; at += length_of(tiles_of<ROWS>(read_entry(a, e, bad).y)); }
+      if (tid == 0) a.prefix[a.n] = total;
+      if (bad && a.status) atomicOr(a.status, bad);
+    }
+    if (!stretch()) return false;
+    if (x0 >= (long long)before * a.U && x0 < (long long)(before + mine) * a.U) {        // one thread
+      for (int e = e0; e < e1; ++e) {
+        const int len = length_of(tiles_of<ROWS>(read_entry(a, e, bad).y));
+        if (x0 < (long long)(before + len) * a.U) { scan[NT / 32] = e; scan[NT / 32 + 1] = before; break; }
+        before += len;
+      }
+    }
+    __syncthreads();
+    e_at = scan[NT / 32];
+    before_at = scan[NT / 32 + 1];
   }
-  __syncthreads();
-  p.e = s_e;
-  load_entry(a, held, p);
+  p.e = e_at;
+  load_entry<ROWS>(a, held, p);
   p.nt = max(p.nt, 1);                          // (only if another stream changes the lengths during the call: stay in bounds)
-  const long long rel = x0 - s_before * a.U;
+  const long long rel = x0 - (long long)before_at * a.U;
   const int unit = length_of(p.nt);
   p.u = (int)min(rel < (1LL << 31) ? (long long)((unsigned)rel / (unsigned)unit) : rel / unit, (long long)a.U - 1);
   const int o = (int)(rel - (long long)p.u * unit);
@@ -184,7 +232,7 @@ __device__ bool locate(const PagedArgs& a, Place& p, int& end, Held& held, long 
   end = (int)min(x1 - x0 + max(o, 0), (long long)(1 << 30));
   if (p.t >= p.nt) {
     p.t = 0;
-    next_unit(a, held, p);
+    next_unit<ROWS>(a, held, p);
     end -= p.pos;
     p.pos = 0;
     if (p.e >= a.n || end <= 0) return false;
@@ -196,32 +244,35 @@ __device__ __forceinline__ int segment_end(const Place& p, int end) {
   return p.nt <= UNIT_TILES ? p.nt : min(p.nt, max(end - p.pos - UNIT_TILES, 1));
 }
 
-// The CTA's joined result of a segment, [cols][ld] in shared memory, leaves for the output (a whole unit) or the
+// The CTA's result of a segment, the sum of NBUF buffers [cols][ld] in shared memory, leaves for the output (a whole unit) or the
 // scratch of pieces.  L, M: per column in shared memory.
-template <typename T, int NT>
-__device__ __forceinline__ void write_segment(const PagedArgs& a, const float* buf, int ld, const float* M, const float* L, int e, int u,
-                                              int nh, bool whole, int piece) {
+template <typename T, int NT, int NBUF>
+__device__ __forceinline__ void write_segment(const PagedArgs& a, const float* buf, int ld, int buf_stride, const float* M, const float* L,
+                                              int e, int u, int nh, bool whole, int piece) {
   const int tid = threadIdx.x, d4 = a.d_v / 4;
   const int kvh = u / a.nhb, hb = u - kvh * a.nhb;
-  if (whole) {
-    T* out = static_cast<T*>(a.out) + ((long long)e * a.Hq + kvh * a.g + hb * a.gb) * a.d_v;
-    for (int x = tid; x < nh * d4; x += NT) {
-      const int h = x / d4, c = (x - h * d4) * 4;
-      const float4 o = *reinterpret_cast<const float4*>(buf + h * ld + c);
+  T* out = static_cast<T*>(a.out) + ((long long)e * a.Hq + kvh * a.g + hb * a.gb) * a.d_v;
+  float* part = a.o_part + (long long)piece * a.gb * a.d_v;
+#pragma unroll 2
+  for (int x = tid; x < nh * d4; x += NT) {
+    const int h = x / d4, c = (x - h * d4) * 4;
+    float4 o = *reinterpret_cast<const float4*>(buf + h * ld + c);
+#pragma unroll
+    for (int b = 1; b < NBUF; ++b) {
+      const float4 y = *reinterpret_cast<const float4*>(buf + b * buf_stride + h * ld + c);
+      o.x += y.x; o.y += y.y; o.z += y.z; o.w += y.w;
+    }
+    if (whole) {
       const float inv = L[h] > 0.f ? 1.f / L[h] : L[h];                    // no row: zero; NaN stays
       alignas(16) T r[4] = {from_f32<T>(o.x * inv), from_f32<T>(o.y * inv), from_f32<T>(o.z * inv), from_f32<T>(o.w * inv)};
       if (sizeof(T) == 4) *reinterpret_cast<uint4*>(out + h * a.d_v + c) = *reinterpret_cast<const uint4*>(r);
       else *reinterpret_cast<uint2*>(out + h * a.d_v + c) = *reinterpret_cast<const uint2*>(r);
+    } else {
+      *reinterpret_cast<float4*>(part + h * a.d_v + c) = o;
     }
-    if (a.scores && tid < nh) a.ml_unit[((long long)e * a.U + u) * a.gb + tid] = make_float2(M[tid], L[tid]);
-  } else {
-    float* o = a.o_part + (long long)piece * a.gb * a.d_v;
-    for (int x = tid; x < nh * d4; x += NT) {
-      const int h = x / d4, c = (x - h * d4) * 4;
-      *reinterpret_cast<float4*>(o + h * a.d_v + c) = *reinterpret_cast<const float4*>(buf + h * ld + c);
-    }
-    if (tid < nh) a.ml_part[(long long)piece * a.gb + tid] = make_float2(M[tid], L[tid]);
   }
+  if (tid < nh && (!whole || a.scores))
+    (whole ? a.ml_unit + ((long long)e * a.U + u) * a.gb : a.ml_part + (long long)piece * a.gb)[tid] = make_float2(M[tid], L[tid]);
 }
 
 __device__ __forceinline__ bool wait_bounded(uint32_t bar, unsigned parity) {
@@ -264,7 +315,7 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
   float* wl = wm + NWARP * NCOL;
   float* jm = wl + NWARP * NCOL;                                         // [NCOL] joined maxima, then sums
   float* jl = jm + NCOL;
-  __shared__ long long scan[S::NT / 32];
+  __shared__ int scan[S::NT / 32 + 2];
   __shared__ Held held;
 
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, gq = lane >> 2, tq = lane & 3;
@@ -273,6 +324,10 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
   if (lane == 0) {
     for (int s = 0; s < NSTAGE; ++s) mbar_init(bar0 + 8 * s, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    if (w == 0) {
+      asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_k) : "memory");
+      asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_v) : "memory");
+    }
   }
   __syncwarp();
   pdl_wait();
@@ -280,51 +335,31 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
 
   Place at;
   int end;
-  if (!locate<S::NT>(a, at, end, held, scan)) return;
+  if (!locate<TR, S::NT>(a, at, end, held, scan)) return;
 
   // ---- the warp's producer: runs NSTAGE tiles ahead of the consumer, over unit borders; warp w takes the CTA's tiles
   // w, w + NWARP, ... ----
+  // Lane l looks up the page of the warp's tile l, l + 32, ...: one look-up's latency for 32 tiles.
   Place pr = at;
-  bool more = w == 0 || advance(a, held, pr, w, end);
+  bool valid = advance<TR>(a, held, pr, w + NWARP * lane, end);
   int pid = 0, n_issued = 0;
-  unsigned bad_stage = 0;                                                // bit s: the tile in stage s is on a bad page
+  unsigned bad_stage = 0, todo = 0;                                      // bit s: the tile in stage s is on a bad page; lanes with a tile to issue
   const int tpp = a.map.page / TR;
-  const auto fetch_pid = [&]() { pid = pr.len > 0 ? a.map.table[(long long)pr.slot * a.map.max_pages + pr.t / tpp] : -1; };
-  const auto issue = [&]() {
-    const int s = n_issued % NSTAGE;
-    const bool bad = pid < 0 || pid >= a.map.n_pages;
-    bad_stage = bad ? bad_stage | (1u << s) : bad_stage & ~(1u << s);
-    if (lane == 0) {
-      const uint32_t dst = stage0 + s * S::STAGE_B, bar = bar0 + 8 * s;
-      const int row = (pr.t % tpp) * TR, kvh = pr.u / a.nhb, page = bad ? 0 : pid;
-      mbar_expect_tx(bar, (unsigned)S::STAGE_B);
-#pragma unroll
-      for (int h = 0; h < S::NSL; ++h) {
-        tma_load_4d(dst + h * SLAB_B, &tmap_k, 64 * h, row, kvh, page, bar);
-        tma_load_4d(dst + S::TENS_B + h * SLAB_B, &tmap_v, 64 * h, row, kvh, page, bar);
-      }
-      if (bad && a.status) atomicOr(a.status, SNAP_DEV_BAD_PAGE);
+  int kvh_of = 0, row_of = 0;
+  const auto fetch = [&]() {
+    todo = __ballot_sync(0xffffffffu, valid);
+    if (valid) {
+      const int pg = pr.t / tpp;
+      pid = pr.len > 0 ? a.map.table[(long long)pr.slot * a.map.max_pages + pg] : -1;
+      row_of = (pr.t - pg * tpp) * TR;
+      kvh_of = pr.u / a.nhb;
     }
-    ++n_issued;
-    more = advance(a, held, pr, NWARP, end);
-    if (more) fetch_pid();
   };
-  if (more) fetch_pid();
-  for (int s = 0; s < NSTAGE && more; ++s) issue();
-
-  // ldmatrix lane roles: K (plain): row (lane & 7) + 8 * bit3, chunk + bit4; V (transposed): row (lane & 7) + 8 * bit4, chunk + bit3
-  const int k_row = (lane & 7) + ((lane >> 3) & 1) * 8, k_cadd = lane >> 4;
-  const int v_row = (lane & 7) + ((lane >> 4) & 1) * 8, v_cadd = (lane >> 3) & 1;
-
-  bool dead = false;                                                     // a bounded wait ran out: nothing more is read
-  int n = 0, done = 0;                                                   // tiles done by this warp; by the CTA before this segment
+  fetch();
   const __nv_bfloat16* q_all = static_cast<const __nv_bfloat16*>(a.q);
-  while (true) {
-    // ---- a segment: the CTA's tiles [at.t, tb) of one unit ----
-    const int tb = segment_end(at, end), cnt = tb - at.t;
+  uint32_t qb[NG][KS][2];                                                // B fragments of Q^T: column 8 gi + gq, dims 16 ks + 2 tq (+8)
+  const auto load_q = [&]() {
     const int kvh = at.u / a.nhb, hb = at.u - kvh * a.nhb, nh = min(a.gb, a.g - hb * a.gb);
-    const bool whole = cnt == at.nt;
-    uint32_t qb[NG][KS][2];                                              // B fragments of Q^T: column 8 gi + gq, dims 16 ks + 2 tq (+8)
 #pragma unroll
     for (int gi = 0; gi < NG; ++gi) {
       const int col = 8 * gi + gq;
@@ -335,6 +370,44 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
         qb[gi][ks][1] = col < nh ? *reinterpret_cast<const uint32_t*>(qp + 16 * ks + 8) : 0u;
       }
     }
+  };
+  load_q();                                                              // (the first tiles' look-ups wait alongside)
+  const auto issue = [&]() {                                             // the lowest lane's tile of `todo`
+    const int s = n_issued % NSTAGE, l = n_issued & 31;
+    const bool bad_mine = pid < 0 || pid >= a.map.n_pages;
+    const bool bad = (__ballot_sync(0xffffffffu, bad_mine) >> l) & 1u;
+    bad_stage = bad ? bad_stage | (1u << s) : bad_stage & ~(1u << s);
+    if (lane == l) {
+      const uint32_t dst = stage0 + s * S::STAGE_B, bar = bar0 + 8 * s;
+      const int page = bad ? 0 : pid;
+      mbar_expect_tx(bar, (unsigned)S::STAGE_B);
+#pragma unroll
+      for (int h = 0; h < S::NSL; ++h) {
+        tma_load_4d(dst + h * SLAB_B, &tmap_k, 64 * h, row_of, kvh_of, page, bar);
+        tma_load_4d(dst + S::TENS_B + h * SLAB_B, &tmap_v, 64 * h, row_of, kvh_of, page, bar);
+      }
+      if (bad && a.status) atomicOr(a.status, SNAP_DEV_BAD_PAGE);
+    }
+    todo &= todo - 1;
+    if ((++n_issued & 31) == 0) {                                        // 32 tiles issued: the next 32
+      if (valid) valid = advance<TR>(a, held, pr, 32 * NWARP, end);
+      fetch();
+    }
+  };
+#pragma unroll 1
+  for (int s = 0; s < NSTAGE && todo; ++s) issue();
+
+  // ldmatrix lane roles: K (plain): row (lane & 7) + 8 * bit3, chunk + bit4; V (transposed): row (lane & 7) + 8 * bit4, chunk + bit3
+  const int k_row = (lane & 7) + ((lane >> 3) & 1) * 8, k_cadd = lane >> 4;
+  const int v_row = (lane & 7) + ((lane >> 4) & 1) * 8, v_cadd = (lane >> 3) & 1;
+
+  bool dead = false;                                                     // a bounded wait ran out: nothing more is read
+  int n = 0, done = 0;                                                   // tiles done by this warp; by the CTA before this segment
+  while (true) {
+    // ---- a segment: the CTA's tiles [at.t, tb) of one unit ----
+    const int tb = segment_end(at, end), cnt = tb - at.t;
+    const int hb = at.u % a.nhb, nh = min(a.gb, a.g - hb * a.gb);
+    const bool whole = cnt == at.nt;
     float oacc[NG][KS][4], m_ref[NG][2], l_part[NG][2];                  // O^T: dims 16 db + gq (+8), columns 8 gi + 2 tq (+1)
 #pragma unroll
     for (int gi = 0; gi < NG; ++gi) {
@@ -444,7 +517,7 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
         }
       }
       __syncwarp();
-      if (more) {
+      if (todo) {
         // the stage was read, and possibly cleared, through the generic proxy; the copy that refills it is of the async proxy
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         issue();
@@ -487,42 +560,36 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
       for (int ww = 0; ww < NWARP; ++ww) M = fmaxf(M, wm[ww * NCOL + tid]);
 #pragma unroll
       for (int ww = 0; ww < NWARP; ++ww) {
-        const float mw = wm[ww * NCOL + tid];
-        L += mw == -INFINITY ? 0.f : wl[ww * NCOL + tid] * exp2f(mw - M);
+        const float lw = wl[ww * NCOL + tid];
+        L += lw == 0.f ? 0.f : lw * exp2f(wm[ww * NCOL + tid] - M);
       }
       jm[tid] = M; jl[tid] = L;
     }
-    const auto exchange = [&](float* b, bool store) {
+    // the upper half of the warps leave their outputs in a buffer each, the lower half add theirs there
+#pragma unroll 1
+    for (int lower = 0; lower < 2; ++lower) {
+      if ((w < NWARP / 2) == (lower == 1)) {
+        float* b = buf + (w % (NWARP / 2)) * NCOL * LD + 2 * tq * LD + gq;
 #pragma unroll
-      for (int gi = 0; gi < NG; ++gi)
+        for (int gi = 0; gi < NG; ++gi)
 #pragma unroll
-        for (int db = 0; db < KS; ++db)
+          for (int db = 0; db < KS; ++db)
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            float* p = b + (8 * gi + 2 * tq + (x & 1)) * LD + 16 * db + gq + 8 * (x >> 1);
-            if (store) *p = oacc[gi][db][x];
-            else oacc[gi][db][x] += *p;
-          }
-    };
-    if (NWARP == 4) {
-      if (w >= 2) exchange(buf + (w - 2) * NCOL * LD, true);
+            for (int x = 0; x < 4; ++x) {
+              float* p = b + (8 * gi + (x & 1)) * LD + 16 * db + 8 * (x >> 1);
+              *p = lower ? *p + oacc[gi][db][x] : oacc[gi][db][x];
+            }
+      }
       __syncthreads();
-      if (w < 2) exchange(buf + w * NCOL * LD, false);
     }
-    if (w == 1) exchange(buf + NCOL * LD, true);
-    __syncthreads();
-    if (w == 0) {
-      exchange(buf + NCOL * LD, false);
-      exchange(buf, true);
-    }
-    __syncthreads();
-    write_segment<__nv_bfloat16, S::NT>(a, buf, LD, jm, jl, at.e, at.u, nh, whole, 2 * blockIdx.x + (at.t == 0));
+    write_segment<__nv_bfloat16, S::NT, NWARP / 2>(a, buf, LD, NCOL * LD, jm, jl, at.e, at.u, nh, whole, 2 * blockIdx.x + (at.t == 0));
 
     if (tb < at.nt) break;
     done += cnt;
     at.t = 0;
-    next_unit(a, held, at);
+    next_unit<TR>(a, held, at);
     if (at.e >= a.n || at.pos >= end) break;
+    load_q();
   }
   if (dead) {
     if (a.status) atomicOr(a.status, SNAP_DEV_WAIT_TIMEOUT);
@@ -557,7 +624,7 @@ __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_cons
   __shared__ __align__(16) float buf[2 * HB * LD];
   __shared__ float wm[SNW * HB], wl[SNW * HB], jm[HB], jl[HB];
   __shared__ uint64_t bars[SNW * MAX_STAGES];
-  __shared__ long long scan[SNT / 32];
+  __shared__ int scan[SNT / 32 + 2];
   __shared__ Held held;
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
   const unsigned krow_b = a.d_qk * sizeof(T), vrow_b = a.d_v * sizeof(T), stage_b = STR * (krow_b + vrow_b);
@@ -572,70 +639,87 @@ __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_cons
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   Place at;
   int end;
-  if (!locate<SNT>(a, at, end, held, scan)) return;
+  if (!locate<STR, SNT>(a, at, end, held, scan)) return;
   // After the exchange lane l owns row l / 4 of the tile and head (or heads) my_head (+ 1).
   const int my_head = HB >= 8 ? 2 * (lane & 3) : HB == 4 ? (lane & 3) : HB == 2 ? ((lane & 3) >> 1) : 0;
 
-  // ---- the warp's producer: lane r (< 8) looks up row r of the tile after the one being issued ----
+  // ---- the warp's producer: lane l looks up row l % 8 of the warp's tile l / 8, l / 8 + 4, ... ----
   Place pr = at;
-  bool more = w == 0 || advance(a, held, pr, w, end);
-  int pid = -1, prow = 0, s_in = 0, in_flight = 0;
+  bool valid = advance<STR>(a, held, pr, w + SNW * (lane >> 3), end);
+  int pid = -1, prow = 0, kvh_of = 0, s_in = 0, in_flight = 0, next = 0;  // next: which of the four tiles is issued next
+  unsigned todo = 0;                                                     // bit 8 j: tile j is there
   unsigned long long okay_of = 0;                                        // 8 bits per stage: the rows that are there
   const auto fetch = [&]() {
-    const int row = pr.t * STR + (lane & 7);
+    todo = __ballot_sync(0xffffffffu, valid);
     pid = -1;
-    if (row < pr.len) {
+    const int row = pr.t * STR + (lane & 7);
+    if (valid && row < pr.len) {
       const int pg = row / a.map.page;
       prow = row - pg * a.map.page;
       pid = a.map.table[(long long)pr.slot * a.map.max_pages + pg];
+      kvh_of = pr.u / a.nhb;
     }
   };
   const auto issue = [&]() {
-    if (pr.t * STR + (lane & 7) < pr.len && (pid < 0 || pid >= a.map.n_pages)) {
+    const bool mine = lane >> 3 == next, bad = mine && valid && pr.t * STR + (lane & 7) < pr.len && (pid < 0 || pid >= a.map.n_pages);
+    if (bad) {
       pid = -1;
-      if (lane < 8 && a.status) atomicOr(a.status, SNAP_DEV_BAD_PAGE);
+      if (a.status) atomicOr(a.status, SNAP_DEV_BAD_PAGE);
     }
-    const unsigned okay = __ballot_sync(0xffffffffu, pid >= 0) & 0xffu;
+    const unsigned okay = (__ballot_sync(0xffffffffu, pid >= 0) >> (8 * next)) & 0xffu;
     okay_of = (okay_of & ~(0xffull << (8 * s_in))) | ((unsigned long long)okay << (8 * s_in));
     const uint32_t bar = bar0 + 8 * s_in, dst = stage0 + s_in * stage_b;
-    const int rows = __popc(okay), kvh = pr.u / a.nhb;
+    const int rows = __popc(okay), r = lane & 7;
     if (lane == 0) mbar_expect_tx(bar, rows * (krow_b + vrow_b));
     __syncwarp();
-    if (pid >= 0) {
-      const T* ks = static_cast<const T*>(a.kp) + pid * a.map.kp + kvh * a.map.kh + prow * a.map.kr;
-      const T* vs = static_cast<const T*>(a.vp) + pid * a.map.vp + kvh * a.map.vh + prow * a.map.vr;
-      const uint32_t kd = dst + lane * krow_b, vd = dst + STR * krow_b + lane * vrow_b;
-      if (a.joined & 1) { if (lane == 0) bulk_load(kd, ks, rows * krow_b, bar); }
-      else if (lane < 8) bulk_load(kd, ks, krow_b, bar);
-      if (a.joined & 2) { if (lane == 0) bulk_load(vd, vs, rows * vrow_b, bar); }
-      else if (lane < 8) bulk_load(vd, vs, vrow_b, bar);
+    if (mine && pid >= 0) {
+      const T* ks = static_cast<const T*>(a.kp) + pid * a.map.kp + kvh_of * a.map.kh + prow * a.map.kr;
+      const T* vs = static_cast<const T*>(a.vp) + pid * a.map.vp + kvh_of * a.map.vh + prow * a.map.vr;
+      const uint32_t kd = dst + r * krow_b, vd = dst + STR * krow_b + r * vrow_b;
+      if (a.joined & 1) { if (r == 0) bulk_load(kd, ks, rows * krow_b, bar); }
+      else bulk_load(kd, ks, krow_b, bar);
+      if (a.joined & 2) { if (r == 0) bulk_load(vd, vs, rows * vrow_b, bar); }
+      else bulk_load(vd, vs, vrow_b, bar);
     }
     ++in_flight;
     if (++s_in == a.stages) s_in = 0;
-    more = advance(a, held, pr, SNW, end);
-    if (more) fetch();
+    todo &= ~(0xffu << (8 * next));
+    if (++next == 4) {
+      next = 0;
+      if (valid) valid = advance<STR>(a, held, pr, 4 * SNW, end);
+      fetch();
+    }
   };
-  if (more) fetch();
-  for (int s = 0; s < a.stages && more; ++s) issue();
+  fetch();
+  float q[HB][NV][4];
+  const auto load_q = [&]() {
+    const int kvh = at.u / a.nhb, hb = at.u - kvh * a.nhb, nh = min(a.gb, a.g - hb * a.gb);
+    const T* qp = static_cast<const T*>(a.q) + ((long long)at.e * a.Hq + kvh * a.g + hb * a.gb) * a.d_qk + 4 * lane;
+#pragma unroll
+    for (int h = 0; h < HB; ++h)
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (h < nh && 4 * lane + 128 * j < a.d_qk) f = four<T>(qp + h * a.d_qk + 128 * j);
+        q[h][j][0] = f.x; q[h][j][1] = f.y; q[h][j][2] = f.z; q[h][j][3] = f.w;
+      }
+  };
+  load_q();                                                              // (the first tiles' look-ups wait alongside)
+#pragma unroll 1
+  for (int s = 0; s < a.stages && todo; ++s) issue();
 
   bool dead = false;                                                     // a bounded wait ran out: nothing more is read
   int n = 0, done = 0, s_out = 0;
   unsigned parity = 0;
   while (true) {
     const int tb = segment_end(at, end), cnt = tb - at.t;
-    const int kvh = at.u / a.nhb, hb = at.u - kvh * a.nhb, nh = min(a.gb, a.g - hb * a.gb);
+    const int hb = at.u % a.nhb, nh = min(a.gb, a.g - hb * a.gb);
     const bool whole = cnt == at.nt;
-    float q[HB][NV][4], o[HB][NV][4], m_ref[VPL], l_part[VPL];
+    float o[HB][NV][4], m_ref[VPL], l_part[VPL];
 #pragma unroll
     for (int h = 0; h < HB; ++h)
 #pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        const int d = 4 * lane + 128 * j;
-        float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (h < nh && d < a.d_qk) f = four<T>(static_cast<const T*>(a.q) + ((long long)at.e * a.Hq + kvh * a.g + hb * a.gb + h) * a.d_qk + d);
-        q[h][j][0] = f.x; q[h][j][1] = f.y; q[h][j][2] = f.z; q[h][j][3] = f.w;
-        o[h][j][0] = o[h][j][1] = o[h][j][2] = o[h][j][3] = 0.f;
-      }
+      for (int j = 0; j < NV; ++j) o[h][j][0] = o[h][j][1] = o[h][j][2] = o[h][j][3] = 0.f;
 #pragma unroll
     for (int k = 0; k < VPL; ++k) { m_ref[k] = -INFINITY; l_part[k] = 0.f; }
     float* srow = a.scores ? a.scores + ((long long)at.e * a.U + at.u) * a.map.cap * a.gb : nullptr;
@@ -742,7 +826,7 @@ __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_cons
       }
       if (++s_out == a.stages) { s_out = 0; parity ^= 1u; }
       __syncwarp();                                                      // the stage has been read
-      if (more) issue();
+      if (todo) issue();
     }
 
     // ---- join the warps ----
@@ -765,35 +849,35 @@ __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_cons
         float L = 0.f;
 #pragma unroll
         for (int ww = 0; ww < SNW; ++ww) {
-          const float mx = wm[ww * HB + h];
-          L += mx == -INFINITY ? 0.f : wl[ww * HB + h] * exp2f(mx - M);
+          const float lw = wl[ww * HB + h];
+          L += lw == 0.f ? 0.f : lw * exp2f(wm[ww * HB + h] - M);
         }
         jm[h] = M; jl[h] = L;
       }
     }
-    const auto exchange = [&](float* b, bool store) {
+#pragma unroll 1
+    for (int lower = 0; lower < 2; ++lower) {
+      if ((w < SNW / 2) == (lower == 1)) {
+        float* b = buf + (w % (SNW / 2)) * HB * LD + 4 * lane;
 #pragma unroll
-      for (int h = 0; h < HB; ++h)
+        for (int h = 0; h < HB; ++h)
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-          float4* x = reinterpret_cast<float4*>(b + h * LD + 128 * j + 4 * lane);
-          if (store) *x = make_float4(o[h][j][0], o[h][j][1], o[h][j][2], o[h][j][3]);
-          else { const float4 f = *x; o[h][j][0] += f.x; o[h][j][1] += f.y; o[h][j][2] += f.z; o[h][j][3] += f.w; }
-        }
-    };
-    if (w >= 2) exchange(buf + (w - 2) * HB * LD, true);
-    __syncthreads();
-    if (w < 2) exchange(buf + w * HB * LD, false);
-    if (w == 1) exchange(buf + HB * LD, true);
-    __syncthreads();
-    if (w == 0) { exchange(buf + HB * LD, false); exchange(buf, true); }
-    __syncthreads();
-    write_segment<T, SNT>(a, buf, LD, jm, jl, at.e, at.u, nh, whole, 2 * blockIdx.x + (at.t == 0));
+          for (int j = 0; j < NV; ++j) {
+            float4* x = reinterpret_cast<float4*>(b + h * LD + 128 * j);
+            float4 f = make_float4(o[h][j][0], o[h][j][1], o[h][j][2], o[h][j][3]);
+            if (lower) { const float4 y = *x; f.x += y.x; f.y += y.y; f.z += y.z; f.w += y.w; }
+            *x = f;
+          }
+      }
+      __syncthreads();
+    }
+    write_segment<T, SNT, SNW / 2>(a, buf, LD, HB * LD, jm, jl, at.e, at.u, nh, whole, 2 * blockIdx.x + (at.t == 0));
     if (tb < at.nt) break;
     done += cnt;
     at.t = 0;
-    next_unit(a, held, at);
+    next_unit<STR>(a, held, at);
     if (at.e >= a.n || at.pos >= end) break;
+    load_q();
   }
   if (dead) {
     if (a.status) atomicOr(a.status, SNAP_DEV_WAIT_TIMEOUT);
@@ -810,9 +894,9 @@ __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_cons
 constexpr int JNT = 256, JROWS = 4 * JNT;         // rows of a weights CTA
 
 struct Pieces { int np, c0; };                     // pieces of a unit; np <= 1: done whole
-__device__ __forceinline__ Pieces pieces_of(const PagedArgs& a, int u, long long before, long long total, int nt) {
+__device__ __forceinline__ Pieces pieces_of(const PagedArgs& a, int u, int before, int total, int nt) {
   Pieces p;
-  const long long W = total * a.U, x = before * a.U + (long long)u * length_of(nt);
+  const long long W = (long long)total * a.U, x = (long long)before * a.U + (long long)u * length_of(nt);
   const int active = active_ctas(W, a.ctas);
   p.c0 = owner_of(x, W, active);
   p.np = owner_of(x + begin_of(nt - 1, nt), W, active) - p.c0 + 1;
@@ -823,7 +907,7 @@ __device__ __forceinline__ int piece_at(const Pieces& p, int k) { return 2 * (p.
 template <typename T>
 __global__ void __launch_bounds__(JNT) paged_join_kernel(const __grid_constant__ PagedArgs a) {
   __shared__ __align__(16) float acc_s[JNT / 32][256];
-  __shared__ float f_s[MAX_CTAS], red[JNT / 32];
+  __shared__ float red_m[JNT / 32], red_l[JNT / 32];
   __shared__ float mu_s[16];
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
   pdl_wait();
@@ -833,8 +917,7 @@ __global__ void __launch_bounds__(JNT) paged_join_kernel(const __grid_constant__
     // ---- one query head's output ----
     const int e = blockIdx.x / a.Hq, head = blockIdx.x - e * a.Hq;
     const int kvh = head / a.g, x = head - kvh * a.g, hb = x / a.gb, col = x - hb * a.gb;
-    const long long before = a.prefix[e], line = a.prefix[a.n];
-    const int nt = max((int)(a.prefix[e + 1] - before) - UNIT_TILES, 0);
+    const int before = a.prefix[e], line = a.prefix[a.n], nt = max(a.prefix[e + 1] - before - UNIT_TILES, 0);
     T* out = static_cast<T*>(a.out) + (long long)blockIdx.x * a.d_v;
     if (nt == 0) {
       for (int c = tid; c < a.d_v; c += JNT) out[c] = from_f32<T>(0.f);
@@ -842,53 +925,60 @@ __global__ void __launch_bounds__(JNT) paged_join_kernel(const __grid_constant__
     }
     const Pieces p = pieces_of(a, kvh * a.nhb + hb, before, line, nt);
     if (p.np <= 1) return;
-    float m = -INFINITY;
-    for (int k = tid; k < p.np; k += JNT) m = fmaxf(m, a.ml_part[(long long)piece_at(p, k) * a.gb + col].x);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    if (lane == 0) red[w] = m;
-    __syncthreads();
-    m = red[0];
-#pragma unroll
-    for (int k = 1; k < JNT / 32; ++k) m = fmaxf(m, red[k]);
-    float l = 0.f;
-    for (int k = tid; k < p.np; k += JNT) {
-      const float2 ml = a.ml_part[(long long)piece_at(p, k) * a.gb + col];
-      const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - m);
-      f_s[k] = f;
-      l += f == 0.f ? 0.f : ml.y * f;
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-    __syncthreads();                                                     // red has been read
-    if (lane == 0) red[w] = l;
-    __syncthreads();
-    l = 0.f;
-#pragma unroll
-    for (int k = 0; k < JNT / 32; ++k) l += red[k];
-    // a warp per piece, a lane per four dims
+    // a warp takes every eighth piece, four at a time: their (max, sum) and outputs come in together
+    float m = -INFINITY, l = 0.f;
     float4 acc[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
-#pragma unroll 4
-    for (int k = w; k < p.np; k += JNT / 32) {
-      const float* o = a.o_part + ((long long)piece_at(p, k) * a.gb + col) * a.d_v;
-      const float f = f_s[k];
+    for (int k0 = w; k0 < p.np; k0 += 4 * (JNT / 32)) {
+      float2 ml[4];
+      float4 v[4][2];
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
-        if (4 * lane + 128 * j < a.d_v) {
-          const float4 v = *reinterpret_cast<const float4*>(o + 4 * lane + 128 * j);
-          acc[j].x = fmaf(f, v.x, acc[j].x); acc[j].y = fmaf(f, v.y, acc[j].y);
-          acc[j].z = fmaf(f, v.z, acc[j].z); acc[j].w = fmaf(f, v.w, acc[j].w);
+      for (int x = 0; x < 4; ++x) {
+        const int k = k0 + x * (JNT / 32);
+        ml[x] = make_float2(-INFINITY, 0.f);
+        if (k < p.np) ml[x] = a.ml_part[(long long)piece_at(p, k) * a.gb + col];
+        const float* o = a.o_part + ((long long)piece_at(p, k < p.np ? k : 0) * a.gb + col) * a.d_v + 4 * lane;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          v[x][j] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (k < p.np && 4 * lane + 128 * j < a.d_v) v[x][j] = *reinterpret_cast<const float4*>(o + 128 * j);
         }
+      }
+      const float nm = fmaxf(fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)), m);
+      const float f = m == -INFINITY ? 0.f : exp2f(m - nm);
+      m = nm;
+      l *= f;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) { acc[j].x *= f; acc[j].y *= f; acc[j].z *= f; acc[j].w *= f; }
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        if (ml[x].y == 0.f) continue;                                    // a piece without rows
+        const float g = exp2f(ml[x].x - m);
+        l = fmaf(ml[x].y, g, l);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          acc[j].x = fmaf(g, v[x][j].x, acc[j].x); acc[j].y = fmaf(g, v[x][j].y, acc[j].y);
+          acc[j].z = fmaf(g, v[x][j].z, acc[j].z); acc[j].w = fmaf(g, v[x][j].w, acc[j].w);
+        }
+      }
     }
 #pragma unroll
     for (int j = 0; j < 2; ++j)
       if (4 * lane + 128 * j < a.d_v) *reinterpret_cast<float4*>(&acc_s[w][4 * lane + 128 * j]) = acc[j];
+    if (lane == 0) { red_m[w] = m; red_l[w] = l; }
     __syncthreads();
-    const float inv = l > 0.f ? 1.f / l : l;
+    float M = -INFINITY, L = 0.f, f_w[JNT / 32];
+#pragma unroll
+    for (int k = 0; k < JNT / 32; ++k) M = fmaxf(M, red_m[k]);
+#pragma unroll
+    for (int k = 0; k < JNT / 32; ++k) {
+      f_w[k] = red_l[k] == 0.f ? 0.f : exp2f(red_m[k] - M);
+      L = fmaf(red_l[k], f_w[k], L);
+    }
+    const float inv = L > 0.f ? 1.f / L : L;
     for (int c = tid; c < a.d_v; c += JNT) {
       float s = 0.f;
 #pragma unroll
-      for (int k = 0; k < JNT / 32; ++k) s += acc_s[k][c];
+      for (int k = 0; k < JNT / 32; ++k) s = fmaf(acc_s[k][c], f_w[k], s);
       out[c] = from_f32<T>(s * inv);
     }
     return;
@@ -896,8 +986,7 @@ __global__ void __launch_bounds__(JNT) paged_join_kernel(const __grid_constant__
   // ---- JROWS rows' weights of one (sequence, KV head) ----
   const int chunks = (a.map.cap + JROWS - 1) / JROWS;
   const int id = blockIdx.x - merges, chunk = id % chunks, kvh = (id / chunks) % a.Hkv, e = id / chunks / a.Hkv;
-  const long long before = a.prefix[e], line = a.prefix[a.n];
-  const int nt = max((int)(a.prefix[e + 1] - before) - UNIT_TILES, 0);
+  const int before = a.prefix[e], line = a.prefix[a.n], nt = max(a.prefix[e + 1] - before - UNIT_TILES, 0);
   if (chunk * JROWS >= nt * a.tr) return;
   const int slot = a.slots[e];
   int again = 0;                                                         // the slot was listed before: its first entry counts
@@ -923,7 +1012,7 @@ __global__ void __launch_bounds__(JNT) paged_join_kernel(const __grid_constant__
         for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
         for (int k = lane; k < p.np; k += 32) {
           const float2 ml = a.ml_part[(long long)piece_at(p, k) * a.gb + col];
-          l += ml.x == -INFINITY ? 0.f : ml.y * exp2f(ml.x - m);
+          l += ml.y == 0.f ? 0.f : ml.y * exp2f(ml.x - m);
         }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
@@ -1018,10 +1107,11 @@ int paged_decode_plan(int dtype, const Shape& s, const PageMap& m, int n_active,
   const long long chunks = (m.cap + JROWS - 1) / JROWS;
   // grid and index limits; a line of tiles and the scratch have to be countable
   if (units > (1LL << 30) || (long long)n_active * s.Hq + (weights ? (long long)n_active * s.Hkv * chunks : 0) > 0x7fffffffLL ||
-      units * ((m.cap + STR - 1) / STR + UNIT_TILES) > (1LL << 37))
+      units * ((m.cap + STR - 1) / STR + UNIT_TILES) > (1LL << 37) ||
+      (long long)n_active * ((m.cap + STR - 1) / STR + UNIT_TILES) > 0x7fffffffLL)
     return SNAP_ERR_UNSUPPORTED;
   size_t off = 0;
-  p->prefix_off = off; off += align_up((size_t)(n_active + 1) * sizeof(long long));
+  p->prefix_off = off; off += align_up((size_t)(n_active + 1) * sizeof(int));
   p->ml_off = off;     off += align_up(((size_t)units + 2 * (size_t)p->ctas) * p->gb * sizeof(float2));
   p->o_off = off;      off += align_up(2 * (size_t)p->ctas * p->gb * s.d_v * sizeof(float));
   p->score_off = off;
@@ -1039,7 +1129,7 @@ cudaError_t launch_paged_decode(int dtype, const Shape& s, const PageMap& m, con
   a.d_qk = s.d_qk; a.d_v = s.d_v; a.max_seqs = s.max_seqs;
   a.scale_log2 = s.scale * 1.4426950408889634f;
   a.map = m;
-  a.prefix = reinterpret_cast<long long*>(scratch + p.prefix_off);
+  a.prefix = reinterpret_cast<int*>(scratch + p.prefix_off);
   a.ml_unit = reinterpret_cast<float2*>(scratch + p.ml_off);
   a.ml_part = a.ml_unit + (size_t)n_active * a.U * p.gb;
   a.o_part = reinterpret_cast<float*>(scratch + p.o_off);

@@ -311,6 +311,23 @@ def test_paged_decode_of_long_and_single_sequences(dtype, hq, hkv, d):
         assert c.bits() == 0
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [31, 45, 64, 97, 128, 129, 300])
+def test_paged_decode_of_many_ragged_sequences(n, dtype):
+    """Batches around the sizes at which the look-up of sequences changes, lengths of all kinds in every order."""
+    rng = np.random.default_rng(n)
+    lengths = [int(x) for x in rng.choice([0, 0, 1, 7, 8, 9, 16, 40, 64, 65, 72, 150, 333], size=n)]
+    lengths[n // 2] = 2500
+    cfg = config(4, 2, 64, dtype=dtype, max_seqs=n)
+    c = Pages(cfg, dtype, 16, lengths, seed=n)
+    slots = [int(x) for x in rng.permutation(n)]
+    q = torch.randn(n, 4, 64, device="cuda", generator=torch.Generator(device="cuda").manual_seed(n)).to(DT[dtype])
+    w = c.weights()
+    out = run_decode(c, q, slots, weights_out=w)
+    check_decode(c, out, q, slots, dtype, weights=w, weights_before=c.weights())
+    assert c.bits() == 0
+
+
 @pytest.mark.parametrize("dtype,page", [("bf16", 16), ("f32", 16), ("bf16", 4)])
 def test_paged_decode_leaves_out_what_is_not_there(dtype, page):
     """Pages out of range, lengths past the table, negative lengths, slots out of range and listed twice."""
@@ -583,6 +600,24 @@ def test_prompt_steps_eviction_steps(dtype, hq, hkv, d, page):
         torch.cuda.synchronize()
         check_step(w0, [3, 4, 5])
     assert c.bits() == 0
+
+
+@pytest.mark.parametrize("dtype,page", [("bf16", 16), ("f32", 16), ("bf16", 8)])
+def test_paged_decode_carries_nan_and_leaves_other_heads_alone(dtype, page):
+    """A NaN in a row that counts reaches the heads that attend it, over joins too, and no other head."""
+    cfg = config(4, 2, 64, dtype=dtype, max_seqs=3)
+    c = Pages(cfg, dtype, page, [5000, 40, 1], seed=6)
+    row = 3333
+    c.k[int(c.table[0, row // page]), 1, row % page, 3] = float("nan")
+    c.v[int(c.table[1, 5 // page]), 0, 5 % page, 7] = float("nan")
+    c.k[int(c.table[2, 0]), 0, 0, 0] = float("nan")
+    q = torch.randn(3, 4, 64, device="cuda").to(DT[dtype])
+    w = c.weights()
+    out = f64(run_decode(c, q, [0, 1, 2], weights_out=w))
+    assert np.isnan(out[0, 2:]).all() and np.isfinite(out[0, :2]).all()
+    assert np.isnan(out[1, :2, 7]).all() and np.isfinite(np.delete(out[1], 7, axis=1)).all() and np.isfinite(out[1, 2:]).all()
+    assert np.isnan(out[2, :2]).all() and np.isfinite(out[2, 2:]).all()
+    assert np.isnan(f64(w)[0, 1, :5000]).all() and np.isfinite(f64(w)[0, 0]).all() and np.isfinite(f64(w)[1]).all()
 
 
 def test_calls_on_a_side_stream_and_two_at_once():
