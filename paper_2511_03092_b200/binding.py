@@ -387,27 +387,34 @@ def snap_decode_attn_blocks(cfg: SnapConfig, layout: SnapLayout, q, k_new, v_new
 
 
 # --- rotary positions and the paged cache ---
-# These calls check their tensors here: the library sees addresses only.  A serving step makes them many times, so each
-# call tests its tensors with plain expressions and only a failed test goes through _refuse, which finds the words.
+# The library sees addresses only, so the tensors of these calls are checked first (type, shape, strides, device), by the
+# compiled module _marshal: a serving step makes them once per layer.  What it turns down, _refuse finds the words for.
 _DTYPES = {SNAP_F32: torch.float32, SNAP_BF16: torch.bfloat16}
 _I32, _F32, _F64 = torch.int32, torch.float32, torch.float64
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_native = None
 
 
-def _dense(t, dtype, shape, device) -> bool:
-    return t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == device
+def _calls():
+    """(the module _marshal, addresses of the entry points it calls); raises if either is absent."""
+    global _native
+    if _native is None:
+        L = lib()
+        try:
+            from . import _marshal
+        except ImportError as e:
+            raise RuntimeError(f"the module _marshal is missing ({e}): run `python -m paper_2511_03092_b200.build`") from e
+        _native = (_marshal, {name: C.cast(getattr(L, name), C.c_void_p).value
+                              for name in ("snap_rope", "snap_paged_append", "snap_paged_decode_attn", "snap_paged_evict")})
+    return _native
 
 
-def _rows(t, dtype, shape, device) -> bool:
-    """Any strides, the last dim dense."""
-    return t.dtype is dtype and t.shape == shape and t.stride()[-1] == 1 and t.get_device() == device
-
-
-def _refuse(where: str, device: int, *named) -> None:
+def _refuse(where: str, *named) -> None:
     """Raise for the first of (name, tensor or None, dtype, shape or None, dense) that is not what the call is told it is."""
     for name, t, dtype, shape, dense in named:
         if t is None:
             continue
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{where}: {name} is a {type(t).__name__}, not a tensor")
         if dtype is not None and t.dtype != dtype:
             raise ValueError(f"{where}: {name} is {t.dtype}, expected {dtype}")
         if shape is not None and tuple(t.shape) != tuple(shape):
@@ -416,25 +423,29 @@ def _refuse(where: str, device: int, *named) -> None:
             raise ValueError(f"{where}: {name} must be dense")
         if not dense and t.stride()[-1] != 1:
             raise ValueError(f"{where}: {name} needs a dense last dim")
+    device = None
     for name, t, *_ in named:
-        if t is not None and t.get_device() != device:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError(f"{where}: {name} is not on a CUDA device")
+        if device is None:
+            device = t.get_device()
+        if t.get_device() != device:
             raise ValueError(f"{where}: {name} is on device {t.get_device()}, not {device}")
-    raise ValueError(f"{where}: the pages' strides are not those of the description")
-
-
-def _launch_stream(where: str, device: int, stream) -> int:
-    """The stream's handle; the tensors' device has to be the current one (the library launches there)."""
-    if device < 0:
-        raise ValueError(f"{where}: the tensors are not on a CUDA device")
-    if device != torch.cuda.current_device():
+    if device is not None and device != torch.cuda.current_device():
         raise ValueError(f"{where}: the tensors are on device {device}, the current device is {torch.cuda.current_device()}")
-    if stream is None and _raw_stream is not None:
-        return _raw_stream(device)
-    return _stream(stream)
+    raise ValueError(f"{where}: a tensor is missing, or the pages' strides are not those of the description")
 
 
-def _strides(t: Optional[torch.Tensor]):
-    return (0, 0) if t is None else t.stride()[:2]
+def _answer(status: Optional[int], where: str, named) -> None:
+    if status is None:
+        _refuse(where, *named())
+    _check(status, where)
+
+
+def _handle(stream):
+    return None if stream is None else _stream(stream)
 
 
 def make_rope(*, rot_dim: int, rot_offset: int = 0, interleaved: bool = False, scaling="plain", base: float = 10000.0,
@@ -458,16 +469,14 @@ def snap_rope(cfg: SnapConfig, rope: SnapRope, freqs, positions, q=None, k=None,
     """Rotate q [T, Hq, d] and / or k [T, Hkv, d] (any strides with a dense last dim) into q_out and k_out, which may be
     the inputs themselves.  freqs: float64 [rot_dim / 2], positions: int32 [T], on the device.  inverse: by minus the
     angle (the gradient's direction)."""
-    where, dt, n, dev = "snap_rope", _DTYPES.get(cfg.dtype), positions.shape[0], positions.get_device()
-    sq, sk, sf = (n, cfg.n_q_heads, cfg.d_qk), (n, cfg.n_kv_heads, cfg.d_qk), (rope.rot_dim // 2,)
-    if not (_dense(freqs, _F64, sf, dev) and _dense(positions, _I32, (n,), dev) and
-            (q is None or _rows(q, dt, sq, dev)) and (q_out is None or _rows(q_out, dt, sq, dev)) and
-            (k is None or _rows(k, dt, sk, dev)) and (k_out is None or _rows(k_out, dt, sk, dev))):
-        _refuse(where, dev, ("freqs", freqs, _F64, sf, True), ("positions", positions, _I32, (n,), True), ("q", q, dt, sq, False),
-                ("k", k, dt, sk, False), ("q_out", q_out, dt, sq, False), ("k_out", k_out, dt, sk, False))
-    _check(lib().snap_rope(C.byref(cfg), C.byref(rope), freqs.data_ptr(), positions.data_ptr(), n, _ptr(q), *_strides(q), _ptr(q_out),
-                           *_strides(q_out), _ptr(k), *_strides(k), _ptr(k_out), *_strides(k_out), 1 if inverse else 0,
-                           _launch_stream(where, dev, stream)), where)
+    native, entry = _native or _calls()
+    status = native.rope(entry["snap_rope"], cfg, rope, freqs, positions, q, k, q_out, k_out, 1 if inverse else 0, _handle(stream))
+    if status != 0:
+        n, dt = positions.shape[0], _DTYPES.get(cfg.dtype)
+        sq, sk = (n, cfg.n_q_heads, cfg.d_qk), (n, cfg.n_kv_heads, cfg.d_qk)
+        _answer(status, "snap_rope", lambda: (
+            ("freqs", freqs, _F64, (rope.rot_dim // 2,), True), ("positions", positions, _I32, (n,), True), ("q", q, dt, sq, False),
+            ("k", k, dt, sk, False), ("q_out", q_out, dt, sq, False), ("k_out", k_out, dt, sk, False)))
 
 
 def make_paged(k_pages, v_pages, page_table) -> SnapPaged:
@@ -478,16 +487,6 @@ def make_paged(k_pages, v_pages, page_table) -> SnapPaged:
         raise ValueError("make_paged: k_pages and v_pages are [pages, heads, rows, dim], page_table [seqs, pages]")
     (kp, kh, kr, _), (vp, vh, vr, _) = k_pages.stride(), v_pages.stride()
     return SnapPaged(k_pages.shape[2], k_pages.shape[0], page_table.shape[1], 0, kp, kh, kr, vp, vh, vr)
-
-
-def _paged_ok(cfg, paged, dt, dev, k_pages, v_pages, page_table, seq_len, status) -> bool:
-    pages, heads, rows = paged.n_pages, cfg.n_kv_heads, paged.page_tokens
-    return (k_pages.dtype is dt and v_pages.dtype is dt and k_pages.shape == (pages, heads, rows, cfg.d_qk) and
-            v_pages.shape == (pages, heads, rows, cfg.d_v) and v_pages.get_device() == dev and
-            k_pages.stride() == (paged.k_page_stride, paged.k_head_stride, paged.k_row_stride, 1) and
-            v_pages.stride() == (paged.v_page_stride, paged.v_head_stride, paged.v_row_stride, 1) and
-            _dense(page_table, _I32, (cfg.max_seqs, paged.max_pages), dev) and _dense(seq_len, _I32, (cfg.max_seqs,), dev) and
-            (status is None or _dense(status, _I32, status.shape, dev)))
 
 
 def _paged_named(cfg, paged, dt, k_pages, v_pages, page_table, seq_len, status):
@@ -506,26 +505,18 @@ def snap_paged_append(cfg: SnapConfig, paged: SnapPaged, slot_ids_dev, rows_dev,
                       status=None, stream=None) -> None:
     """Write the rows of k [T, Hkv, d_qk], v [T, Hkv, d_v] into the pages, rotated on the way when rope is given; rows_dev
     None: each token is its sequence's next row.  q -> q_out and k_out: the rotated queries and keys, dense."""
-    where, dt, n, dev = "snap_paged_append", _DTYPES.get(cfg.dtype), slot_ids_dev.shape[0], k_pages.get_device()
-    hq, hkv, d, one = cfg.n_q_heads, cfg.n_kv_heads, cfg.d_qk, (n,)
-    sq, sk, sv = (n, hq, d), (n, hkv, d), (n, hkv, cfg.d_v)
-    sf = None if rope is None else (rope.rot_dim // 2,)
-    if not (_paged_ok(cfg, paged, dt, dev, k_pages, v_pages, page_table, seq_len, status) and _dense(slot_ids_dev, _I32, one, dev) and
-            _rows(k, dt, sk, dev) and _rows(v, dt, sv, dev) and (rows_dev is None or _dense(rows_dev, _I32, one, dev)) and
-            (rope is None or freqs is None or _dense(freqs, _F64, sf, dev)) and
-            (positions is None or _dense(positions, _I32, one, dev)) and (q is None or _rows(q, dt, sq, dev)) and
-            (q_out is None or _dense(q_out, dt, sq, dev)) and (k_out is None or _dense(k_out, dt, sk, dev)) and
-            (weights is None or _dense(weights, _F32, _weights_shape(cfg, paged), dev))):
-        _refuse(where, dev, ("slot_ids", slot_ids_dev, _I32, one, True), ("rows", rows_dev, _I32, one, True),
-                ("freqs", None if rope is None else freqs, _F64, sf, True), ("positions", positions, _I32, one, True),
-                ("q", q, dt, sq, False), ("q_out", q_out, dt, sq, True), ("k", k, dt, sk, False), ("k_out", k_out, dt, sk, True),
-                ("v", v, dt, sv, False), ("weights", weights, _F32, _weights_shape(cfg, paged), True),
-                *_paged_named(cfg, paged, dt, k_pages, v_pages, page_table, seq_len, status))
-    _check(lib().snap_paged_append(C.byref(cfg), C.byref(paged), slot_ids_dev.data_ptr(), _ptr(rows_dev), n,
-                                   None if rope is None else C.byref(rope), _ptr(freqs), _ptr(positions), _ptr(q), *_strides(q),
-                                   _ptr(q_out), k.data_ptr(), *k.stride()[:2], _ptr(k_out), v.data_ptr(), *v.stride()[:2],
-                                   k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), seq_len.data_ptr(), _ptr(weights),
-                                   _ptr(status), _launch_stream(where, dev, stream)), where)
+    native, entry = _native or _calls()
+    status_code = native.paged_append(entry["snap_paged_append"], cfg, paged, slot_ids_dev, rows_dev, k, v, k_pages, v_pages, page_table,
+                                      seq_len, rope, freqs, positions, q, q_out, k_out, weights, status, _handle(stream))
+    if status_code != 0:
+        n, dt, hkv = slot_ids_dev.shape[0], _DTYPES.get(cfg.dtype), cfg.n_kv_heads
+        sq, sk, sv, one = (n, cfg.n_q_heads, cfg.d_qk), (n, hkv, cfg.d_qk), (n, hkv, cfg.d_v), (n,)
+        _answer(status_code, "snap_paged_append", lambda: (
+            ("slot_ids", slot_ids_dev, _I32, one, True), ("rows", rows_dev, _I32, one, True),
+            ("freqs", freqs, _F64, None if rope is None else (rope.rot_dim // 2,), True), ("positions", positions, _I32, one, True),
+            ("q", q, dt, sq, False), ("q_out", q_out, dt, sq, True), ("k", k, dt, sk, False), ("k_out", k_out, dt, sk, True),
+            ("v", v, dt, sv, False), ("weights", weights, _F32, _weights_shape(cfg, paged), True),
+            *_paged_named(cfg, paged, dt, k_pages, v_pages, page_table, seq_len, status)))
 
 
 def snap_paged_decode_workspace_bytes(cfg: SnapConfig, paged: SnapPaged, n_active: int, with_weights: bool = False) -> int:
@@ -539,21 +530,16 @@ def snap_paged_decode_attn(cfg: SnapConfig, paged: SnapPaged, q, slot_ids_dev, n
                            seq_len, out, workspace, weights_in=None, weights_out=None, status=None, stream=None) -> None:
     """Attention of one token per sequence, q [n, Hq, d_qk] -> out [n, Hq, d_v], over the rows in its pages; weights_out
     [max_seqs, Hkv, max_pages * page_tokens] float32 receives weights_in (None = 0) plus the group's softmax weights."""
-    where, dt, n, dev = "snap_paged_decode_attn", _DTYPES.get(cfg.dtype), int(n_active), k_pages.get_device()
-    sq, so = (n, cfg.n_q_heads, cfg.d_qk), (n, cfg.n_q_heads, cfg.d_v)
-    if not (_paged_ok(cfg, paged, dt, dev, k_pages, v_pages, page_table, seq_len, status) and _dense(q, dt, sq, dev) and
-            _dense(out, dt, so, dev) and _dense(slot_ids_dev, _I32, (n,), dev) and
-            (weights_in is None or _dense(weights_in, _F32, _weights_shape(cfg, paged), dev)) and
-            (weights_out is None or _dense(weights_out, _F32, _weights_shape(cfg, paged), dev)) and
-            workspace.is_contiguous() and workspace.get_device() == dev):
-        _refuse(where, dev, ("q", q, dt, sq, True), ("out", out, dt, so, True), ("slot_ids", slot_ids_dev, _I32, (n,), True),
-                ("weights_in", weights_in, _F32, _weights_shape(cfg, paged), True),
-                ("weights_out", weights_out, _F32, _weights_shape(cfg, paged), True), ("workspace", workspace, None, None, True),
-                *_paged_named(cfg, paged, dt, k_pages, v_pages, page_table, seq_len, status))
-    _check(lib().snap_paged_decode_attn(C.byref(cfg), C.byref(paged), q.data_ptr(), slot_ids_dev.data_ptr(), n, k_pages.data_ptr(),
-                                        v_pages.data_ptr(), page_table.data_ptr(), seq_len.data_ptr(), _ptr(weights_in),
-                                        _ptr(weights_out), out.data_ptr(), workspace.data_ptr(), workspace.nbytes, _ptr(status),
-                                        _launch_stream(where, dev, stream)), where)
+    native, entry = _native or _calls()
+    status_code = native.paged_decode_attn(entry["snap_paged_decode_attn"], cfg, paged, q, slot_ids_dev, n_active, k_pages, v_pages,
+                                           page_table, seq_len, out, workspace, weights_in, weights_out, status, _handle(stream))
+    if status_code != 0:
+        n, dt, sw = int(n_active), _DTYPES.get(cfg.dtype), _weights_shape(cfg, paged)
+        _answer(status_code, "snap_paged_decode_attn", lambda: (
+            ("q", q, dt, (n, cfg.n_q_heads, cfg.d_qk), True), ("out", out, dt, (n, cfg.n_q_heads, cfg.d_v), True),
+            ("slot_ids", slot_ids_dev, _I32, (n,), True), ("weights_in", weights_in, _F32, sw, True),
+            ("weights_out", weights_out, _F32, sw, True), ("workspace", workspace, None, None, True),
+            *_paged_named(cfg, paged, dt, k_pages, v_pages, page_table, seq_len, status)))
 
 
 def snap_paged_evict_workspace_bytes(cfg: SnapConfig, paged: SnapPaged, n_seqs: int) -> int:
@@ -567,17 +553,14 @@ def snap_paged_evict(cfg: SnapConfig, paged: SnapPaged, src_slots_dev, dst_slots
                      seq_len, weights_in, weights_out, workspace, kept_rows=None, status=None, stream=None) -> None:
     """Copy the rows that stay (sinks, the topk of the middle by weight, the recent ones) of each source slot to its
     destination slot's pages; kept_rows [n, Hkv, l_sink + topk + l_recent] int32 receives their source rows."""
-    where, dt, n, dev = "snap_paged_evict", _DTYPES.get(cfg.dtype), int(n_seqs), k_pages.get_device()
-    sk, sw = (n, cfg.n_kv_heads, cfg.l_sink + cfg.topk + cfg.l_recent), _weights_shape(cfg, paged)
-    if not (_paged_ok(cfg, paged, dt, dev, k_pages, v_pages, page_table, seq_len, status) and _dense(src_slots_dev, _I32, (n,), dev) and
-            _dense(dst_slots_dev, _I32, (n,), dev) and _dense(weights_in, _F32, sw, dev) and
-            (weights_out is None or _dense(weights_out, _F32, sw, dev)) and (kept_rows is None or _dense(kept_rows, _I32, sk, dev)) and
-            workspace.is_contiguous() and workspace.get_device() == dev):
-        _refuse(where, dev, ("src_slots", src_slots_dev, _I32, (n,), True), ("dst_slots", dst_slots_dev, _I32, (n,), True),
-                ("weights_in", weights_in, _F32, sw, True), ("weights_out", weights_out, _F32, sw, True),
-                ("kept_rows", kept_rows, _I32, sk, True), ("workspace", workspace, None, None, True),
-                *_paged_named(cfg, paged, dt, k_pages, v_pages, page_table, seq_len, status))
-    _check(lib().snap_paged_evict(C.byref(cfg), C.byref(paged), src_slots_dev.data_ptr(), dst_slots_dev.data_ptr(), n, k_pages.data_ptr(),
-                                  v_pages.data_ptr(), page_table.data_ptr(), seq_len.data_ptr(), weights_in.data_ptr(),
-                                  _ptr(weights_out), _ptr(kept_rows), workspace.data_ptr(), workspace.nbytes, _ptr(status),
-                                  _launch_stream(where, dev, stream)), where)
+    native, entry = _native or _calls()
+    status_code = native.paged_evict(entry["snap_paged_evict"], cfg, paged, src_slots_dev, dst_slots_dev, n_seqs, k_pages, v_pages,
+                                     page_table, seq_len, weights_in, weights_out, workspace, kept_rows, status, _handle(stream))
+    if status_code != 0:
+        n, dt, sw = int(n_seqs), _DTYPES.get(cfg.dtype), _weights_shape(cfg, paged)
+        _answer(status_code, "snap_paged_evict", lambda: (
+            ("src_slots", src_slots_dev, _I32, (n,), True), ("dst_slots", dst_slots_dev, _I32, (n,), True),
+            ("weights_in", weights_in, _F32, sw, True), ("weights_out", weights_out, _F32, sw, True),
+            ("kept_rows", kept_rows, _I32, (n, cfg.n_kv_heads, cfg.l_sink + cfg.topk + cfg.l_recent), True),
+            ("workspace", workspace, None, None, True),
+            *_paged_named(cfg, paged, dt, k_pages, v_pages, page_table, seq_len, status)))

@@ -4,6 +4,8 @@
 
 Each csrc/*.cu is compiled to an object under csrc/build/ (in parallel, only when its
 sources are newer) and the objects are linked into paper_2511_03092_b200/libsnapstream.so.
+csrc/marshal.cpp becomes paper_2511_03092_b200/_marshal.so, the module that passes torch tensors to the
+rotary and paged-cache entry points (built against the installed torch; it knows the library only by address).
 nvcc cross-compiles, so this works on a machine without a GPU.
 --debug-bounds builds the checked variant instead (-DSNAP_DEBUG_BOUNDS: data-dependent indices are
 tested and a bad one raises a status bit instead of an access; objects under csrc/build_dbg/) as
@@ -23,6 +25,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(CSRC, "build")
 LIB = os.path.join(PKG, "libsnapstream.so")
+MARSHAL = os.path.join(PKG, "_marshal.so")
 
 ARCH = ["-gencode", "arch=compute_100a,code=sm_100a"]
 COMMON = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC",
@@ -38,6 +41,29 @@ def _nvcc() -> str:
 
 def _newest(paths) -> float:
     return max(os.path.getmtime(p) for p in paths)
+
+
+def build_marshal(force: bool = False, verbose: bool = False) -> str:
+    import sysconfig
+    import torch
+    src = os.path.join(CSRC, "marshal.cpp")
+    torch_dir = os.path.dirname(torch.__file__)
+    newest = _newest([src, os.path.join(ROOT, "include", "snapstream.h"), os.path.join(torch_dir, "version.py")])
+    if not force and os.path.exists(MARSHAL) and os.path.getmtime(MARSHAL) >= newest:
+        return MARSHAL
+    cuda = os.path.dirname(os.path.dirname(os.path.realpath(_nvcc())))
+    inc = [os.path.join(torch_dir, "include"), os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"),
+           sysconfig.get_paths()["include"], os.path.join(cuda, "include"), os.path.join(ROOT, "include")]
+    lib = os.path.join(torch_dir, "lib")
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           *[f"-isystem{d}" for d in inc[:-1]], "-I", inc[-1], src, "-o", MARSHAL, "-L", lib, "-lc10", "-lc10_cuda", "-ltorch_cpu",
+           "-ltorch_python", f"-Wl,-rpath,{lib}"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if verbose or r.returncode != 0:
+        sys.stderr.write(" ".join(cmd) + "\n" + r.stdout + r.stderr)
+    if r.returncode != 0:
+        raise RuntimeError("g++ failed for marshal.cpp")
+    return MARSHAL
 
 
 def build(force: bool = False, verbose: bool = False, debug_bounds: bool = False) -> str:
@@ -79,6 +105,7 @@ def build(force: bool = False, verbose: bool = False, debug_bounds: bool = False
         if r.returncode != 0:
             sys.stderr.write(r.stdout + r.stderr)
             raise RuntimeError("link failed")
+    build_marshal(force and not debug_bounds, verbose)
     return lib
 
 
