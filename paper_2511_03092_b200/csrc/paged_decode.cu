@@ -18,9 +18,10 @@
 // numbers (p and what its rounding left), which keeps their rounding out of the result: 2^-17 instead of 2^-9.
 //
 // Portable kernel (fp32, other heads, pages of any size): the same pipelines per warp over tiles of eight rows, brought in
-// by bulk copies (one per row, or one for all where they lie together); a lane holds four dims of a row; the 8 x heads
-// partial dot products are reduced by halving exchanges (after which a lane owns one (row, head) pair: one shuffle per
-// pair instead of five) and every lane does one exponential.
+// by bulk copies (one per row, or one for all where they lie together); a lane holds four dims of a row.  Four rows at a
+// time, the 4 x heads partial dot products are reduced by halving exchanges, after which a lane owns one (row, head)
+// pair: one shuffle per pair instead of five, one exponential per lane.  (Eight rows at a time need twice the code for
+// the same work; a step of short sequences runs through it once, at the speed at which instructions arrive.)
 //
 // With weights, the split kernel also stores the logits, and CTAs of the second launch turn them into the group's
 // attention weight of each row once the unit's maximum and sum are known.
@@ -61,7 +62,7 @@ struct PagedArgs {
   const float* w_in; float* w_out;
   uint32_t* status;
   int ctas;
-  int stages, joined;                           // portable kernel: stages of a warp; 1, 2: a tile's key, value rows lie together
+  int stages, tiled;                            // portable kernel: stages of a warp; tiles come through the tensor maps
 };
 
 __device__ __forceinline__ int rows_of(const PagedArgs& a, int slot) {
@@ -139,10 +140,9 @@ __device__ __forceinline__ int2 read_entry(const PagedArgs& a, int e, unsigned& 
 
 // All threads of the CTA: the place of its first tile and the end of its stretch (both counted from that tile's unit).
 // Returns false (to all) when it has none.  CTA 0 also writes the prefix array and reports bad slots and lengths.
-// Up to MAX_HELD sequences every warp does all of it by itself (no barrier; the shared copies are written by all warps
-// alike), with more the CTA does it together.
-template <int ROWS, int NT>
-__device__ __forceinline__ bool locate(const PagedArgs& a, Place& p, int& end, Held& held, int* scan /* shared, NT / 32 + 2 */) {
+// Up to MAX_HELD sequences the first warp does it (its result handed over in shared memory: a dozen warps of an SM doing the same would wait for one another), with more the CTA together.
+template <int ROWS, int NT, bool SMALL>
+__device__ __forceinline__ bool locate_part(const PagedArgs& a, Place& p, int& end, Held& held, int* scan /* shared, NT / 32 + 2 */) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, c = blockIdx.x;
   unsigned bad = 0;
   int total = 0, e_at = 0, before_at = 0;
@@ -156,7 +156,7 @@ __device__ __forceinline__ bool locate(const PagedArgs& a, Place& p, int& end, H
     x1 = stretch_begin(W, active, c + 1);
     return true;
   };
-  if (a.n <= MAX_HELD) {
+  if (SMALL) {
     const int per = (a.n + 31) / 32, e0 = min(lane * per, a.n), e1 = min(e0 + per, a.n);   // a lane's sequences
     int mine = 0;
 #pragma unroll 1
@@ -168,7 +168,7 @@ __device__ __forceinline__ bool locate(const PagedArgs& a, Place& p, int& end, H
     const int incl = warp_inclusive(mine, lane);
     int before = incl - mine;
     total = __shfl_sync(0xffffffffu, incl, 31);
-    if (c == 0 && warp == 0) {
+    if (c == 0) {
       int at = before;
 #pragma unroll 1
       for (int e = e0; e < e1; ++e) { a.prefix[e] = at; at += length_of(tiles_of<ROWS>(held.e[e].y)); }
@@ -238,6 +238,19 @@ __device__ __forceinline__ bool locate(const PagedArgs& a, Place& p, int& end, H
     if (p.e >= a.n || end <= 0) return false;
   }
   return true;
+}
+struct Found { Place p; int end, any; };
+template <int ROWS, int NT>
+__device__ __forceinline__ bool locate(const PagedArgs& a, Place& p, int& end, Held& held, int* scan, Found& found /* shared */) {
+  if (a.n > MAX_HELD) return locate_part<ROWS, NT, false>(a, p, end, held, scan);
+  if (threadIdx.x < 32) {
+    const bool any = locate_part<ROWS, NT, true>(a, p, end, held, scan);
+    if (threadIdx.x == 0) { found.any = any; found.p = p; found.end = end; }
+  }
+  __syncthreads();
+  p = found.p;
+  end = found.end;
+  return found.any;
 }
 // Tiles of the unit at p, from p.t on, that begin before the end of the stretch: the end of that range of tiles
 __device__ __forceinline__ int segment_end(const Place& p, int end) {
@@ -317,6 +330,7 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
   float* jl = jm + NCOL;
   __shared__ int scan[S::NT / 32 + 2];
   __shared__ Held held;
+  __shared__ Found found;
 
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, gq = lane >> 2, tq = lane & 3;
   unsigned char* wstages = stages + w * NSTAGE * S::STAGE_B;
@@ -335,7 +349,7 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
 
   Place at;
   int end;
-  if (!locate<TR, S::NT>(a, at, end, held, scan)) return;
+  if (!locate<TR, S::NT>(a, at, end, held, scan, found)) return;
 
   // ---- the warp's producer: runs NSTAGE tiles ahead of the consumer, over unit borders; warp w takes the CTA's tiles
   // w, w + NWARP, ... ----
@@ -463,8 +477,11 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
             const int row = row0 + gq + 8 * r8;
             if (row >= at.len) continue;                                 // (a bad page's rows are written: as -inf)
             float* sp = srow + (long long)row * a.gb + col;
-            if (col < nh) sp[0] = v[gi][2 * r8];
-            if (col + 1 < nh) sp[1] = v[gi][2 * r8 + 1];
+            if (a.gb % 2 == 0 && col < nh) *reinterpret_cast<float2*>(sp) = make_float2(v[gi][2 * r8], v[gi][2 * r8 + 1]);   // (nh may end between them)
+            else {
+              if (col < nh) sp[0] = v[gi][2 * r8];
+              if (col + 1 < nh) sp[1] = v[gi][2 * r8 + 1];
+            }
           }
         }
       }
@@ -600,12 +617,22 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
 // ---------------------------------------------------------------------------------------------------------------
 // portable kernel
 // ---------------------------------------------------------------------------------------------------------------
-template <typename T> __device__ __forceinline__ float4 four(const T* p);      // four consecutive elements
-template <> __device__ __forceinline__ float4 four<float>(const float* p) { return *reinterpret_cast<const float4*>(p); }
-template <> __device__ __forceinline__ float4 four<__nv_bfloat16>(const __nv_bfloat16* p) {
+// Two single-precision numbers in one register pair: sm_100a multiplies and adds them in one instruction.
+using F2 = unsigned long long;
+__device__ __forceinline__ F2 pack2(float x, float y) { F2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y)); return r; }
+__device__ __forceinline__ float2 unpack2(F2 v) { float2 r; asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v)); return r; }
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) { F2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+struct Four { F2 a, b; };                          // four consecutive elements
+template <typename T> __device__ __forceinline__ Four four(const T* p);
+template <> __device__ __forceinline__ Four four<float>(const float* p) {
+  const ulonglong2 r = *reinterpret_cast<const ulonglong2*>(p);
+  return {r.x, r.y};
+}
+template <> __device__ __forceinline__ Four four<__nv_bfloat16>(const __nv_bfloat16* p) {
   const uint2 r = *reinterpret_cast<const uint2*>(p);
-  return make_float4(__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xffff0000u), __uint_as_float(r.y << 16),
-                     __uint_as_float(r.y & 0xffff0000u));
+  return {pack2(__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xffff0000u)),
+          pack2(__uint_as_float(r.y << 16), __uint_as_float(r.y & 0xffff0000u))};
 }
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, unsigned bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
@@ -617,15 +644,18 @@ constexpr int MAX_STAGES = 6;                     // of a warp
 
 // NV: 128-dim chunks of a row, HB: heads of a unit (a power of two)
 template <typename T, int NV, int HB, int CTAS>
-__global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_constant__ PagedArgs a) {
+__global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v) {
   constexpr int LD = 128 * NV + 4;
-  constexpr int NVAL = 8 * HB, VPL = NVAL > 32 ? NVAL / 32 : 1;          // (row, head) values of a tile; per lane after the exchange
-  extern __shared__ __align__(128) unsigned char stages[];               // [SNW][a.stages][8 key rows | 8 value rows]
+  constexpr int NVAL = 4 * HB, HL = 8 / HB;                              // (row, head) pairs of four rows; lanes that hold the same pair
+  extern __shared__ unsigned char smem_dyn[];
+  // [SNW][a.stages][8 key rows | 8 value rows], on a 128-byte boundary as every part of it is (rows are multiples of 32 bytes)
+  unsigned char* stages = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 127) & ~uintptr_t(127));
   __shared__ __align__(16) float buf[2 * HB * LD];
   __shared__ float wm[SNW * HB], wl[SNW * HB], jm[HB], jl[HB];
   __shared__ uint64_t bars[SNW * MAX_STAGES];
   __shared__ int scan[SNT / 32 + 2];
   __shared__ Held held;
+  __shared__ Found found;
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
   const unsigned krow_b = a.d_qk * sizeof(T), vrow_b = a.d_v * sizeof(T), stage_b = STR * (krow_b + vrow_b);
   const unsigned char* wstages = stages + w * a.stages * stage_b;
@@ -639,9 +669,8 @@ __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_cons
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   Place at;
   int end;
-  if (!locate<STR, SNT>(a, at, end, held, scan)) return;
-  // After the exchange lane l owns row l / 4 of the tile and head (or heads) my_head (+ 1).
-  const int my_head = HB >= 8 ? 2 * (lane & 3) : HB == 4 ? (lane & 3) : HB == 2 ? ((lane & 3) >> 1) : 0;
+  if (!locate<STR, SNT>(a, at, end, held, scan, found)) return;
+  const int my_head = (lane & 7) / HL;                                   // after the exchange lane l owns row l / 8 and this head
 
   // ---- the warp's producer: lane l looks up row l % 8 of the warp's tile l / 8, l / 8 + 4, ... ----
   Place pr = at;
@@ -669,17 +698,22 @@ __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_cons
     const unsigned okay = (__ballot_sync(0xffffffffu, pid >= 0) >> (8 * next)) & 0xffu;
     okay_of = (okay_of & ~(0xffull << (8 * s_in))) | ((unsigned long long)okay << (8 * s_in));
     const uint32_t bar = bar0 + 8 * s_in, dst = stage0 + s_in * stage_b;
-    const int rows = __popc(okay), r = lane & 7;
-    if (lane == 0) mbar_expect_tx(bar, rows * (krow_b + vrow_b));
-    __syncwarp();
-    if (mine && pid >= 0) {
-      const T* ks = static_cast<const T*>(a.kp) + pid * a.map.kp + kvh_of * a.map.kh + prow * a.map.kr;
-      const T* vs = static_cast<const T*>(a.vp) + pid * a.map.vp + kvh_of * a.map.vh + prow * a.map.vr;
-      const uint32_t kd = dst + r * krow_b, vd = dst + STR * krow_b + r * vrow_b;
-      if (a.joined & 1) { if (r == 0) bulk_load(kd, ks, rows * krow_b, bar); }
-      else bulk_load(kd, ks, krow_b, bar);
-      if (a.joined & 2) { if (r == 0) bulk_load(vd, vs, rows * vrow_b, bar); }
-      else bulk_load(vd, vs, vrow_b, bar);
+    const int r = lane & 7;
+    if (a.tiled) {                                                       // one copy each for the tile's keys and values
+      if (mine && r == 0) {
+        mbar_expect_tx(bar, okay ? stage_b : 0u);
+        if (okay) {
+          tma_load_4d(dst, &tmap_k, 0, prow, kvh_of, pid, bar);
+          tma_load_4d(dst + STR * krow_b, &tmap_v, 0, prow, kvh_of, pid, bar);
+        }
+      }
+    } else {                                                             // a copy per row
+      if (lane == 0) mbar_expect_tx(bar, __popc(okay) * (krow_b + vrow_b));
+      __syncwarp();
+      if (mine && pid >= 0) {
+        bulk_load(dst + r * krow_b, static_cast<const T*>(a.kp) + pid * a.map.kp + kvh_of * a.map.kh + prow * a.map.kr, krow_b, bar);
+        bulk_load(dst + STR * krow_b + r * vrow_b, static_cast<const T*>(a.vp) + pid * a.map.vp + kvh_of * a.map.vh + prow * a.map.vr, vrow_b, bar);
+      }
     }
     ++in_flight;
     if (++s_in == a.stages) s_in = 0;
@@ -691,7 +725,7 @@ __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_cons
     }
   };
   fetch();
-  float q[HB][NV][4];
+  F2 q[HB][NV][2];
   const auto load_q = [&]() {
     const int kvh = at.u / a.nhb, hb = at.u - kvh * a.nhb, nh = min(a.gb, a.g - hb * a.gb);
     const T* qp = static_cast<const T*>(a.q) + ((long long)at.e * a.Hq + kvh * a.g + hb * a.gb) * a.d_qk + 4 * lane;
@@ -699,9 +733,9 @@ __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_cons
     for (int h = 0; h < HB; ++h)
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
-        float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+        Four f = {0, 0};
         if (h < nh && 4 * lane + 128 * j < a.d_qk) f = four<T>(qp + h * a.d_qk + 128 * j);
-        q[h][j][0] = f.x; q[h][j][1] = f.y; q[h][j][2] = f.z; q[h][j][3] = f.w;
+        q[h][j][0] = f.a; q[h][j][1] = f.b;
       }
   };
   load_q();                                                              // (the first tiles' look-ups wait alongside)
@@ -715,13 +749,12 @@ __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_cons
     const int tb = segment_end(at, end), cnt = tb - at.t;
     const int hb = at.u % a.nhb, nh = min(a.gb, a.g - hb * a.gb);
     const bool whole = cnt == at.nt;
-    float o[HB][NV][4], m_ref[VPL], l_part[VPL];
+    F2 o[HB][NV][2];
+    float m_ref = -INFINITY, l_part = 0.f;
 #pragma unroll
     for (int h = 0; h < HB; ++h)
 #pragma unroll
-      for (int j = 0; j < NV; ++j) o[h][j][0] = o[h][j][1] = o[h][j][2] = o[h][j][3] = 0.f;
-#pragma unroll
-    for (int k = 0; k < VPL; ++k) { m_ref[k] = -INFINITY; l_part[k] = 0.f; }
+      for (int j = 0; j < NV; ++j) o[h][j][0] = o[h][j][1] = 0;
     float* srow = a.scores ? a.scores + ((long long)at.e * a.U + at.u) * a.map.cap * a.gb : nullptr;
 
     for (; w + n * SNW < done + cnt && !dead; ++n) {
@@ -730,97 +763,89 @@ __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_cons
       --in_flight;
       const int row0 = (at.t + (w + n * SNW - done)) * STR;
       const unsigned okay = (unsigned)(okay_of >> (8 * s_out)) & 0xffu;
-      const T* kx = reinterpret_cast<const T*>(wstages + s_out * stage_b) + 4 * lane;
-      const T* vx = reinterpret_cast<const T*>(wstages + s_out * stage_b + STR * krow_b) + 4 * lane;
-      float s[NVAL];
+#pragma unroll 1
+      for (int r0 = 0; r0 < STR; r0 += 4) {
+        const unsigned there = (okay >> r0) & 0xfu;
+        if (there == 0u && !srow) continue;
+        const T* kx = reinterpret_cast<const T*>(wstages + s_out * stage_b) + r0 * a.d_qk + 4 * lane;
+        const T* vx = reinterpret_cast<const T*>(wstages + s_out * stage_b + STR * krow_b) + r0 * a.d_v + 4 * lane;
+        float s[NVAL];
 #pragma unroll
-      for (int r = 0; r < 8; ++r) {
-        float4 f[NV];
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-          f[j] = 4 * lane + 128 * j < a.d_qk ? four<T>(kx + r * a.d_qk + 128 * j) : make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int h = 0; h < HB; ++h) {
-          float x = 0.f;
+        for (int r = 0; r < 4; ++r) {
+          Four f[NV];
 #pragma unroll
           for (int j = 0; j < NV; ++j) {
-            x = fmaf(f[j].x, q[h][j][0], x); x = fmaf(f[j].y, q[h][j][1], x);
-            x = fmaf(f[j].z, q[h][j][2], x); x = fmaf(f[j].w, q[h][j][3], x);
+            f[j] = {0, 0};
+            if (4 * lane + 128 * j < a.d_qk) f[j] = four<T>(kx + r * a.d_qk + 128 * j);
           }
-          s[r * HB + h] = x;
-        }
-      }
-      // halving exchange: each step sums over one lane bit and leaves a lane half of the values
-      int left = NVAL;
 #pragma unroll
-      for (int b = 16; b > 0; b >>= 1) {
-        if (left > 1) {
-          left >>= 1;
+          for (int h = 0; h < HB; ++h) {
+            F2 x = mul2(f[0].a, q[h][0][0]);
+            x = fma2(f[0].b, q[h][0][1], x);
 #pragma unroll
-          for (int x = 0; x < NVAL / 2; ++x)
-            if (x < left) {
-              const bool up = lane & b;
-              const float give = up ? s[x] : s[x + left], keep = up ? s[x + left] : s[x];
-              s[x] = keep + __shfl_xor_sync(0xffffffffu, give, b);
+            for (int j = 1; j < NV; ++j) {
+              x = fma2(f[j].a, q[h][j][0], x);
+              x = fma2(f[j].b, q[h][j][1], x);
             }
-        } else {
-          s[0] += __shfl_xor_sync(0xffffffffu, s[0], b);
+            const float2 y = unpack2(x);
+            s[r * HB + h] = y.x + y.y;
+          }
         }
-      }
-      const int row = row0 + (lane >> 2);
-      const bool ok = (okay >> (lane >> 2)) & 1u;                        // rows that are not there hold anything
-      float v[VPL];
-      bool refresh = false;
+        // halving exchange: each step sums over one lane bit and leaves a lane half of the values
+        int left = NVAL;
 #pragma unroll
-      for (int k = 0; k < VPL; ++k) {
-        v[k] = ok ? s[k] * a.scale_log2 : -INFINITY;
-        refresh = refresh || v[k] > m_ref[k] + 8.f;
-      }
-      if (srow && row < at.len) {
-        // HB = 2 and 1: the pairs are held by two and four lanes, all writing the same value
+        for (int b = 16; b > 0; b >>= 1) {
+          if (left > 1) {
+            left >>= 1;
 #pragma unroll
-        for (int k = 0; k < VPL; ++k)
-          if (my_head + k < nh) srow[(long long)row * a.gb + my_head + k] = v[k];
-      }
-      if (__any_sync(0xffffffffu, refresh)) {                            // the reference moves lazily, as in the kernel above
-        float al[VPL];
-#pragma unroll
-        for (int k = 0; k < VPL; ++k) {
-          float mx = v[k];
-#pragma unroll
-          for (int b = 4; b <= 16; b <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, b));
-          const float nm = fmaxf(m_ref[k], mx);
-          al[k] = m_ref[k] == -INFINITY ? 0.f : exp2f(m_ref[k] - nm);
-          m_ref[k] = nm;
-          l_part[k] *= al[k];
+            for (int x = 0; x < NVAL / 2; ++x)
+              if (x < left) {
+                const bool up = lane & b;
+                const float give = up ? s[x] : s[x + left], keep = up ? s[x + left] : s[x];
+                s[x] = keep + __shfl_xor_sync(0xffffffffu, give, b);
+              }
+          } else {
+            s[0] += __shfl_xor_sync(0xffffffffu, s[0], b);
+          }
         }
+        // rows that are not there hold anything
+        const float v = (there >> (lane >> 3)) & 1u ? s[0] * a.scale_log2 : -INFINITY;
+        const int row = row0 + r0 + (lane >> 3);
+        if (srow && row < at.len && my_head < nh) srow[(long long)row * a.gb + my_head] = v;   // (lanes of one pair write the same)
+        if (__any_sync(0xffffffffu, v > m_ref + 8.f)) {                    // the reference moves lazily, as in the kernel above
+          float mx = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+          const float nm = fmaxf(m_ref, mx), al = m_ref == -INFINITY ? 0.f : exp2f(m_ref - nm);
+          m_ref = nm;
+          l_part *= al;
 #pragma unroll
-        for (int h = 0; h < HB; ++h) {
-          const float f = __shfl_sync(0xffffffffu, al[HB >= 8 ? (h & 1) : 0], HB >= 8 ? h / 2 : HB == 4 ? h : HB == 2 ? 2 * h : 0);
+          for (int h = 0; h < HB; ++h) {
+            const float f = __shfl_sync(0xffffffffu, al, h * HL);
+            const F2 f2 = pack2(f, f);
 #pragma unroll
-          for (int j = 0; j < NV; ++j) { o[h][j][0] *= f; o[h][j][1] *= f; o[h][j][2] *= f; o[h][j][3] *= f; }
+            for (int j = 0; j < NV; ++j) { o[h][j][0] = mul2(o[h][j][0], f2); o[h][j][1] = mul2(o[h][j][1], f2); }
+          }
         }
-      }
-      float p[VPL];
+        const float p = fast_exp2(v - (m_ref == -INFINITY ? 0.f : m_ref));
+        l_part += p;
 #pragma unroll
-      for (int k = 0; k < VPL; ++k) {
-        p[k] = fast_exp2(v[k] - (m_ref[k] == -INFINITY ? 0.f : m_ref[k]));
-        l_part[k] += p[k];
-      }
-#pragma unroll
-      for (int r = 0; r < 8; ++r) {
-        if (!((okay >> r) & 1u)) continue;                               // a zero probability does not silence a NaN
-        float4 f[NV];
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-          f[j] = 4 * lane + 128 * j < a.d_v ? four<T>(vx + r * a.d_v + 128 * j) : make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int h = 0; h < HB; ++h) {
-          const float x = __shfl_sync(0xffffffffu, p[HB >= 8 ? (h & 1) : 0], 4 * r + (HB >= 8 ? h / 2 : HB == 4 ? h : HB == 2 ? 2 * h : 0));
+        for (int r = 0; r < 4; ++r) {
+          if (!((there >> r) & 1u)) continue;                              // a zero probability does not silence a NaN
+          Four f[NV];
 #pragma unroll
           for (int j = 0; j < NV; ++j) {
-            o[h][j][0] = fmaf(x, f[j].x, o[h][j][0]); o[h][j][1] = fmaf(x, f[j].y, o[h][j][1]);
-            o[h][j][2] = fmaf(x, f[j].z, o[h][j][2]); o[h][j][3] = fmaf(x, f[j].w, o[h][j][3]);
+            f[j] = {0, 0};
+            if (4 * lane + 128 * j < a.d_v) f[j] = four<T>(vx + r * a.d_v + 128 * j);
+          }
+#pragma unroll
+          for (int h = 0; h < HB; ++h) {
+            const float x = __shfl_sync(0xffffffffu, p, 8 * r + h * HL);
+            const F2 x2 = pack2(x, x);
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+              o[h][j][0] = fma2(x2, f[j].a, o[h][j][0]);
+              o[h][j][1] = fma2(x2, f[j].b, o[h][j][1]);
+            }
           }
         }
       }
@@ -830,30 +855,30 @@ __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_cons
     }
 
     // ---- join the warps ----
-#pragma unroll
-    for (int k = 0; k < VPL; ++k) {
-#pragma unroll
-      for (int b = 4; b <= 16; b <<= 1) l_part[k] += __shfl_xor_sync(0xffffffffu, l_part[k], b);
-      if (lane < 4) { wm[w * HB + my_head + k] = m_ref[k]; wl[w * HB + my_head + k] = l_part[k]; }   // (equal values where lanes share a head)
-    }
+    l_part += __shfl_xor_sync(0xffffffffu, l_part, 8);
+    l_part += __shfl_xor_sync(0xffffffffu, l_part, 16);
+    if (lane < 8) { wm[w * HB + my_head] = m_ref; wl[w * HB + my_head] = l_part; }   // (equal values where lanes share a head)
     __syncthreads();
 #pragma unroll
     for (int h = 0; h < HB; ++h) {
       float M = -INFINITY;
 #pragma unroll
       for (int ww = 0; ww < SNW; ++ww) M = fmaxf(M, wm[ww * HB + h]);
-      const float mw = wm[w * HB + h], f = mw == -INFINITY ? 0.f : exp2f(mw - M);
+      const float mw = wm[w * HB + h], f = mw == -INFINITY ? 0.f : fast_exp2(mw - M);
+      const F2 f2 = pack2(f, f);
 #pragma unroll
-      for (int j = 0; j < NV; ++j) { o[h][j][0] *= f; o[h][j][1] *= f; o[h][j][2] *= f; o[h][j][3] *= f; }
-      if (tid == h) {
-        float L = 0.f;
+      for (int j = 0; j < NV; ++j) { o[h][j][0] = mul2(o[h][j][0], f2); o[h][j][1] = mul2(o[h][j][1], f2); }
+    }
+    if (tid < HB) {
+      float M = -INFINITY, L = 0.f;
 #pragma unroll
-        for (int ww = 0; ww < SNW; ++ww) {
-          const float lw = wl[ww * HB + h];
-          L += lw == 0.f ? 0.f : lw * exp2f(wm[ww * HB + h] - M);
-        }
-        jm[h] = M; jl[h] = L;
+      for (int ww = 0; ww < SNW; ++ww) M = fmaxf(M, wm[ww * HB + tid]);
+#pragma unroll
+      for (int ww = 0; ww < SNW; ++ww) {
+        const float lw = wl[ww * HB + tid];
+        L += lw == 0.f ? 0.f : lw * fast_exp2(wm[ww * HB + tid] - M);
       }
+      jm[tid] = M; jl[tid] = L;
     }
 #pragma unroll 1
     for (int lower = 0; lower < 2; ++lower) {
@@ -864,7 +889,8 @@ __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_cons
 #pragma unroll
           for (int j = 0; j < NV; ++j) {
             float4* x = reinterpret_cast<float4*>(b + h * LD + 128 * j);
-            float4 f = make_float4(o[h][j][0], o[h][j][1], o[h][j][2], o[h][j][3]);
+            const float2 f0 = unpack2(o[h][j][0]), f1 = unpack2(o[h][j][1]);
+            float4 f = make_float4(f0.x, f0.y, f1.x, f1.y);
             if (lower) { const float4 y = *x; f.x += y.x; f.y += y.y; f.z += y.z; f.w += y.w; }
             *x = f;
           }
@@ -904,89 +930,134 @@ __device__ __forceinline__ Pieces pieces_of(const PagedArgs& a, int u, int befor
 }
 __device__ __forceinline__ int piece_at(const Pieces& p, int k) { return 2 * (p.c0 + k) + (k == 0); }
 
+// Grid: `joins` CTAs for the outputs, then the weights'.  The outputs go either by query head (a CTA each: the shorter way
+// to the pieces), or, where there are many heads, by the borders between the stretches of the first launch: the unit that
+// a border cuts is joined by the CTAs of the borders that cut it, which take its heads in turn, so that no more CTAs
+// than borders are started however many units there are.  (By heads against by borders: one sequence of 5124 rows, 32
+// heads 11.4 / 13.1 us a call; 16 sequences, 512 heads 332 / 335; 48 short ones, 1536 heads 25.2 / 22.0.)
+//
+// This kernel lets the next one start only when it ends: blocks of the split kernel that start beside blocks of this
+// one get the registers in between them, and once these end the rest of an SM's registers is in pieces too small for
+// the third block, which then waits for a whole stretch to end (16 long sequences: 366 instead of 332 us a call).
 template <typename T>
-__global__ void __launch_bounds__(JNT) paged_join_kernel(const __grid_constant__ PagedArgs a) {
+__global__ void __launch_bounds__(JNT) paged_join_kernel(const __grid_constant__ PagedArgs a, int joins, int by_heads) {
   __shared__ __align__(16) float acc_s[JNT / 32][256];
   __shared__ float red_m[JNT / 32], red_l[JNT / 32];
   __shared__ float mu_s[16];
+  __shared__ int s_e;
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+  if (tid == 0) s_e = -1;
   pdl_wait();
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const int merges = a.n * a.Hq;
-  if ((int)blockIdx.x < merges) {
-    // ---- one query head's output ----
-    const int e = blockIdx.x / a.Hq, head = blockIdx.x - e * a.Hq;
-    const int kvh = head / a.g, x = head - kvh * a.g, hb = x / a.gb, col = x - hb * a.gb;
-    const int before = a.prefix[e], line = a.prefix[a.n], nt = max(a.prefix[e + 1] - before - UNIT_TILES, 0);
-    T* out = static_cast<T*>(a.out) + (long long)blockIdx.x * a.d_v;
-    if (nt == 0) {
-      for (int c = tid; c < a.d_v; c += JNT) out[c] = from_f32<T>(0.f);
-      return;
+  const int line = a.prefix[a.n];
+  if ((int)blockIdx.x < joins) {
+    int e, u, nt, col0, step;
+    Pieces p;
+    const auto zero = [&](int row, int rows) {                             // outputs of a sequence without rows
+      T* out = static_cast<T*>(a.out) + (long long)row * a.d_v;
+      for (int x = tid; x < rows * a.d_v; x += JNT) out[x] = from_f32<T>(0.f);
+    };
+    if (by_heads) {
+      e = blockIdx.x / a.Hq;
+      const int head = blockIdx.x - e * a.Hq, kvh = head / a.g, x = head - kvh * a.g, hb = x / a.gb;
+      u = kvh * a.nhb + hb;
+      col0 = x - hb * a.gb;
+      step = a.gb;
+      const int before = a.prefix[e];
+      nt = a.prefix[e + 1] - before - UNIT_TILES;
+      if (nt <= 0) { zero(blockIdx.x, 1); return; }
+      p = pieces_of(a, u, before, line, nt);
+      if (p.np <= 1) return;                                               // written by the split kernel
+    } else {
+      for (int i = blockIdx.x; i < a.n; i += joins)
+        if (a.prefix[i + 1] == a.prefix[i]) zero(i * a.Hq, a.Hq);
+      const long long W = (long long)line * a.U;
+      const int active = active_ctas(W, a.ctas), c = blockIdx.x + 1;
+      if (c >= active) return;
+      const long long x = stretch_begin(W, active, c);
+      __syncthreads();
+      for (int i = tid; i < a.n; i += JNT)                                 // one thread has it
+        if ((long long)a.prefix[i] * a.U <= x && x < (long long)a.prefix[i + 1] * a.U) s_e = i;
+      __syncthreads();
+      e = s_e;
+      if (e < 0) return;                                                   // (only if the lengths change during the call)
+      const int before = a.prefix[e], unit = a.prefix[e + 1] - before;
+      const long long rel = x - (long long)before * a.U;
+      nt = unit - UNIT_TILES;
+      u = rel < (1LL << 31) ? (int)((unsigned)rel / (unsigned)unit) : (int)(rel / unit);
+      p = pieces_of(a, u, before, line, nt);
+      // the unit's pieces are those of the CTAs c0 .. c0 + np - 1: the border before CTA c0 + k is its k-th
+      const int kth = c - p.c0;
+      if (p.np <= 1 || kth < 1 || kth >= p.np) return;                     // not cut, or cut elsewhere
+      col0 = kth - 1;
+      step = p.np - 1;
     }
-    const Pieces p = pieces_of(a, kvh * a.nhb + hb, before, line, nt);
-    if (p.np <= 1) return;
-    // a warp takes every eighth piece, four at a time: their (max, sum) and outputs come in together
-    float m = -INFINITY, l = 0.f;
-    float4 acc[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
-    for (int k0 = w; k0 < p.np; k0 += 4 * (JNT / 32)) {
-      float2 ml[4];
-      float4 v[4][2];
+    const int kvh = u / a.nhb, hb = u - kvh * a.nhb, nh = min(a.gb, a.g - hb * a.gb);
+    for (int col = col0; col < nh; col += step) {
+      // a warp takes every eighth piece, four at a time: their (max, sum) and outputs come in together
+      float m = -INFINITY, l = 0.f;
+      float4 acc[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
+      for (int k0 = w; k0 < p.np; k0 += 4 * (JNT / 32)) {
+        float2 ml[4];
+        float4 v[4][2];
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const int k = k0 + x * (JNT / 32);
-        ml[x] = make_float2(-INFINITY, 0.f);
-        if (k < p.np) ml[x] = a.ml_part[(long long)piece_at(p, k) * a.gb + col];
-        const float* o = a.o_part + ((long long)piece_at(p, k < p.np ? k : 0) * a.gb + col) * a.d_v + 4 * lane;
+        for (int y = 0; y < 4; ++y) {
+          const int k = k0 + y * (JNT / 32);
+          ml[y] = make_float2(-INFINITY, 0.f);
+          if (k < p.np) ml[y] = a.ml_part[(long long)piece_at(p, k) * a.gb + col];
+          const float* o = a.o_part + ((long long)piece_at(p, k < p.np ? k : 0) * a.gb + col) * a.d_v + 4 * lane;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          v[x][j] = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (k < p.np && 4 * lane + 128 * j < a.d_v) v[x][j] = *reinterpret_cast<const float4*>(o + 128 * j);
+          for (int j = 0; j < 2; ++j) {
+            v[y][j] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (k < p.np && 4 * lane + 128 * j < a.d_v) v[y][j] = *reinterpret_cast<const float4*>(o + 128 * j);
+          }
+        }
+        const float nm = fmaxf(fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)), m);
+        const float f = m == -INFINITY ? 0.f : fast_exp2(m - nm);
+        m = nm;
+        l *= f;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) { acc[j].x *= f; acc[j].y *= f; acc[j].z *= f; acc[j].w *= f; }
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          if (ml[y].y == 0.f) continue;                                    // a piece without rows
+          const float g = fast_exp2(ml[y].x - m);
+          l = fmaf(ml[y].y, g, l);
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            acc[j].x = fmaf(g, v[y][j].x, acc[j].x); acc[j].y = fmaf(g, v[y][j].y, acc[j].y);
+            acc[j].z = fmaf(g, v[y][j].z, acc[j].z); acc[j].w = fmaf(g, v[y][j].w, acc[j].w);
+          }
         }
       }
-      const float nm = fmaxf(fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)), m);
-      const float f = m == -INFINITY ? 0.f : exp2f(m - nm);
-      m = nm;
-      l *= f;
+      __syncthreads();                                                     // the column before has been read
 #pragma unroll
-      for (int j = 0; j < 2; ++j) { acc[j].x *= f; acc[j].y *= f; acc[j].z *= f; acc[j].w *= f; }
+      for (int j = 0; j < 2; ++j)
+        if (4 * lane + 128 * j < a.d_v) *reinterpret_cast<float4*>(&acc_s[w][4 * lane + 128 * j]) = acc[j];
+      if (lane == 0) { red_m[w] = m; red_l[w] = l; }
+      __syncthreads();
+      float M = -INFINITY, L = 0.f, f_w[JNT / 32];
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        if (ml[x].y == 0.f) continue;                                    // a piece without rows
-        const float g = exp2f(ml[x].x - m);
-        l = fmaf(ml[x].y, g, l);
+      for (int k = 0; k < JNT / 32; ++k) M = fmaxf(M, red_m[k]);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          acc[j].x = fmaf(g, v[x][j].x, acc[j].x); acc[j].y = fmaf(g, v[x][j].y, acc[j].y);
-          acc[j].z = fmaf(g, v[x][j].z, acc[j].z); acc[j].w = fmaf(g, v[x][j].w, acc[j].w);
-        }
+      for (int k = 0; k < JNT / 32; ++k) {
+        f_w[k] = red_l[k] == 0.f ? 0.f : fast_exp2(red_m[k] - M);
+        L = fmaf(red_l[k], f_w[k], L);
       }
-    }
+      const float inv = L > 0.f ? 1.f / L : L;
+      T* out = static_cast<T*>(a.out) + ((long long)e * a.Hq + kvh * a.g + hb * a.gb + col) * a.d_v;
+      for (int x2 = tid; x2 < a.d_v; x2 += JNT) {
+        float s = 0.f;
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
-      if (4 * lane + 128 * j < a.d_v) *reinterpret_cast<float4*>(&acc_s[w][4 * lane + 128 * j]) = acc[j];
-    if (lane == 0) { red_m[w] = m; red_l[w] = l; }
-    __syncthreads();
-    float M = -INFINITY, L = 0.f, f_w[JNT / 32];
-#pragma unroll
-    for (int k = 0; k < JNT / 32; ++k) M = fmaxf(M, red_m[k]);
-#pragma unroll
-    for (int k = 0; k < JNT / 32; ++k) {
-      f_w[k] = red_l[k] == 0.f ? 0.f : exp2f(red_m[k] - M);
-      L = fmaf(red_l[k], f_w[k], L);
-    }
-    const float inv = L > 0.f ? 1.f / L : L;
-    for (int c = tid; c < a.d_v; c += JNT) {
-      float s = 0.f;
-#pragma unroll
-      for (int k = 0; k < JNT / 32; ++k) s = fmaf(acc_s[k][c], f_w[k], s);
-      out[c] = from_f32<T>(s * inv);
+        for (int k = 0; k < JNT / 32; ++k) s = fmaf(acc_s[k][x2], f_w[k], s);
+        out[x2] = from_f32<T>(s * inv);
+      }
     }
     return;
   }
   // ---- JROWS rows' weights of one (sequence, KV head) ----
   const int chunks = (a.map.cap + JROWS - 1) / JROWS;
-  const int id = blockIdx.x - merges, chunk = id % chunks, kvh = (id / chunks) % a.Hkv, e = id / chunks / a.Hkv;
-  const int before = a.prefix[e], line = a.prefix[a.n], nt = max(a.prefix[e + 1] - before - UNIT_TILES, 0);
+  const int id = blockIdx.x - joins, chunk = id % chunks, kvh = (id / chunks) % a.Hkv, e = id / chunks / a.Hkv;
+  const int before = a.prefix[e], nt = max(a.prefix[e + 1] - before - UNIT_TILES, 0);
   if (chunk * JROWS >= nt * a.tr) return;
   const int slot = a.slots[e];
   int again = 0;                                                         // the slot was listed before: its first entry counts
@@ -996,7 +1067,34 @@ __global__ void __launch_bounds__(JNT) paged_join_kernel(const __grid_constant__
     return;
   }
   const int len = rows_of(a, slot);
-  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+  const long long base = ((long long)slot * a.Hkv + kvh) * a.map.cap;
+  float old[4], sum[4] = {0.f, 0.f, 0.f, 0.f};                            // (added last: one rounding at the size of the total)
+  float4 v[4];
+  // four logits of each of the thread's rows, columns c .. c + 3 of head block hb
+  const auto load = [&](int hb, int c, int nh) {
+    const float* sc = a.scores + ((long long)e * a.U + kvh * a.nhb + hb) * a.map.cap * a.gb + c;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int row = chunk * JROWS + j * JNT + tid;
+      v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (row < len) {
+        const float* sr = sc + (long long)row * a.gb;
+        if (a.gb % 4 == 0) v[j] = *reinterpret_cast<const float4*>(sr);
+        else {
+          v[j].x = sr[0];
+          if (c + 1 < nh) v[j].y = sr[1];
+          if (c + 2 < nh) v[j].z = sr[2];
+          if (c + 3 < nh) v[j].w = sr[3];
+        }
+      }
+    }
+  };
+  load(0, 0, min(a.gb, a.g));                                            // under way while the maxima and sums are put together
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int row = chunk * JROWS + j * JNT + tid;
+    old[j] = a.w_in && row < len ? a.w_in[base + row] : 0.f;
+  }
   for (int hb = 0; hb < a.nhb; ++hb) {
     const int u = kvh * a.nhb + hb, nh = min(a.gb, a.g - hb * a.gb);
     const Pieces p = pieces_of(a, u, before, line, nt);
@@ -1020,31 +1118,21 @@ __global__ void __launch_bounds__(JNT) paged_join_kernel(const __grid_constant__
       if (lane == 0) mu_s[col] = l == 0.f ? INFINITY : m + log2f(l);     // p = 2^(score - mu); no valid row: 0
     }
     __syncthreads();
-    const float* sc = a.scores + ((long long)e * a.U + u) * a.map.cap * a.gb;
+    for (int c = 0; c < nh; c += 4) {
+      if (hb > 0 || c > 0) load(hb, c, nh);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int row = chunk * JROWS + j * JNT + tid;
-      if (row < len) {
-        const float* sr = sc + (long long)row * a.gb;
-        if (a.gb % 4 == 0) {
-          for (int c = 0; c < nh; c += 4) {
-            const float4 v = *reinterpret_cast<const float4*>(sr + c);
-            sum[j] += exp2f(v.x - mu_s[c]);
-            if (c + 1 < nh) sum[j] += exp2f(v.y - mu_s[c + 1]);
-            if (c + 2 < nh) sum[j] += exp2f(v.z - mu_s[c + 2]);
-            if (c + 3 < nh) sum[j] += exp2f(v.w - mu_s[c + 3]);
-          }
-        } else {
-          for (int c = 0; c < nh; ++c) sum[j] += exp2f(sr[c] - mu_s[c]);
-        }
+      for (int j = 0; j < 4; ++j) {
+        sum[j] += exp2f(v[j].x - mu_s[c]);
+        if (c + 1 < nh) sum[j] += exp2f(v[j].y - mu_s[c + 1]);
+        if (c + 2 < nh) sum[j] += exp2f(v[j].z - mu_s[c + 2]);
+        if (c + 3 < nh) sum[j] += exp2f(v[j].w - mu_s[c + 3]);
       }
     }
   }
-  const long long base = ((long long)slot * a.Hkv + kvh) * a.map.cap;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const int row = chunk * JROWS + j * JNT + tid;
-    if (row < len) a.w_out[base + row] = (a.w_in ? a.w_in[base + row] : 0.f) + sum[j];
+    if (row < len) a.w_out[base + row] = old[j] + sum[j];
   }
 }
 
@@ -1063,7 +1151,7 @@ cudaError_t launch_mma(const PagedArgs& a, const CUtensorMap& tk, const CUtensor
 
 // CTAs per SM that the kernels are built for (launch bounds, and the shared memory of the tensor-core ones)
 constexpr int kMmaCtas = 3, kMmaCtasWide = 2;
-constexpr int simt_ctas(bool wide, int gb) { return wide ? 2 : gb <= 4 ? 3 : 2; }
+constexpr int simt_ctas(bool wide, int gb) { return wide ? 2 : 3; }
 // Stages of a warp of the portable kernel: what the CTAs of an SM leave each other of its shared memory.
 int simt_stages(const Shape& s, int eb, int ctas) {
   const int stage = STR * (s.d_qk + s.d_v) * eb, n = (210 * 1024 / ctas - 20 * 1024) / (SNW * stage);
@@ -1071,21 +1159,21 @@ int simt_stages(const Shape& s, int eb, int ctas) {
 }
 
 template <typename T, int NV, int HB>
-cudaError_t launch_simt_hb(const PagedArgs& a, cudaStream_t st) {
+cudaError_t launch_simt_hb(const PagedArgs& a, const CUtensorMap& tk, const CUtensorMap& tv, cudaStream_t st) {
   constexpr int C = simt_ctas(NV > 1, HB);
   static SmemLimit limit = {};
-  const size_t smem = (size_t)SNW * a.stages * STR * (a.d_qk + a.d_v) * sizeof(T);
+  const size_t smem = (size_t)SNW * a.stages * STR * (a.d_qk + a.d_v) * sizeof(T) + 128;
   if (cudaError_t e = ensure_dyn_smem(paged_simt_kernel<T, NV, HB, C>, smem, limit)) return e;
-  const cudaError_t e = launch_pdl(paged_simt_kernel<T, NV, HB, C>, dim3(a.ctas), dim3(SNT), smem, st, a);
+  const cudaError_t e = launch_pdl(paged_simt_kernel<T, NV, HB, C>, dim3(a.ctas), dim3(SNT), smem, st, a, tk, tv);
   count_launch();
   return e;
 }
 template <typename T, int NV>
-cudaError_t launch_simt(const PagedArgs& a, cudaStream_t st) {
-  if (a.gb <= 1) return launch_simt_hb<T, NV, 1>(a, st);
-  if (a.gb <= 2) return launch_simt_hb<T, NV, 2>(a, st);
-  if (NV > 1 || a.gb <= 4) return launch_simt_hb<T, NV, 4>(a, st);
-  return launch_simt_hb<T, 1, 8>(a, st);
+cudaError_t launch_simt(const PagedArgs& a, const CUtensorMap& tk, const CUtensorMap& tv, cudaStream_t st) {
+  if (a.gb <= 1) return launch_simt_hb<T, NV, 1>(a, tk, tv, st);
+  if (a.gb <= 2) return launch_simt_hb<T, NV, 2>(a, tk, tv, st);
+  if (NV > 1 || a.gb <= 4) return launch_simt_hb<T, NV, 4>(a, tk, tv, st);
+  return launch_simt_hb<T, 1, 8>(a, tk, tv, st);
 }
 
 bool mma_shape(int dtype, const Shape& s, const PageMap& m) {
@@ -1106,7 +1194,7 @@ int paged_decode_plan(int dtype, const Shape& s, const PageMap& m, int n_active,
   const long long units = (long long)n_active * s.Hkv * p->nhb;
   const long long chunks = (m.cap + JROWS - 1) / JROWS;
   // grid and index limits; a line of tiles and the scratch have to be countable
-  if (units > (1LL << 30) || (long long)n_active * s.Hq + (weights ? (long long)n_active * s.Hkv * chunks : 0) > 0x7fffffffLL ||
+  if (units > (1LL << 30) || (long long)n_active * s.Hq > 0x7fffffffLL || (weights && (long long)n_active * s.Hkv * chunks > 0x7fff0000LL) ||
       units * ((m.cap + STR - 1) / STR + UNIT_TILES) > (1LL << 37) ||
       (long long)n_active * ((m.cap + STR - 1) / STR + UNIT_TILES) > 0x7fffffffLL)
     return SNAP_ERR_UNSUPPORTED;
@@ -1138,35 +1226,39 @@ cudaError_t launch_paged_decode(int dtype, const Shape& s, const PageMap& m, con
   a.tr = p.mma ? TR : STR;
   const bool wide = s.d_qk > 128 || s.d_v > 128;
   a.stages = simt_stages(s, elt_bytes(dtype), simt_ctas(wide, p.gb));
-  a.joined = m.page % STR ? 0 : (m.kr == s.d_qk ? 1 : 0) | (m.vr == s.d_v ? 2 : 0);
+  // Tiles come through tensor maps where a page holds whole ones: 64 dims wide with the 128-byte swizzle for the
+  // tensor-core kernel, whole rows for the portable one.  (Encoding both takes the host under a microsecond.)
+  CUtensorMap tk = {}, tv = {};
+  const umma::EncodeTiledFn enc = umma::encode_tiled_fn();
+  const auto encode = [&](CUtensorMap* t, const void* base, int d, long long ps, long long hs, long long rs) {
+    const cuuint64_t eb = (cuuint64_t)elt_bytes(dtype);
+    const cuuint64_t dims[4] = {(cuuint64_t)d, (cuuint64_t)m.page, (cuuint64_t)s.Hkv, (cuuint64_t)m.n_pages};
+    // a stride that is never applied (one KV head, one page) may be anything: the map gets one that it takes
+    const cuuint64_t strides[3] = {(cuuint64_t)rs * eb, (cuuint64_t)(s.Hkv > 1 ? hs : d) * eb, (cuuint64_t)(m.n_pages > 1 ? ps : d) * eb};
+    const cuuint32_t box[4] = {(cuuint32_t)(p.mma ? 64 : d), (cuuint32_t)a.tr, 1, 1}, estr[4] = {1, 1, 1, 1};
+    return enc(t, dtype == SNAP_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims,
+               strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, p.mma ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  };
+  a.tiled = m.page % a.tr == 0 && enc && encode(&tk, k_pages, s.d_qk, m.kp, m.kh, m.kr) && encode(&tv, v_pages, s.d_v, m.vp, m.vh, m.vr);
   cudaError_t e;
   if (p.mma) {
-    const umma::EncodeTiledFn enc = umma::encode_tiled_fn();
-    CUtensorMap tk, tv;
-    const auto encode = [&](CUtensorMap* t, const void* base, long long ps, long long hs, long long rs) {
-      const cuuint64_t dims[4] = {(cuuint64_t)s.d_qk, (cuuint64_t)m.page, (cuuint64_t)s.Hkv, (cuuint64_t)m.n_pages};
-      // a stride that is never applied (one KV head, one page) may be anything: the map gets one that it takes
-      const cuuint64_t strides[3] = {(cuuint64_t)rs * 2, s.Hkv > 1 ? (cuuint64_t)hs * 2 : (cuuint64_t)s.d_qk * 2,
-                                     m.n_pages > 1 ? (cuuint64_t)ps * 2 : (cuuint64_t)s.d_qk * 2};
-      const cuuint32_t box[4] = {64, (cuuint32_t)TR, 1, 1}, estr[4] = {1, 1, 1, 1};
-      return enc(t, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                 CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-    };
-    if (!encode(&tk, k_pages, m.kp, m.kh, m.kr) || !encode(&tv, v_pages, m.vp, m.vh, m.vr)) return cudaErrorInvalidValue;
+    if (!a.tiled) return cudaErrorInvalidValue;
     const bool two = p.gb > 8;
     if (s.d_qk == 128) e = two ? launch_mma<128, 4, 2, 2, kMmaCtasWide>(a, tk, tv, st) : launch_mma<128, 4, 2, 1, kMmaCtas>(a, tk, tv, st);
     else if (s.d_qk == 64) e = two ? launch_mma<64, 4, 4, 2, kMmaCtasWide>(a, tk, tv, st) : launch_mma<64, 4, 4, 1, kMmaCtas>(a, tk, tv, st);
     else e = two ? launch_mma<256, 2, 2, 2, kMmaCtasWide>(a, tk, tv, st) : launch_mma<256, 2, 2, 1, kMmaCtas>(a, tk, tv, st);
   } else if (dtype == SNAP_F32) {
-    e = wide ? launch_simt<float, 2>(a, st) : launch_simt<float, 1>(a, st);
+    e = wide ? launch_simt<float, 2>(a, tk, tv, st) : launch_simt<float, 1>(a, tk, tv, st);
   } else {
-    e = wide ? launch_simt<__nv_bfloat16, 2>(a, st) : launch_simt<__nv_bfloat16, 1>(a, st);
+    e = wide ? launch_simt<__nv_bfloat16, 2>(a, tk, tv, st) : launch_simt<__nv_bfloat16, 1>(a, tk, tv, st);
   }
   if (e != cudaSuccess) return e;
-  const int chunks = (m.cap + JROWS - 1) / JROWS;
-  const dim3 grid((unsigned)(n_active * s.Hq + (w_out ? n_active * s.Hkv * chunks : 0)));
-  e = dtype == SNAP_F32 ? launch_pdl(paged_join_kernel<float>, grid, dim3(JNT), 0, st, a)
-                        : launch_pdl(paged_join_kernel<__nv_bfloat16>, grid, dim3(JNT), 0, st, a);
+  const int chunks = (m.cap + JROWS - 1) / JROWS, heads = n_active * s.Hq, by_heads = heads <= 512 || p.ctas < 2;
+  const int joins = by_heads ? heads : p.ctas - 1;
+  const dim3 grid((unsigned)(joins + (w_out ? n_active * s.Hkv * chunks : 0)));
+  e = dtype == SNAP_F32 ? launch_pdl(paged_join_kernel<float>, grid, dim3(JNT), 0, st, a, joins, by_heads)
+                        : launch_pdl(paged_join_kernel<__nv_bfloat16>, grid, dim3(JNT), 0, st, a, joins, by_heads);
   count_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
 }

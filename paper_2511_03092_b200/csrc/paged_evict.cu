@@ -218,7 +218,6 @@ __global__ void __launch_bounds__(CNT, 4) evict_copy_kernel(const __grid_constan
   const int kvh = blockIdx.y, i = blockIdx.z, lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   const int keep = a.Ls + a.K + a.Lr, r0 = (blockIdx.x * (CNT / 32) + w) * CROWS;
   pdl_wait();
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (r0 >= keep) return;
   const int len = a.len[i], rows = len < keep ? len : keep;
   const int src = len >= 0 ? a.src[i] : 0, dst = len >= 0 ? a.dst[i] : 0;

@@ -11,6 +11,9 @@
 // its token with the loads of several heads in flight; the angles of a token are computed once, by the whole
 // block, and handed over in shared memory.  Threads are laid out as [tokens][heads][items of a head]: consecutive
 // threads are on consecutive vectors, and few tokens spread over more threads per token.
+//
+// The kernel after it starts when this one ends, not beside its last blocks: attention over the pages comes next, whose
+// blocks fill an SM's registers to the last thousand and would find them in pieces.
 #include "snap_internal.cuh"
 
 namespace snap {
@@ -56,7 +59,6 @@ __global__ void __launch_bounds__(NT, 4) rope_kernel(const __grid_constant__ Rop
   const bool paged = a.k_pages != nullptr;
   if (tid < L.Z) dup[tid] = 0;
   pdl_wait();
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
   // ---- where the token goes ----
   bool skip = !mine;
