@@ -62,6 +62,12 @@ PageMap page_map(const snap_paged_t* p, const int* table) {
   return m;
 }
 
+// Do the blocks that move a call's rows (64 or more rows each) fit one grid, and its KV heads and sequences the selection's?
+bool evict_countable(const snap_config_t* c, int n_seqs) {
+  const long long keep = (long long)c->l_sink + c->l_recent + c->topk;
+  return c->n_kv_heads <= 65535 && (keep / 64 + 1) * c->n_kv_heads * n_seqs <= 0x7fffffffLL;
+}
+
 int status_of(cudaError_t e) { return e == cudaSuccess ? SNAP_OK : SNAP_ERR_CUDA; }
 
 }  // namespace
@@ -230,6 +236,7 @@ int64_t snap_paged_evict_workspace_bytes(const snap_config_t* cfg, const snap_pa
   const int rc = check_paged(cfg, paged);
   if (rc != SNAP_OK) return rc;
   if (n_seqs < 0 || n_seqs > 65535) return SNAP_ERR_INVALID_ARG;
+  if (!evict_countable(cfg, n_seqs)) return SNAP_ERR_UNSUPPORTED;
   return (int64_t)paged_evict_scratch_bytes(make_shape(cfg), n_seqs);
 }
 
@@ -246,6 +253,7 @@ int snap_paged_evict(const snap_config_t* cfg, const snap_paged_t* paged, const 
       !workspace_dev)
     return SNAP_ERR_NULL_POINTER;
   if (misaligned(k_pages_dev, v_pages_dev, workspace_dev)) return SNAP_ERR_INVALID_ARG;
+  if (!evict_countable(cfg, n_seqs)) return SNAP_ERR_UNSUPPORTED;
   const Shape s = make_shape(cfg);
   if (workspace_bytes < paged_evict_scratch_bytes(s, n_seqs)) return SNAP_ERR_WORKSPACE_TOO_SMALL;
   return status_of(launch_paged_evict(cfg->dtype, s, page_map(paged, page_table_dev), src_slots_dev, dst_slots_dev, n_seqs, k_pages_dev,

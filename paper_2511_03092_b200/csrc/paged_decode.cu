@@ -28,6 +28,7 @@
 #include <cuda.h>
 
 #include "mma_helpers.cuh"
+#include "packed_f32.cuh"
 #include "snap_internal.cuh"
 #include "umma_helpers.cuh"
 
@@ -617,12 +618,6 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
 // ---------------------------------------------------------------------------------------------------------------
 // portable kernel
 // ---------------------------------------------------------------------------------------------------------------
-// Two single-precision numbers in one register pair: sm_100a multiplies and adds them in one instruction.
-using F2 = unsigned long long;
-__device__ __forceinline__ F2 pack2(float x, float y) { F2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y)); return r; }
-__device__ __forceinline__ float2 unpack2(F2 v) { float2 r; asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v)); return r; }
-__device__ __forceinline__ F2 mul2(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
-__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) { F2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
 struct Four { F2 a, b; };                          // four consecutive elements
 template <typename T> __device__ __forceinline__ Four four(const T* p);
 template <> __device__ __forceinline__ Four four<float>(const float* p) {

@@ -2,7 +2,7 @@
 // sinks, the topk rows of the middle with the largest weight and the last l_recent rows move, in order, to the
 // pages of another slot.
 //
-// Selection: one CTA per (sequence, KV head), or a cluster of eight for very long middles, with its slice of the
+// Selection: one CTA per (sequence, KV head), or a cluster of up to eight for long middles, with its slice of the
 // middle's weights in shared memory as order-preserving integers.  The topk-th largest is found by radix steps of
 // 11 bits over the range that the keys really span (weights of one layer lie within a few octaves, so the digits
 // of the raw bit pattern would fall into a handful of bins and the counting atomics would queue on them); the CTAs
@@ -11,7 +11,9 @@
 // timing).
 //
 // Copy: bound by HBM (each kept row read and written once).  A lane looks up one row's pages, then the warp moves
-// its rows with eight 16-byte loads per lane in flight.
+// its rows with eight 16-byte loads per lane in flight.  The rows that stay whatever the selection says (sinks, last
+// rows, sequences within the budget) are copied while the selection, which leaves most SMs idle, is still running: the
+// blocks are in the order that starts with the last rows, and a warp waits only where it has rows of the middle.
 #include <cooperative_groups.h>
 
 #include "snap_internal.cuh"
@@ -31,7 +33,6 @@ struct EvictArgs {
   int* seq_len;
   const float* w_in; float* w_out;
   int* idx;                            // [n][Hkv][K] selected rows, ascending
-  int* len;                            // [n] rows of each sequence, -1: skipped
   int* kept;                           // NULL or [n][Hkv][Ls + K + Lr]
   char* kp; char* vp;
   int k_vecs, v_vecs, eb;              // 16-byte pieces of a row; bytes of an element
@@ -57,7 +58,7 @@ __device__ bool entry_ok(const EvictArgs& a, int i, int& src, int& dst) {
   return !__syncthreads_or(clash);
 }
 
-// CLUSTER: eight CTAs share a middle; otherwise one has it all and the cluster's barriers and reads fall away.
+// CLUSTER: two to eight CTAs share a middle; otherwise one has it all and the cluster's barriers and reads fall away.
 template <bool CLUSTER>
 __global__ void __launch_bounds__(ENT) evict_select_kernel(const __grid_constant__ EvictArgs a) {
   extern __shared__ unsigned keys[];                     // [keys_cap]
@@ -80,7 +81,6 @@ __global__ void __launch_bounds__(ENT) evict_select_kernel(const __grid_constant
     if (kvh == 0) {
       const unsigned bad = (ok ? 0u : SNAP_DEV_BAD_SLOT) | (len > a.map.cap ? SNAP_DEV_BAD_PAGE : 0u);
       if (bad && a.status) atomicOr(a.status, bad);
-      a.len[i] = s_len;
     }
   }
   barrier();
@@ -211,33 +211,35 @@ __global__ void __launch_bounds__(ENT) evict_select_kernel(const __grid_constant
 
 constexpr int CNT = 256;                                 // threads of a copy CTA
 
-// grid (row groups, KV heads, sequences); a warp moves CROWS rows.  SAME: keys and values are laid out alike, so that one
-// offset serves both.
+// Grid: row groups x (sequence, KV head), the last row group of all of those first; a warp moves CROWS rows.  SAME: keys and
+// values are laid out alike, so that one offset serves both.  What is read before the wait was written before the
+// selection kernel started; it is read past L1.
 template <int CROWS, bool SAME>
-__global__ void __launch_bounds__(CNT, 4) evict_copy_kernel(const __grid_constant__ EvictArgs a) {
-  const int kvh = blockIdx.y, i = blockIdx.z, lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  const int keep = a.Ls + a.K + a.Lr, r0 = (blockIdx.x * (CNT / 32) + w) * CROWS;
-  pdl_wait();
-  if (r0 >= keep) return;
-  const int len = a.len[i], rows = len < keep ? len : keep;
-  const int src = len >= 0 ? a.src[i] : 0, dst = len >= 0 ? a.dst[i] : 0;
-  if (len >= 0 && kvh == 0 && blockIdx.x == 0 && threadIdx.x == 0) a.seq_len[dst] = rows;
+__global__ void __launch_bounds__(CNT, 4) evict_copy_kernel(const __grid_constant__ EvictArgs a, int groups) {
+  const int units = a.n * a.Hkv, group = groups - 1 - (int)(blockIdx.x / units), unit = blockIdx.x % units;
+  const int i = unit / a.Hkv, kvh = unit - i * a.Hkv, lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  const int keep = a.Ls + a.K + a.Lr, r0 = (group * (CNT / 32) + w) * CROWS;
+  int src, dst;
+  const bool ok = entry_ok<CNT>(a, i, src, dst);
+  const int len = ok ? min(max(__ldcg(a.seq_len + src), 0), a.map.cap) : -1, rows = len < keep ? len : keep;
+  const bool selected = len > keep && r0 < a.Ls + a.K && r0 + CROWS > a.Ls;      // rows of the middle among the warp's
+  if (selected) pdl_wait();
   // lane l < CROWS: row r0 + l of the destination; byte offsets of its source and destination, ks < 0: nothing to copy
   long long ks = -1, kd = 0, vs = 0, vd = 0;
-  if (lane < CROWS) {
+  if (lane < CROWS && r0 + lane < keep) {
     const int r = r0 + lane;
     int from = -1;
     if (r < rows) {
       if (len <= keep || r < a.Ls) from = r;
-      else if (r < a.Ls + a.K) from = a.idx[((long long)i * a.Hkv + kvh) * a.K + r - a.Ls];
+      else if (r < a.Ls + a.K) from = __ldcg(a.idx + ((long long)i * a.Hkv + kvh) * a.K + r - a.Ls);
       else from = len - keep + r;
       if (!index_ok(from, len, a.status)) from = -1;
     }
-    if (a.kept && r < keep) a.kept[((long long)i * a.Hkv + kvh) * keep + r] = from;
+    if (a.kept) a.kept[((long long)i * a.Hkv + kvh) * keep + r] = from;
     if (from >= 0) {
       const int sp = from / a.map.page, dp = r / a.map.page;
-      const int s_page = a.map.table[(long long)src * a.map.max_pages + sp];
-      const int d_page = dp < a.map.max_pages ? a.map.table[(long long)dst * a.map.max_pages + dp] : -1;
+      const int s_page = __ldcg(a.map.table + (long long)src * a.map.max_pages + sp);
+      const int d_page = dp < a.map.max_pages ? __ldcg(a.map.table + (long long)dst * a.map.max_pages + dp) : -1;
       if (s_page < 0 || s_page >= a.map.n_pages || d_page < 0 || d_page >= a.map.n_pages) {
         if (a.status) atomicOr(a.status, SNAP_DEV_BAD_PAGE);
       } else {
@@ -248,7 +250,7 @@ __global__ void __launch_bounds__(CNT, 4) evict_copy_kernel(const __grid_constan
         vd = (d_page * a.map.vp + kvh * a.map.vh + dof * a.map.vr) * a.eb;
         if (a.w_out) {
           const long long b = (long long)kvh * a.map.cap, per = (long long)a.Hkv * a.map.cap;
-          a.w_out[dst * per + b + r] = a.w_in[src * per + b + from];
+          a.w_out[dst * per + b + r] = __ldcg(a.w_in + src * per + b + from);
         }
       }
     }
@@ -266,8 +268,8 @@ __global__ void __launch_bounds__(CNT, 4) evict_copy_kernel(const __grid_constan
         const long long s = __shfl_sync(0xffffffffu, s_off, from), d = __shfl_sync(0xffffffffu, d_off, from);
         to[u] = row < CROWS && s >= 0 ? d + 16 * c : -1;
         if (to[u] >= 0) {
-          x[u] = *reinterpret_cast<const uint4*>(p0 + s + 16 * c);
-          if (SAME) y[SAME ? u : 0] = *reinterpret_cast<const uint4*>(p1 + s + 16 * c);
+          x[u] = __ldcg(reinterpret_cast<const uint4*>(p0 + s + 16 * c));
+          if (SAME) y[SAME ? u : 0] = __ldcg(reinterpret_cast<const uint4*>(p1 + s + 16 * c));
         }
       }
 #pragma unroll
@@ -280,20 +282,23 @@ __global__ void __launch_bounds__(CNT, 4) evict_copy_kernel(const __grid_constan
   };
   move(a.k_vecs, a.k_magic, ks, kd, a.kp, a.vp);
   if (!SAME) move(a.v_vecs, a.v_magic, ks < 0 ? -1 : vs, vd, a.vp, nullptr);
+  pdl_wait();                                              // nobody leaves before the selection has ended
+  if (ok && kvh == 0 && group == 0 && threadIdx.x == 0) a.seq_len[dst] = rows;
 }
 
 template <int CROWS>
 cudaError_t launch_copy(const EvictArgs& a, int keep, bool same, cudaStream_t st) {
   constexpr int per = CNT / 32 * CROWS;
-  const dim3 grid((keep + per - 1) / per, a.Hkv, a.n);
-  return same ? launch_pdl(evict_copy_kernel<CROWS, true>, grid, dim3(CNT), 0, st, a)
-              : launch_pdl(evict_copy_kernel<CROWS, false>, grid, dim3(CNT), 0, st, a);
+  const int groups = (keep + per - 1) / per;
+  const dim3 grid((unsigned)((long long)groups * a.n * a.Hkv));
+  return same ? launch_pdl(evict_copy_kernel<CROWS, true>, grid, dim3(CNT), 0, st, a, groups)
+              : launch_pdl(evict_copy_kernel<CROWS, false>, grid, dim3(CNT), 0, st, a, groups);
 }
 
 }  // namespace
 
 size_t paged_evict_scratch_bytes(const Shape& s, int n_seqs) {
-  return align_up((size_t)n_seqs * s.Hkv * (s.K > 0 ? s.K : 1) * sizeof(int)) + align_up((size_t)n_seqs * sizeof(int));
+  return align_up((size_t)n_seqs * s.Hkv * (s.K > 0 ? s.K : 1) * sizeof(int));
 }
 
 cudaError_t launch_paged_evict(int dtype, const Shape& s, const PageMap& m, const int* src, const int* dst, int n_seqs,
@@ -303,15 +308,18 @@ cudaError_t launch_paged_evict(int dtype, const Shape& s, const PageMap& m, cons
   a.src = src; a.dst = dst; a.n = n_seqs; a.Hkv = s.Hkv; a.Ls = s.Ls; a.Lr = s.Lr; a.K = s.K; a.max_seqs = s.max_seqs;
   a.map = m; a.seq_len = seq_len; a.w_in = w_in; a.w_out = w_out; a.kept = kept; a.status = status;
   a.idx = reinterpret_cast<int*>(scratch);
-  a.len = reinterpret_cast<int*>(scratch + align_up((size_t)n_seqs * s.Hkv * (s.K > 0 ? s.K : 1) * sizeof(int)));
   a.kp = static_cast<char*>(k_pages); a.vp = static_cast<char*>(v_pages);
   a.eb = elt_bytes(dtype);
   a.k_vecs = s.d_qk * a.eb / 16; a.v_vecs = s.d_v * a.eb / 16;
   a.k_magic = ((1u << 20) + a.k_vecs - 1) / a.k_vecs;       // exact below 2^20 / vecs: a warp has 32 rows of 64 pieces at most
   a.v_magic = ((1u << 20) + a.v_vecs - 1) / a.v_vecs;
   const int most = m.cap - s.Ls - s.Lr;                    // candidates there can be
-  const bool cluster = most > MAX_KEYS;
-  const int CL = cluster ? 8 : 1, per = most > 0 ? (most + CL - 1) / CL : 0;
+  // CTAs of a middle: as many as bring a slice down to 8192 keys while all of them are resident at once (two per SM),
+  // more where a slice would not fit shared memory.
+  int CL = 1;
+  while (CL < 8 && (most / CL > MAX_KEYS || (most / CL > 8192 && 2LL * CL * n_seqs * s.Hkv <= 2LL * sm_count()))) CL *= 2;
+  const bool cluster = CL > 1;
+  const int per = most > 0 ? (most + CL - 1) / CL : 0;
   a.keys_cap = per <= MAX_KEYS ? per : 0;
   const size_t smem = (size_t)a.keys_cap * sizeof(unsigned);
   cudaError_t e;

@@ -8,8 +8,11 @@
 //
 // A pass reads and writes every element once and computes next to nothing, so memory bounds it.  A thread keeps
 // the cosines and sines of its V pairs (two 16-byte vectors of a head) in registers and walks over the heads of
-// its token with the loads of several heads in flight; the angles of a token are computed once, by the whole
-// block, and handed over in shared memory.  Threads are laid out as [tokens][heads][items of a head]: consecutive
+// its token; the angles of a token are computed once, by the whole block, and handed over in shared memory.  What
+// counts is how many warps are resident, not how much each has in flight: one head at a time and five blocks per SM
+// turn a 32768-token prompt of 40 heads of 128 dims in 110 us (6.1 TB/s); two heads at a time and four blocks take
+// 113 us, three and three 125, and looping over tokens in as many blocks as fit 124 to 144.  Appending 26003 tokens of
+// the same layer (queries, keys twice, values) takes 121 us (5.7 TB/s).  Threads are laid out as [tokens][heads][items of a head]: consecutive
 // threads are on consecutive vectors, and few tokens spread over more threads per token.
 //
 // The kernel after it starts when this one ends, not beside its last blocks: attention over the pages comes next, whose
@@ -20,7 +23,6 @@ namespace snap {
 namespace {
 
 constexpr int NT = 256;
-constexpr int BATCH = 2;           // heads whose loads a thread has in flight
 
 template <int BYTES> struct RawOf;
 template <> struct RawOf<16> { using type = uint4; };
@@ -46,8 +48,8 @@ __device__ __forceinline__ float2 cos_sin(int pos, double f) {
   return make_float2(fmaf(-rl, s, c), fmaf(rl, c, s));
 }
 
-template <typename T, int V, bool INTER>
-__global__ void __launch_bounds__(NT, 4) rope_kernel(const __grid_constant__ RopeLaunch L) {
+template <typename T, int V, bool INTER, bool PAGED>
+__global__ void __launch_bounds__(NT, 5) rope_kernel(const __grid_constant__ RopeLaunch L) {
   using VT = Vec<T, V>;
   using Raw = decltype(VT::raw);
   const RopeArgs& a = L.a;
@@ -56,7 +58,7 @@ __global__ void __launch_bounds__(NT, 4) rope_kernel(const __grid_constant__ Rop
   const int tid = threadIdx.x, x = tid % L.X, y = (tid / L.X) % L.Y, z = tid / (L.X * L.Y);
   const int t = blockIdx.x * L.Z + z, half = a.rot / 2;
   const bool mine = z < L.Z && t < a.n_tokens;                            // the block may have spare threads
-  const bool paged = a.k_pages != nullptr;
+  constexpr bool paged = PAGED;
   if (tid < L.Z) dup[tid] = 0;
   pdl_wait();
 
@@ -79,10 +81,14 @@ __global__ void __launch_bounds__(NT, 4) rope_kernel(const __grid_constant__ Rop
       }
     }
   }
-  __syncthreads();                                                        // dup is zero
-  if (paged && !a.rows && !skip)                                          // listed earlier in this call?
-    for (int e = tid - z * L.X * L.Y; e < t; e += L.X * L.Y)
-      if (a.slots[e] == slot) dup[z] = 1;
+  if (paged && !a.rows) {
+    __syncthreads();                                                      // dup is zero
+    if (!skip)                                                            // listed earlier in this call?
+      for (int e = tid - z * L.X * L.Y; e < t; e += L.X * L.Y)
+        if (a.slots[e] == slot) dup[z] = 1;
+    __syncthreads();
+    if (!skip && dup[z]) { skip = true; bad = SNAP_DEV_BAD_SLOT; }
+  }
 
   const T* q = static_cast<const T*>(a.q) + t * a.q_tok;
   const T* k = static_cast<const T*>(a.k) + t * a.k_tok;
@@ -91,19 +97,28 @@ __global__ void __launch_bounds__(NT, 4) rope_kernel(const __grid_constant__ Rop
   // item j of a head: its two vectors
   const auto first_of = [&](int j) { return a.offset + (INTER ? 2 * j * V : j * V); };
   const int to_second = INTER ? V : half;
-  VT va[BATCH], vb[BATCH];
-  const auto load = [&](int j, int h0) {
-#pragma unroll
-    for (int u = 0; u < BATCH; ++u) {
-      const int h = h0 + u * L.Y;
-      if (h < H) {
-        const T* s = source(h) + first_of(j);
-        va[u].raw = *reinterpret_cast<const Raw*>(s);
-        vb[u].raw = *reinterpret_cast<const Raw*>(s + to_second);
-      }
-    }
+  VT va, vb;
+  const auto load = [&](int j, int h) {
+    const T* s = source(h) + first_of(j);
+    va.raw = *reinterpret_cast<const Raw*>(s);
+    vb.raw = *reinterpret_cast<const Raw*>(s + to_second);
   };
-  if (mine && x < L.nj) load(x, y);                                       // on their way while the angles are computed
+  if (mine && x < L.nj && y < H) load(x, y);                              // on their way while the angles are computed
+
+  // ---- values: copied to the page while the angles are on their way ----
+  if (paged && !skip) {
+    const T* v = static_cast<const T*>(a.v) + t * a.v_tok;
+    T* vp = static_cast<T*>(a.v_pages) + page * a.map.vp + off * a.map.vr;
+    const int n = a.d_v / V;
+    for (int h = y; h < a.Hkv; h += L.Y)
+      for (int c = x; c < n; c += 2 * L.X) {
+        Raw r0, r1;
+        r0 = *reinterpret_cast<const Raw*>(v + h * a.v_head + c * V);
+        if (c + L.X < n) r1 = *reinterpret_cast<const Raw*>(v + h * a.v_head + (c + L.X) * V);
+        *reinterpret_cast<Raw*>(vp + h * a.map.vh + c * V) = r0;
+        if (c + L.X < n) *reinterpret_cast<Raw*>(vp + h * a.map.vh + (c + L.X) * V) = r1;
+      }
+  }
 
   // ---- the angles of the block's tokens ----
   for (int e = tid; e < L.Z * half; e += NT) {
@@ -117,7 +132,6 @@ __global__ void __launch_bounds__(NT, 4) rope_kernel(const __grid_constant__ Rop
     table[e] = make_float2(cs.x * a.magnitude, cs.y * (a.magnitude * a.sign));
   }
   __syncthreads();                                                        // everyone has read seq_len
-  if (mine && paged && dup[z] && !skip) { skip = true; bad = SNAP_DEV_BAD_SLOT; }
   if (mine && paged && x == 0 && y == 0) {
     if (bad && a.status) atomicOr(a.status, bad);
     if (!skip) {
@@ -144,31 +158,25 @@ __global__ void __launch_bounds__(NT, 4) rope_kernel(const __grid_constant__ Rop
 #pragma unroll
     for (int i = 0; i < V; ++i) cs[i] = table[z * half + j * V + i];
     const int at_a = first_of(j), at_b = at_a + to_second;
-    for (int h0 = y; h0 < H; h0 += BATCH * L.Y) {
-      if (j != x || h0 != y) load(j, h0);
+    for (int h = y; h < H; h += L.Y) {
+      if (j != x || h != y) load(j, h);
+      VT oa, ob;
 #pragma unroll
-      for (int u = 0; u < BATCH; ++u) {
-        const int h = h0 + u * L.Y;
-        if (h < H) {
-          VT oa, ob;
-#pragma unroll
-          for (int i = 0; i < V; ++i) {
-            // interleaved: the item's 2 V elements are V neighbouring pairs, else pair i is (va[i], vb[i])
-            const float p = to_f32<T>(INTER ? (2 * i < V ? va[u].e[(2 * i) % V] : vb[u].e[(2 * i) % V]) : va[u].e[i]);
-            const float r = to_f32<T>(INTER ? (2 * i + 1 < V ? va[u].e[(2 * i + 1) % V] : vb[u].e[(2 * i + 1) % V]) : vb[u].e[i]);
-            const T c0 = from_f32<T>(fmaf(p, cs[i].x, -(r * cs[i].y))), c1 = from_f32<T>(fmaf(r, cs[i].x, p * cs[i].y));
-            if (INTER) {
-              if (2 * i < V) oa.e[(2 * i) % V] = c0; else ob.e[(2 * i) % V] = c0;
-              if (2 * i + 1 < V) oa.e[(2 * i + 1) % V] = c1; else ob.e[(2 * i + 1) % V] = c1;
-            } else {
-              oa.e[i] = c0;
-              ob.e[i] = c1;
-            }
-          }
-          put(h, at_a, oa.raw);
-          put(h, at_b, ob.raw);
+      for (int i = 0; i < V; ++i) {
+        // interleaved: the item's 2 V elements are V neighbouring pairs, else pair i is (va[i], vb[i])
+        const float p = to_f32<T>(INTER ? (2 * i < V ? va.e[(2 * i) % V] : vb.e[(2 * i) % V]) : va.e[i]);
+        const float r = to_f32<T>(INTER ? (2 * i + 1 < V ? va.e[(2 * i + 1) % V] : vb.e[(2 * i + 1) % V]) : vb.e[i]);
+        const T c0 = from_f32<T>(fmaf(p, cs[i].x, -(r * cs[i].y))), c1 = from_f32<T>(fmaf(r, cs[i].x, p * cs[i].y));
+        if (INTER) {
+          if (2 * i < V) oa.e[(2 * i) % V] = c0; else ob.e[(2 * i) % V] = c0;
+          if (2 * i + 1 < V) oa.e[(2 * i + 1) % V] = c1; else ob.e[(2 * i + 1) % V] = c1;
+        } else {
+          oa.e[i] = c0;
+          ob.e[i] = c1;
         }
       }
+      put(h, at_a, oa.raw);
+      put(h, at_b, ob.raw);
     }
   }
   // ---- the head's other dims ----
@@ -176,13 +184,7 @@ __global__ void __launch_bounds__(NT, 4) rope_kernel(const __grid_constant__ Rop
     const int at = c * V < a.offset ? c * V : c * V + a.rot;
     for (int h = y; h < H; h += L.Y) put(h, at, *reinterpret_cast<const Raw*>(source(h) + at));
   }
-  // ---- values: copied to the page ----
   if (paged) {
-    const T* v = static_cast<const T*>(a.v) + t * a.v_tok;
-    T* vp = static_cast<T*>(a.v_pages) + page * a.map.vp + off * a.map.vr;
-    for (int h = y; h < a.Hkv; h += L.Y)
-      for (int c = x; c < a.d_v / V; c += L.X)
-        *reinterpret_cast<Raw*>(vp + h * a.map.vh + c * V) = *reinterpret_cast<const Raw*>(v + h * a.v_head + c * V);
     if (a.weights && x == 0)
       for (int h = y; h < a.Hkv; h += L.Y) a.weights[((long long)slot * a.Hkv + h) * a.map.cap + row] = 0.f;
   }
@@ -212,8 +214,9 @@ cudaError_t launch_v(const RopeArgs& a, int sms, cudaStream_t st) {
   if (L.Z > a.n_tokens) L.Z = a.n_tokens;
   const size_t smem = (size_t)L.Z * (a.rot / 2) * sizeof(float2);        // at most 2048 pairs: X covers them or Z is small
   const dim3 grid((a.n_tokens + L.Z - 1) / L.Z);
-  const cudaError_t e = a.interleaved ? launch_pdl(rope_kernel<T, V, true>, grid, dim3(NT), smem, st, L)
-                                      : launch_pdl(rope_kernel<T, V, false>, grid, dim3(NT), smem, st, L);
+  cudaError_t e;
+  if (a.k_pages) e = a.interleaved ? launch_pdl(rope_kernel<T, V, true, true>, grid, dim3(NT), smem, st, L) : launch_pdl(rope_kernel<T, V, false, true>, grid, dim3(NT), smem, st, L);
+  else e = a.interleaved ? launch_pdl(rope_kernel<T, V, true, false>, grid, dim3(NT), smem, st, L) : launch_pdl(rope_kernel<T, V, false, false>, grid, dim3(NT), smem, st, L);
   count_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
 }
