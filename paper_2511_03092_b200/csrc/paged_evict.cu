@@ -24,6 +24,7 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr int ENT = 1024, NB = 2048, NB_BITS = 11;      // threads of a selection CTA, bins of a radix step
+constexpr int LOADS = 16;                                // loads of a thread in flight
 constexpr int MAX_KEYS = 45000;                          // keys of a slice that are kept in shared memory (180 KB)
 
 struct EvictArgs {
@@ -98,12 +99,19 @@ __global__ void __launch_bounds__(ENT) evict_select_kernel(const __grid_constant
 
   // ---- the range the keys span ----
   unsigned lo = 0xffffffffu, hi = 0u;
-#pragma unroll 8
-  for (int e = tid; e < mine; e += ENT) {
-    const unsigned k = key_of(wt[e]);
-    if (held) keys[e] = k;
-    lo = min(lo, k);
-    hi = max(hi, k);
+  for (int e0 = tid; e0 < mine; e0 += LOADS * ENT) {     // (one CTA's loads in flight are all there is to hide the latency)
+    float x[LOADS];
+#pragma unroll
+    for (int u = 0; u < LOADS; ++u)
+      if (e0 + u * ENT < mine) x[u] = __ldcg(wt + e0 + u * ENT);
+#pragma unroll
+    for (int u = 0; u < LOADS; ++u)
+      if (e0 + u * ENT < mine) {
+        const unsigned k = key_of(x[u]);
+        if (held) keys[e0 + u * ENT] = k;
+        lo = min(lo, k);
+        hi = max(hi, k);
+      }
   }
   lo = __reduce_min_sync(0xffffffffu, lo);
   hi = __reduce_max_sync(0xffffffffu, hi);
@@ -171,23 +179,28 @@ __global__ void __launch_bounds__(ENT) evict_select_kernel(const __grid_constant
   // keys in [base, base + 2^bits) are at the threshold: `need` of them are taken, the lower rows first; above: all
   const unsigned span = bits == 32 ? 0xffffffffu : (1u << bits) - 1u;
 
-  // ---- emission in row order: counts per CTA, then per warp ----
-  const int seg = ((mine + ENT / 32 - 1) / (ENT / 32) + 31) & ~31, e0 = min(w * seg, mine), e1 = min(e0 + seg, mine);
+  // ---- emission in row order: a thread has a run of consecutive candidates (an odd number of them, so that the threads
+  // of a warp read different banks), counts them, and learns from a scan where its rows go ----
+  const int run = ((mine + ENT - 1) / ENT) | 1, e0 = min(tid * run, mine), e1 = min(e0 + run, mine);
   int gt = 0, eq = 0;
-#pragma unroll 4
-  for (int e = e0 + lane; e < e1; e += 32) {
+  for (int e = e0; e < e1; ++e) {
     const unsigned k = key(e);
     const bool at = k >= base && k - base <= span;
     gt += k >= base && !at;
     eq += at;
   }
-  gt = __reduce_add_sync(0xffffffffu, gt);
-  eq = __reduce_add_sync(0xffffffffu, eq);
+  const auto scan = [&](int v, int* warps) {             // exclusive over the CTA
+    int incl = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const int x = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += x; }
+    if (lane == 31) warps[w] = incl;
+    return incl - v;
+  };
   __syncthreads();                                       // warp_s has been read
-  if (lane == 0) { warp_s[w] = gt; warp_e[w] = eq; }
+  int gt_before = scan(gt, warp_s), eq_before = scan(eq, warp_e);
   __syncthreads();
-  int gt_before = __reduce_add_sync(0xffffffffu, lane < w ? warp_s[lane] : 0);
-  int eq_before = __reduce_add_sync(0xffffffffu, lane < w ? warp_e[lane] : 0);
+  gt_before += __reduce_add_sync(0xffffffffu, lane < w ? warp_s[lane] : 0);
+  eq_before += __reduce_add_sync(0xffffffffu, lane < w ? warp_e[lane] : 0);
   if (CLUSTER) {
     if (tid == ENT - 1) { s_cnt[0] = gt_before + gt; s_cnt[1] = eq_before + eq; }
     cl.sync();
@@ -195,16 +208,16 @@ __global__ void __launch_bounds__(ENT) evict_select_kernel(const __grid_constant
     eq_before += __reduce_add_sync(0xffffffffu, lane < rank ? cl.map_shared_rank(s_cnt, lane)[1] : 0);
   }
   int* out = a.idx + ((long long)i * a.Hkv + kvh) * a.K;
-  const unsigned below = (1u << lane) - 1u;
-  for (int e = e0; e < e1; e += 32) {
-    const int x = e + lane;
-    const unsigned k = x < e1 ? key(x) : 0u;
-    const bool at = x < e1 && k >= base && k - base <= span, up = x < e1 && k >= base && !at;
-    const unsigned m_gt = __ballot_sync(0xffffffffu, up), m_eq = __ballot_sync(0xffffffffu, at);
-    const int my_eq = eq_before + __popc(m_eq & below), pos = gt_before + __popc(m_gt & below) + min(my_eq, need);
-    if ((up || (at && my_eq < need)) && index_ok(pos, a.K, a.status)) out[pos] = a.Ls + c0 + x;
-    gt_before += __popc(m_gt);
-    eq_before += __popc(m_eq);
+  int pos = gt_before + min(eq_before, need);
+  for (int e = e0; e < e1; ++e) {
+    const unsigned k = key(e);
+    if (k < base) continue;
+    const bool at = k - base <= span, take = !at || eq_before < need;
+    eq_before += at;
+    if (take) {
+      if (index_ok(pos, a.K, a.status)) out[pos] = a.Ls + c0 + e;
+      ++pos;
+    }
   }
   if (CLUSTER) cl.sync();                                // no CTA leaves while another may read its counts
 }
@@ -314,10 +327,10 @@ cudaError_t launch_paged_evict(int dtype, const Shape& s, const PageMap& m, cons
   a.k_magic = ((1u << 20) + a.k_vecs - 1) / a.k_vecs;       // exact below 2^20 / vecs: a warp has 32 rows of 64 pieces at most
   a.v_magic = ((1u << 20) + a.v_vecs - 1) / a.v_vecs;
   const int most = m.cap - s.Ls - s.Lr;                    // candidates there can be
-  // CTAs of a middle: as many as bring a slice down to 8192 keys while all of them are resident at once (two per SM),
-  // more where a slice would not fit shared memory.
+  // CTAs of a middle: as many as bring a slice down to 8192 keys while each has an SM to itself (96 middles of 32k on one
+  // CTA each take 20 us, on two 25), more where a slice would not fit shared memory.
   int CL = 1;
-  while (CL < 8 && (most / CL > MAX_KEYS || (most / CL > 8192 && 2LL * CL * n_seqs * s.Hkv <= 2LL * sm_count()))) CL *= 2;
+  while (CL < 8 && (most / CL > MAX_KEYS || (most / CL > 8192 && 2LL * CL * n_seqs * s.Hkv <= (long long)sm_count()))) CL *= 2;
   const bool cluster = CL > 1;
   const int per = most > 0 ? (most + CL - 1) / CL : 0;
   a.keys_cap = per <= MAX_KEYS ? per : 0;
