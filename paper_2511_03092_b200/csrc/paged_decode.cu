@@ -10,9 +10,9 @@
 // unit's output is written at once; a cut one leaves the sum, the maximum and the unnormalised output of its piece,
 // which the second launch joins in a fixed order (no atomics: equal inputs give equal bits).
 //
-// Tensor-core kernel (bf16, heads of 64, 128 or 256, pages of a multiple of 16 rows): the group's heads are the N
-// side of mma.sync.m16n8k16, S^T = K tile . Q^T and O^T += V tile^T . P^T, so the cost of a row does not grow with
-// the group.  Each warp runs a pipeline of its own over tiles fetched by TMA (four-dimensional map: dim, row of a
+// Tensor-core kernel (bf16, pages of a multiple of 8 rows): the group's heads are the N side of mma.sync.m16n8k16,
+// S^T = K tile . Q^T and O^T += V tile^T . P^T, so the cost of a row does not grow with the group.  It is built for
+// heads of up to 64, 128 and 256 dims; what a head lacks is neither read nor multiplied.  Each warp runs a pipeline of its own over tiles fetched by TMA (four-dimensional map: dim, row of a
 // page, KV head, page) with the 128-byte swizzle; the pipeline runs ahead over unit borders, and the page number
 // of the tile after next is fetched while a tile is computed.  The probabilities enter the second product as two bf16
 // numbers (p and what its rounding left), which keeps their rounding out of the result: 2^-17 instead of 2^-9.
@@ -41,7 +41,8 @@ using umma::mbar_init;
 using umma::mbar_try_wait;
 using umma::smem_u32;
 
-constexpr int TR = 16, STR = 8;                 // rows of a tile: tensor-core kernel, portable kernel
+constexpr int TR = 16;                          // rows of a tile of the tensor-core kernel
+__host__ __device__ constexpr int simt_rows(bool wide) { return wide ? 4 : 8; }   // ... of the portable kernel: 8 KB of single precision either way
 constexpr int UNIT_TILES = 6;                   // what a unit costs besides its tiles, in tiles; units of at most that many stay whole
 constexpr int MIN_TILES = 1;                    // a CTA gets at least that much beyond one unit's share (at least one: no stretch is empty)
 // (Measured over 40 calls of all sizes: 4 and 4 take 8 % longer, 8 and 1 2 %, 4 and 1 as long but 4 % longer for many short sequences.)
@@ -317,7 +318,9 @@ template <int D, int NWARP, int NSTAGE, int NG> struct MmaShape {
   static constexpr size_t smem = 1024 + stages_b + bars_b + (size_t)(2 * NCOL * LD + 2 * NWARP * NCOL + 2 * NCOL) * sizeof(float);
 };
 
-template <int D, int NWARP, int NSTAGE, int NG, int CTAS>
+// EXACT: heads of D dims and pages of a multiple of 16 rows, without the tests that other shapes need in the inner loops
+// (with them a 128-wide call takes 4 to 15 % longer, a 256-wide one half as long again).
+template <int D, int NWARP, int NSTAGE, int NG, int CTAS, bool EXACT>
 __global__ void __launch_bounds__(NWARP * 32, CTAS)
 paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v) {
   using S = MmaShape<D, NWARP, NSTAGE, NG>;
@@ -358,17 +361,24 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
   // Lane l looks up the page of the warp's tile l, l + 32, ...: one look-up's latency for 32 tiles.
   Place pr = at;
   bool valid = advance<TR>(a, held, pr, w + NWARP * lane, end);
-  int pid = 0, n_issued = 0;
-  unsigned bad_stage = 0, todo = 0;                                      // bit s: the tile in stage s is on a bad page; lanes with a tile to issue
-  const int tpp = a.map.page / TR;
-  int kvh_of = 0, row_of = 0;
+  // A page holds a multiple of 8 rows; where it is no multiple of 16, the tile's halves are looked up apart (one box each).
+  const bool halves = !EXACT && a.map.page % TR != 0;
+  int pid = -1, pid_hi = -1, n_issued = 0;
+  unsigned bad_stage = 0, todo = 0;                                      // bits 2 s, 2 s + 1: the halves of stage s are on a bad page; lanes with a tile to issue
+  int kvh_of = 0, row_of = 0, row_hi = 0;
   const auto fetch = [&]() {
     todo = __ballot_sync(0xffffffffu, valid);
-    if (valid) {
-      const int pg = pr.t / tpp;
-      pid = pr.len > 0 ? a.map.table[(long long)pr.slot * a.map.max_pages + pg] : -1;
-      row_of = (pr.t - pg * tpp) * TR;
+    if (valid && pr.len > 0) {
+      const int* table = a.map.table + (long long)pr.slot * a.map.max_pages;
+      const int row = pr.t * TR, pg = row / a.map.page;
+      pid = table[pg];
+      row_of = row - pg * a.map.page;
       kvh_of = pr.u / a.nhb;
+      if (halves) {
+        const int pg_hi = (row + TR / 2) / a.map.page;
+        pid_hi = row + TR / 2 < pr.len ? table[pg_hi] : 0;               // (no row there: any page will do)
+        row_hi = row + TR / 2 - pg_hi * a.map.page;
+      }
     }
   };
   fetch();
@@ -379,28 +389,36 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
 #pragma unroll
     for (int gi = 0; gi < NG; ++gi) {
       const int col = 8 * gi + gq;
-      const __nv_bfloat16* qp = q_all + ((long long)at.e * a.Hq + kvh * a.g + hb * a.gb + (col < nh ? col : 0)) * D + 2 * tq;
+      const __nv_bfloat16* qp = q_all + ((long long)at.e * a.Hq + kvh * a.g + hb * a.gb + (col < nh ? col : 0)) * (EXACT ? D : a.d_qk) + 2 * tq;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        qb[gi][ks][0] = col < nh ? *reinterpret_cast<const uint32_t*>(qp + 16 * ks) : 0u;
-        qb[gi][ks][1] = col < nh ? *reinterpret_cast<const uint32_t*>(qp + 16 * ks + 8) : 0u;
+        const bool there = col < nh && (EXACT || 16 * ks < a.d_qk);
+        qb[gi][ks][0] = there ? *reinterpret_cast<const uint32_t*>(qp + 16 * ks) : 0u;
+        qb[gi][ks][1] = there ? *reinterpret_cast<const uint32_t*>(qp + 16 * ks + 8) : 0u;
       }
     }
   };
   load_q();                                                              // (the first tiles' look-ups wait alongside)
+  const int d_qk = EXACT ? D : a.d_qk, d_v = EXACT ? D : a.d_v;
+  const unsigned tile_b = (unsigned)((d_qk + 63) / 64 + (d_v + 63) / 64) * SLAB_B;   // the slabs that hold anything
   const auto issue = [&]() {                                             // the lowest lane's tile of `todo`
     const int s = n_issued % NSTAGE, l = n_issued & 31;
-    const bool bad_mine = pid < 0 || pid >= a.map.n_pages;
-    const bool bad = (__ballot_sync(0xffffffffu, bad_mine) >> l) & 1u;
-    bad_stage = bad ? bad_stage | (1u << s) : bad_stage & ~(1u << s);
+    const unsigned lo = __ballot_sync(0xffffffffu, pid < 0 || pid >= a.map.n_pages);
+    const unsigned hi = halves ? __ballot_sync(0xffffffffu, pid_hi < 0 || pid_hi >= a.map.n_pages) : lo;
+    const unsigned bad = ((lo >> l) & 1u) | ((hi >> l) & 1u) << 1;
+    bad_stage = (bad_stage & ~(3u << (2 * s))) | bad << (2 * s);
     if (lane == l) {
       const uint32_t dst = stage0 + s * S::STAGE_B, bar = bar0 + 8 * s;
-      const int page = bad ? 0 : pid;
-      mbar_expect_tx(bar, (unsigned)S::STAGE_B);
+      mbar_expect_tx(bar, tile_b);
+#pragma unroll 1
+      for (int half = 0; half <= (int)halves; ++half) {
+        const int page = (bad >> half) & 1u ? 0 : half ? pid_hi : pid, row = half ? row_hi : row_of;
+        const uint32_t at = dst + half * (SLAB_B / 2);
 #pragma unroll
-      for (int h = 0; h < S::NSL; ++h) {
-        tma_load_4d(dst + h * SLAB_B, &tmap_k, 64 * h, row_of, kvh_of, page, bar);
-        tma_load_4d(dst + S::TENS_B + h * SLAB_B, &tmap_v, 64 * h, row_of, kvh_of, page, bar);
+        for (int h = 0; h < S::NSL; ++h) {
+          if (64 * h < d_qk) tma_load_4d(at + h * SLAB_B, &tmap_k, 64 * h, row, kvh_of, page, bar);
+          if (64 * h < d_v) tma_load_4d(at + S::TENS_B + h * SLAB_B, &tmap_v, 64 * h, row, kvh_of, page, bar);
+        }
       }
       if (bad && a.status) atomicOr(a.status, SNAP_DEV_BAD_PAGE);
     }
@@ -441,14 +459,16 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
       const bool landed = wait_bounded(bar0 + 8 * s, (unsigned)(n / NSTAGE) & 1u);
       if (__any_sync(0xffffffffu, !landed)) { dead = true; break; }
       const int row0 = (at.t + (w + n * NWARP - done)) * TR;
-      const int nrows = (bad_stage >> s) & 1u ? 0 : min(at.len - row0, TR);
+      const int nrows = min(at.len - row0, TR);
+      const unsigned bad = (bad_stage >> (2 * s)) & 3u;
       const uint32_t sK = stage0 + s * S::STAGE_B, sV = sK + S::TENS_B;
-      if (nrows < TR) {
-        // rows past the end may hold anything, and a zero probability does not silence a NaN in V: clear them
+      if (nrows < TR || bad) {
+        // rows past the end, or on a bad page, may hold anything, and a zero probability does not silence a NaN in V: clear them
         constexpr int CPR = D / 8;
-        for (int x = lane; x < (TR - nrows) * CPR; x += 32) {
-          const int r = nrows + x / CPR, c = x % CPR;
-          *reinterpret_cast<uint4*>(wstages + s * S::STAGE_B + S::TENS_B + (c >> 3) * SLAB_B + swz(r, c & 7)) = make_uint4(0, 0, 0, 0);
+        for (int x = lane; x < TR * CPR; x += 32) {
+          const int r = x / CPR, c = x % CPR;
+          if (r >= nrows || (bad >> (r >> 3)) & 1u)
+            *reinterpret_cast<uint4*>(wstages + s * S::STAGE_B + S::TENS_B + (c >> 3) * SLAB_B + swz(r, c & 7)) = make_uint4(0, 0, 0, 0);
         }
         __syncwarp();
       }
@@ -458,6 +478,7 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
       for (int gi = 0; gi < NG; ++gi) v[gi][0] = v[gi][1] = v[gi][2] = v[gi][3] = 0.f;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
+        if (!EXACT && 16 * ks >= d_qk) break;
         uint32_t af[4];
         ldsm4(sK + (ks >> 2) * SLAB_B + swz(k_row, (ks & 3) * 2 + k_cadd), af);
 #pragma unroll
@@ -467,7 +488,8 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
 #pragma unroll
       for (int gi = 0; gi < NG; ++gi) {
 #pragma unroll
-        for (int x = 0; x < 4; ++x) v[gi][x] = gq + (x >> 1) * 8 < nrows ? v[gi][x] * a.scale_log2 : -INFINITY;
+        for (int x = 0; x < 4; ++x)
+          v[gi][x] = gq + (x >> 1) * 8 < nrows && !((bad >> (x >> 1)) & 1u) ? v[gi][x] * a.scale_log2 : -INFINITY;
         refresh = refresh || fmaxf(v[gi][0], v[gi][2]) > m_ref[gi][0] + 8.f || fmaxf(v[gi][1], v[gi][3]) > m_ref[gi][1] + 8.f;
       }
       if (srow) {
@@ -527,6 +549,7 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
       // ---- O^T += V tile^T . P^T ----
 #pragma unroll
       for (int db = 0; db < KS; ++db) {
+        if (!EXACT && 16 * db >= d_v) break;
         uint32_t af[4];
         ldsm4t(sV + (db >> 2) * SLAB_B + swz(v_row, (db & 3) * 2 + v_cadd), af);
 #pragma unroll
@@ -641,10 +664,10 @@ constexpr int MAX_STAGES = 6;                     // of a warp
 // NV: 128-dim chunks of a row, HB: heads of a unit (a power of two)
 template <typename T, int NV, int HB, int CTAS>
 __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v) {
-  constexpr int LD = 128 * NV + 4;
+  constexpr int LD = 128 * NV + 4, STR = simt_rows(NV > 1), TPL = 32 / STR;   // tiles that a warp looks up at once, a lane per row
   constexpr int NVAL = 4 * HB, HL = 8 / HB;                              // (row, head) pairs of four rows; lanes that hold the same pair
   extern __shared__ unsigned char smem_dyn[];
-  // [SNW][a.stages][8 key rows | 8 value rows], on a 128-byte boundary as every part of it is (rows are multiples of 32 bytes)
+  // [SNW][a.stages][STR key rows | STR value rows], on a 128-byte boundary as every part of it is (rows are multiples of 32 bytes)
   unsigned char* stages = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 127) & ~uintptr_t(127));
   __shared__ __align__(16) float buf[2 * HB * LD];
   __shared__ float wm[SNW * HB], wl[SNW * HB], jm[HB], jl[HB];
@@ -668,16 +691,17 @@ __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_cons
   if (!locate<STR, SNT>(a, at, end, held, scan, found)) return;
   const int my_head = (lane & 7) / HL;                                   // after the exchange lane l owns row l / 8 and this head
 
-  // ---- the warp's producer: lane l looks up row l % 8 of the warp's tile l / 8, l / 8 + 4, ... ----
+  // ---- the warp's producer: lane l looks up row l % STR of the warp's tile l / STR, l / STR + TPL, ... ----
   Place pr = at;
-  bool valid = advance<STR>(a, held, pr, w + SNW * (lane >> 3), end);
-  int pid = -1, prow = 0, kvh_of = 0, s_in = 0, in_flight = 0, next = 0;  // next: which of the four tiles is issued next
-  unsigned todo = 0;                                                     // bit 8 j: tile j is there
+  bool valid = advance<STR>(a, held, pr, w + SNW * (lane / STR), end);
+  int pid = -1, prow = 0, kvh_of = 0, s_in = 0, in_flight = 0, next = 0;  // next: which of the TPL tiles is issued next
+  constexpr unsigned ROWS = (1u << STR) - 1u;
+  unsigned todo = 0;                                                     // bit STR j: tile j is there
   unsigned long long okay_of = 0;                                        // 8 bits per stage: the rows that are there
   const auto fetch = [&]() {
     todo = __ballot_sync(0xffffffffu, valid);
     pid = -1;
-    const int row = pr.t * STR + (lane & 7);
+    const int row = pr.t * STR + lane % STR;
     if (valid && row < pr.len) {
       const int pg = row / a.map.page;
       prow = row - pg * a.map.page;
@@ -686,15 +710,15 @@ __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_cons
     }
   };
   const auto issue = [&]() {
-    const bool mine = lane >> 3 == next, bad = mine && valid && pr.t * STR + (lane & 7) < pr.len && (pid < 0 || pid >= a.map.n_pages);
+    const bool mine = lane / STR == next, bad = mine && valid && pr.t * STR + lane % STR < pr.len && (pid < 0 || pid >= a.map.n_pages);
     if (bad) {
       pid = -1;
       if (a.status) atomicOr(a.status, SNAP_DEV_BAD_PAGE);
     }
-    const unsigned okay = (__ballot_sync(0xffffffffu, pid >= 0) >> (8 * next)) & 0xffu;
+    const unsigned okay = (__ballot_sync(0xffffffffu, pid >= 0) >> (STR * next)) & ROWS;
     okay_of = (okay_of & ~(0xffull << (8 * s_in))) | ((unsigned long long)okay << (8 * s_in));
     const uint32_t bar = bar0 + 8 * s_in, dst = stage0 + s_in * stage_b;
-    const int r = lane & 7;
+    const int r = lane % STR;
     if (a.tiled) {                                                       // one copy each for the tile's keys and values
       if (mine && r == 0) {
         mbar_expect_tx(bar, okay ? stage_b : 0u);
@@ -713,10 +737,10 @@ __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_cons
     }
     ++in_flight;
     if (++s_in == a.stages) s_in = 0;
-    todo &= ~(0xffu << (8 * next));
-    if (++next == 4) {
+    todo &= ~(ROWS << (STR * next));
+    if (++next == TPL) {
       next = 0;
-      if (valid) valid = advance<STR>(a, held, pr, 4 * SNW, end);
+      if (valid) valid = advance<STR>(a, held, pr, TPL * SNW, end);
       fetch();
     }
   };
@@ -1135,30 +1159,36 @@ __global__ void __launch_bounds__(JNT) paged_join_kernel(const __grid_constant__
 // ---------------------------------------------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------------------------------------------
-template <int D, int NWARP, int NSTAGE, int NG, int CTAS>
-cudaError_t launch_mma(const PagedArgs& a, const CUtensorMap& tk, const CUtensorMap& tv, cudaStream_t st) {
+template <int D, int NWARP, int NSTAGE, int NG, int CTAS, bool EXACT>
+cudaError_t launch_mma_as(const PagedArgs& a, const CUtensorMap& tk, const CUtensorMap& tv, cudaStream_t st) {
   using S = MmaShape<D, NWARP, NSTAGE, NG>;
   static SmemLimit limit = {};
-  if (cudaError_t e = ensure_dyn_smem(paged_mma_kernel<D, NWARP, NSTAGE, NG, CTAS>, S::smem, limit)) return e;
-  const cudaError_t e = launch_pdl(paged_mma_kernel<D, NWARP, NSTAGE, NG, CTAS>, dim3(a.ctas), dim3(S::NT), S::smem, st, a, tk, tv);
+  if (cudaError_t e = ensure_dyn_smem(paged_mma_kernel<D, NWARP, NSTAGE, NG, CTAS, EXACT>, S::smem, limit)) return e;
+  const cudaError_t e = launch_pdl(paged_mma_kernel<D, NWARP, NSTAGE, NG, CTAS, EXACT>, dim3(a.ctas), dim3(S::NT), S::smem, st, a, tk, tv);
   count_launch();
   return e;
+}
+
+template <int D, int NWARP, int NSTAGE, int NG, int CTAS>
+cudaError_t launch_mma(const PagedArgs& a, const CUtensorMap& tk, const CUtensorMap& tv, cudaStream_t st) {
+  return a.d_qk == D && a.d_v == D && a.map.page % TR == 0 ? launch_mma_as<D, NWARP, NSTAGE, NG, CTAS, true>(a, tk, tv, st)
+                                                           : launch_mma_as<D, NWARP, NSTAGE, NG, CTAS, false>(a, tk, tv, st);
 }
 
 // CTAs per SM that the kernels are built for (launch bounds, and the shared memory of the tensor-core ones)
 constexpr int kMmaCtas = 3, kMmaCtasWide = 2;
 constexpr int simt_ctas(bool wide, int gb) { return wide ? 2 : 3; }
 // Stages of a warp of the portable kernel: what the CTAs of an SM leave each other of its shared memory.
-int simt_stages(const Shape& s, int eb, int ctas) {
-  const int stage = STR * (s.d_qk + s.d_v) * eb, n = (210 * 1024 / ctas - 20 * 1024) / (SNW * stage);
-  return n < 2 ? 2 : n > MAX_STAGES ? MAX_STAGES : n;
+int simt_stages(const Shape& s, int eb, int ctas, bool wide) {
+  const int stage = simt_rows(wide) * (s.d_qk + s.d_v) * eb, n = (228 * 1024 / ctas - 11500) / (SNW * stage);   // 11.5 KB: static and reserved
+  return n < 1 ? 1 : n > MAX_STAGES ? MAX_STAGES : n;
 }
 
 template <typename T, int NV, int HB>
 cudaError_t launch_simt_hb(const PagedArgs& a, const CUtensorMap& tk, const CUtensorMap& tv, cudaStream_t st) {
   constexpr int C = simt_ctas(NV > 1, HB);
   static SmemLimit limit = {};
-  const size_t smem = (size_t)SNW * a.stages * STR * (a.d_qk + a.d_v) * sizeof(T) + 128;
+  const size_t smem = (size_t)SNW * a.stages * a.tr * (a.d_qk + a.d_v) * sizeof(T) + 128;
   if (cudaError_t e = ensure_dyn_smem(paged_simt_kernel<T, NV, HB, C>, smem, limit)) return e;
   const cudaError_t e = launch_pdl(paged_simt_kernel<T, NV, HB, C>, dim3(a.ctas), dim3(SNT), smem, st, a, tk, tv);
   count_launch();
@@ -1172,15 +1202,14 @@ cudaError_t launch_simt(const PagedArgs& a, const CUtensorMap& tk, const CUtenso
   return launch_simt_hb<T, 1, 8>(a, tk, tv, st);
 }
 
-bool mma_shape(int dtype, const Shape& s, const PageMap& m) {
-  return dtype == SNAP_BF16 && s.d_qk == s.d_v && (s.d_qk == 64 || s.d_qk == 128 || s.d_qk == 256) && m.page % TR == 0 &&
-         umma::encode_tiled_fn() != nullptr;
+bool mma_shape(int dtype, const PageMap& m) {
+  return dtype == SNAP_BF16 && m.page % (TR / 2) == 0 && umma::encode_tiled_fn() != nullptr;
 }
 
 }  // namespace
 
 int paged_decode_plan(int dtype, const Shape& s, const PageMap& m, int n_active, bool weights, int sms, PagedDecodePlan* p) {
-  p->mma = mma_shape(dtype, s, m);
+  p->mma = mma_shape(dtype, m);
   const bool wide = s.d_qk > 128 || s.d_v > 128;
   const int most = p->mma ? 16 : wide ? 4 : 8;                          // heads of a unit
   p->nhb = (s.g + most - 1) / most;
@@ -1191,8 +1220,7 @@ int paged_decode_plan(int dtype, const Shape& s, const PageMap& m, int n_active,
   const long long chunks = (m.cap + JROWS - 1) / JROWS;
   // grid and index limits; a line of tiles and the scratch have to be countable
   if (units > (1LL << 30) || (long long)n_active * s.Hq > 0x7fffffffLL || (weights && (long long)n_active * s.Hkv * chunks > 0x7fff0000LL) ||
-      units * ((m.cap + STR - 1) / STR + UNIT_TILES) > (1LL << 37) ||
-      (long long)n_active * ((m.cap + STR - 1) / STR + UNIT_TILES) > 0x7fffffffLL)
+      units * (m.cap / 4LL + 1 + UNIT_TILES) > (1LL << 37) || n_active * (m.cap / 4LL + 1 + UNIT_TILES) > 0x7fffffffLL)
     return SNAP_ERR_UNSUPPORTED;
   size_t off = 0;
   p->prefix_off = off; off += align_up((size_t)(n_active + 1) * sizeof(int));
@@ -1219,30 +1247,32 @@ cudaError_t launch_paged_decode(int dtype, const Shape& s, const PageMap& m, con
   a.o_part = reinterpret_cast<float*>(scratch + p.o_off);
   a.scores = w_out ? reinterpret_cast<float*>(scratch + p.score_off) : nullptr;
   a.w_in = w_in; a.w_out = w_out; a.status = status; a.ctas = p.ctas;
-  a.tr = p.mma ? TR : STR;
   const bool wide = s.d_qk > 128 || s.d_v > 128;
-  a.stages = simt_stages(s, elt_bytes(dtype), simt_ctas(wide, p.gb));
+  a.tr = p.mma ? TR : simt_rows(wide);
+  a.stages = simt_stages(s, elt_bytes(dtype), simt_ctas(wide, p.gb), wide);
   // Tiles come through tensor maps where a page holds whole ones: 64 dims wide with the 128-byte swizzle for the
   // tensor-core kernel, whole rows for the portable one.  (Encoding both takes the host under a microsecond.)
   CUtensorMap tk = {}, tv = {};
   const umma::EncodeTiledFn enc = umma::encode_tiled_fn();
+  const int rows = p.mma && m.page % TR ? TR / 2 : a.tr;       // of a box
   const auto encode = [&](CUtensorMap* t, const void* base, int d, long long ps, long long hs, long long rs) {
     const cuuint64_t eb = (cuuint64_t)elt_bytes(dtype);
     const cuuint64_t dims[4] = {(cuuint64_t)d, (cuuint64_t)m.page, (cuuint64_t)s.Hkv, (cuuint64_t)m.n_pages};
     // a stride that is never applied (one KV head, one page) may be anything: the map gets one that it takes
     const cuuint64_t strides[3] = {(cuuint64_t)rs * eb, (cuuint64_t)(s.Hkv > 1 ? hs : d) * eb, (cuuint64_t)(m.n_pages > 1 ? ps : d) * eb};
-    const cuuint32_t box[4] = {(cuuint32_t)(p.mma ? 64 : d), (cuuint32_t)a.tr, 1, 1}, estr[4] = {1, 1, 1, 1};
+    const cuuint32_t box[4] = {(cuuint32_t)(p.mma ? 64 : d), (cuuint32_t)rows, 1, 1}, estr[4] = {1, 1, 1, 1};
     return enc(t, dtype == SNAP_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims,
                strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, p.mma ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
   };
-  a.tiled = m.page % a.tr == 0 && enc && encode(&tk, k_pages, s.d_qk, m.kp, m.kh, m.kr) && encode(&tv, v_pages, s.d_v, m.vp, m.vh, m.vr);
+  a.tiled = m.page % rows == 0 && enc && encode(&tk, k_pages, s.d_qk, m.kp, m.kh, m.kr) && encode(&tv, v_pages, s.d_v, m.vp, m.vh, m.vr);
   cudaError_t e;
   if (p.mma) {
     if (!a.tiled) return cudaErrorInvalidValue;
     const bool two = p.gb > 8;
-    if (s.d_qk == 128) e = two ? launch_mma<128, 4, 2, 2, kMmaCtasWide>(a, tk, tv, st) : launch_mma<128, 4, 2, 1, kMmaCtas>(a, tk, tv, st);
-    else if (s.d_qk == 64) e = two ? launch_mma<64, 4, 4, 2, kMmaCtasWide>(a, tk, tv, st) : launch_mma<64, 4, 4, 1, kMmaCtas>(a, tk, tv, st);
+    const int d = s.d_qk > s.d_v ? s.d_qk : s.d_v;
+    if (d <= 64) e = two ? launch_mma<64, 4, 4, 2, kMmaCtasWide>(a, tk, tv, st) : launch_mma<64, 4, 4, 1, kMmaCtas>(a, tk, tv, st);
+    else if (d <= 128) e = two ? launch_mma<128, 4, 2, 2, kMmaCtasWide>(a, tk, tv, st) : launch_mma<128, 4, 2, 1, kMmaCtas>(a, tk, tv, st);
     else e = two ? launch_mma<256, 2, 2, 2, kMmaCtasWide>(a, tk, tv, st) : launch_mma<256, 2, 2, 1, kMmaCtas>(a, tk, tv, st);
   } else if (dtype == SNAP_F32) {
     e = wide ? launch_simt<float, 2>(a, tk, tv, st) : launch_simt<float, 1>(a, tk, tv, st);

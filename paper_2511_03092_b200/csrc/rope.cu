@@ -55,6 +55,7 @@ __global__ void __launch_bounds__(NT, 5) rope_kernel(const __grid_constant__ Rop
   const RopeArgs& a = L.a;
   extern __shared__ float2 table[];                                      // [Z][rot / 2]
   __shared__ int dup[NT];
+  __shared__ int2 placed[NT];                                             // slot and row of each of the block's tokens, row -1: skipped
   const int tid = threadIdx.x, x = tid % L.X, y = (tid / L.X) % L.Y, z = tid / (L.X * L.Y);
   const int t = blockIdx.x * L.Z + z, half = a.rot / 2;
   const bool mine = z < L.Z && t < a.n_tokens;                            // the block may have spare threads
@@ -105,6 +106,7 @@ __global__ void __launch_bounds__(NT, 5) rope_kernel(const __grid_constant__ Rop
   };
   if (mine && x < L.nj && y < H) load(x, y);                              // on their way while the angles are computed
 
+  if (paged && x == 0 && y == 0 && z < L.Z) placed[z] = make_int2(slot, skip ? -1 : row);
   // ---- values: copied to the page while the angles are on their way ----
   if (paged && !skip) {
     const T* v = static_cast<const T*>(a.v) + t * a.v_tok;
@@ -135,7 +137,10 @@ __global__ void __launch_bounds__(NT, 5) rope_kernel(const __grid_constant__ Rop
   if (mine && paged && x == 0 && y == 0) {
     if (bad && a.status) atomicOr(a.status, bad);
     if (!skip) {
-      if (a.rows) atomicMax(&a.seq_len[slot], row + 1);
+      // of a run of a sequence's rows the last one speaks for all (thousands of tokens share a length)
+      if (a.rows) {
+        if (!(z + 1 < L.Z && placed[z + 1].x == slot && placed[z + 1].y > row)) atomicMax(&a.seq_len[slot], row + 1);
+      }
       else a.seq_len[slot] = row + 1;                                     // this token alone has the slot
     }
   }
@@ -182,7 +187,15 @@ __global__ void __launch_bounds__(NT, 5) rope_kernel(const __grid_constant__ Rop
   // ---- the head's other dims ----
   for (int c = x; c < L.nc; c += L.X) {
     const int at = c * V < a.offset ? c * V : c * V + a.rot;
-    for (int h = y; h < H; h += L.Y) put(h, at, *reinterpret_cast<const Raw*>(source(h) + at));
+    for (int h0 = y; h0 < H; h0 += 4 * L.Y) {
+      Raw r[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (h0 + u * L.Y < H) r[u] = *reinterpret_cast<const Raw*>(source(h0 + u * L.Y) + at);
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (h0 + u * L.Y < H) put(h0 + u * L.Y, at, r[u]);
+    }
   }
   if (paged) {
     if (a.weights && x == 0)
