@@ -315,7 +315,7 @@ template <int D, int NWARP, int NSTAGE, int NG> struct MmaShape {
   static constexpr int LD = D + 4;               // column stride of the exchange buffers: fragments store without bank conflicts
   static constexpr size_t stages_b = (size_t)NWARP * NSTAGE * STAGE_B;
   static constexpr size_t bars_b = NWARP * NSTAGE * 8;
-  static constexpr size_t smem = 1024 + stages_b + bars_b + (size_t)(2 * NCOL * LD + 2 * NWARP * NCOL + 2 * NCOL) * sizeof(float);
+  static constexpr size_t smem = 1024 + stages_b + bars_b + (size_t)(NWARP / 2 * NCOL * LD + 2 * NWARP * NCOL + 2 * NCOL) * sizeof(float);
 };
 
 // EXACT: heads of D dims and pages of a multiple of 16 rows, without the tests that other shapes need in the inner loops
@@ -328,8 +328,8 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
   extern __shared__ unsigned char smem_dyn[];
   unsigned char* stages = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~uintptr_t(1023));
   uint64_t* bars = reinterpret_cast<uint64_t*>(stages + S::stages_b);
-  float* buf = reinterpret_cast<float*>(bars + NWARP * NSTAGE);          // [2][NCOL][LD]
-  float* wm = buf + 2 * NCOL * LD;                                       // [NWARP][NCOL] maxima, then sums
+  float* buf = reinterpret_cast<float*>(bars + NWARP * NSTAGE);          // [NWARP / 2][NCOL][LD]
+  float* wm = buf + NWARP / 2 * NCOL * LD;                                       // [NWARP][NCOL] maxima, then sums
   float* wl = wm + NWARP * NCOL;
   float* jm = wl + NWARP * NCOL;                                         // [NCOL] joined maxima, then sums
   float* jl = jm + NCOL;
@@ -473,17 +473,28 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
         __syncwarp();
       }
       // ---- S^T = K tile . Q^T ----
-      float v[NG][4];
+      // one column group: two accumulators, of even and odd steps, make the chain of dependent products half as long
+      constexpr int CH = NG == 1 ? 2 : 1;
+      float vc[CH][NG][4];
 #pragma unroll
-      for (int gi = 0; gi < NG; ++gi) v[gi][0] = v[gi][1] = v[gi][2] = v[gi][3] = 0.f;
+      for (int ch = 0; ch < CH; ++ch)
+#pragma unroll
+        for (int gi = 0; gi < NG; ++gi)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) vc[ch][gi][x] = 0.f;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         if (!EXACT && 16 * ks >= d_qk) break;
         uint32_t af[4];
         ldsm4(sK + (ks >> 2) * SLAB_B + swz(k_row, (ks & 3) * 2 + k_cadd), af);
 #pragma unroll
-        for (int gi = 0; gi < NG; ++gi) mma16816(v[gi], af, qb[gi][ks][0], qb[gi][ks][1]);
+        for (int gi = 0; gi < NG; ++gi) mma16816(vc[ks % CH][gi], af, qb[gi][ks][0], qb[gi][ks][1]);
       }
+      float v[NG][4];
+#pragma unroll
+      for (int gi = 0; gi < NG; ++gi)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) v[gi][x] = CH == 2 ? vc[0][gi][x] + vc[CH - 1][gi][x] : vc[0][gi][x];
       bool refresh = false;
 #pragma unroll
       for (int gi = 0; gi < NG; ++gi) {
@@ -1162,6 +1173,7 @@ __global__ void __launch_bounds__(JNT) paged_join_kernel(const __grid_constant__
 template <int D, int NWARP, int NSTAGE, int NG, int CTAS, bool EXACT>
 cudaError_t launch_mma_as(const PagedArgs& a, const CUtensorMap& tk, const CUtensorMap& tv, cudaStream_t st) {
   using S = MmaShape<D, NWARP, NSTAGE, NG>;
+  static_assert(CTAS * (S::smem + sizeof(Held) + 1280) <= 228 * 1024, "all CTAs of the grid are resident at once");
   static SmemLimit limit = {};
   if (cudaError_t e = ensure_dyn_smem(paged_mma_kernel<D, NWARP, NSTAGE, NG, CTAS, EXACT>, S::smem, limit)) return e;
   const cudaError_t e = launch_pdl(paged_mma_kernel<D, NWARP, NSTAGE, NG, CTAS, EXACT>, dim3(a.ctas), dim3(S::NT), S::smem, st, a, tk, tv);
