@@ -471,7 +471,9 @@ int snap_rope(const snap_config_t* cfg, const snap_rope_config_t* rope, const do
  * Rows need not be in position order: attention does not depend on it, and snap_paged_append takes
  * positions apart from rows.  Sequences may share pages that are only read.
  * The calls take heads up to 256 wide and no latent layout (SNAP_ERR_UNSUPPORTED otherwise); bf16 layers with
- * d_qk = d_v of 64, 128 or 256 and pages of a multiple of 16 rows run on tensor cores.  All are safe to capture.
+ * pages of a multiple of 8 rows run on tensor cores, fastest with heads of 64, 128 or 256 and pages of a multiple of 16.
+ * All can be captured into CUDA graphs.  Lengths, tables and slots are read on the device when a call runs; nothing may
+ * change them while it does.
  */
 typedef struct snap_paged {
   int32_t page_tokens;    /* rows of a page, >= 1 */
@@ -489,7 +491,7 @@ typedef struct snap_paged {
  *   rows_dev  [n_tokens] int32: the row each token is written to; afterwards seq_len[slot] is at least row + 1.
  *             No (slot, row) twice.  NULL: every token is its sequence's next one, row = seq_len[slot], and
  *             seq_len[slot] grows by one; a slot that is listed a second time in the call is skipped
- *             (SNAP_DEV_BAD_SLOT).
+ *             (SNAP_DEV_BAD_SLOT); at most 65536 tokens (SNAP_ERR_INVALID_ARG).
  *   rope, freqs_dev, positions_dev: as in snap_rope; rope NULL = the keys are stored as given (the other
  *             two are ignored); positions_dev NULL = the position is the row
  *   k_dev, v_dev  (t, h, c) at [t * token_stride + h * head_stride + c]

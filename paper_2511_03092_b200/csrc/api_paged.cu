@@ -164,7 +164,7 @@ int snap_paged_append(const snap_config_t* cfg, const snap_paged_t* paged,
     if (rc != SNAP_OK) return rc;
     if (rope->rot_dim > cfg->d_qk - rope->rot_offset) return SNAP_ERR_INVALID_ARG;
   }
-  if (n_tokens < 0) return SNAP_ERR_INVALID_ARG;
+  if (n_tokens < 0 || (!rows_dev && n_tokens > 65536)) return SNAP_ERR_INVALID_ARG;   // (each token looks for its slot among those before it)
   if (n_tokens == 0) return SNAP_OK;
   if (!slot_ids_dev || !k_dev || !v_dev || !k_pages_dev || !v_pages_dev || !page_table_dev || !seq_len_dev || (rope && !freqs_dev) ||
       !q_dev != !q_out_dev)

@@ -637,3 +637,51 @@ def test_calls_on_a_side_stream_and_two_at_once():
     for i in range(2):
         assert all(torch.equal(x, want[i]) for x in got[i])
     assert c.bits() == 0
+
+
+def test_first_calls_inside_a_capture():
+    """Shapes that no call has used before, captured at once: what a call sets up on the host is not a stream operation."""
+    cfg = config(6, 2, 32, 48, "bf16", max_seqs=2, sink=1, recent=2, topk=5)
+    c = Pages(cfg, "bf16", 8, [30, 8], seed=2)
+    c.lengths = [30, 0]
+    c.seq_len.copy_(i32(c.lengths))
+    q = torch.randn(1, 6, 32, device="cuda").to(torch.bfloat16)
+    k, v = torch.randn(1, 2, 32, device="cuda").to(torch.bfloat16), torch.randn(1, 2, 48, device="cuda").to(torch.bfloat16)
+    w, out = c.weights(), torch.zeros(1, 6, 48, dtype=torch.bfloat16, device="cuda")
+    before = (f64(c.k), f64(c.v))
+    ids, src, dst = i32([0]), i32([0]), i32([1])
+    rope, freqs = B.make_rope(rot_dim=12, rot_offset=2), torch.from_numpy(orc.rope_table(12, 10000.0)).cuda()
+    ws = torch.empty(B.snap_paged_decode_workspace_bytes(cfg, c.paged, 1, True), dtype=torch.uint8, device="cuda")
+    ws2 = torch.empty(B.snap_paged_evict_workspace_bytes(cfg, c.paged, 1), dtype=torch.uint8, device="cuda")
+    kept = torch.zeros(1, 2, 8, dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.snap_paged_append(cfg, c.paged, ids, None, k, v, c.k, c.v, c.table, c.seq_len, rope=rope, freqs=freqs, weights=w, status=c.status)
+        B.snap_paged_decode_attn(cfg, c.paged, q, ids, 1, c.k, c.v, c.table, c.seq_len, out, ws, weights_in=w, weights_out=w, status=c.status)
+        B.snap_paged_evict(cfg, c.paged, src, dst, 1, c.k, c.v, c.table, c.seq_len, w, w, ws2, kept_rows=kept, status=c.status)
+    torch.cuda.synchronize()
+    np.testing.assert_array_equal(f64(c.k), before[0])      # capturing ran nothing
+    graph.replay()
+    torch.cuda.synchronize()
+    c.lengths = [31, 0]
+    assert c.seq_len.tolist() == [31, 8] and c.bits() == 0
+    check_decode(c, out, q, [0], "bf16")
+    for h in range(2):
+        np.testing.assert_array_equal(kept.cpu().numpy()[0, h], orc.kept_rows(f64(w)[0, h], 31, 1, 2, 5))
+
+
+def test_the_paged_calls_under_the_checked_build():
+    """Eviction, append and attention once more with the build that tests data-dependent indices (a bad one raises a status
+    bit, which these tests require to be clear)."""
+    import os
+    import subprocess
+    import sys
+    from paper_2511_03092_b200 import build as snap_build
+    lib = snap_build.build(debug_bounds=True)
+    env = dict(os.environ, SNAP_LIBRARY=os.path.basename(lib))
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-m", "pytest", "tests/test_gpu_paged.py", "-m", "gpu", "-q", "-x", "-p", "no:cacheprovider",
+                        "-k", "evict or append or ragged or together or steps"], cwd=root, env=env, capture_output=True, text=True, timeout=900)
+    assert r.returncode == 0, r.stdout[-3000:] + r.stderr[-2000:]
+    assert " passed" in r.stdout

@@ -126,6 +126,7 @@ def test_paged_calls_refuse_bad_arguments():
     assert ap(rope=B.make_rope(rot_dim=128)) == -4                      # no frequencies
     assert ap(rope=B.make_rope(rot_dim=256), freqs=one) == -1
     assert ap(ks=(1024, 100)) == -1 and ap(vs=(-1024, 128)) == -1 and ap(k=odd) == -1 and ap(q=one, qo=odd) == -1
+    assert ap(rows=None, n=65537) == -1                                 # every token the next one of its sequence: a batch, not a prompt
     assert ap(ko=one, ks=(6144, 128)) == -1                             # in place, but not dense like the output
     assert dec(slots=None) == -4 and dec(q=None) == -4 and dec(out=None) == -4 and dec(ws=None) == -4 and dec(wi=one) == -4
     assert dec(q=odd) == -1 and dec(out=odd) == -1 and dec(ws=odd) == -1
