@@ -318,13 +318,18 @@ template <int D, int NWARP, int NSTAGE, int NG> struct MmaShape {
   static constexpr size_t smem = 1024 + stages_b + bars_b + (size_t)(NWARP / 2 * NCOL * LD + 2 * NWARP * NCOL + 2 * NCOL) * sizeof(float);
 };
 
-// EXACT: heads of D dims and pages of a multiple of 16 rows, without the tests that other shapes need in the inner loops
-// (with them a 128-wide call takes 4 to 15 % longer, a 256-wide one half as long again).
-template <int D, int NWARP, int NSTAGE, int NG, int CTAS, bool EXACT>
+// How a tile comes in.  EXACT: through the tensor maps, heads of D dims and pages of a multiple of 16 rows, without the
+// tests that other shapes need in the inner loops (with them a 128-wide call takes 4 to 15 % longer, a 256-wide one half
+// as long again).  BOXES: through the tensor maps, pages of a multiple of 8 rows.  ROWS: any pages; the lanes copy a
+// row's 16-byte pieces themselves (cp.async), each from the page of its row.
+enum class Tiles { EXACT, BOXES, ROWS };
+template <int D, int NWARP, int NSTAGE, int NG, int CTAS, Tiles MODE>
 __global__ void __launch_bounds__(NWARP * 32, CTAS)
 paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v) {
   using S = MmaShape<D, NWARP, NSTAGE, NG>;
   constexpr int KS = S::KS, NCOL = S::NCOL, LD = S::LD;
+  constexpr bool EXACT = MODE == Tiles::EXACT, BY_ROWS = MODE == Tiles::ROWS;
+  constexpr int LOOK = BY_ROWS ? 32 / TR : 32;                           // tiles that a warp looks up at once
   extern __shared__ unsigned char smem_dyn[];
   unsigned char* stages = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~uintptr_t(1023));
   uint64_t* bars = reinterpret_cast<uint64_t*>(stages + S::stages_b);
@@ -341,9 +346,9 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
   unsigned char* wstages = stages + w * NSTAGE * S::STAGE_B;
   const uint32_t stage0 = smem_u32(wstages), bar0 = smem_u32(bars + w * NSTAGE);
   if (lane == 0) {
-    for (int s = 0; s < NSTAGE; ++s) mbar_init(bar0 + 8 * s, 1);
+    for (int s = 0; s < NSTAGE; ++s) mbar_init(bar0 + 8 * s, BY_ROWS ? 32 : 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    if (w == 0) {
+    if (w == 0 && !BY_ROWS) {
       asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_k) : "memory");
       asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_v) : "memory");
     }
@@ -358,16 +363,30 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
 
   // ---- the warp's producer: runs NSTAGE tiles ahead of the consumer, over unit borders; warp w takes the CTA's tiles
   // w, w + NWARP, ... ----
-  // Lane l looks up the page of the warp's tile l, l + 32, ...: one look-up's latency for 32 tiles.
+  // Lane l looks up the page of the warp's tile l, l + 32, ...: one look-up's latency for 32 tiles.  (ROWS: of row l % 16
+  // of tile l / 16, l / 16 + 2, ...)
   Place pr = at;
-  bool valid = advance<TR>(a, held, pr, w + NWARP * lane, end);
-  // A page holds a multiple of 8 rows; where it is no multiple of 16, the tile's halves are looked up apart (one box each).
-  const bool halves = !EXACT && a.map.page % TR != 0;
+  bool valid = advance<TR>(a, held, pr, w + NWARP * (lane / (32 / LOOK)), end);
+  // BOXES: where a page is no multiple of 16 rows, the tile's halves are looked up apart (one box each).
+  const bool halves = MODE == Tiles::BOXES && a.map.page % TR != 0;
   int pid = -1, pid_hi = -1, n_issued = 0;
   unsigned bad_stage = 0, todo = 0;                                      // bits 2 s, 2 s + 1: the halves of stage s are on a bad page; lanes with a tile to issue
+  unsigned long long rows_stage = 0;                                     // ROWS: 16 bits per stage, the rows that are there
   int kvh_of = 0, row_of = 0, row_hi = 0;
   const auto fetch = [&]() {
     todo = __ballot_sync(0xffffffffu, valid);
+    if (BY_ROWS) {
+      pid = -1;
+      const int row = pr.t * TR + lane % TR;
+      if (valid && row < pr.len) {
+        const int pg = row / a.map.page;
+        row_of = row - pg * a.map.page;
+        kvh_of = pr.u / a.nhb;
+        pid = a.map.table[(long long)pr.slot * a.map.max_pages + pg];
+        if (pid < 0) pid = a.map.n_pages;                                // (bad, not absent)
+      }
+      return;
+    }
     if (valid && pr.len > 0) {
       const int* table = a.map.table + (long long)pr.slot * a.map.max_pages;
       const int row = pr.t * TR, pg = row / a.map.page;
@@ -401,7 +420,36 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
   load_q();                                                              // (the first tiles' look-ups wait alongside)
   const int d_qk = EXACT ? D : a.d_qk, d_v = EXACT ? D : a.d_v;
   const unsigned tile_b = (unsigned)((d_qk + 63) / 64 + (d_v + 63) / 64) * SLAB_B;   // the slabs that hold anything
+  const auto issue_rows = [&]() {                                        // the tile of the lower or upper half of the lanes
+    const int s = n_issued % NSTAGE, l = (n_issued % LOOK) * TR;
+    const unsigned okay = (__ballot_sync(0xffffffffu, pid >= 0 && pid < a.map.n_pages) >> l) & 0xffffu;
+    rows_stage = (rows_stage & ~(0xffffull << (16 * s))) | (unsigned long long)okay << (16 * s);
+    if (lane / TR == l / TR && pid >= a.map.n_pages && a.status) atomicOr(a.status, SNAP_DEV_BAD_PAGE);
+    const long long k_off = pid * a.map.kp + kvh_of * a.map.kh + row_of * a.map.kr, v_off = pid * a.map.vp + kvh_of * a.map.vh + row_of * a.map.vr;
+    // D / 8 lanes to a row (of a narrower head some have nothing to copy), RPI rows at a time
+    constexpr int CPR = D / 8, RPI = 32 / CPR;
+    const int c = lane % CPR;
+    const uint32_t dst = stage0 + s * S::STAGE_B + (c >> 3) * SLAB_B;
+    const __nv_bfloat16* kp = static_cast<const __nv_bfloat16*>(a.kp) + 8 * c;
+    const __nv_bfloat16* vp = static_cast<const __nv_bfloat16*>(a.vp) + 8 * c;
+#pragma unroll
+    for (int r0 = 0; r0 < TR; r0 += RPI) {
+      const int r = r0 + lane / CPR;
+      const long long ko = __shfl_sync(0xffffffffu, k_off, l + r), vo = __shfl_sync(0xffffffffu, v_off, l + r);
+      if ((okay >> r) & 1u) {
+        if (8 * c < d_qk) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + swz(r, c & 7)), "l"(kp + ko) : "memory");
+        if (8 * c < d_v) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + S::TENS_B + swz(r, c & 7)), "l"(vp + vo) : "memory");
+      }
+    }
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar0 + 8 * s) : "memory");
+    todo &= ~(0xffffu << l);
+    if (++n_issued % LOOK == 0) {
+      if (valid) valid = advance<TR>(a, held, pr, LOOK * NWARP, end);
+      fetch();
+    }
+  };
   const auto issue = [&]() {                                             // the lowest lane's tile of `todo`
+    if (BY_ROWS) { issue_rows(); return; }
     const int s = n_issued % NSTAGE, l = n_issued & 31;
     const unsigned lo = __ballot_sync(0xffffffffu, pid < 0 || pid >= a.map.n_pages);
     const unsigned hi = halves ? __ballot_sync(0xffffffffu, pid_hi < 0 || pid_hi >= a.map.n_pages) : lo;
@@ -460,14 +508,15 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
       if (__any_sync(0xffffffffu, !landed)) { dead = true; break; }
       const int row0 = (at.t + (w + n * NWARP - done)) * TR;
       const int nrows = min(at.len - row0, TR);
-      const unsigned bad = (bad_stage >> (2 * s)) & 3u;
+      const unsigned bad = BY_ROWS ? ~(unsigned)(rows_stage >> (16 * s)) & 0xffffu : (bad_stage >> (2 * s)) & 3u;
+      const auto there = [&](int r) { return BY_ROWS ? !((bad >> r) & 1u) : r < nrows && !((bad >> (r >> 3)) & 1u); };
       const uint32_t sK = stage0 + s * S::STAGE_B, sV = sK + S::TENS_B;
       if (nrows < TR || bad) {
         // rows past the end, or on a bad page, may hold anything, and a zero probability does not silence a NaN in V: clear them
         constexpr int CPR = D / 8;
         for (int x = lane; x < TR * CPR; x += 32) {
           const int r = x / CPR, c = x % CPR;
-          if (r >= nrows || (bad >> (r >> 3)) & 1u)
+          if (!there(r))
             *reinterpret_cast<uint4*>(wstages + s * S::STAGE_B + S::TENS_B + (c >> 3) * SLAB_B + swz(r, c & 7)) = make_uint4(0, 0, 0, 0);
         }
         __syncwarp();
@@ -500,7 +549,7 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
       for (int gi = 0; gi < NG; ++gi) {
 #pragma unroll
         for (int x = 0; x < 4; ++x)
-          v[gi][x] = gq + (x >> 1) * 8 < nrows && !((bad >> (x >> 1)) & 1u) ? v[gi][x] * a.scale_log2 : -INFINITY;
+          v[gi][x] = there(gq + (x >> 1) * 8) ? v[gi][x] * a.scale_log2 : -INFINITY;
         refresh = refresh || fmaxf(v[gi][0], v[gi][2]) > m_ref[gi][0] + 8.f || fmaxf(v[gi][1], v[gi][3]) > m_ref[gi][1] + 8.f;
       }
       if (srow) {
@@ -654,15 +703,9 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
 // portable kernel
 // ---------------------------------------------------------------------------------------------------------------
 struct Four { F2 a, b; };                          // four consecutive elements
-template <typename T> __device__ __forceinline__ Four four(const T* p);
-template <> __device__ __forceinline__ Four four<float>(const float* p) {
+__device__ __forceinline__ Four four(const float* p) {
   const ulonglong2 r = *reinterpret_cast<const ulonglong2*>(p);
   return {r.x, r.y};
-}
-template <> __device__ __forceinline__ Four four<__nv_bfloat16>(const __nv_bfloat16* p) {
-  const uint2 r = *reinterpret_cast<const uint2*>(p);
-  return {pack2(__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xffff0000u)),
-          pack2(__uint_as_float(r.y << 16), __uint_as_float(r.y & 0xffff0000u))};
 }
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, unsigned bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
@@ -673,7 +716,7 @@ constexpr int SNW = 4, SNT = SNW * 32;            // warps and threads of a CTA
 constexpr int MAX_STAGES = 6;                     // of a warp
 
 // NV: 128-dim chunks of a row, HB: heads of a unit (a power of two)
-template <typename T, int NV, int HB, int CTAS>
+template <int NV, int HB, int CTAS>
 __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v) {
   constexpr int LD = 128 * NV + 4, STR = simt_rows(NV > 1), TPL = 32 / STR;   // tiles that a warp looks up at once, a lane per row
   constexpr int NVAL = 4 * HB, HL = 8 / HB;                              // (row, head) pairs of four rows; lanes that hold the same pair
@@ -687,7 +730,7 @@ __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_cons
   __shared__ Held held;
   __shared__ Found found;
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
-  const unsigned krow_b = a.d_qk * sizeof(T), vrow_b = a.d_v * sizeof(T), stage_b = STR * (krow_b + vrow_b);
+  const unsigned krow_b = a.d_qk * sizeof(float), vrow_b = a.d_v * sizeof(float), stage_b = STR * (krow_b + vrow_b);
   const unsigned char* wstages = stages + w * a.stages * stage_b;
   const uint32_t stage0 = smem_u32(wstages), bar0 = smem_u32(bars + w * MAX_STAGES);
   if (lane == 0) {
@@ -742,8 +785,8 @@ __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_cons
       if (lane == 0) mbar_expect_tx(bar, __popc(okay) * (krow_b + vrow_b));
       __syncwarp();
       if (mine && pid >= 0) {
-        bulk_load(dst + r * krow_b, static_cast<const T*>(a.kp) + pid * a.map.kp + kvh_of * a.map.kh + prow * a.map.kr, krow_b, bar);
-        bulk_load(dst + STR * krow_b + r * vrow_b, static_cast<const T*>(a.vp) + pid * a.map.vp + kvh_of * a.map.vh + prow * a.map.vr, vrow_b, bar);
+        bulk_load(dst + r * krow_b, static_cast<const float*>(a.kp) + pid * a.map.kp + kvh_of * a.map.kh + prow * a.map.kr, krow_b, bar);
+        bulk_load(dst + STR * krow_b + r * vrow_b, static_cast<const float*>(a.vp) + pid * a.map.vp + kvh_of * a.map.vh + prow * a.map.vr, vrow_b, bar);
       }
     }
     ++in_flight;
@@ -759,13 +802,13 @@ __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_cons
   F2 q[HB][NV][2];
   const auto load_q = [&]() {
     const int kvh = at.u / a.nhb, hb = at.u - kvh * a.nhb, nh = min(a.gb, a.g - hb * a.gb);
-    const T* qp = static_cast<const T*>(a.q) + ((long long)at.e * a.Hq + kvh * a.g + hb * a.gb) * a.d_qk + 4 * lane;
+    const float* qp = static_cast<const float*>(a.q) + ((long long)at.e * a.Hq + kvh * a.g + hb * a.gb) * a.d_qk + 4 * lane;
 #pragma unroll
     for (int h = 0; h < HB; ++h)
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
         Four f = {0, 0};
-        if (h < nh && 4 * lane + 128 * j < a.d_qk) f = four<T>(qp + h * a.d_qk + 128 * j);
+        if (h < nh && 4 * lane + 128 * j < a.d_qk) f = four(qp + h * a.d_qk + 128 * j);
         q[h][j][0] = f.a; q[h][j][1] = f.b;
       }
   };
@@ -798,8 +841,8 @@ __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_cons
       for (int r0 = 0; r0 < STR; r0 += 4) {
         const unsigned there = (okay >> r0) & 0xfu;
         if (there == 0u && !srow) continue;
-        const T* kx = reinterpret_cast<const T*>(wstages + s_out * stage_b) + r0 * a.d_qk + 4 * lane;
-        const T* vx = reinterpret_cast<const T*>(wstages + s_out * stage_b + STR * krow_b) + r0 * a.d_v + 4 * lane;
+        const float* kx = reinterpret_cast<const float*>(wstages + s_out * stage_b) + r0 * a.d_qk + 4 * lane;
+        const float* vx = reinterpret_cast<const float*>(wstages + s_out * stage_b + STR * krow_b) + r0 * a.d_v + 4 * lane;
         float s[NVAL];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
@@ -807,7 +850,7 @@ __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_cons
 #pragma unroll
           for (int j = 0; j < NV; ++j) {
             f[j] = {0, 0};
-            if (4 * lane + 128 * j < a.d_qk) f[j] = four<T>(kx + r * a.d_qk + 128 * j);
+            if (4 * lane + 128 * j < a.d_qk) f[j] = four(kx + r * a.d_qk + 128 * j);
           }
 #pragma unroll
           for (int h = 0; h < HB; ++h) {
@@ -866,7 +909,7 @@ __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_cons
 #pragma unroll
           for (int j = 0; j < NV; ++j) {
             f[j] = {0, 0};
-            if (4 * lane + 128 * j < a.d_v) f[j] = four<T>(vx + r * a.d_v + 128 * j);
+            if (4 * lane + 128 * j < a.d_v) f[j] = four(vx + r * a.d_v + 128 * j);
           }
 #pragma unroll
           for (int h = 0; h < HB; ++h) {
@@ -928,7 +971,7 @@ __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_cons
       }
       __syncthreads();
     }
-    write_segment<T, SNT, SNW / 2>(a, buf, LD, HB * LD, jm, jl, at.e, at.u, nh, whole, 2 * blockIdx.x + (at.t == 0));
+    write_segment<float, SNT, SNW / 2>(a, buf, LD, HB * LD, jm, jl, at.e, at.u, nh, whole, 2 * blockIdx.x + (at.t == 0));
     if (tb < at.nt) break;
     done += cnt;
     at.t = 0;
@@ -1170,21 +1213,22 @@ __global__ void __launch_bounds__(JNT) paged_join_kernel(const __grid_constant__
 // ---------------------------------------------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------------------------------------------
-template <int D, int NWARP, int NSTAGE, int NG, int CTAS, bool EXACT>
+template <int D, int NWARP, int NSTAGE, int NG, int CTAS, Tiles MODE>
 cudaError_t launch_mma_as(const PagedArgs& a, const CUtensorMap& tk, const CUtensorMap& tv, cudaStream_t st) {
   using S = MmaShape<D, NWARP, NSTAGE, NG>;
   static_assert(CTAS * (S::smem + sizeof(Held) + 1280) <= 228 * 1024, "all CTAs of the grid are resident at once");
   static SmemLimit limit = {};
-  if (cudaError_t e = ensure_dyn_smem(paged_mma_kernel<D, NWARP, NSTAGE, NG, CTAS, EXACT>, S::smem, limit)) return e;
-  const cudaError_t e = launch_pdl(paged_mma_kernel<D, NWARP, NSTAGE, NG, CTAS, EXACT>, dim3(a.ctas), dim3(S::NT), S::smem, st, a, tk, tv);
+  if (cudaError_t e = ensure_dyn_smem(paged_mma_kernel<D, NWARP, NSTAGE, NG, CTAS, MODE>, S::smem, limit)) return e;
+  const cudaError_t e = launch_pdl(paged_mma_kernel<D, NWARP, NSTAGE, NG, CTAS, MODE>, dim3(a.ctas), dim3(S::NT), S::smem, st, a, tk, tv);
   count_launch();
   return e;
 }
 
 template <int D, int NWARP, int NSTAGE, int NG, int CTAS>
 cudaError_t launch_mma(const PagedArgs& a, const CUtensorMap& tk, const CUtensorMap& tv, cudaStream_t st) {
-  return a.d_qk == D && a.d_v == D && a.map.page % TR == 0 ? launch_mma_as<D, NWARP, NSTAGE, NG, CTAS, true>(a, tk, tv, st)
-                                                           : launch_mma_as<D, NWARP, NSTAGE, NG, CTAS, false>(a, tk, tv, st);
+  if (!a.tiled) return launch_mma_as<D, NWARP, NSTAGE, NG, CTAS, Tiles::ROWS>(a, tk, tv, st);
+  return a.d_qk == D && a.d_v == D && a.map.page % TR == 0 ? launch_mma_as<D, NWARP, NSTAGE, NG, CTAS, Tiles::EXACT>(a, tk, tv, st)
+                                                           : launch_mma_as<D, NWARP, NSTAGE, NG, CTAS, Tiles::BOXES>(a, tk, tv, st);
 }
 
 // CTAs per SM that the kernels are built for (launch bounds, and the shared memory of the tensor-core ones)
@@ -1196,32 +1240,28 @@ int simt_stages(const Shape& s, int eb, int ctas, bool wide) {
   return n < 1 ? 1 : n > MAX_STAGES ? MAX_STAGES : n;
 }
 
-template <typename T, int NV, int HB>
+template <int NV, int HB>
 cudaError_t launch_simt_hb(const PagedArgs& a, const CUtensorMap& tk, const CUtensorMap& tv, cudaStream_t st) {
   constexpr int C = simt_ctas(NV > 1, HB);
   static SmemLimit limit = {};
-  const size_t smem = (size_t)SNW * a.stages * a.tr * (a.d_qk + a.d_v) * sizeof(T) + 128;
-  if (cudaError_t e = ensure_dyn_smem(paged_simt_kernel<T, NV, HB, C>, smem, limit)) return e;
-  const cudaError_t e = launch_pdl(paged_simt_kernel<T, NV, HB, C>, dim3(a.ctas), dim3(SNT), smem, st, a, tk, tv);
+  const size_t smem = (size_t)SNW * a.stages * a.tr * (a.d_qk + a.d_v) * sizeof(float) + 128;
+  if (cudaError_t e = ensure_dyn_smem(paged_simt_kernel<NV, HB, C>, smem, limit)) return e;
+  const cudaError_t e = launch_pdl(paged_simt_kernel<NV, HB, C>, dim3(a.ctas), dim3(SNT), smem, st, a, tk, tv);
   count_launch();
   return e;
 }
-template <typename T, int NV>
+template <int NV>
 cudaError_t launch_simt(const PagedArgs& a, const CUtensorMap& tk, const CUtensorMap& tv, cudaStream_t st) {
-  if (a.gb <= 1) return launch_simt_hb<T, NV, 1>(a, tk, tv, st);
-  if (a.gb <= 2) return launch_simt_hb<T, NV, 2>(a, tk, tv, st);
-  if (NV > 1 || a.gb <= 4) return launch_simt_hb<T, NV, 4>(a, tk, tv, st);
-  return launch_simt_hb<T, 1, 8>(a, tk, tv, st);
-}
-
-bool mma_shape(int dtype, const PageMap& m) {
-  return dtype == SNAP_BF16 && m.page % (TR / 2) == 0 && umma::encode_tiled_fn() != nullptr;
+  if (a.gb <= 1) return launch_simt_hb<NV, 1>(a, tk, tv, st);
+  if (a.gb <= 2) return launch_simt_hb<NV, 2>(a, tk, tv, st);
+  if (NV > 1 || a.gb <= 4) return launch_simt_hb<NV, 4>(a, tk, tv, st);
+  return launch_simt_hb<1, 8>(a, tk, tv, st);
 }
 
 }  // namespace
 
 int paged_decode_plan(int dtype, const Shape& s, const PageMap& m, int n_active, bool weights, int sms, PagedDecodePlan* p) {
-  p->mma = mma_shape(dtype, m);
+  p->mma = dtype == SNAP_BF16;
   const bool wide = s.d_qk > 128 || s.d_v > 128;
   const int most = p->mma ? 16 : wide ? 4 : 8;                          // heads of a unit
   p->nhb = (s.g + most - 1) / most;
@@ -1280,16 +1320,13 @@ cudaError_t launch_paged_decode(int dtype, const Shape& s, const PageMap& m, con
   a.tiled = m.page % rows == 0 && enc && encode(&tk, k_pages, s.d_qk, m.kp, m.kh, m.kr) && encode(&tv, v_pages, s.d_v, m.vp, m.vh, m.vr);
   cudaError_t e;
   if (p.mma) {
-    if (!a.tiled) return cudaErrorInvalidValue;
     const bool two = p.gb > 8;
     const int d = s.d_qk > s.d_v ? s.d_qk : s.d_v;
     if (d <= 64) e = two ? launch_mma<64, 4, 4, 2, kMmaCtasWide>(a, tk, tv, st) : launch_mma<64, 4, 4, 1, kMmaCtas>(a, tk, tv, st);
     else if (d <= 128) e = two ? launch_mma<128, 4, 2, 2, kMmaCtasWide>(a, tk, tv, st) : launch_mma<128, 4, 2, 1, kMmaCtas>(a, tk, tv, st);
     else e = two ? launch_mma<256, 2, 2, 2, kMmaCtasWide>(a, tk, tv, st) : launch_mma<256, 2, 2, 1, kMmaCtas>(a, tk, tv, st);
-  } else if (dtype == SNAP_F32) {
-    e = wide ? launch_simt<float, 2>(a, tk, tv, st) : launch_simt<float, 1>(a, tk, tv, st);
   } else {
-    e = wide ? launch_simt<__nv_bfloat16, 2>(a, tk, tv, st) : launch_simt<__nv_bfloat16, 1>(a, tk, tv, st);
+    e = wide ? launch_simt<2>(a, tk, tv, st) : launch_simt<1>(a, tk, tv, st);
   }
   if (e != cudaSuccess) return e;
   const int chunks = (m.cap + JROWS - 1) / JROWS, heads = n_active * s.Hq, by_heads = heads <= 512 || p.ctas < 2;

@@ -263,7 +263,9 @@ def check_decode(c, out, q, slots, dtype, weights=None, weights_before=None, len
 DECODES = [  # hq, hkv, d, dv, page, layout
     (8, 2, 128, 128, 16, "hnd"), (32, 8, 128, 128, 64, "nhd"), (4, 4, 64, 64, 48, "hnd"), (14, 2, 256, 256, 16, "nhd"),
     (12, 1, 128, 128, 32, "hnd"), (32, 1, 64, 64, 16, "nhd"), (40, 2, 256, 256, 32, "hnd"), (9, 3, 80, 80, 16, "hnd"),
-    (6, 1, 128, 64, 8, "nhd"), (2, 1, 48, 96, 5, "hnd"), (16, 2, 64, 64, 1, "nhd"), (11, 1, 192, 256, 24, "hnd"), (5, 5, 16, 16, 7, "hnd")]
+    (6, 1, 128, 64, 8, "nhd"), (2, 1, 48, 96, 5, "hnd"), (16, 2, 64, 64, 1, "nhd"), (11, 1, 192, 256, 24, "hnd"), (5, 5, 16, 16, 7, "hnd"),
+    (8, 2, 128, 128, 1, "hnd"), (20, 1, 128, 112, 3, "hnd"), (40, 2, 256, 256, 1, "nhd"), (6, 2, 64, 64, 9, "nhd"), (7, 1, 256, 256, 13, "hnd"),
+    (12, 1, 64, 48, 2, "hnd")]
 LENGTHS = [0, 1, 15, 16, 17, 31, 333, 0, 2, 1300, 64, 47]
 
 
@@ -292,12 +294,13 @@ def test_paged_decode_matches_its_definition(hq, hkv, d, dv, page, layout, dtype
     assert c.bits() == 0
 
 
-@pytest.mark.parametrize("dtype,hq,hkv,d", [("bf16", 32, 8, 128), ("f32", 8, 2, 128), ("bf16", 8, 8, 64), ("f32", 16, 2, 96)])
-def test_paged_decode_of_long_and_single_sequences(dtype, hq, hkv, d):
+@pytest.mark.parametrize("dtype,hq,hkv,d,page", [("bf16", 32, 8, 128, 32), ("f32", 8, 2, 128, 32), ("bf16", 8, 8, 64, 32), ("f32", 16, 2, 96, 32),
+                                                 ("bf16", 32, 8, 128, 1), ("bf16", 24, 2, 256, 12)])
+def test_paged_decode_of_long_and_single_sequences(dtype, hq, hkv, d, page):
     """One sequence over all CTAs, few tiles per CTA, and many short ones: every way a unit can be cut."""
     for lengths in ([9001], [16 * 37], [5, 20011, 1, 700], [33] * 200):
         cfg = config(hq, hkv, d, dtype=dtype, max_seqs=len(lengths))
-        c = Pages(cfg, dtype, 32, lengths, seed=len(lengths))
+        c = Pages(cfg, dtype, page, lengths, seed=len(lengths))
         slots = list(range(len(lengths)))[::-1]
         q = torch.randn(len(slots), hq, d, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)).to(DT[dtype])
         w = c.weights()
@@ -602,7 +605,7 @@ def test_prompt_steps_eviction_steps(dtype, hq, hkv, d, page):
     assert c.bits() == 0
 
 
-@pytest.mark.parametrize("dtype,page", [("bf16", 16), ("f32", 16), ("bf16", 8)])
+@pytest.mark.parametrize("dtype,page", [("bf16", 16), ("f32", 16), ("bf16", 8), ("bf16", 3)])
 def test_paged_decode_carries_nan_and_leaves_other_heads_alone(dtype, page):
     """A NaN in a row that counts reaches the heads that attend it, over joins too, and no other head."""
     cfg = config(4, 2, 64, dtype=dtype, max_seqs=3)
