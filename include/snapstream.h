@@ -470,8 +470,8 @@ int snap_rope(const snap_config_t* cfg, const snap_rope_config_t* rope, const do
  *   weights         [max_seqs][Hkv][max_pages * page_tokens] float: accumulated attention weight of each row
  * Rows need not be in position order: attention does not depend on it, and snap_paged_append takes
  * positions apart from rows.  Sequences may share pages that are only read.
- * The calls take heads up to 256 wide and no latent layout (SNAP_ERR_UNSUPPORTED otherwise); bf16 layers with
- * pages of a multiple of 8 rows run on tensor cores, fastest with heads of 64, 128 or 256 and pages of a multiple of 16.
+ * The calls take heads up to 256 wide and no latent layout (SNAP_ERR_UNSUPPORTED otherwise).  bf16 layers are attended
+ * fastest with heads of 64, 128 or 256 dims and pages of a multiple of 16 rows, then of 8.
  * All can be captured into CUDA graphs.  Lengths, tables and slots are read on the device when a call runs; nothing may
  * change them while it does.
  */
@@ -523,7 +523,10 @@ int snap_paged_append(const snap_config_t* cfg, const snap_paged_t* paged,
  *                 weights_out[slot][kvh][r] = weights_in[slot][kvh][r] + sum over the group's heads of its softmax weight
  *             (weights_in_dev NULL = 0; it may be weights_out_dev).  Other entries are left alone.  The slots of
  *             one call must then be distinct: of a slot that is listed again only the first entry's weights
- *             count (SNAP_DEV_BAD_SLOT).
+ *             count (SNAP_DEV_BAD_SLOT).  At most 2048 query heads per KV head (SNAP_ERR_UNSUPPORTED).
+ * A NaN or an infinity among the rows a token attends makes the outputs it enters non-finite, which of the two is not
+ * specified; rows that are left out, and what lies behind a sequence's last row, may hold anything.  A token whose every
+ * logit is -infinity gets zeros.
  * The rows of all sequences are split evenly over the GPU whatever their lengths and joined in a fixed order:
  * equal inputs give equal bits.
  * Scratch: snap_paged_decode_workspace_bytes(cfg, paged, n_active, with_weights); calls that can overlap on the

@@ -2,29 +2,38 @@
 //
 //     out[i][h] = sum_r p_r V_r / sum_r p_r,   p_r = exp(scale q.K_r - max),   r over the sequence's rows
 //
-// Every cache row is read once and serves the whole head group, so HBM bounds the call.  (sequence, KV head, head
-// block) is a unit; its rows are cut into tiles.  The units in a row form one line, each as long as its tiles plus a
-// fixed share for what a unit costs however short it is (its queries, its joining), and the line is divided evenly
-// between the CTAs: sequences of any lengths load the GPU evenly and the host need not know the lengths.  A CTA walks over
-// its stretch, which holds whole units and at most one cut one at either end; units of a few tiles are never cut.  A whole
-// unit's output is written at once; a cut one leaves the sum, the maximum and the unnormalised output of its piece,
-// which the second launch joins in a fixed order (no atomics: equal inputs give equal bits).
+// Every cache row is read once and serves the whole head group, so HBM bounds the call: 16 sequences of 8192 to 65536
+// rows (32 heads on 8, 128 dims, 2.2 GB) take 328 us, 6.7 TB/s.  One sequence of 5124 rows takes 11.8 us for 21 MB, and 45
+// of up to 333 rows 14.5: there the chain of slot, length, page, tile, join is what counts.
 //
-// Tensor-core kernel (bf16, pages of a multiple of 8 rows): the group's heads are the N side of mma.sync.m16n8k16,
-// S^T = K tile . Q^T and O^T += V tile^T . P^T, so the cost of a row does not grow with the group.  It is built for
-// heads of up to 64, 128 and 256 dims; what a head lacks is neither read nor multiplied.  Each warp runs a pipeline of its own over tiles fetched by TMA (four-dimensional map: dim, row of a
-// page, KV head, page) with the 128-byte swizzle; the pipeline runs ahead over unit borders, and the page number
-// of the tile after next is fetched while a tile is computed.  The probabilities enter the second product as two bf16
-// numbers (p and what its rounding left), which keeps their rounding out of the result: 2^-17 instead of 2^-9.
+// (sequence, KV head, head block) is a unit; its rows are cut into tiles.  The units in a row form one line, each as
+// long as its tiles plus a fixed share for what a unit costs however short it is (its queries, its joining), and the line
+// is divided evenly between the CTAs: sequences of any lengths load the GPU evenly and the host need not know the
+// lengths.  A CTA walks over its stretch, which holds whole units and at most one cut one at either end; units of a few
+// tiles are never cut.  A whole unit's output is written at once; a cut one leaves the sum, the maximum and the
+// unnormalised output of its piece, which the second launch joins in a fixed order (no atomics: equal inputs give equal
+// bits).
 //
-// Portable kernel (fp32, other heads, pages of any size): the same pipelines per warp over tiles of eight rows, brought in
-// by bulk copies (one per row, or one for all where they lie together); a lane holds four dims of a row.  Four rows at a
-// time, the 4 x heads partial dot products are reduced by halving exchanges, after which a lane owns one (row, head)
-// pair: one shuffle per pair instead of five, one exponential per lane.  (Eight rows at a time need twice the code for
-// the same work; a step of short sequences runs through it once, at the speed at which instructions arrive.)
+// Tensor-core kernel (bf16): the group's heads are the N side of mma.sync.m16n8k16, S^T = K tile . Q^T and
+// O^T += V tile^T . P^T, so the cost of a row does not grow with the group.  It is built for heads of up to 64, 128 and
+// 256 dims; what a head lacks is neither read nor multiplied.  Each warp runs a pipeline of its own over tiles of 16
+// rows that TMA fetches (four-dimensional map: dim, row of a page, KV head, page) with the 128-byte swizzle, or, where a
+// page holds no whole boxes of eight rows, that the lanes copy piece by piece; the pipeline runs ahead over unit borders,
+// and the pages of the tiles after next are looked up while a tile is computed.  The probabilities enter the second
+// product as two bf16 numbers (p and what its rounding left), which keeps their rounding out of the result: 2^-17
+// instead of 2^-9 a row.
+//
+// Portable kernel (single precision): the same pipelines per warp over tiles of 8 KB, brought in through tensor maps or
+// by a bulk copy per row; a lane holds four dims of a row.  Four rows at a time, the 4 x heads partial dot products are
+// reduced by halving exchanges, after which a lane owns one (row, head) pair: one shuffle per pair instead of five, one
+// exponential per lane.  (Eight rows at a time need twice the code for the same work; a step of short sequences runs
+// through it once, at the speed at which instructions arrive.)  Up to four heads per KV head it is bound by latency and
+// HBM; with eight and more by instruction issue (36 sequences of 19000 rows, 16 heads on one of 80 dims: 295 us, 23 % of
+// the HBM rate).
 //
 // With weights, the split kernel also stores the logits, and CTAs of the second launch turn them into the group's
-// attention weight of each row once the unit's maximum and sum are known.
+// attention weight of each row once the unit's maximum and sum are known: 8 sequences of 9000 to 16384 rows take 85 us
+// with weights, 72 without.
 #include <cuda.h>
 
 #include "mma_helpers.cuh"
@@ -54,14 +63,15 @@ struct PagedArgs {
   const void* kp; const void* vp;
   const int* slots; const int* seq_len;
   int n, Hq, Hkv, g, gb, nhb, U, d_qk, d_v, max_seqs;    // U = Hkv * nhb units per sequence, gb heads each (the last block fewer)
+  int gs;                                       // logits of a row: gb, or up to the next multiple of 4
   float scale_log2;
   PageMap map;
   int tr;                                       // rows of a tile
-  int* prefix;                                  // [n + 1]: the line before sequence i, per unit of a sequence
+  int4* entry;                                  // [n + 1]: (the line before sequence i, per unit of a sequence; its slot, rows, tiles)
   float2* ml_unit;                              // [n * U][gb]: (max, sum), log2 domain, of units that one CTA did whole
   float2* ml_part; float* o_part;               // [2 * CTAs][gb], [2 * CTAs][gb][d_v]: pieces of cut units; CTA c's is 2 c, or
                                                 // 2 c + 1 when it holds the unit's first tile (it has one of either at most)
-  float* scores;                                // NULL, or [n * U][cap][gb] logits in the log2 domain
+  float* scores;                                // NULL, or [n * U][cap][gs] logits in the log2 domain
   const float* w_in; float* w_out;
   uint32_t* status;
   int ctas;
@@ -142,8 +152,9 @@ __device__ __forceinline__ int2 read_entry(const PagedArgs& a, int e, unsigned& 
 }
 
 // All threads of the CTA: the place of its first tile and the end of its stretch (both counted from that tile's unit).
-// Returns false (to all) when it has none.  CTA 0 also writes the prefix array and reports bad slots and lengths.
-// Up to MAX_HELD sequences the first warp does it (its result handed over in shared memory: a dozen warps of an SM doing the same would wait for one another), with more the CTA together.
+// Returns false (to all) when it has none.  CTA 0 also writes the entries and reports bad slots and lengths.
+// Up to MAX_HELD sequences the first warp does it (its result handed over in shared memory: a dozen warps of an SM doing
+// the same would wait for one another), with more the CTA together.
 template <int ROWS, int NT, bool SMALL>
 __device__ __forceinline__ bool locate_part(const PagedArgs& a, Place& p, int& end, Held& held, int* scan /* shared, NT / 32 + 2 */) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, c = blockIdx.x;
@@ -174,8 +185,13 @@ __device__ __forceinline__ bool locate_part(const PagedArgs& a, Place& p, int& e
     if (c == 0) {
       int at = before;
 #pragma unroll 1
-      for (int e = e0; e < e1; ++e) { a.prefix[e] = at; at += length_of(tiles_of<ROWS>(held.e[e].y)); }
-      if (lane == 0) a.prefix[a.n] = total;
+      for (int e = e0; e < e1; ++e) {
+        const int2 v = held.e[e];
+        const int nt = tiles_of<ROWS>(v.y);
+        a.entry[e] = make_int4(at, v.x, v.y, nt);
+        at += length_of(nt);
+      }
+      if (lane == 0) a.entry[a.n] = make_int4(total, -1, 0, 0);
       if (bad && a.status) atomicOr(a.status, bad);
     }
     __syncwarp();
@@ -206,8 +222,13 @@ __device__ __forceinline__ bool locate_part(const PagedArgs& a, Place& p, int& e
     for (int w = 0; w < NT / 32; ++w) { const int x = scan[w]; total += x; if (w < warp) before += x; }
     if (c == 0) {
       int at = before;
-      for (int e = e0; e < e1; ++e) { a.prefix[e] = at; at += length_of(tiles_of<ROWS>(read_entry(a, e, bad).y)); }
-      if (tid == 0) a.prefix[a.n] = total;
+      for (int e = e0; e < e1; ++e) {
+        const int2 v = read_entry(a, e, bad);
+        const int nt = tiles_of<ROWS>(v.y);
+        a.entry[e] = make_int4(at, v.x, v.y, nt);
+        at += length_of(nt);
+      }
+      if (tid == 0) a.entry[a.n] = make_int4(total, -1, 0, 0);
       if (bad && a.status) atomicOr(a.status, bad);
     }
     if (!stretch()) return false;
@@ -500,7 +521,7 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
 #pragma unroll
         for (int x = 0; x < 4; ++x) oacc[gi][db][x] = 0.f;
     }
-    float* srow = a.scores ? a.scores + ((long long)at.e * a.U + at.u) * a.map.cap * a.gb : nullptr;
+    float* srow = a.scores ? a.scores + ((long long)at.e * a.U + at.u) * a.map.cap * a.gs : nullptr;
 
     for (; w + n * NWARP < done + cnt && !dead; ++n) {
       const int s = n % NSTAGE;
@@ -560,8 +581,8 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
           for (int r8 = 0; r8 < 2; ++r8) {
             const int row = row0 + gq + 8 * r8;
             if (row >= at.len) continue;                                 // (a bad page's rows are written: as -inf)
-            float* sp = srow + (long long)row * a.gb + col;
-            if (a.gb % 2 == 0 && col < nh) *reinterpret_cast<float2*>(sp) = make_float2(v[gi][2 * r8], v[gi][2 * r8 + 1]);   // (nh may end between them)
+            float* sp = srow + (long long)row * a.gs + col;
+            if (a.gs % 2 == 0 && col < nh) *reinterpret_cast<float2*>(sp) = make_float2(v[gi][2 * r8], v[gi][2 * r8 + 1]);   // (nh may end between them)
             else {
               if (col < nh) sp[0] = v[gi][2 * r8];
               if (col + 1 < nh) sp[1] = v[gi][2 * r8 + 1];
@@ -829,7 +850,7 @@ __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_cons
     for (int h = 0; h < HB; ++h)
 #pragma unroll
       for (int j = 0; j < NV; ++j) o[h][j][0] = o[h][j][1] = 0;
-    float* srow = a.scores ? a.scores + ((long long)at.e * a.U + at.u) * a.map.cap * a.gb : nullptr;
+    float* srow = a.scores ? a.scores + ((long long)at.e * a.U + at.u) * a.map.cap * a.gs : nullptr;
 
     for (; w + n * SNW < done + cnt && !dead; ++n) {
       const bool landed = wait_bounded(bar0 + 8 * s_out, parity);
@@ -885,7 +906,7 @@ __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_cons
         // rows that are not there hold anything
         const float v = (there >> (lane >> 3)) & 1u ? s[0] * a.scale_log2 : -INFINITY;
         const int row = row0 + r0 + (lane >> 3);
-        if (srow && row < at.len && my_head < nh) srow[(long long)row * a.gb + my_head] = v;   // (lanes of one pair write the same)
+        if (srow && row < at.len && my_head < nh) srow[(long long)row * a.gs + my_head] = v;   // (lanes of one pair write the same)
         if (__any_sync(0xffffffffu, v > m_ref + 8.f)) {                    // the reference moves lazily, as in the kernel above
           float mx = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
@@ -991,7 +1012,9 @@ __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_cons
 // ---------------------------------------------------------------------------------------------------------------
 // second launch: joins the pieces of cut units, zeroes the outputs of empty sequences, sums the weights
 // ---------------------------------------------------------------------------------------------------------------
-constexpr int JNT = 256, JROWS = 4 * JNT;         // rows of a weights CTA
+constexpr int JNT = 256;
+__host__ __device__ constexpr int join_rows(int quads) { return quads == 1 ? 2 : 1; }   // of a thread at a time
+constexpr int MAX_MU = 2048;                       // heads of a KV head whose weights are summed (in the shared memory that a join's outputs take)
 
 struct Pieces { int np, c0; };                     // pieces of a unit; np <= 1: done whole
 __device__ __forceinline__ Pieces pieces_of(const PagedArgs& a, int u, int before, int total, int nt) {
@@ -1004,26 +1027,149 @@ __device__ __forceinline__ Pieces pieces_of(const PagedArgs& a, int u, int befor
 }
 __device__ __forceinline__ int piece_at(const Pieces& p, int k) { return 2 * (p.c0 + k) + (k == 0); }
 
-// Grid: `joins` CTAs for the outputs, then the weights'.  The outputs go either by query head (a CTA each: the shorter way
-// to the pieces), or, where there are many heads, by the borders between the stretches of the first launch: the unit that
-// a border cuts is joined by the CTAs of the borders that cut it, which take its heads in turn, so that no more CTAs
-// than borders are started however many units there are.  (By heads against by borders: one sequence of 5124 rows, 32
-// heads 11.4 / 13.1 us a call; 16 sequences, 512 heads 332 / 335; 48 short ones, 1536 heads 25.2 / 22.0.)
+// Weights of (sequence, KV head) id / per: the rows of batches id mod per, + per, ...  line: the line's length; mu_s:
+// shared, [nhb][gb], p = 2^(logit - mu)
+template <int Q>
+__device__ __forceinline__ void join_weights(const PagedArgs& a, int id, int per, int line, float* mu_s) {
+  constexpr int R = join_rows(Q), BATCH = R * JNT;                         // rows of a thread, of the CTA
+  __shared__ float piece_m[JNT], piece_l[JNT];
+  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+  const int part = id % per, kvh = (id / per) % a.Hkv, e = id / per / a.Hkv;
+  const int4 at = a.entry[e];
+  const int before = at.x, slot = at.y, len = at.z, nt = at.w;
+  if ((long long)part * BATCH >= len) return;
+  const long long base = ((long long)slot * a.Hkv + kvh) * a.map.cap;
+  float4 v[R][Q], ahead[R][Q];                                            // logits of this and of the next step
+  float old[R], old_ahead[R];
+  const auto load = [&](int row0, int hb, float4 (&to)[R][Q]) {
+    const float* sc = a.scores + ((long long)e * a.U + kvh * a.nhb + hb) * a.map.cap * a.gs;
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+      const int row = row0 + j * JNT + tid;
+      const float* sr = sc + (long long)row * a.gs;
+#pragma unroll
+      for (int c = 0; c < Q; ++c) {
+        to[j][c] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (row >= len || 4 * c >= a.gs) continue;
+        if (a.gs >= 4) to[j][c] = *reinterpret_cast<const float4*>(sr + 4 * c);
+        else {
+          to[j][c].x = sr[0];
+          if (a.gs == 2) to[j][c].y = sr[1];
+        }
+      }
+    }
+  };
+  const auto load_old = [&](int row0, float (&to)[R]) {
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+      const int row = row0 + j * JNT + tid;
+      to[j] = a.w_in && row < len ? a.w_in[base + row] : 0.f;
+    }
+  };
+  load(part * BATCH, 0, v);                                               // under way while the maxima and sums are put together
+  load_old(part * BATCH, old);
+  int again = 0;                                                         // the slot was listed before: its first entry counts
+  for (int x = tid; x < e; x += JNT) again |= a.slots[x] == slot;
+  if (__syncthreads_or(again)) {
+    if (tid == 0 && a.status) atomicOr(a.status, SNAP_DEV_BAD_SLOT);
+    return;
+  }
+  const int npar = JNT / a.gb, mine = tid % a.gb, k0 = tid / a.gb;         // pieces read at once, this thread's column and first piece
+  for (int hb = 0; hb < a.nhb; ++hb) {
+    const int u = kvh * a.nhb + hb, nh = min(a.gb, a.g - hb * a.gb);
+    const Pieces p = pieces_of(a, u, before, line, nt);
+    float m = -INFINITY, l = 0.f;
+    if (mine < nh && k0 < npar) {
+      if (p.np <= 1) {
+        if (k0 == 0) {
+          const float2 ml = a.ml_unit[((long long)e * a.U + u) * a.gb + mine];
+          m = ml.x; l = ml.y;
+        }
+      } else {
+#pragma unroll 4
+        for (int k = k0; k < p.np; k += npar) {
+          const float2 ml = a.ml_part[(long long)piece_at(p, k) * a.gb + mine];
+          if (ml.y == 0.f) continue;                                       // a piece without rows
+          const float nm = fmaxf(m, ml.x);
+          l = (m == -INFINITY ? 0.f : l * exp2f(m - nm)) + ml.y * exp2f(ml.x - nm);
+          m = nm;
+        }
+      }
+    }
+    __syncthreads();                                                       // the block before has been read
+    piece_m[tid] = m;
+    piece_l[tid] = l;
+    __syncthreads();
+    for (int col = w; col < nh; col += JNT / 32) {
+      float M = -INFINITY, L = 0.f;
+      for (int k = lane; k < npar; k += 32) M = fmaxf(M, piece_m[k * a.gb + col]);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+      for (int k = lane; k < npar; k += 32) {
+        const float pl = piece_l[k * a.gb + col];
+        L += pl == 0.f ? 0.f : pl * exp2f(piece_m[k * a.gb + col] - M);
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
+      if (lane == 0) mu_s[hb * a.gb + col] = L == 0.f ? INFINITY : M + log2f(L);   // no valid row: all weights 0
+    }
+  }
+  __syncthreads();
+  for (int row0 = part * BATCH; row0 < len;) {
+    const int next = (int)min((long long)row0 + (long long)per * BATCH, (long long)len);
+    float sum[R];                                                          // (the old weight is added last: one rounding at the size of the total)
+#pragma unroll
+    for (int j = 0; j < R; ++j) sum[j] = 0.f;
+    for (int hb = 0; hb < a.nhb; ++hb) {
+      const int nh = min(a.gb, a.g - hb * a.gb);
+      const float* mu = mu_s + hb * a.gb;
+      if (hb + 1 < a.nhb) load(row0, hb + 1, ahead);
+      else { load(next, 0, ahead); load_old(next, old_ahead); }
+#pragma unroll
+      for (int c = 0; c < Q; ++c)
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+          if (4 * c < nh) sum[j] += fast_exp2(v[j][c].x - mu[4 * c]);
+          if (4 * c + 1 < nh) sum[j] += fast_exp2(v[j][c].y - mu[4 * c + 1]);
+          if (4 * c + 2 < nh) sum[j] += fast_exp2(v[j][c].z - mu[4 * c + 2]);
+          if (4 * c + 3 < nh) sum[j] += fast_exp2(v[j][c].w - mu[4 * c + 3]);
+          v[j][c] = ahead[j][c];
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+      const int row = row0 + j * JNT + tid;
+      if (row < len) a.w_out[base + row] = old[j] + sum[j];
+      old[j] = old_ahead[j];
+    }
+    row0 = next;
+  }
+}
+
+// Grid: `first` CTAs for the weights, which take longer, then the outputs'.  The outputs go either by query head (a CTA
+// each: the shorter way to the pieces), or, where there are many heads, by the borders between the stretches of the first
+// launch: the unit that a border cuts is joined by the CTAs of the borders that cut it, which take its heads in turn, so
+// that no more CTAs than borders are started however many units there are.  (By heads against by borders: one sequence
+// of 5124 rows, 32 heads 11.4 / 13.1 us a call; 16 sequences, 512 heads 332 / 335; 48 short ones, 1536 heads 25.2 / 22.0.)
 //
 // This kernel lets the next one start only when it ends: blocks of the split kernel that start beside blocks of this
 // one get the registers in between them, and once these end the rest of an SM's registers is in pieces too small for
 // the third block, which then waits for a whole stretch to end (16 long sequences: 366 instead of 332 us a call).
-template <typename T>
-__global__ void __launch_bounds__(JNT) paged_join_kernel(const __grid_constant__ PagedArgs a, int joins, int by_heads) {
+//
+// Weights: `per` CTAs for each (sequence, KV head) put together the maximum and sum of every head of the group (thread t
+// reads the pieces of column t mod gb: all of them in one latency), then walk over the rows, a thread to a row and all of
+// a row's logits at once, the next rows' on their way meanwhile.  Q: 16-byte pieces of a row's logits (0: no weights).
+template <typename T, int Q>
+__global__ void __launch_bounds__(JNT, 3) paged_join_kernel(const __grid_constant__ PagedArgs a, int first, int by_heads, int per) {
   __shared__ __align__(16) float acc_s[JNT / 32][256];
   __shared__ float red_m[JNT / 32], red_l[JNT / 32];
-  __shared__ float mu_s[16];
   __shared__ int s_e;
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
   if (tid == 0) s_e = -1;
   pdl_wait();
-  const int line = a.prefix[a.n];
-  if ((int)blockIdx.x < joins) {
+  const int line = a.entry[a.n].x;
+  const int joins = gridDim.x - first, id = (int)blockIdx.x - first;       // of the outputs
+  if (Q == 0 || id >= 0) {
     int e, u, nt, col0, step;
     Pieces p;
     const auto zero = [&](int row, int rows) {                             // outputs of a sequence without rows
@@ -1031,32 +1177,36 @@ __global__ void __launch_bounds__(JNT) paged_join_kernel(const __grid_constant__
       for (int x = tid; x < rows * a.d_v; x += JNT) out[x] = from_f32<T>(0.f);
     };
     if (by_heads) {
-      e = blockIdx.x / a.Hq;
-      const int head = blockIdx.x - e * a.Hq, kvh = head / a.g, x = head - kvh * a.g, hb = x / a.gb;
+      e = id / a.Hq;
+      const int head = id - e * a.Hq, kvh = head / a.g, x = head - kvh * a.g, hb = x / a.gb;
       u = kvh * a.nhb + hb;
       col0 = x - hb * a.gb;
       step = a.gb;
-      const int before = a.prefix[e];
-      nt = a.prefix[e + 1] - before - UNIT_TILES;
-      if (nt <= 0) { zero(blockIdx.x, 1); return; }
+      const int4 at = a.entry[e];
+      const int before = at.x;
+      nt = at.w;
+      if (nt == 0) { zero(id, 1); return; }
       p = pieces_of(a, u, before, line, nt);
       if (p.np <= 1) return;                                               // written by the split kernel
     } else {
-      for (int i = blockIdx.x; i < a.n; i += joins)
-        if (a.prefix[i + 1] == a.prefix[i]) zero(i * a.Hq, a.Hq);
+      for (int i = id; i < a.n; i += joins)
+        if (a.entry[i].w == 0) zero(i * a.Hq, a.Hq);
       const long long W = (long long)line * a.U;
-      const int active = active_ctas(W, a.ctas), c = blockIdx.x + 1;
+      const int active = active_ctas(W, a.ctas), c = id + 1;
       if (c >= active) return;
       const long long x = stretch_begin(W, active, c);
       __syncthreads();
-      for (int i = tid; i < a.n; i += JNT)                                 // one thread has it
-        if ((long long)a.prefix[i] * a.U <= x && x < (long long)a.prefix[i + 1] * a.U) s_e = i;
+      for (int i = tid; i < a.n; i += JNT) {                               // one thread has it
+        const int4 at = a.entry[i];
+        if ((long long)at.x * a.U <= x && x < (long long)(at.x + length_of(at.w)) * a.U) s_e = i;
+      }
       __syncthreads();
       e = s_e;
       if (e < 0) return;                                                   // (only if the lengths change during the call)
-      const int before = a.prefix[e], unit = a.prefix[e + 1] - before;
+      const int4 at = a.entry[e];
+      const int before = at.x, unit = length_of(at.w);
       const long long rel = x - (long long)before * a.U;
-      nt = unit - UNIT_TILES;
+      nt = at.w;
       u = rel < (1LL << 31) ? (int)((unsigned)rel / (unsigned)unit) : (int)(rel / unit);
       p = pieces_of(a, u, before, line, nt);
       // the unit's pieces are those of the CTAs c0 .. c0 + np - 1: the border before CTA c0 + k is its k-th
@@ -1128,86 +1278,7 @@ __global__ void __launch_bounds__(JNT) paged_join_kernel(const __grid_constant__
     }
     return;
   }
-  // ---- JROWS rows' weights of one (sequence, KV head) ----
-  const int chunks = (a.map.cap + JROWS - 1) / JROWS;
-  const int id = blockIdx.x - joins, chunk = id % chunks, kvh = (id / chunks) % a.Hkv, e = id / chunks / a.Hkv;
-  const int before = a.prefix[e], nt = max(a.prefix[e + 1] - before - UNIT_TILES, 0);
-  if (chunk * JROWS >= nt * a.tr) return;
-  const int slot = a.slots[e];
-  int again = 0;                                                         // the slot was listed before: its first entry counts
-  for (int x = tid; x < e; x += JNT) again |= a.slots[x] == slot;
-  if (__syncthreads_or(again)) {
-    if (tid == 0 && a.status) atomicOr(a.status, SNAP_DEV_BAD_SLOT);
-    return;
-  }
-  const int len = rows_of(a, slot);
-  const long long base = ((long long)slot * a.Hkv + kvh) * a.map.cap;
-  float old[4], sum[4] = {0.f, 0.f, 0.f, 0.f};                            // (added last: one rounding at the size of the total)
-  float4 v[4];
-  // four logits of each of the thread's rows, columns c .. c + 3 of head block hb
-  const auto load = [&](int hb, int c, int nh) {
-    const float* sc = a.scores + ((long long)e * a.U + kvh * a.nhb + hb) * a.map.cap * a.gb + c;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int row = chunk * JROWS + j * JNT + tid;
-      v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (row < len) {
-        const float* sr = sc + (long long)row * a.gb;
-        if (a.gb % 4 == 0) v[j] = *reinterpret_cast<const float4*>(sr);
-        else {
-          v[j].x = sr[0];
-          if (c + 1 < nh) v[j].y = sr[1];
-          if (c + 2 < nh) v[j].z = sr[2];
-          if (c + 3 < nh) v[j].w = sr[3];
-        }
-      }
-    }
-  };
-  load(0, 0, min(a.gb, a.g));                                            // under way while the maxima and sums are put together
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int row = chunk * JROWS + j * JNT + tid;
-    old[j] = a.w_in && row < len ? a.w_in[base + row] : 0.f;
-  }
-  for (int hb = 0; hb < a.nhb; ++hb) {
-    const int u = kvh * a.nhb + hb, nh = min(a.gb, a.g - hb * a.gb);
-    const Pieces p = pieces_of(a, u, before, line, nt);
-    __syncthreads();                                                     // mu_s of the block before has been read
-    for (int col = w; col < nh; col += JNT / 32) {
-      float m = -INFINITY, l = 0.f;
-      if (p.np <= 1) {
-        const float2 ml = a.ml_unit[((long long)e * a.U + u) * a.gb + col];
-        m = ml.x; l = ml.y;
-      } else {
-        for (int k = lane; k < p.np; k += 32) m = fmaxf(m, a.ml_part[(long long)piece_at(p, k) * a.gb + col].x);
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-        for (int k = lane; k < p.np; k += 32) {
-          const float2 ml = a.ml_part[(long long)piece_at(p, k) * a.gb + col];
-          l += ml.y == 0.f ? 0.f : ml.y * exp2f(ml.x - m);
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-      }
-      if (lane == 0) mu_s[col] = l == 0.f ? INFINITY : m + log2f(l);     // p = 2^(score - mu); no valid row: 0
-    }
-    __syncthreads();
-    for (int c = 0; c < nh; c += 4) {
-      if (hb > 0 || c > 0) load(hb, c, nh);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        sum[j] += exp2f(v[j].x - mu_s[c]);
-        if (c + 1 < nh) sum[j] += exp2f(v[j].y - mu_s[c + 1]);
-        if (c + 2 < nh) sum[j] += exp2f(v[j].z - mu_s[c + 2]);
-        if (c + 3 < nh) sum[j] += exp2f(v[j].w - mu_s[c + 3]);
-      }
-    }
-  }
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int row = chunk * JROWS + j * JNT + tid;
-    if (row < len) a.w_out[base + row] = old[j] + sum[j];
-  }
+  if constexpr (Q > 0) join_weights<Q>(a, blockIdx.x, per, line, &acc_s[0][0]);
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -1258,6 +1329,9 @@ cudaError_t launch_simt(const PagedArgs& a, const CUtensorMap& tk, const CUtenso
   return launch_simt_hb<1, 8>(a, tk, tv, st);
 }
 
+// Logits stored of a row: vectors of four, when there are more than two.
+int logits_of(int gb) { return gb <= 2 ? gb : (gb + 3) / 4 * 4; }
+
 }  // namespace
 
 int paged_decode_plan(int dtype, const Shape& s, const PageMap& m, int n_active, bool weights, int sms, PagedDecodePlan* p) {
@@ -1269,17 +1343,16 @@ int paged_decode_plan(int dtype, const Shape& s, const PageMap& m, int n_active,
   const int per_sm = p->mma ? (p->gb > 8 ? kMmaCtasWide : kMmaCtas) : simt_ctas(wide, p->gb);
   p->ctas = sms * per_sm < MAX_CTAS ? sms * per_sm : MAX_CTAS;
   const long long units = (long long)n_active * s.Hkv * p->nhb;
-  const long long chunks = (m.cap + JROWS - 1) / JROWS;
   // grid and index limits; a line of tiles and the scratch have to be countable
-  if (units > (1LL << 30) || (long long)n_active * s.Hq > 0x7fffffffLL || (weights && (long long)n_active * s.Hkv * chunks > 0x7fff0000LL) ||
+  if (units > (1LL << 30) || (long long)n_active * s.Hq > 0x7fffffffLL || (weights && p->nhb * p->gb > MAX_MU) ||
       units * (m.cap / 4LL + 1 + UNIT_TILES) > (1LL << 37) || n_active * (m.cap / 4LL + 1 + UNIT_TILES) > 0x7fffffffLL)
     return SNAP_ERR_UNSUPPORTED;
   size_t off = 0;
-  p->prefix_off = off; off += align_up((size_t)(n_active + 1) * sizeof(int));
+  p->entry_off = off; off += align_up((size_t)(n_active + 1) * sizeof(int4));
   p->ml_off = off;     off += align_up(((size_t)units + 2 * (size_t)p->ctas) * p->gb * sizeof(float2));
   p->o_off = off;      off += align_up(2 * (size_t)p->ctas * p->gb * s.d_v * sizeof(float));
   p->score_off = off;
-  if (weights) off += align_up((size_t)units * m.cap * p->gb * sizeof(float));
+  if (weights) off += align_up((size_t)units * m.cap * logits_of(p->gb) * sizeof(float));
   p->bytes = off;
   return SNAP_OK;
 }
@@ -1293,11 +1366,12 @@ cudaError_t launch_paged_decode(int dtype, const Shape& s, const PageMap& m, con
   a.d_qk = s.d_qk; a.d_v = s.d_v; a.max_seqs = s.max_seqs;
   a.scale_log2 = s.scale * 1.4426950408889634f;
   a.map = m;
-  a.prefix = reinterpret_cast<int*>(scratch + p.prefix_off);
+  a.entry = reinterpret_cast<int4*>(scratch + p.entry_off);
   a.ml_unit = reinterpret_cast<float2*>(scratch + p.ml_off);
   a.ml_part = a.ml_unit + (size_t)n_active * a.U * p.gb;
   a.o_part = reinterpret_cast<float*>(scratch + p.o_off);
   a.scores = w_out ? reinterpret_cast<float*>(scratch + p.score_off) : nullptr;
+  a.gs = logits_of(p.gb);
   a.w_in = w_in; a.w_out = w_out; a.status = status; a.ctas = p.ctas;
   const bool wide = s.d_qk > 128 || s.d_v > 128;
   a.tr = p.mma ? TR : simt_rows(wide);
@@ -1329,11 +1403,23 @@ cudaError_t launch_paged_decode(int dtype, const Shape& s, const PageMap& m, con
     e = wide ? launch_simt<2>(a, tk, tv, st) : launch_simt<1>(a, tk, tv, st);
   }
   if (e != cudaSuccess) return e;
-  const int chunks = (m.cap + JROWS - 1) / JROWS, heads = n_active * s.Hq, by_heads = heads <= 512 || p.ctas < 2;
-  const int joins = by_heads ? heads : p.ctas - 1;
-  const dim3 grid((unsigned)(joins + (w_out ? n_active * s.Hkv * chunks : 0)));
-  e = dtype == SNAP_F32 ? launch_pdl(paged_join_kernel<float>, grid, dim3(JNT), 0, st, a, joins, by_heads)
-                        : launch_pdl(paged_join_kernel<__nv_bfloat16>, grid, dim3(JNT), 0, st, a, joins, by_heads);
+  const int sms = sm_count(), heads = n_active * s.Hq, by_heads = heads <= 512 || p.ctas < 2;
+  const int joins = by_heads ? heads : p.ctas - 1, pairs = n_active * s.Hkv;
+  // CTAs of a (sequence, KV head)'s weights: as many as run at once beside half of the outputs' (which end sooner), and no
+  // more than it can have batches of rows.  (A CTA per 1024 rows instead, each with the maxima and sums to put together:
+  // 3 sequences of 22670 to 49189 rows, 16 heads on one, 35.7 us a call against 27.9; 8 heads 28.0 / 24.2; 8 sequences,
+  // 4 heads on each of 8 the same.)
+  const int quads = (p.gb + 3) / 4, batch = join_rows(quads) * JNT, most = (m.cap + batch - 1) / batch;
+  const int room = 3 * sms, want = (joins < room ? room - joins / 2 : room / 2) / pairs, per = want < 1 ? 1 : want < most ? want : most;
+  const int first = w_out ? pairs * per : 0;
+  const dim3 grid((unsigned)(first + joins));
+  const auto join = [&](auto kernel) { return launch_pdl(kernel, grid, dim3(JNT), 0, st, a, first, by_heads, per); };
+  if (dtype == SNAP_F32) {
+    e = !w_out ? join(paged_join_kernel<float, 0>) : quads == 1 ? join(paged_join_kernel<float, 1>) : join(paged_join_kernel<float, 2>);
+  } else {
+    e = !w_out ? join(paged_join_kernel<__nv_bfloat16, 0>) : quads == 1 ? join(paged_join_kernel<__nv_bfloat16, 1>)
+        : quads == 2 ? join(paged_join_kernel<__nv_bfloat16, 2>) : join(paged_join_kernel<__nv_bfloat16, 4>);
+  }
   count_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
 }

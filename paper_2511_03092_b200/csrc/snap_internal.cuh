@@ -266,7 +266,7 @@ cudaError_t launch_rope(int dtype, const RopeArgs& a, cudaStream_t st);
 struct PagedDecodePlan {
   bool mma;
   int ctas, gb, nhb;                // CTAs of the split kernel; heads of a unit, units per KV head
-  size_t prefix_off, ml_off, o_off, score_off, bytes;
+  size_t entry_off, ml_off, o_off, score_off, bytes;
 };
 int paged_decode_plan(int dtype, const Shape& s, const PageMap& m, int n_active, bool weights, int sms, PagedDecodePlan* p);
 cudaError_t launch_paged_decode(int dtype, const Shape& s, const PageMap& m, const PagedDecodePlan& p, const void* q,

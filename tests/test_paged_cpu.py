@@ -144,6 +144,17 @@ def test_paged_calls_refuse_bad_arguments():
     assert ap(cfg=_cfg(n_q_heads=4, n_kv_heads=1), paged=_paged(k_head_stride=0, v_head_stride=0), n=0) == 0
 
 
+def test_paged_weights_of_very_large_groups_are_refused():
+    for dtype, d in ((B.SNAP_BF16, 128), (B.SNAP_F32, 128), (B.SNAP_F32, 256)):
+        cfg = _cfg(n_q_heads=2048, n_kv_heads=1, d_qk=d, d_v=d, dtype=dtype)
+        paged = _paged(k_row_stride=1024, v_row_stride=1024)
+        assert B.snap_paged_decode_workspace_bytes(cfg, paged, 1, True) > 800 * 2048 * 4
+        cfg.n_q_heads = 2049
+        assert B.snap_paged_decode_workspace_bytes(cfg, paged, 1) > 0
+        with pytest.raises(B.SnapError):
+            B.snap_paged_decode_workspace_bytes(cfg, paged, 1, True)
+
+
 def test_binding_checks_what_tensors_are():
     """The Python calls refuse tensors of another type, shape or place before the library sees their addresses."""
     cfg = _cfg()
