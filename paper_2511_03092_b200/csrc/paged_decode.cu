@@ -14,7 +14,7 @@
 // unnormalised output of its piece, which the second launch joins in a fixed order (no atomics: equal inputs give equal
 // bits).
 //
-// Tensor-core kernel (bf16): the group's heads are the N side of mma.sync.m16n8k16, S^T = K tile . Q^T and
+// Tensor-core kernel: the group's heads are the N side of mma.sync.m16n8k16, S^T = K tile . Q^T and
 // O^T += V tile^T . P^T, so the cost of a row does not grow with the group.  It is built for heads of up to 64, 128 and
 // 256 dims; what a head lacks is neither read nor multiplied.  Each warp runs a pipeline of its own over tiles of 16
 // rows that TMA fetches (four-dimensional map: dim, row of a page, KV head, page) with the 128-byte swizzle, or, where a
@@ -23,13 +23,16 @@
 // product as two bf16 numbers (p and what its rounding left), which keeps their rounding out of the result: 2^-17
 // instead of 2^-9 a row.
 //
-// Portable kernel (single precision): the same pipelines per warp over tiles of 8 KB, brought in through tensor maps or
-// by a bulk copy per row; a lane holds four dims of a row.  Four rows at a time, the 4 x heads partial dot products are
-// reduced by halving exchanges, after which a lane owns one (row, head) pair: one shuffle per pair instead of five, one
-// exponential per lane.  (Eight rows at a time need twice the code for the same work; a step of short sequences runs
-// through it once, at the speed at which instructions arrive.)  Up to four heads per KV head it is bound by latency and
-// HBM; with eight and more by instruction issue (36 sequences of 19000 rows, 16 heads on one of 80 dims: 295 us, 23 % of
-// the HBM rate).
+// In single precision it multiplies with m16n8k8 on numbers split in two: three products, together within 2^-20 of the
+// exact one, less than summing a few dozen of them in single precision may lose.  Groups of up to four wide heads are
+// faster on the portable kernel.
+//
+// Portable kernel: the same pipelines per warp over tiles of 8 KB, brought in through tensor maps or by a bulk copy per
+// row; a lane holds four dims of a row.  Four rows at a time, the 4 x heads partial dot products are reduced by halving
+// exchanges, after which a lane owns one (row, head) pair: one shuffle per pair instead of five, one exponential per lane.
+// (Eight rows at a time need twice the code for the same work; a step of short sequences runs through it once, at the speed
+// at which instructions arrive.)  4 sequences of 2001 to 4100 rows, 8 heads on 2, take 15 us (latency); 28 of 1324 to 2196, 8
+// on 4, 41.6 us, 74 % of the HBM rate.
 //
 // With weights, the split kernel also stores the logits, and CTAs of the second launch turn them into the group's
 // attention weight of each row once the unit's maximum and sum are known: 8 sequences of 9000 to 16384 rows take 85 us
@@ -328,10 +331,11 @@ __device__ __forceinline__ uint32_t swz(int r, int c) { return (uint32_t)(r * 12
 // ---------------------------------------------------------------------------------------------------------------
 // tensor-core kernel
 // ---------------------------------------------------------------------------------------------------------------
-constexpr int SLAB_B = TR * 128;                 // one 64-dim slab of a tile
+constexpr int SLAB_B = TR * 128;                 // one 128-byte-wide slab of a tile
+template <typename T> __host__ __device__ constexpr int slab_dims() { return 128 / (int)sizeof(T); }
 
-template <int D, int NWARP, int NSTAGE, int NG> struct MmaShape {
-  static constexpr int NT = NWARP * 32, NSL = D / 64, KS = D / 16, NCOL = 8 * NG;
+template <typename T, int D, int NWARP, int NSTAGE, int NG> struct MmaShape {
+  static constexpr int NT = NWARP * 32, NSL = D / slab_dims<T>(), KS = D / 16, NCOL = 8 * NG;
   static constexpr int TENS_B = NSL * SLAB_B, STAGE_B = 2 * TENS_B;
   static constexpr int LD = D + 4;               // column stride of the exchange buffers: fragments store without bank conflicts
   static constexpr size_t stages_b = (size_t)NWARP * NSTAGE * STAGE_B;
@@ -339,15 +343,39 @@ template <int D, int NWARP, int NSTAGE, int NG> struct MmaShape {
   static constexpr size_t smem = 1024 + stages_b + bars_b + (size_t)(NWARP / 2 * NCOL * LD + 2 * NWARP * NCOL + 2 * NCOL) * sizeof(float);
 };
 
+// A single-precision number as two of the tensor cores' 11 bits: x = hi + lo within 2^-21 of x, hi rounded and lo cut off.
+// (In integer arithmetic: with the conversion instruction, which has a fraction of its rate, 8 sequences of 2000 to 6000
+// rows and 8 heads on each of 4 took 40.6 us instead of 35.3.)  A NaN leaves one part NaN at least; above 2^128 (1 - 2^-12) x counts as infinite.
+struct Tf32 { uint32_t hi, lo; };
+__device__ __forceinline__ Tf32 tf32_of(float x) {
+  Tf32 t;
+  t.hi = (__float_as_uint(x) + 0x1000u) & 0xffffe000u;
+  t.lo = __float_as_uint(x - __uint_as_float(t.hi)) & 0xffffe000u;
+  return t;
+}
+__device__ __forceinline__ void mma1688(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// c += a . b in single precision: hi hi + hi lo + lo hi; what is left out is 2^-22 of a product
+__device__ __forceinline__ void mma_3tf32(float (&c)[4], const Tf32* a, const Tf32& b0, const Tf32& b1) {
+  mma1688(c, a[0].lo, a[1].lo, a[2].lo, a[3].lo, b0.hi, b1.hi);
+  mma1688(c, a[0].hi, a[1].hi, a[2].hi, a[3].hi, b0.lo, b1.lo);
+  mma1688(c, a[0].hi, a[1].hi, a[2].hi, a[3].hi, b0.hi, b1.hi);
+}
+
 // How a tile comes in.  EXACT: through the tensor maps, heads of D dims and pages of a multiple of 16 rows, without the
 // tests that other shapes need in the inner loops (with them a 128-wide call takes 4 to 15 % longer, a 256-wide one half
 // as long again).  BOXES: through the tensor maps, pages of a multiple of 8 rows.  ROWS: any pages; the lanes copy a
 // row's 16-byte pieces themselves (cp.async), each from the page of its row.
 enum class Tiles { EXACT, BOXES, ROWS };
-template <int D, int NWARP, int NSTAGE, int NG, int CTAS, Tiles MODE>
+template <typename T, int D, int NWARP, int NSTAGE, int NG, int CTAS, Tiles MODE>
 __global__ void __launch_bounds__(NWARP * 32, CTAS)
 paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v) {
-  using S = MmaShape<D, NWARP, NSTAGE, NG>;
+  using S = MmaShape<T, D, NWARP, NSTAGE, NG>;
+  constexpr bool F32 = sizeof(T) == 4;
+  constexpr int SD = slab_dims<T>();
   constexpr int KS = S::KS, NCOL = S::NCOL, LD = S::LD;
   constexpr bool EXACT = MODE == Tiles::EXACT, BY_ROWS = MODE == Tiles::ROWS;
   constexpr int LOOK = BY_ROWS ? 32 / TR : 32;                           // tiles that a warp looks up at once
@@ -422,44 +450,49 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
     }
   };
   fetch();
-  const __nv_bfloat16* q_all = static_cast<const __nv_bfloat16*>(a.q);
-  uint32_t qb[NG][KS][2];                                                // B fragments of Q^T: column 8 gi + gq, dims 16 ks + 2 tq (+8)
+  const T* q_all = static_cast<const T*>(a.q);
+  // B fragments of Q^T.  bf16: column 8 gi + gq, dims 16 ks + 2 tq (+1), + 8 (+9).  Single precision: dims 16 ks + 4 tq .. + 3
+  uint32_t qb[NG][KS][F32 ? 4 : 2];
   const auto load_q = [&]() {
     const int kvh = at.u / a.nhb, hb = at.u - kvh * a.nhb, nh = min(a.gb, a.g - hb * a.gb);
 #pragma unroll
     for (int gi = 0; gi < NG; ++gi) {
       const int col = 8 * gi + gq;
-      const __nv_bfloat16* qp = q_all + ((long long)at.e * a.Hq + kvh * a.g + hb * a.gb + (col < nh ? col : 0)) * (EXACT ? D : a.d_qk) + 2 * tq;
+      const T* qp = q_all + ((long long)at.e * a.Hq + kvh * a.g + hb * a.gb + (col < nh ? col : 0)) * (EXACT ? D : a.d_qk) + (F32 ? 4 : 2) * tq;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         const bool there = col < nh && (EXACT || 16 * ks < a.d_qk);
-        qb[gi][ks][0] = there ? *reinterpret_cast<const uint32_t*>(qp + 16 * ks) : 0u;
-        qb[gi][ks][1] = there ? *reinterpret_cast<const uint32_t*>(qp + 16 * ks + 8) : 0u;
+        if constexpr (F32) {
+          const uint4 x = there ? *reinterpret_cast<const uint4*>(qp + 16 * ks) : make_uint4(0, 0, 0, 0);
+          qb[gi][ks][0] = x.x; qb[gi][ks][1] = x.y; qb[gi][ks][2] = x.z; qb[gi][ks][3] = x.w;
+        } else {
+          qb[gi][ks][0] = there ? *reinterpret_cast<const uint32_t*>(qp + 16 * ks) : 0u;
+          qb[gi][ks][1] = there ? *reinterpret_cast<const uint32_t*>(qp + 16 * ks + 8) : 0u;
+        }
       }
     }
   };
   load_q();                                                              // (the first tiles' look-ups wait alongside)
   const int d_qk = EXACT ? D : a.d_qk, d_v = EXACT ? D : a.d_v;
-  const unsigned tile_b = (unsigned)((d_qk + 63) / 64 + (d_v + 63) / 64) * SLAB_B;   // the slabs that hold anything
+  const unsigned tile_b = (unsigned)((d_qk + SD - 1) / SD + (d_v + SD - 1) / SD) * SLAB_B;   // the slabs that hold anything
   const auto issue_rows = [&]() {                                        // the tile of the lower or upper half of the lanes
     const int s = n_issued % NSTAGE, l = (n_issued % LOOK) * TR;
     const unsigned okay = (__ballot_sync(0xffffffffu, pid >= 0 && pid < a.map.n_pages) >> l) & 0xffffu;
     rows_stage = (rows_stage & ~(0xffffull << (16 * s))) | (unsigned long long)okay << (16 * s);
     if (lane / TR == l / TR && pid >= a.map.n_pages && a.status) atomicOr(a.status, SNAP_DEV_BAD_PAGE);
     const long long k_off = pid * a.map.kp + kvh_of * a.map.kh + row_of * a.map.kr, v_off = pid * a.map.vp + kvh_of * a.map.vh + row_of * a.map.vr;
-    // D / 8 lanes to a row (of a narrower head some have nothing to copy), RPI rows at a time
-    constexpr int CPR = D / 8, RPI = 32 / CPR;
-    const int c = lane % CPR;
-    const uint32_t dst = stage0 + s * S::STAGE_B + (c >> 3) * SLAB_B;
-    const __nv_bfloat16* kp = static_cast<const __nv_bfloat16*>(a.kp) + 8 * c;
-    const __nv_bfloat16* vp = static_cast<const __nv_bfloat16*>(a.vp) + 8 * c;
+    // CPR lanes to a row (of a narrower head some have nothing to copy)
+    constexpr int EPC = 16 / (int)sizeof(T), CPR = D / EPC;
+    const T* kp = static_cast<const T*>(a.kp);
+    const T* vp = static_cast<const T*>(a.vp);
 #pragma unroll
-    for (int r0 = 0; r0 < TR; r0 += RPI) {
-      const int r = r0 + lane / CPR;
+    for (int x0 = 0; x0 < TR * CPR; x0 += 32) {
+      const int r = (x0 + lane) / CPR, c = (x0 + lane) % CPR;
       const long long ko = __shfl_sync(0xffffffffu, k_off, l + r), vo = __shfl_sync(0xffffffffu, v_off, l + r);
+      const uint32_t dst = stage0 + s * S::STAGE_B + (c >> 3) * SLAB_B + swz(r, c & 7);
       if ((okay >> r) & 1u) {
-        if (8 * c < d_qk) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + swz(r, c & 7)), "l"(kp + ko) : "memory");
-        if (8 * c < d_v) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + S::TENS_B + swz(r, c & 7)), "l"(vp + vo) : "memory");
+        if (EPC * c < d_qk) cp_async16(dst, kp + ko + EPC * c, 16);
+        if (EPC * c < d_v) cp_async16(dst + S::TENS_B, vp + vo + EPC * c, 16);
       }
     }
     asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar0 + 8 * s) : "memory");
@@ -485,8 +518,8 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
         const uint32_t at = dst + half * (SLAB_B / 2);
 #pragma unroll
         for (int h = 0; h < S::NSL; ++h) {
-          if (64 * h < d_qk) tma_load_4d(at + h * SLAB_B, &tmap_k, 64 * h, row, kvh_of, page, bar);
-          if (64 * h < d_v) tma_load_4d(at + S::TENS_B + h * SLAB_B, &tmap_v, 64 * h, row, kvh_of, page, bar);
+          if (SD * h < d_qk) tma_load_4d(at + h * SLAB_B, &tmap_k, SD * h, row, kvh_of, page, bar);
+          if (SD * h < d_v) tma_load_4d(at + S::TENS_B + h * SLAB_B, &tmap_v, SD * h, row, kvh_of, page, bar);
         }
       }
       if (bad && a.status) atomicOr(a.status, SNAP_DEV_BAD_PAGE);
@@ -534,7 +567,7 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
       const uint32_t sK = stage0 + s * S::STAGE_B, sV = sK + S::TENS_B;
       if (nrows < TR || bad) {
         // rows past the end, or on a bad page, may hold anything, and a zero probability does not silence a NaN in V: clear them
-        constexpr int CPR = D / 8;
+        constexpr int CPR = D * (int)sizeof(T) / 16;
         for (int x = lane; x < TR * CPR; x += 32) {
           const int r = x / CPR, c = x % CPR;
           if (!there(r))
@@ -555,10 +588,28 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         if (!EXACT && 16 * ks >= d_qk) break;
-        uint32_t af[4];
-        ldsm4(sK + (ks >> 2) * SLAB_B + swz(k_row, (ks & 3) * 2 + k_cadd), af);
+        if constexpr (F32) {
+          // (the queries are split anew for every tile: their two parts would take the registers of two more blocks)
 #pragma unroll
-        for (int gi = 0; gi < NG; ++gi) mma16816(vc[ks % CH][gi], af, qb[gi][ks][0], qb[gi][ks][1]);
+          for (int gi = 0; gi < NG; ++gi)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) asm volatile("" : "+r"(qb[gi][ks][F32 ? x : 0]));
+          // two steps of eight dims: of the 16, a thread's four are k = tq, tq + 4 of the first step, then of the second
+          const unsigned char* sk = wstages + s * S::STAGE_B + (ks >> 1) * SLAB_B;
+          const float4 lo8 = *reinterpret_cast<const float4*>(sk + swz(gq, (ks & 1) * 4 + tq));
+          const float4 hi8 = *reinterpret_cast<const float4*>(sk + swz(gq + 8, (ks & 1) * 4 + tq));
+          const Tf32 kx[8] = {tf32_of(lo8.x), tf32_of(hi8.x), tf32_of(lo8.y), tf32_of(hi8.y), tf32_of(lo8.z), tf32_of(hi8.z), tf32_of(lo8.w), tf32_of(hi8.w)};
+#pragma unroll
+          for (int st = 0; st < 2; ++st)
+#pragma unroll
+            for (int gi = 0; gi < NG; ++gi)
+              mma_3tf32(vc[CH == 2 ? st : 0][gi], kx + 4 * st, tf32_of(__uint_as_float(qb[gi][ks][2 * st])), tf32_of(__uint_as_float(qb[gi][ks][2 * st + 1])));
+        } else {
+          uint32_t af[4];
+          ldsm4(sK + (ks >> 2) * SLAB_B + swz(k_row, (ks & 3) * 2 + k_cadd), af);
+#pragma unroll
+          for (int gi = 0; gi < NG; ++gi) mma16816(vc[ks % CH][gi], af, qb[gi][ks][0], qb[gi][ks][1]);
+        }
       }
       float v[NG][4];
 #pragma unroll
@@ -612,31 +663,65 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
           }
         }
       }
-      uint32_t ph[NG][2], pl[NG][2];                                     // P^T as B operands: the rounded p and the rest
-#pragma unroll
-      for (int gi = 0; gi < NG; ++gi) {
-        const float r0 = m_ref[gi][0] == -INFINITY ? 0.f : m_ref[gi][0], r1 = m_ref[gi][1] == -INFINITY ? 0.f : m_ref[gi][1];
-#pragma unroll
-        for (int r8 = 0; r8 < 2; ++r8) {
-          const float p0 = fast_exp2(v[gi][2 * r8] - r0), p1 = fast_exp2(v[gi][2 * r8 + 1] - r1);
-          l_part[gi][0] += p0;
-          l_part[gi][1] += p1;
-          const uint32_t hi = pack_bf16(p0, p1);
-          const float h0 = __uint_as_float(hi << 16), h1 = __uint_as_float(hi & 0xffff0000u);
-          ph[gi][r8] = movmatrix_t(hi);
-          pl[gi][r8] = movmatrix_t(pack_bf16(p0 - h0, p1 - h1));
-        }
-      }
-      // ---- O^T += V tile^T . P^T ----
-#pragma unroll
-      for (int db = 0; db < KS; ++db) {
-        if (!EXACT && 16 * db >= d_v) break;
-        uint32_t af[4];
-        ldsm4t(sV + (db >> 2) * SLAB_B + swz(v_row, (db & 3) * 2 + v_cadd), af);
+      if constexpr (F32) {
+        Tf32 pb[NG][2][2];                                                 // P^T as B operands: [k block of 8 rows][k = tq: row 2 tq, k = tq + 4: row 2 tq + 1]
 #pragma unroll
         for (int gi = 0; gi < NG; ++gi) {
-          mma16816(oacc[gi][db], af, ph[gi][0], ph[gi][1]);
-          mma16816(oacc[gi][db], af, pl[gi][0], pl[gi][1]);
+          const float r0 = m_ref[gi][0] == -INFINITY ? 0.f : m_ref[gi][0], r1 = m_ref[gi][1] == -INFINITY ? 0.f : m_ref[gi][1];
+#pragma unroll
+          for (int r8 = 0; r8 < 2; ++r8) {
+            const float p0 = fast_exp2(v[gi][2 * r8] - r0), p1 = fast_exp2(v[gi][2 * r8 + 1] - r1);
+            l_part[gi][0] += p0;
+            l_part[gi][1] += p1;
+            // transposed as two matrices of 16-bit halves
+            const uint32_t up = movmatrix_t(__byte_perm(__float_as_uint(p0), __float_as_uint(p1), 0x7632));
+            const uint32_t dn = movmatrix_t(__byte_perm(__float_as_uint(p0), __float_as_uint(p1), 0x5410));
+            pb[gi][r8][0] = tf32_of(__uint_as_float(__byte_perm(dn, up, 0x5410)));
+            pb[gi][r8][1] = tf32_of(__uint_as_float(__byte_perm(dn, up, 0x7632)));
+          }
+        }
+        // ---- O^T += V tile^T . P^T ----  (even rows first: the threads of a warp then read different banks)
+#pragma unroll
+        for (int db = 0; db < KS; ++db) {
+          if (!EXACT && 16 * db >= d_v) break;
+          const unsigned char* sv = wstages + s * S::STAGE_B + S::TENS_B + (db >> 1) * SLAB_B + (gq & 3) * 4;
+          const int c = (db & 1) * 4 + (gq >> 2);
+#pragma unroll
+          for (int r8 = 0; r8 < 2; ++r8) {
+            const int r = 8 * r8 + 2 * tq;
+            const auto val = [&](int row, int chunk) { return tf32_of(*reinterpret_cast<const float*>(sv + swz(row, chunk))); };
+            const Tf32 vx[4] = {val(r, c), val(r, c + 2), val(r + 1, c), val(r + 1, c + 2)};
+#pragma unroll
+            for (int gi = 0; gi < NG; ++gi) mma_3tf32(oacc[gi][db], vx, pb[gi][r8][0], pb[gi][r8][1]);
+          }
+        }
+      } else {
+        uint32_t ph[NG][2], pl[NG][2];                                     // P^T as B operands: the rounded p and the rest
+#pragma unroll
+        for (int gi = 0; gi < NG; ++gi) {
+          const float r0 = m_ref[gi][0] == -INFINITY ? 0.f : m_ref[gi][0], r1 = m_ref[gi][1] == -INFINITY ? 0.f : m_ref[gi][1];
+#pragma unroll
+          for (int r8 = 0; r8 < 2; ++r8) {
+            const float p0 = fast_exp2(v[gi][2 * r8] - r0), p1 = fast_exp2(v[gi][2 * r8 + 1] - r1);
+            l_part[gi][0] += p0;
+            l_part[gi][1] += p1;
+            const uint32_t hi = pack_bf16(p0, p1);
+            const float h0 = __uint_as_float(hi << 16), h1 = __uint_as_float(hi & 0xffff0000u);
+            ph[gi][r8] = movmatrix_t(hi);
+            pl[gi][r8] = movmatrix_t(pack_bf16(p0 - h0, p1 - h1));
+          }
+        }
+        // ---- O^T += V tile^T . P^T ----
+#pragma unroll
+        for (int db = 0; db < KS; ++db) {
+          if (!EXACT && 16 * db >= d_v) break;
+          uint32_t af[4];
+          ldsm4t(sV + (db >> 2) * SLAB_B + swz(v_row, (db & 3) * 2 + v_cadd), af);
+#pragma unroll
+          for (int gi = 0; gi < NG; ++gi) {
+            mma16816(oacc[gi][db], af, ph[gi][0], ph[gi][1]);
+            mma16816(oacc[gi][db], af, pl[gi][0], pl[gi][1]);
+          }
         }
       }
       __syncwarp();
@@ -705,7 +790,7 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
       }
       __syncthreads();
     }
-    write_segment<__nv_bfloat16, S::NT, NWARP / 2>(a, buf, LD, NCOL * LD, jm, jl, at.e, at.u, nh, whole, 2 * blockIdx.x + (at.t == 0));
+    write_segment<T, S::NT, NWARP / 2>(a, buf, LD, NCOL * LD, jm, jl, at.e, at.u, nh, whole, 2 * blockIdx.x + (at.t == 0));
 
     if (tb < at.nt) break;
     done += cnt;
@@ -1284,27 +1369,27 @@ __global__ void __launch_bounds__(JNT, 3) paged_join_kernel(const __grid_constan
 // ---------------------------------------------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------------------------------------------
-template <int D, int NWARP, int NSTAGE, int NG, int CTAS, Tiles MODE>
+template <typename T, int D, int NWARP, int NSTAGE, int NG, int CTAS, Tiles MODE>
 cudaError_t launch_mma_as(const PagedArgs& a, const CUtensorMap& tk, const CUtensorMap& tv, cudaStream_t st) {
-  using S = MmaShape<D, NWARP, NSTAGE, NG>;
+  using S = MmaShape<T, D, NWARP, NSTAGE, NG>;
   static_assert(CTAS * (S::smem + sizeof(Held) + 1280) <= 228 * 1024, "all CTAs of the grid are resident at once");
   static SmemLimit limit = {};
-  if (cudaError_t e = ensure_dyn_smem(paged_mma_kernel<D, NWARP, NSTAGE, NG, CTAS, MODE>, S::smem, limit)) return e;
-  const cudaError_t e = launch_pdl(paged_mma_kernel<D, NWARP, NSTAGE, NG, CTAS, MODE>, dim3(a.ctas), dim3(S::NT), S::smem, st, a, tk, tv);
+  if (cudaError_t e = ensure_dyn_smem(paged_mma_kernel<T, D, NWARP, NSTAGE, NG, CTAS, MODE>, S::smem, limit)) return e;
+  const cudaError_t e = launch_pdl(paged_mma_kernel<T, D, NWARP, NSTAGE, NG, CTAS, MODE>, dim3(a.ctas), dim3(S::NT), S::smem, st, a, tk, tv);
   count_launch();
   return e;
 }
 
-template <int D, int NWARP, int NSTAGE, int NG, int CTAS>
+template <typename T, int D, int NWARP, int NSTAGE, int NG, int CTAS>
 cudaError_t launch_mma(const PagedArgs& a, const CUtensorMap& tk, const CUtensorMap& tv, cudaStream_t st) {
-  if (!a.tiled) return launch_mma_as<D, NWARP, NSTAGE, NG, CTAS, Tiles::ROWS>(a, tk, tv, st);
-  return a.d_qk == D && a.d_v == D && a.map.page % TR == 0 ? launch_mma_as<D, NWARP, NSTAGE, NG, CTAS, Tiles::EXACT>(a, tk, tv, st)
-                                                           : launch_mma_as<D, NWARP, NSTAGE, NG, CTAS, Tiles::BOXES>(a, tk, tv, st);
+  if (!a.tiled) return launch_mma_as<T, D, NWARP, NSTAGE, NG, CTAS, Tiles::ROWS>(a, tk, tv, st);
+  return a.d_qk == D && a.d_v == D && a.map.page % TR == 0 ? launch_mma_as<T, D, NWARP, NSTAGE, NG, CTAS, Tiles::EXACT>(a, tk, tv, st)
+                                                           : launch_mma_as<T, D, NWARP, NSTAGE, NG, CTAS, Tiles::BOXES>(a, tk, tv, st);
 }
 
 // CTAs per SM that the kernels are built for (launch bounds, and the shared memory of the tensor-core ones)
 constexpr int kMmaCtas = 3, kMmaCtasWide = 2;
-constexpr int simt_ctas(bool wide, int gb) { return wide ? 2 : 3; }
+constexpr int simt_ctas(bool wide) { return wide ? 2 : 3; }
 // Stages of a warp of the portable kernel: what the CTAs of an SM leave each other of its shared memory.
 int simt_stages(const Shape& s, int eb, int ctas, bool wide) {
   const int stage = simt_rows(wide) * (s.d_qk + s.d_v) * eb, n = (228 * 1024 / ctas - 11500) / (SNW * stage);   // 11.5 KB: static and reserved
@@ -1313,7 +1398,7 @@ int simt_stages(const Shape& s, int eb, int ctas, bool wide) {
 
 template <int NV, int HB>
 cudaError_t launch_simt_hb(const PagedArgs& a, const CUtensorMap& tk, const CUtensorMap& tv, cudaStream_t st) {
-  constexpr int C = simt_ctas(NV > 1, HB);
+  constexpr int C = simt_ctas(NV > 1);
   static SmemLimit limit = {};
   const size_t smem = (size_t)SNW * a.stages * a.tr * (a.d_qk + a.d_v) * sizeof(float) + 128;
   if (cudaError_t e = ensure_dyn_smem(paged_simt_kernel<NV, HB, C>, smem, limit)) return e;
@@ -1325,8 +1410,7 @@ template <int NV>
 cudaError_t launch_simt(const PagedArgs& a, const CUtensorMap& tk, const CUtensorMap& tv, cudaStream_t st) {
   if (a.gb <= 1) return launch_simt_hb<NV, 1>(a, tk, tv, st);
   if (a.gb <= 2) return launch_simt_hb<NV, 2>(a, tk, tv, st);
-  if (NV > 1 || a.gb <= 4) return launch_simt_hb<NV, 4>(a, tk, tv, st);
-  return launch_simt_hb<1, 8>(a, tk, tv, st);
+  return launch_simt_hb<NV, 4>(a, tk, tv, st);
 }
 
 // Logits stored of a row: vectors of four, when there are more than two.
@@ -1335,12 +1419,16 @@ int logits_of(int gb) { return gb <= 2 ? gb : (gb + 3) / 4 * 4; }
 }  // namespace
 
 int paged_decode_plan(int dtype, const Shape& s, const PageMap& m, int n_active, bool weights, int sms, PagedDecodePlan* p) {
-  p->mma = dtype == SNAP_BF16;
+  // Single precision: on the tensor cores a group of any size costs the same, but a tile's numbers have to be split.  8
+  // sequences of 2000 to 6000 rows, 4 KV heads, portable against tensor cores in us: 64 dims, groups of 1, 4, 16: 26.9 / 20.2,
+  // 33.5 / 21.4, 66.4 / 27.2; 128 dims, 1, 4, 8, 16: 29.3 / 33.5, 33.1 / 34.1, 38.9 / 35.3, 66.9 / 45.2; 256 dims, 4, 8: 52.0 /
+  // 68.0, 79.7 / 69.5.
+  p->mma = dtype == SNAP_BF16 || s.g > 4 || (s.d_qk <= 64 && s.d_v <= 64);
   const bool wide = s.d_qk > 128 || s.d_v > 128;
-  const int most = p->mma ? 16 : wide ? 4 : 8;                          // heads of a unit
+  const int most = p->mma ? (dtype == SNAP_F32 && wide ? 8 : 16) : 4;     // heads of a unit
   p->nhb = (s.g + most - 1) / most;
   p->gb = (s.g + p->nhb - 1) / p->nhb;
-  const int per_sm = p->mma ? (p->gb > 8 ? kMmaCtasWide : kMmaCtas) : simt_ctas(wide, p->gb);
+  const int per_sm = p->mma ? (p->gb > 8 ? kMmaCtasWide : kMmaCtas) : simt_ctas(wide);
   p->ctas = sms * per_sm < MAX_CTAS ? sms * per_sm : MAX_CTAS;
   const long long units = (long long)n_active * s.Hkv * p->nhb;
   // grid and index limits; a line of tiles and the scratch have to be countable
@@ -1375,7 +1463,7 @@ cudaError_t launch_paged_decode(int dtype, const Shape& s, const PageMap& m, con
   a.w_in = w_in; a.w_out = w_out; a.status = status; a.ctas = p.ctas;
   const bool wide = s.d_qk > 128 || s.d_v > 128;
   a.tr = p.mma ? TR : simt_rows(wide);
-  a.stages = simt_stages(s, elt_bytes(dtype), simt_ctas(wide, p.gb), wide);
+  a.stages = simt_stages(s, elt_bytes(dtype), simt_ctas(wide), wide);
   // Tiles come through tensor maps where a page holds whole ones: 64 dims wide with the 128-byte swizzle for the
   // tensor-core kernel, whole rows for the portable one.  (Encoding both takes the host under a microsecond.)
   CUtensorMap tk = {}, tv = {};
@@ -1386,7 +1474,7 @@ cudaError_t launch_paged_decode(int dtype, const Shape& s, const PageMap& m, con
     const cuuint64_t dims[4] = {(cuuint64_t)d, (cuuint64_t)m.page, (cuuint64_t)s.Hkv, (cuuint64_t)m.n_pages};
     // a stride that is never applied (one KV head, one page) may be anything: the map gets one that it takes
     const cuuint64_t strides[3] = {(cuuint64_t)rs * eb, (cuuint64_t)(s.Hkv > 1 ? hs : d) * eb, (cuuint64_t)(m.n_pages > 1 ? ps : d) * eb};
-    const cuuint32_t box[4] = {(cuuint32_t)(p.mma ? 64 : d), (cuuint32_t)rows, 1, 1}, estr[4] = {1, 1, 1, 1};
+    const cuuint32_t box[4] = {(cuuint32_t)(p.mma ? 128 / elt_bytes(dtype) : d), (cuuint32_t)rows, 1, 1}, estr[4] = {1, 1, 1, 1};
     return enc(t, dtype == SNAP_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims,
                strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, p.mma ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
@@ -1396,9 +1484,15 @@ cudaError_t launch_paged_decode(int dtype, const Shape& s, const PageMap& m, con
   if (p.mma) {
     const bool two = p.gb > 8;
     const int d = s.d_qk > s.d_v ? s.d_qk : s.d_v;
-    if (d <= 64) e = two ? launch_mma<64, 4, 4, 2, kMmaCtasWide>(a, tk, tv, st) : launch_mma<64, 4, 4, 1, kMmaCtas>(a, tk, tv, st);
-    else if (d <= 128) e = two ? launch_mma<128, 4, 2, 2, kMmaCtasWide>(a, tk, tv, st) : launch_mma<128, 4, 2, 1, kMmaCtas>(a, tk, tv, st);
-    else e = two ? launch_mma<256, 2, 2, 2, kMmaCtasWide>(a, tk, tv, st) : launch_mma<256, 2, 2, 1, kMmaCtas>(a, tk, tv, st);
+    using BF = __nv_bfloat16;
+    if (dtype == SNAP_F32) {
+      if (d <= 64) e = two ? launch_mma<float, 64, 4, 2, 2, kMmaCtasWide>(a, tk, tv, st) : launch_mma<float, 64, 4, 2, 1, kMmaCtas>(a, tk, tv, st);
+      else if (d <= 128) e = two ? launch_mma<float, 128, 4, 1, 2, kMmaCtasWide>(a, tk, tv, st) : launch_mma<float, 128, 4, 1, 1, kMmaCtas>(a, tk, tv, st);
+      else e = launch_mma<float, 256, 2, 1, 1, kMmaCtas>(a, tk, tv, st);
+    }
+    else if (d <= 64) e = two ? launch_mma<BF, 64, 4, 4, 2, kMmaCtasWide>(a, tk, tv, st) : launch_mma<BF, 64, 4, 4, 1, kMmaCtas>(a, tk, tv, st);
+    else if (d <= 128) e = two ? launch_mma<BF, 128, 4, 2, 2, kMmaCtasWide>(a, tk, tv, st) : launch_mma<BF, 128, 4, 2, 1, kMmaCtas>(a, tk, tv, st);
+    else e = two ? launch_mma<BF, 256, 2, 2, 2, kMmaCtasWide>(a, tk, tv, st) : launch_mma<BF, 256, 2, 2, 1, kMmaCtas>(a, tk, tv, st);
   } else {
     e = wide ? launch_simt<2>(a, tk, tv, st) : launch_simt<1>(a, tk, tv, st);
   }
@@ -1415,7 +1509,8 @@ cudaError_t launch_paged_decode(int dtype, const Shape& s, const PageMap& m, con
   const dim3 grid((unsigned)(first + joins));
   const auto join = [&](auto kernel) { return launch_pdl(kernel, grid, dim3(JNT), 0, st, a, first, by_heads, per); };
   if (dtype == SNAP_F32) {
-    e = !w_out ? join(paged_join_kernel<float, 0>) : quads == 1 ? join(paged_join_kernel<float, 1>) : join(paged_join_kernel<float, 2>);
+    e = !w_out ? join(paged_join_kernel<float, 0>) : quads == 1 ? join(paged_join_kernel<float, 1>)
+        : quads == 2 ? join(paged_join_kernel<float, 2>) : join(paged_join_kernel<float, 4>);
   } else {
     e = !w_out ? join(paged_join_kernel<__nv_bfloat16, 0>) : quads == 1 ? join(paged_join_kernel<__nv_bfloat16, 1>)
         : quads == 2 ? join(paged_join_kernel<__nv_bfloat16, 2>) : join(paged_join_kernel<__nv_bfloat16, 4>);

@@ -265,7 +265,7 @@ DECODES = [  # hq, hkv, d, dv, page, layout
     (12, 1, 128, 128, 32, "hnd"), (32, 1, 64, 64, 16, "nhd"), (40, 2, 256, 256, 32, "hnd"), (9, 3, 80, 80, 16, "hnd"),
     (6, 1, 128, 64, 8, "nhd"), (2, 1, 48, 96, 5, "hnd"), (16, 2, 64, 64, 1, "nhd"), (11, 1, 192, 256, 24, "hnd"), (5, 5, 16, 16, 7, "hnd"),
     (8, 2, 128, 128, 1, "hnd"), (20, 1, 128, 112, 3, "hnd"), (40, 2, 256, 256, 1, "nhd"), (6, 2, 64, 64, 9, "nhd"), (7, 1, 256, 256, 13, "hnd"),
-    (12, 1, 64, 48, 2, "hnd")]
+    (12, 1, 64, 48, 2, "hnd"), (8, 2, 256, 256, 16, "hnd"), (3, 1, 256, 192, 3, "nhd"), (16, 1, 128, 128, 16, "nhd")]
 LENGTHS = [0, 1, 15, 16, 17, 31, 333, 0, 2, 1300, 64, 47]
 
 
@@ -295,7 +295,8 @@ def test_paged_decode_matches_its_definition(hq, hkv, d, dv, page, layout, dtype
 
 
 @pytest.mark.parametrize("dtype,hq,hkv,d,page", [("bf16", 32, 8, 128, 32), ("f32", 8, 2, 128, 32), ("bf16", 8, 8, 64, 32), ("f32", 16, 2, 96, 32),
-                                                 ("bf16", 32, 8, 128, 1), ("bf16", 24, 2, 256, 12)])
+                                                 ("bf16", 32, 8, 128, 1), ("bf16", 24, 2, 256, 12), ("f32", 6, 2, 256, 16),
+                                                 ("f32", 8, 8, 64, 20)])
 def test_paged_decode_of_long_and_single_sequences(dtype, hq, hkv, d, page):
     """One sequence over all CTAs, few tiles per CTA, and many short ones: every way a unit can be cut."""
     for lengths in ([9001], [16 * 37], [5, 20011, 1, 700], [33] * 200):
@@ -606,15 +607,16 @@ def test_prompt_steps_eviction_steps(dtype, hq, hkv, d, page):
 
 
 @pytest.mark.parametrize("dtype,page", [("bf16", 16), ("f32", 16), ("bf16", 8), ("bf16", 3)])
-def test_paged_decode_carries_nan_and_leaves_other_heads_alone(dtype, page):
+@pytest.mark.parametrize("d", [64, 96])
+def test_paged_decode_carries_nan_and_leaves_other_heads_alone(dtype, page, d):
     """A NaN in a row that counts reaches the heads that attend it, over joins too, and no other head."""
-    cfg = config(4, 2, 64, dtype=dtype, max_seqs=3)
+    cfg = config(4, 2, d, dtype=dtype, max_seqs=3)
     c = Pages(cfg, dtype, page, [5000, 40, 1], seed=6)
     row = 3333
     c.k[int(c.table[0, row // page]), 1, row % page, 3] = float("nan")
     c.v[int(c.table[1, 5 // page]), 0, 5 % page, 7] = float("nan")
     c.k[int(c.table[2, 0]), 0, 0, 0] = float("nan")
-    q = torch.randn(3, 4, 64, device="cuda").to(DT[dtype])
+    q = torch.randn(3, 4, d, device="cuda").to(DT[dtype])
     w = c.weights()
     out = f64(run_decode(c, q, [0, 1, 2], weights_out=w))
     assert np.isnan(out[0, 2:]).all() and np.isfinite(out[0, :2]).all()
