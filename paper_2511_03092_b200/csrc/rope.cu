@@ -12,8 +12,8 @@
 // counts is how many warps are resident, not how much each has in flight: one head at a time and five blocks per SM
 // turn a 32768-token prompt of 40 heads of 128 dims in 110 us (6.1 TB/s); two heads at a time and four blocks take
 // 113 us, three and three 125, and looping over tokens in as many blocks as fit 124 to 144.  Appending 26003 tokens of
-// the same layer (queries, keys twice, values) takes 121 us (5.7 TB/s).  Threads are laid out as [tokens][heads][items of a head]: consecutive
-// threads are on consecutive vectors, and few tokens spread over more threads per token.
+// the same layer (queries, keys twice, values) takes 121 us (5.7 TB/s).  Threads are laid out as [tokens][heads][items of
+// a head]: consecutive threads are on consecutive vectors, and few tokens spread over more threads per token.
 //
 // The kernel after it starts when this one ends, not beside its last blocks: attention over the pages comes next, whose
 // blocks fill an SM's registers to the last thousand and would find them in pieces.
@@ -36,7 +36,7 @@ template <typename T, int V> union Vec {
   __device__ Vec() {}
 };
 
-struct RopeLaunch { RopeArgs a; int nj, nc, X, Y, Z; };   // items and copied vectors of a head; thread layout
+struct RopeLaunch { RopeArgs a; int nj, ni, nc, X, Y, Z; };   // items of a head that turn, all items, copied vectors; thread layout
 
 // cos and sin of position * f, the angle taken in half turns: its whole turns come off exactly
 __device__ __forceinline__ float2 cos_sin(int pos, double f) {
@@ -48,7 +48,9 @@ __device__ __forceinline__ float2 cos_sin(int pos, double f) {
   return make_float2(fmaf(-rl, s, c), fmaf(rl, c, s));
 }
 
-template <typename T, int V, bool INTER, bool PAGED>
+// Which of a head's dims turn: all that this call moves (of an unpaged call in place, the others stay where they are), some, none.
+enum class Turns { ALL, SOME, NONE };
+template <typename T, int V, bool INTER, bool PAGED, Turns TURNS>
 __global__ void __launch_bounds__(NT, 5) rope_kernel(const __grid_constant__ RopeLaunch L) {
   using VT = Vec<T, V>;
   using Raw = decltype(VT::raw);
@@ -95,16 +97,26 @@ __global__ void __launch_bounds__(NT, 5) rope_kernel(const __grid_constant__ Rop
   const T* k = static_cast<const T*>(a.k) + t * a.k_tok;
   const int H = a.Hq + a.Hkv;
   const auto source = [&](int h) { return h < a.Hq ? q + h * a.q_head : k + (h - a.Hq) * a.k_head; };
-  // item j of a head: its two vectors
-  const auto first_of = [&](int j) { return a.offset + (INTER ? 2 * j * V : j * V); };
-  const int to_second = INTER ? V : half;
-  VT va, vb;
-  const auto load = [&](int j, int h) {
-    const T* s = source(h) + first_of(j);
-    va.raw = *reinterpret_cast<const Raw*>(s);
-    vb.raw = *reinterpret_cast<const Raw*>(s + to_second);
+  // Item j of a head: two vectors that turn, or, behind those, two neighbours of the head's other dims.  (All of them in
+  // one loop: a head's row is read and written as a whole.  With the other dims copied afterwards 28357 tokens of 51 heads of
+  // 64 dims, half of them turned, took 115 us instead of 74.)
+  int at_a, at_b;
+  bool turn, two;
+  const auto item = [&](int j) {
+    turn = TURNS == Turns::ALL || j < L.nj;
+    two = turn || 2 * (j - L.nj) + 1 < L.nc;
+    const auto other = [&](int c) { return c * V < a.offset ? c * V : c * V + a.rot; };
+    at_a = turn ? a.offset + (INTER ? 2 * j * V : j * V) : other(2 * (j - L.nj));
+    at_b = turn ? at_a + (INTER ? V : half) : other(2 * (j - L.nj) + 1);
   };
-  if (mine && x < L.nj && y < H) load(x, y);                              // on their way while the angles are computed
+  VT va, vb;
+  const auto load = [&](int h) {
+    const T* s = source(h);
+    va.raw = *reinterpret_cast<const Raw*>(s + at_a);
+    if (two) vb.raw = *reinterpret_cast<const Raw*>(s + at_b);
+  };
+  if (TURNS != Turns::NONE) item(x);
+  if (TURNS != Turns::NONE && mine && x < L.ni && y < H) load(y);                                 // on their way while the angles are computed
 
   if (paged && x == 0 && y == 0 && z < L.Z) placed[z] = make_int2(slot, skip ? -1 : row);
   // ---- values: copied to the page while the angles are on their way ----
@@ -157,44 +169,53 @@ __global__ void __launch_bounds__(NT, 5) rope_kernel(const __grid_constant__ Rop
     }
   };
 
-  // ---- rotated dims ----
-  for (int j = x; j < L.nj; j += L.X) {
+  for (int j = x; TURNS != Turns::NONE && j < L.ni; j += L.X) {
+    if (j != x) item(j);
     float2 cs[V];
+    if (turn) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) cs[i] = table[z * half + j * V + i];
-    const int at_a = first_of(j), at_b = at_a + to_second;
+      for (int i = 0; i < V; ++i) cs[i] = table[z * half + j * V + i];
+    }
     for (int h = y; h < H; h += L.Y) {
-      if (j != x || h != y) load(j, h);
-      VT oa, ob;
+      if (j != x || h != y) load(h);
+      if (turn) {
+        VT oa, ob;
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        // interleaved: the item's 2 V elements are V neighbouring pairs, else pair i is (va[i], vb[i])
-        const float p = to_f32<T>(INTER ? (2 * i < V ? va.e[(2 * i) % V] : vb.e[(2 * i) % V]) : va.e[i]);
-        const float r = to_f32<T>(INTER ? (2 * i + 1 < V ? va.e[(2 * i + 1) % V] : vb.e[(2 * i + 1) % V]) : vb.e[i]);
-        const T c0 = from_f32<T>(fmaf(p, cs[i].x, -(r * cs[i].y))), c1 = from_f32<T>(fmaf(r, cs[i].x, p * cs[i].y));
-        if (INTER) {
-          if (2 * i < V) oa.e[(2 * i) % V] = c0; else ob.e[(2 * i) % V] = c0;
-          if (2 * i + 1 < V) oa.e[(2 * i + 1) % V] = c1; else ob.e[(2 * i + 1) % V] = c1;
-        } else {
-          oa.e[i] = c0;
-          ob.e[i] = c1;
+        for (int i = 0; i < V; ++i) {
+          // interleaved: the item's 2 V elements are V neighbouring pairs, else pair i is (va[i], vb[i])
+          const float p = to_f32<T>(INTER ? (2 * i < V ? va.e[(2 * i) % V] : vb.e[(2 * i) % V]) : va.e[i]);
+          const float r = to_f32<T>(INTER ? (2 * i + 1 < V ? va.e[(2 * i + 1) % V] : vb.e[(2 * i + 1) % V]) : vb.e[i]);
+          const T c0 = from_f32<T>(fmaf(p, cs[i].x, -(r * cs[i].y))), c1 = from_f32<T>(fmaf(r, cs[i].x, p * cs[i].y));
+          if (INTER) {
+            if (2 * i < V) oa.e[(2 * i) % V] = c0; else ob.e[(2 * i) % V] = c0;
+            if (2 * i + 1 < V) oa.e[(2 * i + 1) % V] = c1; else ob.e[(2 * i + 1) % V] = c1;
+          } else {
+            oa.e[i] = c0;
+            ob.e[i] = c1;
+          }
         }
+        if (TURNS == Turns::ALL) {                                         // (through va and vb: 113 instead of 110 us for the prompt above)
+          put(h, at_a, oa.raw);
+          put(h, at_b, ob.raw);
+          continue;
+        }
+        va = oa;
+        vb = ob;
       }
-      put(h, at_a, oa.raw);
-      put(h, at_b, ob.raw);
+      put(h, at_a, va.raw);
+      if (two) put(h, at_b, vb.raw);
     }
   }
-  // ---- the head's other dims ----
-  for (int c = x; c < L.nc; c += L.X) {
-    const int at = c * V < a.offset ? c * V : c * V + a.rot;
+  // ---- no dims that turn: four heads at a time ----
+  for (int c = x; TURNS == Turns::NONE && c < L.nc; c += L.X) {
     for (int h0 = y; h0 < H; h0 += 4 * L.Y) {
       Raw r[4];
 #pragma unroll
       for (int u = 0; u < 4; ++u)
-        if (h0 + u * L.Y < H) r[u] = *reinterpret_cast<const Raw*>(source(h0 + u * L.Y) + at);
+        if (h0 + u * L.Y < H) r[u] = *reinterpret_cast<const Raw*>(source(h0 + u * L.Y) + c * V);
 #pragma unroll
       for (int u = 0; u < 4; ++u)
-        if (h0 + u * L.Y < H) put(h0 + u * L.Y, at, r[u]);
+        if (h0 + u * L.Y < H) put(h0 + u * L.Y, c * V, r[u]);
     }
   }
   if (paged) {
@@ -210,15 +231,19 @@ cudaError_t launch_v(const RopeArgs& a, int sms, cudaStream_t st) {
   const bool in_place = !a.k_pages && (!a.q || a.q == a.q_out) && (!a.k || a.k == a.k_out);
   L.nj = a.rot / 2 / V;
   L.nc = in_place ? 0 : (a.d_qk - a.rot) / V;
-  const int items = L.nj > 0 ? L.nj : L.nc;
+  L.ni = L.nj + (L.nc + 1) / 2;
+  const int items = L.nj > 0 ? L.ni : L.nc;
   L.X = items < 64 ? items : 64;
   const int H = a.Hq + a.Hkv, per = NT / L.X;                             // (token, head) pairs of a block
-  // Few tokens: as many threads per token as there are heads.  Many: a thread takes four to eight heads of its token, so
-  // that the angles it reads are used that often, in the split that leaves the fewest threads without one.
+  // As many threads as there is work for, up to what the GPU holds at once; more work: a thread takes several heads of its
+  // token, at most four to eight, so that the angles it reads are used that often, in the split that leaves the fewest
+  // threads without one.
   L.Y = H < per ? H : per;
-  if ((long long)a.n_tokens * H / per >= 4LL * sms) {
+  const long long work = (long long)a.n_tokens * H * L.X, full = (work + 5LL * sms * NT - 1) / (5LL * sms * NT);
+  if (full > 1) {
     int best = 0;
-    for (int its = 8; its >= 4; --its) {
+    const int least = full < 4 ? (int)full : 4, most = full < 4 ? least + 1 : 8;
+    for (int its = most; its >= least; --its) {
       const int Y = (H + its - 1) / its, used = Y <= per ? per / Y * H * 64 / its : 0;   // head slots that do work
       if (used > best) { best = used; L.Y = Y; }
     }
@@ -227,9 +252,13 @@ cudaError_t launch_v(const RopeArgs& a, int sms, cudaStream_t st) {
   if (L.Z > a.n_tokens) L.Z = a.n_tokens;
   const size_t smem = (size_t)L.Z * (a.rot / 2) * sizeof(float2);        // at most 2048 pairs: X covers them or Z is small
   const dim3 grid((a.n_tokens + L.Z - 1) / L.Z);
+  const auto launch = [&](auto kernel) { return launch_pdl(kernel, grid, dim3(NT), smem, st, L); };
   cudaError_t e;
-  if (a.k_pages) e = a.interleaved ? launch_pdl(rope_kernel<T, V, true, true>, grid, dim3(NT), smem, st, L) : launch_pdl(rope_kernel<T, V, false, true>, grid, dim3(NT), smem, st, L);
-  else e = a.interleaved ? launch_pdl(rope_kernel<T, V, true, false>, grid, dim3(NT), smem, st, L) : launch_pdl(rope_kernel<T, V, false, false>, grid, dim3(NT), smem, st, L);
+  if (L.nj == 0) e = launch(rope_kernel<T, V, false, true, Turns::NONE>);                  // (an append)
+  else if (L.nc == 0 && a.k_pages) e = a.interleaved ? launch(rope_kernel<T, V, true, true, Turns::ALL>) : launch(rope_kernel<T, V, false, true, Turns::ALL>);
+  else if (L.nc == 0) e = a.interleaved ? launch(rope_kernel<T, V, true, false, Turns::ALL>) : launch(rope_kernel<T, V, false, false, Turns::ALL>);
+  else if (a.k_pages) e = a.interleaved ? launch(rope_kernel<T, V, true, true, Turns::SOME>) : launch(rope_kernel<T, V, false, true, Turns::SOME>);
+  else e = a.interleaved ? launch(rope_kernel<T, V, true, false, Turns::SOME>) : launch(rope_kernel<T, V, false, false, Turns::SOME>);
   count_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
 }
