@@ -97,14 +97,14 @@ __global__ void __launch_bounds__(NT, 5) rope_kernel(const __grid_constant__ Rop
   const T* k = static_cast<const T*>(a.k) + t * a.k_tok;
   const int H = a.Hq + a.Hkv;
   const auto source = [&](int h) { return h < a.Hq ? q + h * a.q_head : k + (h - a.Hq) * a.k_head; };
-  // Item j of a head: two vectors that turn, or, behind those, two neighbours of the head's other dims.  (All of them in
+  // Item j of a head: two vectors that turn, or, behind those, two neighbours of the head's other dims (whose number is
+  // even: heads are multiples of 16 dims, the part that turns of two vectors).  (All of them in
   // one loop: a head's row is read and written as a whole.  With the other dims copied afterwards 28357 tokens of 51 heads of
   // 64 dims, half of them turned, took 115 us instead of 74.)
   int at_a, at_b;
-  bool turn, two;
+  bool turn;
   const auto item = [&](int j) {
     turn = TURNS == Turns::ALL || j < L.nj;
-    two = turn || 2 * (j - L.nj) + 1 < L.nc;
     const auto other = [&](int c) { return c * V < a.offset ? c * V : c * V + a.rot; };
     at_a = turn ? a.offset + (INTER ? 2 * j * V : j * V) : other(2 * (j - L.nj));
     at_b = turn ? at_a + (INTER ? V : half) : other(2 * (j - L.nj) + 1);
@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(NT, 5) rope_kernel(const __grid_constant__ Rop
   const auto load = [&](int h) {
     const T* s = source(h);
     va.raw = *reinterpret_cast<const Raw*>(s + at_a);
-    if (two) vb.raw = *reinterpret_cast<const Raw*>(s + at_b);
+    vb.raw = *reinterpret_cast<const Raw*>(s + at_b);
   };
   if (TURNS != Turns::NONE) item(x);
   if (TURNS != Turns::NONE && mine && x < L.ni && y < H) load(y);                                 // on their way while the angles are computed
@@ -203,7 +203,7 @@ __global__ void __launch_bounds__(NT, 5) rope_kernel(const __grid_constant__ Rop
         vb = ob;
       }
       put(h, at_a, va.raw);
-      if (two) put(h, at_b, vb.raw);
+      put(h, at_b, vb.raw);
     }
   }
   // ---- no dims that turn: four heads at a time ----
@@ -231,7 +231,7 @@ cudaError_t launch_v(const RopeArgs& a, int sms, cudaStream_t st) {
   const bool in_place = !a.k_pages && (!a.q || a.q == a.q_out) && (!a.k || a.k == a.k_out);
   L.nj = a.rot / 2 / V;
   L.nc = in_place ? 0 : (a.d_qk - a.rot) / V;
-  L.ni = L.nj + (L.nc + 1) / 2;
+  L.ni = L.nj + L.nc / 2;
   const int items = L.nj > 0 ? L.ni : L.nc;
   L.X = items < 64 ? items : 64;
   const int H = a.Hq + a.Hkv, per = NT / L.X;                             // (token, head) pairs of a block
