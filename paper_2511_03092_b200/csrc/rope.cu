@@ -111,12 +111,14 @@ __global__ void __launch_bounds__(NT, 5) rope_kernel(const __grid_constant__ Rop
   };
   VT va, vb;
   const auto load = [&](int h) {
+    if (PAGED && !index_ok(slot, a.max_seqs, a.status)) return;
     const T* s = source(h);
     va.raw = *reinterpret_cast<const Raw*>(s + at_a);
     vb.raw = *reinterpret_cast<const Raw*>(s + at_b);
   };
   if (TURNS != Turns::NONE) item(x);
-  if (TURNS != Turns::NONE && mine && x < L.ni && y < H) load(y);                                 // on their way while the angles are computed
+  // on their way while the angles (and a paged token's page) are looked up; a token without a slot is padding and has no rows
+  if (TURNS != Turns::NONE && mine && (!PAGED || (slot >= 0 && slot < a.max_seqs)) && x < L.ni && y < H) load(y);
 
   if (paged && x == 0 && y == 0 && z < L.Z) placed[z] = make_int2(slot, skip ? -1 : row);
   // ---- values: copied to the page while the angles are on their way ----
@@ -138,10 +140,13 @@ __global__ void __launch_bounds__(NT, 5) rope_kernel(const __grid_constant__ Rop
   for (int e = tid; e < L.Z * half; e += NT) {
     const int ez = e / half, et = blockIdx.x * L.Z + ez, i = e - ez * half;
     if (et >= a.n_tokens) break;
+    const int es = PAGED ? a.slots[et] : 0;
     int pos = 0;
-    if (a.positions) pos = a.positions[et];
-    else if (a.rows) pos = a.rows[et];
-    else { const int es = a.slots[et]; if (es >= 0 && es < a.max_seqs) pos = a.seq_len[es]; }
+    if (!PAGED || (es >= 0 && es < a.max_seqs)) {                          // (padding has no position)
+      if (!index_ok(es, PAGED ? a.max_seqs : 1, a.status)) pos = 0;
+      else if (a.positions) pos = a.positions[et];
+      else pos = a.rows ? a.rows[et] : a.seq_len[es];
+    }
     const float2 cs = cos_sin(pos, a.freqs[i]);
     table[e] = make_float2(cs.x * a.magnitude, cs.y * (a.magnitude * a.sign));
   }

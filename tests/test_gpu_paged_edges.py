@@ -1,0 +1,81 @@
+"""Calls at the edge of what the rotary and paged-cache entry points promise: what of a padded batch is read, what is
+left alone, and layouts beside the usual two."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged_oracle as orc
+from paper_2511_03092_b200 import binding as B
+from tests.test_gpu_paged import DT, Pages, check_rotation, config, f64, i32
+
+pytestmark = pytest.mark.gpu
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# append
+# ---------------------------------------------------------------------------------------------------------------
+def raw_append(cfg, c, slots, rows, n, k, v, rope=None, freqs=None, positions=None, q=None, q_out=None, k_out=None, weights=None):
+    """snap_paged_append by addresses: the buffers need not have n_tokens tokens."""
+    at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    strides = lambda t: (0, 0) if t is None else t.stride()[:2]  # noqa: E731
+    rc = B.lib().snap_paged_append(C.byref(cfg), C.byref(c.paged), at(slots), at(rows), n, C.byref(rope) if rope else None, at(freqs),
+                                   at(positions), at(q), *strides(q), at(q_out), at(k), *strides(k), at(k_out), at(v), *strides(v), at(c.k),
+                                   at(c.v), at(c.table), at(c.seq_len), at(weights), at(c.status), B._stream(None))
+    assert rc == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rot", [64, 32, 0])
+@pytest.mark.parametrize("by_rows", [True, False])
+def test_append_reads_nothing_of_padding(by_rows, rot, dtype):
+    """Slot -1 is padding: a batch padded at its end may come in buffers that stop at its last live token.  (The checked
+    build raises a bit for a load that belongs to a token without a slot.)"""
+    live, padded, hq, hkv, d = 5, 64, 4, 2, 64
+    cfg = config(hq, hkv, d, dtype=dtype, max_seqs=live)
+    c = Pages(cfg, dtype, 16, [48] * live, seed=3)
+    start = [0, 7, 15, 16, 40]
+    c.seq_len.copy_(i32(start))
+    g = torch.Generator(device="cuda").manual_seed(5)
+    q, k, v = (torch.randn(live, h, d, device="cuda", generator=g).to(DT[dtype]) for h in (hq, hkv, hkv))
+    q_out, k_out = torch.empty_like(q), torch.empty_like(k)
+    positions = [9, 100001, 3, 0, 77]
+    slots = i32([3, 1, 0, 4, 2] + [-1] * (padded - live))
+    order = slots[:live].tolist()
+    rows = i32([start[s] for s in order]) if by_rows else None
+    freqs = orc.rope_table(rot, 10000.0) if rot else None
+    rope = B.make_rope(rot_dim=rot, rot_offset=d - rot) if rot else None
+    before = f64(c.k)
+    raw_append(cfg, c, slots, rows, padded, k, v, rope=rope, freqs=torch.from_numpy(freqs).cuda() if rot else None,
+               positions=i32(positions) if rot else None, q=q, q_out=q_out, k_out=k_out)
+    assert c.bits() == 0
+    assert c.seq_len.tolist() == [x + 1 for x in start]
+    if rot:
+        for got, x in ((q_out, q), (k_out, k)):
+            check_rotation(f64(got), f64(x), positions, freqs, rot, d - rot, False, 1.0, False, dtype)
+    else:
+        assert torch.equal(q_out, q) and torch.equal(k_out, k)
+    table = c.table.cpu().numpy()
+    for i, s in enumerate(order):
+        before[table[s, start[s] // 16], :, start[s] % 16] = f64(k_out)[i]
+    np.testing.assert_array_equal(f64(c.k), before)
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# everything above under the checked build
+# ---------------------------------------------------------------------------------------------------------------
+def test_these_calls_under_the_checked_build():
+    import os
+    import subprocess
+    import sys
+    from paper_2511_03092_b200 import build as snap_build
+    if "SNAP_LIBRARY" in os.environ:
+        return                                              # (this is that run)
+    lib = snap_build.build(debug_bounds=True)
+    env = dict(os.environ, SNAP_LIBRARY=os.path.basename(lib))
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-m", "pytest", "tests/test_gpu_paged_edges.py", "-m", "gpu", "-q", "-x", "-p", "no:cacheprovider"],
+                       cwd=root, env=env, capture_output=True, text=True, timeout=900)
+    assert r.returncode == 0, r.stdout[-3000:] + r.stderr[-2000:]
+    assert " passed" in r.stdout
