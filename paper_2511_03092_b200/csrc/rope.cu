@@ -85,12 +85,15 @@ __global__ void __launch_bounds__(NT, 5) rope_kernel(const __grid_constant__ Rop
     }
   }
   if (paged && !a.rows) {
+    // Listed earlier in this call?  Then it is skipped for that alone: its row is the first one's next, or not, as that one's
+    // block ends sooner or later, and with it what the page table would say.
+    const bool listed = mine && slot >= 0 && slot < a.max_seqs;
     __syncthreads();                                                      // dup is zero
-    if (!skip)                                                            // listed earlier in this call?
+    if (listed)
       for (int e = tid - z * L.X * L.Y; e < t; e += L.X * L.Y)
         if (a.slots[e] == slot) dup[z] = 1;
     __syncthreads();
-    if (!skip && dup[z]) { skip = true; bad = SNAP_DEV_BAD_SLOT; }
+    if (listed && dup[z]) { skip = true; bad = SNAP_DEV_BAD_SLOT; }
   }
 
   const T* q = static_cast<const T*>(a.q) + t * a.q_tok;

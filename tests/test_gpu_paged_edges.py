@@ -62,6 +62,27 @@ def test_append_reads_nothing_of_padding(by_rows, rot, dtype):
     np.testing.assert_array_equal(f64(c.k), before)
 
 
+def test_a_slot_listed_again_is_said_so_whatever_its_pages():
+    """Next rows: a second listing is skipped as such (SNAP_DEV_BAD_SLOT) and for nothing else, wherever in the call it stands
+    and whether or not the row after the first one's has a page."""
+    cfg = config(4, 2, 64, max_seqs=4)
+    c = Pages(cfg, "bf16", 16, [32, 32, 32, 32], seed=2)
+    k = torch.randn(2000, 2, 64, device="cuda").to(torch.bfloat16)
+    # the first listing takes the last row there is: the one after it lies past the table
+    for others in (1, 1500):
+        c.seq_len.copy_(i32([31, 4, 5, 6]))
+        c.status.zero_()
+        slots = [0] + [-1] * others + [0]
+        B.snap_paged_append(cfg, c.paged, i32(slots), None, k[:len(slots)], k[:len(slots)], c.k, c.v, c.table, c.seq_len, status=c.status)
+        assert c.bits() == B.SNAP_DEV_BAD_SLOT and c.seq_len.tolist() == [32, 4, 5, 6]
+    # no page for the next row: the first listing is skipped for that, the second for being the second
+    c.table[1, 1] = -1
+    c.seq_len.copy_(i32([0, 20, 0, 0]))
+    c.status.zero_()
+    B.snap_paged_append(cfg, c.paged, i32([1, 1]), None, k[:2], k[:2], c.k, c.v, c.table, c.seq_len, status=c.status)
+    assert c.bits() == B.SNAP_DEV_BAD_SLOT | B.SNAP_DEV_BAD_PAGE and c.seq_len.tolist() == [0, 20, 0, 0]
+
+
 # ---------------------------------------------------------------------------------------------------------------
 # everything above under the checked build
 # ---------------------------------------------------------------------------------------------------------------
