@@ -1205,6 +1205,18 @@ __device__ __forceinline__ void join_weights(const PagedArgs& a, int id, int per
     float sum[R];                                                          // (the old weight is added last: one rounding at the size of the total)
 #pragma unroll
     for (int j = 0; j < R; ++j) sum[j] = 0.f;
+    // A row on a page that is not there was left out: its entry stays.  Its logits are -infinity, which those of a row that
+    // counts may be too, so the page table decides (looked up for such rows only).
+    bool stays[R];
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+      const int row = row0 + j * JNT + tid;
+      stays[j] = row >= len;
+      if (!stays[j] && v[j][0].x == -INFINITY) {
+        const int page = a.map.table[(long long)slot * a.map.max_pages + row / a.map.page];
+        stays[j] = page < 0 || page >= a.map.n_pages;
+      }
+    }
     for (int hb = 0; hb < a.nhb; ++hb) {
       const int nh = min(a.gb, a.g - hb * a.gb);
       const float* mu = mu_s + hb * a.gb;
@@ -1224,7 +1236,7 @@ __device__ __forceinline__ void join_weights(const PagedArgs& a, int id, int per
 #pragma unroll
     for (int j = 0; j < R; ++j) {
       const int row = row0 + j * JNT + tid;
-      if (row < len) a.w_out[base + row] = old[j] + sum[j];
+      if (!stays[j]) a.w_out[base + row] = old[j] + sum[j];
       old[j] = old_ahead[j];
     }
     row0 = next;

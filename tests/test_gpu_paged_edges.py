@@ -8,7 +8,7 @@ import torch
 
 from oracle import paged_oracle as orc
 from paper_2511_03092_b200 import binding as B
-from tests.test_gpu_paged import DT, Pages, check_rotation, config, f64, i32
+from tests.test_gpu_paged import DT, Pages, check_decode, check_rotation, config, f64, i32, run_decode
 
 pytestmark = pytest.mark.gpu
 
@@ -81,6 +81,70 @@ def test_a_slot_listed_again_is_said_so_whatever_its_pages():
     c.status.zero_()
     B.snap_paged_append(cfg, c.paged, i32([1, 1]), None, k[:2], k[:2], c.k, c.v, c.table, c.seq_len, status=c.status)
     assert c.bits() == B.SNAP_DEV_BAD_SLOT | B.SNAP_DEV_BAD_PAGE and c.seq_len.tolist() == [0, 20, 0, 0]
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# attention
+# ---------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype,hq,hkv,d,page", [("bf16", 8, 2, 128, 16), ("bf16", 4, 2, 64, 8), ("bf16", 3, 1, 80, 5), ("f32", 4, 2, 128, 32),
+                                                 ("f32", 12, 2, 64, 16), ("bf16", 40, 2, 64, 16)])
+def test_weights_of_rows_that_are_left_out_stay(dtype, hq, hkv, d, page):
+    """Rows on a page number out of range are not attended: their entries keep what they hold."""
+    lengths = [3 * page + 2, 700, 6 * page, 0]
+    cfg = config(hq, hkv, d, dtype=dtype, max_seqs=4)
+    c = Pages(cfg, dtype, page, lengths, seed=8)
+    c.table[0, 1] = -1
+    c.table[1, 0] = 10 ** 6
+    c.table[1, 300 // page] = c.k.shape[0]
+    c.table[2, :] = -5                                      # nothing of this one is there
+    g = torch.Generator(device="cuda").manual_seed(2)
+    q = torch.randn(4, hq, d, device="cuda", generator=g).to(DT[dtype])
+    before = torch.rand(c.weights().shape, device="cuda", generator=g)
+    for with_in in (True, False):
+        w, kept = before.clone(), before + 3.0
+        if with_in:
+            run_decode(c, q, [0, 1, 2, 3], weights_in=w, weights_out=w)
+            other = kept.clone()
+            run_decode(c, q, [0, 1, 2, 3], weights_in=before, weights_out=other)
+        else:
+            run_decode(c, q, [0, 1, 2, 3], weights_out=w)
+            other = None
+        for slot in range(4):
+            _, _, there = c.rows(slot)
+            out = np.ones(c.width * page, dtype=bool)
+            out[there] = False
+            np.testing.assert_array_equal(f64(w)[slot][:, out], f64(before)[slot][:, out])
+            if other is not None:
+                np.testing.assert_array_equal(f64(other)[slot][:, out], f64(kept)[slot][:, out])
+        start = before if with_in else torch.zeros_like(before)
+        inside = torch.zeros(w.shape, dtype=torch.bool, device="cuda")
+        for slot in range(4):
+            inside[slot, :, torch.from_numpy(c.rows(slot)[2]).cuda()] = True
+        got = torch.where(inside, w, start)
+        check_decode(c, run_decode(c, q, [0, 1, 2, 3]), q, [0, 1, 2, 3], dtype, weights=got, weights_before=start)
+    assert c.bits() == B.SNAP_DEV_BAD_PAGE
+
+
+@pytest.mark.parametrize("dtype,hq,d,page", [("bf16", 4, 128, 16), ("f32", 2, 128, 16), ("f32", 8, 64, 16)])
+def test_a_row_of_logit_minus_infinity_is_attended(dtype, hq, d, page):
+    """... with weight zero: its entry is written (the old weight, or zero), unlike one that is left out.  A sequence whose every
+    logit is -infinity gets zeros, and its weights are written too."""
+    cfg = config(hq, 1, d, dtype=dtype, max_seqs=2)
+    c = Pages(cfg, dtype, page, [40, 7], seed=8)
+    big = 3e38
+    q = torch.full((2, hq, d), 2.0, device="cuda").to(DT[dtype])
+    c.k[int(c.table[0, 1]), 0, 3] = -big                    # row 19: the sum of its products overflows
+    c.k[int(c.table[1, 0]), 0] = -big
+    before = torch.rand(c.weights().shape, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+    w = before.clone()
+    out = run_decode(c, q, [0, 1], weights_in=before, weights_out=w)
+    np.testing.assert_array_equal(f64(w)[1], f64(before)[1])
+    assert f64(w)[0, 0, 19] == f64(before)[0, 0, 19] and (f64(out)[1] == 0).all() and np.isfinite(f64(out)).all()
+    run_decode(c, q, [0, 1], weights_out=w)
+    want = f64(before)
+    assert f64(w)[0, 0, 19] == 0 and (f64(w)[1, 0, :7] == 0).all()
+    np.testing.assert_array_equal(f64(w)[1, 0, 7:], want[1, 0, 7:])
+    assert c.bits() == 0
 
 
 # ---------------------------------------------------------------------------------------------------------------
