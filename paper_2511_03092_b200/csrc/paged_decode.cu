@@ -1176,7 +1176,7 @@ __device__ __forceinline__ void join_weights(const PagedArgs& a, int id, int per
           const float2 ml = a.ml_part[(long long)piece_at(p, k) * a.gb + mine];
           if (ml.y == 0.f) continue;                                       // a piece without rows
           const float nm = fmaxf(m, ml.x);
-          l = (m == -INFINITY ? 0.f : l * exp2f(m - nm)) + ml.y * exp2f(ml.x - nm);
+          l = (l == 0.f ? 0.f : l * exp2f(m - nm)) + ml.y * exp2f(ml.x - nm);   // (a NaN stays, also of a piece with no other maximum)
           m = nm;
         }
       }

@@ -147,6 +147,23 @@ def test_a_row_of_logit_minus_infinity_is_attended(dtype, hq, d, page):
     assert c.bits() == 0
 
 
+@pytest.mark.parametrize("dtype,hq,d", [("bf16", 4, 128), ("f32", 4, 128), ("f32", 16, 64)])
+def test_weights_carry_a_nan_whatever_piece_it_is_in(dtype, hq, d):
+    """One sequence cut into several hundred pieces, the first rows NaN, up to the whole first piece: the outputs and all weights of
+    their KV head are NaN."""
+    n, page = 50000, 16
+    cfg = config(hq, 1, d, dtype=dtype, max_seqs=1)
+    c = Pages(cfg, dtype, page, [n], seed=4)
+    q = torch.randn(1, hq, d, device="cuda", generator=torch.Generator(device="cuda").manual_seed(3)).to(DT[dtype])
+    for p in range(10):
+        for half in (slice(0, 8), slice(8, 16)):
+            c.k[int(c.table[0, p]), :, half] = float("nan")
+            w = c.weights()
+            out = run_decode(c, q, [0], weights_out=w)
+            assert np.isnan(f64(out)).all() and np.isnan(f64(w)[0, 0, :n]).all(), (p, half)
+    assert c.bits() == 0
+
+
 # ---------------------------------------------------------------------------------------------------------------
 # everything above under the checked build
 # ---------------------------------------------------------------------------------------------------------------
