@@ -525,8 +525,9 @@ int snap_paged_append(const snap_config_t* cfg, const snap_paged_t* paged,
  *             one call must then be distinct: of a slot that is listed again only the first entry's weights
  *             count (SNAP_DEV_BAD_SLOT).  At most 2048 query heads per KV head (SNAP_ERR_UNSUPPORTED).
  * A NaN or an infinity among the rows a token attends makes the outputs it enters non-finite, which of the two is not
- * specified (in single precision a finite number above 3.402e38 may count as infinite); rows that are left out, and what lies behind a sequence's last row, may hold anything.  A token whose every
- * logit is -infinity gets zeros.
+ * specified (in single precision a key or query above 3.402e38 may count as infinite); rows that are left out, and what lies
+ * behind a sequence's last row, may hold anything.  A token whose every logit is -infinity gets zeros; a sequence of one row
+ * returns its value row, bit for bit.
  * The rows of all sequences are split evenly over the GPU whatever their lengths and joined in a fixed order:
  * equal inputs give equal bits.
  * Scratch: snap_paged_decode_workspace_bytes(cfg, paged, n_active, with_weights); calls that can overlap on the

@@ -23,9 +23,12 @@
 // product as two bf16 numbers (p and what its rounding left), which keeps their rounding out of the result: 2^-17
 // instead of 2^-9 a row.
 //
-// In single precision it multiplies with m16n8k8 on numbers split in two: three products, together within 2^-20 of the
-// exact one, less than summing a few dozen of them in single precision may lose.  Groups of up to four wide heads are
-// faster on the portable kernel.
+// In single precision it multiplies with m16n8k8 on numbers split into parts of 11 bits.  Keys, queries and probabilities have
+// two (off by 2^-23 at most; the exponential is good to 2^-22) and a logit's product is three, together within 2^-20 of the exact one,
+// less than summing a few dozen of them in single precision may lose.  Values have three parts and lose nothing: with two, a
+// sequence of one row did not return its value row, at 1 to 7 % less time (8 sequences of 2000 to 6000 rows, 64 dims, 4 KV heads,
+// groups of 1, 4, 16: 20.3 / 20.7, 21.3 / 21.6, 27.0 / 28.0 us; 128 dims, 8, 16: 35.3 / 36.2, 45.7 / 48.5; 256 dims, 8: 68.7 / 72.9).
+// Groups of up to four wide heads are faster on the portable kernel.
 //
 // Portable kernel: the same pipelines per warp over tiles of 8 KB, brought in through tensor maps or by a bulk copy per
 // row; a lane holds four dims of a row.  Four rows at a time, the 4 x heads partial dot products are reduced by halving
@@ -345,7 +348,8 @@ template <typename T, int D, int NWARP, int NSTAGE, int NG> struct MmaShape {
 
 // A single-precision number as two of the tensor cores' 11 bits: x = hi + lo within 2^-21 of x, hi rounded and lo cut off.
 // (In integer arithmetic: with the conversion instruction, which has a fraction of its rate, 8 sequences of 2000 to 6000
-// rows and 8 heads on each of 4 took 40.6 us instead of 35.3.)  A NaN leaves one part NaN at least; above 2^128 (1 - 2^-12) x counts as infinite.
+// rows and 8 heads on each of 4 took 40.6 us instead of 35.3, both with values in two parts.)  A NaN leaves one part NaN at least; above
+// 2^128 (1 - 2^-12) x counts as infinite.
 struct Tf32 { uint32_t hi, lo; };
 __device__ __forceinline__ Tf32 tf32_of(float x) {
   Tf32 t;
@@ -358,8 +362,26 @@ __device__ __forceinline__ void mma1688(float (&c)[4], uint32_t a0, uint32_t a1,
       "mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// A value as three, exactly: x = hi + lo + rest, hi and lo cut off (so that nothing finite becomes infinite).  Outputs are
+// averages of value rows: a row whose weight is 1 comes out as it is.
+struct Tf32x3 { uint32_t hi, lo, rest; };
+__device__ __forceinline__ Tf32x3 tf32x3_of(float x) {
+  Tf32x3 t;
+  t.hi = __float_as_uint(x) & 0xffffe000u;
+  const float r = x - __uint_as_float(t.hi);
+  t.lo = __float_as_uint(r) & 0xffffe000u;
+  t.rest = __float_as_uint(r - __uint_as_float(t.lo));
+  return t;
+}
 // c += a . b in single precision: hi hi + hi lo + lo hi; what is left out is 2^-22 of a product
 __device__ __forceinline__ void mma_3tf32(float (&c)[4], const Tf32* a, const Tf32& b0, const Tf32& b1) {
+  mma1688(c, a[0].lo, a[1].lo, a[2].lo, a[3].lo, b0.hi, b1.hi);
+  mma1688(c, a[0].hi, a[1].hi, a[2].hi, a[3].hi, b0.lo, b1.lo);
+  mma1688(c, a[0].hi, a[1].hi, a[2].hi, a[3].hi, b0.hi, b1.hi);
+}
+// ... with a exact; lo lo, 2^-21 of a product, is left out
+__device__ __forceinline__ void mma_3tf32(float (&c)[4], const Tf32x3* a, const Tf32& b0, const Tf32& b1) {
+  mma1688(c, a[0].rest, a[1].rest, a[2].rest, a[3].rest, b0.hi, b1.hi);
   mma1688(c, a[0].lo, a[1].lo, a[2].lo, a[3].lo, b0.hi, b1.hi);
   mma1688(c, a[0].hi, a[1].hi, a[2].hi, a[3].hi, b0.lo, b1.lo);
   mma1688(c, a[0].hi, a[1].hi, a[2].hi, a[3].hi, b0.hi, b1.hi);
@@ -689,8 +711,8 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
 #pragma unroll
           for (int r8 = 0; r8 < 2; ++r8) {
             const int r = 8 * r8 + 2 * tq;
-            const auto val = [&](int row, int chunk) { return tf32_of(*reinterpret_cast<const float*>(sv + swz(row, chunk))); };
-            const Tf32 vx[4] = {val(r, c), val(r, c + 2), val(r + 1, c), val(r + 1, c + 2)};
+            const auto val = [&](int row, int chunk) { return tf32x3_of(*reinterpret_cast<const float*>(sv + swz(row, chunk))); };
+            const Tf32x3 vx[4] = {val(r, c), val(r, c + 2), val(r + 1, c), val(r + 1, c + 2)};
 #pragma unroll
             for (int gi = 0; gi < NG; ++gi) mma_3tf32(oacc[gi][db], vx, pb[gi][r8][0], pb[gi][r8][1]);
           }
@@ -1432,9 +1454,9 @@ int logits_of(int gb) { return gb <= 2 ? gb : (gb + 3) / 4 * 4; }
 
 int paged_decode_plan(int dtype, const Shape& s, const PageMap& m, int n_active, bool weights, int sms, PagedDecodePlan* p) {
   // Single precision: on the tensor cores a group of any size costs the same, but a tile's numbers have to be split.  8
-  // sequences of 2000 to 6000 rows, 4 KV heads, portable against tensor cores in us: 64 dims, groups of 1, 4, 16: 26.9 / 20.2,
-  // 33.5 / 21.4, 66.4 / 27.2; 128 dims, 1, 4, 8, 16: 29.3 / 33.5, 33.1 / 34.1, 38.9 / 35.3, 66.9 / 45.2; 256 dims, 4, 8: 52.0 /
-  // 68.0, 79.7 / 69.5.
+  // sequences of 2000 to 6000 rows, 4 KV heads, portable against tensor cores in us: 64 dims, groups of 1, 4, 16: 26.9 / 20.7,
+  // 33.5 / 21.6, 66.4 / 28.0; 128 dims, 1, 4, 8, 16: 29.2 / 34.5, 32.8 / 35.1, 38.9 / 36.1, 66.9 / 48.5; 256 dims, 4, 8: 50.6 /
+  // 71.9, 79.7 / 72.9.
   p->mma = dtype == SNAP_BF16 || s.g > 4 || (s.d_qk <= 64 && s.d_v <= 64);
   const bool wide = s.d_qk > 128 || s.d_v > 128;
   const int most = p->mma ? (dtype == SNAP_F32 && wide ? 8 : 16) : 4;     // heads of a unit

@@ -164,6 +164,23 @@ def test_weights_carry_a_nan_whatever_piece_it_is_in(dtype, hq, d):
     assert c.bits() == 0
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hkv,d,dv,page", [(4, 2, 64, 64, 16), (8, 1, 128, 128, 16), (24, 2, 128, 128, 16), (9, 1, 256, 256, 8), (4, 2, 128, 128, 16),
+                                              (2, 1, 256, 256, 16), (5, 1, 80, 48, 5), (16, 2, 64, 64, 1)])
+def test_a_sequence_of_one_row_returns_its_value_row(hq, hkv, d, dv, page, dtype):
+    """Its softmax weight is 1, so nothing is to be rounded: the output holds the value row's bits, the largest finite numbers among them."""
+    cfg = config(hq, hkv, d, dv, dtype, max_seqs=3)
+    c = Pages(cfg, dtype, page, [1, 1, 1], seed=12)
+    top = torch.finfo(DT[dtype]).max
+    c.v[int(c.table[1, 0]), :, 0, :4] = torch.tensor([top, -top, top * 0.75, 1e-30], device="cuda").to(DT[dtype])
+    q = torch.randn(3, hq, d, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)).to(DT[dtype])
+    out = run_decode(c, q, [2, 0, 1])
+    for i, slot in enumerate((2, 0, 1)):
+        want = c.v[int(c.table[slot, 0]), :, 0].repeat_interleave(hq // hkv, dim=0)
+        assert torch.equal(out[i], want)
+    assert c.bits() == 0
+
+
 # ---------------------------------------------------------------------------------------------------------------
 # everything above under the checked build
 # ---------------------------------------------------------------------------------------------------------------
