@@ -438,7 +438,17 @@ def _refuse(where: str, *named) -> None:
     raise ValueError(f"{where}: a tensor is missing, or the pages' strides are not those of the description")
 
 
+def _tokens(where: str, name: str, t) -> int:
+    """Length of the list whose entries are the call's tokens."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{where}: {name} is a {type(t).__name__}, not a tensor")
+    if t.dim() != 1:
+        raise ValueError(f"{where}: {name} has shape {tuple(t.shape)}, expected one dim")
+    return t.shape[0]
+
+
 def _answer(status: Optional[int], where: str, named) -> None:
+    """Raise for a call's status; None: a tensor was turned down (only then are the arguments looked at)."""
     if status is None:
         _refuse(where, *named())
     _check(status, where)
@@ -472,11 +482,12 @@ def snap_rope(cfg: SnapConfig, rope: SnapRope, freqs, positions, q=None, k=None,
     native, entry = _native or _calls()
     status = native.rope(entry["snap_rope"], cfg, rope, freqs, positions, q, k, q_out, k_out, 1 if inverse else 0, _handle(stream))
     if status != 0:
-        n, dt = positions.shape[0], _DTYPES.get(cfg.dtype)
-        sq, sk = (n, cfg.n_q_heads, cfg.d_qk), (n, cfg.n_kv_heads, cfg.d_qk)
-        _answer(status, "snap_rope", lambda: (
-            ("freqs", freqs, _F64, (rope.rot_dim // 2,), True), ("positions", positions, _I32, (n,), True), ("q", q, dt, sq, False),
-            ("k", k, dt, sk, False), ("q_out", q_out, dt, sq, False), ("k_out", k_out, dt, sk, False)))
+        def named():
+            n, dt = _tokens("snap_rope", "positions", positions), _DTYPES.get(cfg.dtype)
+            sq, sk = (n, cfg.n_q_heads, cfg.d_qk), (n, cfg.n_kv_heads, cfg.d_qk)
+            return (("freqs", freqs, _F64, (rope.rot_dim // 2,), True), ("positions", positions, _I32, (n,), True), ("q", q, dt, sq, False),
+                    ("k", k, dt, sk, False), ("q_out", q_out, dt, sq, False), ("k_out", k_out, dt, sk, False))
+        _answer(status, "snap_rope", named)
 
 
 def make_paged(k_pages, v_pages, page_table) -> SnapPaged:
@@ -509,14 +520,15 @@ def snap_paged_append(cfg: SnapConfig, paged: SnapPaged, slot_ids_dev, rows_dev,
     status_code = native.paged_append(entry["snap_paged_append"], cfg, paged, slot_ids_dev, rows_dev, k, v, k_pages, v_pages, page_table,
                                       seq_len, rope, freqs, positions, q, q_out, k_out, weights, status, _handle(stream))
     if status_code != 0:
-        n, dt, hkv = slot_ids_dev.shape[0], _DTYPES.get(cfg.dtype), cfg.n_kv_heads
-        sq, sk, sv, one = (n, cfg.n_q_heads, cfg.d_qk), (n, hkv, cfg.d_qk), (n, hkv, cfg.d_v), (n,)
-        _answer(status_code, "snap_paged_append", lambda: (
-            ("slot_ids", slot_ids_dev, _I32, one, True), ("rows", rows_dev, _I32, one, True),
-            ("freqs", freqs, _F64, None if rope is None else (rope.rot_dim // 2,), True), ("positions", positions, _I32, one, True),
-            ("q", q, dt, sq, False), ("q_out", q_out, dt, sq, True), ("k", k, dt, sk, False), ("k_out", k_out, dt, sk, True),
-            ("v", v, dt, sv, False), ("weights", weights, _F32, _weights_shape(cfg, paged), True),
-            *_paged_named(cfg, paged, dt, k_pages, v_pages, page_table, seq_len, status)))
+        def named():
+            n, dt, hkv = _tokens("snap_paged_append", "slot_ids", slot_ids_dev), _DTYPES.get(cfg.dtype), cfg.n_kv_heads
+            sq, sk, sv, one = (n, cfg.n_q_heads, cfg.d_qk), (n, hkv, cfg.d_qk), (n, hkv, cfg.d_v), (n,)
+            return (("slot_ids", slot_ids_dev, _I32, one, True), ("rows", rows_dev, _I32, one, True),
+                    ("freqs", freqs, _F64, None if rope is None else (rope.rot_dim // 2,), True), ("positions", positions, _I32, one, True),
+                    ("q", q, dt, sq, False), ("q_out", q_out, dt, sq, True), ("k", k, dt, sk, False), ("k_out", k_out, dt, sk, True),
+                    ("v", v, dt, sv, False), ("weights", weights, _F32, _weights_shape(cfg, paged), True),
+                    *_paged_named(cfg, paged, dt, k_pages, v_pages, page_table, seq_len, status))
+        _answer(status_code, "snap_paged_append", named)
 
 
 def snap_paged_decode_workspace_bytes(cfg: SnapConfig, paged: SnapPaged, n_active: int, with_weights: bool = False) -> int:
@@ -534,12 +546,13 @@ def snap_paged_decode_attn(cfg: SnapConfig, paged: SnapPaged, q, slot_ids_dev, n
     status_code = native.paged_decode_attn(entry["snap_paged_decode_attn"], cfg, paged, q, slot_ids_dev, n_active, k_pages, v_pages,
                                            page_table, seq_len, out, workspace, weights_in, weights_out, status, _handle(stream))
     if status_code != 0:
-        n, dt, sw = int(n_active), _DTYPES.get(cfg.dtype), _weights_shape(cfg, paged)
-        _answer(status_code, "snap_paged_decode_attn", lambda: (
-            ("q", q, dt, (n, cfg.n_q_heads, cfg.d_qk), True), ("out", out, dt, (n, cfg.n_q_heads, cfg.d_v), True),
-            ("slot_ids", slot_ids_dev, _I32, (n,), True), ("weights_in", weights_in, _F32, sw, True),
-            ("weights_out", weights_out, _F32, sw, True), ("workspace", workspace, None, None, True),
-            *_paged_named(cfg, paged, dt, k_pages, v_pages, page_table, seq_len, status)))
+        def named():
+            n, dt, sw = int(n_active), _DTYPES.get(cfg.dtype), _weights_shape(cfg, paged)
+            return (("q", q, dt, (n, cfg.n_q_heads, cfg.d_qk), True), ("out", out, dt, (n, cfg.n_q_heads, cfg.d_v), True),
+                    ("slot_ids", slot_ids_dev, _I32, (n,), True), ("weights_in", weights_in, _F32, sw, True),
+                    ("weights_out", weights_out, _F32, sw, True), ("workspace", workspace, None, None, True),
+                    *_paged_named(cfg, paged, dt, k_pages, v_pages, page_table, seq_len, status))
+        _answer(status_code, "snap_paged_decode_attn", named)
 
 
 def snap_paged_evict_workspace_bytes(cfg: SnapConfig, paged: SnapPaged, n_seqs: int) -> int:
@@ -557,10 +570,11 @@ def snap_paged_evict(cfg: SnapConfig, paged: SnapPaged, src_slots_dev, dst_slots
     status_code = native.paged_evict(entry["snap_paged_evict"], cfg, paged, src_slots_dev, dst_slots_dev, n_seqs, k_pages, v_pages,
                                      page_table, seq_len, weights_in, weights_out, workspace, kept_rows, status, _handle(stream))
     if status_code != 0:
-        n, dt, sw = int(n_seqs), _DTYPES.get(cfg.dtype), _weights_shape(cfg, paged)
-        _answer(status_code, "snap_paged_evict", lambda: (
-            ("src_slots", src_slots_dev, _I32, (n,), True), ("dst_slots", dst_slots_dev, _I32, (n,), True),
-            ("weights_in", weights_in, _F32, sw, True), ("weights_out", weights_out, _F32, sw, True),
-            ("kept_rows", kept_rows, _I32, (n, cfg.n_kv_heads, cfg.l_sink + cfg.topk + cfg.l_recent), True),
-            ("workspace", workspace, None, None, True),
-            *_paged_named(cfg, paged, dt, k_pages, v_pages, page_table, seq_len, status)))
+        def named():
+            n, dt, sw = int(n_seqs), _DTYPES.get(cfg.dtype), _weights_shape(cfg, paged)
+            return (("src_slots", src_slots_dev, _I32, (n,), True), ("dst_slots", dst_slots_dev, _I32, (n,), True),
+                    ("weights_in", weights_in, _F32, sw, True), ("weights_out", weights_out, _F32, sw, True),
+                    ("kept_rows", kept_rows, _I32, (n, cfg.n_kv_heads, cfg.l_sink + cfg.topk + cfg.l_recent), True),
+                    ("workspace", workspace, None, None, True),
+                    *_paged_named(cfg, paged, dt, k_pages, v_pages, page_table, seq_len, status))
+        _answer(status_code, "snap_paged_evict", named)

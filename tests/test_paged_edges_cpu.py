@@ -1,0 +1,46 @@
+"""Rotary and paged-cache calls without a GPU: what the Python calls say of arguments that are not what they should be."""
+import pytest
+import torch
+
+from paper_2511_03092_b200 import binding as B
+from paper_2511_03092_b200 import build as snap_build
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    snap_build.build()
+
+
+def _layer():
+    cfg = B.make_config(n_q_heads=4, n_kv_heads=2, d_qk=64, d_v=64, dtype=B.SNAP_BF16, l_sink=1, l_recent=4, topk=8, l_obs=1, pool_kernel=1,
+                        softmax_scale=0.125, max_seqs=3)
+    k = torch.zeros(10, 2, 16, 64, dtype=torch.bfloat16)
+    table = torch.zeros(3, 5, dtype=torch.int32)
+    return cfg, k, table, B.make_paged(k, k, table)
+
+
+def i32(*shape, device="cpu"):
+    return torch.zeros(*shape, dtype=torch.int32, device=device)
+
+
+@pytest.mark.parametrize("bad,error,word", [(None, TypeError, "NoneType"), ([0, 1], TypeError, "list"), (i32(()), ValueError, "one dim"),
+                                            (i32(2, 1), ValueError, "one dim")])
+def test_what_counts_the_tokens_is_named_when_it_is_not_a_list_of_them(bad, error, word):
+    cfg, k, table, paged = _layer()
+    q = torch.zeros(2, 4, 64, dtype=torch.bfloat16)
+    with pytest.raises(error, match=f"snap_rope: positions .*{word}"):
+        B.snap_rope(cfg, B.make_rope(rot_dim=64), torch.zeros(32, dtype=torch.float64), bad, q=q, q_out=q)
+    with pytest.raises(error, match=f"snap_paged_append: slot_ids .*{word}"):
+        B.snap_paged_append(cfg, paged, bad, None, k[0], k[0], k, k, table, i32(3))
+
+
+def test_the_library_s_own_answer_comes_first():
+    """A status that the call itself returned is raised as such, whatever else is wrong with the arguments."""
+    cfg, k, table, paged = _layer()
+    for call in (lambda: B.snap_rope(None, B.make_rope(rot_dim=64), None, None), lambda: B.snap_rope(cfg, None, None, None),
+                 lambda: B.snap_paged_append(None, paged, None, None, None, None, k, k, table, None),
+                 lambda: B.snap_paged_decode_attn(cfg, None, None, None, 2, k, k, table, None, None, None),
+                 lambda: B.snap_paged_evict(None, paged, None, None, 2, k, k, table, None, None, None, None)):
+        with pytest.raises(B.SnapError) as e:
+            call()
+        assert e.value.code == -4
