@@ -438,13 +438,19 @@ def _refuse(where: str, *named) -> None:
     raise ValueError(f"{where}: a tensor is missing, or the pages' strides are not those of the description")
 
 
+def _count(where: str, name: str, n) -> int:
+    if int(n) >= 2 ** 31:
+        raise ValueError(f"{where}: {name} counts {int(n)}, at most 2^31 - 1")
+    return int(n)
+
+
 def _tokens(where: str, name: str, t) -> int:
     """Length of the list whose entries are the call's tokens."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{where}: {name} is a {type(t).__name__}, not a tensor")
     if t.dim() != 1:
         raise ValueError(f"{where}: {name} has shape {tuple(t.shape)}, expected one dim")
-    return t.shape[0]
+    return _count(where, name, t.shape[0])
 
 
 def _answer(status: Optional[int], where: str, named) -> None:
@@ -547,7 +553,7 @@ def snap_paged_decode_attn(cfg: SnapConfig, paged: SnapPaged, q, slot_ids_dev, n
                                            page_table, seq_len, out, workspace, weights_in, weights_out, status, _handle(stream))
     if status_code != 0:
         def named():
-            n, dt, sw = int(n_active), _DTYPES.get(cfg.dtype), _weights_shape(cfg, paged)
+            n, dt, sw = _count("snap_paged_decode_attn", "n_active", n_active), _DTYPES.get(cfg.dtype), _weights_shape(cfg, paged)
             return (("q", q, dt, (n, cfg.n_q_heads, cfg.d_qk), True), ("out", out, dt, (n, cfg.n_q_heads, cfg.d_v), True),
                     ("slot_ids", slot_ids_dev, _I32, (n,), True), ("weights_in", weights_in, _F32, sw, True),
                     ("weights_out", weights_out, _F32, sw, True), ("workspace", workspace, None, None, True),
@@ -571,7 +577,7 @@ def snap_paged_evict(cfg: SnapConfig, paged: SnapPaged, src_slots_dev, dst_slots
                                      page_table, seq_len, weights_in, weights_out, workspace, kept_rows, status, _handle(stream))
     if status_code != 0:
         def named():
-            n, dt, sw = int(n_seqs), _DTYPES.get(cfg.dtype), _weights_shape(cfg, paged)
+            n, dt, sw = _count("snap_paged_evict", "n_seqs", n_seqs), _DTYPES.get(cfg.dtype), _weights_shape(cfg, paged)
             return (("src_slots", src_slots_dev, _I32, (n,), True), ("dst_slots", dst_slots_dev, _I32, (n,), True),
                     ("weights_in", weights_in, _F32, sw, True), ("weights_out", weights_out, _F32, sw, True),
                     ("kept_rows", kept_rows, _I32, (n, cfg.n_kv_heads, cfg.l_sink + cfg.topk + cfg.l_recent), True),

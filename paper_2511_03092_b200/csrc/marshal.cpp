@@ -126,9 +126,14 @@ void* scratch(Call& c, int i, size_t& bytes) {
   bytes = c.good ? t->nbytes() : 0;
   return c.good ? t->data_ptr() : nullptr;
 }
+// Counts are passed on as 32-bit integers.
+int64_t countable(Call& c, int64_t n) {
+  c.good = c.good && n <= INT32_MAX;
+  return n;
+}
 int64_t length(Call& c, int i) {
   const Tensor* t = c.at(i);
-  if (t && t->dim() == 1) return t->size(0);
+  if (t && t->dim() == 1) return countable(c, t->size(0));
   c.good = false;
   return 0;
 }
@@ -200,7 +205,7 @@ PyObject* paged_decode_attn(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   if (!fn || !cfg.ok || !p.ok) return PyErr_Occurred() ? nullptr : (PyErr_SetString(PyExc_TypeError, "no entry point"), nullptr);
   if (!cfg.p || !p.p) return PyLong_FromLong(SNAP_ERR_NULL_POINTER);
   Call c{a};
-  const int64_t n = PyLong_AsLong(a[5]), hq = cfg.p->n_q_heads;
+  const int64_t n = countable(c, PyLong_AsLong(a[5])), hq = cfg.p->n_q_heads;
   const at::ScalarType t = type_of(cfg.p);
   const PagedParts pp = paged_parts(c, cfg.p, p.p, 6, 7, 8, 9, 14);
   size_t bytes;
@@ -226,7 +231,7 @@ PyObject* paged_evict(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   if (!fn || !cfg.ok || !p.ok) return PyErr_Occurred() ? nullptr : (PyErr_SetString(PyExc_TypeError, "no entry point"), nullptr);
   if (!cfg.p || !p.p) return PyLong_FromLong(SNAP_ERR_NULL_POINTER);
   Call c{a};
-  const int64_t n = PyLong_AsLong(a[5]);
+  const int64_t n = countable(c, PyLong_AsLong(a[5]));
   const PagedParts pp = paged_parts(c, cfg.p, p.p, 6, 7, 8, 9, 14);
   size_t bytes;
   const int32_t* src = ints(c, 3, n);

@@ -24,7 +24,8 @@ def i32(*shape, device="cpu"):
 
 
 @pytest.mark.parametrize("bad,error,word", [(None, TypeError, "NoneType"), ([0, 1], TypeError, "list"), (i32(()), ValueError, "one dim"),
-                                            (i32(2, 1), ValueError, "one dim")])
+                                            (i32(2, 1), ValueError, "one dim"), (i32(2 ** 31, device="meta"), ValueError, "at most"),
+                                            (i32(2 ** 32, device="meta"), ValueError, "at most")])
 def test_what_counts_the_tokens_is_named_when_it_is_not_a_list_of_them(bad, error, word):
     cfg, k, table, paged = _layer()
     q = torch.zeros(2, 4, 64, dtype=torch.bfloat16)
@@ -32,6 +33,17 @@ def test_what_counts_the_tokens_is_named_when_it_is_not_a_list_of_them(bad, erro
         B.snap_rope(cfg, B.make_rope(rot_dim=64), torch.zeros(32, dtype=torch.float64), bad, q=q, q_out=q)
     with pytest.raises(error, match=f"snap_paged_append: slot_ids .*{word}"):
         B.snap_paged_append(cfg, paged, bad, None, k[0], k[0], k, k, table, i32(3))
+
+
+@pytest.mark.parametrize("n", [2 ** 31, 2 ** 32 + 2, -1])
+def test_counts_that_the_library_cannot_take_are_refused(n):
+    cfg, k, table, paged = _layer()
+    q, ws = torch.zeros(2, 4, 64, dtype=torch.bfloat16), i32(4)
+    word = "at most" if n > 0 else "shape"
+    with pytest.raises(ValueError, match=word):
+        B.snap_paged_decode_attn(cfg, paged, q, i32(2), n, k, k, table, i32(3), q, ws)
+    with pytest.raises(ValueError, match=word):
+        B.snap_paged_evict(cfg, paged, i32(2), i32(2), n, k, k, table, i32(3), torch.zeros(3, 2, 80), None, ws)
 
 
 def test_the_library_s_own_answer_comes_first():
