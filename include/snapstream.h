@@ -438,7 +438,7 @@ typedef struct snap_rope_config {
 int snap_rope_table(const snap_rope_config_t* rope, double* freqs_host, double* magnitude_host);
 
 /*
- * Rotates the queries and / or keys of n_tokens tokens; token t is at positions_dev[t].
+ * Rotates the queries and / or keys of n_tokens tokens (at most 2^31 - 256); token t is at positions_dev[t].
  *   q_dev, q_out_dev  element (t, h, c) at [t * token_stride + h * head_stride + c], Hq heads; k_dev, k_out_dev
  *             alike with Hkv heads.  q_dev and q_out_dev, or k_dev and k_out_dev, may both be NULL.
  *             An output may be its own input (same pointer and strides); any other overlap is not allowed.
@@ -485,7 +485,7 @@ typedef struct snap_paged {
 } snap_paged_t;
 
 /*
- * Writes the K/V rows of n_tokens new tokens, rotating the keys (and queries) on the way when rope is given.
+ * Writes the K/V rows of n_tokens new tokens (at most 2^31 - 256), rotating the keys (and queries) on the way when rope is given.
  *   slot_ids_dev [n_tokens] int32: the slot of each token's sequence; -1 = padding, nothing of that token is
  *             read or written
  *   rows_dev  [n_tokens] int32: the row each token is written to; afterwards seq_len[slot] is at least row + 1.

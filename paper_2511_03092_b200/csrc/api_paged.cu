@@ -7,6 +7,7 @@
 namespace snap {
 namespace {
 
+constexpr int kMaxTokens = INT_MAX - 255;      // a block of the rotary pass has 256 tokens at most: the last one's numbers stay within 32 bits
 constexpr double kTwoPi = 6.283185307179586;
 
 // The fields the kernels use: snap_rope_table checks the rest.
@@ -125,7 +126,7 @@ int snap_rope(const snap_config_t* cfg, const snap_rope_config_t* rope, const do
   if (rc != SNAP_OK) return rc;
   rc = check_rope(rope);
   if (rc != SNAP_OK) return rc;
-  if (rope->rot_dim > cfg->d_qk - rope->rot_offset || n_tokens < 0 || (inverse != 0 && inverse != 1)) return SNAP_ERR_INVALID_ARG;
+  if (rope->rot_dim > cfg->d_qk - rope->rot_offset || n_tokens < 0 || n_tokens > kMaxTokens || (inverse != 0 && inverse != 1)) return SNAP_ERR_INVALID_ARG;
   if (n_tokens == 0) return SNAP_OK;
   if (!freqs_dev || !positions_dev || !q_dev != !q_out_dev || !k_dev != !k_out_dev || (!q_dev && !k_dev)) return SNAP_ERR_NULL_POINTER;
   if (misaligned(q_dev, q_out_dev, k_dev, k_out_dev)) return SNAP_ERR_INVALID_ARG;
@@ -164,7 +165,7 @@ int snap_paged_append(const snap_config_t* cfg, const snap_paged_t* paged,
     if (rc != SNAP_OK) return rc;
     if (rope->rot_dim > cfg->d_qk - rope->rot_offset) return SNAP_ERR_INVALID_ARG;
   }
-  if (n_tokens < 0 || (!rows_dev && n_tokens > 65536)) return SNAP_ERR_INVALID_ARG;   // (each token looks for its slot among those before it)
+  if (n_tokens < 0 || n_tokens > kMaxTokens || (!rows_dev && n_tokens > 65536)) return SNAP_ERR_INVALID_ARG;   // (each token looks for its slot among those before it)
   if (n_tokens == 0) return SNAP_OK;
   if (!slot_ids_dev || !k_dev || !v_dev || !k_pages_dev || !v_pages_dev || !page_table_dev || !seq_len_dev || (rope && !freqs_dev) ||
       !q_dev != !q_out_dev)

@@ -1,4 +1,6 @@
 """Rotary and paged-cache calls without a GPU: what the Python calls say of arguments that are not what they should be."""
+import ctypes as C
+
 import pytest
 import torch
 
@@ -56,3 +58,13 @@ def test_the_library_s_own_answer_comes_first():
         with pytest.raises(B.SnapError) as e:
             call()
         assert e.value.code == -4
+
+
+def test_more_tokens_than_a_grid_can_number_are_refused():
+    """The last block's spare threads number tokens past the last one: in 32 bits, up to 255 of them."""
+    cfg, _, _, paged = _layer()
+    lib, one, rope = B.lib(), C.c_void_p(256), B.make_rope(rot_dim=64)
+    for n in (2 ** 31 - 1, 2 ** 31 - 255):
+        assert lib.snap_rope(C.byref(cfg), C.byref(rope), one, one, n, one, 256, 64, one, 256, 64, None, 0, 0, None, 0, 0, 0, None) == -1
+        assert lib.snap_paged_append(C.byref(cfg), C.byref(paged), one, one, n, None, None, None, None, 0, 0, None, one, 128, 64, None, one,
+                                     128, 64, one, one, one, one, None, None, None) == -1
