@@ -403,6 +403,8 @@ def _calls():
             from . import _marshal
         except ImportError as e:
             raise RuntimeError(f"the module _marshal is missing ({e}): run `python -m paper_2511_03092_b200.build`") from e
+        if getattr(_marshal, "torch_version", "") != str(torch.__version__):
+            raise RuntimeError(f"the module _marshal is not built for torch {torch.__version__}: run `python -m paper_2511_03092_b200.build`")
         _native = (_marshal, {name: C.cast(getattr(L, name), C.c_void_p).value
                               for name in ("snap_rope", "snap_paged_append", "snap_paged_decode_attn", "snap_paged_evict")})
     return _native

@@ -4,8 +4,10 @@
 
 Each csrc/*.cu is compiled to an object under csrc/build/ (in parallel, only when its
 sources are newer) and the objects are linked into paper_2511_03092_b200/libsnapstream.so.
-csrc/marshal.cpp becomes paper_2511_03092_b200/_marshal.so, the module that passes torch tensors to the
-rotary and paged-cache entry points (built against the installed torch; it knows the library only by address).
+csrc/marshal.cpp becomes the extension module paper_2511_03092_b200/_marshal, which passes torch tensors to the
+rotary and paged-cache entry points (it knows the library only by address).  It is built for one interpreter and one
+torch: the file carries the interpreter's tag, the module the torch version, and either one's change builds it anew.
+Without torch the library alone is built.
 nvcc cross-compiles, so this works on a machine without a GPU.
 --debug-bounds builds the checked variant instead (-DSNAP_DEBUG_BOUNDS: data-dependent indices are
 tested and a bad one raises a status bit instead of an access; objects under csrc/build_dbg/) as
@@ -14,10 +16,12 @@ libsnapstream_dbg.so; the binding loads it when SNAP_LIBRARY names it.
 from __future__ import annotations
 
 import glob
+import importlib.util
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -25,7 +29,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(CSRC, "build")
 LIB = os.path.join(PKG, "libsnapstream.so")
-MARSHAL = os.path.join(PKG, "_marshal.so")
+MARSHAL = os.path.join(PKG, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
 
 ARCH = ["-gencode", "arch=compute_100a,code=sm_100a"]
 COMMON = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC",
@@ -43,21 +47,32 @@ def _newest(paths) -> float:
     return max(os.path.getmtime(p) for p in paths)
 
 
+def _built_for(path: str) -> str:
+    """The torch version that a built module names, '' where there is none."""
+    mark = b"built for torch "
+    try:
+        with open(path, "rb") as f:
+            data = f.read()
+    except OSError:
+        return ""
+    at = data.find(mark)
+    return data[at + len(mark):data.index(b"\0", at)].decode() if at >= 0 else ""
+
+
 def build_marshal(force: bool = False, verbose: bool = False) -> str:
-    import sysconfig
     import torch
     src = os.path.join(CSRC, "marshal.cpp")
     torch_dir = os.path.dirname(torch.__file__)
     newest = _newest([src, os.path.join(ROOT, "include", "snapstream.h"), os.path.join(torch_dir, "version.py")])
-    if not force and os.path.exists(MARSHAL) and os.path.getmtime(MARSHAL) >= newest:
+    if not force and _built_for(MARSHAL) == str(torch.__version__) and os.path.getmtime(MARSHAL) >= newest:
         return MARSHAL
     cuda = os.path.dirname(os.path.dirname(os.path.realpath(_nvcc())))
     inc = [os.path.join(torch_dir, "include"), os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"),
            sysconfig.get_paths()["include"], os.path.join(cuda, "include"), os.path.join(ROOT, "include")]
     lib = os.path.join(torch_dir, "lib")
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
-           *[f"-isystem{d}" for d in inc[:-1]], "-I", inc[-1], src, "-o", MARSHAL, "-L", lib, "-lc10", "-lc10_cuda", "-ltorch_cpu",
-           "-ltorch_python", f"-Wl,-rpath,{lib}"]
+           f'-DBUILT_FOR_TORCH="{torch.__version__}"', *[f"-isystem{d}" for d in inc[:-1]], "-I", inc[-1], src, "-o", MARSHAL, "-L", lib,
+           "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python", f"-Wl,-rpath,{lib}"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if verbose or r.returncode != 0:
         sys.stderr.write(" ".join(cmd) + "\n" + r.stdout + r.stderr)
@@ -105,7 +120,10 @@ def build(force: bool = False, verbose: bool = False, debug_bounds: bool = False
         if r.returncode != 0:
             sys.stderr.write(r.stdout + r.stderr)
             raise RuntimeError("link failed")
-    build_marshal(force and not debug_bounds, verbose)
+    if importlib.util.find_spec("torch") is None:
+        sys.stderr.write("torch is not installed: the library is built without the module that passes tensors to it\n")
+    else:
+        build_marshal(force and not debug_bounds, verbose)
     return lib
 
 

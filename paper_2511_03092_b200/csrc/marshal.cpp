@@ -274,4 +274,14 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "Argument marshalling o
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__marshal() { return PyModule_Create(&module); }
+#ifndef BUILT_FOR_TORCH
+#define BUILT_FOR_TORCH "unknown"
+#endif
+// Tensors are read through torch's own classes, so the module fits one torch only; the build looks for this line in the file.
+const char built_for[] = "built for torch " BUILT_FOR_TORCH;
+
+PyMODINIT_FUNC PyInit__marshal() {
+  PyObject* m = PyModule_Create(&module);
+  if (m && PyModule_AddStringConstant(m, "torch_version", built_for + sizeof("built for torch ") - 1) != 0) { Py_DECREF(m); return nullptr; }
+  return m;
+}

@@ -1,5 +1,6 @@
 """Rotary and paged-cache calls without a GPU: what the Python calls say of arguments that are not what they should be."""
 import ctypes as C
+import os
 
 import pytest
 import torch
@@ -68,3 +69,32 @@ def test_more_tokens_than_a_grid_can_number_are_refused():
         assert lib.snap_rope(C.byref(cfg), C.byref(rope), one, one, n, one, 256, 64, one, 256, 64, None, 0, 0, None, 0, 0, 0, None) == -1
         assert lib.snap_paged_append(C.byref(cfg), C.byref(paged), one, one, n, None, None, None, None, 0, 0, None, one, 128, 64, None, one,
                                      128, 64, one, one, one, one, None, None, None) == -1
+
+
+def test_the_module_belongs_to_its_interpreter_and_torch(monkeypatch, tmp_path):
+    """_marshal is rebuilt for another torch even when the file is newer, and a stale one is refused, not used."""
+    import sysconfig
+    assert os.path.basename(snap_build.MARSHAL) == "_marshal" + sysconfig.get_config_var("EXT_SUFFIX")
+    from paper_2511_03092_b200 import _marshal
+    assert os.path.samefile(_marshal.__file__, snap_build.MARSHAL) and _marshal.torch_version == torch.__version__
+    ran = []
+
+    class Done:
+        returncode, stdout, stderr = 0, "", ""
+    monkeypatch.setattr(snap_build.subprocess, "run", lambda cmd, **kw: ran.append(cmd) or Done)
+    snap_build.build_marshal()
+    assert not ran                                          # up to date
+    monkeypatch.setattr(torch, "__version__", "0.0.1")
+    snap_build.build_marshal()
+    assert len(ran) == 1 and '-DBUILT_FOR_TORCH="0.0.1"' in ran[0]
+    monkeypatch.setattr(B, "_native", None)
+    cfg, *_ = _layer()
+    with pytest.raises(RuntimeError, match="not built for torch 0.0.1"):
+        B.snap_rope(cfg, B.make_rope(rot_dim=64), torch.zeros(32, dtype=torch.float64), i32(2))
+
+
+def test_the_library_builds_without_torch(monkeypatch, capsys):
+    monkeypatch.setattr(snap_build.importlib.util, "find_spec", lambda name: None)
+    monkeypatch.setattr(snap_build, "build_marshal", lambda *a: pytest.fail("the module needs torch"))
+    assert snap_build.build() == snap_build.LIB
+    assert "torch is not installed" in capsys.readouterr().err
