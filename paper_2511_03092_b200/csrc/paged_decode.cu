@@ -293,6 +293,7 @@ template <typename T, int NT, int NBUF>
 __device__ __forceinline__ void write_segment(const PagedArgs& a, const float* buf, int ld, int buf_stride, const float* M, const float* L,
                                               int e, int u, int nh, bool whole, int piece) {
   const int tid = threadIdx.x, d4 = a.d_v / 4;
+  if (!index_ok(e, a.n, a.status) || !index_ok(u, a.U, a.status) || !(whole || index_ok(piece, 2LL * a.ctas, a.status))) return;
   const int kvh = u / a.nhb, hb = u - kvh * a.nhb;
   T* out = static_cast<T*>(a.out) + ((long long)e * a.Hq + kvh * a.g + hb * a.gb) * a.d_v;
   float* part = a.o_part + (long long)piece * a.gb * a.d_v;
@@ -453,7 +454,7 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
         const int pg = row / a.map.page;
         row_of = row - pg * a.map.page;
         kvh_of = pr.u / a.nhb;
-        pid = a.map.table[(long long)pr.slot * a.map.max_pages + pg];
+        if (index_ok(pg, a.map.max_pages, a.status)) pid = a.map.table[(long long)pr.slot * a.map.max_pages + pg];
         if (pid < 0) pid = a.map.n_pages;                                // (bad, not absent)
       }
       return;
@@ -461,12 +462,12 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
     if (valid && pr.len > 0) {
       const int* table = a.map.table + (long long)pr.slot * a.map.max_pages;
       const int row = pr.t * TR, pg = row / a.map.page;
-      pid = table[pg];
+      pid = index_ok(pg, a.map.max_pages, a.status) ? table[pg] : -1;
       row_of = row - pg * a.map.page;
       kvh_of = pr.u / a.nhb;
       if (halves) {
         const int pg_hi = (row + TR / 2) / a.map.page;
-        pid_hi = row + TR / 2 < pr.len ? table[pg_hi] : 0;               // (no row there: any page will do)
+        pid_hi = row + TR / 2 < pr.len && index_ok(pg_hi, a.map.max_pages, a.status) ? table[pg_hi] : 0;   // (no row there: any page will do)
         row_hi = row + TR / 2 - pg_hi * a.map.page;
       }
     }
@@ -653,7 +654,7 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
 #pragma unroll
           for (int r8 = 0; r8 < 2; ++r8) {
             const int row = row0 + gq + 8 * r8;
-            if (row >= at.len) continue;                                 // (a bad page's rows are written: as -inf)
+            if (row >= at.len || !index_ok(row, a.map.cap, a.status)) continue;   // (a bad page's rows are written: as -inf)
             float* sp = srow + (long long)row * a.gs + col;
             if (a.gs % 2 == 0 && col < nh) *reinterpret_cast<float2*>(sp) = make_float2(v[gi][2 * r8], v[gi][2 * r8 + 1]);   // (nh may end between them)
             else {
@@ -887,7 +888,7 @@ __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_cons
     if (valid && row < pr.len) {
       const int pg = row / a.map.page;
       prow = row - pg * a.map.page;
-      pid = a.map.table[(long long)pr.slot * a.map.max_pages + pg];
+      if (index_ok(pg, a.map.max_pages, a.status)) pid = a.map.table[(long long)pr.slot * a.map.max_pages + pg];
       kvh_of = pr.u / a.nhb;
     }
   };
@@ -1013,7 +1014,7 @@ __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_cons
         // rows that are not there hold anything
         const float v = (there >> (lane >> 3)) & 1u ? s[0] * a.scale_log2 : -INFINITY;
         const int row = row0 + r0 + (lane >> 3);
-        if (srow && row < at.len && my_head < nh) srow[(long long)row * a.gs + my_head] = v;   // (lanes of one pair write the same)
+        if (srow && row < at.len && my_head < nh && index_ok(row, a.map.cap, a.status)) srow[(long long)row * a.gs + my_head] = v;   // (lanes of one pair write the same)
         if (__any_sync(0xffffffffu, v > m_ref + 8.f)) {                    // the reference moves lazily, as in the kernel above
           float mx = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
@@ -1195,6 +1196,7 @@ __device__ __forceinline__ void join_weights(const PagedArgs& a, int id, int per
       } else {
 #pragma unroll 4
         for (int k = k0; k < p.np; k += npar) {
+          if (!index_ok(piece_at(p, k), 2LL * a.ctas, a.status)) continue;
           const float2 ml = a.ml_part[(long long)piece_at(p, k) * a.gb + mine];
           if (ml.y == 0.f) continue;                                       // a piece without rows
           const float nm = fmaxf(m, ml.x);
@@ -1258,7 +1260,7 @@ __device__ __forceinline__ void join_weights(const PagedArgs& a, int id, int per
 #pragma unroll
     for (int j = 0; j < R; ++j) {
       const int row = row0 + j * JNT + tid;
-      if (!stays[j]) a.w_out[base + row] = old[j] + sum[j];
+      if (!stays[j] && index_ok(row, a.map.cap, a.status)) a.w_out[base + row] = old[j] + sum[j];
       old[j] = old_ahead[j];
     }
     row0 = next;
@@ -1345,13 +1347,14 @@ __global__ void __launch_bounds__(JNT, 3) paged_join_kernel(const __grid_constan
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
           const int k = k0 + y * (JNT / 32);
+          const bool there = k < p.np && index_ok(piece_at(p, k), 2LL * a.ctas, a.status);
           ml[y] = make_float2(-INFINITY, 0.f);
-          if (k < p.np) ml[y] = a.ml_part[(long long)piece_at(p, k) * a.gb + col];
-          const float* o = a.o_part + ((long long)piece_at(p, k < p.np ? k : 0) * a.gb + col) * a.d_v + 4 * lane;
+          if (there) ml[y] = a.ml_part[(long long)piece_at(p, k) * a.gb + col];
+          const float* o = a.o_part + ((long long)piece_at(p, there ? k : 0) * a.gb + col) * a.d_v + 4 * lane;
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             v[y][j] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (k < p.np && 4 * lane + 128 * j < a.d_v) v[y][j] = *reinterpret_cast<const float4*>(o + 128 * j);
+            if (there && 4 * lane + 128 * j < a.d_v) v[y][j] = *reinterpret_cast<const float4*>(o + 128 * j);
           }
         }
         const float nm = fmaxf(fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)), m);

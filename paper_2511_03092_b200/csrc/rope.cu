@@ -79,7 +79,8 @@ __global__ void __launch_bounds__(NT, 5) rope_kernel(const __grid_constant__ Rop
       if (row < 0 || row >= a.map.cap) { skip = true; bad = SNAP_DEV_BAD_PAGE; }
       else {
         off = row % a.map.page;
-        page = a.map.table[(long long)slot * a.map.max_pages + row / a.map.page];
+        if (!index_ok(row / a.map.page, a.map.max_pages, a.status)) page = -1;
+        else page = a.map.table[(long long)slot * a.map.max_pages + row / a.map.page];
         if (page < 0 || page >= a.map.n_pages) { skip = true; bad = SNAP_DEV_BAD_PAGE; }
       }
     }
@@ -227,7 +228,7 @@ __global__ void __launch_bounds__(NT, 5) rope_kernel(const __grid_constant__ Rop
     }
   }
   if (paged) {
-    if (a.weights && x == 0)
+    if (a.weights && x == 0 && index_ok(row, a.map.cap, a.status))
       for (int h = y; h < a.Hkv; h += L.Y) a.weights[((long long)slot * a.Hkv + h) * a.map.cap + row] = 0.f;
   }
 }

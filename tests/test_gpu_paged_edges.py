@@ -182,9 +182,11 @@ def test_a_sequence_of_one_row_returns_its_value_row(hq, hkv, d, dv, page, dtype
 
 
 # ---------------------------------------------------------------------------------------------------------------
-# everything above under the checked build
+# under the checked build
 # ---------------------------------------------------------------------------------------------------------------
-def test_these_calls_under_the_checked_build():
+@pytest.mark.parametrize("which", [["tests/test_gpu_paged_edges.py"], ["tests/test_gpu_paged.py", "-k", "decode"]], ids=["these", "attention"])
+def test_paged_calls_under_the_checked_build(which):
+    """The calls of this file, and attention: units, pieces, pages, logit rows and weights are tested against their arrays."""
     import os
     import subprocess
     import sys
@@ -194,7 +196,7 @@ def test_these_calls_under_the_checked_build():
     lib = snap_build.build(debug_bounds=True)
     env = dict(os.environ, SNAP_LIBRARY=os.path.basename(lib))
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
-    r = subprocess.run([sys.executable, "-m", "pytest", "tests/test_gpu_paged_edges.py", "-m", "gpu", "-q", "-x", "-p", "no:cacheprovider"],
+    r = subprocess.run([sys.executable, "-m", "pytest", *which, "-m", "gpu", "-q", "-x", "-p", "no:cacheprovider"],
                        cwd=root, env=env, capture_output=True, text=True, timeout=900)
     assert r.returncode == 0, r.stdout[-3000:] + r.stderr[-2000:]
     assert " passed" in r.stdout
