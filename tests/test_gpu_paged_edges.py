@@ -8,7 +8,7 @@ import torch
 
 from oracle import paged_oracle as orc
 from paper_2511_03092_b200 import binding as B
-from tests.test_gpu_paged import DT, Pages, check_decode, check_rotation, config, f64, i32, run_decode
+from tests.test_gpu_paged import DT, Pages, check_decode, check_evict, check_rotation, config, f64, i32, run_decode, run_evict
 
 pytestmark = pytest.mark.gpu
 
@@ -179,6 +179,179 @@ def test_a_sequence_of_one_row_returns_its_value_row(hq, hkv, d, dv, page, dtype
         want = c.v[int(c.table[slot, 0]), :, 0].repeat_interleave(hq // hkv, dim=0)
         assert torch.equal(out[i], want)
     assert c.bits() == 0
+
+
+def laid_out(c, how):
+    """The same cache in other memory: keys and values as views of one pool, one tensor heads first and the other rows first,
+    rows with room between them."""
+    pages, hkv, page, dqk, dv = *c.k.shape, c.v.shape[3]
+    empty = lambda *shape: torch.full(shape, float("nan"), dtype=c.k.dtype, device="cuda")  # noqa: E731
+    if how == "one pool":
+        pool = empty(pages, 2, hkv, page, max(dqk, dv))
+        k, v = pool[:, 0, ..., :dqk], pool[:, 1, ..., :dv]
+    elif how == "one pool, rows first":
+        pool = empty(pages, page, 2, hkv, max(dqk, dv))
+        k, v = pool[:, :, 0, :, :dqk].transpose(1, 2), pool[:, :, 1, :, :dv].transpose(1, 2)
+    elif how == "keys heads first, values rows first":
+        k, v = empty(pages, hkv, page, dqk), empty(pages, page, hkv, dv).transpose(1, 2)
+    elif how == "keys rows first, values heads first":
+        k, v = empty(pages, page, hkv, dqk).transpose(1, 2), empty(pages, hkv, page, dv)
+    else:
+        k, v = empty(pages, hkv, page + 1, dqk + 16)[:, :, :page, :dqk], empty(hkv, pages, page, dv + 48)[..., 16:16 + dv].transpose(0, 1)
+    k.copy_(c.k)
+    v.copy_(c.v)
+    c.k, c.v = k, v
+    c.paged = B.make_paged(k, v, c.table)
+
+
+LAYOUTS = ["one pool", "one pool, rows first", "keys heads first, values rows first", "keys rows first, values heads first", "room between"]
+
+
+@pytest.mark.parametrize("how", LAYOUTS)
+@pytest.mark.parametrize("dtype,hq,hkv,d,dv,page", [("bf16", 8, 2, 128, 128, 16), ("f32", 4, 2, 128, 128, 16), ("bf16", 6, 3, 80, 48, 5),
+                                                    ("f32", 12, 2, 64, 64, 24)])
+def test_append_attention_and_eviction_in_other_layouts(dtype, hq, hkv, d, dv, page, how):
+    sink, recent, topk = 2, 20, 33
+    keep, lengths = sink + recent + topk, [300, 40, 55, 56, 1]
+    n = len(lengths)
+    cfg = config(hq, hkv, d, dv, dtype, max_seqs=2 * n, sink=sink, recent=recent, topk=topk)
+    c = Pages(cfg, dtype, page, [x + 2 for x in lengths] + [min(x + 2, keep) for x in lengths], seed=2)
+    laid_out(c, how)
+    c.seq_len.copy_(i32(lengths + [0] * n))
+    g = torch.Generator(device="cuda").manual_seed(4)
+    # two tokens a sequence, rotated into their pages
+    k, v = (torch.randn(2 * n, hkv, x, device="cuda", generator=g).to(DT[dtype]) for x in (d, dv))
+    slots, rows = [i for i in range(n) for _ in range(2)], [x + j for x in lengths for j in range(2)]
+    freqs, rope = orc.rope_table(d, 10000.0), B.make_rope(rot_dim=d)
+    want_k, want_v, k_out = f64(c.k), f64(c.v), torch.empty_like(k)
+    B.snap_paged_append(cfg, c.paged, i32(slots), i32(rows), k, v, c.k, c.v, c.table, c.seq_len, rope=rope, freqs=torch.from_numpy(freqs).cuda(),
+                        k_out=k_out, status=c.status)
+    check_rotation(f64(k_out), f64(k), rows, freqs, d, 0, False, 1.0, False, dtype)
+    table = c.table.cpu().numpy()
+    for i, (s, r) in enumerate(zip(slots, rows)):
+        want_k[table[s, r // page], :, r % page], want_v[table[s, r // page], :, r % page] = f64(k_out)[i], f64(v)[i]
+    np.testing.assert_array_equal(f64(c.k), want_k)
+    np.testing.assert_array_equal(f64(c.v), want_v)
+    c.lengths = [x + 2 for x in lengths] + [0] * n
+    assert c.seq_len.tolist() == c.lengths
+    # a step's attention, with the weights that the eviction goes by
+    q = torch.randn(n, hq, d, device="cuda", generator=g).to(DT[dtype])
+    w = torch.rand(c.weights().shape, device="cuda", generator=g)
+    before, live = w.clone(), list(range(n))
+    out = run_decode(c, q, live, weights_in=w, weights_out=w)
+    check_decode(c, out, q, live, dtype, weights=w, weights_before=before)
+    before, k0, v0 = w.clone(), f64(c.k), f64(c.v)
+    kept = run_evict(c, live, [n + i for i in live], w, w)
+    check_evict(c, live, [n + i for i in live], w, before, kept, k0, v0, set(live))
+    assert c.bits() == 0
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,d", [("f32", 520, 130, 128), ("f32", 136, 34, 256), ("f32", 520, 520, 80), ("bf16", 520, 130, 128),
+                                            ("bf16", 600, 40, 64)])
+def test_cut_units_of_many_heads_are_joined(dtype, hq, hkv, d):
+    """More than 512 query heads in a call: outputs are joined by the borders between the CTAs' stretches."""
+    lengths = [1100, 3, 0, 700]
+    cfg = config(hq, hkv, d, dtype=dtype, max_seqs=len(lengths))
+    c = Pages(cfg, dtype, 16, lengths, seed=9)
+    g = torch.Generator(device="cuda").manual_seed(6)
+    q = torch.randn(4, hq, d, device="cuda", generator=g).to(DT[dtype])
+    before = torch.rand(c.weights().shape, device="cuda", generator=g)
+    w = before.clone()
+    out = run_decode(c, q, [3, 2, 0, 1], weights_in=w, weights_out=w)
+    check_decode(c, out, q, [3, 2, 0, 1], dtype, weights=w, weights_before=before)
+    assert torch.equal(run_decode(c, q, [3, 2, 0, 1]), out) and c.bits() == 0
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,d,n,most", [("bf16", 32, 8, 128, 16, 9000), ("bf16", 12, 12, 64, 45, 333), ("f32", 8, 2, 128, 4, 4100),
+                                                   ("f32", 16, 2, 64, 20, 3000), ("bf16", 8, 2, 128, 150, 500)])
+def test_equal_inputs_give_equal_bits_with_other_calls_between(dtype, hq, hkv, d, n, most):
+    """... nothing waited for between the calls: neither what scratch holds nor how the CTAs of one call follow those of the
+    one before may show."""
+    rng = np.random.default_rng(n)
+    lengths = [int(x) for x in rng.integers(0, most + 1, size=n)]
+    cfg = config(hq, hkv, d, dtype=dtype, max_seqs=n)
+    c = Pages(cfg, dtype, 16, lengths, seed=n)
+    g = torch.Generator(device="cuda").manual_seed(n)
+    qs = [torch.randn(n, hq, d, device="cuda", generator=g).to(DT[dtype]) for _ in range(2)]
+    slots = [i32(rng.permutation(n).tolist()) for _ in range(2)]
+    ws = torch.full((B.snap_paged_decode_workspace_bytes(cfg, c.paged, n, True),), 0xff, dtype=torch.uint8, device="cuda")
+    got = []
+    for rep in range(30):
+        i = int(rep % 3 == 1)
+        out, w = torch.full((n, hq, d), float("nan"), dtype=DT[dtype], device="cuda"), c.weights() if rep % 2 else None
+        B.snap_paged_decode_attn(cfg, c.paged, qs[i], slots[i], n, c.k, c.v, c.table, c.seq_len, out, ws, weights_out=w, status=c.status)
+        got.append((i, out, w))
+    for i in (0, 1):
+        outs, ws_ = [o for j, o, _ in got if j == i], [w for j, _, w in got if j == i and w is not None]
+        assert all(torch.equal(o, outs[0]) for o in outs) and all(torch.equal(w, ws_[0]) for w in ws_)
+    some = [int(x) for x in slots[0][:5]]
+    check_decode(c, got[0][1][:5], qs[0], some, dtype)
+    assert c.bits() == 0
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# offsets past 32 bits
+# ---------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("rot", [128, 64])
+def test_rotation_past_32_bit_offsets(rot):
+    """More than 2^31 elements of queries, apart and in place: the first, middle and last tokens."""
+    t, h, d = 262150, 64, 128
+    cfg = config(h, 1, d)
+    rope, freqs = B.make_rope(rot_dim=rot, rot_offset=d - rot), torch.from_numpy(orc.rope_table(rot, 10000.0)).cuda()
+    q = torch.empty(t, h, d, dtype=torch.bfloat16, device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(1))
+    assert q.numel() > 2 ** 31
+    pos = torch.arange(t, dtype=torch.int32, device="cuda")
+    parts = [slice(0, 7), slice(131069, 131080), slice(t - 9, t)]
+    before = [q[s].clone() for s in parts]
+    out = torch.empty_like(q)
+    B.snap_rope(cfg, rope, freqs, pos, q=q, q_out=out)
+    B.snap_rope(cfg, rope, freqs, pos, q=q, q_out=q)
+    for s, x in zip(parts, before):
+        assert torch.equal(q[s], out[s])
+        check_rotation(f64(out[s]), f64(x), pos[s].cpu().numpy(), freqs.cpu().numpy(), rot, d - rot, False, 1.0, False, "bf16")
+
+
+@pytest.mark.parametrize("dtype,d,pages", [("bf16", 128, 140000), ("f32", 128, 140000)])
+def test_append_and_eviction_past_32_bit_offsets(dtype, d, pages):
+    """Pools of more than 2^31 elements, tokens further apart than that in their own tensors: what a small cache gives."""
+    page, sink, recent, topk, length, hkv = 16, 2, 12, 30, 90, 8
+    cfg = config(hkv, hkv, d, dtype=dtype, max_seqs=2, sink=sink, recent=recent, topk=topk)
+    c = Pages(cfg, dtype, page, [length + 40, 44], seed=1, spare=0)
+    c.lengths = [length, 0]
+    c.seq_len.copy_(i32(c.lengths))
+    small_k, small_v, small_table = c.k.clone(), c.v.clone(), c.table.clone()
+    used = c.k.shape[0]
+    far = torch.tensor([(i * 11939) % pages if i % 2 else pages - 1 - i for i in range(used)], dtype=torch.int32, device="cuda")
+    assert far.unique().numel() == used
+    ks, vs = (torch.empty(pages, hkv, page, d, dtype=DT[dtype], device="cuda") for _ in range(2))
+    assert ks.numel() > 2 ** 31
+    for new, old in ((ks, small_k), (vs, small_v)):
+        new[far.long()] = old
+    table = torch.where(small_table >= 0, far[small_table.clamp(min=0).long()], small_table).to(torch.int32).contiguous()
+    tokens = 40
+    apart = (2 ** 31 // (tokens - 2)) // 64 * 64 + 64       # the last tokens' offsets pass 2^31 elements
+    flat = torch.empty(apart * (tokens - 1) + hkv * d, dtype=DT[dtype], device="cuda")
+    k = flat.as_strided((tokens, hkv, d), (apart, d, 1))
+    k.copy_(torch.randn(tokens, hkv, d, device="cuda", generator=torch.Generator(device="cuda").manual_seed(2)))
+    near = k.contiguous()
+    slots, rows = i32([0] * tokens), i32(list(range(length, length + tokens)))
+    rope, freqs = B.make_rope(rot_dim=d), torch.from_numpy(orc.rope_table(d, 10000.0)).cuda()
+    lens = c.seq_len.clone()
+    B.snap_paged_append(cfg, c.paged, slots, rows, near, near, c.k, c.v, c.table, c.seq_len, rope=rope, freqs=freqs, status=c.status)
+    paged = B.make_paged(ks, vs, table)
+    B.snap_paged_append(cfg, paged, slots, rows, k, k, ks, vs, table, lens, rope=rope, freqs=freqs, status=c.status)
+    assert torch.equal(lens, c.seq_len) and lens.tolist() == [length + tokens, 0]
+    same = lambda: all(torch.equal(x[far.long()].nan_to_num(7.0), y.nan_to_num(7.0)) for x, y in ((ks, c.k), (vs, c.v)))  # noqa: E731
+    assert same()
+    w = torch.rand(c.weights().shape, device="cuda", generator=torch.Generator(device="cuda").manual_seed(3))
+    c.lengths = [length + tokens, 0]
+    before, k0, v0 = w.clone(), f64(c.k), f64(c.v)
+    kept = run_evict(c, [0], [1], w, w)
+    check_evict(c, [0], [1], w, before, kept, k0, v0, {0})
+    other, kept_far = before.clone(), torch.empty_like(kept)
+    ws = torch.empty(B.snap_paged_evict_workspace_bytes(cfg, paged, 1), dtype=torch.uint8, device="cuda")
+    B.snap_paged_evict(cfg, paged, i32([0]), i32([1]), 1, ks, vs, table, lens, other, other, ws, kept_rows=kept_far, status=c.status)
+    assert torch.equal(kept_far, kept) and torch.equal(other, w) and same() and c.bits() == 0
 
 
 # ---------------------------------------------------------------------------------------------------------------
