@@ -289,6 +289,60 @@ def test_equal_inputs_give_equal_bits_with_other_calls_between(dtype, hq, hkv, d
     assert c.bits() == 0
 
 
+def test_evictions_replayed_with_other_slots_and_weights():
+    """A captured eviction, one after the other without a wait: slots, lengths, weights and tables that kernels just before it
+    wrote are the ones it goes by (its copy starts beside its selection, and reads them on every SM)."""
+    n, sink, recent, topk, lengths = 6, 2, 30, 60, [300, 90, 250, 500, 93, 420]
+    keep = sink + recent + topk
+    cfg = config(4, 2, 64, max_seqs=3 * n, sink=sink, recent=recent, topk=topk)
+    c = Pages(cfg, "bf16", 16, lengths + [keep] * (2 * n), seed=3)
+    g = torch.Generator(device="cuda").manual_seed(8)
+    weights = [torch.rand(c.weights().shape, device="cuda", generator=g) for _ in range(2)]
+    plans = [([3, 1, 5, 0, 2, 4], [n + i for i in range(n)]), ([0, 4, 2, 5, 3, 1], [2 * n + i for i in range(n)])]
+    lens = [i32(lengths + [0] * (2 * n)), i32([x - 40 for x in lengths] + [0] * (2 * n))]
+    src, dst, w = i32(plans[0][0]), i32(plans[0][1]), weights[0].clone()
+    kept = torch.full((n, 2, keep), -9, dtype=torch.int32, device="cuda")
+    ws = torch.empty(B.snap_paged_evict_workspace_bytes(cfg, c.paged, n), dtype=torch.uint8, device="cuda")
+    call = lambda: B.snap_paged_evict(cfg, c.paged, src, dst, n, c.k, c.v, c.table, c.seq_len, w, None, ws, kept_rows=kept, status=c.status)  # noqa: E731
+    call()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    ids = [(i32(a), i32(b)) for a, b in plans]
+    inputs = [(ids[r % 2][0], ids[r % 2][1], lens[r // 2 % 2], weights[r // 3 % 2]) for r in range(12)]
+    want = []
+    for a, b, ln, wt in inputs:                             # each of them alone, waited for
+        for to, x in ((src, a), (dst, b), (c.seq_len, ln), (w, wt)):
+            to.copy_(x)
+        torch.cuda.synchronize()
+        call()
+        torch.cuda.synchronize()
+        for i, s in enumerate(a.tolist()):
+            for h in range(2):
+                rows = orc.kept_rows(f64(wt)[s, h], int(ln[s]), sink, recent, topk)
+                assert kept[i, h, :len(rows)].tolist() == rows.tolist()
+        pages = c.table[b.long(), :-(-keep // 16)].long()
+        want.append((kept.clone(), c.seq_len.clone(), c.k[pages], c.v[pages]))
+    got = []
+    for r in range(240):
+        a, b, ln, wt = inputs[r % 12]
+        c.k[c.table[b.long(), :-(-keep // 16)].long()] = 0.0
+        for to, x in ((w, wt), (c.seq_len, ln), (dst, b), (src, a)):      # the last things before the call
+            to.copy_(x)
+        graph.replay() if r % 3 else call()
+        pages = c.table[b.long(), :-(-keep // 16)].long()
+        got.append((kept.clone(), c.seq_len.clone(), c.k[pages], c.v[pages]))
+    for r, x in enumerate(got):
+        for y, z in zip(x[:2], want[r % 12][:2]):
+            assert torch.equal(y, z), r
+        for i in range(n):                                  # (rows past a sequence's last are anything)
+            rows, b = int(x[1][inputs[r % 12][1][i]]), -(-keep // 16)
+            for y, z in zip(x[2:], want[r % 12][2:]):
+                mine, its = (t[i].transpose(1, 2).flatten(0, 1)[:rows] for t in (y, z))
+                assert torch.equal(mine, its), (r, i)
+    assert c.bits() == 0
+
+
 # ---------------------------------------------------------------------------------------------------------------
 # offsets past 32 bits
 # ---------------------------------------------------------------------------------------------------------------
