@@ -521,7 +521,8 @@ int snap_paged_append(const snap_config_t* cfg, const snap_paged_t* paged,
  *   seq_len_dev  need not be the cache's own lengths: with shorter ones the token sees the rows before them
  *   weights_out_dev  NULL, or the weights array: for every row r the token attends,
  *                 weights_out[slot][kvh][r] = weights_in[slot][kvh][r] + sum over the group's heads of its softmax weight
- *             (weights_in_dev NULL = 0; it may be weights_out_dev).  Other entries are left alone.  The slots of
+ *             (weights_in_dev NULL = 0; it may be weights_out_dev).  Other entries are left alone, those of rows that are
+ *             left out among them.  The slots of
  *             one call must then be distinct: of a slot that is listed again only the first entry's weights
  *             count (SNAP_DEV_BAD_SLOT).  At most 2048 query heads per KV head (SNAP_ERR_UNSUPPORTED).
  * A NaN or an infinity among the rows a token attends makes the outputs it enters non-finite, which of the two is not
@@ -529,7 +530,8 @@ int snap_paged_append(const snap_config_t* cfg, const snap_paged_t* paged,
  * behind a sequence's last row, may hold anything.  A token whose every logit is -infinity gets zeros; a sequence of one row
  * returns its value row, bit for bit.
  * The rows of all sequences are split evenly over the GPU whatever their lengths and joined in a fixed order:
- * equal inputs give equal bits.
+ * equal inputs give equal bits.  n_active times the rows that a slot can have must stay below about
+ * 2^33, and times the KV heads below 2^39 (SNAP_ERR_UNSUPPORTED).
  * Scratch: snap_paged_decode_workspace_bytes(cfg, paged, n_active, with_weights); calls that can overlap on the
  * GPU need scratch of their own.
  */

@@ -3,8 +3,8 @@
 //     out[i][h] = sum_r p_r V_r / sum_r p_r,   p_r = exp(scale q.K_r - max),   r over the sequence's rows
 //
 // Every cache row is read once and serves the whole head group, so HBM bounds the call: 16 sequences of 8192 to 65536
-// rows (32 heads on 8, 128 dims, 2.2 GB) take 328 us, 6.7 TB/s.  One sequence of 5124 rows takes 11.8 us for 21 MB, and 45
-// of up to 333 rows 14.5: there the chain of slot, length, page, tile, join is what counts.
+// rows (32 heads on 8, 128 dims, 2.2 GB) take 322 to 328 us, 6.7 TB/s.  One sequence of 5124 rows takes 11.7 to 12.1 us for 21 MB,
+// and 45 of up to 333 rows 14.4 to 15.0: there the chain of slot, length, page, tile, join is what counts.
 //
 // (sequence, KV head, head block) is a unit; its rows are cut into tiles.  The units in a row form one line, each as
 // long as its tiles plus a fixed share for what a unit costs however short it is (its queries, its joining), and the line
@@ -34,7 +34,7 @@
 // row; a lane holds four dims of a row.  Four rows at a time, the 4 x heads partial dot products are reduced by halving
 // exchanges, after which a lane owns one (row, head) pair: one shuffle per pair instead of five, one exponential per lane.
 // (Eight rows at a time need twice the code for the same work; a step of short sequences runs through it once, at the speed
-// at which instructions arrive.)  4 sequences of 2001 to 4100 rows, 8 heads on 2, take 15 us (latency); 28 of 1324 to 2196, 8
+// at which instructions arrive.)  4 sequences of 2001 to 4100 rows, 8 heads on 2, take 15.2 to 16.1 us (latency); 28 of 1324 to 2196, 8
 // on 4, 41.6 us, 74 % of the HBM rate.
 //
 // With weights, the split kernel also stores the logits, and CTAs of the second launch turn them into the group's
@@ -62,6 +62,8 @@ constexpr int UNIT_TILES = 6;                   // what a unit costs besides its
 constexpr int MIN_TILES = 1;                    // a CTA gets at least that much beyond one unit's share (at least one: no stretch is empty)
 // (Measured over 40 calls of all sizes: 4 and 4 take 8 % longer, 8 and 1 2 %, 4 and 1 as long but 4 % longer for many short sequences.)
 constexpr int MAX_CTAS = 1024, MAX_HELD = 128;  // sequences whose slot and length a CTA keeps in shared memory
+// (Held against looked up in the batch's arrays: 17 sequences of up to 400 rows 14.4 / 14.95 us, 45 of 333 14.75 / 15.0, 100 of 500 35.7 /
+// 35.8, 128 of 2000 96.7 / 97.0: the more sequences, the less it is worth.)
 constexpr unsigned kPagedWaitLimit = 1u << 22;
 
 struct PagedArgs {
@@ -1271,7 +1273,8 @@ __device__ __forceinline__ void join_weights(const PagedArgs& a, int id, int per
 // each: the shorter way to the pieces), or, where there are many heads, by the borders between the stretches of the first
 // launch: the unit that a border cuts is joined by the CTAs of the borders that cut it, which take its heads in turn, so
 // that no more CTAs than borders are started however many units there are.  (By heads against by borders: one sequence
-// of 5124 rows, 32 heads 11.4 / 13.1 us a call; 16 sequences, 512 heads 332 / 335; 48 short ones, 1536 heads 25.2 / 22.0.)
+// of 5124 rows, 32 heads 11.9 / 12.9 us a call; 16 of up to 6000 rows, 512 heads 41.9 / 43.7; 24, 768 heads 55.8 / 57.3; 48 of up
+// to 400 rows, 1536 heads 24.6 / 23.3, 20 of them, 640 heads 13.9 / 14.2.)
 //
 // This kernel lets the next one start only when it ends: blocks of the split kernel that start beside blocks of this
 // one get the registers in between them, and once these end the rest of an SM's registers is in pieces too small for

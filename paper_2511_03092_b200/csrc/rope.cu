@@ -10,9 +10,10 @@
 // the cosines and sines of its V pairs (two 16-byte vectors of a head) in registers and walks over the heads of
 // its token; the angles of a token are computed once, by the whole block, and handed over in shared memory.  What
 // counts is how many warps are resident, not how much each has in flight: one head at a time and five blocks per SM
-// turn a 32768-token prompt of 40 heads of 128 dims in 110 us (6.1 TB/s); two heads at a time and four blocks take
-// 113 us, three and three 125, and looping over tokens in as many blocks as fit 124 to 144.  Appending 26003 tokens of
-// the same layer (queries, keys twice, values) takes 121 us (5.7 TB/s).  Threads are laid out as [tokens][heads][items of
+// turn a 32768-token prompt of 40 heads of 128 dims in 110 to 114 us by the GPU (6.1 to 5.9 TB/s); where that took 110,
+// two heads at a time and four blocks took 113 us, three and three 125, and looping over tokens in as many blocks as fit 124 to
+// 144.  Appending 26003 tokens of the same layer (queries, keys twice, values) takes 122 to 126 us (5.7 to 5.5 TB/s).  Threads are
+// laid out as [tokens][heads][items of
 // a head]: consecutive threads are on consecutive vectors, and few tokens spread over more threads per token.
 //
 // The kernel after it starts when this one ends, not beside its last blocks: attention over the pages comes next, whose

@@ -181,6 +181,29 @@ def test_a_sequence_of_one_row_returns_its_value_row(hq, hkv, d, dv, page, dtype
     assert c.bits() == 0
 
 
+@pytest.mark.parametrize("dtype,hq,hkv,d", [("bf16", 4, 2, 128), ("f32", 4, 2, 128), ("f32", 16, 2, 64)])
+@pytest.mark.parametrize("n", [1, 3, 128, 129, 700])
+def test_batches_of_which_nothing_is_there(n, dtype, hq, hkv, d):
+    """Only padding, only empty sequences, both; then one row in the last of them: zeros, but for that one's value row."""
+    cfg = config(hq, hkv, d, dtype=dtype, max_seqs=n)
+    c = Pages(cfg, dtype, 16, [0] * (n - 1) + [1], seed=n)
+    q = torch.randn(n, hq, d, device="cuda").to(DT[dtype])
+    none = torch.zeros(n, dtype=torch.int32, device="cuda")
+    w = c.weights(2.5)
+    for slots, seq_len in (([-1] * n, c.seq_len), (list(range(n)), none), ([i if i % 2 else -1 for i in range(n)], none)):
+        for keep in (None, w):
+            assert (f64(run_decode(c, q, slots, weights_in=keep, weights_out=keep, seq_len=seq_len)) == 0).all()
+    assert (f64(w) == 2.5).all()
+    out = run_decode(c, q, list(range(n)), weights_out=w)
+    assert (f64(out)[:-1] == 0).all()
+    assert torch.equal(out[-1], c.v[int(c.table[n - 1, 0]), :, 0].repeat_interleave(hq // hkv, dim=0))
+    want = np.full(w.shape, 2.5)
+    want[n - 1, :, 0] = hq // hkv
+    # a head's only weight is 1, off by what exp2(x - (x + log2 1)) is: nothing but the logit's rounding, which cancels
+    np.testing.assert_allclose(f64(w), want, rtol=2.0 ** -20)
+    assert c.bits() == 0
+
+
 def laid_out(c, how):
     """The same cache in other memory: keys and values as views of one pool, one tensor heads first and the other rows first,
     rows with room between them."""
