@@ -527,8 +527,8 @@ int snap_paged_append(const snap_config_t* cfg, const snap_paged_t* paged,
  *             count (SNAP_DEV_BAD_SLOT).  At most 2048 query heads per KV head (SNAP_ERR_UNSUPPORTED).
  * A NaN or an infinity among the rows a token attends makes the outputs it enters non-finite, which of the two is not
  * specified (in single precision a key or query above 3.402e38 may count as infinite); rows that are left out, and what lies
- * behind a sequence's last row, may hold anything.  A token whose every logit is -infinity gets zeros; a sequence of one row
- * returns its value row, bit for bit.
+ * behind a sequence's last row, may hold anything.  A token whose every logit is -infinity gets zeros.  A sequence of one
+ * row returns its values unrounded (those of at least 1e-30 in size; a zero may lose its sign).
  * The rows of all sequences are split evenly over the GPU whatever their lengths and joined in a fixed order:
  * equal inputs give equal bits.  n_active times the rows that a slot can have must stay below about
  * 2^33, and times the KV heads below 2^39 (SNAP_ERR_UNSUPPORTED).

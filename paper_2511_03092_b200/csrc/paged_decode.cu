@@ -366,7 +366,7 @@ __device__ __forceinline__ void mma1688(float (&c)[4], uint32_t a0, uint32_t a1,
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 // A value as three, exactly: x = hi + lo + rest, hi and lo cut off (so that nothing finite becomes infinite).  Outputs are
-// averages of value rows: a row whose weight is 1 comes out as it is.
+// averages of value rows: a row whose weight is 1 comes out unrounded.  (Below some 1e-31 the last part leaves the normal numbers.)
 struct Tf32x3 { uint32_t hi, lo, rest; };
 __device__ __forceinline__ Tf32x3 tf32x3_of(float x) {
   Tf32x3 t;
