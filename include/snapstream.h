@@ -24,7 +24,11 @@
  * and, for the uncompressed cache a serving program keeps next to it: snap_rope (rotary positions
  * of queries and keys), snap_paged_append + snap_paged_decode_attn (a cache in pages and the
  * attention of one new token per sequence over it) and snap_paged_evict (cutting a paged cache
- * back to l_sink + topk + l_recent rows by accumulated attention weight).
+ * back to l_sink + topk + l_recent rows by accumulated attention weight); snap_paged_plan (which
+ * pages a step's new tokens go to, decided on the device); and the same cache in 8 bits:
+ * snap_paged_q8_append, snap_paged_q8_decode_attn (one or several tokens per sequence) and
+ * snap_paged_q8_gather (rows back as the dense keys and values that snap_prefill_attn and
+ * snap_compress take).
  *
  * Conventions
  *   - "dev" pointers are CUDA device pointers on the current device, "host" pointers are plain
@@ -92,6 +96,8 @@ typedef enum snap_status {
 
 #define SNAP_DEV_BAD_PAGE 16u       /* paged cache: a page number outside [0, n_pages), or a row or a length past
                                        the page table: those rows were skipped */
+#define SNAP_DEV_NO_ROOM 32u        /* snap_paged_plan: not enough free pages, or no room in the list of tokens: those
+                                       requests were refused */
 
 /* One attention layer's shape and SnapStream hyper-parameters (appendix table
  * "SnapStream Hyperparameters": sink, top-K, recent, observation window, pooling kernel). */
@@ -568,6 +574,126 @@ int snap_paged_evict(const snap_config_t* cfg, const snap_paged_t* paged, const 
                      const int32_t* page_table_dev, int32_t* seq_len_dev, const float* weights_in_dev,
                      float* weights_out_dev, int32_t* kept_rows_dev, void* workspace_dev, size_t workspace_bytes,
                      uint32_t* status_dev, void* cuda_stream);
+
+/*
+ * A step's pages and tokens, decided on the device: which pages the new rows of each sequence go to, and the lists that
+ * snap_paged_append, snap_rope and snap_paged_q8_append take.  Request i is slot slot_ids[i] and n = new_tokens[i]; requests
+ * are served as if one after the other:
+ *   n < 0   the sequence has ended.  Every page that its table row holds (an entry in [0, n_pages)) goes onto the stack of free
+ *           pages, in the row's order; the row becomes -1 and seq_len[slot] 0.  (The pages of all sequences that end go onto
+ *           the stack before any is granted.)
+ *   n >= 0  the sequence, of len = seq_len[slot] rows, is to grow by n.  Missing are those of the entries
+ *           [ceil(len / page_tokens), ceil((len + n) / page_tokens)) of its row that hold no page (others keep the one they hold: one
+ *           set aside before, or granted to tokens that were given up); the k-th page granted in the call is the k-th from the
+ *           stack's top.  Refused, as a whole, is a request whose len + n lies past the page table (SNAP_DEV_BAD_PAGE), or with
+ *           which the tokens wanted so far (its own and those of all requests before it, refused ones as well, but for those
+ *           past the table) exceed n_tokens_max, or, when it misses any, the pages missing so far those that are
+ *           free (SNAP_DEV_NO_ROOM).
+ *   A slot of -1 is padding; a slot out of range or listed before is skipped (SNAP_DEV_BAD_SLOT).
+ *   page_table_in_dev, page_table_out_dev  [max_seqs][max_pages], the same array or two that do not overlap: with two, the rows of the
+ *             slots listed are written whole and the table that a running step reads stays as it is
+ *   seq_len_dev [max_seqs]: read; 0 where the sequence has ended (appending counts the new rows, not this call)
+ *   free_pages_dev [n_pages]: the stack of free pages, its top last; n_free_in_dev, n_free_out_dev [1]: how many it holds before and
+ *             after (the same or two).  Entries are written only from n_free_in on.  More than n_pages: SNAP_DEV_BAD_PAGE, the rest is dropped.
+ *   granted_dev NULL, or [n_seqs]: n of the requests served, 0 of the others
+ *   first_rows_dev [n_seqs]: the row of each request's first new token, seq_len[slot] (0: ended, skipped)
+ *   cu_tokens_dev [n_seqs + 1]: sums of the granted tokens before each request, and of all
+ *   token_slots_dev, token_rows_dev [n_tokens_max]: slot and row of every token granted, request by request; -1 and 0 behind the last
+ * Of paged, only page_tokens, n_pages and max_pages are used; of cfg, max_seqs.  At most 65536 requests.  Sequences that share
+ * pages must not end through this call (a page would go onto the stack twice).
+ * Scratch: snap_paged_plan_workspace_bytes(cfg, paged, n_seqs).
+ */
+int64_t snap_paged_plan_workspace_bytes(const snap_config_t* cfg, const snap_paged_t* paged, int32_t n_seqs);
+int snap_paged_plan(const snap_config_t* cfg, const snap_paged_t* paged, const int32_t* slot_ids_dev,
+                    const int32_t* new_tokens_dev, int32_t n_seqs, const int32_t* page_table_in_dev,
+                    int32_t* page_table_out_dev, int32_t* seq_len_dev, int32_t* free_pages_dev,
+                    const int32_t* n_free_in_dev, int32_t* n_free_out_dev, int32_t n_tokens_max, int32_t* granted_dev,
+                    int32_t* first_rows_dev, int32_t* cu_tokens_dev, int32_t* token_slots_dev, int32_t* token_rows_dev,
+                    void* workspace_dev, size_t workspace_bytes, uint32_t* status_dev, void* cuda_stream);
+
+/*
+ * A cache in pages of 8-bit numbers.  Element c of row o of KV head h of page p is
+ *     e4m3(k_pages_dev[p * k_page_stride + h * k_head_stride + o * k_row_stride + c])
+ *         * k_scales_dev[(p * Hkv + h) * (page_tokens / block_tokens) + o / block_tokens]
+ * (strides in bytes, multiples of 16), V alike: block_tokens consecutive rows of a KV head share a scale, positive and finite.
+ * What the append writes are powers of two: of a floating format a finer scale keeps no more bits, and a number moves to
+ * a larger one unrounded, unless it falls below 2^-6 of it.  Page tables, lengths and slots are those of the cache
+ * in pages above; cfg->dtype is the type of queries, keys, values and outputs.  Heads up to 256 wide, no latent layout.
+ */
+typedef struct snap_paged_q8 {
+  snap_paged_t pages;     /* strides in bytes */
+  int32_t block_tokens;   /* rows that share a scale: a divisor of page_tokens */
+  int32_t reserved;       /* 0 */
+} snap_paged_q8_t;
+
+/*
+ * Writes the K/V rows of new tokens, rotating the keys (and queries) on the way when rope is given.  Entry i adds the tokens
+ * [cu_tokens[i], cu_tokens[i + 1]) to sequence slot_ids[i] as the rows from first_rows[i] on, which then are its last:
+ * seq_len[slot] = first_rows[i] + their number (no tokens: it stays).
+ *   slot_ids_dev [n_seqs]: -1 = padding, nothing of that entry is read or written; a slot out of range, or listed before, is
+ *             skipped (SNAP_DEV_BAD_SLOT).  At most 65536 entries.
+ *   cu_tokens_dev [n_seqs + 1]: must not decrease (not checked).  Tokens from cu_tokens[n_seqs] on are padding, of which nothing is
+ *             read or written; n_tokens (at most 2^31 - 65536) is what there is room for.
+ *   first_rows_dev [n_seqs]: may be less than the sequence's length: rows from there on are given up.  May not be seq_len_dev itself.
+ *   rope, freqs_dev, positions_dev [n_tokens], k_dev, v_dev, k_out_dev, q_dev, q_out_dev: as in snap_paged_append (positions_dev
+ *             NULL: the row; k_out is rounded from the rotated key, not from what the page holds)
+ * The scale of a block is 2^e, e the smallest integer from -126 to 120 with f * max |x| <= 448 * 2^e over the inputs x of the
+ * rows written to it, f = max(1, sqrt(2) magnitude) for keys that are rotated and 1 otherwise (a pair grows by sqrt(2) magnitude
+ * at most); of a block that holds rows of the sequence already, below first_rows, it is no less than before, and where it
+ * grows those rows move to it.  A number is rotated in single precision, divided by the scale and rounded once, to
+ * nearest even; beyond 448 (only past 2^120) it is 448.  NaN stays NaN and does not count for the scale; a block with an infinity has the scale 2^120.
+ * Rows past the page table or on a page number out of range are skipped (SNAP_DEV_BAD_PAGE), their outputs too; so is an
+ * entry with a negative first row, as a whole.  A page that is written may be listed once (not checked).  No workspace.
+ */
+int snap_paged_q8_append(const snap_config_t* cfg, const snap_paged_q8_t* paged,
+                         const int32_t* slot_ids_dev, const int32_t* cu_tokens_dev, const int32_t* first_rows_dev,
+                         int32_t n_seqs, int32_t n_tokens,
+                         const snap_rope_config_t* rope, const double* freqs_dev, const int32_t* positions_dev,
+                         const void* q_dev, int64_t q_token_stride, int64_t q_head_stride, void* q_out_dev,
+                         const void* k_dev, int64_t k_token_stride, int64_t k_head_stride, void* k_out_dev,
+                         const void* v_dev, int64_t v_token_stride, int64_t v_head_stride,
+                         void* k_pages_dev, void* v_pages_dev, float* k_scales_dev, float* v_scales_dev,
+                         const int32_t* page_table_dev, int32_t* seq_len_dev, uint32_t* status_dev, void* cuda_stream);
+
+/*
+ * Attention of the last q_len tokens of each sequence over its pages: with len = seq_len[slot_ids[i]],
+ *     out[i][u][h] = softmax(scale * q[i][u][h] . K^T) V   over rows [0, len - q_len + 1 + u)
+ * of KV head h / (Hq/Hkv): every token sees the rows up to its own.  Nothing is appended.
+ *   q_dev [n_active][q_len][Hq][d_qk], out_dev [n_active][q_len][Hq][d_v], dense; 1 <= q_len <= 1024.  A token that sees no row gets zeros;
+ *             slots, padding, page numbers out of range and lengths as in snap_paged_decode_attn
+ * Numbers enter the products as they are stored; logits, weights and sums are in single precision (bf16 layers: each weight rounded
+ * to 11 bits before it multiplies the values).  A NaN or an infinity among the rows that any of the q_len tokens attends makes
+ * the outputs it enters non-finite; a value row with a NaN among the last q_len may enter the tokens before it too.
+ * Rows that are left out, and what lies behind a sequence's last row, may hold anything, their scales too.
+ * Work is split and joined as in snap_paged_decode_attn: equal inputs give equal bits.
+ * Scratch: snap_paged_q8_decode_workspace_bytes(cfg, paged, n_active, q_len); calls that can overlap on the GPU need scratch
+ * of their own.
+ */
+int64_t snap_paged_q8_decode_workspace_bytes(const snap_config_t* cfg, const snap_paged_q8_t* paged, int32_t n_active,
+                                             int32_t q_len);
+int snap_paged_q8_decode_attn(const snap_config_t* cfg, const snap_paged_q8_t* paged, const void* q_dev,
+                              const int32_t* slot_ids_dev, int32_t n_active, int32_t q_len,
+                              const void* k_pages_dev, const void* v_pages_dev, const float* k_scales_dev,
+                              const float* v_scales_dev, const int32_t* page_table_dev, const int32_t* seq_len_dev,
+                              void* out_dev, void* workspace_dev, size_t workspace_bytes, uint32_t* status_dev,
+                              void* cuda_stream);
+
+/*
+ * The reverse of the append: token cu_tokens[i] + j of k_dev and v_dev receives row first_rows[i] + j of sequence slot_ids[i],
+ * rounded once (bf16: exact, unless the scale leaves its range).  Entries, tokens and padding as in snap_paged_q8_append, but a
+ * slot may be listed any number of times and no length is looked at.
+ *   k_dev, v_dev  (t, h, c) at [t * token_stride + h * head_stride + c], strides multiples of 16 bytes, no head of an
+ *             output may overlap another
+ * Tokens of rows past the page table, or on a page number out of range (SNAP_DEV_BAD_PAGE), are left as they are.  No workspace.
+ */
+int snap_paged_q8_gather(const snap_config_t* cfg, const snap_paged_q8_t* paged,
+                         const int32_t* slot_ids_dev, const int32_t* cu_tokens_dev, const int32_t* first_rows_dev,
+                         int32_t n_seqs, int32_t n_tokens,
+                         const void* k_pages_dev, const void* v_pages_dev, const float* k_scales_dev, const float* v_scales_dev,
+                         const int32_t* page_table_dev,
+                         void* k_dev, int64_t k_token_stride, int64_t k_head_stride,
+                         void* v_dev, int64_t v_token_stride, int64_t v_head_stride,
+                         uint32_t* status_dev, void* cuda_stream);
 
 /*
  * Testing and tuning aids (the paper has no counterpart).  Each option is one non-negative

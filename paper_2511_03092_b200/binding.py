@@ -20,7 +20,7 @@ _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)),
 SNAP_F32, SNAP_BF16 = 0, 1
 SNAP_POOL_AVG, SNAP_POOL_MAX = 0, 1
 SNAP_DEV_BAD_SLOT, SNAP_DEV_WAIT_TIMEOUT, SNAP_DEV_BAND_OVERFLOW, SNAP_DEV_INDEX_CHECK = 1, 2, 4, 8
-SNAP_DEV_BAD_PAGE = 16
+SNAP_DEV_BAD_PAGE, SNAP_DEV_NO_ROOM = 16, 32
 SNAP_ROPE_PLAIN, SNAP_ROPE_LINEAR, SNAP_ROPE_LLAMA3, SNAP_ROPE_YARN = range(4)
 
 
@@ -47,6 +47,10 @@ class SnapPaged(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("page_tokens", "n_pages", "max_pages", "reserved")]
     _fields_ += [(n, C.c_int64) for n in ("k_page_stride", "k_head_stride", "k_row_stride", "v_page_stride", "v_head_stride",
                                           "v_row_stride")]
+
+
+class SnapPagedQ8(C.Structure):
+    _fields_ = [("pages", SnapPaged), ("block_tokens", C.c_int32), ("reserved", C.c_int32)]
 
 
 class SnapError(RuntimeError):
@@ -129,6 +133,20 @@ def lib() -> C.CDLL:
     L.snap_paged_evict_workspace_bytes.argtypes = [pcfg, ppaged, i32]
     L.snap_paged_evict.restype = C.c_int
     L.snap_paged_evict.argtypes = [pcfg, ppaged, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp, vp]
+    pq8 = C.POINTER(SnapPagedQ8)
+    L.snap_paged_plan_workspace_bytes.restype = i64
+    L.snap_paged_plan_workspace_bytes.argtypes = [pcfg, ppaged, i32]
+    L.snap_paged_plan.restype = C.c_int
+    L.snap_paged_plan.argtypes = [pcfg, ppaged, vp, vp, i32] + [vp] * 6 + [i32] + [vp] * 6 + [sz, vp, vp]
+    L.snap_paged_q8_append.restype = C.c_int
+    L.snap_paged_q8_append.argtypes = [pcfg, pq8, vp, vp, vp, i32, i32, prope, vp, vp, vp, i64, i64, vp, vp, i64, i64, vp, vp, i64, i64,
+                                       vp, vp, vp, vp, vp, vp, vp, vp]
+    L.snap_paged_q8_decode_workspace_bytes.restype = i64
+    L.snap_paged_q8_decode_workspace_bytes.argtypes = [pcfg, pq8, i32, i32]
+    L.snap_paged_q8_decode_attn.restype = C.c_int
+    L.snap_paged_q8_decode_attn.argtypes = [pcfg, pq8, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp, vp]
+    L.snap_paged_q8_gather.restype = C.c_int
+    L.snap_paged_q8_gather.argtypes = [pcfg, pq8, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, i64, i64, vp, i64, i64, vp, vp]
     _lib = L
     return L
 
@@ -140,7 +158,9 @@ EXPORTS = ("snap_cache_layout", "snap_compress_workspace_bytes", "snap_decode_wo
            "snap_block_stats_bytes", "snap_block_stats", "snap_block_select", "snap_block_select_workspace_bytes",
            "snap_decode_blocks_workspace_bytes",
            "snap_decode_attn_blocks", "snap_rope_table", "snap_rope", "snap_paged_append", "snap_paged_decode_workspace_bytes",
-           "snap_paged_decode_attn", "snap_paged_evict_workspace_bytes", "snap_paged_evict")
+           "snap_paged_decode_attn", "snap_paged_evict_workspace_bytes", "snap_paged_evict",
+           "snap_paged_plan_workspace_bytes", "snap_paged_plan", "snap_paged_q8_append", "snap_paged_q8_decode_workspace_bytes",
+           "snap_paged_q8_decode_attn", "snap_paged_q8_gather")
 
 # testing / tuning options of snap_debug_set_option
 (SNAP_OPT_SCORE_KERNEL, SNAP_OPT_DECODE_GQA_KERNEL, SNAP_OPT_DECODE_LATENT_KERNEL, SNAP_OPT_DECODE_NSPLIT,
@@ -406,7 +426,8 @@ def _calls():
         if getattr(_marshal, "torch_version", "") != str(torch.__version__):
             raise RuntimeError(f"the module _marshal is not built for torch {torch.__version__}: run `python -m paper_2511_03092_b200.build`")
         _native = (_marshal, {name: C.cast(getattr(L, name), C.c_void_p).value
-                              for name in ("snap_rope", "snap_paged_append", "snap_paged_decode_attn", "snap_paged_evict")})
+                              for name in ("snap_rope", "snap_paged_append", "snap_paged_decode_attn", "snap_paged_evict", "snap_paged_plan",
+                                           "snap_paged_q8_append", "snap_paged_q8_decode_attn", "snap_paged_q8_gather")})
     return _native
 
 
@@ -586,3 +607,137 @@ def snap_paged_evict(cfg: SnapConfig, paged: SnapPaged, src_slots_dev, dst_slots
                     ("workspace", workspace, None, None, True),
                     *_paged_named(cfg, paged, dt, k_pages, v_pages, page_table, seq_len, status))
         _answer(status_code, "snap_paged_evict", named)
+
+
+# --- pages of a step, and the cache in pages of 8-bit numbers ---
+_E4M3 = torch.float8_e4m3fn
+
+
+def make_page_map(page_tokens: int, n_pages: int, page_table) -> SnapPaged:
+    """What snap_paged_plan needs of a cache in pages of any kind: rows of a page, pages of the pool, page_table
+    [max_seqs, max_pages].  (A description by make_paged, or that of make_paged_q8, does as well.)"""
+    if page_table.dim() != 2:
+        raise ValueError("make_page_map: page_table is [seqs, pages]")
+    return SnapPaged(int(page_tokens), int(n_pages), page_table.shape[1], 0, 0, 0, 0, 0, 0, 0)
+
+
+def make_paged_q8(k_pages, v_pages, page_table, block_tokens: int) -> SnapPagedQ8:
+    """Describe a cache in pages of 8-bit numbers: k_pages, v_pages float8_e4m3fn, otherwise as in make_paged; block_tokens
+    rows of a KV head share a scale, k_scales and v_scales being float32 [n_pages, Hkv, page_tokens // block_tokens]."""
+    return SnapPagedQ8(make_paged(k_pages, v_pages, page_table), int(block_tokens), 0)
+
+
+def snap_paged_plan_workspace_bytes(cfg: SnapConfig, paged, n_seqs: int) -> int:
+    pages = paged.pages if isinstance(paged, SnapPagedQ8) else paged
+    n = lib().snap_paged_plan_workspace_bytes(C.byref(cfg), C.byref(pages), int(n_seqs))
+    if n < 0:
+        raise SnapError(int(n), "snap_paged_plan_workspace_bytes")
+    return int(n)
+
+
+def snap_paged_plan(cfg: SnapConfig, paged, slot_ids_dev, new_tokens_dev, page_table, seq_len, free_pages, n_free, first_rows, cu_tokens,
+                    token_slots, token_rows, workspace, page_table_out=None, n_free_out=None, granted=None, status=None,
+                    stream=None) -> None:
+    """Hand out the pages of a step: request i adds new_tokens[i] rows to slot_ids[i], or, negative, ends it.  first_rows [n],
+    cu_tokens [n + 1] and the lists token_slots, token_rows (their length is the room there is) receive what the appends
+    take.  page_table_out, n_free_out None: page_table and n_free [1] are updated in place."""
+    native, entry = _native or _calls()
+    pages = paged.pages if isinstance(paged, SnapPagedQ8) else paged
+    out, free_out = page_table if page_table_out is None else page_table_out, n_free if n_free_out is None else n_free_out
+    status_code = native.paged_plan(entry["snap_paged_plan"], cfg, pages, slot_ids_dev, new_tokens_dev, page_table, out, seq_len, free_pages,
+                                    n_free, free_out, granted, first_rows, cu_tokens, token_slots, token_rows, workspace, status,
+                                    _handle(stream))
+    if status_code != 0:
+        def named():
+            n, most = _tokens("snap_paged_plan", "slot_ids", slot_ids_dev), _tokens("snap_paged_plan", "token_slots", token_slots)
+            one, table = (n,), (cfg.max_seqs, pages.max_pages)
+            return (("slot_ids", slot_ids_dev, _I32, one, True), ("new_tokens", new_tokens_dev, _I32, one, True),
+                    ("page_table", page_table, _I32, table, True), ("page_table_out", out, _I32, table, True),
+                    ("seq_len", seq_len, _I32, (cfg.max_seqs,), True), ("free_pages", free_pages, _I32, (pages.n_pages,), True),
+                    ("n_free", n_free, _I32, (1,), True), ("n_free_out", free_out, _I32, (1,), True), ("granted", granted, _I32, one, True),
+                    ("first_rows", first_rows, _I32, one, True), ("cu_tokens", cu_tokens, _I32, (n + 1,), True),
+                    ("token_slots", token_slots, _I32, (most,), True), ("token_rows", token_rows, _I32, (most,), True),
+                    ("workspace", workspace, None, None, True), ("status", status, _I32, None, True))
+        _answer(status_code, "snap_paged_plan", named)
+
+
+def _q8_named(cfg, paged, k_pages, v_pages, k_scales, v_scales, page_table, status):
+    p = paged.pages
+    head = (p.n_pages, cfg.n_kv_heads, p.page_tokens)
+    scales = (p.n_pages, cfg.n_kv_heads, p.page_tokens // paged.block_tokens if paged.block_tokens > 0 else 0)
+    return (("k_pages", k_pages, _E4M3, head + (cfg.d_qk,), False), ("v_pages", v_pages, _E4M3, head + (cfg.d_v,), False),
+            ("k_scales", k_scales, _F32, scales, True), ("v_scales", v_scales, _F32, scales, True),
+            ("page_table", page_table, _I32, (cfg.max_seqs, p.max_pages), True), ("status", status, _I32, None, True))
+
+
+def _entries_named(where, slot_ids_dev, cu_tokens, first_rows, k):
+    """The lists of an append or gather, and its number of tokens."""
+    n = _tokens(where, "slot_ids", slot_ids_dev)
+    if not isinstance(k, torch.Tensor) or k.dim() != 3:
+        raise ValueError(f"{where}: k is [tokens, heads, dim]")
+    return (("slot_ids", slot_ids_dev, _I32, (n,), True), ("cu_tokens", cu_tokens, _I32, (n + 1,), True),
+            ("first_rows", first_rows, _I32, (n,), True)), _count(where, "k", k.shape[0])
+
+
+def snap_paged_q8_append(cfg: SnapConfig, paged: SnapPagedQ8, slot_ids_dev, cu_tokens, first_rows, k, v, k_pages, v_pages, k_scales,
+                         v_scales, page_table, seq_len, rope: Optional[SnapRope] = None, freqs=None, positions=None, q=None, q_out=None,
+                         k_out=None, status=None, stream=None) -> None:
+    """Write tokens [cu_tokens[i], cu_tokens[i + 1]) of k [T, Hkv, d_qk], v [T, Hkv, d_v] into the pages of slot_ids[i], from row
+    first_rows[i] on, rotated when rope is given and quantised; q -> q_out and k_out: the rotated queries and keys, dense."""
+    native, entry = _native or _calls()
+    status_code = native.paged_q8_append(entry["snap_paged_q8_append"], cfg, paged, slot_ids_dev, cu_tokens, first_rows, k, v, k_pages, v_pages,
+                                         k_scales, v_scales, page_table, seq_len, rope, freqs, positions, q, q_out, k_out, status,
+                                         _handle(stream))
+    if status_code != 0:
+        def named():
+            lists, t = _entries_named("snap_paged_q8_append", slot_ids_dev, cu_tokens, first_rows, k)
+            dt, hkv = _DTYPES.get(cfg.dtype), cfg.n_kv_heads
+            sq, sk, sv = (t, cfg.n_q_heads, cfg.d_qk), (t, hkv, cfg.d_qk), (t, hkv, cfg.d_v)
+            return (*lists, ("freqs", freqs, _F64, None if rope is None else (rope.rot_dim // 2,), True), ("positions", positions, _I32, (t,), True),
+                    ("q", q, dt, sq, False), ("q_out", q_out, dt, sq, True), ("k", k, dt, sk, False), ("k_out", k_out, dt, sk, True),
+                    ("v", v, dt, sv, False), ("seq_len", seq_len, _I32, (cfg.max_seqs,), True),
+                    *_q8_named(cfg, paged, k_pages, v_pages, k_scales, v_scales, page_table, status))
+        _answer(status_code, "snap_paged_q8_append", named)
+
+
+def snap_paged_q8_decode_workspace_bytes(cfg: SnapConfig, paged: SnapPagedQ8, n_active: int, q_len: int = 1) -> int:
+    n = lib().snap_paged_q8_decode_workspace_bytes(C.byref(cfg), C.byref(paged), int(n_active), int(q_len))
+    if n < 0:
+        raise SnapError(int(n), "snap_paged_q8_decode_workspace_bytes")
+    return int(n)
+
+
+def snap_paged_q8_decode_attn(cfg: SnapConfig, paged: SnapPagedQ8, q, slot_ids_dev, k_pages, v_pages, k_scales, v_scales, page_table, seq_len,
+                              out, workspace, status=None, stream=None) -> None:
+    """Attention of the last tokens of each sequence, q [n, q_len, Hq, d_qk] (or [n, Hq, d_qk] of one) -> out alike with d_v, over
+    the rows in its pages: each token sees those up to its own."""
+    native, entry = _native or _calls()
+    if not isinstance(q, torch.Tensor) or q.dim() not in (3, 4):
+        raise ValueError("snap_paged_q8_decode_attn: q is [sequences, tokens, heads, dim]")
+    n, q_len = q.shape[0], q.shape[1] if q.dim() == 4 else 1
+    status_code = native.paged_q8_decode_attn(entry["snap_paged_q8_decode_attn"], cfg, paged, q, slot_ids_dev, n, q_len, k_pages, v_pages,
+                                              k_scales, v_scales, page_table, seq_len, out, workspace, status, _handle(stream))
+    if status_code != 0:
+        def named():
+            dt, head = _DTYPES.get(cfg.dtype), (*q.shape[:-2], cfg.n_q_heads)
+            _count("snap_paged_q8_decode_attn", "q", n)
+            return (("q", q, dt, (*head, cfg.d_qk), True), ("out", out, dt, (*head, cfg.d_v), True), ("slot_ids", slot_ids_dev, _I32, (n,), True),
+                    ("seq_len", seq_len, _I32, (cfg.max_seqs,), True), ("workspace", workspace, None, None, True),
+                    *_q8_named(cfg, paged, k_pages, v_pages, k_scales, v_scales, page_table, status))
+        _answer(status_code, "snap_paged_q8_decode_attn", named)
+
+
+def snap_paged_q8_gather(cfg: SnapConfig, paged: SnapPagedQ8, slot_ids_dev, cu_tokens, first_rows, k_pages, v_pages, k_scales, v_scales,
+                         page_table, k, v, status=None, stream=None) -> None:
+    """Read rows back: tokens [cu_tokens[i], cu_tokens[i + 1]) of k [T, Hkv, d_qk], v [T, Hkv, d_v] (any strides with a dense
+    last dim) receive the rows of slot_ids[i] from first_rows[i] on."""
+    native, entry = _native or _calls()
+    status_code = native.paged_q8_gather(entry["snap_paged_q8_gather"], cfg, paged, slot_ids_dev, cu_tokens, first_rows, k_pages, v_pages, k_scales,
+                                         v_scales, page_table, k, v, status, _handle(stream))
+    if status_code != 0:
+        def named():
+            lists, t = _entries_named("snap_paged_q8_gather", slot_ids_dev, cu_tokens, first_rows, k)
+            dt, hkv = _DTYPES.get(cfg.dtype), cfg.n_kv_heads
+            return (*lists, ("k", k, dt, (t, hkv, cfg.d_qk), False), ("v", v, dt, (t, hkv, cfg.d_v), False),
+                    *_q8_named(cfg, paged, k_pages, v_pages, k_scales, v_scales, page_table, status))
+        _answer(status_code, "snap_paged_q8_gather", named)

@@ -5,10 +5,13 @@
 #include "snap_internal.cuh"
 
 namespace snap {
+
 namespace {
 
 constexpr int kMaxTokens = INT_MAX - 255;      // a block of the rotary pass has 256 tokens at most: the last one's numbers stay within 32 bits
 constexpr double kTwoPi = 6.283185307179586;
+
+}  // namespace
 
 // The fields the kernels use: snap_rope_table checks the rest.
 int check_rope(const snap_rope_config_t* r) {
@@ -37,15 +40,21 @@ bool out_strides_ok(long long tok, long long head, int tokens, int heads, int d,
   return token_major || head_major;
 }
 
-int check_paged(const snap_config_t* cfg, const snap_paged_t* p) {
+int check_page_counts(const snap_config_t* cfg, const snap_paged_t* p) {
   const int rc = validate_config(cfg);
   if (rc != SNAP_OK) return rc;
   if (!p) return SNAP_ERR_NULL_POINTER;
   if (p->page_tokens < 1 || p->n_pages < 1 || p->max_pages < 1 || p->reserved != 0) return SNAP_ERR_INVALID_ARG;
   if ((long long)p->page_tokens * p->max_pages > (1LL << 30)) return SNAP_ERR_INVALID_ARG;
+  return SNAP_OK;
+}
+
+int check_paged(const snap_config_t* cfg, const snap_paged_t* p, int eb) {
+  const int rc = check_page_counts(cfg, p);
+  if (rc != SNAP_OK) return rc;
   const long long st[6] = {p->k_page_stride, p->k_head_stride, p->k_row_stride, p->v_page_stride, p->v_head_stride, p->v_row_stride};
   for (const long long x : st)
-    if (x < 0 || x > (1LL << 40) || (x * elt_bytes(cfg->dtype)) % 16) return SNAP_ERR_INVALID_ARG;
+    if (x < 0 || x > (1LL << 40) || (x * eb) % 16) return SNAP_ERR_INVALID_ARG;
   if ((p->page_tokens > 1 && (p->k_row_stride < cfg->d_qk || p->v_row_stride < cfg->d_v)) ||
       (cfg->n_kv_heads > 1 && (p->k_head_stride < cfg->d_qk || p->v_head_stride < cfg->d_v)) ||
       (p->n_pages > 1 && (p->k_page_stride < cfg->d_qk || p->v_page_stride < cfg->d_v)))
@@ -63,15 +72,18 @@ PageMap page_map(const snap_paged_t* p, const int* table) {
   return m;
 }
 
+namespace {
+
 // Do the blocks that move a call's rows (64 or more rows each) fit one grid, and its KV heads and sequences the selection's?
 bool evict_countable(const snap_config_t* c, int n_seqs) {
   const long long keep = (long long)c->l_sink + c->l_recent + c->topk;
   return c->n_kv_heads <= 65535 && (keep / 64 + 1) * c->n_kv_heads * n_seqs <= 0x7fffffffLL;
 }
 
+}  // namespace
+
 int status_of(cudaError_t e) { return e == cudaSuccess ? SNAP_OK : SNAP_ERR_CUDA; }
 
-}  // namespace
 }  // namespace snap
 
 using namespace snap;
@@ -158,7 +170,7 @@ int snap_paged_append(const snap_config_t* cfg, const snap_paged_t* paged,
                       const void* v_dev, int64_t v_token_stride, int64_t v_head_stride,
                       void* k_pages_dev, void* v_pages_dev, const int32_t* page_table_dev,
                       int32_t* seq_len_dev, float* weights_dev, uint32_t* status_dev, void* cuda_stream) {
-  int rc = check_paged(cfg, paged);
+  int rc = check_paged(cfg, paged, cfg ? elt_bytes(cfg->dtype) : 0);
   if (rc != SNAP_OK) return rc;
   if (rope) {
     rc = check_rope(rope);
@@ -200,7 +212,7 @@ int snap_paged_append(const snap_config_t* cfg, const snap_paged_t* paged,
 }
 
 int64_t snap_paged_decode_workspace_bytes(const snap_config_t* cfg, const snap_paged_t* paged, int32_t n_active, int32_t with_weights) {
-  const int rc = check_paged(cfg, paged);
+  const int rc = check_paged(cfg, paged, cfg ? elt_bytes(cfg->dtype) : 0);
   if (rc != SNAP_OK) return rc;
   if (n_active < 0) return SNAP_ERR_INVALID_ARG;
   PagedDecodePlan p;
@@ -214,7 +226,7 @@ int snap_paged_decode_attn(const snap_config_t* cfg, const snap_paged_t* paged, 
                            const int32_t* seq_len_dev, const float* weights_in_dev, float* weights_out_dev,
                            void* out_dev, void* workspace_dev, size_t workspace_bytes,
                            uint32_t* status_dev, void* cuda_stream) {
-  const int rc = check_paged(cfg, paged);
+  const int rc = check_paged(cfg, paged, cfg ? elt_bytes(cfg->dtype) : 0);
   if (rc != SNAP_OK) return rc;
   if (n_active < 0) return SNAP_ERR_INVALID_ARG;
   if (n_active == 0) return SNAP_OK;
@@ -234,7 +246,7 @@ int snap_paged_decode_attn(const snap_config_t* cfg, const snap_paged_t* paged, 
 }
 
 int64_t snap_paged_evict_workspace_bytes(const snap_config_t* cfg, const snap_paged_t* paged, int32_t n_seqs) {
-  const int rc = check_paged(cfg, paged);
+  const int rc = check_paged(cfg, paged, cfg ? elt_bytes(cfg->dtype) : 0);
   if (rc != SNAP_OK) return rc;
   if (n_seqs < 0 || n_seqs > 65535) return SNAP_ERR_INVALID_ARG;
   if (!evict_countable(cfg, n_seqs)) return SNAP_ERR_UNSUPPORTED;
@@ -246,7 +258,7 @@ int snap_paged_evict(const snap_config_t* cfg, const snap_paged_t* paged, const 
                      const int32_t* page_table_dev, int32_t* seq_len_dev, const float* weights_in_dev,
                      float* weights_out_dev, int32_t* kept_rows_dev, void* workspace_dev, size_t workspace_bytes,
                      uint32_t* status_dev, void* cuda_stream) {
-  const int rc = check_paged(cfg, paged);
+  const int rc = check_paged(cfg, paged, cfg ? elt_bytes(cfg->dtype) : 0);
   if (rc != SNAP_OK) return rc;
   if (n_seqs < 0 || n_seqs > 65535) return SNAP_ERR_INVALID_ARG;
   if (n_seqs == 0) return SNAP_OK;

@@ -1,0 +1,35 @@
+// Numbers of 8 bits (e4m3: a sign, four bits of exponent, three of mantissa; 448 at most, a NaN, no infinity).
+#pragma once
+
+#include <cuda_fp16.h>
+#include <stdint.h>
+
+namespace snap {
+
+// Two codes (low byte first) as two half-precision numbers, exactly.  64 lanes per clock and SM; masks and shifts on four codes
+// at a time take 2.5 times as long as these two conversions and a byte permutation.
+__device__ __forceinline__ uint32_t halves_of_codes(uint32_t two) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((unsigned short)two));
+  return r;
+}
+__device__ __forceinline__ float2 floats_of_codes(uint32_t two) {
+  const uint32_t h = halves_of_codes(two);
+  return __half22float2(*reinterpret_cast<const __half2*>(&h));
+}
+// Rounded to nearest even; 448 at most in size, NaN stays.
+__device__ __forceinline__ uint32_t codes_of_floats(float lo, float hi) {
+  unsigned short r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+// The exponent of a block's scale: the smallest e from -126 to 120 with `largest` <= 448 * 2^e, 448 being 1.75 * 2^8.
+__device__ __forceinline__ int scale_exponent(float largest) {
+  const uint32_t b = __float_as_uint(largest);                           // not negative
+  const int e = (int)(b >> 23) - 127 - 8 + ((b & 0x7fffffu) > 0x600000u);
+  return min(max(e, -126), 120);
+}
+__device__ __forceinline__ float exp2_of(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
+
+}  // namespace snap

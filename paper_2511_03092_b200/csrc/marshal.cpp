@@ -1,4 +1,4 @@
-// Argument marshalling of the rotary and paged-cache calls: checks that the tensors of a call are what the library is
+// Argument marshalling of the rotary and paged-cache calls, those of the 8-bit cache among them: checks that the tensors of a call are what the library is
 // told they are and passes their addresses on.  A serving step makes these calls once per layer, and the same checks
 // cost 5 to 10 us a call as Python expressions, more than the kernels of a small step take.
 //
@@ -247,6 +247,151 @@ PyObject* paged_evict(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   return answer(c, rc);
 }
 
+// entry, cfg, paged, slots, new_tokens, table_in, table_out, seq_len, free, n_free_in, n_free_out, granted, first, cu, token_slots, token_rows,
+// workspace, status, stream
+PyObject* paged_plan(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (!count(n_args, 19)) return nullptr;
+  const auto fn = reinterpret_cast<decltype(&snap_paged_plan)>(PyLong_AsVoidPtr(a[0]));
+  Struct<snap_config_t> cfg(a[1]);
+  Struct<snap_paged_t> p(a[2]);
+  if (!fn || !cfg.ok || !p.ok) return PyErr_Occurred() ? nullptr : (PyErr_SetString(PyExc_TypeError, "no entry point"), nullptr);
+  if (!cfg.p || !p.p) return PyLong_FromLong(SNAP_ERR_NULL_POINTER);
+  Call c{a};
+  const int64_t n = length(c, 3), most = length(c, 14);
+  const Sizes table{cfg.p->max_seqs, p.p->max_pages};
+  size_t bytes;
+  const int32_t* slots = ints(c, 3, n);
+  const int32_t* fresh = ints(c, 4, n);
+  const int32_t* in = static_cast<int32_t*>(c.dense(5, at::kInt, table));
+  int32_t* out = static_cast<int32_t*>(c.dense(6, at::kInt, table));
+  int32_t* seq_len = ints(c, 7, cfg.p->max_seqs);
+  int32_t* stack = ints(c, 8, p.p->n_pages);
+  const int32_t* free_in = ints(c, 9, 1);
+  int32_t* free_out = ints(c, 10, 1);
+  int32_t* granted = ints(c, 11, n);
+  int32_t* first = ints(c, 12, n);
+  int32_t* cu = ints(c, 13, n + 1);
+  int32_t* ts = ints(c, 14, most);
+  int32_t* tr = ints(c, 15, most);
+  void* ws = scratch(c, 16, bytes);
+  uint32_t* status = static_cast<uint32_t*>(c.dense(17, at::kInt));
+  void* st = c.stream(a[18]);
+  int rc = 0;
+  if (c.good && !PyErr_Occurred())
+    rc = fn(cfg.p, p.p, slots, fresh, (int32_t)n, in, out, seq_len, stack, free_in, free_out, (int32_t)most, granted, first, cu, ts, tr, ws, bytes,
+            status, st);
+  return answer(c, rc);
+}
+
+// The parts of a call on the 8-bit cache that all three share: codes, their scales, table, status.
+struct Q8Parts { void* k; void* v; float* ks; float* vs; int32_t* table; uint32_t* status; };
+Q8Parts q8_parts(Call& c, const snap_config_t* cfg, const snap_paged_q8_t* q, int k, int status) {
+  Q8Parts r;
+  const snap_paged_t* p = &q->pages;
+  r.k = c.pages(k, at::kFloat8_e4m3fn, Sizes{p->n_pages, cfg->n_kv_heads, p->page_tokens, cfg->d_qk},
+                Sizes{p->k_page_stride, p->k_head_stride, p->k_row_stride, 1});
+  r.v = c.pages(k + 1, at::kFloat8_e4m3fn, Sizes{p->n_pages, cfg->n_kv_heads, p->page_tokens, cfg->d_v},
+                Sizes{p->v_page_stride, p->v_head_stride, p->v_row_stride, 1});
+  const Sizes scales{p->n_pages, cfg->n_kv_heads, q->block_tokens > 0 ? p->page_tokens / q->block_tokens : 0};
+  c.need(r.ks = static_cast<float*>(c.dense(k + 2, at::kFloat, scales)));
+  c.need(r.vs = static_cast<float*>(c.dense(k + 3, at::kFloat, scales)));
+  c.need(r.table = static_cast<int32_t*>(c.dense(k + 4, at::kInt, Sizes{cfg->max_seqs, p->max_pages})));
+  r.status = static_cast<uint32_t*>(c.dense(status, at::kInt));
+  return r;
+}
+
+// entry, cfg, paged, slots, cu, first, k, v, k_pages, v_pages, k_scales, v_scales, table, seq_len, rope, freqs, positions, q, q_out, k_out, status, stream
+PyObject* paged_q8_append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (!count(n_args, 22)) return nullptr;
+  const auto fn = reinterpret_cast<decltype(&snap_paged_q8_append)>(PyLong_AsVoidPtr(a[0]));
+  Struct<snap_config_t> cfg(a[1]);
+  Struct<snap_paged_q8_t> p(a[2]);
+  Struct<snap_rope_config_t> rp(a[14]);
+  if (!fn || !cfg.ok || !p.ok || !rp.ok) return PyErr_Occurred() ? nullptr : (PyErr_SetString(PyExc_TypeError, "no entry point"), nullptr);
+  if (!cfg.p || !p.p) return PyLong_FromLong(SNAP_ERR_NULL_POINTER);
+  Call c{a};
+  const Tensor* kt = c.at(6);
+  const int64_t n = length(c, 3), hq = cfg.p->n_q_heads, hkv = cfg.p->n_kv_heads, d = cfg.p->d_qk;
+  const int64_t t = kt && kt->dim() == 3 ? countable(c, kt->size(0)) : (c.good = false, 0);
+  const at::ScalarType type = type_of(cfg.p);
+  const Q8Parts pp = q8_parts(c, cfg.p, p.p, 8, 20);
+  int64_t ks[2], vs[2], qs[2];
+  const int32_t* slots = ints(c, 3, n);
+  const int32_t* cu = ints(c, 4, n + 1);
+  const int32_t* first = ints(c, 5, n);
+  void* k = c.rows(6, type, Sizes{t, hkv, d}, ks);
+  void* v = c.rows(7, type, Sizes{t, hkv, cfg.p->d_v}, vs);
+  int32_t* seq_len = ints(c, 13, cfg.p->max_seqs);
+  const double* freqs = rp.p ? static_cast<const double*>(c.dense(15, at::kDouble, Sizes{rp.p->rot_dim / 2})) : nullptr;
+  const int32_t* pos = rp.p ? ints(c, 16, t) : nullptr;
+  void* q = c.rows(17, type, Sizes{t, hq, d}, qs);
+  void* qo = c.dense(18, type, Sizes{t, hq, d});
+  void* ko = c.dense(19, type, Sizes{t, hkv, d});
+  void* st = c.stream(a[21]);
+  int rc = 0;
+  if (c.good && !PyErr_Occurred())
+    rc = fn(cfg.p, p.p, slots, cu, first, (int32_t)n, (int32_t)t, rp.p, freqs, pos, q, qs[0], qs[1], qo, k, ks[0], ks[1], ko, v, vs[0], vs[1],
+            pp.k, pp.v, pp.ks, pp.vs, pp.table, seq_len, pp.status, st);
+  return answer(c, rc);
+}
+
+// entry, cfg, paged, q, slots, n, q_len, k_pages, v_pages, k_scales, v_scales, table, seq_len, out, workspace, status, stream
+PyObject* paged_q8_decode_attn(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (!count(n_args, 17)) return nullptr;
+  const auto fn = reinterpret_cast<decltype(&snap_paged_q8_decode_attn)>(PyLong_AsVoidPtr(a[0]));
+  Struct<snap_config_t> cfg(a[1]);
+  Struct<snap_paged_q8_t> p(a[2]);
+  if (!fn || !cfg.ok || !p.ok) return PyErr_Occurred() ? nullptr : (PyErr_SetString(PyExc_TypeError, "no entry point"), nullptr);
+  if (!cfg.p || !p.p) return PyLong_FromLong(SNAP_ERR_NULL_POINTER);
+  Call c{a};
+  const int64_t n = countable(c, PyLong_AsLong(a[5])), ql = countable(c, PyLong_AsLong(a[6])), hq = cfg.p->n_q_heads;
+  const at::ScalarType type = type_of(cfg.p);
+  const Q8Parts pp = q8_parts(c, cfg.p, p.p, 7, 15);
+  // one token per sequence: with or without the dim of tokens
+  const auto tokens = [&](int i, int64_t d) -> void* {
+    const Tensor* t = c.at(i);
+    return ql == 1 && t && t->dim() == 3 ? c.dense(i, type, Sizes{n, hq, d}) : c.dense(i, type, Sizes{n, ql, hq, d});
+  };
+  size_t bytes;
+  void* q = tokens(3, cfg.p->d_qk);
+  const int32_t* slots = ints(c, 4, n);
+  const int32_t* seq_len = ints(c, 12, cfg.p->max_seqs);
+  void* out = tokens(13, cfg.p->d_v);
+  void* ws = scratch(c, 14, bytes);
+  void* st = c.stream(a[16]);
+  int rc = 0;
+  if (c.good && !PyErr_Occurred())
+    rc = fn(cfg.p, p.p, q, slots, (int32_t)n, (int32_t)ql, pp.k, pp.v, pp.ks, pp.vs, pp.table, seq_len, out, ws, bytes, pp.status, st);
+  return answer(c, rc);
+}
+
+// entry, cfg, paged, slots, cu, first, k_pages, v_pages, k_scales, v_scales, table, k, v, status, stream
+PyObject* paged_q8_gather(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (!count(n_args, 15)) return nullptr;
+  const auto fn = reinterpret_cast<decltype(&snap_paged_q8_gather)>(PyLong_AsVoidPtr(a[0]));
+  Struct<snap_config_t> cfg(a[1]);
+  Struct<snap_paged_q8_t> p(a[2]);
+  if (!fn || !cfg.ok || !p.ok) return PyErr_Occurred() ? nullptr : (PyErr_SetString(PyExc_TypeError, "no entry point"), nullptr);
+  if (!cfg.p || !p.p) return PyLong_FromLong(SNAP_ERR_NULL_POINTER);
+  Call c{a};
+  const Tensor* kt = c.at(11);
+  const int64_t n = length(c, 3), hkv = cfg.p->n_kv_heads;
+  const int64_t t = kt && kt->dim() == 3 ? countable(c, kt->size(0)) : (c.good = false, 0);
+  const at::ScalarType type = type_of(cfg.p);
+  const Q8Parts pp = q8_parts(c, cfg.p, p.p, 6, 13);
+  int64_t ks[2], vs[2];
+  const int32_t* slots = ints(c, 3, n);
+  const int32_t* cu = ints(c, 4, n + 1);
+  const int32_t* first = ints(c, 5, n);
+  void* k = c.rows(11, type, Sizes{t, hkv, cfg.p->d_qk}, ks);
+  void* v = c.rows(12, type, Sizes{t, hkv, cfg.p->d_v}, vs);
+  void* st = c.stream(a[14]);
+  int rc = 0;
+  if (c.good && !PyErr_Occurred())
+    rc = fn(cfg.p, p.p, slots, cu, first, (int32_t)n, (int32_t)t, pp.k, pp.v, pp.ks, pp.vs, pp.table, k, ks[0], ks[1], v, vs[0], vs[1], pp.status, st);
+  return answer(c, rc);
+}
+
 // What torch or the language runtime throws becomes a Python error.
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
 PyObject* guarded(PyObject* self, PyObject* const* args, Py_ssize_t n) {
@@ -268,6 +413,10 @@ PyMethodDef methods[] = {{"rope", method<rope>(), METH_FASTCALL, nullptr},
                          {"paged_append", method<paged_append>(), METH_FASTCALL, nullptr},
                          {"paged_decode_attn", method<paged_decode_attn>(), METH_FASTCALL, nullptr},
                          {"paged_evict", method<paged_evict>(), METH_FASTCALL, nullptr},
+                         {"paged_plan", method<paged_plan>(), METH_FASTCALL, nullptr},
+                         {"paged_q8_append", method<paged_q8_append>(), METH_FASTCALL, nullptr},
+                         {"paged_q8_decode_attn", method<paged_q8_decode_attn>(), METH_FASTCALL, nullptr},
+                         {"paged_q8_gather", method<paged_q8_gather>(), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "Argument marshalling of the rotary and paged-cache calls.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};

@@ -273,10 +273,70 @@ cudaError_t launch_paged_decode(int dtype, const Shape& s, const PageMap& m, con
                                 const int* slots, int n_active, const void* k_pages, const void* v_pages, const int* seq_len,
                                 const float* w_in, float* w_out, void* out, char* scratch, uint32_t* status, cudaStream_t st);
 
+// Checks that the entry points of the caches in pages share (api_paged.cu): a rotation's fields and magnitude, strides of
+// [tokens][heads][d] tensors that are read and that are written, page counts, a pool's description (eb: bytes of its elements).
+int check_rope(const snap_rope_config_t* r);
+double rope_magnitude(const snap_rope_config_t* r);
+bool strides_ok(long long tok, long long head, int eb);
+bool out_strides_ok(long long tok, long long head, int tokens, int heads, int d, int eb);
+int check_page_counts(const snap_config_t* cfg, const snap_paged_t* p);
+int check_paged(const snap_config_t* cfg, const snap_paged_t* p, int eb);
+PageMap page_map(const snap_paged_t* p, const int* table);
+int status_of(cudaError_t e);
+
 size_t paged_evict_scratch_bytes(const Shape& s, int n_seqs);
 cudaError_t launch_paged_evict(int dtype, const Shape& s, const PageMap& m, const int* src, const int* dst, int n_seqs,
                                void* k_pages, void* v_pages, int* seq_len, const float* w_in, float* w_out, int* kept,
                                char* scratch, uint32_t* status, cudaStream_t st);
+
+// --- pages of a step (paged_plan.cu) ---
+struct PlanArgs {
+  const int* slots; const int* new_tokens;
+  const int* table_in; int* table_out;
+  int* seq_len; int* stack; const int* n_free_in; int* n_free_out;
+  int* granted; int* first_rows; int* cu; int* token_slots; int* token_rows;
+  int n, n_tokens_max, max_seqs, page, n_pages, max_pages;
+  char* scratch;
+  uint32_t* status;
+};
+size_t paged_plan_scratch_bytes(int max_seqs, int n_seqs);
+cudaError_t launch_paged_plan(const PlanArgs& a, cudaStream_t st);
+
+// --- the cache in pages of 8-bit numbers (q8_rows.cu, q8_decode.cu; entry points in api_q8.cu) ---
+struct Q8Map {                      // scales: [n_pages][Hkv][blocks] each; rows of a block, blocks of a page
+  PageMap pages;
+  int block, blocks;
+};
+// Rows of n sequences between dense tensors and their pages: entry i's tokens are [cu[i], cu[i + 1]), its rows begin at first[i].
+struct Q8Rows {
+  const int* slots; const int* cu; const int* first;
+  int n_seqs, n_tokens, Hq, Hkv, d_qk, d_v, max_seqs;
+  Q8Map map;
+  uint8_t* k_pages; uint8_t* v_pages; float* k_scales; float* v_scales;   // (a gather only reads them)
+  uint32_t* status;
+};
+struct Q8AppendArgs {
+  Q8Rows r;
+  const void* q; const void* k; const void* v; void* q_out; void* k_out;
+  long long q_tok, q_head, k_tok, k_head, v_tok, v_head;            // elements
+  const double* freqs; const int* positions;
+  int rot, offset, interleaved;     // rot = 0: no rotation
+  float magnitude, growth;          // growth: what a key's largest number is multiplied by for the scale
+  int* seq_len;
+};
+struct Q8GatherArgs {
+  Q8Rows r;
+  void* k; void* v;
+  long long k_tok, k_head, v_tok, v_head;
+};
+cudaError_t launch_q8_append(int dtype, const Q8AppendArgs& a, cudaStream_t st);
+cudaError_t launch_q8_gather(int dtype, const Q8GatherArgs& a, cudaStream_t st);
+
+struct Q8DecodePlan { int ctas, gb, nhb; size_t entry_off, ml_off, o_off, bytes; };
+int q8_decode_plan(int dtype, const Shape& s, const Q8Map& m, int n_active, int q_len, int sms, Q8DecodePlan* p);
+cudaError_t launch_q8_decode(int dtype, const Shape& s, const Q8Map& m, const Q8DecodePlan& p, const void* q, const int* slots,
+                             int n_active, int q_len, const void* k_pages, const void* v_pages, const float* k_scales,
+                             const float* v_scales, const int* seq_len, void* out, char* scratch, uint32_t* status, cudaStream_t st);
 
 // Checked indexing for the debugging build (-DSNAP_DEBUG_BOUNDS): a data-dependent index that falls
 // outside [0, n) raises SNAP_DEV_INDEX_CHECK in the status word and the access is skipped -- nothing
