@@ -140,18 +140,16 @@ q8_mma_kernel(const __grid_constant__ Q8Args a, const __grid_constant__ CUtensor
   // lane l looks up the page of the tile's row l ----
   Place pr = at;
   bool more = advance<TR>(a, held, pr, w, end);
-  struct Look { int page, off, kvh; bool tile; };                        // page: -1 no row, n_pages: a row on a page that is not there
-  const auto look_up = [&]() {
-    Look r = {-1, 0, 0, more};
+  struct Look { int page, off, kvh; bool tile; };                        // off: row of the page, -1 no row
+  const auto look_up = [&]() {                                           // (nothing waits here for what the table says)
+    Look r = {-1, -1, 0, more};
     if (more) {
       const int row = pr.t * TR + lane;
       r.kvh = pr.u / a.nhb;
       if (row < pr.len) {
         const int pg = a.by_page.quotient(row);
         r.off = row - pg * a.map.page;
-        r.page = a.map.n_pages;
         if (index_ok(pg, a.map.max_pages, a.status)) r.page = a.map.table[(long long)pr.slot * a.map.max_pages + pg];
-        if (r.page < 0) r.page = a.map.n_pages;
       }
       more = advance<TR>(a, held, pr, NWARP, end);
     }
@@ -220,10 +218,10 @@ q8_mma_kernel(const __grid_constant__ Q8Args a, const __grid_constant__ CUtensor
 #pragma unroll
     for (int x = 0; x + 1 < LOOK; ++x) look[x] = look[x + 1];
     look[LOOK - 1] = look_up();
-    const bool okay = l.page >= 0 && l.page < a.map.n_pages;
+    const bool okay = l.off >= 0 && l.page >= 0 && l.page < a.map.n_pages;
     const unsigned rows = __ballot_sync(0xffffffffu, okay);
     there_of = (there_of & ~(0xffffffffull << (32 * s))) | (unsigned long long)rows << (32 * s);
-    if (l.page >= a.map.n_pages && a.status) atomicOr(a.status, SNAP_DEV_BAD_PAGE);
+    if (!okay && l.off >= 0 && a.status) atomicOr(a.status, SNAP_DEV_BAD_PAGE);
     const uint32_t dst = stage0 + s * S::STAGE_B, bar = bar0 + 8 * s, sc = scale0 + (s * 2 * TR + lane) * 4;
     if (okay) {
       const long long x = ((long long)l.page * a.Hkv + l.kvh) * a.blocks + a.by_block.quotient(l.off);
