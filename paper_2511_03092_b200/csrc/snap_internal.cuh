@@ -332,7 +332,11 @@ struct Q8GatherArgs {
 cudaError_t launch_q8_append(int dtype, const Q8AppendArgs& a, cudaStream_t st);
 cudaError_t launch_q8_gather(int dtype, const Q8GatherArgs& a, cudaStream_t st);
 
-struct Q8DecodePlan { int ctas, gb, nhb; size_t entry_off, ml_off, o_off, bytes; };
+struct Q8DecodePlan {
+  int ctas, gb, nhb;                // CTAs of the split kernel; columns of a unit, units per KV head
+  int heads;                        // KV heads of a unit
+  size_t entry_off, ml_off, o_off, bytes;
+};
 int q8_decode_plan(int dtype, const Shape& s, const Q8Map& m, int n_active, int q_len, int sms, Q8DecodePlan* p);
 cudaError_t launch_q8_decode(int dtype, const Shape& s, const Q8Map& m, const Q8DecodePlan& p, const void* q, const int* slots,
                              int n_active, int q_len, const void* k_pages, const void* v_pages, const float* k_scales,

@@ -4,12 +4,13 @@ Tolerances.  u is half a step of the output type (2^-8 bf16, 2^-24 fp32), e = 2^
 Append: codes and scales of what is not rotated are those of the definition.  A rotated key is off by at most 8 e m (|a| + |b|)
 before it is rounded (two products and a sum in single precision, cosines and sines off by a few e), so the number that its code
 stands for is at most twice that further from the exact one than the nearest code's; scales do not depend on the rotation.
-Attention: a logit is a sum of d products, off by at most (d + 8) e R (queries enter as two numbers of 11 bits, 2^-22 off; the
-change of base and two scales), R the largest scale sum_c |q_c k_rc|; a query's smallest parts are cut off 2^-38 below its
-largest: d 2^-38 max|q| max|k|.  A probability is then off by a factor 1 +- 2 (that) to first order, the exponential's own 2^-22
-and 2^-11 (bf16: rounded to 11 bits before it multiplies the values; fp32: two such numbers, 2^-21); it is cut off 2^-31 below the
-largest product of probability and scale; sums over n rows add n e.  So
-|err| <= u |out| + (2 L + 2^-20 + 2^-11 [bf16] + 2 n e) sum_r p_r |v_r| + n 2^-31 448 max_r(p_r s_r)."""
+Attention: a logit is a sum of d products, off by at most (d + 8) e R (a single-precision query enters as two numbers of 11 bits,
+2^-22 off; the change of base and two scales), R the largest scale sum_c |q_c k_rc|; a query's smallest parts are cut off 2^-38
+below its largest number Q: 2^-38 Q of any.  A probability is then off by a factor 1 +- 2 (that) to first order, the exponential's own 2^-22,
+and 2^-11 (bf16: rounded to 11 bits before it multiplies the values) or 2^-21 (fp32: two such numbers); of small ones 2^-31 of the largest
+product of probability and scale is cut (2^-25 is half the last step of half precision, the largest is 2^6 or more), times its row's code;
+sums over n rows add n e.  So
+|err| <= u |out| + (2 L + 2^-20 + 2^-11 [bf16] + 2 n e) sum_r p_r |v_r| + 2^-31 max_r(p_r s_r) sum_r |code_r|."""
 import numpy as np
 import pytest
 import torch
@@ -301,15 +302,17 @@ def check_decode(c, q, slots, out, dtype, lengths=None):
             seen = int((there < n - q.shape[1] + 1 + u).sum())
             want, _, mass, reach = porc.decode(x[i, u], k[:seen], v[:seen], cfg.softmax_scale)
             d, g = cfg.d_qk, cfg.n_q_heads // cfg.n_kv_heads
-            largest = np.zeros((cfg.n_q_heads, 1))
+            floor, cut = np.zeros_like(want), np.zeros(cfg.n_q_heads)
             for h in range(cfg.n_q_heads if seen else 0):
-                z = (k[:seen, h // g] @ x[i, u, h]) * cfg.softmax_scale
+                kh, size = k[:seen, h // g], np.abs(x[i, u, h])
+                z = (kh @ x[i, u, h]) * cfg.softmax_scale
                 p = np.exp(z - z.max())
-                largest[h] = (p / p.sum() * s[:seen, h // g]).max()
-            cut = d * 2.0 ** -38 * np.abs(x[i, u]).max(axis=-1) * (np.abs(k[:seen]).max() if seen else 0) * cfg.softmax_scale
+                codes = np.abs(v[:seen, h // g]) / s[:seen, h // g, None]
+                floor[h] = 2.0 ** -31 * (p / p.sum() * s[:seen, h // g]).max() * codes.sum(axis=0)
+                cut[h] = np.abs(kh).sum(axis=1).max() * 2.0 ** -38 * size.max() * cfg.softmax_scale
             L = (d + 8) * E * reach + cut
             bound = HALF_STEP[dtype] * np.abs(want) + (2 * L[:, None] + 2.0 ** -20 + (2.0 ** -11 if dtype == "bf16" else 0) + 2 * seen * E) * mass
-            bound += seen * 2.0 ** -31 * 448 * largest
+            bound += floor
             err = np.abs(got[i, u] - want)
             assert (err <= bound).all(), f"entry {i} (slot {slot}, {seen} rows), token {u}: {(err - bound).max():.3e} over {bound.max():.3e}"
 
