@@ -21,6 +21,8 @@
 //
 // Where a row's heads lie side by side (pages stored rows first), two warps of a CTA take one head and two the next, over the same rows: HBM
 // then delivers twice as much in a row (128-byte heads, 16 long sequences: 208 us without, SIDES with; heads first 168).
+#include <type_traits>
+
 #include "e4m3.cuh"
 #include "paged_line.cuh"
 
@@ -71,7 +73,7 @@ template <int D, int NWARP, int NSTAGE, int NG, int SIDES> struct Q8Shape {
   static constexpr int SW = D < 128 ? D : 128, NSL = D / SW;             // bytes of a slab's rows; slabs
   static constexpr int SLAB_B = TR * SW, TENS_B = NSL * SLAB_B, STAGE_B = 2 * TENS_B;
   // column stride of the exchange buffers: fragments store without bank conflicts; as many buffers as leave room for the CTAs of an SM
-  static constexpr int LD = D + 4, NBUF = SIDES == 1 && D * NG < 128 ? NWARP / 2 : 1;
+  static constexpr int LD = D + 4, NBUF = SIDES == 1 && D * NG <= 128 ? NWARP / 2 : 1;
   static constexpr size_t stages_b = (size_t)NWARP * NSTAGE * STAGE_B;
   static constexpr size_t rows_b = (size_t)NWARP * NSTAGE * 2 * TR * sizeof(float);     // the rows' scales
   static constexpr size_t bars_b = NWARP * NSTAGE * 8;
@@ -190,24 +192,31 @@ q8_mma_kernel(const __grid_constant__ Q8Args a, const __grid_constant__ CUtensor
   const T* q_all = static_cast<const T*>(a.q);
   uint32_t qb[NG][KS][PARTS][2];
   float q_scale[NG][2];                                                  // of this thread's two columns of the logits
-  const auto load_q = [&]() {                                            // (the first tiles' copies wait alongside)
+  using Four = std::conditional_t<F32, uint4, uint2>;                    // four numbers' bits
+  const auto load_q = [&]() {                                            // the numbers themselves, to begin with
     const int k = at.u / a.nhb, hb = at.u - k * a.nhb, x0 = hb * a.gb + side * a.sc, nh = min(a.sc, a.g - x0);
 #pragma unroll
     for (int gi = 0; gi < NG; ++gi) {
       const int col = 8 * gi + gq;
       const T* qp = q_all + a.out_row(at.e, k, col < nh ? x0 + col : 0) * d_qk + 4 * tq;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        Four v = {};
+        if (col < nh && (EXACT || 16 * ks < d_qk)) v = *reinterpret_cast<const Four*>(qp + 16 * ks);
+        qb[gi][ks][0][0] = v.x; qb[gi][ks][0][1] = v.y;
+        if constexpr (F32) { qb[gi][ks][PARTS - 1][0] = v.z; qb[gi][ks][PARTS - 1][1] = v.w; }
+      }
+    }
+  };
+  const auto make_q = [&]() {
+#pragma unroll
+    for (int gi = 0; gi < NG; ++gi) {
       float x[KS][4], big = 0.f;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        const bool there = col < nh && (EXACT || 16 * ks < d_qk);
-        if constexpr (F32) {
-          const float4 v = there ? *reinterpret_cast<const float4*>(qp + 16 * ks) : make_float4(0.f, 0.f, 0.f, 0.f);
-          x[ks][0] = v.x; x[ks][1] = v.y; x[ks][2] = v.z; x[ks][3] = v.w;
-        } else {
-          const uint2 v = there ? *reinterpret_cast<const uint2*>(qp + 16 * ks) : make_uint2(0, 0);
-          x[ks][0] = __uint_as_float(v.x << 16); x[ks][1] = __uint_as_float(v.x & 0xffff0000u);
-          x[ks][2] = __uint_as_float(v.y << 16); x[ks][3] = __uint_as_float(v.y & 0xffff0000u);
-        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          x[ks][c] = __uint_as_float(F32 ? qb[gi][ks][F32 ? c / 2 : 0][c % 2] : c % 2 ? qb[gi][ks][0][c / 2] & 0xffff0000u : qb[gi][ks][0][c / 2] << 16);
 #pragma unroll
         for (int c = 0; c < 4; ++c) big = fmaxf(big, fabsf(x[ks][c]));
       }
@@ -224,7 +233,7 @@ q8_mma_kernel(const __grid_constant__ Q8Args a, const __grid_constant__ CUtensor
           qb[gi][ks][0][c] = pack_f16(lo, hi);
           if constexpr (F32) qb[gi][ks][PARTS - 1][c] = rest_f16(lo, hi, qb[gi][ks][0][c]);
         }
-      const float back = a.scale_log2 / f0 / f1;
+      const float back = a.scale_log2 * power_of(-(up / 2)) * power_of(up / 2 - up);
 #pragma unroll
       for (int c = 0; c < 2; ++c) q_scale[gi][c] = __shfl_sync(0xffffffffu, back, (2 * tq + c) * 4);
     }
@@ -318,9 +327,11 @@ q8_mma_kernel(const __grid_constant__ Q8Args a, const __grid_constant__ CUtensor
         for (int x = 0; x < 4; ++x) oacc[gi][db][x] = 0.f;
     }
 
-    load_q();
+    load_q();                                                            // on its way while the first copies are looked up
+    bool fresh = true;
     for (;; ++n) {
       while (steps < LOOK || (look[0].tile && n_issued < n + NSTAGE)) step();
+      if (fresh) make_q();
       if (ws + n * WPS >= done + cnt || dead) break;
       const int s = n % NSTAGE;
       const bool landed = wait_bounded(bar0 + 8 * s, (unsigned)(n / NSTAGE) & 1u);
@@ -396,27 +407,30 @@ q8_mma_kernel(const __grid_constant__ Q8Args a, const __grid_constant__ CUtensor
       // ---- weights, and weights times scales: in range with the reference as it is? ----
       float p[MT][NG][4], add[NG][2];
 #pragma unroll 1
-      for (int pass = 0;; ++pass) {
+      for (int pass = 0;; ++pass) {                                      // (a unit's first tile has no reference yet)
         float largest = 0.f;
+        if (!fresh || pass > 0) {
 #pragma unroll
-        for (int gi = 0; gi < NG; ++gi) add[gi][0] = add[gi][1] = 0.f;
+          for (int gi = 0; gi < NG; ++gi) add[gi][0] = add[gi][1] = 0.f;
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+          for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-          for (int r8 = 0; r8 < 2; ++r8) {
-            const float v_scale = sc[TR + row_of(mt, r8)];
+            for (int r8 = 0; r8 < 2; ++r8) {
+              const float v_scale = sc[TR + row_of(mt, r8)];
 #pragma unroll
-            for (int gi = 0; gi < NG; ++gi)
+              for (int gi = 0; gi < NG; ++gi)
 #pragma unroll
-              for (int c = 0; c < 2; ++c) {
-                const float e = fast_exp2(v[mt][gi][2 * r8 + c] - ref[gi][c]);
-                add[gi][c] += e;
-                p[mt][gi][2 * r8 + c] = e * (v_scale * f[gi][c]);
-                largest = fmaxf(largest, p[mt][gi][2 * r8 + c]);
-              }
-          }
-        const bool over = largest > LIMIT;                               // (a NaN is none: it ends in the sums whatever the reference)
-        if (pass > 0 || !__any_sync(0xffffffffu, over)) break;
+                for (int c = 0; c < 2; ++c) {
+                  const float e = fast_exp2(v[mt][gi][2 * r8 + c] - ref[gi][c]);
+                  add[gi][c] += e;
+                  p[mt][gi][2 * r8 + c] = e * (v_scale * f[gi][c]);
+                  largest = fmaxf(largest, p[mt][gi][2 * r8 + c]);
+                }
+            }
+        }
+        // (a NaN is no reason: it ends in the sums whatever the reference)
+        if (pass > 0 || !(fresh || __any_sync(0xffffffffu, largest > LIMIT))) break;
+        fresh = false;
 #pragma unroll
         for (int gi = 0; gi < NG; ++gi)
 #pragma unroll
@@ -527,13 +541,19 @@ q8_mma_kernel(const __grid_constant__ Q8Args a, const __grid_constant__ CUtensor
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
             if (SIDES > 1 && 2 * tq + c >= a.sc) continue;               // (the other side's)
+            float* to = b + (8 * gi + c) * LD;
+            if (add) {                                                   // (all loads before the first store, which they might wait for)
 #pragma unroll
-            for (int db = 0; db < KS; ++db)
-#pragma unroll
-              for (int y = 0; y < 2; ++y) {
-                float* to = b + (8 * gi + c) * LD + 16 * db + 8 * y;
-                *to = add ? *to + oacc[gi][db][2 * y + c] : oacc[gi][db][2 * y + c];
+              for (int db = 0; db < KS; ++db) {
+                oacc[gi][db][c] += to[16 * db];
+                oacc[gi][db][2 + c] += to[16 * db + 8];
               }
+            }
+#pragma unroll
+            for (int db = 0; db < KS; ++db) {
+              to[16 * db] = oacc[gi][db][c];
+              to[16 * db + 8] = oacc[gi][db][2 + c];
+            }
           }
       }
       __syncthreads();
@@ -581,7 +601,9 @@ cudaError_t launch_split(const Q8Args& a, const CUtensorMap& tk, const CUtensorM
                                    : launch_as<T, D, NWARP, NSTAGE, NG, SIDES, CTAS, Tiles::BOXES>(a, tk, tv, st);
 }
 
-constexpr int kCtas = 3, kCtasWide = 2;         // per SM: heads of up to 128 dims and eight columns; else
+// CTAs per SM: heads of up to 64 dims and eight columns; else.  (128 dims with three CTAs of two stages a warp instead of two of three: the
+// 16 long sequences 188.7 us instead of 173.8.)
+constexpr int kCtas = 3, kCtasWide = 2;
 
 template <typename T>
 cudaError_t launch_type(const Q8Args& a, int d, const CUtensorMap& tk, const CUtensorMap& tv, cudaStream_t st) {
@@ -589,8 +611,8 @@ cudaError_t launch_type(const Q8Args& a, int d, const CUtensorMap& tk, const CUt
     return a.heads > 1 ? launch_split<T, 64, 4, 2, 1, 2, kCtas>(a, tk, tv, st) : a.gb > 8 ? launch_split<T, 64, 4, 3, 2, 1, kCtasWide>(a, tk, tv, st)
                                                                                          : launch_split<T, 64, 4, 2, 1, 1, kCtas>(a, tk, tv, st);
   if (d <= 128)
-    return a.heads > 1 ? launch_split<T, 128, 4, 2, 1, 2, kCtas>(a, tk, tv, st) : a.gb > 8 ? launch_split<T, 128, 4, 3, 2, 1, kCtasWide>(a, tk, tv, st)
-                                                                                          : launch_split<T, 128, 4, 2, 1, 1, kCtas>(a, tk, tv, st);
+    return a.heads > 1 ? launch_split<T, 128, 4, 3, 1, 2, kCtasWide>(a, tk, tv, st) : a.gb > 8 ? launch_split<T, 128, 4, 3, 2, 1, kCtasWide>(a, tk, tv, st)
+                                                                                          : launch_split<T, 128, 4, 3, 1, 1, kCtasWide>(a, tk, tv, st);
   if (a.heads > 1) return launch_split<T, 256, 4, 1, 1, 2, kCtasWide>(a, tk, tv, st);
   if constexpr (sizeof(T) == 2)
     if (a.gb > 8) return launch_split<T, 256, 4, 1, 2, 1, kCtasWide>(a, tk, tv, st);
@@ -607,7 +629,7 @@ int q8_decode_plan(int dtype, const Shape& s, const Q8Map& m, int n_active, int 
   const int most = wide && dtype == SNAP_F32 ? 8 : 16;                    // columns of a unit
   p->nhb = (int)((cols + most - 1) / most);
   p->gb = p->heads > 1 ? 2 * (int)cols : (int)((cols + p->nhb - 1) / p->nhb);
-  const int per_sm = p->gb > 8 || wide ? kCtasWide : kCtas;
+  const int per_sm = p->gb > 8 || s.d_qk > 64 || s.d_v > 64 ? kCtasWide : kCtas;
   p->ctas = sms * per_sm < MAX_CTAS ? sms * per_sm : MAX_CTAS;
   const long long units = (long long)n_active * s.Hkv * p->nhb, tiles = m.pages.cap / (long long)TR + 1 + UNIT_TILES;
   // grid and index limits; a line of tiles and the scratch have to be countable
