@@ -128,7 +128,7 @@ int64_t snap_paged_q8_decode_workspace_bytes(const snap_config_t* cfg, const sna
   if (rc != SNAP_OK) return rc;
   if (n_active < 0 || q_len < 1 || q_len > 1024) return SNAP_ERR_INVALID_ARG;
   Q8DecodePlan p;
-  const int rp = q8_decode_plan(cfg->dtype, make_shape(cfg), q8_map(paged, nullptr), n_active, q_len, sm_count(), &p);
+  const int rp = q8_decode_plan(make_shape(cfg), q8_map(paged, nullptr), n_active, q_len, sm_count(), &p);
   return rp == SNAP_OK ? (int64_t)p.bytes : rp;
 }
 
@@ -149,7 +149,7 @@ int snap_paged_q8_decode_attn(const snap_config_t* cfg, const snap_paged_q8_t* p
   const Shape s = make_shape(cfg);
   const Q8Map m = q8_map(paged, page_table_dev);
   Q8DecodePlan p;
-  const int rp = q8_decode_plan(cfg->dtype, s, m, n_active, q_len, sm_count(), &p);
+  const int rp = q8_decode_plan(s, m, n_active, q_len, sm_count(), &p);
   if (rp != SNAP_OK) return rp;
   if (workspace_bytes < p.bytes) return SNAP_ERR_WORKSPACE_TOO_SMALL;
   return status_of(launch_q8_decode(cfg->dtype, s, m, p, q_dev, slot_ids_dev, n_active, q_len, k_pages_dev, v_pages_dev, k_scales_dev, v_scales_dev,

@@ -106,9 +106,8 @@ __device__ __forceinline__ int warp_inclusive(int v, int lane) {
   for (int o = 1; o < 32; o <<= 1) { const int x = __shfl_up_sync(0xffffffffu, v, o); if (lane >= o) v += x; }
   return v;
 }
-// Slot and rows of sequence e; conditions to report
-template <typename A> __device__ __forceinline__ int2 read_entry(const A& a, int e, unsigned& bad) {
-  const int slot = a.slots[e];
+// Slot and rows of the sequence in a slot; conditions to report
+template <typename A> __device__ __forceinline__ int2 read_entry(const A& a, int slot, unsigned& bad) {
   int len = 0;
   if (slot >= 0 && slot < a.max_seqs) {
     len = a.seq_len[slot];
@@ -142,12 +141,19 @@ __device__ __forceinline__ bool locate_part(const A& a, Place& p, int& end, Held
   if (SMALL) {
     const int per = (a.n + 31) / 32, e0 = min(lane * per, a.n), e1 = min(e0 + per, a.n);   // a lane's sequences
     int mine = 0;
-#pragma unroll 1
-    for (int e = e0; e < e1; ++e) {
-      const int2 v = read_entry(a, e, bad);
-      held.e[e] = v;
-      mine += length_of(tiles_of<ROWS>(v.y));
-    }
+    constexpr int MOST = (MAX_HELD + 31) / 32;
+    int slots[MOST];                                                     // (all slots on their way at once, then all lengths)
+#pragma unroll
+    for (int x = 0; x < MOST; ++x) slots[x] = e0 + x < e1 ? a.slots[e0 + x] : -1;
+    int2 v[MOST];
+#pragma unroll
+    for (int x = 0; x < MOST; ++x) v[x] = read_entry(a, slots[x], bad);
+#pragma unroll
+    for (int x = 0; x < MOST; ++x)
+      if (e0 + x < e1) {
+        held.e[e0 + x] = v[x];
+        mine += length_of(tiles_of<ROWS>(v[x].y));
+      }
     const int incl = warp_inclusive(mine, lane);
     int before = incl - mine;
     total = __shfl_sync(0xffffffffu, incl, 31);
@@ -181,7 +187,7 @@ __device__ __forceinline__ bool locate_part(const A& a, Place& p, int& end, Held
   } else {
     const int per = (a.n + NT - 1) / NT, e0 = min(tid * per, a.n), e1 = min(e0 + per, a.n);
     int mine = 0;
-    for (int e = e0; e < e1; ++e) mine += length_of(tiles_of<ROWS>(read_entry(a, e, bad).y));
+    for (int e = e0; e < e1; ++e) mine += length_of(tiles_of<ROWS>(read_entry(a, a.slots[e], bad).y));
     const int incl = warp_inclusive(mine, lane);
     if (lane == 31) scan[warp] = incl;
     if (tid == 0) scan[NT / 32] = scan[NT / 32 + 1] = 0;
@@ -192,7 +198,7 @@ __device__ __forceinline__ bool locate_part(const A& a, Place& p, int& end, Held
     if (c == 0) {
       int at = before;
       for (int e = e0; e < e1; ++e) {
-        const int2 v = read_entry(a, e, bad);
+        const int2 v = read_entry(a, a.slots[e], bad);
         const int nt = tiles_of<ROWS>(v.y);
         a.entry[e] = make_int4(at, v.x, v.y, nt);
         at += length_of(nt);
@@ -203,7 +209,7 @@ __device__ __forceinline__ bool locate_part(const A& a, Place& p, int& end, Held
     if (!stretch()) return false;
     if (x0 >= (long long)before * a.U && x0 < (long long)(before + mine) * a.U) {        // one thread
       for (int e = e0; e < e1; ++e) {
-        const int len = length_of(tiles_of<ROWS>(read_entry(a, e, bad).y));
+        const int len = length_of(tiles_of<ROWS>(read_entry(a, a.slots[e], bad).y));
         if (x0 < (long long)(before + len) * a.U) { scan[NT / 32] = e; scan[NT / 32 + 1] = before; break; }
         before += len;
       }

@@ -58,7 +58,7 @@ struct Q8Args : LineArgs {
   int Hq, q_len, gq, gc, d_qk;                  // gq query heads of a KV head, gc = gq * q_len columns
   int heads, sc;                                // KV heads of a unit, a side each; columns of a side
   float scale_log2;
-  Divisor by_page, by_block, by_gq, by_gc;
+  Divisor by_page, by_block, by_gq, by_gc, by_nhb;
   int blocks;                                   // scales of a page and KV head
   int box;                                      // rows of a copy, 0: rows are copied by the lanes
   __device__ __forceinline__ long long out_row(int e, int k, int x) const {
@@ -157,7 +157,7 @@ q8_mma_kernel(const __grid_constant__ Q8Args a, const __grid_constant__ CUtensor
 
   // ---- the warp's producer: NSTAGE tiles ahead of the consumer, over unit borders; of a side's WPS warps the ws-th takes the CTA's
   // tiles ws, ws + WPS, ...; lane l looks up the page of the tile's row l ----
-  const auto head_of = [&](int u) { return SIDES == 1 ? u / a.nhb : 2 * u + side; };
+  const auto head_of = [&](int u) { return SIDES == 1 ? a.by_nhb.quotient(u) : 2 * u + side; };
   Place pr = at;
   int pr_stop = segment_end(pr, end), pr_head = head_of(pr.u);           // the CTA's tiles of pr's unit end there
   const int* pr_table = a.map.table + (long long)max(pr.slot, 0) * a.map.max_pages;
@@ -194,7 +194,7 @@ q8_mma_kernel(const __grid_constant__ Q8Args a, const __grid_constant__ CUtensor
   float q_scale[NG][2];                                                  // of this thread's two columns of the logits
   using Four = std::conditional_t<F32, uint4, uint2>;                    // four numbers' bits
   const auto load_q = [&]() {                                            // the numbers themselves, to begin with
-    const int k = at.u / a.nhb, hb = at.u - k * a.nhb, x0 = hb * a.gb + side * a.sc, nh = min(a.sc, a.g - x0);
+    const int k = a.by_nhb.quotient(at.u), hb = at.u - k * a.nhb, x0 = hb * a.gb + side * a.sc, nh = min(a.sc, a.g - x0);
 #pragma unroll
     for (int gi = 0; gi < NG; ++gi) {
       const int col = 8 * gi + gq;
@@ -310,7 +310,7 @@ q8_mma_kernel(const __grid_constant__ Q8Args a, const __grid_constant__ CUtensor
   while (true) {
     // ---- a segment: the CTA's tiles [at.t, tb) of one unit ----
     const int tb = segment_end(at, end), cnt = tb - at.t;
-    const int hb = at.u % a.nhb, nh = min(a.gb, a.g - hb * a.gb);
+    const int hb = at.u - a.by_nhb.quotient(at.u) * a.nhb, nh = min(a.gb, a.g - hb * a.gb);
     const bool whole = cnt == at.nt;
     const int all_see = at.len - a.q_len + 1;                            // rows that every column sees
     // O^T: dims 16 db + gq (+ 8: the upper two), columns 8 gi + 2 tq (+ 1)
@@ -614,19 +614,19 @@ cudaError_t launch_type(const Q8Args& a, int d, const CUtensorMap& tk, const CUt
     return a.heads > 1 ? launch_split<T, 128, 4, 3, 1, 2, kCtasWide>(a, tk, tv, st) : a.gb > 8 ? launch_split<T, 128, 4, 3, 2, 1, kCtasWide>(a, tk, tv, st)
                                                                                           : launch_split<T, 128, 4, 3, 1, 1, kCtasWide>(a, tk, tv, st);
   if (a.heads > 1) return launch_split<T, 256, 4, 1, 1, 2, kCtasWide>(a, tk, tv, st);
-  if constexpr (sizeof(T) == 2)
-    if (a.gb > 8) return launch_split<T, 256, 4, 1, 2, 1, kCtasWide>(a, tk, tv, st);
   return launch_split<T, 256, 4, 1, 1, 1, kCtasWide>(a, tk, tv, st);
 }
 
 }  // namespace
 
-int q8_decode_plan(int dtype, const Shape& s, const Q8Map& m, int n_active, int q_len, int sms, Q8DecodePlan* p) {
+int q8_decode_plan(const Shape& s, const Q8Map& m, int n_active, int q_len, int sms, Q8DecodePlan* p) {
   const bool wide = s.d_qk > 128 || s.d_v > 128;
   const long long cols = (long long)s.g * q_len;
   // Two KV heads to a unit, as its two sides: where they lie side by side and eight columns hold both.
   p->heads = s.Hkv % 2 == 0 && 2 * cols <= 8 && m.pages.kh < m.pages.kr ? 2 : 1;
-  const int most = wide && dtype == SNAP_F32 ? 8 : 16;                    // columns of a unit
+  // Columns of a unit.  (Sixteen of more than 128 dims take more registers than there are: 32 heads of 256 dims on 2, 8 sequences of 4000 to
+  // 8000 rows 43.2 us instead of 28.4 in two units.)
+  const int most = wide ? 8 : 16;
   p->nhb = (int)((cols + most - 1) / most);
   p->gb = p->heads > 1 ? 2 * (int)cols : (int)((cols + p->nhb - 1) / p->nhb);
   const int per_sm = p->gb > 8 || s.d_qk > 64 || s.d_v > 64 ? kCtasWide : kCtas;
@@ -661,7 +661,7 @@ cudaError_t launch_q8_decode(int dtype, const Shape& s, const Q8Map& m, const Q8
   a.q = q; a.kp = static_cast<const uint8_t*>(k_pages); a.vp = static_cast<const uint8_t*>(v_pages); a.ks = k_scales; a.vs = v_scales;
   a.Hq = s.Hq; a.q_len = q_len; a.gq = s.g; a.gc = s.g * q_len; a.d_qk = s.d_qk; a.heads = p.heads; a.sc = p.gb / p.heads;
   a.scale_log2 = s.scale * 1.4426950408889634f;
-  a.by_page = divisor((uint32_t)pm.page); a.by_block = divisor((uint32_t)m.block); a.by_gq = divisor((uint32_t)a.gq); a.by_gc = divisor((uint32_t)a.gc); a.blocks = m.blocks;
+  a.by_page = divisor((uint32_t)pm.page); a.by_block = divisor((uint32_t)m.block); a.by_gq = divisor((uint32_t)a.gq); a.by_gc = divisor((uint32_t)a.gc); a.by_nhb = divisor((uint32_t)a.nhb); a.blocks = m.blocks;
   // Tiles come through tensor maps of boxes 64 or 128 bytes wide, as many rows at once as a page always holds whole.
   const int d = s.d_qk > s.d_v ? s.d_qk : s.d_v, sw = d <= 64 ? 64 : 128, rows = pm.page % 32 == 0 ? 32 : pm.page % 16 == 0 ? 16 : 8;
   CUtensorMap tk = {}, tv = {};

@@ -337,7 +337,7 @@ struct Q8DecodePlan {
   int heads;                        // KV heads of a unit
   size_t entry_off, ml_off, o_off, bytes;
 };
-int q8_decode_plan(int dtype, const Shape& s, const Q8Map& m, int n_active, int q_len, int sms, Q8DecodePlan* p);
+int q8_decode_plan(const Shape& s, const Q8Map& m, int n_active, int q_len, int sms, Q8DecodePlan* p);
 cudaError_t launch_q8_decode(int dtype, const Shape& s, const Q8Map& m, const Q8DecodePlan& p, const void* q, const int* slots,
                              int n_active, int q_len, const void* k_pages, const void* v_pages, const float* k_scales,
                              const float* v_scales, const int* seq_len, void* out, char* scratch, uint32_t* status, cudaStream_t st);
