@@ -4,6 +4,8 @@
 // The scale of a block (rows of one KV head that share it) goes by the largest of the inputs, not of the rotated keys: a pair
 // (a, b) turned and multiplied by m is at most sqrt(2) m max(|a|, |b|) in either place.  So it does not depend on how sines
 // are rounded, and the pass that looks for it computes no angles.
+#include <cstring>
+
 #include "e4m3.cuh"
 #include "snap_internal.cuh"
 
@@ -39,7 +41,38 @@ __device__ __forceinline__ int entry_of(const Q8Rows& r, int t) {
   return lo;
 }
 
-struct AppendLaunch { Q8AppendArgs a; int group, chunk, nj, ni, nhk, nhq; };   // rows of a group, tokens of a CTA; items of a head; heads of a CTA at most
+constexpr int HOLD = 4;                         // pairs of vectors that a lane keeps between the look for the largest number and the rounding
+
+// Where a warp's lanes stand in `rows` rows of a head cut into `items` (pairs of vectors): in pass k lane l has item j of row r.
+struct Lanes {
+  int items, rpp, chunks, r0, j0;               // rows of a pass; passes of a row of more than 32 items
+  __device__ __forceinline__ Lanes(int items_) : items(items_) {
+    const int lane = threadIdx.x & 31;
+    rpp = items < 32 ? 32 / items : 1;
+    chunks = (items + 31) / 32;
+    r0 = items < 32 ? lane / items : 0;
+    j0 = items < 32 ? lane - r0 * items : lane;
+    if (r0 >= rpp) j0 = items;                  // (a spare lane)
+  }
+  __device__ __forceinline__ int passes(int rows) const { return chunks > 1 ? rows * chunks : (rows + rpp - 1) / rpp; }
+  __device__ __forceinline__ int row(int k) const { return chunks > 1 ? k / chunks : r0 + k * rpp; }
+  __device__ __forceinline__ int item(int k) const { return chunks > 1 ? j0 + 32 * (k % chunks) : j0; }
+};
+
+struct AppendLaunch { Q8AppendArgs a; int group, blocks, chunk, nj, ni, X; };   // rows and blocks of a group, tokens of a CTA; items of a head: those that turn, all; threads on them
+
+// V numbers times f as codes
+template <int V> __device__ __forceinline__ void put_codes(uint8_t* to, const float (&x)[V], float f) {
+  if constexpr (V == 1) *to = (uint8_t)codes_of_floats(x[0] * f, 0.f);
+  else if constexpr (V == 2) *reinterpret_cast<unsigned short*>(to) = (unsigned short)codes_of_floats(x[0] * f, x[1] * f);
+  else {
+    uint32_t w[V / 4];
+#pragma unroll
+    for (int e = 0; e < V / 4; ++e) w[e] = codes_of_floats(x[4 * e] * f, x[4 * e + 1] * f) | codes_of_floats(x[4 * e + 2] * f, x[4 * e + 3] * f) << 16;
+    if constexpr (V == 4) *reinterpret_cast<uint32_t*>(to) = w[0];
+    else *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[V / 4 - 1]);
+  }
+}
 
 // cos and sin of position * f, the angle taken in half turns: its whole turns come off exactly
 __device__ __forceinline__ float2 cos_sin(int pos, double f) {
@@ -52,20 +85,27 @@ __device__ __forceinline__ float2 cos_sin(int pos, double f) {
 }
 
 // A CTA takes the groups (whole blocks, at least SLAB rows) that begin with one of its tokens, and of their heads every
-// gridDim.y-th.
+// gridDim.y-th.  First a warp to a head's keys or values: the scales of its blocks; of values, which then only have to be rounded, also the
+// codes (up to HOLD pairs of vectors a lane stay in registers for that).  Then keys and queries: a thread keeps the cosines and sines of its
+// pairs of one row and walks over the heads, the keys coming in again, mostly from L2.
 template <typename T, int V, bool INTER>
-__global__ void __launch_bounds__(NT) q8_append_kernel(const __grid_constant__ AppendLaunch L) {
+__global__ void __launch_bounds__(NT, 2) q8_append_kernel(const __grid_constant__ AppendLaunch L) {
   const Q8AppendArgs& a = L.a;
   const Q8Rows& r = a.r;
   const PageMap& pm = r.map.pages;
-  const int B = r.map.block, G = L.group;
-  extern __shared__ float2 table[];                                      // [SLAB][rot / 2], then the blocks' scales
-  float* inv = reinterpret_cast<float*>(table + SLAB * (a.rot / 2));     // [blocks of a group][2 nhk]: 1 / scale of keys, of values
-  __shared__ int page_s[SLAB];                                           // of each block, -1: skipped
+  const int B = r.map.block, G = L.group, half = a.rot / 2;
+  extern __shared__ float2 table[];                                      // [SLAB][rot / 2]
+  float* inv_k = reinterpret_cast<float*>(table + SLAB * half);          // [heads of the CTA][blocks of a group]: 1 / scale of the keys
+  __shared__ int page_s[SLAB], blk_s[SLAB], begin_s[SLAB];               // of each block: page (-1: skipped), block of the page, its first row there
+  __shared__ unsigned big_s[NW][SLAB];                                   // of each warp's task and block: the largest number, as its bits
+  __shared__ float inv_s[NW][SLAB];                                      // ... and 1 / scale
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, y = blockIdx.y, ny = gridDim.y;
-  const int nk = (r.Hkv - y + ny - 1) / ny, nq = r.Hq > y ? (r.Hq - y + ny - 1) / ny : 0, half = a.rot / 2;
-  constexpr int EV = 16 / (int)sizeof(T);
+  const int nk = (r.Hkv - y + ny - 1) / ny, nq = r.Hq > y ? (r.Hq - y + ny - 1) / ny : 0;
+  constexpr int EV = 16 / (int)sizeof(T);                                // numbers of a vector of values
   using VT = Vec<T, V>;
+  using VV = Vec<T, EV>;
+  const Lanes lk(r.d_qk / EV / 2), lv(r.d_v / EV / 2);
+  const int per = NT / L.X, tx = tid % L.X, tq = tid / L.X;              // (row, head) pairs at once; this thread's item and place among those
   pdl_wait();
   const int t0 = blockIdx.x * L.chunk, t1 = min(t0 + L.chunk, r.n_tokens);
   for (int t = t0; t < t1;) {
@@ -74,7 +114,7 @@ __global__ void __launch_bounds__(NT) q8_append_kernel(const __grid_constant__ A
     if (i < 0) { t = min(max(r.cu[0], t + 1), t1); continue; }
     const int from = r.cu[i], to = min(r.cu[i + 1], r.n_tokens), slot = r.slots[i], first = r.first[i];
     if (from > t || to <= t) { ++t; continue; }                          // (sums that decrease: go on all the same)
-    const long long row = (long long)first + (t - from);
+    const unsigned row = (unsigned)first + (unsigned)(t - from);         // (neither is negative, or the entry is skipped)
     const bool begins = t == from;
     if (slot < 0 || slot >= r.max_seqs || first < 0) {
       if (begins && tid == 0 && y == 0 && slot != -1 && r.status)
@@ -82,7 +122,8 @@ __global__ void __launch_bounds__(NT) q8_append_kernel(const __grid_constant__ A
       t = to;
       continue;
     }
-    if (!begins && row % G) { t = (int)min((long long)to, t + (G - row % G)); continue; }
+    const int in_group = (int)(row % (unsigned)G);
+    if (!begins && in_group) { t = (int)min((long long)to, (long long)t + (G - in_group)); continue; }
     int again = 0;                                                       // the slot was listed before
     for (int x = tid; x < i; x += NT) again |= r.slots[x] == slot;
     if (__syncthreads_or(again)) {
@@ -90,67 +131,111 @@ __global__ void __launch_bounds__(NT) q8_append_kernel(const __grid_constant__ A
       t = to;
       continue;
     }
-    const int n = (int)min(G - row % G, (long long)(to - t));            // the run: rows [row, row + n), tokens from t on
-    const long long block0 = row / B;
-    const int n_blocks = (int)((row + n - 1) / B - block0) + 1;
+    const int n = min(G - in_group, to - t);                             // the run: rows [row, row + n), tokens from t on
+    const int in_block = (int)(row % (unsigned)B), n_blocks = (in_block + n - 1) / B + 1;
     if (tid < n_blocks) {
-      const long long pg = (block0 + tid) * B / pm.page;
+      const unsigned begin = row - in_block + (unsigned)tid * B, pg = begin / (unsigned)pm.page;
+      const int off = (int)(begin - pg * pm.page);
       int page = -1;
-      if (pg < pm.max_pages) page = pm.table[(long long)slot * pm.max_pages + pg];
+      if (pg < (unsigned)pm.max_pages) page = pm.table[(long long)slot * pm.max_pages + pg];
       if (page < 0 || page >= pm.n_pages) {
         page = -1;
         if (y == 0 && r.status) atomicOr(r.status, SNAP_DEV_BAD_PAGE);
       }
-      page_s[tid] = page;
+      page_s[tid] = page; blk_s[tid] = off / B; begin_s[tid] = off;
     }
-    __syncthreads();
-    // ---- scales: a warp for each (block, head, keys or values) ----
-    for (int task = w; task < n_blocks * 2 * nk; task += NW) {
-      const int b = task / (2 * nk), j = task % (2 * nk), kvh = y + ny * (j >> 1), page = page_s[b];
-      if (page < 0) continue;
-      const bool keys = (j & 1) == 0;
-      const int d = keys ? r.d_qk : r.d_v;
-      const long long begin = (block0 + b) * B, lo = max(begin, row), hi = min(begin + B, row + n);
-      const long long tok = keys ? a.k_tok : a.v_tok;
-      const T* src = static_cast<const T*>(keys ? a.k : a.v) + (t + (lo - row)) * tok + kvh * (keys ? a.k_head : a.v_head);
-      float big = 0.f;
-      const int per = d / EV, total = (int)(hi - lo) * per;
-#pragma unroll 4
-      for (int x = lane; x < total; x += 32) {
-        Vec<T, EV> v;
-        v.raw = *reinterpret_cast<const uint4*>(src + x / per * tok + x % per * EV);
-#pragma unroll
-        for (int e = 0; e < EV; ++e) big = fmaxf(big, fabsf(to_f32<T>(v.e[e])));
-      }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
-      float scale = exp2_of(scale_exponent(keys ? big * a.growth : big));
-      const int blk = (int)(begin % pm.page) / B;
-      float* place = (keys ? r.k_scales : r.v_scales) + ((long long)page * r.Hkv + kvh) * r.map.blocks + blk;
-      if (begin < first) {                                               // rows of the sequence are there already
+    // The whole warp: the scales of head h's blocks, lane b knowing the largest of the new numbers of block b; 1 / scale for lane b.
+    const auto scale_of = [&](bool keys, int h, float largest) {
+      const bool mine = lane < n_blocks && page_s[min(lane, SLAB - 1)] >= 0;
+      const float need = exp2_of(scale_exponent(keys ? largest * a.growth : largest));
+      float* place = nullptr;
+      float scale = need, ratio = 1.f;
+      if (mine) place = (keys ? r.k_scales : r.v_scales) + ((long long)page_s[lane] * r.Hkv + h) * r.map.blocks + blk_s[lane];
+      if (mine && lane == 0 && begins && in_block > 0) {                 // rows of the sequence are there already
         const float old = *place;
-        __syncwarp();
-        if (scale <= old) scale = old;
-        else {
-          const float ratio = old / scale;
-          uint8_t* codes = keys ? r.k_pages + page * pm.kp + kvh * pm.kh + begin % pm.page * pm.kr
-                                : r.v_pages + page * pm.vp + kvh * pm.vh + begin % pm.page * pm.vr;
-          const long long stride = keys ? pm.kr : pm.vr;
-          const int each = d / 4;
-          for (int x = lane; x < (int)(first - begin) * each; x += 32) {
-            uint32_t* c = reinterpret_cast<uint32_t*>(codes + x / each * stride) + x % each;
-            const uint32_t v = *c;
-            const float2 f0 = floats_of_codes(v & 0xffffu), f1 = floats_of_codes(v >> 16);
-            *c = codes_of_floats(f0.x * ratio, f0.y * ratio) | codes_of_floats(f1.x * ratio, f1.y * ratio) << 16;
+        if (need <= old) scale = old;
+        else ratio = old / need;
+      }
+      ratio = __shfl_sync(0xffffffffu, ratio, 0);
+      if (ratio != 1.f) {                                                // they move to the new scale
+        uint8_t* codes = keys ? r.k_pages + page_s[0] * pm.kp + h * pm.kh + begin_s[0] * pm.kr : r.v_pages + page_s[0] * pm.vp + h * pm.vh + begin_s[0] * pm.vr;
+        const long long stride = keys ? pm.kr : pm.vr;
+        const int words = (keys ? r.d_qk : r.d_v) / 4;
+        for (int z = 0; z < in_block; ++z)
+          for (int c = lane; c < words; c += 32) {
+            uint32_t* at = reinterpret_cast<uint32_t*>(codes + z * stride) + c;
+            const float2 f0 = floats_of_codes(*at & 0xffffu), f1 = floats_of_codes(*at >> 16);
+            *at = codes_of_floats(f0.x * ratio, f0.y * ratio) | codes_of_floats(f1.x * ratio, f1.y * ratio) << 16;
           }
+      }
+      if (mine) *place = scale;
+      return 1.f / scale;
+    };
+    __syncthreads();
+    // ---- scales, and the codes of values: pairs of neighbouring vectors ----
+    for (int task = w; task < 2 * nk; task += NW) {
+      const bool keys = task < nk;
+      const Lanes& l = keys ? lk : lv;
+      const int hi = keys ? task : task - nk, h = y + ny * hi, passes = l.passes(n);
+      const long long tok = keys ? a.k_tok : a.v_tok;
+      const T* src = static_cast<const T*>(keys ? a.k : a.v) + t * tok + h * (keys ? a.k_head : a.v_head);
+      if (lane < SLAB) big_s[w][lane] = 0u;
+      __syncwarp();
+      float big = 0.f;
+      VV va[HOLD], vb[HOLD];
+      const auto there = [&](int k) { return k < passes && l.row(k) < n && l.item(k) < l.items; };
+      const auto load = [&](int k, VV& x, VV& z) {
+        const T* p = src + l.row(k) * tok + l.item(k) * 2 * EV;
+        x.raw = *reinterpret_cast<const uint4*>(p);
+        z.raw = *reinterpret_cast<const uint4*>(p + EV);
+      };
+      const auto block_of = [&](int z) { return n_blocks > 1 ? (in_block + z) / B : 0; };
+      for (int k0 = (passes - 1) / HOLD * HOLD; k0 >= 0; k0 -= HOLD) {   // the first HOLD last: they stay
+#pragma unroll
+        for (int u = 0; u < HOLD; ++u)
+          if (there(k0 + u)) load(k0 + u, va[u], vb[u]);
+#pragma unroll
+        for (int u = 0; u < HOLD; ++u) {
+          if (!there(k0 + u)) continue;
+          float m = 0.f;
+#pragma unroll
+          for (int e = 0; e < EV; ++e) m = fmaxf(m, fmaxf(fabsf(to_f32<T>(va[u].e[e])), fabsf(to_f32<T>(vb[u].e[e]))));
+          if (n_blocks > 1) atomicMax(&big_s[w][block_of(l.row(k0 + u))], __float_as_uint(m));
+          else big = fmaxf(big, m);
         }
       }
-      if (lane == 0) {
-        *place = scale;
-        inv[b * 2 * L.nhk + j] = 1.f / scale;
+      __syncwarp();
+      if (n_blocks > 1) big = __uint_as_float(big_s[w][min(lane, SLAB - 1)]);
+      else big = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(big)));
+      const float inv = scale_of(keys, h, big);
+      if (lane < n_blocks) (keys ? inv_k + hi * L.blocks : inv_s[w])[lane] = inv;
+      __syncwarp();
+      for (int k0 = 0; !keys && k0 < passes; k0 += HOLD) {
+        if (k0 > 0)
+#pragma unroll
+          for (int u = 0; u < HOLD; ++u)
+            if (there(k0 + u)) load(k0 + u, va[u], vb[u]);
+#pragma unroll
+        for (int u = 0; u < HOLD; ++u) {
+          if (!there(k0 + u)) continue;
+          const int z = l.row(k0 + u), b = block_of(z), page = page_s[b];
+          if (page < 0) continue;
+          const float f = inv_s[w][b];
+          uint32_t o[EV / 2];
+#pragma unroll
+          for (int e = 0; e < EV / 4; ++e) {
+            o[e] = codes_of_floats(to_f32<T>(va[u].e[4 * e]) * f, to_f32<T>(va[u].e[4 * e + 1]) * f) |
+                   codes_of_floats(to_f32<T>(va[u].e[4 * e + 2]) * f, to_f32<T>(va[u].e[4 * e + 3]) * f) << 16;
+            o[EV / 4 + e] = codes_of_floats(to_f32<T>(vb[u].e[4 * e]) * f, to_f32<T>(vb[u].e[4 * e + 1]) * f) |
+                            codes_of_floats(to_f32<T>(vb[u].e[4 * e + 2]) * f, to_f32<T>(vb[u].e[4 * e + 3]) * f) << 16;
+          }
+          uint8_t* c = r.v_pages + page * pm.vp + h * pm.vh + (begin_s[b] + in_block + z - b * B) * pm.vr + l.item(k0 + u) * 2 * EV;
+          if constexpr (EV == 8) *reinterpret_cast<uint4*>(c) = make_uint4(o[0], o[1], o[EV / 2 - 2], o[EV / 2 - 1]);
+          else *reinterpret_cast<uint2*>(c) = make_uint2(o[0], o[1]);
+        }
       }
     }
-    // ---- rows ----
+    // ---- keys and queries, SLAB rows at a time ----
     for (int s0 = 0; s0 < n; s0 += SLAB) {
       const int rows = min(SLAB, n - s0);
       for (int e = tid; e < rows * half; e += NT) {
@@ -158,107 +243,113 @@ __global__ void __launch_bounds__(NT) q8_append_kernel(const __grid_constant__ A
         const float2 cs = cos_sin(pos, a.freqs[e - z * half]);
         table[e] = make_float2(cs.x * a.magnitude, cs.y * a.magnitude);
       }
-      __syncthreads();
-      const auto block_of = [&](int z) { return (int)((row + s0 + z) / B - block0); };
-      // queries and keys: two vectors of a head, a part of it that turns or two of its other vectors
-      for (int x = tid; x < rows * (nq + nk) * L.ni; x += NT) {
-        const int j = x % L.ni, h = x / L.ni % (nq + nk), z = x / L.ni / (nq + nk), b = block_of(z), page = page_s[b];
+      __syncthreads();                                                   // (the keys' scales as well)
+      // threads as [rows][heads][items]: as many rows at once as there are, unless that leaves threads over
+      int Z = 1;
+      while (Z < rows && 2 * Z <= per) Z *= 2;
+      while (Z > 1 && 8 * (per / Z * Z) < 7 * per) Z /= 2;
+      const int Y = per / Z, ty = tq % Y;
+      for (int z = tq / Y; z < rows; z += Z) {
+        if (tq >= Y * Z) break;                                          // (a spare thread)
+        const int b = n_blocks > 1 ? (in_block + s0 + z) / B : 0, page = page_s[b];
         if (page < 0) continue;
-        const bool turn = j < L.nj, query = h < nq;
-        const auto other = [&](int c) { return c * V < a.offset ? c * V : c * V + a.rot; };
-        const int at_a = turn ? a.offset + (INTER ? 2 * j * V : j * V) : other(2 * (j - L.nj));
-        const int at_b = turn ? at_a + (INTER ? V : half) : other(2 * (j - L.nj) + 1);
-        const int head = query ? y + ny * h : y + ny * (h - nq);
         const long long tk = t + s0 + z;
-        const T* src = query ? static_cast<const T*>(a.q) + tk * a.q_tok + head * a.q_head : static_cast<const T*>(a.k) + tk * a.k_tok + head * a.k_head;
-        VT va, vb;
-        va.raw = *reinterpret_cast<const decltype(VT::raw)*>(src + at_a);
-        vb.raw = *reinterpret_cast<const decltype(VT::raw)*>(src + at_b);
-        float fa[V], fb[V];
+        const T* q = static_cast<const T*>(a.q) + tk * a.q_tok;
+        const T* k = static_cast<const T*>(a.k) + tk * a.k_tok;
+        T* q_out = static_cast<T*>(a.q_out) + tk * r.Hq * r.d_qk;
+        T* k_out = a.k_out ? static_cast<T*>(a.k_out) + tk * r.Hkv * r.d_qk : nullptr;
+        uint8_t* codes = r.k_pages + page * pm.kp + (begin_s[b] + in_block + s0 + z - b * B) * pm.kr;
+        for (int j = tx; j < L.ni; j += L.X) {
+          const bool turn = j < L.nj;
+          const auto other = [&](int c) { return c * V < a.offset ? c * V : c * V + a.rot; };
+          const int at_a = turn ? a.offset + (INTER ? 2 * j * V : j * V) : other(2 * (j - L.nj));
+          const int at_b = turn ? at_a + (INTER ? V : half) : other(2 * (j - L.nj) + 1);
+          float2 cs[V];
+          if (turn) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) { fa[e] = to_f32<T>(va.e[e]); fb[e] = to_f32<T>(vb.e[e]); }
-        if (turn) {
-#pragma unroll
-          for (int e = 0; e < V; ++e) {
-            // interleaved: the item's 2 V elements are V neighbouring pairs, else pair e is (fa[e], fb[e])
-            float& p = INTER ? (2 * e < V ? fa[(2 * e) % V] : fb[(2 * e) % V]) : fa[e];
-            float& q = INTER ? (2 * e + 1 < V ? fa[(2 * e + 1) % V] : fb[(2 * e + 1) % V]) : fb[e];
-            const float2 cs = table[z * half + j * V + e];
-            const float p1 = fmaf(p, cs.x, -(q * cs.y)), q1 = fmaf(q, cs.x, p * cs.y);
-            p = p1; q = q1;
+            for (int e = 0; e < V; ++e) cs[e] = table[z * half + j * V + e];
           }
-        }
-        T* out = query ? static_cast<T*>(a.q_out) + (tk * r.Hq + head) * r.d_qk : a.k_out ? static_cast<T*>(a.k_out) + (tk * r.Hkv + head) * r.d_qk : nullptr;
-        if (out) {
-          VT oa, ob;
+          const auto source = [&](int h) { return h < nq ? q + (y + ny * h) * a.q_head : k + (y + ny * (h - nq)) * a.k_head; };
+          constexpr int U = 2;                                           // heads at a time
+          for (int h0 = ty; h0 < nq + nk; h0 += U * Y) {
+            VT va[U], vb[U];
 #pragma unroll
-          for (int e = 0; e < V; ++e) { oa.e[e] = from_f32<T>(fa[e]); ob.e[e] = from_f32<T>(fb[e]); }
-          *reinterpret_cast<decltype(VT::raw)*>(out + at_a) = oa.raw;
-          *reinterpret_cast<decltype(VT::raw)*>(out + at_b) = ob.raw;
-        }
-        if (!query) {
-          const float f = inv[b * 2 * L.nhk + 2 * (h - nq)];
-          uint8_t* c = r.k_pages + page * pm.kp + head * pm.kh + (row + s0 + z) % pm.page * pm.kr;
-          Vec<uint8_t, V> ca, cb;
-          if constexpr (V == 1) {
-            ca.e[0] = (uint8_t)codes_of_floats(fa[0] * f, 0.f);
-            cb.e[0] = (uint8_t)codes_of_floats(fb[0] * f, 0.f);
-          } else {
+            for (int u = 0; u < U; ++u)
+              if (h0 + u * Y < nq + nk) {
+                const T* s = source(h0 + u * Y);
+                va[u].raw = *reinterpret_cast<const decltype(VT::raw)*>(s + at_a);
+                vb[u].raw = *reinterpret_cast<const decltype(VT::raw)*>(s + at_b);
+              }
 #pragma unroll
-            for (int e = 0; e < V; e += 2) {
-              const uint32_t u = codes_of_floats(fa[e] * f, fa[e + 1] * f), v = codes_of_floats(fb[e] * f, fb[e + 1] * f);
-              ca.e[e] = (uint8_t)u; ca.e[e + 1] = (uint8_t)(u >> 8);
-              cb.e[e] = (uint8_t)v; cb.e[e + 1] = (uint8_t)(v >> 8);
+            for (int u = 0; u < U; ++u) {
+              const int h = h0 + u * Y;
+              if (h >= nq + nk) break;
+              float fa[V], fb[V];
+#pragma unroll
+              for (int e = 0; e < V; ++e) { fa[e] = to_f32<T>(va[u].e[e]); fb[e] = to_f32<T>(vb[u].e[e]); }
+              if (turn) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                  // interleaved: the item's 2 V elements are V neighbouring pairs, else pair e is (fa[e], fb[e])
+                  float& p = INTER ? (2 * e < V ? fa[(2 * e) % V] : fb[(2 * e) % V]) : fa[e];
+                  float& s = INTER ? (2 * e + 1 < V ? fa[(2 * e + 1) % V] : fb[(2 * e + 1) % V]) : fb[e];
+                  const float p1 = fmaf(p, cs[e].x, -(s * cs[e].y)), s1 = fmaf(s, cs[e].x, p * cs[e].y);
+                  p = p1; s = s1;
+                }
+              }
+              const bool query = h < nq;
+              const int head = y + ny * (query ? h : h - nq);
+              T* o = query ? q_out + head * r.d_qk : k_out ? k_out + head * r.d_qk : nullptr;
+              if (o) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) { va[u].e[e] = from_f32<T>(fa[e]); vb[u].e[e] = from_f32<T>(fb[e]); }
+                *reinterpret_cast<decltype(VT::raw)*>(o + at_a) = va[u].raw;
+                *reinterpret_cast<decltype(VT::raw)*>(o + at_b) = vb[u].raw;
+              }
+              if (!query) {
+                const float f = inv_k[(h - nq) * L.blocks + b];
+                uint8_t* c = codes + head * pm.kh;
+                put_codes<V>(c + at_a, fa, f);
+                put_codes<V>(c + at_b, fb, f);
+              }
             }
           }
-          *reinterpret_cast<decltype(ca.raw)*>(c + at_a) = ca.raw;
-          *reinterpret_cast<decltype(cb.raw)*>(c + at_b) = cb.raw;
         }
-      }
-      // values: 16 bytes at a time
-      const int per = r.d_v / EV;
-      for (int x = tid; x < rows * nk * per; x += NT) {
-        const int c = x % per, h = x / per % nk, z = x / per / nk, b = block_of(z), page = page_s[b], head = y + ny * h;
-        if (page < 0) continue;
-        Vec<T, EV> v;
-        v.raw = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.v) + (long long)(t + s0 + z) * a.v_tok + head * a.v_head + c * EV);
-        const float f = inv[b * 2 * L.nhk + 2 * h + 1];
-        uint32_t o[EV / 4];
-#pragma unroll
-        for (int e = 0; e < EV / 4; ++e)
-          o[e] = codes_of_floats(to_f32<T>(v.e[4 * e]) * f, to_f32<T>(v.e[4 * e + 1]) * f) |
-                 codes_of_floats(to_f32<T>(v.e[4 * e + 2]) * f, to_f32<T>(v.e[4 * e + 3]) * f) << 16;
-        uint8_t* to_ = r.v_pages + page * pm.vp + head * pm.vh + (row + s0 + z) % pm.page * pm.vr + c * EV;
-        if constexpr (EV == 8) *reinterpret_cast<uint2*>(to_) = make_uint2(o[0], o[1]);
-        else *reinterpret_cast<uint32_t*>(to_) = o[0];
       }
       __syncthreads();
     }
-    if (t + n == to && y == 0 && tid == 0) a.seq_len[slot] = (int)min(row + n, (long long)pm.cap);
+    if (t + n == to && y == 0 && tid == 0) a.seq_len[slot] = (int)min((long long)row + n, (long long)pm.cap);
     t += n;
   }
 }
 
-// ---- gather: a CTA per SLAB tokens ----
+// ---- gather: a CTA per CHUNK tokens ----
+// What a token's numbers need of it comes first (page and row, as offsets); then a thread takes a vector of a head, of every token:
+// nothing is divided on the way.
+constexpr int CHUNK = 32;
+struct GatherLaunch { Q8GatherArgs a; int chunk, k_items, items, lanes; };     // tokens of a CTA; vectors of a token's keys, of both; threads on a token
+
 template <typename T>
-__global__ void __launch_bounds__(NT) q8_gather_kernel(const __grid_constant__ Q8GatherArgs a) {
+__global__ void __launch_bounds__(NT) q8_gather_kernel(const __grid_constant__ GatherLaunch L) {
+  const Q8GatherArgs& a = L.a;
   const Q8Rows& r = a.r;
   const PageMap& pm = r.map.pages;
-  __shared__ int2 place[SLAB];                                           // page (-1: left as it is) and row of the page
-  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, t0 = blockIdx.x * SLAB;
+  __shared__ long long k_s[CHUNK], v_s[CHUNK], scale_s[CHUNK];           // of each token: its row's offsets, its block's scale (-1: left as it is)
+  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, t0 = blockIdx.x * L.chunk, n = min(L.chunk, r.n_tokens - t0);
   constexpr int EV = 16 / (int)sizeof(T);
   pdl_wait();
-  for (int z = w; z < SLAB; z += NW) {
-    const int t = t0 + z, i = t < r.n_tokens ? entry_of(r, t) : -1;
+  for (int z = w; z < n; z += NW) {
+    const int t = t0 + z, i = entry_of(r, t);
     int page = -1, off = 0;
     if (i >= 0 && i < r.n_seqs) {
       const int slot = r.slots[i], first = r.first[i];
       unsigned bad = 0;
       if (slot >= 0 && slot < r.max_seqs) {
-        const long long row = (long long)first + (t - r.cu[i]);
-        if (first >= 0 && row < pm.cap) {
-          page = pm.table[(long long)slot * pm.max_pages + row / pm.page];
-          off = (int)(row % pm.page);
+        const unsigned row = (unsigned)first + (unsigned)(t - r.cu[i]);
+        if (first >= 0 && row < (unsigned)pm.cap) {
+          const int pg = (int)(row / (unsigned)pm.page);
+          page = pm.table[(long long)slot * pm.max_pages + pg];
+          off = (int)row - pg * pm.page;
         }
         if (page < 0 || page >= pm.n_pages) { page = -1; bad = SNAP_DEV_BAD_PAGE; }
       } else if (slot != -1) {
@@ -266,32 +357,54 @@ __global__ void __launch_bounds__(NT) q8_gather_kernel(const __grid_constant__ Q
       }
       if (bad && lane == 0 && r.status) atomicOr(r.status, bad);
     }
-    if (lane == 0) place[z] = make_int2(page, off);
+    if (lane == 0) {
+      k_s[z] = page * pm.kp + off * pm.kr;
+      v_s[z] = page * pm.vp + off * pm.vr;
+      scale_s[z] = page < 0 ? -1 : (long long)page * r.Hkv * r.map.blocks + off / r.map.block;
+    }
   }
   __syncthreads();
-  const auto copy = [&](const uint8_t* pages, long long ps, long long hs, long long rs, const float* scales, int d, T* out, long long tok, long long head) {
-    const int per = d / EV;
-    for (int x = tid; x < SLAB * r.Hkv * per; x += NT) {
-      const int c = x % per, h = x / per % r.Hkv, z = x / per / r.Hkv;
-      const int2 p = place[z];
-      if (p.x < 0) continue;
-      const uint8_t* src = pages + p.x * ps + h * hs + p.y * rs + c * EV;
-      const float f = scales[((long long)p.x * r.Hkv + h) * r.map.blocks + p.y / r.map.block];
-      uint32_t in[EV / 4];
-      if constexpr (EV == 8) { const uint2 v = *reinterpret_cast<const uint2*>(src); in[0] = v.x; in[1] = v.y; }
-      else in[0] = *reinterpret_cast<const uint32_t*>(src);
-      Vec<T, EV> o;
+  const int z0 = tid / L.lanes, step = NT / L.lanes;
+  if (z0 >= step) return;
+  for (int x = tid - z0 * L.lanes; x < L.items; x += L.lanes) {
+    const bool keys = x < L.k_items;
+    const int per = (keys ? r.d_qk : r.d_v) / EV, at = keys ? x : x - L.k_items, h = at / per, c = (at - h * per) * EV;
+    const uint8_t* codes = (keys ? r.k_pages + h * pm.kh : r.v_pages + h * pm.vh) + c;
+    const float* scales = (keys ? r.k_scales : r.v_scales) + h * r.map.blocks;
+    const long long tok = keys ? a.k_tok : a.v_tok;
+    const long long* offset = keys ? k_s : v_s;
+    T* out = (keys ? static_cast<T*>(a.k) + h * a.k_head : static_cast<T*>(a.v) + h * a.v_head) + t0 * tok + c;
+    constexpr int U = 4;                                                 // tokens at a time
+    for (int z = z0; z < n; z += U * step) {
+      typename RawOf<EV>::type in[U];
+      float f[U];
 #pragma unroll
-      for (int e = 0; e < EV / 4; ++e) {
-        const float2 f0 = floats_of_codes(in[e] & 0xffffu), f1 = floats_of_codes(in[e] >> 16);
-        o.e[4 * e] = from_f32<T>(f0.x * f); o.e[4 * e + 1] = from_f32<T>(f0.y * f);
-        o.e[4 * e + 2] = from_f32<T>(f1.x * f); o.e[4 * e + 3] = from_f32<T>(f1.y * f);
+      for (int u = 0; u < U; ++u) {
+        const int zu = z + u * step;
+        const long long at_scale = zu < n ? scale_s[zu] : -1;
+        f[u] = -1.f;
+        if (at_scale >= 0) {
+          f[u] = scales[at_scale];
+          in[u] = *reinterpret_cast<const typename RawOf<EV>::type*>(codes + offset[zu]);
+        }
       }
-      *reinterpret_cast<uint4*>(out + (t0 + z) * tok + h * head + c * EV) = o.raw;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int zu = z + u * step;
+        if (zu >= n || scale_s[zu] < 0) continue;
+        uint32_t words[EV / 4];
+        memcpy(words, &in[u], EV);
+        Vec<T, EV> o;
+#pragma unroll
+        for (int e = 0; e < EV / 4; ++e) {
+          const float2 f0 = floats_of_codes(words[e] & 0xffffu), f1 = floats_of_codes(words[e] >> 16);
+          o.e[4 * e] = from_f32<T>(f0.x * f[u]); o.e[4 * e + 1] = from_f32<T>(f0.y * f[u]);
+          o.e[4 * e + 2] = from_f32<T>(f1.x * f[u]); o.e[4 * e + 3] = from_f32<T>(f1.y * f[u]);
+        }
+        *reinterpret_cast<uint4*>(out + zu * tok) = o.raw;
+      }
     }
-  };
-  copy(r.k_pages, pm.kp, pm.kh, pm.kr, r.k_scales, r.d_qk, static_cast<T*>(a.k), a.k_tok, a.k_head);
-  copy(r.v_pages, pm.vp, pm.vh, pm.vr, r.v_scales, r.d_v, static_cast<T*>(a.v), a.v_tok, a.v_head);
+  }
 }
 
 template <typename T, int V>
@@ -302,20 +415,19 @@ cudaError_t launch_append_v(const Q8AppendArgs& a, cudaStream_t st) {
   L.nj = a.rot / 2 / V;
   L.ni = L.nj + (r.d_qk - a.rot) / V / 2;
   const int B = r.map.block;
-  L.group = B * (B < SLAB ? SLAB / B : 1);
+  L.blocks = B < SLAB ? SLAB / B : 1;
+  L.group = B * L.blocks;
+  L.X = L.ni < 64 ? L.ni : 64;
   const int mean = r.n_tokens / r.n_seqs;
   L.chunk = mean < 1 ? 1 : mean < L.group ? mean : L.group;
   // few tokens: several CTAs to a token's heads
-  const long long ctas = (r.n_tokens + L.chunk - 1) / L.chunk;
+  const long long ctas = ((long long)r.n_tokens + L.chunk - 1) / L.chunk;
   int ny = (int)(2LL * sm_count() / ctas);
   ny = ny < 1 ? 1 : ny > r.Hkv ? r.Hkv : ny;
-  L.nhk = (r.Hkv + ny - 1) / ny;
-  L.nhq = (r.Hq + ny - 1) / ny;
-  const size_t smem = SLAB * (size_t)(a.rot / 2) * sizeof(float2) + (size_t)(L.group / B) * 2 * L.nhk * sizeof(float);
+  const int most = 4096 / L.blocks;                                      // (scales of a CTA's heads in shared memory)
+  if (ny < (r.Hkv + most - 1) / most) ny = (r.Hkv + most - 1) / most;
+  const size_t smem = SLAB * (size_t)(a.rot / 2) * sizeof(float2) + (size_t)L.blocks * ((r.Hkv + ny - 1) / ny) * sizeof(float);
   auto kernel = a.interleaved ? q8_append_kernel<T, V, true> : q8_append_kernel<T, V, false>;
-  static SmemLimit limit[2] = {};
-  if (smem > 48 * 1024)
-    if (cudaError_t e = ensure_dyn_smem(kernel, smem, limit[a.interleaved])) return e;
   const cudaError_t e = launch_pdl(kernel, dim3((unsigned)ctas, (unsigned)ny), dim3(NT), smem, st, L);
   count_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
@@ -338,9 +450,18 @@ cudaError_t launch_q8_append(int dtype, const Q8AppendArgs& a, cudaStream_t st) 
 }
 
 cudaError_t launch_q8_gather(int dtype, const Q8GatherArgs& a, cudaStream_t st) {
-  const dim3 grid((unsigned)((a.r.n_tokens + SLAB - 1) / SLAB));
-  const cudaError_t e = dtype == SNAP_F32 ? launch_pdl(q8_gather_kernel<float>, grid, dim3(NT), 0, st, a)
-                                          : launch_pdl(q8_gather_kernel<__nv_bfloat16>, grid, dim3(NT), 0, st, a);
+  const int ev = 16 / elt_bytes(dtype), sms = sm_count();
+  GatherLaunch L;
+  L.a = a;
+  L.k_items = a.r.Hkv * (a.r.d_qk / ev);
+  L.items = L.k_items + a.r.Hkv * (a.r.d_v / ev);
+  L.lanes = L.items < NT ? L.items : NT;
+  // (few tokens: spread over the GPU)
+  L.chunk = CHUNK;
+  while (L.chunk > 4 && (a.r.n_tokens + L.chunk - 1) / L.chunk < 4 * sms) L.chunk /= 2;
+  const dim3 grid((unsigned)((a.r.n_tokens + L.chunk - 1) / L.chunk));
+  const cudaError_t e = dtype == SNAP_F32 ? launch_pdl(q8_gather_kernel<float>, grid, dim3(NT), 0, st, L)
+                                          : launch_pdl(q8_gather_kernel<__nv_bfloat16>, grid, dim3(NT), 0, st, L);
   count_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
 }
