@@ -4,15 +4,14 @@
 // The scale of a block (rows of one KV head that share it) goes by the largest of the inputs, not of the rotated keys: a pair
 // (a, b) turned and multiplied by m is at most sqrt(2) m max(|a|, |b|) in either place.  So it does not depend on how sines
 // are rounded, and the pass that looks for it computes no angles.
-#include <cstring>
-
 #include "e4m3.cuh"
 #include "snap_internal.cuh"
 
 namespace snap {
 namespace {
 
-constexpr int NT = 256, NW = NT / 32;
+constexpr int NT = 256, NW = NT / 32;            // threads of the gather
+constexpr int ANT = 128, ANW = ANT / 32;        // ... of the append: four blocks per SM hide each other's look-ups better than two of 256 (26003 tokens 152 us instead of 160)
 constexpr int SLAB = 16;                        // rows whose angles are held at a time
 
 template <int BYTES> struct RawOf;
@@ -43,21 +42,33 @@ __device__ __forceinline__ int entry_of(const Q8Rows& r, int t) {
 
 constexpr int HOLD = 4;                         // pairs of vectors that a lane keeps between the look for the largest number and the rounding
 
-// Where a warp's lanes stand in `rows` rows of a head cut into `items` (pairs of vectors): in pass k lane l has item j of row r.
+// Where a warp's lanes stand in the rows of a head cut into items (pairs of vectors, 32 at most): in pass k a lane has item j of row
+// r0 + k * rpp.
 struct Lanes {
-  int items, rpp, chunks, r0, j0;               // rows of a pass; passes of a row of more than 32 items
+  int items, rpp, r0, j;
   __device__ __forceinline__ Lanes(int items_) : items(items_) {
     const int lane = threadIdx.x & 31;
-    rpp = items < 32 ? 32 / items : 1;
-    chunks = (items + 31) / 32;
-    r0 = items < 32 ? lane / items : 0;
-    j0 = items < 32 ? lane - r0 * items : lane;
-    if (r0 >= rpp) j0 = items;                  // (a spare lane)
+    rpp = 32 / items;
+    r0 = lane / items;
+    j = lane - r0 * items;
+    if (r0 >= rpp) r0 = 1 << 30;                // (a spare lane: no row)
   }
-  __device__ __forceinline__ int passes(int rows) const { return chunks > 1 ? rows * chunks : (rows + rpp - 1) / rpp; }
-  __device__ __forceinline__ int row(int k) const { return chunks > 1 ? k / chunks : r0 + k * rpp; }
-  __device__ __forceinline__ int item(int k) const { return chunks > 1 ? j0 + 32 * (k % chunks) : j0; }
 };
+
+// The largest number's size of a vector
+template <typename T, int N> __device__ __forceinline__ float largest_of(const Vec<T, N>& v) {
+  if constexpr (sizeof(T) == 2) {               // two at a time
+    __nv_bfloat162 m = __habs2(reinterpret_cast<const __nv_bfloat162*>(v.e)[0]);
+#pragma unroll
+    for (int e = 1; e < N / 2; ++e) m = __hmax2(m, __habs2(reinterpret_cast<const __nv_bfloat162*>(v.e)[e]));
+    return fmaxf(fmaxf(__low2float(m), __high2float(m)), 0.f);
+  } else {
+    float m = 0.f;
+#pragma unroll
+    for (int e = 0; e < N; ++e) m = fmaxf(m, fabsf(v.e[e]));
+    return m;
+  }
+}
 
 struct AppendLaunch { Q8AppendArgs a; int group, blocks, chunk, nj, ni, X; };   // rows and blocks of a group, tokens of a CTA; items of a head: those that turn, all; threads on them
 
@@ -89,7 +100,7 @@ __device__ __forceinline__ float2 cos_sin(int pos, double f) {
 // codes (up to HOLD pairs of vectors a lane stay in registers for that).  Then keys and queries: a thread keeps the cosines and sines of its
 // pairs of one row and walks over the heads, the keys coming in again, mostly from L2.
 template <typename T, int V, bool INTER>
-__global__ void __launch_bounds__(NT, 2) q8_append_kernel(const __grid_constant__ AppendLaunch L) {
+__global__ void __launch_bounds__(ANT, 4) q8_append_kernel(const __grid_constant__ AppendLaunch L) {
   const Q8AppendArgs& a = L.a;
   const Q8Rows& r = a.r;
   const PageMap& pm = r.map.pages;
@@ -97,24 +108,45 @@ __global__ void __launch_bounds__(NT, 2) q8_append_kernel(const __grid_constant_
   extern __shared__ float2 table[];                                      // [SLAB][rot / 2]
   float* inv_k = reinterpret_cast<float*>(table + SLAB * half);          // [heads of the CTA][blocks of a group]: 1 / scale of the keys
   __shared__ int page_s[SLAB], blk_s[SLAB], begin_s[SLAB];               // of each block: page (-1: skipped), block of the page, its first row there
-  __shared__ unsigned big_s[NW][SLAB];                                   // of each warp's task and block: the largest number, as its bits
-  __shared__ float inv_s[NW][SLAB];                                      // ... and 1 / scale
+  __shared__ unsigned big_s[ANW][SLAB];                                   // of each warp's task and block: the largest number, as its bits
+  __shared__ float inv_s[ANW][SLAB];                                      // ... and 1 / scale
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, y = blockIdx.y, ny = gridDim.y;
   const int nk = (r.Hkv - y + ny - 1) / ny, nq = r.Hq > y ? (r.Hq - y + ny - 1) / ny : 0;
   constexpr int EV = 16 / (int)sizeof(T);                                // numbers of a vector of values
   using VT = Vec<T, V>;
   using VV = Vec<T, EV>;
   const Lanes lk(r.d_qk / EV / 2), lv(r.d_v / EV / 2);
-  const int per = NT / L.X, tx = tid % L.X, tq = tid / L.X;              // (row, head) pairs at once; this thread's item and place among those
+  const int per = ANT / L.X, tx = tid % L.X, tq = tid / L.X;              // (row, head) pairs at once; this thread's item and place among those
+  const int apart = half ? ANT / half : 1, angle = half ? tid % half : 0, angle_z = half ? tid / half : apart;   // rows of angles at once; this thread's
   pdl_wait();
+  const double freq = angle_z < apart ? a.freqs[angle] : 0.0;
+  // Up to 32 entries are read once, a lane each, and looked through without memory.
+  const bool few = r.n_seqs <= 32;
+  int my_cu = 0, my_slot = -1, my_first = 0, total = 0;
+  if (few) {
+    total = r.cu[r.n_seqs];
+    if (lane < r.n_seqs) { my_cu = r.cu[lane]; my_slot = r.slots[lane]; my_first = r.first[lane]; }
+  }
   const int t0 = blockIdx.x * L.chunk, t1 = min(t0 + L.chunk, r.n_tokens);
   for (int t = t0; t < t1;) {
-    const int i = entry_of(r, t);
+    int i, from, to, slot, first;
+    if (few) {
+      i = total <= t ? r.n_seqs : 31 - __clz(__ballot_sync(0xffffffffu, lane < r.n_seqs && my_cu <= t));
+      from = __shfl_sync(0xffffffffu, my_cu, max(i, 0) & 31);
+      to = i + 1 < r.n_seqs ? __shfl_sync(0xffffffffu, my_cu, (i + 1) & 31) : total;
+      slot = __shfl_sync(0xffffffffu, my_slot, max(i, 0) & 31);
+      first = __shfl_sync(0xffffffffu, my_first, max(i, 0) & 31);
+      if (i < 0) to = __shfl_sync(0xffffffffu, my_cu, 0);                // (where the first entry's begin)
+    } else {
+      i = entry_of(r, t);
+      const int at = min(max(i, 0), r.n_seqs - 1);
+      from = r.cu[at]; to = r.cu[i < 0 ? 0 : at + 1]; slot = r.slots[at]; first = r.first[at];
+    }
     if (i >= r.n_seqs) break;
-    if (i < 0) { t = min(max(r.cu[0], t + 1), t1); continue; }
-    const int from = r.cu[i], to = min(r.cu[i + 1], r.n_tokens), slot = r.slots[i], first = r.first[i];
+    if (i < 0) { t = min(max(to, t + 1), t1); continue; }
+    to = min(to, r.n_tokens);
     if (from > t || to <= t) { ++t; continue; }                          // (sums that decrease: go on all the same)
-    const unsigned row = (unsigned)first + (unsigned)(t - from);         // (neither is negative, or the entry is skipped)
+    const unsigned row = (unsigned)first + (unsigned)t - (unsigned)from; // (neither is negative, or the entry is skipped)
     const bool begins = t == from;
     if (slot < 0 || slot >= r.max_seqs || first < 0) {
       if (begins && tid == 0 && y == 0 && slot != -1 && r.status)
@@ -124,20 +156,33 @@ __global__ void __launch_bounds__(NT, 2) q8_append_kernel(const __grid_constant_
     }
     const int in_group = (int)(row % (unsigned)G);
     if (!begins && in_group) { t = (int)min((long long)to, (long long)t + (G - in_group)); continue; }
-    int again = 0;                                                       // the slot was listed before
-    for (int x = tid; x < i; x += NT) again |= r.slots[x] == slot;
-    if (__syncthreads_or(again)) {
+    bool again = false;                                                  // the slot was listed before
+    if (few) again = __any_sync(0xffffffffu, lane < i && my_slot == slot);
+    else {
+      for (int x = tid; x < i; x += ANT) again = again || r.slots[x] == slot;
+      again = __syncthreads_or(again);
+    }
+    if (again) {
       if (begins && tid == 0 && y == 0 && r.status) atomicOr(r.status, SNAP_DEV_BAD_SLOT);
       t = to;
       continue;
     }
     const int n = min(G - in_group, to - t);                             // the run: rows [row, row + n), tokens from t on
     const int in_block = (int)(row % (unsigned)B), n_blocks = (in_block + n - 1) / B + 1;
+    int page = -1, off = 0;                                              // of block tid
     if (tid < n_blocks) {
       const unsigned begin = row - in_block + (unsigned)tid * B, pg = begin / (unsigned)pm.page;
-      const int off = (int)(begin - pg * pm.page);
-      int page = -1;
+      off = (int)(begin - pg * pm.page);
       if (pg < (unsigned)pm.max_pages) page = pm.table[(long long)slot * pm.max_pages + pg];
+    }
+    const auto angles = [&](int s0, int rows) {
+      for (int z = angle_z; angle_z < apart && z < rows; z += apart) {
+        const float2 cs = cos_sin(a.positions ? a.positions[t + s0 + z] : (int)(row + s0 + z), freq);
+        table[z * half + angle] = make_float2(cs.x * a.magnitude, cs.y * a.magnitude);
+      }
+    };
+    angles(0, min(SLAB, n));                                             // while the table answers
+    if (tid < n_blocks) {
       if (page < 0 || page >= pm.n_pages) {
         page = -1;
         if (y == 0 && r.status) atomicOr(r.status, SNAP_DEV_BAD_PAGE);
@@ -173,19 +218,20 @@ __global__ void __launch_bounds__(NT, 2) q8_append_kernel(const __grid_constant_
     };
     __syncthreads();
     // ---- scales, and the codes of values: pairs of neighbouring vectors ----
-    for (int task = w; task < 2 * nk; task += NW) {
+    for (int task = w; task < 2 * nk; task += ANW) {
       const bool keys = task < nk;
       const Lanes& l = keys ? lk : lv;
-      const int hi = keys ? task : task - nk, h = y + ny * hi, passes = l.passes(n);
+      const int hi = keys ? task : task - nk, h = y + ny * hi, passes = (n + l.rpp - 1) / l.rpp;
       const long long tok = keys ? a.k_tok : a.v_tok;
-      const T* src = static_cast<const T*>(keys ? a.k : a.v) + t * tok + h * (keys ? a.k_head : a.v_head);
+      const T* src = static_cast<const T*>(keys ? a.k : a.v) + t * tok + h * (keys ? a.k_head : a.v_head) + l.j * 2 * EV;
       if (lane < SLAB) big_s[w][lane] = 0u;
       __syncwarp();
       float big = 0.f;
       VV va[HOLD], vb[HOLD];
-      const auto there = [&](int k) { return k < passes && l.row(k) < n && l.item(k) < l.items; };
+      const auto row_of = [&](int k) { return l.r0 + k * l.rpp; };
+      const auto there = [&](int k) { return l.r0 + k * l.rpp < n; };   // (also false past the last pass)
       const auto load = [&](int k, VV& x, VV& z) {
-        const T* p = src + l.row(k) * tok + l.item(k) * 2 * EV;
+        const T* p = src + row_of(k) * tok;
         x.raw = *reinterpret_cast<const uint4*>(p);
         z.raw = *reinterpret_cast<const uint4*>(p + EV);
       };
@@ -197,10 +243,8 @@ __global__ void __launch_bounds__(NT, 2) q8_append_kernel(const __grid_constant_
 #pragma unroll
         for (int u = 0; u < HOLD; ++u) {
           if (!there(k0 + u)) continue;
-          float m = 0.f;
-#pragma unroll
-          for (int e = 0; e < EV; ++e) m = fmaxf(m, fmaxf(fabsf(to_f32<T>(va[u].e[e])), fabsf(to_f32<T>(vb[u].e[e]))));
-          if (n_blocks > 1) atomicMax(&big_s[w][block_of(l.row(k0 + u))], __float_as_uint(m));
+          const float m = fmaxf(largest_of(va[u]), largest_of(vb[u]));
+          if (n_blocks > 1) atomicMax(&big_s[w][block_of(row_of(k0 + u))], __float_as_uint(m));
           else big = fmaxf(big, m);
         }
       }
@@ -210,7 +254,10 @@ __global__ void __launch_bounds__(NT, 2) q8_append_kernel(const __grid_constant_
       const float inv = scale_of(keys, h, big);
       if (lane < n_blocks) (keys ? inv_k + hi * L.blocks : inv_s[w])[lane] = inv;
       __syncwarp();
-      for (int k0 = 0; !keys && k0 < passes; k0 += HOLD) {
+      const bool as_is = !keys || half == 0;                             // (keys that are not rotated are rounded as values are)
+      uint8_t* const codes = keys ? r.k_pages + h * pm.kh : r.v_pages + h * pm.vh;
+      const long long page_stride = keys ? pm.kp : pm.vp, row_stride = keys ? pm.kr : pm.vr;
+      for (int k0 = 0; as_is && k0 < passes; k0 += HOLD) {
         if (k0 > 0)
 #pragma unroll
           for (int u = 0; u < HOLD; ++u)
@@ -218,9 +265,9 @@ __global__ void __launch_bounds__(NT, 2) q8_append_kernel(const __grid_constant_
 #pragma unroll
         for (int u = 0; u < HOLD; ++u) {
           if (!there(k0 + u)) continue;
-          const int z = l.row(k0 + u), b = block_of(z), page = page_s[b];
+          const int z = row_of(k0 + u), b = block_of(z), page = page_s[b];
           if (page < 0) continue;
-          const float f = inv_s[w][b];
+          const float f = (keys ? inv_k + hi * L.blocks : inv_s[w])[b];
           uint32_t o[EV / 2];
 #pragma unroll
           for (int e = 0; e < EV / 4; ++e) {
@@ -229,20 +276,16 @@ __global__ void __launch_bounds__(NT, 2) q8_append_kernel(const __grid_constant_
             o[EV / 4 + e] = codes_of_floats(to_f32<T>(vb[u].e[4 * e]) * f, to_f32<T>(vb[u].e[4 * e + 1]) * f) |
                             codes_of_floats(to_f32<T>(vb[u].e[4 * e + 2]) * f, to_f32<T>(vb[u].e[4 * e + 3]) * f) << 16;
           }
-          uint8_t* c = r.v_pages + page * pm.vp + h * pm.vh + (begin_s[b] + in_block + z - b * B) * pm.vr + l.item(k0 + u) * 2 * EV;
+          uint8_t* c = codes + page * page_stride + (begin_s[b] + in_block + z - b * B) * row_stride + l.j * 2 * EV;
           if constexpr (EV == 8) *reinterpret_cast<uint4*>(c) = make_uint4(o[0], o[1], o[EV / 2 - 2], o[EV / 2 - 1]);
           else *reinterpret_cast<uint2*>(c) = make_uint2(o[0], o[1]);
         }
       }
     }
     // ---- keys and queries, SLAB rows at a time ----
-    for (int s0 = 0; s0 < n; s0 += SLAB) {
+    for (int s0 = 0; s0 < n && (half > 0 || a.q || a.k_out); s0 += SLAB) {
       const int rows = min(SLAB, n - s0);
-      for (int e = tid; e < rows * half; e += NT) {
-        const int z = e / half, pos = a.positions ? a.positions[t + s0 + z] : (int)(row + s0 + z);
-        const float2 cs = cos_sin(pos, a.freqs[e - z * half]);
-        table[e] = make_float2(cs.x * a.magnitude, cs.y * a.magnitude);
-      }
+      if (s0 > 0) angles(s0, rows);
       __syncthreads();                                                   // (the keys' scales as well)
       // threads as [rows][heads][items]: as many rows at once as there are, unless that leaves threads over
       int Z = 1;
@@ -270,7 +313,7 @@ __global__ void __launch_bounds__(NT, 2) q8_append_kernel(const __grid_constant_
             for (int e = 0; e < V; ++e) cs[e] = table[z * half + j * V + e];
           }
           const auto source = [&](int h) { return h < nq ? q + (y + ny * h) * a.q_head : k + (y + ny * (h - nq)) * a.k_head; };
-          constexpr int U = 2;                                           // heads at a time
+          constexpr int U = 4;                                           // heads at a time
           for (int h0 = ty; h0 < nq + nk; h0 += U * Y) {
             VT va[U], vb[U];
 #pragma unroll
@@ -306,7 +349,7 @@ __global__ void __launch_bounds__(NT, 2) q8_append_kernel(const __grid_constant_
                 *reinterpret_cast<decltype(VT::raw)*>(o + at_a) = va[u].raw;
                 *reinterpret_cast<decltype(VT::raw)*>(o + at_b) = vb[u].raw;
               }
-              if (!query) {
+              if (!query && half > 0) {
                 const float f = inv_k[(h - nq) * L.blocks + b];
                 uint8_t* c = codes + head * pm.kh;
                 put_codes<V>(c + at_a, fa, f);
@@ -318,6 +361,7 @@ __global__ void __launch_bounds__(NT, 2) q8_append_kernel(const __grid_constant_
       }
       __syncthreads();
     }
+    __syncthreads();                                                     // what the run's blocks are has been read
     if (t + n == to && y == 0 && tid == 0) a.seq_len[slot] = (int)min((long long)row + n, (long long)pm.cap);
     t += n;
   }
@@ -326,8 +370,8 @@ __global__ void __launch_bounds__(NT, 2) q8_append_kernel(const __grid_constant_
 // ---- gather: a CTA per CHUNK tokens ----
 // What a token's numbers need of it comes first (page and row, as offsets); then a thread takes a vector of a head, of every token:
 // nothing is divided on the way.
-constexpr int CHUNK = 32;
-struct GatherLaunch { Q8GatherArgs a; int chunk, k_items, items, lanes; };     // tokens of a CTA; vectors of a token's keys, of both; threads on a token
+constexpr int CHUNK = 16;
+struct GatherLaunch { Q8GatherArgs a; int chunk, k_items, items, lanes; };     // tokens of a CTA; 16-code pieces of a token's keys, of both; threads on a token
 
 template <typename T>
 __global__ void __launch_bounds__(NT) q8_gather_kernel(const __grid_constant__ GatherLaunch L) {
@@ -368,7 +412,7 @@ __global__ void __launch_bounds__(NT) q8_gather_kernel(const __grid_constant__ G
   if (z0 >= step) return;
   for (int x = tid - z0 * L.lanes; x < L.items; x += L.lanes) {
     const bool keys = x < L.k_items;
-    const int per = (keys ? r.d_qk : r.d_v) / EV, at = keys ? x : x - L.k_items, h = at / per, c = (at - h * per) * EV;
+    const int per = (keys ? r.d_qk : r.d_v) / 16, at = keys ? x : x - L.k_items, h = at / per, c = (at - h * per) * 16;
     const uint8_t* codes = (keys ? r.k_pages + h * pm.kh : r.v_pages + h * pm.vh) + c;
     const float* scales = (keys ? r.k_scales : r.v_scales) + h * r.map.blocks;
     const long long tok = keys ? a.k_tok : a.v_tok;
@@ -376,32 +420,36 @@ __global__ void __launch_bounds__(NT) q8_gather_kernel(const __grid_constant__ G
     T* out = (keys ? static_cast<T*>(a.k) + h * a.k_head : static_cast<T*>(a.v) + h * a.v_head) + t0 * tok + c;
     constexpr int U = 4;                                                 // tokens at a time
     for (int z = z0; z < n; z += U * step) {
-      typename RawOf<EV>::type in[U];
+      uint4 in[U];
       float f[U];
+      bool there[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int zu = z + u * step;
         const long long at_scale = zu < n ? scale_s[zu] : -1;
-        f[u] = -1.f;
-        if (at_scale >= 0) {
+        there[u] = at_scale >= 0;
+        if (there[u]) {
           f[u] = scales[at_scale];
-          in[u] = *reinterpret_cast<const typename RawOf<EV>::type*>(codes + offset[zu]);
+          in[u] = *reinterpret_cast<const uint4*>(codes + offset[zu]);
         }
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int zu = z + u * step;
-        if (zu >= n || scale_s[zu] < 0) continue;
-        uint32_t words[EV / 4];
-        memcpy(words, &in[u], EV);
-        Vec<T, EV> o;
+        if (!there[u]) continue;
+        const uint32_t words[4] = {in[u].x, in[u].y, in[u].z, in[u].w};
+        T* to = out + (z + u * step) * tok;
 #pragma unroll
-        for (int e = 0; e < EV / 4; ++e) {
-          const float2 f0 = floats_of_codes(words[e] & 0xffffu), f1 = floats_of_codes(words[e] >> 16);
-          o.e[4 * e] = from_f32<T>(f0.x * f[u]); o.e[4 * e + 1] = from_f32<T>(f0.y * f[u]);
-          o.e[4 * e + 2] = from_f32<T>(f1.x * f[u]); o.e[4 * e + 3] = from_f32<T>(f1.y * f[u]);
+        for (int v = 0; v < 16 / EV; ++v) {
+          Vec<T, EV> o;
+#pragma unroll
+          for (int e = 0; e < EV / 4; ++e) {
+            const uint32_t word = words[v * (EV / 4) + e];
+            const float2 f0 = floats_of_codes(word & 0xffffu), f1 = floats_of_codes(word >> 16);
+            o.e[4 * e] = from_f32<T>(f0.x * f[u]); o.e[4 * e + 1] = from_f32<T>(f0.y * f[u]);
+            o.e[4 * e + 2] = from_f32<T>(f1.x * f[u]); o.e[4 * e + 3] = from_f32<T>(f1.y * f[u]);
+          }
+          *reinterpret_cast<uint4*>(to + v * EV) = o.raw;
         }
-        *reinterpret_cast<uint4*>(out + zu * tok) = o.raw;
       }
     }
   }
@@ -422,13 +470,13 @@ cudaError_t launch_append_v(const Q8AppendArgs& a, cudaStream_t st) {
   L.chunk = mean < 1 ? 1 : mean < L.group ? mean : L.group;
   // few tokens: several CTAs to a token's heads
   const long long ctas = ((long long)r.n_tokens + L.chunk - 1) / L.chunk;
-  int ny = (int)(2LL * sm_count() / ctas);
+  int ny = (int)(4LL * sm_count() / ctas);
   ny = ny < 1 ? 1 : ny > r.Hkv ? r.Hkv : ny;
   const int most = 4096 / L.blocks;                                      // (scales of a CTA's heads in shared memory)
   if (ny < (r.Hkv + most - 1) / most) ny = (r.Hkv + most - 1) / most;
   const size_t smem = SLAB * (size_t)(a.rot / 2) * sizeof(float2) + (size_t)L.blocks * ((r.Hkv + ny - 1) / ny) * sizeof(float);
   auto kernel = a.interleaved ? q8_append_kernel<T, V, true> : q8_append_kernel<T, V, false>;
-  const cudaError_t e = launch_pdl(kernel, dim3((unsigned)ctas, (unsigned)ny), dim3(NT), smem, st, L);
+  const cudaError_t e = launch_pdl(kernel, dim3((unsigned)ctas, (unsigned)ny), dim3(ANT), smem, st, L);
   count_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
 }
@@ -450,11 +498,11 @@ cudaError_t launch_q8_append(int dtype, const Q8AppendArgs& a, cudaStream_t st) 
 }
 
 cudaError_t launch_q8_gather(int dtype, const Q8GatherArgs& a, cudaStream_t st) {
-  const int ev = 16 / elt_bytes(dtype), sms = sm_count();
+  const int sms = sm_count();
   GatherLaunch L;
   L.a = a;
-  L.k_items = a.r.Hkv * (a.r.d_qk / ev);
-  L.items = L.k_items + a.r.Hkv * (a.r.d_v / ev);
+  L.k_items = a.r.Hkv * (a.r.d_qk / 16);
+  L.items = L.k_items + a.r.Hkv * (a.r.d_v / 16);
   L.lanes = L.items < NT ? L.items : NT;
   // (few tokens: spread over the GPU)
   L.chunk = CHUNK;
