@@ -2,7 +2,7 @@
 //
 // Requests are served as if one after the other; the prefix sums of what each of them wants (pages it gives back, tokens,
 // pages it misses) tell which are served and where each one's pages lie in the stack, so that all of it is parallel but for one scan.
-// One thread-block cluster does the call, its phases apart by cluster barriers: count, scan (one CTA), move (pages given back,
+// One thread-block cluster, or one CTA, does the call, its phases apart by barriers: count, scan (one CTA), move (pages given back,
 // table rows, lists of tokens), fill (the granted pages, read from a stack that is then complete).
 #include <climits>
 
@@ -11,8 +11,9 @@
 namespace snap {
 namespace {
 
-constexpr int NT = 1024, NW = NT / 32;
 constexpr int MAX_HELD = 2048;                  // requests whose sums a CTA keeps in shared memory for the lists
+constexpr int NT = 1024, NW = NT / 32;
+constexpr int SMALL_N = 256;                    // a call of few requests: one CTA, which keeps all that phases leave each other in shared memory
 
 struct Head { int n0, there, tokens; };         // stack before the call, with what was given back; tokens granted
 struct Scratch {
@@ -42,81 +43,143 @@ __device__ __forceinline__ void cluster_barrier() {
 __device__ __forceinline__ int cluster_rank() { int r; asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
 __device__ __forceinline__ int cluster_size() { int r; asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r)); return r; }
 
-// Sum over the block's threads before this one, and of all; every thread calls it.
-__device__ __forceinline__ long long block_exclusive(long long v, long long* part /* shared, NW + 1 */, long long& total) {
+// Sums over the block's threads before this one, and of all, of three numbers at once; every thread calls it.
+struct Three { long long x[3]; };
+__device__ __forceinline__ Three block_exclusive(Three v, long long (*part)[NW + 1] /* shared, three rows */, Three& total) {
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  long long x = v;
+  Three s = v;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) { const long long y = __shfl_up_sync(0xffffffffu, x, o); if (lane >= o) x += y; }
+  for (int o = 1; o < 32; o <<= 1)
+#pragma unroll
+    for (int k = 0; k < 3; ++k) { const long long y = __shfl_up_sync(0xffffffffu, s.x[k], o); if (lane >= o) s.x[k] += y; }
   __syncthreads();                                                       // what was there has been read
-  if (lane == 31) part[w] = x;
+  if (lane == 31)
+#pragma unroll
+    for (int k = 0; k < 3; ++k) part[k][w] = s.x[k];
   __syncthreads();
-  if (w == 0) {
-    const long long p = part[lane];
+  if (w < 3) {
+    const long long p = lane < NW ? part[w][lane] : 0;
     long long q = p;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) { const long long y = __shfl_up_sync(0xffffffffu, q, o); if (lane >= o) q += y; }
-    part[lane] = q - p;
-    if (lane == 31) part[NW] = q;
+    if (lane < NW) part[w][lane] = q - p;
+    if (lane == 31) part[w][NW] = q;
   }
   __syncthreads();
-  total = part[NW];
-  return part[w] + x - v;
+#pragma unroll
+  for (int k = 0; k < 3; ++k) { total.x[k] = part[k][NW]; s.x[k] += part[k][w] - v.x[k]; }
+  return s;
 }
 
 __device__ __forceinline__ bool held(const PlanArgs& a, int entry) { return entry >= 0 && entry < a.n_pages; }
 __device__ __forceinline__ int pages_of(const PlanArgs& a, long long rows) { return (int)((rows + a.page - 1) / a.page); }
 
+// What one phase leaves the next is read past the first-level cache, which keeps no order between CTAs.
+template <typename V> __device__ __forceinline__ V left(const V* p) { return __isShared(p) ? *p : __ldcg(p); }
+
+// A group's threads over `count` entries from `from` on, four at a time where the row is on a 16-byte boundary: f(entry's number, entry)
+template <typename F>
+__device__ __forceinline__ void over(const int* row, int from, int count, int t, int threads, F f) {
+  if (((reinterpret_cast<uintptr_t>(row + from) & 15) == 0) && count % 4 == 0) {
+#pragma unroll 4
+    for (int j = 4 * t; j < count; j += 4 * threads) {
+      const int4 e = *reinterpret_cast<const int4*>(row + from + j);
+      f(from + j, e.x); f(from + j + 1, e.y); f(from + j + 2, e.z); f(from + j + 3, e.w);
+    }
+  } else {
+#pragma unroll 8
+    for (int j = t; j < count; j += threads) f(from + j, row[from + j]);
+  }
+}
+
+// SMALL: one CTA, at most SMALL_N requests
+template <bool SMALL>
 __global__ void __launch_bounds__(NT) paged_plan_kernel(const __grid_constant__ PlanArgs a) {
-  __shared__ long long part[NW + 1];
+  constexpr int HELD = SMALL ? SMALL_N : MAX_HELD;
+  __shared__ long long part[3][NW + 1];
   __shared__ int sums[NW], lasts[NW];
-  __shared__ int cu_s[MAX_HELD + 1], slot_s[MAX_HELD], row_s[MAX_HELD];
-  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, rank = cluster_rank(), C = cluster_size();
+  __shared__ int cu_s[HELD + 1], slot_s[HELD], row_s[HELD];
+  __shared__ int new_s[SMALL ? SMALL_N : 1], len_s[SMALL ? SMALL_N : 1];
+  __shared__ int4 rec_s[SMALL ? SMALL_N : 1], res_s[SMALL ? SMALL_N : 1];
+  __shared__ int last_s[SMALL ? SMALL_N : 1];
+  __shared__ Head head_s;
+  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, rank = SMALL ? 0 : cluster_rank(), C = SMALL ? 1 : cluster_size();
   Scratch s;
   carve(a.scratch, a.max_seqs, a.n, &s);
+  if (SMALL) { s.rec = rec_s; s.res = res_s; s.last = last_s; s.head = &head_s; }
+  const auto phase = [&]() { if (SMALL) __syncthreads(); else cluster_barrier(); };
   pdl_wait();
   const auto report = [&](unsigned bad) { if (bad && a.status) atomicOr(a.status, bad); };
 
   // ---- who lists a slot first ----
-  for (int i = rank * NT + tid; i < a.n; i += C * NT) {
-    const int slot = a.slots[i];
-    if (slot >= 0 && slot < a.max_seqs) s.owner[slot] = INT_MAX;
-    else if (slot != -1) report(SNAP_DEV_BAD_SLOT);
+  if (SMALL) {
+    if (tid < a.n) {
+      const int slot = a.slots[tid], fresh = a.new_tokens[tid];
+      const bool valid = slot >= 0 && slot < a.max_seqs;
+      slot_s[tid] = slot; new_s[tid] = fresh; len_s[tid] = valid ? a.seq_len[slot] : 0;
+      if (!valid && slot != -1) report(SNAP_DEV_BAD_SLOT);
+    }
+    __syncthreads();
+  } else {
+    for (int i = rank * NT + tid; i < a.n; i += C * NT) {
+      const int slot = a.slots[i];
+      if (slot >= 0 && slot < a.max_seqs) s.owner[slot] = INT_MAX;
+      else if (slot != -1) report(SNAP_DEV_BAD_SLOT);
+    }
+    phase();
+    for (int i = rank * NT + tid; i < a.n; i += C * NT) {
+      const int slot = a.slots[i];
+      if (slot >= 0 && slot < a.max_seqs) atomicMin(&s.owner[slot], i);
+    }
+    phase();
   }
-  cluster_barrier();
-  for (int i = rank * NT + tid; i < a.n; i += C * NT) {
-    const int slot = a.slots[i];
-    if (slot >= 0 && slot < a.max_seqs) atomicMin(&s.owner[slot], i);
-  }
-  cluster_barrier();
 
-  // ---- pages that each request misses, or gives back: `group` warps to a request ----
+  const bool apart = a.table_in != a.table_out;
+  const auto fours = [&](const int* row, const int* out) {
+    return a.max_pages % 4 == 0 && ((reinterpret_cast<uintptr_t>(row) | reinterpret_cast<uintptr_t>(out)) & 15) == 0;
+  };
+  // ---- pages that each request misses, or gives back: `group` warps to a request.  Table rows that go on are copied alongside ----
   int group = 1;
   while (group < NW && (long long)a.n * group * 2 <= (long long)C * NW) group *= 2;
-  const int groups = NW / group, mine = w / group, gt = tid % (group * 32);   // groups of a CTA, this thread's and its place in it
+  const int groups = NW / group, mine = w / group, gt = tid % (group * 32), gn = group * 32;   // groups of a CTA, this thread's and its place in it
   for (int i0 = rank * groups; i0 < a.n; i0 += C * groups) {
     const int i = i0 + mine;
     int count = 0, last = -1;
     int4 rec = make_int4(-1, 0, 0, 0);
     if (i < a.n) {
-      const int slot = a.slots[i];
+      const int slot = SMALL ? slot_s[i] : a.slots[i];
       if (slot >= 0 && slot < a.max_seqs) {
-        if (__ldcg(&s.owner[slot]) == i) rec.x = slot;
+        bool first = true;
+        if (SMALL) {
+          for (int x = lane; x < i; x += 32) first = first && slot_s[x] != slot;
+          first = __all_sync(0xffffffffu, first);
+        } else {
+          first = __ldcg(&s.owner[slot]) == i;
+        }
+        if (first) rec.x = slot;
         else if (gt == 0) report(SNAP_DEV_BAD_SLOT);
       }
       if (rec.x >= 0) {
-        rec.y = a.new_tokens[i];
-        rec.z = rec.y < 0 ? 0 : max(a.seq_len[slot], 0);
+        rec.y = SMALL ? new_s[i] : a.new_tokens[i];
+        rec.z = max(SMALL ? len_s[i] : a.seq_len[slot], 0);
+        if (rec.y < 0) rec.z = 0;
         const int* row = a.table_in + (long long)slot * a.max_pages;
         const long long rows = (long long)rec.z + rec.y;
+        if (rec.y >= 0 && apart) {                                       // (what is granted is written over it, phases later)
+          int* out = a.table_out + (long long)slot * a.max_pages;
+          if (fours(row, out)) {
+#pragma unroll 4
+            for (int j = 4 * gt; j < a.max_pages; j += 4 * gn) *reinterpret_cast<int4*>(out + j) = *reinterpret_cast<const int4*>(row + j);
+          } else {
+#pragma unroll 8
+            for (int j = gt; j < a.max_pages; j += gn) out[j] = row[j];
+          }
+        }
         if (rec.y < 0) {
-#pragma unroll 4
-          for (int j = gt; j < a.max_pages; j += group * 32)
-            if (held(a, row[j])) { ++count; last = j; }
+          over(row, 0, a.max_pages, gt, gn, [&](int j, int e) { if (held(a, e)) { ++count; last = j; } });
         } else if (rows <= (long long)a.page * a.max_pages) {
-          const int j1 = pages_of(a, rows);
-#pragma unroll 4
-          for (int j = pages_of(a, rec.z) + gt; j < j1; j += group * 32) count += !held(a, row[j]);
+          const int j0 = pages_of(a, rec.z);
+          over(row, j0, pages_of(a, rows) - j0, gt, gn, [&](int, int e) { count += !held(a, e); });
         } else {
           count = -1;                                                    // past the table
         }
@@ -136,51 +199,47 @@ __global__ void __launch_bounds__(NT) paged_plan_kernel(const __grid_constant__ 
     }
     __syncthreads();
   }
-  cluster_barrier();
+  phase();
 
   // ---- the scan ----
   if (rank == 0) {
     const int per = (a.n + NT - 1) / NT, i0 = min(tid * per, a.n), i1 = min(i0 + per, a.n);
-    long long back = 0, want = 0, miss = 0, all_back, all_want, all_miss;
-    const auto tokens = [](const int4& r) { return r.x >= 0 && r.y > 0 && r.w >= 0 ? r.y : 0; };
-    for (int i = i0; i < i1; ++i) {
-      const int4 r = __ldcg(&s.rec[i]);
-      if (r.x < 0) continue;
-      if (r.y < 0) back += r.w;
-      else if (r.w > 0) miss += r.w;
-      want += tokens(r);
-    }
-    back = block_exclusive(back, part, all_back);
-    want = block_exclusive(want, part, all_want);
-    miss = block_exclusive(miss, part, all_miss);
     const int given = *a.n_free_in, n0 = min(max(given, 0), a.n_pages);
-    const int there = (int)min(n0 + all_back, (long long)a.n_pages);
-    if (tid == 0 && (given != n0 || n0 + all_back > a.n_pages)) report(SNAP_DEV_BAD_PAGE);
-    long long got = 0, taken = 0, all_got, all_taken;
+    Three sum = {{0, 0, 0}}, all;                                        // pages given back, tokens wanted, pages missing
+    for (int i = i0; i < i1; ++i) {
+      const int4 r = left(&s.rec[i]);
+      if (r.x < 0 || r.w < 0) continue;
+      if (r.y < 0) sum.x[0] += r.w;
+      else { sum.x[1] += r.y; sum.x[2] += r.w; }
+    }
+    const Three before = block_exclusive(sum, part, all);
+    const int there = (int)min(n0 + all.x[0], (long long)a.n_pages);
+    if (tid == 0 && (given != n0 || n0 + all.x[0] > a.n_pages)) report(SNAP_DEV_BAD_PAGE);
+    const auto fits = [&](long long wanted, long long missing, int own) { return wanted <= a.n_tokens_max && (own == 0 || missing <= there); };
+    Three got = {{0, 0, 0}}, all_got;                                    // tokens and pages granted
     unsigned bad = 0;
-    {
-      long long wn = want, ms = miss;
-      for (int i = i0; i < i1; ++i) {
-        const int4 r = __ldcg(&s.rec[i]);
-        if (r.x < 0 || r.y < 0 || r.w < 0) continue;
-        wn += r.y;
-        ms += r.w;
-        if (wn <= a.n_tokens_max && (r.w == 0 || ms <= there)) { got += r.y; taken += r.w; }
-        else bad = SNAP_DEV_NO_ROOM;
-      }
+    long long want = before.x[1], miss = before.x[2];
+    for (int i = i0; i < i1; ++i) {
+      const int4 r = left(&s.rec[i]);
+      if (r.x < 0 || r.y < 0 || r.w < 0) continue;
+      want += r.y;
+      miss += r.w;
+      if (fits(want, miss, r.w)) { got.x[0] += r.y; got.x[1] += r.w; }
+      else bad = SNAP_DEV_NO_ROOM;
     }
     report(bad);
-    long long at = block_exclusive(got, part, all_got);
-    block_exclusive(taken, part, all_taken);
+    long long at = block_exclusive(got, part, all_got).x[0], back = before.x[0];
+    want = before.x[1];
+    miss = before.x[2];
     for (int i = i0; i < i1; ++i) {
-      const int4 r = __ldcg(&s.rec[i]);
+      const int4 r = left(&s.rec[i]);
       int4 res = make_int4((int)min(back, (long long)INT_MAX), 0, -1, (int)at);
       if (r.x >= 0 && r.y < 0) back += r.w;
       else if (r.x >= 0 && r.w >= 0) {
         want += r.y;
         res.y = (int)min(miss, (long long)INT_MAX);
         miss += r.w;
-        if (want <= a.n_tokens_max && (r.w == 0 || miss <= there)) { res.z = r.y; at += r.y; }
+        if (fits(want, miss, r.w)) { res.z = r.y; at += r.y; }
       }
       s.res[i] = res;
       a.cu[i] = res.w;
@@ -188,34 +247,39 @@ __global__ void __launch_bounds__(NT) paged_plan_kernel(const __grid_constant__ 
       if (a.granted) a.granted[i] = max(res.z, 0);
     }
     if (tid == 0) {
-      a.cu[a.n] = (int)all_got;
-      *a.n_free_out = there - (int)all_taken;
-      *s.head = {n0, there, (int)all_got};
+      a.cu[a.n] = (int)all_got.x[0];
+      *a.n_free_out = there - (int)all_got.x[1];
+      *s.head = {n0, there, (int)all_got.x[0]};
     }
   }
-  cluster_barrier();
+  phase();
 
-  // ---- pages given back; table rows ----
-  const int n0 = __ldcg(&s.head->n0), there = __ldcg(&s.head->there), all = __ldcg(&s.head->tokens);
-  const bool apart = a.table_in != a.table_out;
+  // ---- pages given back ----
+  const Head head = {left(&s.head->n0), left(&s.head->there), left(&s.head->tokens)};
+  const int all = head.tokens;
   for (int i = rank * groups + mine; i < a.n; i += C * groups) {
-    const int4 r = __ldcg(&s.rec[i]);
-    if (r.x < 0) continue;
+    const int4 r = left(&s.rec[i]);
+    if (r.x < 0 || r.y >= 0) continue;
     const int* row = a.table_in + (long long)r.x * a.max_pages;
     int* out = a.table_out + (long long)r.x * a.max_pages;
-    if (r.y >= 0) {
-      if (apart)
+    const long long at = (long long)head.n0 + left(&s.res[i]).x;
+    if (left(&s.last[i]) + 1 == r.w) {                                   // they are the row's first entries
+      const auto back = [&](int j, int e) { if (j < r.w && at + j < a.n_pages) a.stack[at + j] = e; };
+      if (fours(row, out)) {
 #pragma unroll 4
-        for (int j = gt; j < a.max_pages; j += group * 32) out[j] = row[j];
-      continue;
-    }
-    const long long at = (long long)n0 + __ldcg(&s.res[i]).x;
-    if (__ldcg(&s.last[i]) + 1 == r.w) {                                 // they are the row's first entries
-#pragma unroll 4
-      for (int j = gt; j < a.max_pages; j += group * 32) {
-        const int e = row[j];
-        if (j < r.w && at + j < a.n_pages) a.stack[at + j] = e;
-        out[j] = -1;
+        for (int j = 4 * gt; j < a.max_pages; j += 4 * gn) {
+          if (j < r.w) {
+            const int4 e = *reinterpret_cast<const int4*>(row + j);
+            back(j, e.x); back(j + 1, e.y); back(j + 2, e.z); back(j + 3, e.w);
+          }
+          *reinterpret_cast<int4*>(out + j) = make_int4(-1, -1, -1, -1);
+        }
+      } else {
+#pragma unroll 8
+        for (int j = gt; j < a.max_pages; j += gn) {
+          if (j < r.w) back(j, row[j]);
+          out[j] = -1;
+        }
       }
     } else if (gt < 32) {
       int k = 0;
@@ -231,11 +295,11 @@ __global__ void __launch_bounds__(NT) paged_plan_kernel(const __grid_constant__ 
     if (gt == 0) a.seq_len[r.x] = 0;
   }
   // ---- the lists of tokens, four at a time ----
-  const bool in_smem = a.n <= MAX_HELD;
+  const bool in_smem = a.n <= HELD;
   if (in_smem) {
     for (int i = tid; i < a.n; i += NT) {
-      const int4 r = __ldcg(&s.rec[i]);
-      cu_s[i] = __ldcg(&s.res[i]).w; slot_s[i] = r.x; row_s[i] = r.z;
+      const int4 r = left(&s.rec[i]);
+      cu_s[i] = left(&s.res[i]).w; slot_s[i] = r.x; row_s[i] = r.z;
     }
     if (tid == 0) cu_s[a.n] = all;
   }
@@ -262,18 +326,18 @@ __global__ void __launch_bounds__(NT) paged_plan_kernel(const __grid_constant__ 
       for (int x = 0; x < 4 && t0 + x < a.n_tokens_max; ++x) { a.token_slots[t0 + x] = slot[x]; a.token_rows[t0 + x] = row[x]; }
     }
   }
-  cluster_barrier();
+  phase();
 
   // ---- the granted pages ----
   for (int i = rank * groups + mine; i < a.n; i += C * groups) {
-    const int4 r = __ldcg(&s.rec[i]), res = __ldcg(&s.res[i]);
+    const int4 r = left(&s.rec[i]), res = left(&s.res[i]);
     if (res.z < 0 || r.w <= 0) continue;
     const int* row = a.table_in + (long long)r.x * a.max_pages;
     int* out = a.table_out + (long long)r.x * a.max_pages;
-    const int j0 = pages_of(a, r.z), j1 = pages_of(a, (long long)r.z + r.y), top = there - 1 - res.y;
+    const int j0 = pages_of(a, r.z), j1 = pages_of(a, (long long)r.z + r.y), top = head.there - 1 - res.y;
     if (r.w == j1 - j0) {                                                // none of them holds a page
 #pragma unroll 4
-      for (int j = j0 + gt; j < j1; j += group * 32) out[j] = __ldcg(&a.stack[top - (j - j0)]);
+      for (int j = j0 + gt; j < j1; j += gn) out[j] = __ldcg(&a.stack[top - (j - j0)]);
     } else if (gt < 32) {
       int k = 0;
       for (int b = j0; b < j1; b += 32) {
@@ -291,20 +355,45 @@ __global__ void __launch_bounds__(NT) paged_plan_kernel(const __grid_constant__ 
 
 size_t paged_plan_scratch_bytes(int max_seqs, int n_seqs) { return carve(nullptr, max_seqs, n_seqs, nullptr); }
 
+// One CTA where there is little to do.  Else a cluster with a CTA for every 16384 entries of table rows and of the list, up to 16.
 cudaError_t launch_paged_plan(const PlanArgs& a, cudaStream_t st) {
-  const int cluster = 8;
+  const long long entries = (long long)a.n * (a.table_in != a.table_out ? a.max_pages : 64) + a.n_tokens_max;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = cluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t lc = {};
-  lc.gridDim = dim3(cluster);
-  lc.blockDim = dim3(NT);
   lc.stream = st;
   lc.attrs = attr;
-  lc.numAttrs = 2;
-  const cudaError_t e = cudaLaunchKernelEx(&lc, paged_plan_kernel, a);
+  lc.numAttrs = 1;
+  cudaError_t e;
+  if (a.n <= SMALL_N && entries <= 32768) {
+    lc.gridDim = dim3(1);
+    lc.blockDim = dim3(NT);
+    e = cudaLaunchKernelEx(&lc, paged_plan_kernel<true>, a);
+  } else {
+    const auto kernel = paged_plan_kernel<false>;
+    static int widest[kMaxDevices] = {};                                 // CTAs of a cluster that the device takes
+    int dev = 0;
+    if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
+    if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 16; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    lc.blockDim = dim3(NT);
+    lc.gridDim = dim3(16);
+    lc.numAttrs = 2;
+    if (widest[dev] == 0) {
+      int fit = 0;
+      const bool wide = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+                        cudaOccupancyMaxActiveClusters(&fit, kernel, &lc) == cudaSuccess && fit > 0;
+      (void)cudaGetLastError();
+      widest[dev] = wide ? 16 : 8;
+    }
+    int cluster = 1;
+    while (cluster < widest[dev] && cluster * 16384LL < entries) cluster *= 2;
+    attr[1].val.clusterDim.x = cluster;
+    lc.gridDim = dim3(cluster);
+    e = cudaLaunchKernelEx(&lc, kernel, a);
+  }
   count_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
 }
