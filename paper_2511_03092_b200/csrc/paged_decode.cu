@@ -295,7 +295,7 @@ paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ CU
   int n = 0, done = 0;                                                   // tiles done by this warp; by the CTA before this segment
   while (true) {
     // ---- a segment: the CTA's tiles [at.t, tb) of one unit ----
-    const int tb = segment_end(at, end), cnt = tb - at.t;
+    const int tb = segment_end(a, at, end), cnt = tb - at.t;
     const int hb = at.u % a.nhb, nh = min(a.gb, a.g - hb * a.gb);
     const bool whole = cnt == at.nt;
     float oacc[NG][KS][4], m_ref[NG][2], l_part[NG][2];                  // O^T: dims 16 db + gq (+8), columns 8 gi + 2 tq (+1)
@@ -680,7 +680,7 @@ __global__ void __launch_bounds__(SNT, CTAS) paged_simt_kernel(const __grid_cons
   int n = 0, done = 0, s_out = 0;
   unsigned parity = 0;
   while (true) {
-    const int tb = segment_end(at, end), cnt = tb - at.t;
+    const int tb = segment_end(a, at, end), cnt = tb - at.t;
     const int hb = at.u % a.nhb, nh = min(a.gb, a.g - hb * a.gb);
     const bool whole = cnt == at.nt;
     F2 o[HB][NV][2];

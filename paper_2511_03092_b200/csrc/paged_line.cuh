@@ -23,6 +23,7 @@ using mmasync::fast_exp2;
 using umma::mbar_try_wait;
 
 constexpr int UNIT_TILES = 6;                   // what a unit costs besides its tiles, in tiles; units of at most that many stay whole
+                                                // (a kernel's arguments may have other numbers: share(), whole())
 constexpr int MIN_TILES = 1;                    // a CTA gets at least that much beyond one unit's share (at least one: no stretch is empty)
 // (Measured over 40 calls of all sizes: 4 and 4 take 8 % longer, 8 and 1 2 %, 4 and 1 as long but 4 % longer for many short sequences.)
 constexpr int MAX_CTAS = 1024, MAX_HELD = 128;  // sequences whose slot and length a CTA keeps in shared memory
@@ -45,6 +46,8 @@ struct LineArgs {
   bool keep_ml;                                 // ml_unit is wanted
   uint32_t* status;
   int ctas;
+  __device__ __forceinline__ constexpr int share() const { return UNIT_TILES; }
+  __device__ __forceinline__ constexpr int whole() const { return UNIT_TILES; }
 };
 
 template <typename A> __device__ __forceinline__ int rows_of(const A& a, int slot) {
@@ -52,16 +55,17 @@ template <typename A> __device__ __forceinline__ int rows_of(const A& a, int slo
   return min(max(a.seq_len[slot], 0), a.map.cap);
 }
 template <int ROWS> __device__ __forceinline__ int tiles_of(int rows) { return (int)(((unsigned)rows + ROWS - 1) / ROWS); }
-__device__ __forceinline__ int length_of(int nt) { return nt > 0 ? nt + UNIT_TILES : 0; }           // on the line
+template <typename A> __device__ __forceinline__ int length_of(const A& a, int nt) { return nt > 0 ? nt + a.share() : 0; }   // on the line
 // Where tile t of a unit begins on the line, counted from the unit: the first tile carries the unit's share, and all
 // tiles of a short unit begin (and so stay) with the first.
-__device__ __forceinline__ int begin_of(int t, int nt) { return t == 0 || nt <= UNIT_TILES ? 0 : UNIT_TILES + t; }
+template <typename A> __device__ __forceinline__ int begin_of(const A& a, int t, int nt) { return t == 0 || nt <= a.whole() ? 0 : a.share() + t; }
 
 // CTAs that share a line of length W, where CTA c's stretch begins, and whose stretch position x lies in.  (32-bit
 // arithmetic where it suffices: 64-bit divisions are long instruction sequences.)
-__device__ __forceinline__ int active_ctas(long long W, int ctas) {
-  if (W >= (long long)ctas * (MIN_TILES + UNIT_TILES)) return ctas;
-  return W > 0 ? max((int)W / (MIN_TILES + UNIT_TILES), 1) : 0;
+template <typename A> __device__ __forceinline__ int active_ctas(const A& a, long long W) {
+  const int least = MIN_TILES + a.share();
+  if (W >= (long long)a.ctas * least) return a.ctas;
+  return W > 0 ? max((int)W / least, 1) : 0;
 }
 __device__ __forceinline__ long long stretch_begin(long long W, int active, int c) {
   return W < (1 << 21) ? (long long)((unsigned)W * (unsigned)c / (unsigned)active) : W * c / active;
@@ -84,7 +88,7 @@ template <int ROWS, typename A> __device__ __forceinline__ void load_entry(const
   p.nt = tiles_of<ROWS>(p.len);
 }
 template <int ROWS, typename A> __device__ __forceinline__ void next_unit(const A& a, const Held& held, Place& p) {
-  p.pos += length_of(p.nt);
+  p.pos += length_of(a, p.nt);
   if (++p.u == a.U) {
     p.u = 0;
     do { ++p.e; load_entry<ROWS>(a, held, p); } while (p.nt == 0);
@@ -98,7 +102,7 @@ template <int ROWS, typename A> __device__ __forceinline__ bool advance(const A&
     next_unit<ROWS>(a, held, p);
     if (p.e >= a.n || p.pos >= end) return false;
   }
-  return p.pos + begin_of(p.t, p.nt) < end;
+  return p.pos + begin_of(a, p.t, p.nt) < end;
 }
 
 __device__ __forceinline__ int warp_inclusive(int v, int lane) {
@@ -132,7 +136,7 @@ __device__ __forceinline__ bool locate_part(const A& a, Place& p, int& end, Held
   int active = 0;
   const auto stretch = [&]() {
     W = (long long)total * a.U;
-    active = active_ctas(W, a.ctas);
+    active = active_ctas(a, W);
     if (c >= active) return false;
     x0 = stretch_begin(W, active, c);
     x1 = stretch_begin(W, active, c + 1);
@@ -152,7 +156,7 @@ __device__ __forceinline__ bool locate_part(const A& a, Place& p, int& end, Held
     for (int x = 0; x < MOST; ++x)
       if (e0 + x < e1) {
         held.e[e0 + x] = v[x];
-        mine += length_of(tiles_of<ROWS>(v[x].y));
+        mine += length_of(a, tiles_of<ROWS>(v[x].y));
       }
     const int incl = warp_inclusive(mine, lane);
     int before = incl - mine;
@@ -164,7 +168,7 @@ __device__ __forceinline__ bool locate_part(const A& a, Place& p, int& end, Held
         const int2 v = held.e[e];
         const int nt = tiles_of<ROWS>(v.y);
         a.entry[e] = make_int4(at, v.x, v.y, nt);
-        at += length_of(nt);
+        at += length_of(a, nt);
       }
       if (lane == 0) a.entry[a.n] = make_int4(total, -1, 0, 0);
       if (bad && a.status) atomicOr(a.status, bad);
@@ -176,7 +180,7 @@ __device__ __forceinline__ bool locate_part(const A& a, Place& p, int& end, Held
     if (here) {
 #pragma unroll 1
       for (; e < e1 - 1; ++e) {
-        const int len = length_of(tiles_of<ROWS>(held.e[e].y));
+        const int len = length_of(a, tiles_of<ROWS>(held.e[e].y));
         if (x0 < (long long)(before + len) * a.U) break;
         before += len;
       }
@@ -187,7 +191,7 @@ __device__ __forceinline__ bool locate_part(const A& a, Place& p, int& end, Held
   } else {
     const int per = (a.n + NT - 1) / NT, e0 = min(tid * per, a.n), e1 = min(e0 + per, a.n);
     int mine = 0;
-    for (int e = e0; e < e1; ++e) mine += length_of(tiles_of<ROWS>(read_entry(a, a.slots[e], bad).y));
+    for (int e = e0; e < e1; ++e) mine += length_of(a, tiles_of<ROWS>(read_entry(a, a.slots[e], bad).y));
     const int incl = warp_inclusive(mine, lane);
     if (lane == 31) scan[warp] = incl;
     if (tid == 0) scan[NT / 32] = scan[NT / 32 + 1] = 0;
@@ -201,7 +205,7 @@ __device__ __forceinline__ bool locate_part(const A& a, Place& p, int& end, Held
         const int2 v = read_entry(a, a.slots[e], bad);
         const int nt = tiles_of<ROWS>(v.y);
         a.entry[e] = make_int4(at, v.x, v.y, nt);
-        at += length_of(nt);
+        at += length_of(a, nt);
       }
       if (tid == 0) a.entry[a.n] = make_int4(total, -1, 0, 0);
       if (bad && a.status) atomicOr(a.status, bad);
@@ -209,7 +213,7 @@ __device__ __forceinline__ bool locate_part(const A& a, Place& p, int& end, Held
     if (!stretch()) return false;
     if (x0 >= (long long)before * a.U && x0 < (long long)(before + mine) * a.U) {        // one thread
       for (int e = e0; e < e1; ++e) {
-        const int len = length_of(tiles_of<ROWS>(read_entry(a, a.slots[e], bad).y));
+        const int len = length_of(a, tiles_of<ROWS>(read_entry(a, a.slots[e], bad).y));
         if (x0 < (long long)(before + len) * a.U) { scan[NT / 32] = e; scan[NT / 32 + 1] = before; break; }
         before += len;
       }
@@ -222,11 +226,11 @@ __device__ __forceinline__ bool locate_part(const A& a, Place& p, int& end, Held
   load_entry<ROWS>(a, held, p);
   p.nt = max(p.nt, 1);                          // (only if another stream changes the lengths during the call: stay in bounds)
   const long long rel = x0 - (long long)before_at * a.U;
-  const int unit = length_of(p.nt);
+  const int unit = length_of(a, p.nt);
   p.u = (int)min(rel < (1LL << 31) ? (long long)((unsigned)rel / (unsigned)unit) : rel / unit, (long long)a.U - 1);
   const int o = (int)(rel - (long long)p.u * unit);
   // the first tile that begins at or after x0
-  p.t = o <= 0 ? 0 : p.nt <= UNIT_TILES ? p.nt : max(1, o - UNIT_TILES);
+  p.t = o <= 0 ? 0 : p.nt <= a.whole() ? p.nt : max(1, o - a.share());
   p.pos = 0;
   end = (int)min(x1 - x0 + max(o, 0), (long long)(1 << 30));
   if (p.t >= p.nt) {
@@ -252,8 +256,8 @@ __device__ __forceinline__ bool locate(const A& a, Place& p, int& end, Held& hel
   return found.any;
 }
 // Tiles of the unit at p, from p.t on, that begin before the end of the stretch: the end of that range of tiles
-__device__ __forceinline__ int segment_end(const Place& p, int end) {
-  return p.nt <= UNIT_TILES ? p.nt : min(p.nt, max(end - p.pos - UNIT_TILES, 1));
+template <typename A> __device__ __forceinline__ int segment_end(const A& a, const Place& p, int end) {
+  return p.nt <= a.whole() ? p.nt : min(p.nt, max(end - p.pos - a.share(), 1));
 }
 
 // The CTA's result of a segment, the sum of NBUF buffers [cols][ld] in shared memory, leaves for the output (a whole unit) or the
@@ -310,10 +314,10 @@ constexpr int JNT = 256;
 struct Pieces { int np, c0; };                     // pieces of a unit; np <= 1: done whole
 template <typename A> __device__ __forceinline__ Pieces pieces_of(const A& a, int u, int before, int total, int nt) {
   Pieces p;
-  const long long W = (long long)total * a.U, x = (long long)before * a.U + (long long)u * length_of(nt);
-  const int active = active_ctas(W, a.ctas);
+  const long long W = (long long)total * a.U, x = (long long)before * a.U + (long long)u * length_of(a, nt);
+  const int active = active_ctas(a, W);
   p.c0 = owner_of(x, W, active);
-  p.np = owner_of(x + begin_of(nt - 1, nt), W, active) - p.c0 + 1;
+  p.np = owner_of(x + begin_of(a, nt - 1, nt), W, active) - p.c0 + 1;
   return p;
 }
 __device__ __forceinline__ int piece_at(const Pieces& p, int k) { return 2 * (p.c0 + k) + (k == 0); }
@@ -358,19 +362,19 @@ __device__ __forceinline__ void join_outputs(const A& a, int id, int joins, int 
     for (int i = id; i < a.n; i += joins)
       if (a.entry[i].w == 0) zero((long long)i * a.rows_seq, a.rows_seq);
     const long long W = (long long)line * a.U;
-    const int active = active_ctas(W, a.ctas), c = id + 1;
+    const int active = active_ctas(a, W), c = id + 1;
     if (c >= active) return;
     const long long x = stretch_begin(W, active, c);
     __syncthreads();
     for (int i = tid; i < a.n; i += JNT) {                               // one thread has it
       const int4 at = a.entry[i];
-      if ((long long)at.x * a.U <= x && x < (long long)(at.x + length_of(at.w)) * a.U) s_e = i;
+      if ((long long)at.x * a.U <= x && x < (long long)(at.x + length_of(a, at.w)) * a.U) s_e = i;
     }
     __syncthreads();
     e = s_e;
     if (e < 0) return;                                                   // (only if the lengths change during the call)
     const int4 at = a.entry[e];
-    const int before = at.x, unit = length_of(at.w);
+    const int before = at.x, unit = length_of(a, at.w);
     const long long rel = x - (long long)before * a.U;
     nt = at.w;
     u = rel < (1LL << 31) ? (int)((unsigned)rel / (unsigned)unit) : (int)(rel / unit);

@@ -8,7 +8,7 @@
 // A warp's tile is 32 rows, S^T = K tile . Q^T and O^T += V tile^T . P^T with m16n8k16 on half-precision numbers, the columns on
 // the N side: a code is one exactly, and converting two takes one instruction.  (Products of 8-bit numbers, m16n8k32, are no way around it: the
 // conversions are then in what the instruction expands to, and four columns, split in two numbers each, cost what eight do here: four tokens
-// a step 112 us instead of TOKENS4.)  The order of the inner dims of a product is free, so codes are used as ldmatrix delivers them: four
+// a step 112 us instead of 60.)  The order of the inner dims of a product is free, so codes are used as ldmatrix delivers them: four
 // neighbouring dims of a key row are positions 2t, 2t + 1, 2t + 8, 2t + 9 of a step of 16, and the queries are read in that order;
 // four rows of a value dim, transposed by bytes, are those positions as well, the rows being addressed in the order that
 // movmatrix leaves of the weights.
@@ -20,7 +20,7 @@
 // product leaves that range.  They round to 11 bits (bf16: an eighth of the output's own rounding) or are two numbers (single precision).
 //
 // Where a row's heads lie side by side (pages stored rows first), two warps of a CTA take one head and two the next, over the same rows: HBM
-// then delivers twice as much in a row (128-byte heads, 16 long sequences: 208 us without, SIDES with; heads first 168).
+// then delivers twice as much in a row (128-byte heads, 16 long sequences: 208 us without, 172 with; heads first 168).
 #include <type_traits>
 
 #include "e4m3.cuh"
@@ -37,6 +37,10 @@ using umma::smem_u32;
 
 constexpr int TR = 32;                          // rows of a tile, a lane each
 constexpr float NOTHING = -3.402823466e38f;     // the reference of a column that has seen no row: every logit lies far above it
+// What a unit costs besides its tiles, in tiles; units of at most WHOLE tiles stay whole, since a call that cuts none has nothing to join.
+// (48 calls of 1 to 100 sequences of up to 20000 rows: 6 and 6 take 7 % longer, 4 and 6 4 %, 4 and 8 4 %, 3 and 12 2 %, 6 and 12 2 %, 4 and
+// 24 0.5 %; 45 sequences of up to 333 rows, 8 KV heads of 128 dims 16.2 us, with 6 and 6 22.1.)
+constexpr int SHARE = 4, WHOLE = 12;
 constexpr int LOOK = 2;                         // tiles whose pages are looked up ahead of their copies
 
 // n / d for 0 <= n < 2^31 by a multiplication
@@ -61,6 +65,8 @@ struct Q8Args : LineArgs {
   Divisor by_page, by_block, by_gq, by_gc, by_nhb;
   int blocks;                                   // scales of a page and KV head
   int box;                                      // rows of a copy, 0: rows are copied by the lanes
+  __device__ __forceinline__ constexpr int share() const { return SHARE; }
+  __device__ __forceinline__ constexpr int whole() const { return WHOLE; }
   __device__ __forceinline__ long long out_row(int e, int k, int x) const {
     const int h = heads > 1 ? by_gc.quotient(x) : 0, y = x - h * gc, u = by_gq.quotient(y);
     return ((long long)e * q_len + u) * Hq + (k * heads + h) * gq + (y - u * gq);
@@ -159,7 +165,7 @@ q8_mma_kernel(const __grid_constant__ Q8Args a, const __grid_constant__ CUtensor
   // tiles ws, ws + WPS, ...; lane l looks up the page of the tile's row l ----
   const auto head_of = [&](int u) { return SIDES == 1 ? a.by_nhb.quotient(u) : 2 * u + side; };
   Place pr = at;
-  int pr_stop = segment_end(pr, end), pr_head = head_of(pr.u);           // the CTA's tiles of pr's unit end there
+  int pr_stop = segment_end(a, pr, end), pr_head = head_of(pr.u);           // the CTA's tiles of pr's unit end there
   const int* pr_table = a.map.table + (long long)max(pr.slot, 0) * a.map.max_pages;
   bool more = true;
   const auto settle = [&]() {                                            // pr.t may have passed its unit's tiles: the unit that has it
@@ -168,7 +174,7 @@ q8_mma_kernel(const __grid_constant__ Q8Args a, const __grid_constant__ CUtensor
       pr.t -= pr.nt;
       next_unit<TR>(a, held, pr);
       if (pr.e >= a.n || pr.pos >= end) { more = false; return; }
-      pr_stop = segment_end(pr, end);
+      pr_stop = segment_end(a, pr, end);
       pr_head = head_of(pr.u);
       pr_table = a.map.table + (long long)pr.slot * a.map.max_pages;
     }
@@ -309,7 +315,7 @@ q8_mma_kernel(const __grid_constant__ Q8Args a, const __grid_constant__ CUtensor
   int n = 0, done = 0;                                                   // tiles done by this warp; by the CTA before this segment
   while (true) {
     // ---- a segment: the CTA's tiles [at.t, tb) of one unit ----
-    const int tb = segment_end(at, end), cnt = tb - at.t;
+    const int tb = segment_end(a, at, end), cnt = tb - at.t;
     const int hb = at.u - a.by_nhb.quotient(at.u) * a.nhb, nh = min(a.gb, a.g - hb * a.gb);
     const bool whole = cnt == at.nt;
     const int all_see = at.len - a.q_len + 1;                            // rows that every column sees
@@ -631,7 +637,7 @@ int q8_decode_plan(const Shape& s, const Q8Map& m, int n_active, int q_len, int 
   p->gb = p->heads > 1 ? 2 * (int)cols : (int)((cols + p->nhb - 1) / p->nhb);
   const int per_sm = p->gb > 8 || s.d_qk > 64 || s.d_v > 64 ? kCtasWide : kCtas;
   p->ctas = sms * per_sm < MAX_CTAS ? sms * per_sm : MAX_CTAS;
-  const long long units = (long long)n_active * s.Hkv * p->nhb, tiles = m.pages.cap / (long long)TR + 1 + UNIT_TILES;
+  const long long units = (long long)n_active * s.Hkv * p->nhb, tiles = m.pages.cap / (long long)TR + 1 + SHARE;
   // grid and index limits; a line of tiles and the scratch have to be countable
   if (cols > (1 << 20) || units > (1LL << 30) || n_active * (long long)s.Hq * q_len > 0x7fffffffLL || units * tiles > (1LL << 37) ||
       n_active * tiles > 0x7fffffffLL)

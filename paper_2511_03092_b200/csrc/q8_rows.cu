@@ -313,7 +313,7 @@ __global__ void __launch_bounds__(ANT, 4) q8_append_kernel(const __grid_constant
             for (int e = 0; e < V; ++e) cs[e] = table[z * half + j * V + e];
           }
           const auto source = [&](int h) { return h < nq ? q + (y + ny * h) * a.q_head : k + (y + ny * (h - nq)) * a.k_head; };
-          constexpr int U = 4;                                           // heads at a time
+          constexpr int U = sizeof(T) == 4 ? 2 : 4;                        // heads at a time
           for (int h0 = ty; h0 < nq + nk; h0 += U * Y) {
             VT va[U], vb[U];
 #pragma unroll
