@@ -2,8 +2,9 @@
 //
 // Requests are served as if one after the other; the prefix sums of what each of them wants (pages it gives back, tokens,
 // pages it misses) tell which are served and where each one's pages lie in the stack, so that all of it is parallel but for one scan.
-// One thread-block cluster, or one CTA, does the call, its phases apart by barriers: count, scan (one CTA), move (pages given back,
-// table rows, lists of tokens), fill (the granted pages, read from a stack that is then complete).
+// A small call is one CTA's, its phases apart by barriers: count (and copy table rows), scan, move (pages given back, lists of tokens), fill
+// (the granted pages, read from a stack that is then complete).  Of a larger one a thread-block cluster counts, scans and gives back, and a
+// second launch writes table rows and lists with the whole GPU.
 #include <climits>
 
 #include "snap_internal.cuh"
@@ -13,6 +14,7 @@ namespace {
 
 constexpr int MAX_HELD = 2048;                  // requests whose sums a CTA keeps in shared memory for the lists
 constexpr int NT = 1024, NW = NT / 32;
+constexpr int RNT = 256, PIECE = 4 * RNT;       // threads of the second launch; tokens or entries of a table row that a CTA writes at a time
 constexpr int SMALL_N = 256;                    // a call of few requests: one CTA, which keeps all that phases leave each other in shared memory
 
 struct Head { int n0, there, tokens; };         // stack before the call, with what was given back; tokens granted
@@ -92,10 +94,62 @@ __device__ __forceinline__ void over(const int* row, int from, int count, int t,
   }
 }
 
+// The lists of tokens, four at a time, from what a CTA keeps of the requests in shared memory, or from the scratch.
+struct Lists {
+  int* cu_s; int* slot_s; int* row_s; const Scratch& s; int n, all; bool held;
+  __device__ __forceinline__ void take(int threads) const {
+    for (int i = threadIdx.x; held && i < n; i += threads) {
+      const int4 r = left(&s.rec[i]);
+      cu_s[i] = left(&s.res[i]).w; slot_s[i] = r.x; row_s[i] = r.z;
+    }
+    if (held && threadIdx.x == 0) cu_s[n] = all;
+  }
+  __device__ __forceinline__ int cu(int i) const { return held ? cu_s[i] : i < n ? __ldcg(&s.res[i]).w : all; }
+  __device__ __forceinline__ void write(const PlanArgs& a, long long t0) const {
+    alignas(16) int slot[4] = {-1, -1, -1, -1}, row[4] = {0, 0, 0, 0};
+    if (t0 < all) {
+      int lo = 0, hi = n;                                                // cu(lo) <= t0 < cu(hi)
+      while (hi - lo > 1) { const int mid = (lo + hi) / 2; if (cu(mid) <= t0) lo = mid; else hi = mid; }
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const long long t = t0 + x;
+        if (t >= all) break;
+        while (cu(lo + 1) <= t) ++lo;
+        slot[x] = held ? slot_s[lo] : __ldcg(&s.rec[lo]).x;
+        row[x] = (held ? row_s[lo] : __ldcg(&s.rec[lo]).z) + (int)(t - cu(lo));
+      }
+    }
+    if (t0 + 4 <= a.n_tokens_max) {
+      *reinterpret_cast<int4*>(a.token_slots + t0) = *reinterpret_cast<const int4*>(slot);
+      *reinterpret_cast<int4*>(a.token_rows + t0) = *reinterpret_cast<const int4*>(row);
+    } else {
+      for (int x = 0; x < 4 && t0 + x < a.n_tokens_max; ++x) { a.token_slots[t0 + x] = slot[x]; a.token_rows[t0 + x] = row[x]; }
+    }
+  }
+};
+
+// Entries of a row can go four at a time
+__device__ __forceinline__ bool fours(const PlanArgs& a, const int* row, const int* out) {
+  return a.max_pages % 4 == 0 && ((reinterpret_cast<uintptr_t>(row) | reinterpret_cast<uintptr_t>(out)) & 15) == 0;
+}
+
+// One warp: the granted pages of a row some of whose entries [j0, j1) hold a page already
+__device__ __forceinline__ void fill_gaps(const PlanArgs& a, const int* row, int* out, int j0, int j1, int top) {
+  const int lane = threadIdx.x & 31;
+  int k = 0;
+  for (int b = j0; b < j1; b += 32) {
+    const int j = b + lane, e = j < j1 ? row[j] : 0;
+    const bool need = j < j1 && !held(a, e);
+    const unsigned some = __ballot_sync(0xffffffffu, need);
+    if (j < j1) out[j] = need ? __ldcg(&a.stack[top - k - __popc(some & ((1u << lane) - 1u))]) : e;
+    k += __popc(some);
+  }
+}
+
 // SMALL: one CTA, at most SMALL_N requests
 template <bool SMALL>
 __global__ void __launch_bounds__(NT) paged_plan_kernel(const __grid_constant__ PlanArgs a) {
-  constexpr int HELD = SMALL ? SMALL_N : MAX_HELD;
+  constexpr int HELD = SMALL ? SMALL_N : 1;
   __shared__ long long part[3][NW + 1];
   __shared__ int sums[NW], lasts[NW];
   __shared__ int cu_s[HELD + 1], slot_s[HELD], row_s[HELD];
@@ -135,9 +189,6 @@ __global__ void __launch_bounds__(NT) paged_plan_kernel(const __grid_constant__ 
   }
 
   const bool apart = a.table_in != a.table_out;
-  const auto fours = [&](const int* row, const int* out) {
-    return a.max_pages % 4 == 0 && ((reinterpret_cast<uintptr_t>(row) | reinterpret_cast<uintptr_t>(out)) & 15) == 0;
-  };
   // ---- pages that each request misses, or gives back: `group` warps to a request.  Table rows that go on are copied alongside ----
   int group = 1;
   while (group < NW && (long long)a.n * group * 2 <= (long long)C * NW) group *= 2;
@@ -165,9 +216,9 @@ __global__ void __launch_bounds__(NT) paged_plan_kernel(const __grid_constant__ 
         if (rec.y < 0) rec.z = 0;
         const int* row = a.table_in + (long long)slot * a.max_pages;
         const long long rows = (long long)rec.z + rec.y;
-        if (rec.y >= 0 && apart) {                                       // (what is granted is written over it, phases later)
+        if (SMALL && rec.y >= 0 && apart) {                              // (what is granted is written over it, phases later)
           int* out = a.table_out + (long long)slot * a.max_pages;
-          if (fours(row, out)) {
+          if (fours(a, row, out)) {
 #pragma unroll 4
             for (int j = 4 * gt; j < a.max_pages; j += 4 * gn) *reinterpret_cast<int4*>(out + j) = *reinterpret_cast<const int4*>(row + j);
           } else {
@@ -256,7 +307,6 @@ __global__ void __launch_bounds__(NT) paged_plan_kernel(const __grid_constant__ 
 
   // ---- pages given back ----
   const Head head = {left(&s.head->n0), left(&s.head->there), left(&s.head->tokens)};
-  const int all = head.tokens;
   for (int i = rank * groups + mine; i < a.n; i += C * groups) {
     const int4 r = left(&s.rec[i]);
     if (r.x < 0 || r.y >= 0) continue;
@@ -265,7 +315,7 @@ __global__ void __launch_bounds__(NT) paged_plan_kernel(const __grid_constant__ 
     const long long at = (long long)head.n0 + left(&s.res[i]).x;
     if (left(&s.last[i]) + 1 == r.w) {                                   // they are the row's first entries
       const auto back = [&](int j, int e) { if (j < r.w && at + j < a.n_pages) a.stack[at + j] = e; };
-      if (fours(row, out)) {
+      if (fours(a, row, out)) {
 #pragma unroll 4
         for (int j = 4 * gt; j < a.max_pages; j += 4 * gn) {
           if (j < r.w) {
@@ -294,39 +344,13 @@ __global__ void __launch_bounds__(NT) paged_plan_kernel(const __grid_constant__ 
     }
     if (gt == 0) a.seq_len[r.x] = 0;
   }
-  // ---- the lists of tokens, four at a time ----
-  const bool in_smem = a.n <= HELD;
-  if (in_smem) {
-    for (int i = tid; i < a.n; i += NT) {
-      const int4 r = left(&s.rec[i]);
-      cu_s[i] = left(&s.res[i]).w; slot_s[i] = r.x; row_s[i] = r.z;
-    }
-    if (tid == 0) cu_s[a.n] = all;
-  }
+  // ---- the lists of tokens ----
+  if (!SMALL) return;
+  const Lists lists = {cu_s, slot_s, row_s, s, a.n, head.tokens, true};
+  lists.take(NT);
   __syncthreads();
-  const auto cu = [&](int i) { return in_smem ? cu_s[i] : i < a.n ? __ldcg(&s.res[i]).w : all; };
-  for (long long t0 = 4LL * (rank * NT + tid); t0 < a.n_tokens_max; t0 += 4LL * C * NT) {
-    alignas(16) int slot[4] = {-1, -1, -1, -1}, row[4] = {0, 0, 0, 0};
-    if (t0 < all) {
-      int lo = 0, hi = a.n;                                              // cu(lo) <= t0 < cu(hi)
-      while (hi - lo > 1) { const int mid = (lo + hi) / 2; if (cu(mid) <= t0) lo = mid; else hi = mid; }
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const long long t = t0 + x;
-        if (t >= all) break;
-        while (cu(lo + 1) <= t) ++lo;
-        slot[x] = in_smem ? slot_s[lo] : __ldcg(&s.rec[lo]).x;
-        row[x] = (in_smem ? row_s[lo] : __ldcg(&s.rec[lo]).z) + (int)(t - cu(lo));
-      }
-    }
-    if (t0 + 4 <= a.n_tokens_max) {
-      *reinterpret_cast<int4*>(a.token_slots + t0) = *reinterpret_cast<const int4*>(slot);
-      *reinterpret_cast<int4*>(a.token_rows + t0) = *reinterpret_cast<const int4*>(row);
-    } else {
-      for (int x = 0; x < 4 && t0 + x < a.n_tokens_max; ++x) { a.token_slots[t0 + x] = slot[x]; a.token_rows[t0 + x] = row[x]; }
-    }
-  }
-  phase();
+  for (long long t0 = 4LL * tid; t0 < a.n_tokens_max; t0 += 4LL * NT) lists.write(a, t0);
+  __syncthreads();
 
   // ---- the granted pages ----
   for (int i = rank * groups + mine; i < a.n; i += C * groups) {
@@ -339,15 +363,66 @@ __global__ void __launch_bounds__(NT) paged_plan_kernel(const __grid_constant__ 
 #pragma unroll 4
       for (int j = j0 + gt; j < j1; j += gn) out[j] = __ldcg(&a.stack[top - (j - j0)]);
     } else if (gt < 32) {
-      int k = 0;
-      for (int b = j0; b < j1; b += 32) {
-        const int j = b + lane;
-        const bool need = j < j1 && !held(a, row[j]);
-        const unsigned some = __ballot_sync(0xffffffffu, need);
-        if (need) out[j] = __ldcg(&a.stack[top - k - __popc(some & ((1u << lane) - 1u))]);
-        k += __popc(some);
+      fill_gaps(a, row, out, j0, j1, top);
+    }
+  }
+}
+
+// The second launch of a larger call: lists, and table rows with what is granted.  A CTA takes PIECE tokens or PIECE entries of a row at a time.
+__global__ void __launch_bounds__(RNT) paged_plan_rows_kernel(const __grid_constant__ PlanArgs a) {
+  __shared__ int cu_s[MAX_HELD + 1], slot_s[MAX_HELD], row_s[MAX_HELD];
+  const int tid = threadIdx.x;
+  Scratch s;
+  carve(a.scratch, a.max_seqs, a.n, &s);
+  pdl_wait();
+  const Head head = {left(&s.head->n0), left(&s.head->there), left(&s.head->tokens)};
+  const Lists lists = {cu_s, slot_s, row_s, s, a.n, head.tokens, a.n <= MAX_HELD};
+  lists.take(RNT);
+  __syncthreads();
+  const bool apart = a.table_in != a.table_out;
+  const int pieces = (a.max_pages + PIECE - 1) / PIECE;
+  const long long of_lists = ((long long)a.n_tokens_max + PIECE - 1) / PIECE, items = of_lists + (long long)a.n * pieces;
+  for (long long x = blockIdx.x; x < items; x += gridDim.x) {
+    if (x < of_lists) {
+      const long long t0 = x * PIECE + 4 * tid;
+      if (t0 < a.n_tokens_max) lists.write(a, t0);
+      continue;
+    }
+    const int i = (int)((x - of_lists) / pieces), b0 = (int)((x - of_lists) - (long long)i * pieces) * PIECE, b1 = min(b0 + PIECE, a.max_pages);
+    const int4 r = left(&s.rec[i]), res = left(&s.res[i]);
+    if (r.x < 0 || r.y < 0) continue;
+    const int* row = a.table_in + (long long)r.x * a.max_pages;
+    int* out = a.table_out + (long long)r.x * a.max_pages;
+    const bool granted = res.z >= 0 && r.w > 0;
+    const int j0 = granted ? pages_of(a, r.z) : 0, j1 = granted ? pages_of(a, (long long)r.z + r.y) : 0, top = head.there - 1 - res.y;
+    const bool gaps = granted && r.w != j1 - j0;                         // some of them hold a page: one warp, after the copy
+    if (apart && fours(a, row, out)) {
+      const int j = b0 + 4 * tid;
+      if (j < b1) {
+        int4 e = *reinterpret_cast<const int4*>(row + j);
+        if (!gaps && j < j1 && j + 4 > j0) {
+          if (j >= j0) e.x = __ldcg(&a.stack[top - (j - j0)]);
+          if (j + 1 >= j0 && j + 1 < j1) e.y = __ldcg(&a.stack[top - (j + 1 - j0)]);
+          if (j + 2 >= j0 && j + 2 < j1) e.z = __ldcg(&a.stack[top - (j + 2 - j0)]);
+          if (j + 3 >= j0 && j + 3 < j1) e.w = __ldcg(&a.stack[top - (j + 3 - j0)]);
+        }
+        if (!gaps) *reinterpret_cast<int4*>(out + j) = e;
+        else if (j + 4 <= j0 || j >= j1) *reinterpret_cast<int4*>(out + j) = e;
+        else {
+          if (j < j0) out[j] = e.x;
+          if (j + 1 < j0 || j + 1 >= j1) out[j + 1] = e.y;
+          if (j + 2 < j0 || j + 2 >= j1) out[j + 2] = e.z;
+          if (j + 3 >= j1) out[j + 3] = e.w;
+        }
+      }
+    } else {
+      for (int j = b0 + tid; j < b1; j += RNT) {
+        const bool here = j >= j0 && j < j1;
+        if (here && !gaps) out[j] = __ldcg(&a.stack[top - (j - j0)]);
+        else if (!here && apart) out[j] = row[j];
       }
     }
+    if (gaps && b0 == 0 && tid < 32) fill_gaps(a, row, out, j0, j1, top);
   }
 }
 
@@ -392,7 +467,10 @@ cudaError_t launch_paged_plan(const PlanArgs& a, cudaStream_t st) {
     while (cluster < widest[dev] && cluster * 16384LL < entries) cluster *= 2;
     attr[1].val.clusterDim.x = cluster;
     lc.gridDim = dim3(cluster);
-    e = cudaLaunchKernelEx(&lc, kernel, a);
+    if ((e = cudaLaunchKernelEx(&lc, kernel, a)) != cudaSuccess) return e;
+    count_launch();
+    const long long items = ((long long)a.n_tokens_max + PIECE - 1) / PIECE + (long long)a.n * ((a.max_pages + PIECE - 1) / PIECE), most = 4LL * sm_count();
+    e = launch_pdl(paged_plan_rows_kernel, dim3((unsigned)(items < most ? items : most)), dim3(RNT), 0, st, a);
   }
   count_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
