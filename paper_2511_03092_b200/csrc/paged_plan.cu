@@ -5,6 +5,10 @@
 // A small call is one CTA's, its phases apart by barriers: count (and copy table rows), scan, move (pages given back, lists of tokens), fill
 // (the granted pages, read from a stack that is then complete).  Of a larger one a thread-block cluster counts, scans and gives back, and a
 // second launch writes table rows and lists with the whole GPU.
+//
+// What bounds it: the way of a few numbers through memory, phase after phase, and the launches.  32 requests of a token each take 9.4 us, 6.8 of
+// them without lists, rows and pages; 75 requests of up to 60000 rows and 614405 tokens 22.2 (33.7 in one launch of 16 CTAs), for 10 MB, which
+// HBM brings in 1.5.
 #include <climits>
 
 #include "snap_internal.cuh"
@@ -74,6 +78,7 @@ __device__ __forceinline__ Three block_exclusive(Three v, long long (*part)[NW +
 }
 
 __device__ __forceinline__ bool held(const PlanArgs& a, int entry) { return entry >= 0 && entry < a.n_pages; }
+__device__ __forceinline__ int granted_page(const PlanArgs& a, int at) { return index_ok(at, a.n_pages, a.status) ? __ldcg(&a.stack[at]) : -1; }
 __device__ __forceinline__ int pages_of(const PlanArgs& a, long long rows) { return (int)((rows + a.page - 1) / a.page); }
 
 // What one phase leaves the next is read past the first-level cache, which keeps no order between CTAs.
@@ -141,7 +146,7 @@ __device__ __forceinline__ void fill_gaps(const PlanArgs& a, const int* row, int
     const int j = b + lane, e = j < j1 ? row[j] : 0;
     const bool need = j < j1 && !held(a, e);
     const unsigned some = __ballot_sync(0xffffffffu, need);
-    if (j < j1) out[j] = need ? __ldcg(&a.stack[top - k - __popc(some & ((1u << lane) - 1u))]) : e;
+    if (j < j1) out[j] = need ? granted_page(a, top - k - __popc(some & ((1u << lane) - 1u))) : e;
     k += __popc(some);
   }
 }
@@ -361,7 +366,7 @@ __global__ void __launch_bounds__(NT) paged_plan_kernel(const __grid_constant__ 
     const int j0 = pages_of(a, r.z), j1 = pages_of(a, (long long)r.z + r.y), top = head.there - 1 - res.y;
     if (r.w == j1 - j0) {                                                // none of them holds a page
 #pragma unroll 4
-      for (int j = j0 + gt; j < j1; j += gn) out[j] = __ldcg(&a.stack[top - (j - j0)]);
+      for (int j = j0 + gt; j < j1; j += gn) out[j] = granted_page(a, top - (j - j0));
     } else if (gt < 32) {
       fill_gaps(a, row, out, j0, j1, top);
     }
@@ -401,10 +406,10 @@ __global__ void __launch_bounds__(RNT) paged_plan_rows_kernel(const __grid_const
       if (j < b1) {
         int4 e = *reinterpret_cast<const int4*>(row + j);
         if (!gaps && j < j1 && j + 4 > j0) {
-          if (j >= j0) e.x = __ldcg(&a.stack[top - (j - j0)]);
-          if (j + 1 >= j0 && j + 1 < j1) e.y = __ldcg(&a.stack[top - (j + 1 - j0)]);
-          if (j + 2 >= j0 && j + 2 < j1) e.z = __ldcg(&a.stack[top - (j + 2 - j0)]);
-          if (j + 3 >= j0 && j + 3 < j1) e.w = __ldcg(&a.stack[top - (j + 3 - j0)]);
+          if (j >= j0) e.x = granted_page(a, top - (j - j0));
+          if (j + 1 >= j0 && j + 1 < j1) e.y = granted_page(a, top - (j + 1 - j0));
+          if (j + 2 >= j0 && j + 2 < j1) e.z = granted_page(a, top - (j + 2 - j0));
+          if (j + 3 >= j0 && j + 3 < j1) e.w = granted_page(a, top - (j + 3 - j0));
         }
         if (!gaps) *reinterpret_cast<int4*>(out + j) = e;
         else if (j + 4 <= j0 || j >= j1) *reinterpret_cast<int4*>(out + j) = e;
@@ -418,7 +423,7 @@ __global__ void __launch_bounds__(RNT) paged_plan_rows_kernel(const __grid_const
     } else {
       for (int j = b0 + tid; j < b1; j += RNT) {
         const bool here = j >= j0 && j < j1;
-        if (here && !gaps) out[j] = __ldcg(&a.stack[top - (j - j0)]);
+        if (here && !gaps) out[j] = granted_page(a, top - (j - j0));
         else if (!here && apart) out[j] = row[j];
       }
     }
@@ -430,7 +435,10 @@ __global__ void __launch_bounds__(RNT) paged_plan_rows_kernel(const __grid_const
 
 size_t paged_plan_scratch_bytes(int max_seqs, int n_seqs) { return carve(nullptr, max_seqs, n_seqs, nullptr); }
 
-// One CTA where there is little to do.  Else a cluster with a CTA for every 16384 entries of table rows and of the list, up to 16.
+// One CTA where there is little to do, else a cluster of 16 (8 where the device takes no more) and the second launch.  (One CTA against
+// two launches: 32 requests, rows of 512 entries 9.3 / 12.8 us; 64 13.1 / 13.9; 128 19.3 / 14.0; 32 of 1024 tokens each 15.9 / 13.3; 8 of
+// 4096 13.9 / 13.1.  Clusters of 16 / 8 / 4: 75 requests of 614405 tokens, rows of 8192 entries 22.3 / 25.9 / 31.9; 2000 requests 34.9 / 43.3
+// / 59.1; no call was shorter with fewer.)
 cudaError_t launch_paged_plan(const PlanArgs& a, cudaStream_t st) {
   const long long entries = (long long)a.n * (a.table_in != a.table_out ? a.max_pages : 64) + a.n_tokens_max;
   cudaLaunchAttribute attr[2];
@@ -463,8 +471,7 @@ cudaError_t launch_paged_plan(const PlanArgs& a, cudaStream_t st) {
       (void)cudaGetLastError();
       widest[dev] = wide ? 16 : 8;
     }
-    int cluster = 1;
-    while (cluster < widest[dev] && cluster * 16384LL < entries) cluster *= 2;
+    const int cluster = widest[dev];
     attr[1].val.clusterDim.x = cluster;
     lc.gridDim = dim3(cluster);
     if ((e = cudaLaunchKernelEx(&lc, kernel, a)) != cudaSuccess) return e;

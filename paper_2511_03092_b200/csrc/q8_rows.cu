@@ -183,7 +183,7 @@ __global__ void __launch_bounds__(ANT, 4) q8_append_kernel(const __grid_constant
     };
     angles(0, min(SLAB, n));                                             // while the table answers
     if (tid < n_blocks) {
-      if (page < 0 || page >= pm.n_pages) {
+      if (!index_ok(off / B, r.map.blocks, r.status) || page < 0 || page >= pm.n_pages) {
         page = -1;
         if (y == 0 && r.status) atomicOr(r.status, SNAP_DEV_BAD_PAGE);
       }
@@ -362,7 +362,7 @@ __global__ void __launch_bounds__(ANT, 4) q8_append_kernel(const __grid_constant
       __syncthreads();
     }
     __syncthreads();                                                     // what the run's blocks are has been read
-    if (t + n == to && y == 0 && tid == 0) a.seq_len[slot] = (int)min((long long)row + n, (long long)pm.cap);
+    if (t + n == to && y == 0 && tid == 0 && index_ok(slot, r.max_seqs, r.status)) a.seq_len[slot] = (int)min((long long)row + n, (long long)pm.cap);
     t += n;
   }
 }
