@@ -590,7 +590,7 @@ int snap_paged_evict(const snap_config_t* cfg, const snap_paged_t* paged, const 
  *           past the table) exceed n_tokens_max, or, when it misses any, the pages missing so far those that are
  *           free (SNAP_DEV_NO_ROOM).
  *   A slot of -1 is padding; a slot out of range or listed before is skipped (SNAP_DEV_BAD_SLOT).
- *   page_table_in_dev, page_table_out_dev  [max_seqs][max_pages], the same array or two that do not overlap: with two, the rows of the
+ *   page_table_in_dev, page_table_out_dev  [max_seqs][max_pages], the same array or two that do not overlap (checked): with two, the rows of the
  *             slots listed are written whole and the table that a running step reads stays as it is
  *   seq_len_dev [max_seqs]: read; 0 where the sequence has ended (appending counts the new rows, not this call)
  *   free_pages_dev [n_pages]: the stack of free pages, its top last; n_free_in_dev, n_free_out_dev [1]: how many it holds before and

@@ -61,6 +61,9 @@ int snap_paged_plan(const snap_config_t* cfg, const snap_paged_t* paged, const i
       (n_seqs > 0 && (!slot_ids_dev || !new_tokens_dev || !page_table_in_dev || !page_table_out_dev || !seq_len_dev || !free_pages_dev || !first_rows_dev)))
     return SNAP_ERR_NULL_POINTER;
   if (misaligned(token_slots_dev, token_rows_dev) || misaligned(workspace_dev)) return SNAP_ERR_INVALID_ARG;
+  const uintptr_t in = reinterpret_cast<uintptr_t>(page_table_in_dev), out = reinterpret_cast<uintptr_t>(page_table_out_dev),
+                  size = sizeof(int32_t) * (uintptr_t)cfg->max_seqs * (uintptr_t)paged->max_pages;
+  if (n_seqs > 0 && in != out && (in < out ? out - in : in - out) < size) return SNAP_ERR_INVALID_ARG;   // a row would be read after it was written
   if (workspace_bytes < paged_plan_scratch_bytes(cfg->max_seqs, n_seqs)) return SNAP_ERR_WORKSPACE_TOO_SMALL;
   PlanArgs a;
   a.slots = slot_ids_dev; a.new_tokens = new_tokens_dev; a.table_in = page_table_in_dev; a.table_out = page_table_out_dev;

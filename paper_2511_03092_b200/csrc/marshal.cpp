@@ -1,6 +1,6 @@
-// Argument marshalling of the rotary and paged-cache calls, those of the 8-bit cache among them: checks that the tensors of a call are what the library is
-// told they are and passes their addresses on.  A serving step makes these calls once per layer, and the same checks
-// cost 5 to 10 us a call as Python expressions, more than the kernels of a small step take.
+// Argument marshalling of the rotary and paged-cache calls, those of the 8-bit cache among them: checks that the tensors
+// of a call are what the library is told they are and passes their addresses on.  A serving step makes these calls once
+// per layer, and the same checks cost 5 to 10 us a call as Python expressions, more than the kernels of a small step take.
 //
 // Every function takes the address of the library's entry point, the structures (ctypes objects, read through the buffer
 // protocol), the tensors or None, and the stream's handle or None for the current one.  It returns the entry point's

@@ -25,7 +25,7 @@ using umma::mbar_try_wait;
 constexpr int UNIT_TILES = 6;                   // what a unit costs besides its tiles, in tiles; units of at most that many stay whole
                                                 // (a kernel's arguments may have other numbers: share(), whole())
 constexpr int MIN_TILES = 1;                    // a CTA gets at least that much beyond one unit's share (at least one: no stretch is empty)
-// (Measured over 40 calls of all sizes: 4 and 4 take 8 % longer, 8 and 1 2 %, 4 and 1 as long but 4 % longer for many short sequences.)
+// (Over full-precision pages, 40 calls of all sizes: 4 and 4 take 8 % longer, 8 and 1 2 %, 4 and 1 as long but 4 % longer for many short sequences.)
 constexpr int MAX_CTAS = 1024, MAX_HELD = 128;  // sequences whose slot and length a CTA keeps in shared memory
 // (Held against looked up in the batch's arrays: 17 sequences of up to 400 rows 14.4 / 14.95 us, 45 of 333 14.75 / 15.0, 100 of 500 35.7 /
 // 35.8, 128 of 2000 96.7 / 97.0: the more sequences, the less it is worth.)

@@ -204,3 +204,13 @@ def test_the_binding_checks_what_tensors_are():
         B.snap_paged_q8_gather(cfg, paged.pages, **gat)
     with pytest.raises(ValueError):
         B.make_page_map(16, 10, i32(3))
+
+
+def test_a_plan_refuses_tables_that_overlap():
+    size = 4 * 3 * 50                                       # of a table: 3 sequences, 50 pages each
+    pages = B.make_page_map(64, 100, torch.zeros(3, 50, dtype=torch.int32))
+    base = 1 << 20
+    for off in (4, 200, size - 4, -4, 4 - size):
+        assert _plan(paged=pages, tin=base, tout=base + off) == -1, off
+    for off in (0, size, -size):                            # in place, or apart: the call goes on (to scratch that is too small)
+        assert _plan(paged=pages, tin=base, tout=base + off, size=0) == -3, off
