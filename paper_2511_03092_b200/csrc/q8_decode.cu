@@ -22,8 +22,8 @@
 // Where a row's heads lie side by side (pages stored rows first), two warps of a CTA take one head and two the next, over the same rows: HBM
 // then delivers twice as much in a row (128-byte heads, 16 long sequences: 208 us without, 172 with; heads first 168).
 //
-// What bounds it: 16 sequences of 8192 to 65536 rows, 32 heads on 8 of 128 dims, HBM; four tokens a step (16 columns), instructions, some 780 per
-// tile and warp: 8 sequences of 9000 to 16384 rows 60 us; small calls, the chain of look-up, first tiles, exchange and join, in two
+// What bounds it: 16 sequences of 8192 to 65536 rows, 32 heads on 8 of 128 dims, HBM; four tokens a step (16 columns), some 780 instructions per
+// tile and warp, which wait for one another's results, two warps to a scheduler: 8 sequences of 9000 to 16384 rows 58 to 60 us; small calls, the chain of look-up, first tiles, exchange and join, in two
 // launches: one sequence of 5124 rows 11.7 us, 45 of up to 333 14.8.
 #include <type_traits>
 
@@ -419,9 +419,9 @@ q8_mma_kernel(const __grid_constant__ Q8Args a, const __grid_constant__ CUtensor
 #pragma unroll 1
       for (int pass = 0;; ++pass) {                                      // (a unit's first tile has no reference yet)
         float largest = 0.f;
-        if (!fresh || pass > 0) {
 #pragma unroll
-          for (int gi = 0; gi < NG; ++gi) add[gi][0] = add[gi][1] = 0.f;
+        for (int gi = 0; gi < NG; ++gi) add[gi][0] = add[gi][1] = 0.f;
+        if (!fresh || pass > 0) {
 #pragma unroll
           for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -433,11 +433,14 @@ q8_mma_kernel(const __grid_constant__ Q8Args a, const __grid_constant__ CUtensor
                 for (int c = 0; c < 2; ++c) {
                   const float e = fast_exp2(v[mt][gi][2 * r8 + c] - ref[gi][c]);
                   add[gi][c] += e;
-                  p[mt][gi][2 * r8 + c] = e * (v_scale * f[gi][c]);
+                  p[mt][gi][2 * r8 + c] = e * v_scale * f[gi][c];        // (in this order: no zero meets an infinity)
                   largest = fmaxf(largest, p[mt][gi][2 * r8 + c]);
                 }
             }
         }
+        // (weights far above the reference are a reason too, however small the scales they meet: they would leave single precision)
+#pragma unroll
+        for (int gi = 0; gi < NG; ++gi) largest = fmaxf(largest, (add[gi][0] + add[gi][1]) * 0x1p-45f);
         // (a NaN is no reason: it ends in the sums whatever the reference)
         if (pass > 0 || !(fresh || __any_sync(0xffffffffu, largest > LIMIT))) break;
         fresh = false;
@@ -460,7 +463,8 @@ q8_mma_kernel(const __grid_constant__ Q8Args a, const __grid_constant__ CUtensor
             }
             const float to = fmaxf(ref[gi][c], mx), moved = ref[gi][c] - to, al = exp2f(moved);
             const int was = exponent_of(f[gi][c]);                       // TARGET - was: of the largest product so far
-            const int now = (int)fminf(fmaxf(TARGET - floorf(fmaxf(ref[gi][c] == NOTHING ? NOTHING : (float)(TARGET - was) + moved, big - to)), -100.f), 100.f);
+            const float before = ref[gi][c] == NOTHING ? NOTHING : (float)(TARGET - was) + moved;
+            const int now = (int)fminf(fmaxf(TARGET - floorf(fmaxf(before, big - to)), -126.f), 126.f);
             const float y = al * power_of(now - was);
             l_part[gi][c] *= al;
             ref[gi][c] = to;
@@ -693,7 +697,10 @@ cudaError_t launch_q8_decode(int dtype, const Shape& s, const Q8Map& m, const Q8
   using BF = __nv_bfloat16;
   e = dtype == SNAP_F32 ? launch_type<float>(a, d, tk, tv, st) : launch_type<BF>(a, d, tk, tv, st);
   if (e != cudaSuccess) return e;
-  const int heads = n_active * a.rows_seq, by_heads = heads <= 512 || p.ctas < 2;
+  // Joined by heads unless there is a unit for every CTA: then few are cut.  (By heads / by borders: 192 units on 296 CTAs, 24 sequences of 2000
+  // to 9000 rows 58.3 / 59.9 us; 48, six of 300 to 1000 24.2 / 26.2; 128, 16 of 3000 to 9000 48.6 / 52.6; 384, 48 of 300 to 700 29.1 / 28.5; 540
+  // on 444, 45 of up to 333 16.3 / 14.8.)
+  const int heads = n_active * a.rows_seq, by_heads = ((long long)n_active * a.U <= p.ctas && heads <= 4096) || p.ctas < 2;
   const dim3 grid((unsigned)(by_heads ? heads : p.ctas - 1));
   e = dtype == SNAP_F32 ? launch_pdl(q8_join_kernel<float>, grid, dim3(JNT), 0, st, a, by_heads)
                         : launch_pdl(q8_join_kernel<BF>, grid, dim3(JNT), 0, st, a, by_heads);

@@ -122,6 +122,32 @@ def test_units_around_the_longest_that_stays_whole(lengths):
     assert c.bits() == 0
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("logit,old,new", [(16.0, 46, -110), (-16.0, -126, 40), (16.0, -126, 100), (-16.0, 100, -126), (0.0, 112, 112)])
+def test_weights_and_scales_at_the_ends_of_their_range(logit, old, new, dtype):
+    """Rows with scales of 2^old, then one whose weight is 2^184 times theirs, or 2^-184, among rows with scales of 2^new: products of
+    weights, scales and what brings them to half precision leave single precision at either end."""
+    cfg = config(2, 1, 64, dtype=dtype)
+    c = Pages8(cfg, 64, 16, [400], seed=1)
+    codes = [x.view(torch.uint8) for x in c.pools]
+    codes[0].zero_()
+    codes[1].copy_(torch.from_numpy(orc.encode(50 + np.random.default_rng(0).random(codes[1].shape) * 50)).cuda())
+    c.scales[0].fill_(1.0)
+    c.scales[1].fill_(2.0 ** old)
+    row, p = 130, c.table[0].tolist()
+    codes[0][p[row // 64], 0, row % 64, 0] = int(orc.encode(logit))
+    for r in range(128, 400):
+        c.scales[1][p[r // 64], 0, r % 64 // 16] = 2.0 ** new
+    if old < -100:                                          # (what the append makes of rows of zeros)
+        for r in range(128):
+            codes[1][p[r // 64], 0, r % 64] = 0
+    q = torch.zeros(1, 1, 2, 64, dtype=DT[dtype], device="cuda")
+    q[..., 0] = 64.0
+    out = run_decode(c, q, i32([0]))
+    assert torch.isfinite(out).all()
+    check_decode(c, q, [0], out, dtype)
+
+
 FIRST = """
 import sys
 sys.path.insert(0, %r)
