@@ -465,7 +465,8 @@ q8_mma_kernel(const __grid_constant__ Q8Args a, const __grid_constant__ CUtensor
             const int was = exponent_of(f[gi][c]);                       // TARGET - was: of the largest product so far
             const float before = ref[gi][c] == NOTHING ? NOTHING : (float)(TARGET - was) + moved;
             const int now = (int)fminf(fmaxf(TARGET - floorf(fmaxf(before, big - to)), -126.f), 126.f);
-            const float y = al * power_of(now - was);
+            const int by = now - was;                                    // in two factors: it may pass what one can hold
+            const float y = al * power_of(by / 2) * power_of(by - by / 2);
             l_part[gi][c] *= al;
             ref[gi][c] = to;
             f[gi][c] = exp2_of(now);
