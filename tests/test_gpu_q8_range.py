@@ -7,7 +7,8 @@ within 2^6 of one another, to 1 or more: a weight is off by half a step, 2^-11 o
 largest product.  Sums: each tensor-core product adds 16 rows to a sum and may cut it, 4 e; tiles, warps and pieces come on top, n / 16 + 64
 additions in all.  So
 |err| <= u |out| + (2 L + 2^-20 + 2^-11 [fp32: 2^-21] + 4 (n / 16 + 64) e) sum_r p_r |v_r| + 2^-25 [2^-36] sum_r max_r'(p_r' s_r') |code_r|,
-r' in r's tile with a scale within 2^6 of r's."""
+r' in r's tile with a scale within 2^6 of r's; and half of the smallest step there is, where an output lies below the normal numbers of its
+type: bf16 numbers under 2^-126 are 2^-133 apart, which is 2^-134, of single precision 2^-150 for each addition."""
 import numpy as np
 import pytest
 import torch
@@ -52,6 +53,7 @@ def check_near(c, q, slots, out, dtype, reach_terms=None, sums=None):
                     top[a] = np.where(near, (p * sh)[a][None], 0).max(axis=1)
                 bound = HALF_STEP[dtype] * np.abs(want) + (2 * L + 2.0 ** -20 + step + 4 * (sums or m / 16 + 64) * E) * mass
                 bound = bound + least * (top[:, None] * np.abs(vh) / sh[:, None]).sum(axis=0)
+                bound = bound + (2.0 ** -134 if dtype == "bf16" else (sums or m / 16 + 64) * 2.0 ** -150)
                 err = np.abs(got[h] - want)
                 assert (err <= bound).all(), f"entry {i}, token {u}, head {h}: {err.max():.3e}, {(err / bound).max():.1f} times the bound"
 
@@ -83,3 +85,109 @@ def test_a_tile_of_far_larger_scales_leaves_what_was_summed_before(old, new, dty
     out = run_decode(c, q, i32([0]))
     check_near(c, q, [0], out, dtype)
     assert c.bits() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("old,new", [(-126, 110), (-100, 60), (60, -100), (110, -126)])
+def test_tiles_on_scales_at_both_ends(old, new, dtype):
+    """Whole tiles of zero codes on one scale and of ordinary ones on the other, either first."""
+    cfg = config(4, 2, 64, dtype=dtype)
+    low = min(old, new)
+    for rows in (range(352, 384), range(0, 320), range(160, 192)):
+        c = Pages8(cfg, 32, 32, [384], seed=1, spread=0)
+        c.scales[1].fill_(2.0 ** old)
+        fill(c, rows, scale=2.0 ** new)
+        fill(c, rows if new > low else [r for r in range(384) if r not in rows], codes=0)
+        q = queries(1, 1, 4, 64, dtype)
+        check_near(c, q, [0], run_decode(c, q, i32([0])), dtype)
+        assert c.bits() == 0
+
+
+@pytest.mark.parametrize("layout,hq,hkv,d", [("hnd", 8, 2, 128), ("nhd", 2, 2, 64), ("hnd", 5, 1, 80), ("hnd", 2, 2, 256)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("q_len", [1, 4])
+@pytest.mark.parametrize("at", [0, 176, 368])
+def test_a_block_of_zeros_with_a_far_larger_scale(at, q_len, dtype, layout, hq, hkv, d):
+    """Sixteen rows of zero codes, first, in the middle or last, on scales 2^4 to 2^128 above the others'."""
+    cfg = config(hq, hkv, d, dtype=dtype)
+    c = Pages8(cfg, 64 if at else 8, 16 if at else 8, [384], seed=at + d, layout=layout)
+    q = queries(1, q_len, hq, d, dtype, seed=at)
+    fill(c, range(at, at + 16), codes=0)
+    for up in (4, 8, 12, 16, 20, 24, 40, 128):
+        fill(c, range(at, at + 16), scale=2.0 ** (up - 8))
+        check_near(c, q, [0], run_decode(c, q, i32([0])), dtype)
+    assert c.bits() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("q_len", [1, 3])
+def test_scales_that_fall_from_block_to_block(q_len, dtype):
+    """Each block's scale 2^9 below that of the block before, all codes in use; weights that grow the other way, so that every block counts."""
+    cfg = config(2, 1, 64, dtype=dtype, scale=1.0)
+    c = Pages8(cfg, 16, 4, [44], seed=5)
+    c.k.view(torch.uint8).zero_()
+    c.ks.fill_(1.0)
+    for b in range(11):
+        fill(c, range(4 * b, 4 * b + 4), scale=2.0 ** (40 - 9 * b))
+        for j in range(4):                                  # logits of about 9 ln 2 more each block
+            row = torch.zeros(64, dtype=torch.uint8, device="cuda")
+            row[0], row[1] = int(orc.encode(6.0 * b)), int(orc.encode(0.24 * b + 0.1 * j))
+            fill(c, [4 * b + j], codes=row, which=0)
+    q = torch.zeros(1, q_len, 2, 64, dtype=DT[dtype], device="cuda")
+    q[..., :2] = 1.0
+    check_near(c, q, [0], run_decode(c, q, i32([0])), dtype, reach_terms=2)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_an_outlier_whose_weight_has_vanished(dtype):
+    """One row far larger than the others that almost nobody attends, its neighbours' codes zero on its scale."""
+    cfg = config(4, 1, 64, dtype=dtype, scale=1.0)
+    for logit, scale in ((-40.0, 2.0 ** 40), (-40.0, 2.0 ** 30), (-80.0, 2.0 ** 100), (-200.0, 2.0 ** 100), (-20.0, 2.0 ** 24)):
+        c = Pages8(cfg, 32, 16, [300], seed=2)
+        c.ks.fill_(2.0 ** -9)
+        fill(c, range(160, 176), codes=0, scale=scale)
+        fill(c, [165], codes=int(orc.encode(400.0)))
+        row = torch.zeros(64, dtype=torch.uint8, device="cuda")
+        row[0] = int(orc.encode(logit))
+        fill(c, [165], codes=row, which=0)
+        fill(c, range(160, 176), scale=1.0, which=0)
+        q = queries(1, 1, 4, 64, dtype, seed=3)
+        q[..., 0] = 1.0
+        check_near(c, q, [0], run_decode(c, q, i32([0])), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("value", [float("inf"), 3e30])
+def test_a_draft_that_was_not_finite_is_taken_back(value, dtype):
+    """A draft token with an infinity is appended, attended by its own query alone, and given up; the block keeps its scale."""
+    cfg = config(4, 2, 64, dtype=dtype)
+    c = Pages8(cfg, 64, 16, [200], seed=4, capacity=256)
+    c.table[0, :4] = i32((c.table[0].tolist() + c.free)[:4])
+    k, v = (torch.randn(3, 2, 64, device="cuda", generator=torch.Generator(device="cuda").manual_seed(x)).to(DT[dtype]) for x in (1, 2))
+    v[2, :, 5] = value
+    q = queries(1, 3, 4, 64, dtype)
+    B.snap_paged_q8_append(cfg, c.paged, i32([0]), i32([0, 3]), i32([200]), k, v, *c.cache, c.seq_len, status=c.status)
+    out = run_decode(c, q, i32([0]))
+    c.seq_len.fill_(202)                                    # the draft is taken back
+    check_near(c, q[:, :2], [0], out[:, :2], dtype)
+    check_near(c, q, [0], run_decode(c, q, i32([0])), dtype)
+    B.snap_paged_q8_append(cfg, c.paged, i32([0]), i32([0, 2]), i32([202]), k[:2].contiguous(), v[:2].contiguous(), *c.cache, c.seq_len,
+                           status=c.status)
+    check_near(c, q, [0], run_decode(c, q, i32([0])), dtype)
+    assert c.bits() == 0
+
+
+def test_outputs_do_not_follow_the_power_of_other_tiles():
+    """A row that has nearly all the weight and codes of zero, as an attention sink has, then rows on ever smaller weights."""
+    cfg = config(2, 1, 64, scale=1.0)
+    c = Pages8(cfg, 64, 16, [3000], seed=6, spread=0)
+    c.k.view(torch.uint8).zero_()
+    c.ks.fill_(1.0)
+    c.v.view(torch.uint8).copy_(c.v.view(torch.uint8) & 0x7f)
+    fill(c, [0], codes=0)
+    row = torch.zeros(64, dtype=torch.uint8, device="cuda")
+    row[0] = int(orc.encode(40.0))
+    fill(c, [0], codes=row, which=0)
+    q = torch.zeros(1, 1, 2, 64, dtype=torch.bfloat16, device="cuda")
+    q[..., 0] = 1.0
+    check_near(c, q, [0], run_decode(c, q, i32([0])), "bf16", reach_terms=1)
