@@ -19,8 +19,8 @@
 // taken off again when a tile's outputs are added to the sums: these are of single precision, in the numbers' own size, so that no tile
 // depends on what another one held.  The power and the reference of the exponentials move when a tile's largest product leaves [1, 2^15].  A tile
 // whose value scales lie more than 2^6 apart (a block keeps the scale of a row that was given up) goes through several times, the rows of
-// the largest scales first.  Products round to 11 bits (bf16: an eighth of the output's own rounding) or are two numbers (single precision), below
-// 2^-14 of the largest one to multiples of 2^-25 of it.  (Sums that are held on the columns' powers instead, and lose the rows of smaller scales:
+// the largest scales first.  Products round to 11 bits (bf16: an eighth of the output's own rounding) or are two numbers, the second in units of
+// 2^-11 and summed apart (single precision: 22 bits); below 2^-14 of the largest one they round to multiples of 2^-25 of it (2^-36).  (Sums that are held on the columns' powers instead, and lose the rows of smaller scales:
 // 16 long sequences 181 us instead of 188, four tokens a step 58.6 instead of 61.4, calls of all kinds 0.8 % less.  A loop around a tile's
 // rounds instead of a second way through the loop over tiles: 4 to 5 % more, 72 us for the four tokens.)
 //
@@ -120,10 +120,10 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   const __half2 v = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
-// x as two half-precision numbers: what rounding leaves of it
-__device__ __forceinline__ uint32_t rest_f16(float lo, float hi, uint32_t rounded) {
+// x as two half-precision numbers: what rounding leaves of it, times `by`
+__device__ __forceinline__ uint32_t rest_f16(float lo, float hi, uint32_t rounded, float by = 1.f) {
   const float2 r = __half22float2(*reinterpret_cast<const __half2*>(&rounded));
-  return pack_f16(lo - r.x, hi - r.y);
+  return pack_f16((lo - r.x) * by, (hi - r.y) * by);
 }
 __device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
@@ -145,6 +145,7 @@ q8_mma_kernel(const __grid_constant__ Q8Args a, const __grid_constant__ CUtensor
   // scales that lie further than 2^NEAR apart do not meet.
   constexpr float LEAST = 1.f, LIMIT = 32768.f;
   constexpr int TARGET = 9, NEAR = 6;
+  constexpr float REST = 2048.f;                                         // a second number's unit: it is half a last bit of the first, at most as large again
   constexpr unsigned ALL = NG == 1 ? 0xffu : 0xffffu;                    // a bit for each of the warp's columns
   extern __shared__ unsigned char smem_dyn[];
   unsigned char* stages = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~uintptr_t(1023));
@@ -541,14 +542,14 @@ q8_mma_kernel(const __grid_constant__ Q8Args a, const __grid_constant__ CUtensor
             const float p0 = p[mt][gi][2 * r8], p1 = p[mt][gi][2 * r8 + 1];
             const uint32_t hi = pack_f16(p0, p1);
             pb[mt][gi][0][r8] = movmatrix_t(hi);
-            if constexpr (F32) pb[mt][gi][PARTS - 1][r8] = movmatrix_t(rest_f16(p0, p1, hi));
+            if constexpr (F32) pb[mt][gi][PARTS - 1][r8] = movmatrix_t(rest_f16(p0, p1, hi, REST));
           }
 #pragma unroll
       for (int db = 0; db < KS; ++db) {
         if (!EXACT && 16 * db >= d_v) break;
         uint32_t c[4];                                                   // dims gq and + 8, of the tile's first 16 rows, then of the others
         ldsm_bytes_t((b_V ^ (db % (SW / 16) << 4)) + db * 16 / SW * S::SLAB_B, c);
-        float o[NG][4];
+        float o[NG][PARTS][4];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
           const uint32_t a0 = halves_of_codes(c[2 * mt] & 0xffffu), a2 = halves_of_codes(c[2 * mt] >> 16);
@@ -557,14 +558,17 @@ q8_mma_kernel(const __grid_constant__ Q8Args a, const __grid_constant__ CUtensor
           for (int gi = 0; gi < NG; ++gi)
 #pragma unroll
             for (int y = PARTS - 1; y >= 0; --y) {
-              if (mt == 0 && y == PARTS - 1) mma_f16_first(o[gi], a0, a1, a2, a3, pb[mt][gi][y][0], pb[mt][gi][y][1]);
-              else mma_f16(o[gi], a0, a1, a2, a3, pb[mt][gi][y][0], pb[mt][gi][y][1]);
+              if (mt == 0) mma_f16_first(o[gi][y], a0, a1, a2, a3, pb[mt][gi][y][0], pb[mt][gi][y][1]);
+              else mma_f16(o[gi][y], a0, a1, a2, a3, pb[mt][gi][y][0], pb[mt][gi][y][1]);
             }
         }
 #pragma unroll
         for (int gi = 0; gi < NG; ++gi)
 #pragma unroll
-          for (int x = 0; x < 4; ++x) oacc[gi][db][x] = fmaf(o[gi][x], one_over(f[gi][x & 1]), oacc[gi][db][x]);
+          for (int x = 0; x < 4; ++x) {
+            const float sum = F32 ? fmaf(o[gi][PARTS - 1][x], 1.f / REST, o[gi][0][x]) : o[gi][0][x];
+            oacc[gi][db][x] = fmaf(sum, one_over(f[gi][x & 1]), oacc[gi][db][x]);
+          }
       }
       __syncwarp();
       // the stage was read, and possibly cleared, through the generic proxy; the copy that refills it is of the async proxy

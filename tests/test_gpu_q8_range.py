@@ -191,3 +191,22 @@ def test_outputs_do_not_follow_the_power_of_other_tiles():
     q = torch.zeros(1, 1, 2, 64, dtype=torch.bfloat16, device="cuda")
     q[..., 0] = 1.0
     check_near(c, q, [0], run_decode(c, q, i32([0])), "bf16", reach_terms=1)
+
+
+@pytest.mark.parametrize("n,nats", [(16385, 13.0), (40000, 16.0), (61, 16.0), (700, 20.0)])
+def test_single_precision_keeps_small_weights(n, nats):
+    """A row of zero codes that has nearly all the weight, as an attention sink has: the output is made of weights of 2^-19 to 2^-29, and is
+    as good as it is without that row.  (Each block has the fewest tiles a stretch can have, 5 or 6, or all of a short sequence: a warp
+    adds 2 or 6 of them, two products each, four warps join, then 125 pieces or fewer, a warp taking an eighth of them: 40 additions at most.)"""
+    cfg = config(2, 1, 64, dtype="f32", scale=1.0)
+    c = Pages8(cfg, 64, 64, [n], seed=6, spread=0)
+    c.k.view(torch.uint8).zero_()
+    c.ks.fill_(1.0)
+    c.v.view(torch.uint8).copy_(c.v.view(torch.uint8) & 0x7f)
+    fill(c, [0], codes=0)
+    row = torch.zeros(64, dtype=torch.uint8, device="cuda")
+    row[0] = int(orc.encode(nats))
+    fill(c, [0], codes=row, which=0)
+    q = torch.zeros(1, 1, 2, 64, dtype=torch.float32, device="cuda")
+    q[..., 0] = 1.0 + torch.arange(2, device="cuda") / 32
+    check_near(c, q, [0], run_decode(c, q, i32([0])), "f32", reach_terms=1, sums=40)
