@@ -425,7 +425,7 @@ q8_mma_kernel(const __grid_constant__ Q8Args a, const __grid_constant__ CUtensor
 #pragma unroll
           for (int gi = 0; gi < NG; ++gi)
 #pragma unroll
-            for (int c = 0; c < 2; ++c) v[mt][gi][2 * r8 + c] *= q_scale[gi][c] * k_scale;
+            for (int c = 0; c < 2; ++c) v[mt][gi][2 * r8 + c] *= fminf(q_scale[gi][c] * k_scale, -NOTHING);   // (0 times infinity is no logit)
         }
       if (rows != 0xffffffffu || row0 + TR > all_see) {
 #pragma unroll

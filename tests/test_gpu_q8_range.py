@@ -210,3 +210,16 @@ def test_single_precision_keeps_small_weights(n, nats):
     q = torch.zeros(1, 1, 2, 64, dtype=torch.float32, device="cuda")
     q[..., 0] = 1.0 + torch.arange(2, device="cuda") / 32
     check_near(c, q, [0], run_decode(c, q, i32([0])), "f32", reach_terms=1, sums=40)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("size,scale", [(2.0 ** 24, 2.0 ** 120), (2.0 ** 100, 2.0 ** 60), (2.0 ** 60, 2.0 ** 120)])
+def test_large_queries_meet_zero_keys_on_large_scales(size, scale, dtype):
+    """Keys of zero codes on the scale that a key taken back left: logits of zero, however large the query."""
+    cfg = config(4, 1, 64, dtype=dtype)
+    c = Pages8(cfg, 32, 16, [150], seed=2)
+    c.ks.mul_(1.0 / size)
+    fill(c, range(64, 80), codes=0, scale=scale, which=0)
+    q = queries(1, 2, 4, 64, dtype) * size
+    q[0, 0, 1] /= size                                      # (a column beside it whose logits are next to nothing)
+    check_near(c, q, [0], run_decode(c, q, i32([0])), dtype)
