@@ -125,6 +125,8 @@ __device__ __forceinline__ uint32_t rest_f16(float lo, float hi, uint32_t rounde
   const float2 r = __half22float2(*reinterpret_cast<const __half2*>(&rounded));
   return pack_f16((lo - r.x) * by, (hi - r.y) * by);
 }
+// Of four codes, a one for each that is a NaN, in the lowest bit of its byte
+__device__ __forceinline__ uint32_t nan_codes(uint32_t four) { return ((four & 0x7f7f7f7fu) + 0x01010101u) >> 7 & 0x01010101u; }
 __device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
@@ -159,11 +161,13 @@ q8_mma_kernel(const __grid_constant__ Q8Args a, const __grid_constant__ CUtensor
   __shared__ int scan[S::NT / 32 + 2];
   __shared__ Held held;
   __shared__ Found found;
+  __shared__ int some_nan;                                               // a NaN among a segment's values that not every column sees
 
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, gq = lane >> 2, tq = lane & 3, side = w % SIDES, ws = w / SIDES;
   unsigned char* wstages = stages + w * NSTAGE * S::STAGE_B;
   float* wscales = row_scales + w * NSTAGE * 2 * TR;
   const uint32_t stage0 = smem_u32(wstages), scale0 = smem_u32(wscales), bar0 = smem_u32(bars + w * NSTAGE);
+  if (tid == 0) some_nan = 0;
   if (lane == 0) {
     for (int s = 0; s < NSTAGE; ++s) mbar_init(bar0 + 8 * s, BY_ROWS ? 32 : 33);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -370,13 +374,25 @@ q8_mma_kernel(const __grid_constant__ Q8Args a, const __grid_constant__ CUtensor
 #pragma unroll
       for (int y = 1; y < NSTAGE; ++y) rows = y == s ? there_of[y] : rows;
       const uint32_t l_K = l_at + s * S::STAGE_B, b_V = b_at + s * S::STAGE_B;
-      if (rows != 0xffffffffu) {
-        // rows past the end, or on a bad page, may hold anything, and a zero weight does not silence a NaN in V: clear them
+      if (rows != 0xffffffffu || row0 + TR > all_see) {
+        // Rows past the end, or on a bad page, may hold anything, and a zero weight does not silence a NaN in V: clear them.  Of a row that only
+        // some columns see a NaN becomes a code of zero; those columns get theirs at the segment's end.
         constexpr int CPR = D / 16;
-        for (int x = lane; x < TR * CPR; x += 32) {
+        const int from = min(rows != 0xffffffffu ? __ffs(~rows) - 1 : TR, max(all_see - row0, 0));
+#pragma unroll 1
+        for (int x = from * CPR + lane; x < TR * CPR; x += 32) {
           const int r = x / CPR, c = x % CPR;
-          if (!((rows >> r) & 1u))
-            *reinterpret_cast<uint4*>(wstages + s * S::STAGE_B + S::TENS_B + c / (SW / 16) * S::SLAB_B + swizzled<SW>(r, c % (SW / 16))) = make_uint4(0, 0, 0, 0);
+          if (((rows >> r) & 1u) && row0 + r < all_see) continue;
+          uint4* at = reinterpret_cast<uint4*>(wstages + s * S::STAGE_B + S::TENS_B + c / (SW / 16) * S::SLAB_B + swizzled<SW>(r, c % (SW / 16)));
+          uint4 w = make_uint4(0, 0, 0, 0);
+          if ((rows >> r) & 1u) {
+            w = *at;
+            const uint4 n = make_uint4(nan_codes(w.x), nan_codes(w.y), nan_codes(w.z), nan_codes(w.w));
+            if (!(n.x | n.y | n.z | n.w)) continue;
+            w = make_uint4(w.x & ~(n.x * 255u), w.y & ~(n.y * 255u), w.z & ~(n.z * 255u), w.w & ~(n.w * 255u));
+            some_nan = 1;
+          }
+          *at = w;
         }
         __syncwarp();
       }
@@ -588,6 +604,7 @@ q8_mma_kernel(const __grid_constant__ Q8Args a, const __grid_constant__ CUtensor
         }
       }
     __syncthreads();
+    const bool marked = some_nan != 0;
 #pragma unroll
     for (int gi = 0; gi < NG; ++gi)
 #pragma unroll
@@ -637,6 +654,24 @@ q8_mma_kernel(const __grid_constant__ Q8Args a, const __grid_constant__ CUtensor
             }
           }
       }
+      __syncthreads();
+    }
+    if (marked) {
+      // the segment's rows that only later tokens see, looked at once more: a NaN goes to the columns that see it
+#pragma unroll 1
+      for (int r = max(all_see, at.t * TR); r < min(at.len, tb * TR); ++r) {
+        const int pg = a.by_page.quotient(r), page = index_ok(pg, a.map.max_pages, a.status) ? a.map.table[(long long)at.slot * a.map.max_pages + pg] : -1;
+        if (page < 0 || page >= a.map.n_pages) continue;
+#pragma unroll 1
+        for (int x = tid; x < nh * d_v; x += S::NT) {
+          const int col = x / d_v, dim = x - col * d_v, column = hb * a.gb + col;
+          if (r >= all_see + a.token_of(column)) continue;
+          const int kvh = a.by_nhb.quotient(at.u) * a.heads + (a.heads > 1 ? a.by_gc.quotient(column) : 0);
+          const uint8_t code = a.vp[page * a.map.vp + kvh * a.map.vh + (r - pg * a.map.page) * a.map.vr + dim];
+          if ((code & 0x7f) == 0x7f) buf[col * LD + dim] = NAN;
+        }
+      }
+      if (tid == 0) some_nan = 0;
       __syncthreads();
     }
     write_segment<T, S::NT, S::NBUF>(a, buf, LD, NCOL * LD, jm, jl, at.e, at.u, nh, whole, 2 * blockIdx.x + (at.t == 0));

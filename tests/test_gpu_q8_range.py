@@ -223,3 +223,33 @@ def test_large_queries_meet_zero_keys_on_large_scales(size, scale, dtype):
     q = queries(1, 2, 4, 64, dtype) * size
     q[0, 0, 1] /= size                                      # (a column beside it whose logits are next to nothing)
     check_near(c, q, [0], run_decode(c, q, i32([0])), dtype)
+
+
+@pytest.mark.parametrize("layout", ["hnd", "nhd"])
+@pytest.mark.parametrize("dtype,hq,hkv,d,dv,page,block", [("bf16", 8, 2, 128, 128, 64, 16), ("f32", 4, 2, 64, 64, 16, 16), ("bf16", 2, 2, 80, 48, 5, 5),
+                                                        ("bf16", 2, 2, 256, 256, 16, 8), ("f32", 2, 1, 256, 80, 8, 8)])
+@pytest.mark.parametrize("length,q_len", [(100, 4), (64, 2), (65, 3), (130, 45), (3, 5), (7, 70)])
+def test_a_value_that_is_not_a_number_reaches_no_token_before_it(length, q_len, dtype, hq, hkv, d, dv, page, block, layout):
+    """NaN among the last rows, as a draft may leave it: tokens before that row are as with any other value there, those from it on have a NaN
+    in its columns alone, and a token that sees no row has zeros."""
+    cfg = config(hq, hkv, d, dv, dtype=dtype, max_seqs=2)
+    c = Pages8(cfg, page, block, [length, 40], seed=length, layout=layout)
+    q = queries(2, q_len, hq, d, dtype)
+    places = [(length - 1, 0, 3), (length - 1, hkv - 1, dv - 1), (max(length - q_len // 2, 0), 0, 3), (max(length - q_len + 1, 0), 0, 17)]
+    for r, h, x in places:
+        p, o = c.table[0, r // page].item(), r % page
+        c.v.view(torch.uint8)[p, h, o, x] = 0x31
+    clean = run_decode(c, q, i32([0, 1])).clone()
+    assert torch.isfinite(clean.float()).all()
+    for r, h, x in places:
+        p, o = c.table[0, r // page].item(), r % page
+        c.v.view(torch.uint8)[p, h, o, x] = 0xff if x == 17 else 0x7f
+    out = run_decode(c, q, i32([0, 1]))
+    nan = torch.zeros_like(out, dtype=torch.bool)
+    for r, h, x in places:
+        for u in range(q_len):
+            if r < length - q_len + 1 + u:
+                nan[0, u, h * (hq // hkv):(h + 1) * (hq // hkv), x] = True
+    assert torch.equal(torch.isnan(out.float()), nan)
+    assert torch.equal(out[~nan], clean[~nan])
+    assert (out[0, :max(q_len - length, 0)] == 0).all() and c.bits() == 0
