@@ -640,8 +640,8 @@ typedef struct snap_paged_q8 {
  * The scale of a block is 2^e, e the smallest integer from -126 to 120 with f * max |x| <= 448 * 2^e over the inputs x of the
  * rows written to it, f = max(1, sqrt(2) magnitude) for keys that are rotated and 1 otherwise (a pair grows by sqrt(2) magnitude
  * at most); of a block that holds rows of the sequence already, below first_rows, it is no less than before, and where it
- * grows those rows move to it.  A number is rotated in single precision, divided by the scale and rounded once, to
- * nearest even; beyond 448 (only past 2^120) it is 448.  NaN stays NaN and does not count for the scale; a block with an infinity has the scale 2^120.
+ * grows those rows move to it.  A number is rotated in single precision, divided by the scale (whatever
+ * positive number a block that holds rows has) and rounded once, to nearest even; beyond 448 (only past 2^120) it is 448.  NaN stays NaN and does not count for the scale; a block with an infinity has the scale 2^120.
  * Rows past the page table or on a page number out of range are skipped (SNAP_DEV_BAD_PAGE), their outputs too; so is an
  * entry with a negative first row, as a whole.  A page that is written may be listed once (not checked).  No workspace.
  */

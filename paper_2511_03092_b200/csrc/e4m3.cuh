@@ -24,6 +24,22 @@ __device__ __forceinline__ uint32_t codes_of_floats(float lo, float hi) {
   return r;
 }
 
+// A number that is to be rounded to a few bits, given as single precision holds it (to nearest) and the sign of what that leaves out: where it leaves
+// anything out, the one of the two neighbours whose last bit is set, which lies on no border between codes and on the side where the number is.
+__device__ __forceinline__ float to_odd(float x, float rest) {
+  const uint32_t b = __float_as_uint(x);
+  if (rest == 0.f || x == 0.f || (b & 1u)) return x;
+  return __uint_as_float((rest > 0.f) == (x > 0.f) ? b + 1u : b - 1u);
+}
+// x / scale for a code, |x| <= 448 scale (or not finite)
+__device__ __forceinline__ float quotient_to_odd(float x, float scale) {
+  if (scale < 0x1p-60f) { x *= 0x1p64f; scale *= 0x1p64f; }              // (the remainders below stay above the smallest number)
+  const float inv = 1.f / scale, q = x * inv;
+  if (!(fabsf(q) <= 1024.f)) return q;
+  const float p = fmaf(fmaf(-q, scale, x), inv, q);                      // nearest but for rounding's error of the correction
+  return to_odd(p, fmaf(-p, scale, x));
+}
+
 // The exponent of a block's scale: the smallest e from -126 to 120 with `largest` <= 448 * 2^e, 448 being 1.75 * 2^8.
 __device__ __forceinline__ int scale_exponent(float largest) {
   const uint32_t b = __float_as_uint(largest);                           // not negative

@@ -198,7 +198,9 @@ __global__ void __launch_bounds__(ANT, 4) q8_append_kernel(const __grid_constant
       }
       page_s[tid] = page; blk_s[tid] = off / B; begin_s[tid] = off;
     }
-    // The whole warp: the scales of head h's blocks, lane b knowing the largest of the new numbers of block b; 1 / scale for lane b.
+    // The whole warp: the scales of head h's blocks, lane b knowing the largest of the new numbers of block b; 1 / scale for lane b, or -scale of
+    // a block that keeps one which is no power of two: there 1 / scale is rounded, and numbers have to be divided.
+    bool uneven = false;
     const auto scale_of = [&](bool keys, int h, float largest) {
       const bool mine = lane < n_blocks && page_s[min(lane, SLAB - 1)] >= 0;
       const float need = exp2_of(scale_exponent(keys ? largest * a.growth : largest));
@@ -223,7 +225,9 @@ __global__ void __launch_bounds__(ANT, 4) q8_append_kernel(const __grid_constant
           }
       }
       if (mine) *place = scale;
-      return 1.f / scale;
+      if ((__float_as_uint(scale) & 0x7fffffu) == 0) return 1.f / scale;
+      uneven = true;
+      return -scale;
     };
     __syncthreads();
     // ---- scales, and the codes of values: pairs of neighbouring vectors ----
@@ -277,6 +281,12 @@ __global__ void __launch_bounds__(ANT, 4) q8_append_kernel(const __grid_constant
           const int z = row_of(k0 + u), b = block_of(z), page = page_s[b];
           if (page < 0) continue;
           const float f = (keys ? inv_k + hi * L.blocks : inv_s[w])[b];
+          uint8_t* c = codes + page * page_stride + (begin_s[b] + in_block + z - b * B) * row_stride + l.j * 2 * EV;
+          if (f < 0.f) {
+#pragma unroll 1
+            for (int e = 0; e < 2 * EV; ++e) c[e] = (uint8_t)codes_of_floats(quotient_to_odd(to_f32<T>(src[z * tok + e]), -f), 0.f);
+            continue;
+          }
           uint32_t o[EV / 2];
 #pragma unroll
           for (int e = 0; e < EV / 4; ++e) {
@@ -285,7 +295,6 @@ __global__ void __launch_bounds__(ANT, 4) q8_append_kernel(const __grid_constant
             o[EV / 4 + e] = codes_of_floats(to_f32<T>(vb[u].e[4 * e]) * f, to_f32<T>(vb[u].e[4 * e + 1]) * f) |
                             codes_of_floats(to_f32<T>(vb[u].e[4 * e + 2]) * f, to_f32<T>(vb[u].e[4 * e + 3]) * f) << 16;
           }
-          uint8_t* c = codes + page * page_stride + (begin_s[b] + in_block + z - b * B) * row_stride + l.j * 2 * EV;
           if constexpr (EV == 8) *reinterpret_cast<uint4*>(c) = make_uint4(o[0], o[1], o[EV / 2 - 2], o[EV / 2 - 1]);
           else *reinterpret_cast<uint2*>(c) = make_uint2(o[0], o[1]);
         }
@@ -295,7 +304,32 @@ __global__ void __launch_bounds__(ANT, 4) q8_append_kernel(const __grid_constant
     for (int s0 = 0; s0 < n && (half > 0 || a.q || a.k_out); s0 += SLAB) {
       const int rows = min(SLAB, n - s0);
       if (s0 > 0) angles(s0, rows);
-      __syncthreads();                                                   // (the keys' scales as well)
+      if (__syncthreads_or(uneven) && s0 == 0 && half > 0) {             // (the keys' scales are there as well)
+        // keys of the first block on a scale that is no power of two: nobody below writes their codes
+        const int d = r.d_qk, there = min(n, B - in_block);
+#pragma unroll 1
+        for (int hi = 0; hi < nk; ++hi) {
+          const float scale = -inv_k[hi * L.blocks];
+          if (scale <= 0.f) continue;
+          const int h = y + ny * hi;
+#pragma unroll 1
+          for (int x = tid; x < there * d; x += ANT) {
+            const int z = x / d, c = x - z * d, at = c - a.offset;
+            const T* k = static_cast<const T*>(a.k) + (long long)(t + z) * a.k_tok + h * a.k_head;
+            float v = to_f32<T>(k[c]);
+            if (at >= 0 && at < a.rot) {
+              const int j = INTER ? at / 2 : at % half;
+              const bool second = INTER ? at % 2 : at >= half;
+              const float other = to_f32<T>(k[second ? c - (INTER ? 1 : half) : c + (INTER ? 1 : half)]);
+              const float2 cs = cos_sin(a.positions ? a.positions[t + z] : (int)(row + z), a.freqs[j]);
+              const float co = cs.x * a.magnitude, si = cs.y * a.magnitude;
+              v = second ? fmaf(v, co, other * si) : fmaf(v, co, -(other * si));
+            }
+            r.k_pages[page_s[0] * pm.kp + h * pm.kh + (begin_s[0] + in_block + z) * pm.kr + c] = (uint8_t)codes_of_floats(quotient_to_odd(v, scale), 0.f);
+          }
+        }
+        __syncthreads();                                                 // (the rotated keys may be written over these)
+      }
       // threads as [rows][heads][items]: as many rows at once as there are, unless that leaves threads over
       int Z = 1;
       while (Z < rows && 2 * Z <= per) Z *= 2;
@@ -362,8 +396,10 @@ __global__ void __launch_bounds__(ANT, 4) q8_append_kernel(const __grid_constant
               if (!query && half > 0) {
                 const float f = inv_k[(h - nq) * L.blocks + b];
                 uint8_t* c = codes + head * pm.kh;
-                put_codes<V>(c + at_a, fa, f);
-                put_codes<V>(c + at_b, fb, f);
+                if (f > 0.f) {
+                  put_codes<V>(c + at_a, fa, f);
+                  put_codes<V>(c + at_b, fb, f);
+                }
               }
             }
           }

@@ -1,0 +1,58 @@
+"""Rows in and out of 8-bit pages whose scales are no powers of two, as another program's may be: each number is rounded once.  The expected
+codes and numbers are exact, so nothing is allowed for."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import q8_oracle as orc
+from paper_2511_03092_b200 import binding as B
+from tests.test_gpu_q8 import CODE, DT, Pages8, check_append, config, f64, i32
+
+pytestmark = pytest.mark.gpu
+
+SCALES = [0.7, 6.5, 3.0, 1 / 3, 1.0 + 2.0 ** -23, 2.0 - 2.0 ** -23, 1e-20, 0.9e20, 5e36, 2.0 ** 127 * 1.3]
+BORDERS = np.array([(a + b) / 2 for a, b in zip(orc.VALUES[:126], orc.VALUES[1:127])])     # between neighbouring codes: ties
+
+
+def half_way(values, dtype):
+    """The numbers of a type at, just below and just above the given ones."""
+    t = torch.from_numpy(values).to(DT[dtype])
+    bits = t.view(torch.int16 if dtype == "bf16" else torch.int32)
+    return torch.cat([(bits + x).view(DT[dtype]) for x in (-1, 0, 1)])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rotated", [False, True])
+@pytest.mark.parametrize("kept", [True, False])
+def test_appends_to_a_block_whose_scale_is_no_power_of_two(kept, dtype, rotated):
+    """Numbers at and around the borders between codes, divided by the scale that the block keeps, rounded once; or numbers for which some of
+    the blocks move to the next power of two."""
+    heads, d, n = len(SCALES), 128, 11
+    cfg = config(heads, heads, d, dtype=dtype)
+    c = Pages8(cfg, 16, 16, [5], seed=1, capacity=32)
+    scales = torch.tensor(SCALES, dtype=torch.float32)
+    for s in c.scales:
+        s[c.table[0, 0].item()] = scales.cuda()[:, None]
+    k = torch.zeros(n, heads, d, dtype=DT[dtype])
+    for h, s in enumerate(scales.double().numpy()):
+        x = half_way(np.minimum(BORDERS * s, 3e38 / 1.01), dtype)
+        x = torch.cat([x, -x])
+        x = x[x.double().abs() <= (448 * 2.0 ** np.floor(np.log2(s)) if kept else 440 * s)]     # (kept: what needs no larger power of two)
+        k[:, h] = x[torch.from_numpy(np.random.default_rng(h).integers(0, len(x), n * d))].view(n, d)
+        if rotated:                                         # (the scale has to stay what it is)
+            k[:, h] /= 2
+    k = k.cuda()
+    before = c.host()
+    rope, freqs = (B.make_rope(rot_dim=32, rot_offset=16), 1 / 10000.0 ** (np.arange(16) / 16)) if rotated else (None, None)
+    B.snap_paged_q8_append(cfg, c.paged, i32([0]), i32([0, n]), i32([5]), k, -k, *c.cache, c.seq_len, rope=rope,
+                           freqs=torch.from_numpy(freqs).cuda() if rotated else None, status=c.status)
+    if rotated and kept:                                    # what turns by its distance, the rest by its codes
+        p = c.table[0, 0].item()
+        got = c.k.view(torch.uint8)[p, :, 5:].cpu().numpy()
+        want = orc.encode(f64(k).transpose(1, 0, 2) / scales.double().numpy()[:, None, None])
+        np.testing.assert_array_equal(got[..., :16], want[..., :16])
+        np.testing.assert_array_equal(got[..., 48:], want[..., 48:])
+    check_append(c, before, [0], [5], [0, n], k, -k, rope, freqs, dtype=dtype)
+    for s in c.scales:
+        assert torch.equal(s[c.table[0, 0].item(), :, 0].cpu(), scales) == kept or (rotated and not kept)
+    assert c.bits() == 0
