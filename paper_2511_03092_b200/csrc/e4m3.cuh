@@ -31,6 +31,11 @@ __device__ __forceinline__ float to_odd(float x, float rest) {
   if (rest == 0.f || x == 0.f || (b & 1u)) return x;
   return __uint_as_float((rest > 0.f) == (x > 0.f) ? b + 1u : b - 1u);
 }
+// x * y of which few bits are kept, neither it nor its last bit too small for single precision
+__device__ __forceinline__ float product_to_odd(float x, float y) {
+  const float p = x * y;
+  return to_odd(p, fmaf(x, y, -p));
+}
 // x / scale for a code, |x| <= 448 scale (or not finite)
 __device__ __forceinline__ float quotient_to_odd(float x, float scale) {
   if (scale < 0x1p-60f) { x *= 0x1p64f; scale *= 0x1p64f; }              // (the remainders below stay above the smallest number)

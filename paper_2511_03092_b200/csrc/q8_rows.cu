@@ -221,7 +221,8 @@ __global__ void __launch_bounds__(ANT, 4) q8_append_kernel(const __grid_constant
           for (int c = lane; c < words; c += 32) {
             uint32_t* at = reinterpret_cast<uint32_t*>(codes + z * stride) + c;
             const float2 f0 = floats_of_codes(*at & 0xffffu), f1 = floats_of_codes(*at >> 16);
-            *at = codes_of_floats(f0.x * ratio, f0.y * ratio) | codes_of_floats(f1.x * ratio, f1.y * ratio) << 16;
+            *at = codes_of_floats(product_to_odd(f0.x, ratio), product_to_odd(f0.y, ratio)) |
+                  codes_of_floats(product_to_odd(f1.x, ratio), product_to_odd(f1.y, ratio)) << 16;   // (rounded once, whatever the old scale)
           }
       }
       if (mine) *place = scale;

@@ -56,3 +56,27 @@ def test_appends_to_a_block_whose_scale_is_no_power_of_two(kept, dtype, rotated)
     for s in c.scales:
         assert torch.equal(s[c.table[0, 0].item(), :, 0].cpu(), scales) == kept or (rotated and not kept)
     assert c.bits() == 0
+
+
+def test_rows_that_move_from_a_scale_that_is_no_power_of_two():
+    """Scales at and around those that bring a code to a border between codes of the larger scale."""
+    rng = np.random.default_rng(0)
+    heads, d = 300, 64
+    code = rng.integers(8, 120, heads)
+    ratio = rng.choice(BORDERS[:100], heads) / orc.VALUES[code]
+    ratio = ratio / 2.0 ** np.ceil(np.log2(ratio))          # (of old and new scale: less than 1)
+    old = torch.from_numpy(ratio.astype(np.float32))
+    old = (old.view(torch.int32) + torch.from_numpy(rng.integers(-1, 2, heads).astype(np.int32))).view(torch.float32)
+    cfg = config(heads, heads, d, dtype="f32")
+    c = Pages8(cfg, 16, 16, [9], seed=1, capacity=16)
+    p = c.table[0, 0].item()
+    held = rng.integers(0, 127, (heads, 9, d)).astype(np.uint8) | (rng.integers(0, 2, (heads, 9, d)) << 7).astype(np.uint8)
+    held[:, :, 0] = code[:, None]
+    for pool, scale in zip(c.pools, c.scales):
+        pool.view(torch.uint8)[p, :, :9] = torch.from_numpy(held).cuda()
+        scale[p, :, 0] = old.cuda()
+    x = torch.full((1, heads, d), 448.0, device="cuda")     # (new scale: 1)
+    before = c.host()
+    B.snap_paged_q8_append(cfg, c.paged, i32([0]), i32([0, 1]), i32([9]), x, x, *c.cache, c.seq_len, status=c.status)
+    check_append(c, before, [0], [9], [0, 1], x, x)
+    assert torch.equal(c.scales[0][p, :, 0], old.clamp(min=1).cuda()) and c.bits() == 0
