@@ -682,7 +682,7 @@ int snap_paged_q8_decode_attn(const snap_config_t* cfg, const snap_paged_q8_t* p
 
 /*
  * The reverse of the append: token cu_tokens[i] + j of k_dev and v_dev receives row first_rows[i] + j of sequence slot_ids[i],
- * rounded once (bf16: exact, unless the scale leaves its range).  Entries, tokens and padding as in snap_paged_q8_append, but a
+ * rounded once (bf16: exact on scales that are powers of two, unless they leave its range).  Entries, tokens and padding as in snap_paged_q8_append, but a
  * slot may be listed any number of times and no length is looked at.
  *   k_dev, v_dev  (t, h, c) at [t * token_stride + h * head_stride + c], strides multiples of 16 bytes, no head of an
  *             output may overlap another

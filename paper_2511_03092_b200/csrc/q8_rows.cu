@@ -492,6 +492,12 @@ __global__ void __launch_bounds__(NT, 6) q8_gather_kernel(const __grid_constant_
         if (!there[u]) continue;
         const uint32_t words[4] = {in[u].x, in[u].y, in[u].z, in[u].w};
         T* to = out + (z + u * step) * tok;
+        if (sizeof(T) == 2 && (__float_as_uint(f[u]) & 0x7fffffu)) {     // a product of more bits than single precision has
+          const uint8_t* again = codes + offset[z + u * step];
+#pragma unroll 1
+          for (int e = 0; e < 16; ++e) to[e] = from_f32<T>(product_to_odd(floats_of_codes(again[e]).x, f[u]));
+          continue;
+        }
 #pragma unroll
         for (int v = 0; v < 16 / EV; ++v) {
           Vec<T, EV> o;

@@ -80,3 +80,33 @@ def test_rows_that_move_from_a_scale_that_is_no_power_of_two():
     B.snap_paged_q8_append(cfg, c.paged, i32([0]), i32([0, 1]), i32([9]), x, x, *c.cache, c.seq_len, status=c.status)
     check_append(c, before, [0], [9], [0, 1], x, x)
     assert torch.equal(c.scales[0][p, :, 0], old.clamp(min=1).cuda()) and c.bits() == 0
+
+
+def bf16_of(x):
+    """Numbers in double precision as the nearest bf16 ones, ties to even, in one rounding (normal numbers)."""
+    m, e = np.frexp(x)
+    return np.ldexp(np.rint(m * 256), e - 8)
+
+
+def test_gather_rounds_once():
+    """Scales that bring a code next to the border between two bf16 numbers: product and border agree in 24 bits, not in all."""
+    rng = np.random.default_rng(0)
+    heads, d = 512, 16
+    code = rng.choice([x for x in range(8, 127) if x % 8 not in (0, 4)], heads)      # (an odd factor besides powers of two)
+    border = (2 * rng.integers(128, 256, heads) + 1) / 512.0
+    scale = (border / orc.VALUES[code]).astype(np.float32)
+    cfg = config(heads, heads, d)
+    c = Pages8(cfg, 16, 16, [3], seed=1)
+    p = c.table[0, 0].item()
+    c.k.view(torch.uint8)[p, :, :3] = torch.from_numpy(code.astype(np.uint8)).cuda()[:, None, None]
+    c.v.view(torch.uint8)[p, :, :3] = torch.from_numpy(code.astype(np.uint8) | 0x80).cuda()[:, None, None]
+    for s in c.scales:
+        s[p, :, 0] = torch.from_numpy(scale).cuda()
+    k, v = (torch.zeros(3, heads, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    B.snap_paged_q8_gather(cfg, c.paged, i32([0]), i32([0, 3]), i32([0]), *c.cache, k, v, status=c.status)
+    want = bf16_of(orc.VALUES[code] * scale.astype(np.float64))[None, :, None]
+    twice = f64(torch.from_numpy((orc.VALUES[code] * scale.astype(np.float64)).astype(np.float32)).to(torch.bfloat16))[None, :, None]
+    assert (want != twice).any()                            # (rounding to 24 bits first is not the same)
+    np.testing.assert_array_equal(f64(k), np.broadcast_to(want, k.shape))
+    np.testing.assert_array_equal(f64(v), np.broadcast_to(-want, k.shape))
+    assert c.bits() == 0
