@@ -52,17 +52,17 @@ constexpr float NOTHING = -3.402823466e38f;     // the reference of a column tha
 constexpr int SHARE = 4, WHOLE = 12;
 constexpr int LOOK = 2;                         // tiles whose pages are looked up ahead of their copies
 
-// n / d for 0 <= n < 2^31 by a multiplication
+// n / d for 0 <= n < 2^31 by a multiplication: division by invariant integers (Granlund and Montgomery, 1994), with a reciprocal rounded up.
+// With L = ceil(log2 d) and m = floor(2^(31 + L) / d) + 1 (below 2^32, as d > 2^(L - 1)), d m = 2^(31 + L) + e with 0 < e <= d <= 2^L, so
+// n m / 2^(31 + L) = n / d + n e / (d 2^(31 + L)) lies less than 1 / d above n / d and has the same whole part.
 struct Divisor {
-  uint32_t d, m; int s;
-  __device__ __forceinline__ int quotient(int n) const { return (int)((__umulhi(m, (uint32_t)n) + (uint32_t)n) >> s); }
+  uint32_t m; int L;
+  __device__ __forceinline__ int quotient(int n) const { return (int)(__umulhi(2u * (uint32_t)n, m) >> L); }
 };
 Divisor divisor(uint32_t d) {
-  Divisor r;
-  r.d = d;
-  for (r.s = 0; (1ull << r.s) < d; ++r.s) {}
-  r.m = (uint32_t)(((1ull << 32) * ((1ull << r.s) - d)) / d + 1);
-  return r;
+  int L = 0;
+  while (L < 31 && (1u << L) < d) ++L;
+  return {(uint32_t)((1ull << (31 + L)) / d + 1), L};
 }
 
 struct Q8Args : LineArgs {
