@@ -591,14 +591,16 @@ int snap_paged_evict(const snap_config_t* cfg, const snap_paged_t* paged, const 
  *           free (SNAP_DEV_NO_ROOM).
  *   A slot of -1 is padding; a slot out of range or listed before is skipped (SNAP_DEV_BAD_SLOT).
  *   page_table_in_dev, page_table_out_dev  [max_seqs][max_pages], the same array or two that do not overlap (checked): with two, the rows of the
- *             slots listed are written whole and the table that a running step reads stays as it is
+ *             slots listed are written whole and the table that a running step reads stays as it is; rows of other slots are neither read
+ *             nor written, so a program that uses two tables in turn lists every slot that lives, those that do not grow with 0
  *   seq_len_dev [max_seqs]: read; 0 where the sequence has ended (appending counts the new rows, not this call)
  *   free_pages_dev [n_pages]: the stack of free pages, its top last; n_free_in_dev, n_free_out_dev [1]: how many it holds before and
  *             after (the same or two).  Entries are written only from n_free_in on.  More than n_pages: SNAP_DEV_BAD_PAGE, the rest is dropped.
  *   granted_dev NULL, or [n_seqs]: n of the requests served, 0 of the others
  *   first_rows_dev [n_seqs]: the row of each request's first new token, seq_len[slot] (0: ended, skipped)
  *   cu_tokens_dev [n_seqs + 1]: sums of the granted tokens before each request, and of all
- *   token_slots_dev, token_rows_dev [n_tokens_max]: slot and row of every token granted, request by request; -1 and 0 behind the last
+ *   token_slots_dev, token_rows_dev [n_tokens_max]: slot and row of every token granted, request by request; -1 and 0 behind the last (as
+ *             snap_paged_append takes them for slot_ids and rows, with n_tokens_max tokens, and snap_rope the rows for positions)
  * Of paged, only page_tokens, n_pages and max_pages are used; of cfg, max_seqs.  At most 65536 requests.  Sequences that share
  * pages must not end through this call (a page would go onto the stack twice).
  * Scratch: snap_paged_plan_workspace_bytes(cfg, paged, n_seqs).
