@@ -19,8 +19,10 @@
 // taken off again when a tile's outputs are added to the sums: these are of single precision, in the numbers' own size, so that no tile
 // depends on what another one held.  The power and the reference of the exponentials move when a tile's largest product leaves [1, 2^15].  A tile
 // whose value scales lie more than 2^6 apart (a block keeps the scale of a row that was given up) goes through several times, the rows of
-// the largest scales first.  Products round to 11 bits (bf16: an eighth of the output's own rounding) or are two numbers, the second in units of
-// 2^-11 and summed apart (single precision: 22 bits); below 2^-14 of the largest one they round to multiples of 2^-25 of it (2^-36).  (Sums that are held on the columns' powers instead, and lose the rows of smaller scales:
+// the largest scales first.  Products are two half-precision numbers, 21 bits; what lies far below the largest one rounds to multiples of 2^-24 of
+// it (of 2^-36 where the second numbers are summed apart, times 2^11: single precision, and two heads side by side).  One number of 11 bits, an eighth
+// of a bf16 output's own rounding, puts one output in 30 on the other side of a border between two bf16 numbers; two cost up to 4 columns
+// nothing where spare columns take the second, else 3 to 9 %, 14 % with sixteen columns (four tokens a step 63 -> 72 us).  (Sums that are held on the columns' powers instead, and lose the rows of smaller scales:
 // 16 long sequences 181 us instead of 188, four tokens a step 58.6 instead of 61.4, calls of all kinds 0.8 % less.  A loop around a tile's
 // rounds instead of a second way through the loop over tiles: 4 to 5 % more, 72 us for the four tokens.)
 //
@@ -147,7 +149,11 @@ q8_mma_kernel(const __grid_constant__ Q8Args a, const __grid_constant__ CUtensor
   // scales that lie further than 2^NEAR apart do not meet.
   constexpr float LEAST = 1.f, LIMIT = 32768.f;
   constexpr int TARGET = 9, NEAR = 6;
-  constexpr float REST = 2048.f;                                         // a second number's unit: it is half a last bit of the first, at most as large again
+  // A weight is two half-precision numbers.  Where a side has four columns at most, its other four are the same ones over again, and take the second
+  // numbers; else the values are multiplied twice.
+  constexpr bool PAIR = SIDES == 2;
+  constexpr int NUM = PAIR ? 1 : 2;                                      // products of a tile's values
+  constexpr float REST = 2048.f;                                         // where a second number is summed apart: times this, it has the first one's range
   constexpr unsigned ALL = NG == 1 ? 0xffu : 0xffffu;                    // a bit for each of the warp's columns
   extern __shared__ unsigned char smem_dyn[];
   unsigned char* stages = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~uintptr_t(1023));
@@ -227,7 +233,7 @@ q8_mma_kernel(const __grid_constant__ Q8Args a, const __grid_constant__ CUtensor
     const int k = a.by_nhb.quotient(at.u), hb = at.u - k * a.nhb, x0 = hb * a.gb + side * a.sc, nh = min(a.sc, a.g - x0);
 #pragma unroll
     for (int gi = 0; gi < NG; ++gi) {
-      const int col = 8 * gi + gq;
+      const int col = PAIR ? gq & 3 : 8 * gi + gq;
       const T* qp = q_all + a.out_row(at.e, k, col < nh ? x0 + col : 0) * d_qk + 4 * tq;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
@@ -453,7 +459,7 @@ q8_mma_kernel(const __grid_constant__ Q8Args a, const __grid_constant__ CUtensor
         for (int gi = 0; gi < NG; ++gi)
 #pragma unroll
           for (int c = 0; c < 2; ++c) {                                  // (a column that is not there may see anything)
-            const int sees = all_see + (a.q_len > 1 ? a.token_of(hb * a.gb + side * a.sc + 8 * gi + 2 * tq + c) : 0) - row0;
+            const int sees = all_see + (a.q_len > 1 ? a.token_of(hb * a.gb + side * a.sc + (PAIR ? 2 * (tq & 1) : 8 * gi + 2 * tq) + c) : 0) - row0;
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -548,7 +554,7 @@ q8_mma_kernel(const __grid_constant__ Q8Args a, const __grid_constant__ CUtensor
 #pragma unroll
       for (int gi = 0; gi < NG; ++gi) { l_part[gi][0] += add[gi][0]; l_part[gi][1] += add[gi][1]; }
       // ---- O^T += V tile^T . P^T, the power of two taken off again ----
-      uint32_t pb[MT][NG][PARTS][2];                                     // P^T as B operands: rows 16 mt + 2 tq, + 1, then + 8, + 9, of column 8 gi + gq
+      uint32_t pb[MT][NG][NUM][2];                                       // P^T as B operands: rows 16 mt + 2 tq, + 1, then + 8, + 9, of column 8 gi + gq
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -556,16 +562,23 @@ q8_mma_kernel(const __grid_constant__ Q8Args a, const __grid_constant__ CUtensor
 #pragma unroll
           for (int r8 = 0; r8 < 2; ++r8) {
             const float p0 = p[mt][gi][2 * r8], p1 = p[mt][gi][2 * r8 + 1];
-            const uint32_t hi = pack_f16(p0, p1);
-            pb[mt][gi][0][r8] = movmatrix_t(hi);
-            if constexpr (F32) pb[mt][gi][PARTS - 1][r8] = movmatrix_t(rest_f16(p0, p1, hi, REST));
+            if constexpr (PAIR || F32) {
+              const uint32_t hi = pack_f16(p0, p1), lo = rest_f16(p0, p1, hi, REST);
+              pb[mt][gi][0][r8] = movmatrix_t(PAIR && tq >= 2 ? lo : hi);
+              if constexpr (!PAIR) pb[mt][gi][NUM - 1][r8] = movmatrix_t(lo);
+            } else {                                                     // cut, not rounded: what is cut off needs no conversion back
+              const float h0 = __uint_as_float(__float_as_uint(p0) & 0xffffe000u), h1 = __uint_as_float(__float_as_uint(p1) & 0xffffe000u);
+              pb[mt][gi][0][r8] = movmatrix_t(pack_f16(h0, h1));
+              pb[mt][gi][NUM - 1][r8] = movmatrix_t(pack_f16(p0 - h0, p1 - h1));
+            }
           }
 #pragma unroll
       for (int db = 0; db < KS; ++db) {
         if (!EXACT && 16 * db >= d_v) break;
         uint32_t c[4];                                                   // dims gq and + 8, of the tile's first 16 rows, then of the others
         ldsm_bytes_t((b_V ^ (db % (SW / 16) << 4)) + db * 16 / SW * S::SLAB_B, c);
-        float o[NG][PARTS][4];
+        constexpr int SUMS = NUM == 2 && F32 ? 2 : 1;
+        float o[NG][SUMS][4];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
           const uint32_t a0 = halves_of_codes(c[2 * mt] & 0xffffu), a2 = halves_of_codes(c[2 * mt] >> 16);
@@ -573,16 +586,16 @@ q8_mma_kernel(const __grid_constant__ Q8Args a, const __grid_constant__ CUtensor
 #pragma unroll
           for (int gi = 0; gi < NG; ++gi)
 #pragma unroll
-            for (int y = PARTS - 1; y >= 0; --y) {
-              if (mt == 0) mma_f16_first(o[gi][y], a0, a1, a2, a3, pb[mt][gi][y][0], pb[mt][gi][y][1]);
-              else mma_f16(o[gi][y], a0, a1, a2, a3, pb[mt][gi][y][0], pb[mt][gi][y][1]);
+            for (int y = NUM - 1; y >= 0; --y) {
+              if (mt == 0 && (SUMS == 2 || y == NUM - 1)) mma_f16_first(o[gi][SUMS == 2 ? y : 0], a0, a1, a2, a3, pb[mt][gi][y][0], pb[mt][gi][y][1]);
+              else mma_f16(o[gi][SUMS == 2 ? y : 0], a0, a1, a2, a3, pb[mt][gi][y][0], pb[mt][gi][y][1]);
             }
         }
 #pragma unroll
         for (int gi = 0; gi < NG; ++gi)
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
-            const float sum = F32 ? fmaf(o[gi][PARTS - 1][x], 1.f / REST, o[gi][0][x]) : o[gi][0][x];
+            const float sum = SUMS == 2 ? fmaf(o[gi][SUMS - 1][x], 1.f / REST, o[gi][0][x]) : o[gi][0][x];
             oacc[gi][db][x] = fmaf(sum, one_over(f[gi][x & 1]), oacc[gi][db][x]);
           }
       }
@@ -614,7 +627,13 @@ q8_mma_kernel(const __grid_constant__ Q8Args a, const __grid_constant__ CUtensor
         for (int ww = side; ww < NWARP; ww += SIDES) M = fmaxf(M, wm[ww * NCOL + 8 * gi + 2 * tq + c]);
         const float y = exp2f(ref[gi][c] - M);
 #pragma unroll
-        for (int db = 0; db < KS; ++db) { oacc[gi][db][c] *= y; oacc[gi][db][2 + c] *= y; }
+        for (int db = 0; db < KS; ++db)
+#pragma unroll
+          for (int up = 0; up < 4; up += 2) {
+            float& o = oacc[gi][db][up + c];
+            if (PAIR) o = fmaf(__shfl_xor_sync(0xffffffffu, o, 2), 1.f / REST, o);
+            o *= y;
+          }
       }
     if (tid < NCOL) {
       const int of = SIDES > 1 && tid >= a.sc, col = tid - of * a.sc;    // its side, and the column there

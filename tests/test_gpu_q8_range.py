@@ -253,3 +253,31 @@ def test_a_value_that_is_not_a_number_reaches_no_token_before_it(length, q_len, 
     assert torch.equal(torch.isnan(out.float()), nan)
     assert torch.equal(out[~nan], clean[~nan])
     assert (out[0, :max(q_len - length, 0)] == 0).all() and c.bits() == 0
+
+
+@pytest.mark.parametrize("layout,hq,hkv", [("hnd", 8, 2), ("nhd", 8, 2), ("hnd", 8, 1), ("hnd", 16, 1)])
+def test_bf16_outputs_are_rounded_once(layout, hq, hkv):
+    """Few rows of positive values and exact logits: an output is the exact one's bf16 neighbour, but where that lies next to a border.  What comes
+    before the rounding is off by (2 L + 2^-20 + 2^-21 + 4 (n / 16 + 8) e) of it and 2^-24 of the largest product, by the terms of the tolerance above;
+    a weight of 11 bits alone is off by 2^-12, eight times that."""
+    n, d, g = [2, 3, 5, 8, 9, 31, 33, 40] * 8, 128, hq // hkv
+    cfg = config(hq, hkv, d, max_seqs=len(n), scale=1.0)
+    c = Pages8(cfg, 64, 64, n, seed=3, spread=0, layout=layout)
+    c.v.view(torch.uint8).copy_(c.v.view(torch.uint8) & 0x7f)
+    keys = c.k.view(torch.uint8)
+    keys[..., 1:] = 0                                       # (one product to a logit, of size 3 at most)
+    c.ks.fill_(2.0 ** -7)
+    q = torch.zeros(len(n), 1, hq, d, dtype=torch.bfloat16, device="cuda")
+    q[..., 0] = 1.0 + torch.arange(hq, device="cuda") / 16
+    got, (hk, hv) = f64(run_decode(c, q, i32(list(range(len(n)))))), c.host()
+    for i in range(len(n)):
+        k, _ = hk.rows(c.table[i].tolist(), n[i])
+        v, _ = hv.rows(c.table[i].tolist(), n[i])
+        for h in range(hq):
+            z = k[:, h // g, 0] * f64(q[i, 0, h, 0])
+            p = np.exp(z - z.max())
+            want = p @ v[:, h // g] / p.sum()
+            off = (2 * 9 * E * np.abs(z).max() + 2.0 ** -20 + 2.0 ** -21 + 4 * (n[i] / 16 + 8) * E) * want + 2.0 ** -24 * (p / p.sum()).max() * v[:, h // g].sum(axis=0)
+            half = 2.0 ** (np.floor(np.log2(want)) - 8)
+            err = np.abs(got[i, 0, h] - want)
+            assert (err <= half + off).all(), f"sequence {i}, head {h}: {((err - half) / off).max():.1f} times what may be left out"
