@@ -65,7 +65,7 @@ int snap_paged_plan(const snap_config_t* cfg, const snap_paged_t* paged, const i
                   size = sizeof(int32_t) * (uintptr_t)cfg->max_seqs * (uintptr_t)paged->max_pages;
   if (n_seqs > 0 && in != out && (in < out ? out - in : in - out) < size) return SNAP_ERR_INVALID_ARG;   // a row would be read after it was written
   if (workspace_bytes < paged_plan_scratch_bytes(cfg->max_seqs, n_seqs)) return SNAP_ERR_WORKSPACE_TOO_SMALL;
-  PlanArgs a;
+  PlanArgs a = {};
   a.slots = slot_ids_dev; a.new_tokens = new_tokens_dev; a.table_in = page_table_in_dev; a.table_out = page_table_out_dev;
   a.seq_len = seq_len_dev; a.stack = free_pages_dev; a.n_free_in = n_free_in_dev; a.n_free_out = n_free_out_dev;
   a.granted = granted_dev; a.first_rows = first_rows_dev; a.cu = cu_tokens_dev; a.token_slots = token_slots_dev; a.token_rows = token_rows_dev;

@@ -9,6 +9,7 @@
 // What bounds it: the way of a few numbers through memory, phase after phase, and the launches.  32 requests of a token each take 9.4 us, 6.8 of
 // them without lists, rows and pages; 75 requests of up to 60000 rows and 614405 tokens 22.2 (33.7 in one launch of 16 CTAs), for 10 MB, which
 // HBM brings in 1.5.
+#include <algorithm>
 #include <climits>
 
 #include "snap_internal.cuh"
@@ -385,7 +386,7 @@ __global__ void __launch_bounds__(RNT) paged_plan_rows_kernel(const __grid_const
   lists.take(RNT);
   __syncthreads();
   const bool apart = a.table_in != a.table_out;
-  const int pieces = (a.max_pages + PIECE - 1) / PIECE;
+  const int pieces = a.pieces;                                           // of a request's row, or, in place, of the entries it is granted
   const long long of_lists = ((long long)a.n_tokens_max + PIECE - 1) / PIECE, items = of_lists + (long long)a.n * pieces;
   for (long long x = blockIdx.x; x < items; x += gridDim.x) {
     if (x < of_lists) {
@@ -393,13 +394,14 @@ __global__ void __launch_bounds__(RNT) paged_plan_rows_kernel(const __grid_const
       if (t0 < a.n_tokens_max) lists.write(a, t0);
       continue;
     }
-    const int i = (int)((x - of_lists) / pieces), b0 = (int)((x - of_lists) - (long long)i * pieces) * PIECE, b1 = min(b0 + PIECE, a.max_pages);
+    const int i = (int)((x - of_lists) / pieces), piece = (int)((x - of_lists) - (long long)i * pieces);
     const int4 r = left(&s.rec[i]), res = left(&s.res[i]);
     if (r.x < 0 || r.y < 0) continue;
     const int* row = a.table_in + (long long)r.x * a.max_pages;
     int* out = a.table_out + (long long)r.x * a.max_pages;
     const bool granted = res.z >= 0 && r.w > 0;
     const int j0 = granted ? pages_of(a, r.z) : 0, j1 = granted ? pages_of(a, (long long)r.z + r.y) : 0, top = head.there - 1 - res.y;
+    const int b0 = (apart ? 0 : j0) + piece * PIECE, b1 = min(b0 + PIECE, apart ? a.max_pages : j1);
     const bool gaps = granted && r.w != j1 - j0;                         // some of them hold a page: one warp, after the copy
     if (apart && fours(a, row, out)) {
       const int j = b0 + 4 * tid;
@@ -427,7 +429,7 @@ __global__ void __launch_bounds__(RNT) paged_plan_rows_kernel(const __grid_const
         else if (!here && apart) out[j] = row[j];
       }
     }
-    if (gaps && b0 == 0 && tid < 32) fill_gaps(a, row, out, j0, j1, top);
+    if (gaps && piece == 0 && tid < 32) fill_gaps(a, row, out, j0, j1, top);
   }
 }
 
@@ -439,8 +441,12 @@ size_t paged_plan_scratch_bytes(int max_seqs, int n_seqs) { return carve(nullptr
 // two launches: 32 requests, rows of 512 entries 9.3 / 12.8 us; 64 13.1 / 13.9; 128 19.3 / 14.0; 32 of 1024 tokens each 15.9 / 13.3; 8 of
 // 4096 13.9 / 13.1.  Clusters of 16 / 8 / 4: 75 requests of 614405 tokens, rows of 8192 entries 22.3 / 25.9 / 31.9; 2000 requests 34.9 / 43.3
 // / 59.1; no call was shorter with fewer.)
+// In place a request reads few entries unless it ends, and then the whole row, 5.8 us of one CTA for 8192 entries; the rule takes one in a hundred to
+// end.  (One CTA / two launches, in place: nobody ends, 16 requests 7.4 / 12.3, 32 with rows of 8192 entries 7.0 / 13.9, 128 of 512 12.3 / 14.8, 250
+// of 512 21.4 / 17.2, 250 of 8192 21.3 / 17.6; one in fifty ends, 250 of 8192 51 / 21; one in ten, 64 of 8192 26 / 15.5, 128 of 4096 37 / 17.8, 128
+// of 512 15.2 / 15.6; three in ten, 32 of 8192 27 / 17.6, 250 of 512 27.5 / 20.9, 250 of 8192 182 / 28; all, 200 of 15000 501 / 54, one of 15000 9.8 / 14.7.)
 cudaError_t launch_paged_plan(const PlanArgs& a, cudaStream_t st) {
-  const long long entries = (long long)a.n * (a.table_in != a.table_out ? a.max_pages : 64) + a.n_tokens_max;
+  const long long entries = (long long)a.n * (a.table_in != a.table_out ? a.max_pages : 160 + a.max_pages / 48) + a.n_tokens_max;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -476,8 +482,12 @@ cudaError_t launch_paged_plan(const PlanArgs& a, cudaStream_t st) {
     lc.gridDim = dim3(cluster);
     if ((e = cudaLaunchKernelEx(&lc, kernel, a)) != cudaSuccess) return e;
     count_launch();
-    const long long items = ((long long)a.n_tokens_max + PIECE - 1) / PIECE + (long long)a.n * ((a.max_pages + PIECE - 1) / PIECE), most = 4LL * sm_count();
-    e = launch_pdl(paged_plan_rows_kernel, dim3((unsigned)(items < most ? items : most)), dim3(RNT), 0, st, a);
+    // (in place no row is granted more entries than the list's tokens begin, and one that the first ends in)
+    PlanArgs rows = a;
+    const long long wide = a.table_in != a.table_out ? a.max_pages : std::min<long long>(a.max_pages, a.n_tokens_max / a.page + 2);
+    rows.pieces = (int)((wide + PIECE - 1) / PIECE);
+    const long long items = ((long long)a.n_tokens_max + PIECE - 1) / PIECE + (long long)a.n * rows.pieces, most = 4LL * sm_count();
+    e = launch_pdl(paged_plan_rows_kernel, dim3((unsigned)(items < most ? items : most)), dim3(RNT), 0, st, rows);
   }
   count_launch();
   return e != cudaSuccess ? e : cudaGetLastError();

@@ -296,6 +296,7 @@ struct PlanArgs {
   int* seq_len; int* stack; const int* n_free_in; int* n_free_out;
   int* granted; int* first_rows; int* cu; int* token_slots; int* token_rows;
   int n, n_tokens_max, max_seqs, page, n_pages, max_pages;
+  int pieces;                       // (of the second launch, set by launch_paged_plan)
   char* scratch;
   uint32_t* status;
 };

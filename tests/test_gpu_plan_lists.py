@@ -1,10 +1,12 @@
-"""What the page plan writes, as its readers take it: lists of tokens and rows for the full-precision append, two tables used in turn."""
+"""What the page plan writes, as its readers take it: lists of tokens and rows for the full-precision append, two tables used in turn; and
+plans in place of all sizes."""
 import numpy as np
 import pytest
 import torch
 
 from oracle import paged_oracle as porc
 from paper_2511_03092_b200 import binding as B
+from tests.test_gpu_plan import Step, a_server
 
 pytestmark = pytest.mark.gpu
 
@@ -72,3 +74,14 @@ def test_full_precision_pages_by_the_plans_lists(most, in_turn):
     assert int(status.item()) == 0
     held = tables[at][tables[at] >= 0].tolist()
     assert len(set(held)) == len(held) and len(held) + int(n_free.item()) == pool
+
+
+@pytest.mark.parametrize("n,width,page", [(16, 512, 4), (64, 2048, 4), (128, 512, 4), (128, 8192, 1), (200, 160, 4), (250, 512, 4), (250, 8192, 1), (256, 40, 4), (257, 40, 4)])
+@pytest.mark.parametrize("ended", [0.0, 0.3, 1.0])
+def test_plans_in_place_of_all_sizes(n, width, page, ended):
+    """Steps of a token each in place, in one launch and in two by how many requests there are and how wide their rows."""
+    rng = np.random.default_rng(n + width)
+    slots, grow, table, length, stack, free = a_server(rng, n, width, page, n, width * page // 2, 1, ended=ended, spare=0.8)
+    s = Step(slots, grow, table, length, stack, free, page, n, False)
+    s.call()
+    s.check()
