@@ -495,14 +495,34 @@ q8_mma_kernel(const __grid_constant__ Q8Args a, const __grid_constant__ CUtensor
             }
         }
         if (pass > 0) break;
-        // (weights of 2^10 above the reference are a reason as well, however small the scales they meet)
+        // (weights of 2^6 above the reference are a reason as well, however small the scales they meet: sums have to stay within single precision)
 #pragma unroll
-        for (int gi = 0; gi < NG; ++gi) largest = fmaxf(largest, (add[gi][0] + add[gi][1]) * 32.f);
+        for (int gi = 0; gi < NG; ++gi) largest = fmaxf(largest, (add[gi][0] + add[gi][1]) * 512.f);
         const float least = fminf(fminf(v_scale[0][0], v_scale[0][1]), fminf(v_scale[1][0], v_scale[1][1]));
         const float greatest = fmaxf(fmaxf(v_scale[0][0], v_scale[0][1]), fmaxf(v_scale[1][0], v_scale[1][1]));
         const bool near = least >= lowest && greatest <= highest;
         const unsigned said = __reduce_or_sync(0xffffffffu, good << (2 * NG * tq) | (unsigned)(largest > LIMIT) << 31 | (unsigned)!near << 30);
         if (said == ALL) break;
+        if (!(said >> 30)) {
+          // some columns lie below the range: their power moves, and nothing else
+#pragma unroll
+          for (int gi = 0; gi < NG; ++gi)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              float big = 0.f;
+#pragma unroll
+              for (int mt = 0; mt < MT; ++mt) big = fmaxf(big, fmaxf(p[mt][gi][c], p[mt][gi][2 + c]));
+#pragma unroll
+              for (int o = 4; o <= 16; o <<= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
+              if (((said >> (2 * NG * tq + 2 * gi + c)) & 1u) || big == 0.f) continue;
+              const int was = exponent_of(f[gi][c]), now = min(min(was + TARGET - exponent_of(big), was + 127), exponent_of(most));
+              const float by = exp2_of(now - was);
+              f[gi][c] = exp2_of(now);
+#pragma unroll
+              for (int mt = 0; mt < MT; ++mt) { p[mt][gi][c] *= by; p[mt][gi][2 + c] *= by; }
+            }
+          break;
+        }
         fresh = false;
         if ((said >> 30) & 1u) {
           // lane r has row r: those whose scale lies within 2^NEAR below the largest are taken in now, the others in another round
@@ -540,8 +560,6 @@ q8_mma_kernel(const __grid_constant__ Q8Args a, const __grid_constant__ CUtensor
               mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
               big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
             }
-            // (a column that is in range stays as it is, whatever is beside it; one of NaN may do as it likes)
-            if (!(said >> 30) && ((said >> (2 * NG * tq + 2 * gi + c)) & 1u)) continue;
             const float to = fmaxf(ref[gi][c], mx), al = exp2f(ref[gi][c] - to);
             const int k = (int)fminf(fmaxf(TARGET - floorf(big - to), -126.f), 126.f);
             l_part[gi][c] *= al;

@@ -281,3 +281,32 @@ def test_bf16_outputs_are_rounded_once(layout, hq, hkv):
             half = 2.0 ** (np.floor(np.log2(want)) - 8)
             err = np.abs(got[i, 0, h] - want)
             assert (err <= half + off).all(), f"sequence {i}, head {h}: {((err - half) / off).max():.1f} times what may be left out"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nats", [3.0, 5.0, 40.0])
+def test_large_values_over_many_rows(nats, dtype):
+    """Values of 2^108 in 3000 rows whose weights grow after the first tile: their sum is of a size of 2^120, and nothing on the way passes 2^128."""
+    cfg = config(2, 1, 64, dtype=dtype, scale=1.0)
+    c = Pages8(cfg, 64, 64, [3000], seed=6, spread=0)
+    c.vs.fill_(2.0 ** 102)
+    c.k.view(torch.uint8).zero_()
+    c.ks.fill_(1.0)
+    row = torch.zeros(64, dtype=torch.uint8, device="cuda")
+    row[0] = int(orc.encode(nats))
+    for r in range(64, 3000, 5):
+        fill(c, range(r, min(r + 4, 3000)), codes=row, which=0)
+    q = torch.zeros(1, 1, 2, 64, dtype=DT[dtype], device="cuda")
+    q[..., 0] = 1.0
+    check_near(c, q, [0], run_decode(c, q, i32([0])), dtype, reach_terms=1)
+
+
+@pytest.mark.parametrize("layout,hq,hkv,d,q_len", [("hnd", 8, 2, 128, 1), ("nhd", 2, 2, 64, 3), ("hnd", 16, 1, 128, 1), ("nhd", 2, 2, 256, 1)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("by", [4.0, 16.0, 64.0])
+def test_weights_that_differ_from_tile_to_tile(by, dtype, layout, hq, hkv, d, q_len):
+    """Logits so far apart that most tiles hold next to nothing of a column, each of another one."""
+    cfg = config(hq, hkv, d, dtype=dtype, max_seqs=2)
+    c = Pages8(cfg, 32, 16, [900, 61], seed=3, layout=layout)
+    q = queries(2, q_len, hq, d, dtype, seed=1) * by
+    check_near(c, q, [0, 1], run_decode(c, q, i32([0, 1])), dtype)
