@@ -639,11 +639,13 @@ typedef struct snap_paged_q8 {
  *   first_rows_dev [n_seqs]: may be less than the sequence's length: rows from there on are given up.  May not be seq_len_dev itself.
  *   rope, freqs_dev, positions_dev [n_tokens], k_dev, v_dev, k_out_dev, q_dev, q_out_dev: as in snap_paged_append (positions_dev
  *             NULL: the row; k_out is rounded from the rotated key, not from what the page holds)
- * The scale of a block is 2^e, e the smallest integer from -126 to 120 with f * max |x| <= 448 * 2^e over the inputs x of the
- * rows written to it, f = max(1, sqrt(2) magnitude) for keys that are rotated and 1 otherwise (a pair grows by sqrt(2) magnitude
- * at most); of a block that holds rows of the sequence already, below first_rows, it is no less than before, and where it
- * grows those rows move to it.  A number is rotated in single precision, divided by the scale (whatever
- * positive number a block that holds rows has) and rounded once, to nearest even; beyond 448 (only past 2^120) it is 448.  NaN stays NaN and does not count for the scale; a block with an infinity has the scale 2^120.
+ * The scale of a block is 2^e, e the smallest integer from -126 to 120 with f * max |x| <= 448 * 2^e over the
+ * inputs x of the rows written to it, f = max(1, sqrt(2) magnitude) for keys that are rotated and 1 otherwise
+ * (a pair grows by sqrt(2) magnitude at most); of a block that holds rows of the sequence already, below
+ * first_rows, it is no less than before, and where it grows those rows move to it.  A number is rotated in
+ * single precision, divided by the scale (whatever positive number a block that holds rows has) and rounded
+ * once, to nearest even; beyond 448 (only past 2^120) it is 448.  NaN stays NaN and does not count for the
+ * scale; a block with an infinity has the scale 2^120.
  * Rows past the page table or on a page number out of range are skipped (SNAP_DEV_BAD_PAGE), their outputs too; so is an
  * entry with a negative first row, as a whole.  A page that is written may be listed once (not checked).  No workspace.
  */
@@ -663,11 +665,13 @@ int snap_paged_q8_append(const snap_config_t* cfg, const snap_paged_q8_t* paged,
  * of KV head h / (Hq/Hkv): every token sees the rows up to its own.  Nothing is appended.
  *   q_dev [n_active][q_len][Hq][d_qk], out_dev [n_active][q_len][Hq][d_v], dense; 1 <= q_len <= 1024.  A token that sees no row gets zeros;
  *             slots, padding, page numbers out of range and lengths as in snap_paged_decode_attn
- * Numbers enter the products as they are stored (of a query what lies 2^29 and more below its largest number loses bits, at 2^39 it is cut
- * off); logits, weights and sums are in single precision, whatever the scales.  Each weight enters as a number of 21 bits or, far below the
- * largest product of weight and scale of the same query head among 32 rows on scales within 2^6 of one another, as a multiple of 2^-24 of
- * that (single-precision layers 2^-36).  The largest value times the rows of a sequence has to lie below 2^121 (sums are of single precision).  A NaN among the rows that a token attends makes the
- * outputs it enters NaN, and those of no other token.  (An infinity that was appended is 448 * 2^120, past single precision as a value.)
+ * Numbers enter the products as they are stored (of a query what lies 2^29 and more below its largest number
+ * loses bits, at 2^39 it is cut off); logits, weights and sums are in single precision, whatever the scales.
+ * Each weight enters as a number of 21 bits or, far below the largest product of weight and scale of the same
+ * query head among 32 rows on scales within 2^6 of one another, as a multiple of 2^-24 of that
+ * (single-precision layers 2^-36).  The largest value times the rows of a sequence has to lie below 2^121 (sums
+ * are of single precision).  A NaN among the rows that a token attends makes the outputs it enters NaN, and
+ * those of no other token.  (An infinity that was appended is 448 * 2^120, past single precision as a value.)
  * Rows that are left out, and what lies behind a sequence's last row, may hold anything, their scales too.
  * Work is split and joined as in snap_paged_decode_attn: equal inputs give equal bits.
  * Scratch: snap_paged_q8_decode_workspace_bytes(cfg, paged, n_active, q_len); calls that can overlap on the GPU need scratch
@@ -683,9 +687,10 @@ int snap_paged_q8_decode_attn(const snap_config_t* cfg, const snap_paged_q8_t* p
                               void* cuda_stream);
 
 /*
- * The reverse of the append: token cu_tokens[i] + j of k_dev and v_dev receives row first_rows[i] + j of sequence slot_ids[i],
- * rounded once (bf16: exact on scales that are powers of two, unless they leave its range).  Entries, tokens and padding as in snap_paged_q8_append, but a
- * slot may be listed any number of times and no length is looked at.
+ * The reverse of the append: token cu_tokens[i] + j of k_dev and v_dev receives row first_rows[i] + j of
+ * sequence slot_ids[i], rounded once (bf16: exact on scales that are powers of two, unless they leave its
+ * range).  Entries, tokens and padding as in snap_paged_q8_append, but a slot may be listed any number of times
+ * and no length is looked at.
  *   k_dev, v_dev  (t, h, c) at [t * token_stride + h * head_stride + c], strides multiples of 16 bytes, no head of an
  *             output may overlap another
  * Tokens of rows past the page table, or on a page number out of range (SNAP_DEV_BAD_PAGE), are left as they are.  No workspace.

@@ -6,8 +6,8 @@
 
 namespace snap {
 
-// Two codes (low byte first) as two half-precision numbers, exactly.  64 lanes per clock and SM: registers of four codes come at 21.9 a clock
-// (16.4 where a byte permutation goes before), by masks and shifts at 10.9 to 13.2.
+// Two codes (low byte first) as two half-precision numbers, exactly.  65 lanes per clock and SM: registers of four codes come at 22.0 a clock
+// (16.5 where a byte permutation goes before), by masks and shifts at 11.0 to 13.2.
 __device__ __forceinline__ uint32_t halves_of_codes(uint32_t two) {
   uint32_t r;
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((unsigned short)two));

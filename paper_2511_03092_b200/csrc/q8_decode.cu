@@ -2,13 +2,13 @@
 //
 //     out[i][u][h] = sum_r p_r s'_r V_r / sum_r p_r,   p_r = exp(scale s_r q.K_r - max),   r < len - q_len + 1 + u
 //
-// with K_r, V_r the codes of row r and s_r, s'_r the scales of its block.  Every row is read once and serves all columns (the
-// group's query heads, of each token) at once, so HBM bounds the call.  How the work is divided and joined: paged_line.cuh.
+// with K_r, V_r the codes of row r and s_r, s'_r the scales of its block.  A row that is read serves all columns of a unit at once: the
+// group's query heads, of each token, up to 16 (heads wider than 128 dims: 8); of more columns every 16 read the rows again and convert them
+// again.  How the work is divided and joined: paged_line.cuh.
 //
 // A warp's tile is 32 rows, S^T = K tile . Q^T and O^T += V tile^T . P^T with m16n8k16 on half-precision numbers, the columns on
-// the N side: a code is one exactly, and converting two takes one instruction.  (Products of 8-bit numbers, m16n8k32, are no way around it: the
-// conversions are then in what the instruction expands to, and four columns, split in two numbers each, cost what eight do here: four tokens
-// a step 112 us instead of 60.)  The order of the inner dims of a product is free, so codes are used as ldmatrix delivers them: four
+// the N side: a code is one exactly, and converting two takes one instruction.  (Products of 8-bit numbers, m16n8k32, with queries and weights
+// split in two such numbers, take longer: four tokens a step 112 us where one half-precision number took 60.)  The order of the inner dims of a product is free, so codes are used as ldmatrix delivers them: four
 // neighbouring dims of a key row are positions 2t, 2t + 1, 2t + 8, 2t + 9 of a step of 16, and the queries are read in that order;
 // four rows of a value dim, transposed by bytes, are those positions as well, the rows being addressed in the order that
 // movmatrix leaves of the weights.
@@ -17,21 +17,24 @@
 // largest number (cut off 2^-39 below it); single-precision ones enter as two such numbers.  The scale of a key row multiplies its logits, that
 // of a value row its weight.  The products of weight and scale are brought to the range of half precision by a power of two per column, which is
 // taken off again when a tile's outputs are added to the sums: these are of single precision, in the numbers' own size, so that no tile
-// depends on what another one held.  The power and the reference of the exponentials move when a tile's largest product leaves [1, 2^15].  A tile
-// whose value scales lie more than 2^6 apart (a block keeps the scale of a row that was given up) goes through several times, the rows of
-// the largest scales first.  Products are two half-precision numbers, 21 bits; what lies far below the largest one rounds to multiples of 2^-24 of
-// it (of 2^-36 where the second numbers are summed apart, times 2^11: single precision, and two heads side by side).  One number of 11 bits, an eighth
-// of a bf16 output's own rounding, puts one output in 30 on the other side of a border between two bf16 numbers; two cost up to 4 columns
-// nothing where spare columns take the second, else 3 to 9 %, 14 % with sixteen columns (four tokens a step 63 -> 72 us).  (Sums that are held on the columns' powers instead, and lose the rows of smaller scales:
-// 16 long sequences 181 us instead of 188, four tokens a step 58.6 instead of 61.4, calls of all kinds 0.8 % less.  A loop around a tile's
-// rounds instead of a second way through the loop over tiles: 4 to 5 % more, 72 us for the four tokens.)
+// depends on what another one held.  The power moves when a tile's largest product leaves [1, 2^15], the reference of the exponentials when
+// one passes 2^15 or weights pass 2^6.  A tile whose value scales lie more than 2^6 apart (a block keeps the scale of a row that was given up)
+// goes through several times, the rows of the largest scales first.  (Sums held on the columns' powers, which lose the rows of smaller scales:
+// calls of all kinds 0.8 % less, 16 long sequences 181 us instead of 188, four tokens a step 58.6 instead of 61.4.  A loop around a tile's rounds
+// instead of a second way through the loop over tiles: 4 % more.)
+//
+// A weight is two half-precision numbers, 21 bits; what lies far below the tile's largest rounds to multiples of 2^-24 of it (of 2^-36 where the
+// second numbers are summed apart, times 2^11: single precision, and two heads side by side).  One number of 11 bits, an eighth of a bf16
+// output's own rounding, puts one output in 30 on the other side of a border between two bf16 numbers.  The second costs 3 % where a side's spare
+// columns take it (185 -> 190 us), else 2 to 9 %, 14 % with sixteen columns (63 -> 72 us).
 //
 // Where a row's heads lie side by side (pages stored rows first), two warps of a CTA take one head and two the next, over the same rows: HBM
-// then delivers twice as much in a row (128-byte heads, 16 long sequences: 208 us without, 172 with; heads first 168).
+// then delivers twice as much in a row (128-byte heads, 16 long sequences, with sums on the columns' powers: 208 us without, 172 with; heads first 168).
 //
-// What bounds it: 16 sequences of 8192 to 65536 rows, 32 heads on 8 of 128 dims, HBM; four tokens a step (16 columns), some 780 instructions per
-// tile and warp, which wait for one another's results, two warps to a scheduler: 8 sequences of 9000 to 16384 rows 58 to 60 us; small calls, the chain of look-up, first tiles, exchange and join, in two
-// launches: one sequence of 5124 rows 11.7 us, 45 of up to 333 14.8.
+// What bounds it: 16 sequences of 8192 to 65536 rows, 32 heads on 8 of 128 dims, HBM (1.04 GB 179 us, 89 % of the copy rate); four tokens a step (16
+// columns), some 950 instructions per tile and warp, which wait for one another's results, two warps to a scheduler: 8 sequences of 9000 to 16384 rows
+// 72 us; small calls, the chain of look-up, first tiles, exchange and join, in two launches: one sequence of 5124 rows 12.1 us, 45 of up to 333 16.
+// (The two sides at the shares, the CTAs per SM and the columns of a unit below were measured with weights of one number.)
 #include <type_traits>
 
 #include "e4m3.cuh"
@@ -837,8 +840,8 @@ cudaError_t launch_q8_decode(int dtype, const Shape& s, const Q8Map& m, const Q8
   e = dtype == SNAP_F32 ? launch_type<float>(a, d, tk, tv, st) : launch_type<BF>(a, d, tk, tv, st);
   if (e != cudaSuccess) return e;
   // Joined by heads unless there is a unit for every CTA: then few are cut.  (By heads / by borders: 192 units on 296 CTAs, 24 sequences of 2000
-  // to 9000 rows 58.3 / 59.9 us; 48, six of 300 to 1000 24.2 / 26.2; 128, 16 of 3000 to 9000 48.6 / 52.6; 384, 48 of 300 to 700 29.1 / 28.5; 540
-  // on 444, 45 of up to 333 16.3 / 14.8.)
+  // to 9000 rows 63.5 / 65.2 us; 48, six of 300 to 1000 26.8 / 28.7; 128, 16 of 3000 to 9000 51.8 / 55.7; 384, 48 of 300 to 700 31.3 / 30.8; 540
+  // on 444, 45 of up to 333 18.4 / 18.4.)
   const int heads = n_active * a.rows_seq, by_heads = ((long long)n_active * a.U <= p.ctas && heads <= 4096) || p.ctas < 2;
   const dim3 grid((unsigned)(by_heads ? heads : p.ctas - 1));
   e = dtype == SNAP_F32 ? launch_pdl(q8_join_kernel<float>, grid, dim3(JNT), 0, st, a, by_heads)

@@ -105,9 +105,9 @@ __device__ __forceinline__ float2 cos_sin(int pos, double f) {
 // codes (up to HOLD pairs of vectors a lane stay in registers for that).  Then keys and queries: a thread keeps the cosines and sines of its
 // pairs of one row and walks over the heads, the keys coming in again, mostly from L2.
 //
-// A step of few tokens is bound by its chain of look-ups (entry, table, scale, rows) and the host's call: 32 sequences 6.5 us.  A large one is
-// instructions as much as HBM: conversions, rotations and stores of two or four bytes a lane; 26003 tokens of 32 + 8 heads of 128 dims 140 us
-// for 638 MB, 4.6 TB/s (70 % of the measured copy rate).
+// A step of few tokens is bound by its chain of look-ups (entry, table, scale, rows) and the host's call: 32 sequences 6.6 us.  A large one is
+// instructions as much as HBM: conversions, rotations and stores of two or four bytes a lane; 26003 tokens of 32 + 8 heads of 128 dims 141 us
+// for 638 MB, 4.5 TB/s (69 % of the measured copy rate).
 template <typename T, int V, bool INTER>
 __global__ void __launch_bounds__(ANT, 4) q8_append_kernel(const __grid_constant__ AppendLaunch L) {
   const Q8AppendArgs& a = L.a;
@@ -416,8 +416,8 @@ __global__ void __launch_bounds__(ANT, 4) q8_append_kernel(const __grid_constant
 
 // ---- gather: a CTA per CHUNK tokens ----
 // What a token's numbers need of it comes first (page and row, as offsets); then a thread takes a vector of a head, of every token:
-// nothing is divided on the way.  32768 rows of 8 KV heads of 128 dims 46 us for 201 MB, 4.4 TB/s (67 % of the copy rate: two thirds of the
-// bytes are writes); with divisions on the way 66.  A call of few rows is three dependent reads
+// nothing is divided on the way.  32768 rows of 8 KV heads of 128 dims 46 us for 201 MB, 4.4 TB/s (67 % of the copy rate: a lane's two stores lie
+// 16 bytes apart, so that each covers half of its sectors); with divisions on the way 66.  A call of few rows is three dependent reads
 // and a launch: 23 sequences of single precision 4.2 us.
 constexpr int CHUNK = 16;
 struct GatherLaunch {
