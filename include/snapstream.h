@@ -665,8 +665,8 @@ int snap_paged_q8_append(const snap_config_t* cfg, const snap_paged_q8_t* paged,
  * of KV head h / (Hq/Hkv): every token sees the rows up to its own.  Nothing is appended.
  *   q_dev [n_active][q_len][Hq][d_qk], out_dev [n_active][q_len][Hq][d_v], dense; 1 <= q_len <= 1024.  A token that sees no row gets zeros;
  *             slots, padding, page numbers out of range and lengths as in snap_paged_decode_attn
- * Numbers enter the products as they are stored (of a query what lies 2^29 and more below its largest number
- * loses bits, at 2^39 it is cut off); logits, weights and sums are in single precision, whatever the scales.
+ * Numbers enter the products as they are stored (queries of single precision to 22 bits; of any query what
+ * lies 2^29 and more below its largest number loses bits, at 2^39 it is cut off); logits, weights and sums are in single precision, whatever the scales.
  * Each weight enters as a number of 21 bits or, far below the largest product of weight and scale of the same
  * query head among 32 rows on scales within 2^6 of one another, as a multiple of 2^-24 of that
  * (single-precision layers 2^-36).  The largest value times the rows of a sequence has to lie below 2^121 (sums

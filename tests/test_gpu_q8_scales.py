@@ -110,3 +110,32 @@ def test_gather_rounds_once():
     np.testing.assert_array_equal(f64(k), np.broadcast_to(want, k.shape))
     np.testing.assert_array_equal(f64(v), np.broadcast_to(-want, k.shape))
     assert c.bits() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("positions", [None, 9000])
+def test_keys_rotated_in_place_onto_an_uneven_scale(positions, interleaved, dtype):
+    """More rows than are rotated at a time, the last of them in the next block; the rotated keys are written over the keys."""
+    heads, d, n, first = 6, 64, 60, 7
+    cfg = config(2 * heads, heads, d, dtype=dtype, max_seqs=2)
+    c = Pages8(cfg, 48, 48, [3, first], seed=1, capacity=96)
+    c.table[1, 1] = c.free[0]
+    p = c.table[1, 0].item()
+    scales = torch.tensor(SCALES[:heads], dtype=torch.float32)
+    for s in c.scales:
+        s[p] = scales.cuda()[:, None]
+    g = torch.Generator(device="cuda").manual_seed(2)
+    k, v, q = (torch.randn(n, h, d, device="cuda", generator=g).clamp(-3, 3) for h in (heads, heads, 2 * heads))
+    size = torch.exp2(torch.floor(torch.log2(scales))).cuda()[None, :, None] * 64
+    k, v, q = (k * size).to(DT[dtype]), (v * size).to(DT[dtype]), q.to(DT[dtype])
+    x, before = k.clone(), c.host()
+    freqs = 1 / 10000.0 ** (np.arange(32) / 32)
+    rope = B.make_rope(rot_dim=64, interleaved=interleaved)
+    pos = None if positions is None else [positions + 2 * i for i in range(n)]
+    B.snap_paged_q8_append(cfg, c.paged, i32([1]), i32([0, n]), i32([first]), k, v, *c.cache, c.seq_len, rope=rope, freqs=torch.from_numpy(freqs).cuda(),
+                           positions=None if pos is None else i32(pos), q=q, q_out=q, k_out=k, status=c.status)
+    check_append(c, before, [1], [first], [0, n], x, v, rope, freqs, pos, k, dtype=dtype)
+    for s in c.scales:
+        assert torch.equal(s[p, :, 0].cpu(), scales)
+    assert c.bits() == 0 and c.seq_len.tolist() == [3, first + n]
