@@ -666,12 +666,13 @@ int snap_paged_q8_append(const snap_config_t* cfg, const snap_paged_q8_t* paged,
  *   q_dev [n_active][q_len][Hq][d_qk], out_dev [n_active][q_len][Hq][d_v], dense; 1 <= q_len <= 1024.  A token that sees no row gets zeros;
  *             slots, padding, page numbers out of range and lengths as in snap_paged_decode_attn
  * Numbers enter the products as they are stored (queries of single precision to 22 bits; of any query what
- * lies 2^29 and more below its largest number loses bits, at 2^39 it is cut off); logits, weights and sums are in single precision, whatever the scales.
- * Each weight enters as a number of 21 bits or, far below the largest product of weight and scale of the same
- * query head among 32 rows on scales within 2^6 of one another, as a multiple of 2^-24 of that
- * (single-precision layers 2^-36).  The largest value times the rows of a sequence has to lie below 2^121 (sums
- * are of single precision).  A NaN among the rows that a token attends makes the outputs it enters NaN, and
- * those of no other token.  (An infinity that was appended is 448 * 2^120, past single precision as a value.)
+ * lies 2^29 and more below its largest number loses bits, at 2^39 it is cut off); logits, weights and sums are
+ * in single precision, whatever the scales. Each weight enters as a number of 21 bits or, far below the
+ * largest product of weight and scale of the same query head among 32 rows on scales within 2^6 of one
+ * another, as a multiple of 2^-24 of that (single-precision layers 2^-36); one below 2^-126 of the largest
+ * weight is zero.  The largest value times the rows of a sequence has to lie below 2^121 (sums are of single
+ * precision).  A NaN among the rows that a token attends makes the outputs it enters NaN, and those of no
+ * other token.  (An infinity that was appended is 448 * 2^120, past single precision as a value.)
  * Rows that are left out, and what lies behind a sequence's last row, may hold anything, their scales too.
  * Work is split and joined as in snap_paged_decode_attn: equal inputs give equal bits.
  * Scratch: snap_paged_q8_decode_workspace_bytes(cfg, paged, n_active, q_len); calls that can overlap on the GPU need scratch
